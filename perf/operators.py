@@ -82,11 +82,11 @@ def draw(rng):
     even = rng.random() < 0.5
     size = lambda lo, hi, step: max(step, _log_uniform(rng, lo, hi) // step * step) if even else _log_uniform(rng, lo, hi)  # noqa: E731
     if kind in ("layernorm", "dropout"):
+        x = rng.choice(["float32", "bfloat16"])
         while True:
             M, N = _log_uniform(rng, 1, 16384), size(64, 8192, 64)
-            if M * N <= 16384 * 4096:
+            if M * N <= (16384 * 2048 if x == "float32" else 16384 * 4096):
                 break
-        x = rng.choice(["float32", "bfloat16"])
         if kind == "layernorm":
             return _ln(M=M, N=N, x=x, out=rng.choice(["codes", x]), train=train)
         act = rng.choice(["none", "none", "relu", "gelu", "silu"])
