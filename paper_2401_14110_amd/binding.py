@@ -14,6 +14,8 @@ _LIBPATH = os.path.join(_HERE, "liblba_hip.so")
 ROUND_FLOOR, ROUND_RNE = 0, 1
 STE_IDENTITY, STE_IMMEDIATE_OF, STE_RECURSIVE_OF, STE_COEF_PLANE = 0, 1, 2, 3
 ORDER_SEQ, ORDER_CHUNK16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+F32, BF16, CODE8 = 0, 1, 2
 OK, ERR_NULL, ERR_SHAPE, ERR_FORMAT, ERR_UNSUPPORTED, ERR_ALIGN, ERR_LAUNCH = range(7)
 
 
@@ -28,6 +30,10 @@ class lba_infmt(ctypes.Structure):
 
 def infmt(f):
     return f if isinstance(f, lba_infmt) else lba_infmt(*[int(v) for v in f])
+
+
+class lba_drop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("stream", ctypes.c_uint64), ("step", ctypes.c_void_p)]
 
 
 class lba_conv2d_desc(ctypes.Structure):
@@ -118,6 +124,19 @@ def lib(path=None):
         L.lba_plan_query.restype = ctypes.c_int
         L.lba_plan_query.argtypes = [i64, i64, i64, lba_qfmt, lba_qfmt, i32, i32,
                                      ctypes.POINTER(lba_plan_info)]
+        f32, size = ctypes.c_float, ctypes.c_size_t
+        L.lba_layernorm.restype = ctypes.c_int
+        L.lba_layernorm.argtypes = [vp, i32, vp, vp, f32, vp, i32, lba_infmt, vp, vp, i64, i64, vp]
+        L.lba_layernorm_bwd.restype = ctypes.c_int
+        L.lba_layernorm_bwd.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i64, i64, vp, size, vp]
+        L.lba_layernorm_bwd_workspace_bytes.restype = size
+        L.lba_layernorm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.lba_dropout.restype = ctypes.c_int
+        L.lba_dropout.argtypes = [vp, i32, f32, vp, i32, lba_drop, vp, i32, vp, i32, lba_infmt, i64, i64, vp]
+        L.lba_dropout_bwd.restype = ctypes.c_int
+        L.lba_dropout_bwd.argtypes = [vp, i32, vp, i32, f32, vp, i32, lba_drop, vp, vp, i64, i64, vp, size, vp]
+        L.lba_dropout_bwd_workspace_bytes.restype = size
+        L.lba_dropout_bwd_workspace_bytes.argtypes = [i64, i64]
         _lib = L
     return _lib
 
@@ -295,6 +314,32 @@ def lba_plan_kernel_name_in(M, N, K, fmt_a, fmt_b, qprod, qacc, order=ORDER_SEQ,
     _check(lib().lba_plan_kernel_name_in(M, N, K, infmt(fmt_a), infmt(fmt_b), qfmt(qprod), qfmt(qacc), order, with_masks, buf,
                                          len(buf)))
     return buf.value.decode()
+
+
+def lba_layernorm(X, x_type, gamma, beta, eps, Y, y_type, y_fmt, mean, rstd, M, N, hip_stream=None):
+    return lib().lba_layernorm(X, x_type, gamma, beta, float(eps), Y, y_type, infmt(y_fmt), mean, rstd, M, N, hip_stream)
+
+
+def lba_layernorm_bwd(G, g_type, X, x_type, gamma, mean, rstd, dX, dgamma, dbeta, M, N, workspace, workspace_bytes, hip_stream=None):
+    return lib().lba_layernorm_bwd(G, g_type, X, x_type, gamma, mean, rstd, dX, dgamma, dbeta, M, N, workspace, workspace_bytes,
+                                   hip_stream)
+
+
+def lba_layernorm_bwd_workspace_bytes(M, N):
+    return int(lib().lba_layernorm_bwd_workspace_bytes(M, N))
+
+
+def lba_dropout(X, x_type, scale, bias, act, drop, residual, r_type, Y, y_type, y_fmt, M, N, hip_stream=None):
+    return lib().lba_dropout(X, x_type, float(scale), bias, act, drop, residual, r_type, Y, y_type, infmt(y_fmt), M, N, hip_stream)
+
+
+def lba_dropout_bwd(G, g_type, X, x_type, scale, bias, act, drop, dX, dbias, M, N, workspace, workspace_bytes, hip_stream=None):
+    return lib().lba_dropout_bwd(G, g_type, X, x_type, float(scale), bias, act, drop, dX, dbias, M, N, workspace, workspace_bytes,
+                                 hip_stream)
+
+
+def lba_dropout_bwd_workspace_bytes(M, N):
+    return int(lib().lba_dropout_bwd_workspace_bytes(M, N))
 
 
 # ---- tensor conveniences --------------------------------------------------------------------
@@ -548,3 +593,185 @@ def conv2d(X, W, qprod, qacc, stride=1, pad=0, order=ORDER_SEQ, planes=False, st
                                 of.data_ptr() or None, uf.data_ptr() or None, desc, cout,
                                 qfmt(qprod), qfmt(qacc), order, _stream(stream)))
     return Y, of, uf
+
+
+# ---- the operators of include/lba_layer.h -----------------------------------------------------
+#
+# Codes in and out are uint8 tensors with a format (exp_bits, man_bits, bias), whose bias carries the tensor's power-of-two scale: the
+# E4M3 codes of x * 2^t are those of (4, 3, 7 + t).  Temporaries belong to the stream that the call runs on.
+
+_E4M3 = lba_infmt(4, 3, 7)
+_NO_DROP = lba_drop(0.0, 0, 0, None)
+_TYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.uint8: CODE8}
+_WORD = (1 << 64) - 1
+
+
+class _On:
+    """The stream of one call: its handle, and the tensors made here kept for it where it is not the current stream."""
+
+    __slots__ = ("stream", "handle")
+
+    def __init__(self, stream):
+        self.handle = _stream(stream)
+        if stream is None or hasattr(stream, "cuda_stream"):
+            self.stream = stream
+        else:
+            self.stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+
+    def whole(self, t):
+        """t as the library reads it: contiguous (a copy is made on the call's stream)."""
+        if t.is_contiguous():
+            return t
+        if self.stream is None:
+            return t.contiguous()
+        with torch.cuda.stream(self.stream):
+            return t.contiguous()
+
+    def empty(self, shape, dtype, device):
+        t = torch.empty(shape, dtype=dtype, device=device)
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t
+
+
+def _rows(t, what, dtypes=(torch.float32, torch.bfloat16)):
+    """(M, N) of a device tensor whose rows run along its last axis."""
+    if t.dtype not in dtypes or not t.is_cuda:
+        raise TypeError("%s must be a device tensor of %s" % (what, " or ".join(str(d) for d in dtypes)))
+    if t.dim() < 1:
+        raise ValueError("%s must have at least one axis" % what)
+    n = t.shape[-1]
+    return (t.numel() // n if n else 0), n
+
+
+def _like(t, shape, what, dtypes=(torch.float32, torch.bfloat16)):
+    if t.dtype not in dtypes or not t.is_cuda:
+        raise TypeError("%s must be a device tensor of %s" % (what, " or ".join(str(d) for d in dtypes)))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+    return t
+
+
+def _vector(on, t, n, what):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or not t.is_cuda or tuple(t.shape) != (n,):
+        raise ValueError("%s must be a float32 device tensor [%d]" % (what, n))
+    return on.whole(t)
+
+
+def _out_type(dtype, fmt):
+    """(type code, lba_infmt) of an output."""
+    if dtype not in _TYPE:
+        raise TypeError("an output is torch.float32, torch.bfloat16, or torch.uint8 codes")
+    if dtype is torch.uint8:
+        if fmt is None:
+            raise ValueError("codes need out_fmt = (exp_bits, man_bits, bias)")
+        return CODE8, infmt(fmt)
+    if fmt is not None:
+        raise ValueError("out_fmt is for torch.uint8 codes")
+    return _TYPE[dtype], _E4M3
+
+
+def _output(on, out, shape, dtype, device):
+    if out is None:
+        return on.empty(shape, dtype, device)
+    if out.dtype != dtype or out.shape != shape or not out.is_cuda or not out.is_contiguous():
+        raise ValueError("out must be a contiguous device tensor %s of %s" % (tuple(shape), dtype))
+    return out
+
+
+def _drop(drop):
+    """None, (p, seed, stream) or (p, seed, stream, step) with step a one-element int64 device tensor (read when the kernel runs)."""
+    if drop is None:
+        return _NO_DROP
+    if isinstance(drop, lba_drop):
+        return drop
+    p, seed, stream = drop[:3]
+    step = drop[3] if len(drop) > 3 else None
+    if step is not None and (step.dtype != torch.int64 or not step.is_cuda or step.numel() != 1):
+        raise ValueError("step must be an int64 device tensor of one element")
+    return lba_drop(float(p), int(seed) & _WORD, int(stream) & _WORD, step.data_ptr() if step is not None else None)
+
+
+def _at(t):
+    return (t.data_ptr() or None) if t is not None else None
+
+
+def layernorm(x, gamma=None, beta=None, eps=1e-5, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None):
+    """Layer norm over the last axis of x (float32 or bfloat16): y of out_dtype (x's by default; torch.uint8 codes need out_fmt), and
+    with want_stats (y, mean, rstd), float32 tensors of x's leading shape, which layernorm_bwd reads."""
+    M, N = _rows(x, "x")
+    dtype = out_dtype or x.dtype
+    y_type, fmt = _out_type(dtype, out_fmt)
+    on = _On(stream)
+    x, gamma, beta = on.whole(x), _vector(on, gamma, N, "gamma"), _vector(on, beta, N, "beta")
+    y = _output(on, out, x.shape, dtype, x.device)
+    mean = on.empty(x.shape[:-1], torch.float32, x.device) if want_stats else None
+    rstd = on.empty(x.shape[:-1], torch.float32, x.device) if want_stats else None
+    _check(lib().lba_layernorm(_at(x), _TYPE[x.dtype], _at(gamma), _at(beta), eps, _at(y), y_type, fmt, _at(mean), _at(rstd), M, N,
+                               on.handle))
+    return (y, mean, rstd) if want_stats else y
+
+
+def layernorm_bwd(G, x, gamma, mean, rstd, want_dx=True, want_params=True, stream=None):
+    """Gradients of layernorm: (dx of x's type or None, dgamma, dbeta: float32 or None)."""
+    M, N = _rows(x, "x")
+    _like(G, x.shape, "G")
+    _like(mean, x.shape[:-1], "mean", (torch.float32,))
+    _like(rstd, x.shape[:-1], "rstd", (torch.float32,))
+    on = _On(stream)
+    G, x, mean, rstd, gamma = on.whole(G), on.whole(x), on.whole(mean), on.whole(rstd), _vector(on, gamma, N, "gamma")
+    dx = on.empty(x.shape, x.dtype, x.device) if want_dx else None
+    params = on.empty((2, N), torch.float32, x.device) if want_params else None
+    size = lib().lba_layernorm_bwd_workspace_bytes(M, N) if want_params else 0
+    ws = on.empty((size,), torch.uint8, x.device) if size else None
+    dgamma, dbeta = params if want_params else (None, None)
+    _check(lib().lba_layernorm_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[x.dtype], _at(gamma), _at(mean), _at(rstd), _at(dx),
+                                   _at(dgamma), _at(dbeta), M, N, _at(ws), size, on.handle))
+    return dx, dgamma, dbeta
+
+
+def dropout(x, drop, bias=None, act=ACT_NONE, residual=None, scale=1.0, out_dtype=None, out_fmt=None, out=None, stream=None):
+    """residual + keep * act(scale * x + bias) / (1 - p) with drop = (p, seed, stream[, step]) or None; x and residual are float32
+    or bfloat16, bias runs along the last axis, y is of out_dtype (x's by default; torch.uint8 codes need out_fmt).  After a simulated
+    product scale = 2^-T undoes its operands' scales."""
+    M, N = _rows(x, "x")
+    dtype = out_dtype or x.dtype
+    y_type, fmt = _out_type(dtype, out_fmt)
+    d = _drop(drop)
+    on = _On(stream)
+    x, bias = on.whole(x), _vector(on, bias, N, "bias")
+    if residual is not None:
+        residual = on.whole(_like(residual, x.shape, "residual"))
+    y = _output(on, out, x.shape, dtype, x.device)
+    _check(lib().lba_dropout(_at(x), _TYPE[x.dtype], scale, _at(bias), act, d, _at(residual),
+                             _TYPE[residual.dtype] if residual is not None else F32, _at(y), y_type, fmt, M, N, on.handle))
+    return y
+
+
+def dropout_bwd(G, drop, x=None, bias=None, act=ACT_NONE, scale=1.0, want_dx=True, want_dbias=False, out_dtype=None, stream=None):
+    """Gradients of dropout: (dx or None, dbias or None).  x and bias are needed where act is not ACT_NONE; dx is of x's type, of
+    out_dtype without x, of G's without both.  The residual's gradient is G."""
+    M, N = _rows(G, "G")
+    dtype = x.dtype if x is not None else out_dtype or G.dtype
+    if out_dtype is not None and out_dtype != dtype:
+        raise ValueError("dx has x's type")
+    if x is not None:
+        _like(x, G.shape, "x")
+    elif act != ACT_NONE:
+        raise ValueError("the gradient of an activation needs x")
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("dx is torch.float32 or torch.bfloat16")
+    d = _drop(drop)
+    on = _On(stream)
+    G, bias = on.whole(G), _vector(on, bias, N, "bias")
+    if x is not None:
+        x = on.whole(x)
+    dx = on.empty(G.shape, dtype, G.device) if want_dx else None
+    dbias = on.empty((N,), torch.float32, G.device) if want_dbias else None
+    size = lib().lba_dropout_bwd_workspace_bytes(M, N) if want_dbias else 0
+    ws = on.empty((size,), torch.uint8, G.device) if size else None
+    _check(lib().lba_dropout_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[dtype], scale, _at(bias), act, d, _at(dx), _at(dbias), M, N,
+                                 _at(ws), size, on.handle))
+    return dx, dbias

@@ -1,0 +1,264 @@
+// lba_dropout.hip -- dropout with bias, activation and residual, and its gradients (include/lba_layer.h).
+//
+// The mask is a function of (seed, stream, element index): 16 bits of a splitmix64 word for each element, four elements a word, so the
+// backward pass makes it again and nothing of it is stored.  A word is two 64-bit products; on four elements that is less than
+// the memory time of a bfloat16 element.
+// A lane owns one vector of 16 bytes' worth of columns and walks over rows, so a bias is loaded once and the column sums of the
+// backward pass, dbias, stay in registers; a workgroup writes one row of partial sums, and a second launch adds them in a fixed order.
+// Columns beyond the last full strip of 64 vectors have lanes of their own: as many rows side by side in a wave as they fit.
+#include "lba_layer_device.h"
+#include "lba_internal.h"
+
+namespace lba {
+
+struct DropoutParams {
+    const void* X;
+    const void* G;
+    const void* R;
+    const float* bias;
+    void* Y;                 // forward: y; backward: dx
+    float* part;             // backward: [chunks][N] partial sums, or null
+    int64_t M;
+    int32_t N;
+    int32_t r_type;
+    int32_t act;
+    float scale;
+    int32_t strips;          // full strips of 64 vectors; workgroups below main_blocks belong to them
+    int32_t main_blocks, main_chunks, tail_chunks;
+    int64_t main_rows, tail_rows;     // rows of a chunk
+    int32_t tail_log;        // log2 of the lanes that share a row of the tail
+    DropParams drop;
+    CodeFmt fmt;
+};
+
+// where a lane stands: its columns, its first row, the step to its next one and the end of its chunk
+struct LanePlace { int col, cols; int64_t row, end; int step, chunk, lanes_log; };
+template <int V> __device__ __forceinline__ LanePlace lane_place(const DropoutParams& p) {
+    LanePlace q;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const bool tail = (int)blockIdx.x >= p.main_blocks;
+    const int b = tail ? (int)blockIdx.x - p.main_blocks : (int)blockIdx.x;
+    q.lanes_log = tail ? p.tail_log : 6;
+    const int strip = tail ? p.strips : b % p.strips;
+    q.chunk = tail ? b : b / p.strips;
+    q.col = strip * 64 * V + (lane & ((1 << q.lanes_log) - 1)) * V;
+    q.cols = p.N - q.col;
+    const int64_t rows = tail ? p.tail_rows : p.main_rows;
+    q.row = q.chunk * rows + (wave << (6 - q.lanes_log)) + (lane >> q.lanes_log);
+    q.end = q.chunk * rows + rows < p.M ? q.chunk * rows + rows : p.M;
+    q.step = 4 << (6 - q.lanes_log);
+    return q;
+}
+
+template <int V> __device__ __forceinline__ void load_typed(const void* at, int type, int64_t i, int n, float (&v)[V]) {
+    if (type == LBA_F32) load_some<V>((const float*)at + i, n, v);
+    else load_some<V>((const bf16_t*)at + i, n, v);
+}
+
+template <typename TX, typename TY>
+__global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
+    constexpr int V = 16 / sizeof(TX);
+    const LanePlace q = lane_place<V>(p);
+    if (q.cols <= 0) return;
+    const uint64_t base = drop_base(p.drop);
+    float bias[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) bias[j] = 0.0f;
+    if (p.bias) load_some<V>(p.bias + q.col, q.cols, bias);
+    for (int64_t row = q.row; row < q.end; row += q.step) {
+        const int64_t i = row * p.N + q.col;
+        float x[V], f[V], r[V];
+        load_some<V>((const TX*)p.X + i, q.cols, x);
+        if (p.R) load_typed<V>(p.R, p.r_type, i, q.cols, r);
+        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float z = act_value(fmaf(x[j], p.scale, bias[j]), p.act);
+            if (p.drop.threshold) z = f[j] != 0.0f ? z * f[j] : 0.0f;
+            x[j] = p.R ? z + r[j] : z;
+        }
+        store_some<V>((TY*)p.Y + i, q.cols, x, p.fmt);
+    }
+}
+
+template <typename TG, typename TX>
+__global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
+    constexpr int V = 16 / sizeof(TX);
+    const LanePlace q = lane_place<V>(p);
+    const uint64_t base = drop_base(p.drop);
+    float bias[V], sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) bias[j] = sum[j] = 0.0f;
+    const bool read_x = p.act != LBA_ACT_NONE;
+    if (p.bias && read_x) load_some<V>(p.bias + q.col, q.cols, bias);
+    if (q.cols > 0)
+    for (int64_t row = q.row; row < q.end; row += q.step) {
+        const int64_t i = row * p.N + q.col;
+        float x[V], g[V], f[V];
+        load_some<V>((const TG*)p.G + i, q.cols, g);
+        if (read_x) load_some<V>((const TX*)p.X + i, q.cols, x);
+        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float d = g[j];
+            if (read_x) {
+                float value, slope;
+                act_both(fmaf(x[j], p.scale, bias[j]), p.act, value, slope);
+                d *= slope;
+            }
+            if (p.drop.threshold) d = f[j] != 0.0f ? d * f[j] : 0.0f;
+            sum[j] += d;
+            x[j] = d * p.scale;
+        }
+        if (p.Y) store_some<V>((TX*)p.Y + i, q.cols, x, p.fmt);
+    }
+    if (!p.part) return;
+    // the lanes of the workgroup that own the same columns, one after the other
+    __shared__ float lds[256 * V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) lds[j * 256 + threadIdx.x] = sum[j];
+    __syncthreads();
+    const int lanes = 1 << q.lanes_log;
+    if ((int)threadIdx.x >= lanes || q.cols <= 0) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        float s = 0.0f;
+        for (int t = threadIdx.x; t < 256; t += lanes) s += lds[j * 256 + t];
+        sum[j] = s;
+    }
+    store_some<V>(p.part + (int64_t)q.chunk * p.N + q.col, q.cols, sum, p.fmt);
+}
+
+// ---- launchers ------------------------------------------------------------------------------
+
+// How rows and columns are cut.  A chunk is a multiple of the rows a workgroup has in flight; the chip holds about 2048 workgroups of
+// four waves, and the backward pass writes a row of sums for each chunk, so it takes fewer of them.
+static int64_t chunk_rows(int64_t M, int64_t step, int64_t strips, int64_t most) {
+    const int64_t chunks = most / (strips < 1 ? 1 : strips) < 1 ? 1 : most / (strips < 1 ? 1 : strips);
+    const int64_t rows = (M + chunks - 1) / chunks;
+    return (rows + step - 1) / step * step;
+}
+
+constexpr int64_t kFwdBlocks = 8192, kBwdBlocks = 2048;
+
+// both passes' cut for vectors of v elements; the number of chunks that write partial sums is the larger of the two
+static unsigned dropout_cut(DropoutParams* p, int v, int64_t most) {
+    p->strips = p->N / (64 * v);
+    const int tail_cols = p->N - p->strips * 64 * v;
+    int64_t blocks = 0;
+    p->main_blocks = p->main_chunks = p->tail_chunks = 0;
+    if (p->strips > 0) {
+        p->main_rows = chunk_rows(p->M, 4, p->strips, most);
+        p->main_chunks = (int32_t)((p->M + p->main_rows - 1) / p->main_rows);
+        p->main_blocks = p->main_chunks * p->strips;
+        blocks = p->main_blocks;
+    }
+    if (tail_cols > 0) {
+        p->tail_log = 0;
+        while ((v << p->tail_log) < tail_cols) ++p->tail_log;
+        // as many chunks as the strips beside it have, or as fill the chip alone
+        const int64_t share = p->strips > 0 ? p->main_chunks : most;
+        p->tail_rows = chunk_rows(p->M, 4 << (6 - p->tail_log), 1, share);
+        p->tail_chunks = (int32_t)((p->M + p->tail_rows - 1) / p->tail_rows);
+        blocks += p->tail_chunks;
+    }
+    return (unsigned)blocks;
+}
+
+}  // namespace lba
+
+using namespace lba;
+
+extern "C" {
+
+int lba_dropout(const void* X, int32_t x_type, float scale, const float* bias, int32_t act, lba_drop drop,
+                const void* residual, int32_t r_type, void* Y, int32_t y_type, lba_infmt y_fmt,
+                int64_t M, int64_t N, void* hip_stream) {
+    DropoutParams p = {};
+    int rc = check_rows(M, N);
+    if (rc == LBA_OK) rc = check_float_type(x_type);
+    if (rc == LBA_OK && residual) rc = check_float_type(r_type);
+    if (rc == LBA_OK) rc = check_out_type(y_type, y_fmt);
+    if (rc == LBA_OK) rc = check_act(act);
+    if (rc == LBA_OK) rc = check_drop(drop, &p.drop);
+    if (rc != LBA_OK) return rc;
+    if (M == 0 || N == 0) return LBA_OK;
+    if (!X || !Y) return LBA_ERR_NULL;
+    p.X = X; p.R = residual; p.bias = bias; p.Y = Y; p.M = M; p.N = (int32_t)N; p.r_type = r_type; p.act = act; p.scale = scale;
+    if (y_type == LBA_CODE8) p.fmt = make_code_fmt(y_fmt);
+    const dim3 grid(dropout_cut(&p, x_type == LBA_F32 ? 4 : 8, kFwdBlocks));
+    const hipStream_t st = (hipStream_t)hip_stream;
+#define LBA_DROPOUT(TX, TY) hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY>), grid, dim3(256), 0, st, p)
+    if (x_type == LBA_F32) {
+        if (y_type == LBA_F32) LBA_DROPOUT(float, float);
+        else if (y_type == LBA_BF16) LBA_DROPOUT(float, bf16_t);
+        else LBA_DROPOUT(float, uint8_t);
+    } else {
+        if (y_type == LBA_F32) LBA_DROPOUT(bf16_t, float);
+        else if (y_type == LBA_BF16) LBA_DROPOUT(bf16_t, bf16_t);
+        else LBA_DROPOUT(bf16_t, uint8_t);
+    }
+#undef LBA_DROPOUT
+    return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+}
+
+size_t lba_dropout_bwd_workspace_bytes(int64_t M, int64_t N) {
+    if (check_rows(M, N) != LBA_OK || M == 0 || N == 0) return 0;
+    size_t most = 0;
+    for (int v = 4; v <= 8; v += 4) {                    // either type of X
+        DropoutParams p = {};
+        p.M = M; p.N = (int32_t)N;
+        dropout_cut(&p, v, kBwdBlocks);
+        const size_t chunks = (size_t)(p.main_chunks > p.tail_chunks ? p.main_chunks : p.tail_chunks);
+        if (chunks > most) most = chunks;
+    }
+    return align256(most * (size_t)N * sizeof(float));
+}
+
+int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type, float scale, const float* bias,
+                    int32_t act, lba_drop drop, void* dX, float* dbias, int64_t M, int64_t N,
+                    void* workspace, size_t workspace_bytes, void* hip_stream) {
+    DropoutParams p = {};
+    int rc = check_rows(M, N);
+    if (rc == LBA_OK) rc = check_float_type(g_type);
+    if (rc == LBA_OK) rc = check_float_type(x_type);
+    if (rc == LBA_OK) rc = check_act(act);
+    if (rc == LBA_OK) rc = check_drop(drop, &p.drop);
+    if (rc != LBA_OK) return rc;
+    if (N == 0) return LBA_OK;
+    if (!dX && !dbias) return LBA_ERR_NULL;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (M == 0) {
+        if (dbias) launch_zero(dbias, N, st);
+        return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+    }
+    if (!G || (act != LBA_ACT_NONE && !X)) return LBA_ERR_NULL;
+    if (dbias) {
+        if (!workspace) return LBA_ERR_NULL;
+        if ((uintptr_t)workspace % 256 != 0) return LBA_ERR_ALIGN;
+        if (workspace_bytes < lba_dropout_bwd_workspace_bytes(M, N)) return LBA_ERR_SHAPE;
+    }
+    p.X = X; p.G = G; p.bias = bias; p.Y = dX; p.part = dbias ? (float*)workspace : nullptr;
+    p.M = M; p.N = (int32_t)N; p.act = act; p.scale = scale;
+    const dim3 grid(dropout_cut(&p, x_type == LBA_F32 ? 4 : 8, kBwdBlocks));
+#define LBA_DROPOUT(TG, TX) hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX>), grid, dim3(256), 0, st, p)
+    if (g_type == LBA_F32) {
+        if (x_type == LBA_F32) LBA_DROPOUT(float, float); else LBA_DROPOUT(float, bf16_t);
+    } else {
+        if (x_type == LBA_F32) LBA_DROPOUT(bf16_t, float); else LBA_DROPOUT(bf16_t, bf16_t);
+    }
+#undef LBA_DROPOUT
+    if (dbias) {
+        // full strips and the tail are cut into chunks of their own number
+        const int64_t full = (int64_t)p.strips * 64 * (x_type == LBA_F32 ? 4 : 8);
+        if (p.main_chunks == p.tail_chunks || full == 0 || full == N)
+            launch_column_sum(p.part, full == 0 ? p.tail_chunks : p.main_chunks, N, dbias, nullptr, N, st);
+        else {
+            launch_column_sum(p.part, p.main_chunks, N, dbias, nullptr, full, st);
+            launch_column_sum(p.part + full, p.tail_chunks, N, dbias + full, nullptr, N - full, st);
+        }
+    }
+    return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,234 @@
+// lba_layer_device.h -- what the operators of lba_layer.h share on the device: element types in registers, 8-bit codes,
+// activations, the dropout generator and sums over a wave.
+#ifndef LBA_LAYER_DEVICE_H_
+#define LBA_LAYER_DEVICE_H_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lba_layer.h"
+
+namespace lba {
+
+typedef __bf16 bf16_t;
+
+// vectors of the element's own alignment: rows start anywhere, and the memory system takes unaligned vectors
+template <typename T, int V> struct Vec { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
+template <typename T> struct Vec<T, 1> { typedef T type; };
+
+// an output format of 8-bit codes as the encoder uses it
+struct CodeFmt {
+    float scale;             // 2^(bias - canonical bias)
+    float top;               // largest value at the canonical bias
+    float sub;               // 2^(emin - man + 23): adding it rounds to the subnormal grid
+    float norm;              // 2^emin, the smallest normal number
+    int32_t sh;              // 23 - man_bits
+    int32_t off;             // (127 - canonical bias) << man_bits
+    int32_t e4m3;            // 1: exp_bits 4, the hardware conversion rounds as the format does
+};
+
+inline CodeFmt make_code_fmt(const lba_infmt& f) {
+    CodeFmt c;
+    const int bc = (1 << (f.exp_bits - 1)) - 1, emin = 1 - bc;
+    c.scale = __builtin_ldexpf(1.0f, f.bias - bc);
+    c.e4m3 = f.exp_bits == 4 ? 1 : 0;
+    c.top = c.e4m3 ? 448.0f : __builtin_ldexpf(2.0f - __builtin_ldexpf(1.0f, -f.man_bits), (1 << f.exp_bits) - 1 - bc);
+    c.sub = __builtin_ldexpf(1.0f, emin - f.man_bits + 23);
+    c.norm = __builtin_ldexpf(1.0f, emin);
+    c.sh = 23 - f.man_bits;
+    c.off = (127 - bc) << f.man_bits;
+    return c;
+}
+
+__device__ __forceinline__ uint32_t code_one(float v, const CodeFmt& c) {
+    const uint32_t sign = (__float_as_uint(v) >> 24) & 0x80u;
+    const float u = fabsf(v) * c.scale;
+    const uint32_t b = __float_as_uint(u > c.top ? c.top : u);
+    uint32_t code = ((b + ((1u << (c.sh - 1)) - 1u) + ((b >> c.sh) & 1u)) >> c.sh) - (uint32_t)c.off;
+    if (u < c.norm) code = __float_as_uint(u + c.sub) - __float_as_uint(c.sub);
+    if (u != u) code = 0x7Fu;
+    return code | sign;
+}
+
+// four values -> four codes of one word, the first in the low byte
+__device__ __forceinline__ uint32_t code_four(float a, float b, float c, float d, const CodeFmt& f) {
+    if (f.e4m3) {
+        const float v[4] = {a, b, c, d};
+        float s[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float u = v[j] * f.scale;
+            s[j] = u > 448.0f ? 448.0f : (u < -448.0f ? -448.0f : u);      // a NaN stays one: the conversion writes 0x7f for it
+        }
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], w, true);
+    }
+    return code_one(a, f) | (code_one(b, f) << 8) | (code_one(c, f) << 16) | (code_one(d, f) << 24);
+}
+
+// V consecutive elements <-> float registers
+template <int V> __device__ __forceinline__ void load_vec(const float* p, float (&v)[V]) {
+    const typename Vec<float, V>::type x = *(const typename Vec<float, V>::type*)p;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = x[j];
+}
+template <int V> __device__ __forceinline__ void load_vec(const bf16_t* p, float (&v)[V]) {
+    const typename Vec<uint16_t, V>::type x = *(const typename Vec<uint16_t, V>::type*)p;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = __uint_as_float((uint32_t)x[j] << 16);
+}
+template <int V> __device__ __forceinline__ void store_vec(float* p, const float (&v)[V], const CodeFmt&) {
+    typename Vec<float, V>::type x;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = v[j];
+    *(typename Vec<float, V>::type*)p = x;
+}
+template <int V> __device__ __forceinline__ void store_vec(bf16_t* p, const float (&v)[V], const CodeFmt&) {
+    typename Vec<bf16_t, V>::type x;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = (bf16_t)v[j];
+    *(typename Vec<bf16_t, V>::type*)p = x;
+}
+template <int V> __device__ __forceinline__ void store_vec(uint8_t* p, const float (&v)[V], const CodeFmt& f) {
+    typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(1)));
+    words x;
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) x[j] = code_four(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], f);
+    *(words*)p = x;
+}
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ float load_one(const bf16_t* p) { return (float)*p; }
+__device__ __forceinline__ void store_one(float* p, float v, const CodeFmt&) { *p = v; }
+__device__ __forceinline__ void store_one(bf16_t* p, float v, const CodeFmt&) { *p = (bf16_t)v; }
+__device__ __forceinline__ void store_one(uint8_t* p, float v, const CodeFmt& f) { *p = (uint8_t)code_one(v, f); }
+
+// the first `n` of V elements (n >= V: all); what is past them reads as `fill`
+template <int V, typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&v)[V], float fill = 0.0f) {
+    if (n >= V) { load_vec<V>(p, v); return; }
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = j < n ? load_one(p + j) : fill;
+}
+template <int V, typename T> __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[V], const CodeFmt& f) {
+    if (n >= V) { store_vec<V>(p, v, f); return; }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (j < n) store_one(p + j, v[j], f);
+}
+
+// ---- activations ----------------------------------------------------------------------------
+
+// e^x to 1.5 ulp: 2^t of the rounded product t = x log2 e, corrected by what the rounding left off
+__device__ __forceinline__ float exp_near(float x) {
+    x = fminf(fmaxf(x, -104.0f), 88.8f);
+    const float t = x * 1.44269502f;
+    const float left = fmaf(x, 1.44269502f, -t) + x * 1.92596303e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, left * 0.693147181f, e);
+}
+
+__device__ __forceinline__ float act_value(float z, int act) {
+    if (act == LBA_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (act == LBA_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (act == LBA_ACT_SILU) return z / (1.0f + exp_near(-z));
+    return z;
+}
+// act(z) and its derivative
+__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
+    if (act == LBA_ACT_RELU) {
+        value = z > 0.0f ? z : (z != z ? z : 0.0f);
+        slope = z > 0.0f ? 1.0f : 0.0f;
+    } else if (act == LBA_ACT_GELU) {
+        const float phi = 0.5f * (1.0f + erff(z * 0.70710678f));
+        value = z * phi;
+        slope = fmaf(z * 0.39894228f, exp_near(-0.5f * z * z), phi);
+    } else if (act == LBA_ACT_SILU) {
+        const float h = 1.0f / (1.0f + exp_near(-z));
+        value = z * h;
+        slope = h * (1.0f + z * (1.0f - h));
+    } else {
+        value = z;
+        slope = 1.0f;
+    }
+}
+
+// ---- dropout --------------------------------------------------------------------------------
+
+struct DropParams {
+    uint64_t seed, stream;
+    const uint64_t* step;
+    uint32_t threshold;      // an element stays iff its 16 bits are at least this; 0: nothing is dropped
+    float keep_scale;        // 65536 / (65536 - threshold); 0 where everything is dropped
+};
+
+constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
+
+__host__ __device__ __forceinline__ uint64_t mix64(uint64_t z) {
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+__device__ __forceinline__ uint64_t drop_base(const DropParams& d) {
+    const uint64_t s = d.stream + (d.step ? *d.step : 0ull);
+    return mix64(mix64(d.seed * 2 + 1) ^ ((s * 2 + 1) * kGolden));
+}
+// factors (0 or keep_scale) of V consecutive elements from index i on
+template <int V> __device__ __forceinline__ void drop_factors(uint64_t i, uint64_t base, uint32_t threshold, float keep_scale, float (&f)[V]) {
+    const uint32_t phase = (uint32_t)i & 3u;
+    uint64_t z = (i >> 2) * kGolden + base;
+    if (phase == 0) {                                    // uniform wherever rows are multiples of 4
+#pragma unroll
+        for (int q = 0; q < (V + 3) / 4; ++q, z += kGolden) {
+            const uint64_t w = mix64(z);
+#pragma unroll
+            for (int j = 0; j < 4 && 4 * q + j < V; ++j) f[4 * q + j] = ((uint32_t)(w >> (16 * j)) & 0xFFFFu) >= threshold ? keep_scale : 0.0f;
+        }
+        return;
+    }
+    uint64_t w = mix64(z);
+#pragma unroll
+    for (int q = 0; q < (V + 3) / 4; ++q) {
+        z += kGolden;
+        const uint64_t next = mix64(z);
+        const uint64_t u = (w >> (16 * phase)) | (next << (64 - 16 * phase));
+#pragma unroll
+        for (int j = 0; j < 4 && 4 * q + j < V; ++j) f[4 * q + j] = ((uint32_t)(u >> (16 * j)) & 0xFFFFu) >= threshold ? keep_scale : 0.0f;
+        w = next;
+    }
+}
+
+// ---- sums over a wave -----------------------------------------------------------------------
+
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_zero(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xF, true));
+}
+// the sum of the wave's 64 values, the same in every lane; every lane takes part
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp_zero<0x111, 0xF>(v);                        // within rows of 16: shifted by 1, 2, 4, 8
+    v += dpp_zero<0x112, 0xF>(v);
+    v += dpp_zero<0x114, 0xF>(v);
+    v += dpp_zero<0x118, 0xF>(v);
+    v += dpp_zero<0x142, 0xA>(v);                        // rows 0 and 2 into 1 and 3, then the lower half into the upper
+    v += dpp_zero<0x143, 0xC>(v);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+}
+
+// ---- column sums ----------------------------------------------------------------------------
+
+// out0[n] = sum over `parts` rows of part[row * ld + n], and with out1 out1[n] that of part[row * ld + N + n] (out0 may be null then),
+// always in the same order
+void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st);
+// float32 zeros (a kernel, so that it can be captured)
+void launch_zero(float* out, int64_t n, hipStream_t st);
+
+// ---- host checks ----------------------------------------------------------------------------
+
+inline int check_float_type(int32_t t) { return t == LBA_F32 || t == LBA_BF16 ? LBA_OK : LBA_ERR_UNSUPPORTED; }
+int check_out_type(int32_t t, const lba_infmt& f);
+int check_drop(const lba_drop& d, DropParams* out);
+int check_rows(int64_t M, int64_t N);
+inline int check_act(int32_t a) { return a >= LBA_ACT_NONE && a <= LBA_ACT_SILU ? LBA_OK : LBA_ERR_UNSUPPORTED; }
+
+constexpr size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+}  // namespace lba
+#endif

@@ -1,0 +1,490 @@
+// lba_norm.hip -- layer norm over rows and its gradients (include/lba_layer.h).
+//
+// Forward: a row is read once into registers; mean = sum / N, then the sum of squared differences from that mean, both in
+// float32 over the same registers, so nothing cancels.  Backward: with n = (x - mean) * rstd and h = g * gamma the row sums of h and
+// h * n come from registers too, and the column sums of g * n and g, which dgamma and dbeta are, stay in the registers of the lanes
+// that own the columns while a workgroup walks over its rows; one row of partial sums per workgroup goes to the workspace, and
+// a second launch adds them in a fixed order.
+// Both are bound by memory: every element is moved once.  A row belongs to a wave up to 8 vectors of 16 bytes a lane could not hold,
+// to a workgroup of 256 or 1024 lanes beyond; rows longer than that are read again from cache for each pass.
+#include "lba_layer_device.h"
+#include "lba_internal.h"
+
+namespace lba {
+
+// sums of K values over the T lanes that share a row (T = 64: a wave; else the whole workgroup)
+template <int T, int K> __device__ __forceinline__ void row_sums(float (&v)[K], float* lds, int turn) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
+    if (T == 64) return;
+    constexpr int W = T / 64;
+    float* at = lds + (turn & 1) * (K * W);              // two sets: a wave that is ahead writes the other one
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) at[k * W + threadIdx.x / 64] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += at[k * W + w];
+        v[k] = s;
+    }
+}
+
+struct NormParams {
+    const void* X;
+    const void* G;
+    const float* gamma;
+    const float* beta;
+    void* Y;                 // forward: y; backward: dx
+    float* mean;
+    float* rstd;
+    float* part;             // backward: [blocks][2][N] partial sums, or null
+    int64_t M;
+    int32_t N;
+    float eps, n;             // n: N, which sums are divided by (a rounded 1 / N would give a constant row another mean)
+    CodeFmt fmt;
+};
+
+template <typename TX, typename TY, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_fwd_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
+    __shared__ float lds[2 * (T / 64)];
+    const int t = threadIdx.x % T;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T; row < p.M; row += (int64_t)gridDim.x * RPB) {
+    const TX* x = (const TX*)p.X + row * p.N;
+    float v[NV][V];
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * T + t) * V;
+        load_some<V>(x + c, p.N - c, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[0] += v[i][j];
+    row_sums<T, 1>(s, lds, 0);
+    const float mean = s[0] / p.n;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * T + t) * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            v[i][j] -= mean;
+            if (c + j < p.N) s[0] = fmaf(v[i][j], v[i][j], s[0]);
+        }
+    }
+    row_sums<T, 1>(s, lds, 1);
+    const float rstd = 1.0f / sqrtf(s[0] / p.n + p.eps);
+    if (t == 0) {
+        if (p.mean) p.mean[row] = mean;
+        if (p.rstd) p.rstd[row] = rstd;
+    }
+    TY* y = (TY*)p.Y + row * p.N;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * T + t) * V;
+        if (c >= p.N) break;
+        float ga[V], be[V];
+        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, ga);
+        if (p.beta) load_some<V>(p.beta + c, p.N - c, be);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float o = v[i][j] * rstd;
+            if (p.gamma) o *= ga[j];
+            if (p.beta) o += be[j];
+            v[i][j] = o;
+        }
+        store_some<V>(y + c, p.N - c, v[i], p.fmt);
+    }
+    }
+}
+
+// rows that do not fit the registers of 1024 lanes
+template <typename TX, typename TY>
+__global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(TX), T = 1024;
+    __shared__ float lds[2 * (T / 64)];
+    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
+    const TX* x = (const TX*)p.X + row * p.N;
+    float s[1] = {0.0f}, v[V];
+    for (int c = threadIdx.x * V; c < p.N; c += T * V) {
+        load_some<V>(x + c, p.N - c, v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[0] += v[j];
+    }
+    row_sums<T, 1>(s, lds, 0);
+    const float mean = s[0] / p.n;
+    s[0] = 0.0f;
+    for (int c = threadIdx.x * V; c < p.N; c += T * V) {
+        load_some<V>(x + c, p.N - c, v, mean);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[0] = fmaf(v[j] - mean, v[j] - mean, s[0]);
+    }
+    row_sums<T, 1>(s, lds, 1);
+    const float rstd = 1.0f / sqrtf(s[0] / p.n + p.eps);
+    if (threadIdx.x == 0) {
+        if (p.mean) p.mean[row] = mean;
+        if (p.rstd) p.rstd[row] = rstd;
+    }
+    TY* y = (TY*)p.Y + row * p.N;
+    for (int c = threadIdx.x * V; c < p.N; c += T * V) {
+        load_some<V>(x + c, p.N - c, v);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float o = (v[j] - mean) * rstd;
+            if (c + j < p.N) {
+                if (p.gamma) o *= p.gamma[c + j];
+                if (p.beta) o += p.beta[c + j];
+            }
+            v[j] = o;
+        }
+        store_some<V>(y + c, p.N - c, v, p.fmt);
+    }
+    }
+}
+
+template <typename TG, typename TX, int T, int NV>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
+    __shared__ float lds[4 * (T / 64)];
+    const int t = threadIdx.x % T, sub = threadIdx.x / T;
+    float ga[NV][V], dga[NV][V], dbe[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * T + t) * V;
+        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, ga[i]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (!p.gamma) ga[i][j] = 1.0f;
+            dga[i][j] = dbe[i][j] = 0.0f;
+        }
+    }
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.M; row += (int64_t)gridDim.x * RPB) {
+        const TX* x = (const TX*)p.X + row * p.N;
+        const TG* gr = (const TG*)p.G + row * p.N;
+        float n[NV][V], g[NV][V];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * T + t) * V;
+            load_some<V>(x + c, p.N - c, n[i]);
+            load_some<V>(gr + c, p.N - c, g[i]);
+        }
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * T + t) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                n[i][j] = c + j < p.N ? (n[i][j] - mean) * rstd : 0.0f;
+                const float h = g[i][j] * ga[i][j];
+                dga[i][j] = fmaf(g[i][j], n[i][j], dga[i][j]);
+                dbe[i][j] += g[i][j];
+                s[0] += h;
+                s[1] = fmaf(h, n[i][j], s[1]);
+            }
+        }
+        if (!p.Y) continue;
+        row_sums<T, 2>(s, lds, turn++);
+        const float mh = s[0] / p.n, mhn = s[1] / p.n;
+        TX* dx = (TX*)p.Y + row * p.N;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * T + t) * V;
+            if (c >= p.N) break;
+#pragma unroll
+            for (int j = 0; j < V; ++j) n[i][j] = rstd * (g[i][j] * ga[i][j] - fmaf(n[i][j], mhn, mh));
+            store_some<V>(dx + c, p.N - c, n[i], p.fmt);
+        }
+    }
+    if (!p.part) return;
+    if (RPB > 1) {                                       // the workgroup's rows first: one after the other into LDS
+        __shared__ float acc[RPB > 1 ? 2 * T * NV * V : 1];
+        for (int r = 0; r < RPB; ++r) {
+            if (sub == r) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        float* a = acc + ((i * V + j) * T + t) * 2;
+                        a[0] = r ? a[0] + dga[i][j] : dga[i][j];
+                        a[1] = r ? a[1] + dbe[i][j] : dbe[i][j];
+                    }
+            }
+            __syncthreads();
+        }
+        if (sub != 0) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                dga[i][j] = acc[((i * V + j) * T + t) * 2];
+                dbe[i][j] = acc[((i * V + j) * T + t) * 2 + 1];
+            }
+    }
+    float* out = p.part + (int64_t)blockIdx.x * 2 * p.N;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * T + t) * V;
+        if (c >= p.N) break;
+        store_some<V>(out + c, p.N - c, dga[i], p.fmt);
+        store_some<V>(out + p.N + c, p.N - c, dbe[i], p.fmt);
+    }
+}
+
+// dx of rows that do not fit the registers of 1024 lanes
+template <typename TG, typename TX>
+__global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(TX), T = 1024;
+    __shared__ float lds[4 * (T / 64)];
+    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
+    const TX* x = (const TX*)p.X + row * p.N;
+    const TG* gr = (const TG*)p.G + row * p.N;
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float s[2] = {0.0f, 0.0f}, n[V], g[V];
+    for (int c = threadIdx.x * V; c < p.N; c += T * V) {
+        load_some<V>(x + c, p.N - c, n);
+        load_some<V>(gr + c, p.N - c, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float h = c + j < p.N && p.gamma ? g[j] * p.gamma[c + j] : g[j];
+            s[0] += h;
+            if (c + j < p.N) s[1] = fmaf(h, (n[j] - mean) * rstd, s[1]);
+        }
+    }
+    row_sums<T, 2>(s, lds, 0);
+    const float mh = s[0] / p.n, mhn = s[1] / p.n;
+    TX* dx = (TX*)p.Y + row * p.N;
+    for (int c = threadIdx.x * V; c < p.N; c += T * V) {
+        load_some<V>(x + c, p.N - c, n);
+        load_some<V>(gr + c, p.N - c, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float h = c + j < p.N && p.gamma ? g[j] * p.gamma[c + j] : g[j];
+            n[j] = rstd * (h - fmaf((n[j] - mean) * rstd, mhn, mh));
+        }
+        store_some<V>(dx + c, p.N - c, n, p.fmt);
+    }
+    }
+}
+
+// and the partial column sums of such rows: a workgroup owns 256 * V columns of a slice of the rows
+template <typename TG, typename TX>
+__global__ __launch_bounds__(256) void norm_bwd_long_params_kernel(NormParams p) {
+    constexpr int V = 16 / sizeof(TX);
+    const int c = (blockIdx.y * 256 + threadIdx.x) * V;
+    if (c >= p.N) return;
+    float dga[V], dbe[V], n[V], g[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) dga[j] = dbe[j] = 0.0f;
+    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        load_some<V>((const TX*)p.X + row * p.N + c, p.N - c, n);
+        load_some<V>((const TG*)p.G + row * p.N + c, p.N - c, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            dga[j] = fmaf(g[j], (n[j] - mean) * rstd, dga[j]);
+            dbe[j] += g[j];
+        }
+    }
+    float* out = p.part + (int64_t)blockIdx.x * 2 * p.N;
+    store_some<V>(out + c, p.N - c, dga, p.fmt);
+    store_some<V>(out + p.N + c, p.N - c, dbe, p.fmt);
+}
+
+// ---- column sums ----------------------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N) {
+    __shared__ float lds[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x / 64;
+    const int64_t n = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    const int64_t cols = out1 ? 2 * N : N;
+    if (n < cols) {
+        int64_t r = w;
+        for (; r + 12 < parts; r += 16) {
+            const float a = part[r * ld + n], b = part[(r + 4) * ld + n], c = part[(r + 8) * ld + n], d = part[(r + 12) * ld + n];
+            s += (a + b) + (c + d);
+        }
+        for (; r < parts; r += 4) s += part[r * ld + n];
+    }
+    lds[w][lane] = s;
+    __syncthreads();
+    if (w != 0 || n >= cols) return;
+    const float total = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+    if (n >= N) out1[n - N] = total;
+    else if (out0) out0[n] = total;
+}
+
+void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st) {
+    const int64_t cols = out1 ? 2 * N : N;
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, st, part, parts, ld, out0, out1, N);
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(float* out, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) out[i] = 0.0f;
+}
+void launch_zero(float* out, int64_t n, hipStream_t st) {
+    if (n > 0) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, out, n);
+}
+
+// ---- launchers ------------------------------------------------------------------------------
+
+// lanes that share a row and vectors of 16 bytes a lane holds: the least that hold N elements (0 lanes: none does)
+struct RowShape { int lanes, vecs; };
+static RowShape row_shape(int64_t N, int v) {
+    static const RowShape all[] = {{64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {1024, 2}, {1024, 4}};
+    for (const RowShape& r : all)
+        if (N <= (int64_t)r.lanes * r.vecs * v && r.vecs * v <= 16) return r;
+    return {0, 0};
+}
+
+template <typename TX, typename TY> static void norm_fwd(const NormParams& p, hipStream_t st) {
+    const RowShape r = row_shape(p.N, 16 / (int)sizeof(TX));
+    const int64_t most = 1 << 20;                        // a launch holds fewer than 2^32 lanes: the kernels walk over the rows beyond
+    const dim3 wide((unsigned)(p.M < most ? p.M : most)), four((unsigned)((p.M + 3) / 4 < most ? (p.M + 3) / 4 : most));
+#define LBA_NORM_FWD(T, NV, GRID) \
+    if (r.lanes == T && r.vecs == NV) { hipLaunchKernelGGL((norm_fwd_kernel<TX, TY, T, NV>), GRID, dim3(T < 256 ? 256 : T), 0, st, p); return; }
+    LBA_NORM_FWD(64, 1, four)
+    LBA_NORM_FWD(64, 2, four)
+    LBA_NORM_FWD(256, 2, wide)
+    LBA_NORM_FWD(1024, 2, wide)
+    if constexpr (sizeof(TX) == 4) {
+        LBA_NORM_FWD(64, 4, four)
+        LBA_NORM_FWD(256, 4, wide)
+        LBA_NORM_FWD(1024, 4, wide)
+    }
+#undef LBA_NORM_FWD
+    hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), wide, dim3(1024), 0, st, p);
+}
+
+// Workgroups of the backward pass that write partial sums: enough to fill the chip, few enough that their rows of partial sums stay a
+// small part of the traffic
+static int64_t norm_bwd_blocks(int64_t M, int64_t N) {
+    const int64_t most = N <= 1024 ? 1024 : 512;
+    const int64_t groups = N <= 1024 ? (M + 3) / 4 : M;
+    return groups < most ? groups : most;
+}
+
+template <typename TG, typename TX> static void norm_bwd(NormParams p, hipStream_t st) {
+    const RowShape r = row_shape(p.N, 16 / (int)sizeof(TX));
+    const unsigned blocks = (unsigned)norm_bwd_blocks(p.M, p.N);
+#define LBA_NORM_BWD(T, NV) \
+    if (r.lanes == T && r.vecs == NV) { \
+        hipLaunchKernelGGL((norm_bwd_kernel<TG, TX, T, NV>), dim3(blocks), dim3(T < 256 ? 256 : T), 0, st, p); \
+        return; \
+    }
+    LBA_NORM_BWD(64, 1)
+    LBA_NORM_BWD(64, 2)
+    LBA_NORM_BWD(256, 2)
+    LBA_NORM_BWD(1024, 2)
+    if constexpr (sizeof(TX) == 4) {
+        LBA_NORM_BWD(64, 4)
+        LBA_NORM_BWD(256, 4)
+        LBA_NORM_BWD(1024, 4)
+    }
+#undef LBA_NORM_BWD
+    constexpr int V = 16 / sizeof(TX);
+    if (p.part)
+        hipLaunchKernelGGL((norm_bwd_long_params_kernel<TG, TX>), dim3(blocks, (unsigned)((p.N + 256 * V - 1) / (256 * V))), dim3(256), 0, st, p);
+    if (p.Y) hipLaunchKernelGGL((norm_bwd_long_kernel<TG, TX>), dim3((unsigned)(p.M < (1 << 20) ? p.M : 1 << 20)), dim3(1024), 0, st, p);
+}
+
+int check_out_type(int32_t t, const lba_infmt& f) {
+    if (t == LBA_F32 || t == LBA_BF16) return LBA_OK;
+    if (t != LBA_CODE8) return LBA_ERR_UNSUPPORTED;
+    if (f.exp_bits < 2 || f.exp_bits > 5 || f.man_bits != 7 - f.exp_bits || f.bias < -32 || f.bias > 32) return LBA_ERR_FORMAT;
+    return LBA_OK;
+}
+int check_drop(const lba_drop& d, DropParams* out) {
+    if (!(d.p >= 0.0 && d.p <= 1.0)) return LBA_ERR_FORMAT;
+    out->seed = d.seed; out->stream = d.stream; out->step = d.step;
+    out->threshold = (uint32_t)(d.p * 65536.0 + 0.5);
+    out->keep_scale = out->threshold >= 65536u ? 0.0f : (float)(65536.0 / (65536.0 - out->threshold));
+    return LBA_OK;
+}
+int check_rows(int64_t M, int64_t N) {
+    if (M < 0 || N < 0 || M > 2147483647LL || N > ((int64_t)1 << 21)) return LBA_ERR_SHAPE;
+    return LBA_OK;
+}
+
+}  // namespace lba
+
+using namespace lba;
+
+extern "C" {
+
+int lba_layernorm(const void* X, int32_t x_type, const float* gamma, const float* beta, float eps,
+                  void* Y, int32_t y_type, lba_infmt y_fmt, float* mean, float* rstd,
+                  int64_t M, int64_t N, void* hip_stream) {
+    int rc = check_rows(M, N);
+    if (rc == LBA_OK) rc = check_float_type(x_type);
+    if (rc == LBA_OK) rc = check_out_type(y_type, y_fmt);
+    if (rc != LBA_OK) return rc;
+    if (M == 0 || N == 0) return LBA_OK;
+    if (!X || !Y) return LBA_ERR_NULL;
+    NormParams p = {};
+    p.X = X; p.gamma = gamma; p.beta = beta; p.Y = Y; p.mean = mean; p.rstd = rstd;
+    p.M = M; p.N = (int32_t)N; p.eps = eps; p.n = (float)N;
+    if (y_type == LBA_CODE8) p.fmt = make_code_fmt(y_fmt);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (x_type == LBA_F32) {
+        if (y_type == LBA_F32) norm_fwd<float, float>(p, st);
+        else if (y_type == LBA_BF16) norm_fwd<float, bf16_t>(p, st);
+        else norm_fwd<float, uint8_t>(p, st);
+    } else {
+        if (y_type == LBA_F32) norm_fwd<bf16_t, float>(p, st);
+        else if (y_type == LBA_BF16) norm_fwd<bf16_t, bf16_t>(p, st);
+        else norm_fwd<bf16_t, uint8_t>(p, st);
+    }
+    return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+}
+
+size_t lba_layernorm_bwd_workspace_bytes(int64_t M, int64_t N) {
+    if (check_rows(M, N) != LBA_OK || M == 0 || N == 0) return 0;
+    return align256((size_t)norm_bwd_blocks(M, N) * 2 * (size_t)N * sizeof(float));
+}
+
+int lba_layernorm_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type, const float* gamma,
+                      const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,
+                      int64_t M, int64_t N, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_rows(M, N);
+    if (rc == LBA_OK) rc = check_float_type(g_type);
+    if (rc == LBA_OK) rc = check_float_type(x_type);
+    if (rc != LBA_OK) return rc;
+    if (N == 0) return LBA_OK;
+    if (!dX && !dgamma && !dbeta) return LBA_ERR_NULL;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (M == 0) {
+        if (dgamma) launch_zero(dgamma, N, st);
+        if (dbeta) launch_zero(dbeta, N, st);
+        return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+    }
+    if (!G || !X || !mean || !rstd) return LBA_ERR_NULL;
+    const bool params = dgamma || dbeta;
+    if (params) {
+        if (!workspace) return LBA_ERR_NULL;
+        if ((uintptr_t)workspace % 256 != 0) return LBA_ERR_ALIGN;
+        if (workspace_bytes < lba_layernorm_bwd_workspace_bytes(M, N)) return LBA_ERR_SHAPE;
+    }
+    NormParams p = {};
+    p.X = X; p.G = G; p.gamma = gamma; p.Y = dX; p.mean = (float*)mean; p.rstd = (float*)rstd;
+    p.part = params ? (float*)workspace : nullptr;
+    p.M = M; p.N = (int32_t)N; p.n = (float)N;
+    if (g_type == LBA_F32) {
+        if (x_type == LBA_F32) norm_bwd<float, float>(p, st); else norm_bwd<float, bf16_t>(p, st);
+    } else {
+        if (x_type == LBA_F32) norm_bwd<bf16_t, float>(p, st); else norm_bwd<bf16_t, bf16_t>(p, st);
+    }
+    if (params) launch_column_sum(p.part, norm_bwd_blocks(M, N), 2 * N, dgamma, dbeta, N, st);
+    return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+}
+
+}  // extern "C"
