@@ -76,6 +76,34 @@ int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type
                     void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t lba_dropout_bwd_workspace_bytes(int64_t M, int64_t N);
 
+/* The product of 8-bit codes with float32 accumulation, and what follows it, in one call:
+ *   gated == 0:  Y = residual + keep * act(S + bias) / (1 - p),                     S = value(A) . value(B)^T,   B [N, K]
+ *   gated != 0:  Y = residual + keep * act(S_g + b_g) * (S_u + b_u) / (1 - p),      B [2 N, K], bias [2 N]: the gate's N rows first
+ * A [M, K] codes of fmt_a, B codes of fmt_b (the biases of the formats are the operands' scales: S is in real units), bias float32 or NULL,
+ * residual [M, N] of r_type or NULL, Y [M, N] of y_type.  Products are exact and sums are float32.  The NaN codes of E4M3 are outside the
+ * contract, as in lba.h: the outputs they reach are unspecified.  K == 0: S = 0.
+ * Limits (else LBA_ERR_SHAPE): M <= 2^30, N <= 2^20, K <= 2^30; (else LBA_ERR_FORMAT): the formats' limits of lba.h.
+ * workspace: lba_dense_workspace_bytes(...) bytes, NULL where that is 0; `aligned`: A and B are 16-byte aligned.  E4M3 operands whose rows
+ * are multiples of 16 bytes are used where they are; others are copied there, and codes of other formats as bfloat16, which hold them. */
+int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t K, lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated,
+              const float* bias, int32_t act, lba_drop drop, const void* residual, int32_t r_type,
+              void* Y, int32_t y_type, lba_infmt y_fmt, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t lba_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated, int32_t aligned);
+
+/* Its gradients.  Nothing of the forward call is kept: where act or gated needs S, it is computed again.  With G = dL/dY [M, N] of
+ * g_type and D the gradient of the sums ([M, N], gated [M, 2 N]: the gate's columns first),
+ *   dA = D . value(B) [M, K],   dB = D^T . value(A) [N or 2 N, K],   dbias = sum over rows of D (float32); the residual's gradient is G.
+ * dA and dB are of g_type and gradients of the operands' real values; any of the three may be NULL but not all.  Float32: D is split
+ * exactly into three bfloat16 pieces and the products are exact, sums float32 (a value of D under 2^-100 may lose pieces to the flush of
+ * subnormal numbers, an infinite one gives NaN).  Bfloat16: D is rounded to bfloat16 before the two products, as dA and dB are after
+ * them; dbias sums D before that.
+ * workspace: lba_dense_bwd_workspace_bytes(...) bytes. */
+int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t K,
+                  lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated, const float* bias, int32_t act, lba_drop drop,
+                  void* dA, void* dB, float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t lba_dense_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated, int32_t act,
+                                     int32_t g_type, int32_t aligned);
+
 #ifdef __cplusplus
 }
 #endif

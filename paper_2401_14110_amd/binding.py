@@ -137,6 +137,14 @@ def lib(path=None):
         L.lba_dropout_bwd.argtypes = [vp, i32, vp, i32, f32, vp, i32, lba_drop, vp, vp, i64, i64, vp, size, vp]
         L.lba_dropout_bwd_workspace_bytes.restype = size
         L.lba_dropout_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.lba_dense.restype = ctypes.c_int
+        L.lba_dense.argtypes = [vp, vp, i64, i64, i64, lba_infmt, lba_infmt, i32, vp, i32, lba_drop, vp, i32, vp, i32, lba_infmt, vp, size, vp]
+        L.lba_dense_workspace_bytes.restype = size
+        L.lba_dense_workspace_bytes.argtypes = [i64, i64, i64, lba_infmt, lba_infmt, i32, i32]
+        L.lba_dense_bwd.restype = ctypes.c_int
+        L.lba_dense_bwd.argtypes = [vp, i32, vp, vp, i64, i64, i64, lba_infmt, lba_infmt, i32, vp, i32, lba_drop, vp, vp, vp, vp, size, vp]
+        L.lba_dense_bwd_workspace_bytes.restype = size
+        L.lba_dense_bwd_workspace_bytes.argtypes = [i64, i64, i64, lba_infmt, lba_infmt, i32, i32, i32, i32]
         _lib = L
     return _lib
 
@@ -340,6 +348,26 @@ def lba_dropout_bwd(G, g_type, X, x_type, scale, bias, act, drop, dX, dbias, M, 
 
 def lba_dropout_bwd_workspace_bytes(M, N):
     return int(lib().lba_dropout_bwd_workspace_bytes(M, N))
+
+
+def lba_dense(A, B, M, N, K, fmt_a, fmt_b, gated, bias, act, drop, residual, r_type, Y, y_type, y_fmt, workspace, workspace_bytes,
+              hip_stream=None):
+    return lib().lba_dense(A, B, M, N, K, infmt(fmt_a), infmt(fmt_b), gated, bias, act, drop, residual, r_type, Y, y_type, infmt(y_fmt),
+                           workspace, workspace_bytes, hip_stream)
+
+
+def lba_dense_workspace_bytes(M, N, K, fmt_a, fmt_b, gated, aligned=1):
+    return int(lib().lba_dense_workspace_bytes(M, N, K, infmt(fmt_a), infmt(fmt_b), gated, aligned))
+
+
+def lba_dense_bwd(G, g_type, A, B, M, N, K, fmt_a, fmt_b, gated, bias, act, drop, dA, dB, dbias, workspace, workspace_bytes,
+                  hip_stream=None):
+    return lib().lba_dense_bwd(G, g_type, A, B, M, N, K, infmt(fmt_a), infmt(fmt_b), gated, bias, act, drop, dA, dB, dbias, workspace,
+                               workspace_bytes, hip_stream)
+
+
+def lba_dense_bwd_workspace_bytes(M, N, K, fmt_a, fmt_b, gated, act, g_type, aligned=1):
+    return int(lib().lba_dense_bwd_workspace_bytes(M, N, K, infmt(fmt_a), infmt(fmt_b), gated, act, g_type, aligned))
 
 
 # ---- tensor conveniences --------------------------------------------------------------------
@@ -775,3 +803,58 @@ def dropout_bwd(G, drop, x=None, bias=None, act=ACT_NONE, scale=1.0, want_dx=Tru
     _check(lib().lba_dropout_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[dtype], scale, _at(bias), act, d, _at(dx), _at(dbias), M, N,
                                  _at(ws), size, on.handle))
     return dx, dbias
+
+
+def _codes2(A, B, gated):
+    """(M, N, K) of the operands of a dense product: A [..., K], B [N, K], gated [2 N, K]."""
+    M, K = _rows(A, "A", (torch.uint8,))
+    if B.dtype != torch.uint8 or not B.is_cuda:
+        raise TypeError("B must be a device tensor of torch.uint8 codes")
+    if B.dim() != 2 or B.shape[1] != K or (gated and B.shape[0] % 2):
+        raise ValueError("B must be [%s, %d]" % ("2 N" if gated else "N", K))
+    if K == 0:
+        M = 1
+        for n in A.shape[:-1]:
+            M *= n
+    return M, B.shape[0] // 2 if gated else B.shape[0], K
+
+
+def dense(A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, residual=None, drop=None, gated=False, out_dtype=torch.float32,
+          out_fmt=None, out=None, stream=None):
+    """residual + keep * act(A . B^T + bias) / (1 - p) on codes A [..., K], B [N, K] with float32 accumulation; gated:
+    act(A . Bg^T + bg) * (A . Bu^T + bu) with B [2 N, K] and bias [2 N], the gate's rows first.  drop = (p, seed, stream[, step]) or None."""
+    M, N, K = _codes2(A, B, gated)
+    y_type, y_fmt = _out_type(out_dtype, out_fmt)
+    d = _drop(drop)
+    on = _On(stream)
+    A, B, bias = on.whole(A), on.whole(B), _vector(on, bias, 2 * N if gated else N, "bias")
+    shape = A.shape[:-1] + (N,)
+    if residual is not None:
+        residual = on.whole(_like(residual, shape, "residual"))
+    y = _output(on, out, shape, out_dtype, A.device)
+    L, fa, fb, a, b = lib(), infmt(fmt_a), infmt(fmt_b), _at(A), _at(B)
+    size = L.lba_dense_workspace_bytes(M, N, K, fa, fb, gated, ((a or 0) | (b or 0)) % 16 == 0)
+    ws = on.empty((size,), torch.uint8, A.device) if size else None
+    _check(L.lba_dense(a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(residual), _TYPE[residual.dtype] if residual is not None else F32,
+                       _at(y), y_type, y_fmt, _at(ws), size, on.handle))
+    return y
+
+
+def dense_bwd(G, A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, drop=None, gated=False, want_da=True, want_db=True,
+              want_dbias=False, stream=None):
+    """Gradients of dense: (dA, dB of G's type, dbias float32; None where not asked for), of the operands' real values.  The sums that an
+    activation or a gate needs are computed again from A, B and bias.  The residual's gradient is G."""
+    M, N, K = _codes2(A, B, gated)
+    _like(G, A.shape[:-1] + (N,), "G")
+    d = _drop(drop)
+    on = _On(stream)
+    cols = 2 * N if gated else N
+    G, A, B, bias = on.whole(G), on.whole(A), on.whole(B), _vector(on, bias, cols, "bias")
+    dA = on.empty(A.shape, G.dtype, A.device) if want_da else None
+    dB = on.empty(B.shape, G.dtype, A.device) if want_db else None
+    dbias = on.empty((cols,), torch.float32, A.device) if want_dbias else None
+    L, fa, fb, a, b, t = lib(), infmt(fmt_a), infmt(fmt_b), _at(A), _at(B), _TYPE[G.dtype]
+    size = L.lba_dense_bwd_workspace_bytes(M, N, K, fa, fb, gated, act, t, ((a or 0) | (b or 0)) % 16 == 0)
+    ws = on.empty((size,), torch.uint8, A.device) if size else None
+    _check(L.lba_dense_bwd(_at(G), t, a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(dA), _at(dB), _at(dbias), _at(ws), size, on.handle))
+    return dA, dB, dbias

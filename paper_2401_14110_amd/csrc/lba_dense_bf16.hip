@@ -1,0 +1,7 @@
+// Instantiations of the dense tile for bfloat16 rows: codes of five exponent bits, which are laid out as bfloat16 numbers, and the gradient
+// products.
+#include "lba_dense.h"
+
+namespace lba {
+void launch_dense_bf16(GemmParams& p, int tile, bool gated, int epi, hipStream_t st) { launch_dense<ELEM_BF16>(p, tile, gated, epi, st); }
+}  // namespace lba

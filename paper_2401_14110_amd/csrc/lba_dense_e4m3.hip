@@ -1,0 +1,6 @@
+// Instantiations of the dense tile for E4M3 codes.
+#include "lba_dense.h"
+
+namespace lba {
+void launch_dense_e4m3(GemmParams& p, int tile, bool gated, int epi, hipStream_t st) { launch_dense<ELEM_E4M3>(p, tile, gated, epi, st); }
+}  // namespace lba

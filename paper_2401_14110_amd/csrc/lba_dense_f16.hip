@@ -1,0 +1,6 @@
+// Instantiations of the dense tile for codes of two to four exponent bits.
+#include "lba_dense.h"
+
+namespace lba {
+void launch_dense_f16(GemmParams& p, int tile, bool gated, int epi, hipStream_t st) { launch_dense<ELEM_F16>(p, tile, gated, epi, st); }
+}  // namespace lba

@@ -229,7 +229,7 @@ int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type
     if (!dX && !dbias) return LBA_ERR_NULL;
     const hipStream_t st = (hipStream_t)hip_stream;
     if (M == 0) {
-        if (dbias) launch_zero(dbias, N, st);
+        if (dbias) launch_zero(dbias, N * 4, st);
         return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
     }
     if (!G || (act != LBA_ACT_NONE && !X)) return LBA_ERR_NULL;

@@ -117,13 +117,14 @@ template <int V, typename T> __device__ __forceinline__ void store_some(T* p, in
 
 // ---- activations ----------------------------------------------------------------------------
 
-// e^x to 1.5 ulp: 2^t of the rounded product t = x log2 e, corrected by what the rounding left off
+// e^x to 1.5 ulp: 2^t of the rounded product t = x log2 e, corrected by what the rounding left off.  Beyond float32's range the
+// correction must not meet an infinity: arguments under it are taken as one whose result is flushed, above it infinity is returned.
 __device__ __forceinline__ float exp_near(float x) {
-    x = fminf(fmaxf(x, -104.0f), 88.8f);
-    const float t = x * 1.44269502f;
-    const float left = fmaf(x, 1.44269502f, -t) + x * 1.92596303e-8f;
+    const float y = fminf(fmaxf(x, -104.0f), 88.72f);
+    const float t = y * 1.44269502f;
+    const float left = fmaf(y, 1.44269502f, -t) + y * 1.92596303e-8f;
     const float e = __builtin_amdgcn_exp2f(t);
-    return fmaf(e, left * 0.693147181f, e);
+    return x > 88.72f ? __builtin_inff() : fmaf(e, left * 0.693147181f, e);
 }
 
 __device__ __forceinline__ float act_value(float z, int act) {
@@ -217,8 +218,8 @@ __device__ __forceinline__ float wave_sum(float v) {
 // out0[n] = sum over `parts` rows of part[row * ld + n], and with out1 out1[n] that of part[row * ld + N + n] (out0 may be null then),
 // always in the same order
 void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st);
-// float32 zeros (a kernel, so that it can be captured)
-void launch_zero(float* out, int64_t n, hipStream_t st);
+// zeros (an even number of bytes; a kernel, so that it can be captured)
+void launch_zero(void* out, int64_t bytes, hipStream_t st);
 
 // ---- host checks ----------------------------------------------------------------------------
 

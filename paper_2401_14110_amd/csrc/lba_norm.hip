@@ -327,12 +327,12 @@ void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0
     hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(256), 0, st, part, parts, ld, out0, out1, N);
 }
 
-__global__ __launch_bounds__(256) void zero_kernel(float* out, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) out[i] = 0.0f;
+__global__ __launch_bounds__(256) void zero_kernel(uint16_t* out, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) out[i] = 0;
 }
-void launch_zero(float* out, int64_t n, hipStream_t st) {
-    if (n > 0) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, out, n);
+void launch_zero(void* out, int64_t bytes, hipStream_t st) {
+    const int64_t n = bytes / 2, blocks = (n + 255) / 256;
+    if (n > 0) hipLaunchKernelGGL(zero_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, (uint16_t*)out, n);
 }
 
 // ---- launchers ------------------------------------------------------------------------------
@@ -463,8 +463,8 @@ int lba_layernorm_bwd(const void* G, int32_t g_type, const void* X, int32_t x_ty
     if (!dX && !dgamma && !dbeta) return LBA_ERR_NULL;
     const hipStream_t st = (hipStream_t)hip_stream;
     if (M == 0) {
-        if (dgamma) launch_zero(dgamma, N, st);
-        if (dbeta) launch_zero(dbeta, N, st);
+        if (dgamma) launch_zero(dgamma, N * 4, st);
+        if (dbeta) launch_zero(dbeta, N * 4, st);
         return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
     }
     if (!G || !X || !mean || !rstd) return LBA_ERR_NULL;

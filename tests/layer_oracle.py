@@ -2,9 +2,9 @@
 import math
 
 import numpy as np
+from scipy.special import erf as _erf
 
 U = 2.0 ** -24                       # half a unit in the last place of float32, relative
-_erf = np.vectorize(math.erf, otypes=[np.float64])
 
 
 def code_values(E, M, bias):
@@ -107,3 +107,51 @@ def norm_bwd(G, x, gamma, mean, rstd):
     depth = 64 + n / 512
     tx = depth * U * rstd[:, None] * (np.abs(h) + np.abs(h).mean(-1, keepdims=True) + np.abs(u) * np.abs(h * u).mean(-1, keepdims=True)) + 1e-37
     return (dx, (G * u).sum(0), G.sum(0)), (tx, (m + 64) * U * np.abs(G * u).sum(0) + 1e-37, (m + 64) * U * np.abs(G).sum(0) + 1e-37)
+
+
+def dense(A, B, fa, fb, bias, act_kind, gated, f, residual):
+    """(y, tol, parts): the product of codes and what follows it; f: the dropout factors or None.  A sum of K exact products in float32 is off
+    by at most (K + 16) U of the sum of their magnitudes; activations change by at most 1.2 of what their argument does."""
+    a, b = code_values(*fa)[A], code_values(*fb)[B]
+    K = a.shape[1]
+    z, za = a @ b.T, np.abs(a) @ np.abs(b).T
+    tz = (K + 16) * U * za
+    if bias is not None:
+        z, tz = z + bias, tz + 2 * U * (np.abs(z) + np.abs(bias))
+    n = z.shape[1] // 2 if gated else z.shape[1]
+    v, slope = act(z[:, :n], act_kind)
+    tv = 1.2 * tz[:, :n] + 16 * U * (np.abs(z[:, :n]) + np.abs(v))
+    y, ty = v, tv
+    if gated:
+        u, tu = z[:, n:], tz[:, n:]
+        y, ty = v * u, tv * np.abs(u) + (np.abs(v) + tv) * tu + 2 * U * np.abs(v * u)
+    if f is not None:
+        y, ty = y * f, (ty + 2 * U * np.abs(y)) * f
+    if residual is not None:
+        y, ty = y + residual, ty + 2 * U * (np.abs(y) + np.abs(residual))
+    return y, ty + 1e-37, dict(a=a, b=b, z=z, tz=tz, v=v, tv=tv, slope=slope, n=n, f=f, gated=gated, act=act_kind)
+
+
+def dense_bwd(G, parts, rounded):
+    """((dA, dB, dbias), their bounds).  `rounded`: the gradient of the sums is rounded to bfloat16 before the products."""
+    a, b, z, n = parts["a"], parts["b"], parts["z"], parts["n"]
+    g = G if parts["f"] is None else G * parts["f"]
+    ts = 1.2 * parts["tz"][:, :n] + 24 * U
+    if parts["act"] == 1:                                   # a sum within its error of the corner may fall on either side
+        ts = np.where(np.abs(z[:, :n]) <= parts["tz"][:, :n], 1.0, 0.0) + 2 * U
+    if parts["act"] == 0:
+        ts = 2 * U * np.ones_like(ts)
+    if parts["gated"]:
+        u, tu = z[:, n:], parts["tz"][:, n:]
+        d = np.concatenate([g * u * parts["slope"], g * parts["v"]], 1)
+        t = np.concatenate([np.abs(g) * (ts * (np.abs(u) + tu) + np.abs(parts["slope"]) * tu), np.abs(g) * parts["tv"]], 1) + 4 * U * np.abs(d)
+    else:
+        d = g * parts["slope"]
+        t = np.abs(g) * ts + 4 * U * np.abs(d)
+    m, cols = d.shape
+    db, tb = d.sum(0), t.sum(0) + (m + 64) * U * np.abs(d).sum(0)
+    t = t + (2.0 ** -8 if rounded else 0.0) * np.abs(d)
+    dA, dB = d @ b, d.T @ a
+    tA = t @ np.abs(b) + (3 * cols + 16) * U * (np.abs(d) @ np.abs(b))
+    tB = t.T @ np.abs(a) + (3 * m + 16) * U * (np.abs(d).T @ np.abs(a))
+    return (dA, dB, db), (tA + 1e-37, tB + 1e-37, tb + 1e-37)

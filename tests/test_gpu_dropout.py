@@ -117,6 +117,19 @@ def test_step_word_and_graph_replays():
 
 
 @pytest.mark.gpu
+def test_activations_far_out():
+    z = np.array([-3e38, -1e30, -1e4, -200.0, -104.0, -100.0, -90.0, -88.8, -88.73, -80.0, -20.0, -0.0, 0.0, 1e-30, 20.0, 88.0, 89.0, 1e4, 1e30, 3e38], np.float32)
+    for act in (1, 2, 3):
+        with np.errstate(over="ignore"):
+            v, slope = lo.act(z.astype(np.float64), act)
+        y = lb.dropout(dev(z), None, act=act)
+        dx, _ = lb.dropout_bwd(torch.ones(20, device=DEV), None, x=dev(z), act=act)
+        # 1 + erf cancels below zero: the error is that of the sum, relative to |z|; elsewhere a few roundings
+        near(y, v, 16 * lo.U * (np.abs(v) + np.minimum(np.abs(z.astype(np.float64)), 6.0)) + 1e-37, "f32")
+        near(dx, slope, 24 * lo.U * (np.abs(slope) + 1) + 1e-37, "f32")
+
+
+@pytest.mark.gpu
 def test_differences():
     rng = np.random.default_rng(12)
     M, N, eps = 16, 48, 2.0 ** -7
