@@ -8,7 +8,7 @@
 // LDS and become bfloat16 (E4M3, one conversion instruction for two codes) or FP16 numbers (at most 4 exponent bits: the code's fields moved to
 // FP16's places, which is the value times a power of two) in registers on their way into the matrix cores: products are exact, sums float32.
 // A workgroup owns BM x BN outputs and walks over k in steps of 128 bytes of a row: BM + BN rows of the step go from global memory
-// straight to LDS (16 bytes a lane, no registers in between) into one of two buffers while the matrix cores work on the other.
+// straight to LDS (16 bytes a lane, no registers in between) into one of NST buffers while the matrix cores work on another.
 // A row of 128 bytes is 8 pieces of 16; piece c of row r stands at place c ^ (r / 2 % 8), so that the sixteen rows of a fragment
 // read, 16 bytes each, fall on all 64 banks once.  An operand's pieces beyond the end of its rows are read from a zero page and
 // rows beyond the last one repeat it: their outputs are not stored.
@@ -25,6 +25,9 @@ namespace lba {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
@@ -45,7 +48,7 @@ struct EpiParams {
     const void* G;
     int32_t g_type;
     int32_t pieces;          // 1: rounded to bfloat16; 3: float32 split exactly
-    bf16_t* P;               // [pieces][M][ldp]: N columns and zeros up to `wide`, gated: the second half's from `wide` on
+    bf16_t* P;               // [pieces][M][ldp]: N columns and zeros up to `wide`, gated: then the second half's
     bf16_t* PT;              // [pieces][N or 2 N][ldt]
     int64_t ldp, ldt, p_piece, pt_piece;
     int32_t wide;            // N rounded up to 8
@@ -63,116 +66,126 @@ struct GemmParams {
     int32_t chunks;          // 16-byte pieces of a row
     int32_t steps;           // steps of 128 bytes over all pieces of A
     int32_t gx, gy;          // tiles over m and n
-    int32_t slices;          // the steps are cut into so many slices of `per_slice`, each of which stores its sums (split > 0)
+    int32_t slices;          // > 1: the steps are cut into so many slices of `per_slice`, each of which stores its sums in `split`
     int32_t per_slice;
-    float* split;            // [slices][M][N] raw sums, or null
+    float* split;            // [slices][M][rows_b] raw sums
     int32_t shift_a, shift_b;     // ELEM_F16: M - 2 of the operand's format
-    uint32_t keep_a, keep_b;      // and the magnitude's places in both halves of a word
+    uint32_t keep_a, keep_b;      // and the places of sign and magnitude in both halves of a word
     EpiParams e;
 };
 
-__device__ __forceinline__ void load_typed4(const void* at, int type, int64_t i, int n, float (&v)[4]) {
-    if (type == LBA_F32) load_some<4>((const float*)at + i, n, v);
-    else load_some<4>((const bf16_t*)at + i, n, v);
+// one launch of one product or two: workgroups below `blocks` belong to the first
+struct GemmPair { GemmParams g[2]; int32_t blocks; };
+
+__device__ __forceinline__ int up_to_8(int x) { return (x + 7) & ~7; }
+
+// An element's index in two parts: `u` is the same for a wave in the tile (a scalar register), `o` a lane's 32-bit offset from it.
+struct At { int64_t u; uint32_t o; };
+template <typename T> __device__ __forceinline__ T* at(const T* p, const At& i) {
+    return (T*)((char*)p + i.u * (int64_t)sizeof(T) + (uint32_t)(i.o * (uint32_t)sizeof(T)));
 }
 
-// a lane's four columns: how many there are and their bias
-template <bool GATED> struct Columns { int n, cnt; float b[4], bu[4]; };
-template <bool GATED> __device__ __forceinline__ Columns<GATED> columns_of(const EpiParams& e, int n) {
-    Columns<GATED> c;
+// a lane's V columns: how many of them there are and their bias
+template <bool GATED, int V> struct Columns { int n, cnt; float b[V], bu[V]; };
+template <bool GATED, int V> __device__ __forceinline__ Columns<GATED, V> columns_of(const EpiParams& e, int n) {
+    Columns<GATED, V> c;
     c.n = n;
     c.cnt = e.N - n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c.b[j] = c.bu[j] = 0.0f;
+    for (int j = 0; j < V; ++j) c.b[j] = c.bu[j] = 0.0f;
     if (e.bias && c.cnt > 0) {
-        load_some<4>(e.bias + n, c.cnt, c.b);
-        if (GATED) load_some<4>(e.bias + e.N + n, c.cnt, c.bu);
+        load_some<V>(e.bias + n, c.cnt, c.b);
+        if (GATED) load_some<V>(e.bias + e.N + n, c.cnt, c.bu);
     }
     return c;
 }
 
-// sums of one output's four columns -> Y.  z: the sums (gated: the gate's), u: the second half's, r: the residual's values if there is one
-template <bool GATED> __device__ __forceinline__ void finish_forward(const EpiParams& e, const Columns<GATED>& c, uint64_t base, int m, float (&z)[4],
-                                                                     float (&u)[4], const float (&r)[4]) {
-    if (m >= e.M || c.cnt <= 0) return;
-    const int64_t i = (int64_t)m * e.N + c.n;
+// Sums of one output's V columns -> Y.  z: the sums (gated: the gate's), u: the second half's, r: the residual's values if there is one.
+template <bool GATED, bool INSIDE, int ACT, int V>
+__device__ __forceinline__ void finish_forward(const EpiParams& e, const Columns<GATED, V>& c, uint64_t base, int m, const At& i, float (&z)[V], float (&u)[V],
+                                               const float (&r)[V]) {
+    if (!INSIDE && (m >= e.M || c.cnt <= 0)) return;
+    const int cnt = INSIDE ? V : c.cnt;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        z[j] = fmaf(z[j], e.scale, c.b[j]);
-        if (GATED) u[j] = fmaf(u[j], e.scale, c.bu[j]);
-    }
-    if (e.act != LBA_ACT_NONE) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = act_value(z[j], e.act);
-    }
-    if (GATED) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] *= u[j];
+    for (int j = 0; j < V; ++j) {
+        if (j == 4) __builtin_amdgcn_sched_barrier(0);   // four at a time: more would only cost registers
+        z[j] = act_value<ACT>(fmaf(z[j], e.scale, c.b[j]));
+        if (GATED) z[j] *= fmaf(u[j], e.scale, c.bu[j]);
     }
     if (e.drop.threshold) {
-        float f[4];
-        drop_factors<4>((uint64_t)i, base, e.drop.threshold, e.drop.keep_scale, f);
+        float f[V];
+        drop_factors<V>((uint64_t)i.u + i.o, base, e.drop.threshold, e.drop.keep_scale, (e.N & 3) == 0, f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = f[j] != 0.0f ? z[j] * f[j] : 0.0f;
+        for (int j = 0; j < V; ++j) z[j] = f[j] != 0.0f ? z[j] * f[j] : 0.0f;
     }
     if (e.R) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] += r[j];
+        for (int j = 0; j < V; ++j) z[j] += r[j];
     }
-    if (e.y_type == LBA_F32) store_some<4>((float*)e.Y + i, c.cnt, z, e.fmt);
-    else if (e.y_type == LBA_BF16) store_some<4>((bf16_t*)e.Y + i, c.cnt, z, e.fmt);
-    else store_some<4>((uint8_t*)e.Y + i, c.cnt, z, e.fmt);
+    if (e.y_type == LBA_F32) store_some<V>(at((float*)e.Y, i), cnt, z, e.fmt);
+    else if (e.y_type == LBA_BF16) store_some<V>(at((bf16_t*)e.Y, i), cnt, z, e.fmt);
+    else store_some<V>(at((uint8_t*)e.Y, i), cnt, z, e.fmt);
 }
-// what finish_forward adds and finish_backward starts from
-__device__ __forceinline__ void load_extra(const EpiParams& e, const void* at, int type, int m, int n, float (&r)[4]) {
+// what finish_forward adds, read at once
+template <int V> __device__ __forceinline__ void load_extra(const EpiParams& e, int m, int n, float (&r)[V]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r[j] = 0.0f;
-    if (at && m < e.M && n < e.N) load_typed4(at, type, (int64_t)m * e.N + n, e.N - n, r);
+    for (int j = 0; j < V; ++j) r[j] = 0.0f;
+    if (!e.R || m >= e.M || n >= e.N) return;
+    if (e.r_type == LBA_F32) load_some<V>((const float*)e.R + (int64_t)m * e.N + n, e.N - n, r);
+    else load_some<V>((const bf16_t*)e.R + (int64_t)m * e.N + n, e.N - n, r);
 }
 
-// the pieces of a gradient: one, rounded to nearest, or three that add up to it exactly (truncate, subtract, truncate, subtract)
-__device__ __forceinline__ void bf16_pieces(float d, int pieces, bf16_t (&p)[3]) {
-    if (pieces == 1) { p[0] = p[1] = p[2] = (bf16_t)d; return; }
-    const uint32_t hi = __float_as_uint(d) & 0xFFFF0000u;
-    const float r1 = d - __uint_as_float(hi);
-    const uint32_t mid = __float_as_uint(r1) & 0xFFFF0000u;
-    const float r2 = r1 - __uint_as_float(mid);
-    p[0] = __builtin_bit_cast(bf16_t, (uint16_t)(hi >> 16));
-    p[1] = __builtin_bit_cast(bf16_t, (uint16_t)(mid >> 16));
-    p[2] = __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(r2) >> 16));
-}
-
-// sums of one output's four columns -> the gradients of the sums, in z (and u); g: the output's gradient
-template <bool GATED> __device__ __forceinline__ void finish_backward(const EpiParams& e, const Columns<GATED>& c, uint64_t base, int m, float (&z)[4],
-                                                                      float (&u)[4], const float (&g)[4]) {
-    float f[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-    if (e.drop.threshold) drop_factors<4>((uint64_t)m * (uint64_t)e.N + (uint64_t)c.n, base, e.drop.threshold, e.drop.keep_scale, f);
+// Sums of one output's V columns -> the gradients of the sums, in z (and u); g: the output's gradient.
+template <bool GATED, bool INSIDE, int ACT, int V>
+__device__ __forceinline__ void finish_backward(const EpiParams& e, const Columns<GATED, V>& c, uint64_t base, int m, const At& i, float (&z)[V], float (&u)[V],
+                                                const float (&g)[V]) {
+    float f[V];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool on = m < e.M && j < c.cnt && f[j] != 0.0f;        // a dropped element's sums do not matter
+    for (int j = 0; j < V; ++j) f[j] = 1.0f;
+    if (e.drop.threshold) drop_factors<V>((uint64_t)i.u + i.o, base, e.drop.threshold, e.drop.keep_scale, (e.N & 3) == 0, f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (j == 4) __builtin_amdgcn_sched_barrier(0);
+        const bool on = (INSIDE || (m < e.M && j < c.cnt)) && f[j] != 0.0f;        // a dropped element's sums do not matter
         float value, slope;
-        act_both(fmaf(z[j], e.scale, c.b[j]), e.act, value, slope);
+        act_both<ACT>(fmaf(z[j], e.scale, c.b[j]), value, slope);
         const float d = g[j] * f[j];
         z[j] = on ? (GATED ? d * fmaf(u[j], e.scale, c.bu[j]) * slope : d * slope) : 0.0f;
         if (GATED) u[j] = on ? d * value : 0.0f;
     }
 }
-// and their store along the columns, zeros up to `wide`
-__device__ __forceinline__ void store_gradient(const EpiParams& e, int m, int n, int half, const float (&d)[4]) {
-    if (!e.P || m >= e.M || n >= e.wide) return;                     // wide and n are multiples of 4
-    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-    u16x4 w[3];
+
+// eight values -> bfloat16: rounded to nearest, or (`piece` 0, 1, 2) the piece of float32 values that three pieces add up to exactly
+// (truncate, subtract, truncate, subtract)
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ u16x8 eight_rounded(const float (&d)[8]) {
+    u16x8 w;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        bf16_t p[3];
-        bf16_pieces(d[j], e.pieces, p);
+    for (int j = 0; j < 8; ++j) w[j] = __builtin_bit_cast(uint16_t, (bf16_t)d[j]);
+    return w;
+}
+__device__ __forceinline__ void eight_pieces(const float (&d)[8], u16x8 (&w)[3]) {
 #pragma unroll
-        for (int q = 0; q < 3; ++q) w[q][j] = __builtin_bit_cast(uint16_t, p[q]);
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t hi = __float_as_uint(d[j]) & 0xFFFF0000u;
+        const float r1 = d[j] - __uint_as_float(hi);
+        const uint32_t mid = __float_as_uint(r1) & 0xFFFF0000u;
+        const float r2 = r1 - __uint_as_float(mid);
+        w[0][j] = (uint16_t)(hi >> 16);
+        w[1][j] = (uint16_t)(mid >> 16);
+        w[2][j] = (uint16_t)(__float_as_uint(r2) >> 16);
     }
-    bf16_t* at = e.P + m * e.ldp + half * e.wide + n;
+}
+// stores eight neighbouring values of the gradient matrix (16-byte aligned), or of its transpose
+__device__ __forceinline__ void store_eight(bf16_t* to, const At& i, int pieces, int64_t piece, const float (&d)[8]) {
+    if (pieces == 1) {
+        *(u16x8*)at(to, i) = eight_rounded(d);
+        return;
+    }
+    u16x8 w[3];
+    eight_pieces(d, w);
 #pragma unroll
-    for (int q = 0; q < 3; ++q)
-        if (q < e.pieces) *(u16x4*)(at + q * e.p_piece) = w[q];
+    for (int q = 0; q < 3; ++q) *(u16x8*)at(to + q * piece, i) = w[q];
 }
 
 // which tile a workgroup takes: consecutive workgroups go to the eight dies in turn, so that a die gets a contiguous run of tiles, and
@@ -202,10 +215,15 @@ template <int ELEM> __device__ __forceinline__ i32x4 eight_codes(uint32_t w0, ui
         v[2] = __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
         v[3] = __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
     } else {
+        // A code in the high byte of a half, shifted down with its sign, is the FP16 number but for the sign's copies and what lies below:
+        // `keep` takes those out.  The bytes of a word come in the order 1, 3, 0, 2, for both operands.
+        typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+        const i16x2 s2 = {(int16_t)shift, (int16_t)shift};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                    // the code in the high byte of a half: its sign stays, its magnitude moves down
-            const uint32_t x = __builtin_amdgcn_perm(0, i < 2 ? w0 : w1, i % 2 ? 0x030c020cu : 0x010c000cu);
-            v[i] = (int32_t)((x & 0x80008000u) | ((x >> shift) & keep));
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w = i ? w1 : w0;
+            v[2 * i] = (int32_t)(__builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, w) >> s2) & keep);
+            v[2 * i + 1] = (int32_t)(__builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, w << 8) >> s2) & keep);
         }
     }
     return v;
@@ -215,17 +233,21 @@ template <int ELEM> __device__ __forceinline__ f32x4 product_16x16x32(i32x4 b, i
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b), __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
 }
 
-// WM x WN waves of FM x FN fragments of 16 x 16
-template <int ELEM, int WM, int WN, int FM, int FN, bool GATED, int EPI>
-__global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
+// WM x WN waves of FM x FN fragments of 16 x 16, NST buffers of a step
+template <int ELEM, int WM, int WN, int FM, int FN, int NST, bool GATED, int EPI>
+__global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(GemmPair both) {
+    const bool second = (int)blockIdx.x >= both.blocks;
+    const GemmParams& p = both.g[second];
     constexpr int THREADS = WM * WN * 64, BM = WM * FM * 16, BN = WN * FN * 16;
     constexpr int LA = BM * 8 / THREADS, LB = BN * 8 / THREADS;          // pieces a lane stages for a step
     static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0 && (!GATED || FN % 2 == 0), "tile");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][(BM + BN) * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(BM + BN) * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wm = wave / WN, wn = wave % WN;
     int tm, tn;
-    tile_of(p.gx, p.gy, blockIdx.x, tm, tn);
+    const int id = second ? (int)blockIdx.x - both.blocks : (int)blockIdx.x;
+    const int slice = p.slices > 1 ? id / (p.gx * p.gy) : 0;
+    tile_of(p.gx, p.gy, id - slice * (p.gx * p.gy), tm, tn);
     const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
 
     // staging: lane's rows and its piece of each
@@ -250,20 +272,23 @@ __global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
         }
         src[LA + i] = p.B + r * p.ldb + piece * 16;
     }
-    const int steps_row = p.steps / p.pieces;
+    // what the loop reads of the parameters, once
+    const int pieces = p.pieces, steps_row = p.steps / pieces, chunks = p.chunks, shift_a = p.shift_a, shift_b = p.shift_b;
+    const uint32_t keep_a = p.keep_a, keep_b = p.keep_b;
+    const int64_t a_piece = p.a_piece;
     auto stage = [&](int step, int buf) {
-        const int q = p.pieces > 1 ? step / steps_row : 0, s = step - q * steps_row;
-        const int64_t off = (int64_t)s * 128, off_a = off + q * p.a_piece;
+        const int q = pieces > 1 ? step / steps_row : 0, s = step - q * steps_row;
+        const int64_t off = (int64_t)s * 128, off_a = off + q * a_piece;
         auto to_lds = [&](int i, const uint8_t* g) {
             uint8_t* l = &lds[buf][((i < LA ? i : i - LA) * THREADS + wave * 64) * 16 + (i < LA ? 0 : BM * 128)];
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)g,
                                              (__attribute__((address_space(3))) uint32_t*)l, 16, 0, 0);
         };
-        if (s * 8 + 8 <= p.chunks) {
+        if (s * 8 + 8 <= chunks) {
 #pragma unroll
             for (int i = 0; i < LA + LB; ++i) to_lds(i, src[i] + (i < LA ? off_a : off));
         } else {                                         // the rows end inside this step
-            const bool in = s * 8 + piece < p.chunks;
+            const bool in = s * 8 + piece < chunks;
 #pragma unroll
             for (int i = 0; i < LA + LB; ++i) to_lds(i, in ? src[i] + (i < LA ? off_a : off) : (const uint8_t*)lba_zero_piece);
         }
@@ -276,14 +301,22 @@ __global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int place = ((lane / 16) ^ ((lane & 15) >> 1)) * 16 + (lane & 15) * 128;
-    const int first = p.slices > 1 ? blockIdx.y * p.per_slice : 0;
+    const int first = slice * p.per_slice;
     const int last = p.slices > 1 ? (first + p.per_slice < p.steps ? first + p.per_slice : p.steps) : p.steps;
-    if (first < last) stage(first, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i)
+        if (first + i < last) stage(first + i, i);
+    int buf = 0;
+#pragma unroll 1
     for (int step = first; step < last; ++step) {
-        const int buf = (step - first) & 1;
-        if (step + 1 < last) stage(step + 1, buf ^ 1);
+        // This step's loads have to be done, those of the NST - 2 steps after it may be under way.  A step is LA + LB loads a wave or more,
+        // and loads end in order.
+        if (NST > 3 && step + 2 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (LA + LB)) : "memory");
+        else if (NST > 2 && step + 1 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA + LB) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();                    // every wave's loads of this step are done, and the step before is worked off
+        asm volatile("" ::: "memory");
+        if (step + NST - 1 < last) stage(step + NST - 1, buf == 0 ? NST - 1 : buf - 1);
         const uint8_t* la = &lds[buf][wm * FM * 2048 + place];
         const uint8_t* lb = &lds[buf][BM * 128 + wn * FN * 2048 + place];
         // the second piece of a row is 64 bytes on, modulo the row
@@ -305,23 +338,23 @@ __global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
                 for (int s = 0; s < 2; ++s) {
                     i32x4 fb[FN];
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j] = eight_codes<ELEM>((uint32_t)rb[j][2 * s], (uint32_t)rb[j][2 * s + 1], p.shift_b, p.keep_b);
+                    for (int j = 0; j < FN; ++j) fb[j] = eight_codes<ELEM>((uint32_t)rb[j][2 * s], (uint32_t)rb[j][2 * s + 1], shift_b, keep_b);
 #pragma unroll
                     for (int i = 0; i < FM; ++i) {
-                        const i32x4 fa = eight_codes<ELEM>((uint32_t)ra[i][2 * s], (uint32_t)ra[i][2 * s + 1], p.shift_a, p.keep_a);
+                        const i32x4 fa = eight_codes<ELEM>((uint32_t)ra[i][2 * s], (uint32_t)ra[i][2 * s + 1], shift_a, keep_a);
 #pragma unroll
                         for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(fb[j], fa, acc[i][j]);
                     }
                 }
             }
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        buf = buf == NST - 1 ? 0 : buf + 1;
     }
+    __syncthreads();
 
-    if (p.split) {                                       // one slice of the sum: raw, for the launch that adds the slices
+    if (p.slices > 1) {                                  // one slice of the sum: raw, for the launch that adds the slices
         const int mr = m0 + wm * FM * 16 + (lane & 15), nr = n0 + (GATED ? wn * FN * 8 : wn * FN * 16) + (lane / 16) * 4;
-        float* out = p.split + (int64_t)blockIdx.y * p.e.M * p.rows_b;
+        float* out = p.split + (int64_t)slice * p.e.M * p.rows_b;
         const CodeFmt none = {};
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -336,102 +369,154 @@ __global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
             }
         return;
     }
-    // The sums go through LDS, at most 64 rows of a wave at a time, so that neighbouring lanes have neighbouring columns: a wave works on
-    // its own part, without barriers.  Place of the four columns c of row r: (c / 4) ^ (r % CH), which spreads a column over the banks.
-    constexpr int EH = FM > 4 ? 4 : FM, CH = FN * 4, LPR = GATED ? CH / 2 : CH;      // rows of fragments, fours of a row, lanes of a row
-    constexpr int RPP = 64 / LPR, PASSES = EH * 16 / RPP, PB = PASSES < 4 ? PASSES : 4;      // rows of a pass, passes, passes of a batch
-    static_assert((PASSES == PB || PASSES % (2 * PB) == 0) && sizeof(lds) >= (size_t)WM * WN * EH * 16 * CH * 16, "epilogue");
+    // The sums go through LDS, at most 64 rows of a wave at a time, so that a lane has eight neighbouring columns and neighbouring lanes the next
+    // ones: a wave works on its own part, without barriers.  Place of the four columns c of row r: (c / 4) ^ (r % CH), which spreads a
+    // column over the banks.
+    constexpr int EH = FM == 8 ? 4 : FM == 6 ? 3 : FM, CH = FN * 4, LPR = GATED ? CH / 4 : CH / 2;   // rows of fragments, fours of a row, lanes of a row
+    constexpr int RPP = 64 / LPR, PASSES = EH * 16 / RPP;      // rows of a pass, passes
+    static_assert(PASSES >= 1 && FM / EH <= 2 && FM % EH == 0 && sizeof(lds) >= (size_t)WM * WN * EH * 16 * CH * 16, "epilogue");
     float* mine = (float*)&lds[0][0] + wave * (EH * 16 * CH * 4);
-    const uint64_t base = p.e.drop.threshold ? drop_base(p.e.drop) : 0;
-    const int quad = lane % LPR, row_in = lane / LPR;
-    const int cz = GATED ? quad / 4 * 8 + quad % 4 : quad;                           // its place in the row of sums
-    const int ncol = n0 + wn * (GATED ? FN * 8 : FN * 16) + quad * 4;
-    const Columns<GATED> cols = columns_of<GATED>(p.e, ncol);
-    const void* extra = EPI == EPI_FORWARD ? p.e.R : p.e.G;
-    const int extra_type = EPI == EPI_FORWARD ? p.e.r_type : p.e.g_type;
-    float sz[4] = {0.0f, 0.0f, 0.0f, 0.0f}, su[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const EpiParams e = p.e;
+    const uint64_t base = e.drop.threshold ? drop_base(e.drop) : 0;
+    const int oct = lane % LPR;
+    const int cz = GATED ? oct / 2 * 8 + oct % 2 * 2 : oct * 2;                      // the first of its two places in the row of sums
+    const int nw = n0 + wn * (GATED ? FN * 8 : FN * 16), ncol = nw + oct * 8;
+    const Columns<GATED, 8> cols = columns_of<GATED, 8>(e, ncol);
+    const void* extra = EPI == EPI_FORWARD ? e.R : e.G;
+    const int extra_type = EPI == EPI_FORWARD ? e.r_type : e.g_type;
+    float sz[8], su[8];
 #pragma unroll
-    for (int h = 0; h < FM / EH; ++h) {
-        const int mh = m0 + (wm * FM + h * EH) * 16;
-        float x[2][PB][4];            // a batch's residuals or gradients are on their way while the one before is worked on
-        if (extra) {
+    for (int k = 0; k < 8; ++k) sz[k] = su[k] = 0.0f;
+    auto get = [&](int r, int c, float (&v)[8]) {
 #pragma unroll
-            for (int q = 0; q < PB; ++q) load_extra(p.e, extra, extra_type, mh + q * RPP + row_in, ncol, x[0][q]);
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 x = *(const f32x4*)(mine + (r * CH + ((c + h) ^ (r % CH))) * 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[4 * h + k] = x[k];
         }
+    };
+    auto put = [&](int r, int c, const float (&v)[8]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *(f32x4*)(mine + (r * CH + ((c + h) ^ (r % CH))) * 4) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+    };
+#pragma unroll 1
+    for (int h = 0; h < FM / EH; ++h) {                  // one copy of the code for both halves
+        const int mh = m0 + (wm * FM + h * EH) * 16;
+        int l = lane;
+        asm volatile("" : "+v"(l));                      // addresses are made anew for each half: kept, they would cost the passes' registers
+        const int row_in = l / LPR;
 #pragma unroll
         for (int i = 0; i < EH; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const int r = i * 16 + (lane & 15), c = j * 4 + lane / 16;
-                *(f32x4*)(mine + (r * CH + (c ^ (r % CH))) * 4) = acc[h * EH + i][j];
+                const int r = i * 16 + (l & 15), c = j * 4 + l / 16;
+                *(f32x4*)(mine + (r * CH + (c ^ (r % CH))) * 4) = acc[i][j];
+                // the second half's sums move into the first's registers, which are free while the passes run
+                if (FM > EH) acc[i][j] = acc[FM > EH ? EH + i : i][j];
             }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int g = 0; g < PASSES; g += 2 * PB) {
+        // one pass: a lane's row r (m of the output, at index i; ip in the gradient matrix) with the residual's or gradient's values x
+        auto pass = [&](auto inside, auto act, int r, const At& i, const At& ip, const float (&x)[8]) {
+            constexpr bool INSIDE = decltype(inside)::value != 0;
+            const int m = mh + r;
+            float z[8], u[8];
+            get(r, cz, z);
+            if (GATED) get(r, cz + 4, u);
+            if constexpr (EPI == EPI_FORWARD) {
+                finish_forward<GATED, INSIDE, decltype(act)::value, 8>(e, cols, base, m, i, z, u, x);
+            } else {
+                finish_backward<GATED, INSIDE, decltype(act)::value, 8>(e, cols, base, m, i, z, u, x);
+                if (e.P && (INSIDE || (m < e.M && ncol < e.wide))) {              // wide and ncol are multiples of 8; zeros up to `wide`
+                    store_eight(e.P, ip, e.pieces, e.p_piece, z);
+                    if (GATED) store_eight(e.P + e.wide, ip, e.pieces, e.p_piece, u);
+                }
+                put(r, cz, z);
+                if (GATED) put(r, cz + 4, u);
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                if (PASSES > PB || part == 0) {
-                    const int g0 = g + part * PB;
-                    if (extra && g0 + PB < PASSES) {
-#pragma unroll
-                        for (int q = 0; q < PB; ++q) load_extra(p.e, extra, extra_type, mh + (g0 + PB + q) * RPP + row_in, ncol, x[part ^ 1][q]);
-                    }
-#pragma unroll
-                    for (int q = 0; q < PB; ++q) {
-                        const int r = (g0 + q) * RPP + row_in, m = mh + r;
-                        float* at = mine + (r * CH + (cz ^ (r % CH))) * 4;
-                        float* at2 = mine + (r * CH + ((cz + 4) ^ (r % CH))) * 4;
-                        float z[4], u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        const f32x4 vz = *(const f32x4*)at;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) z[k] = vz[k];
-                        if (GATED) {
-                            const f32x4 vu = *(const f32x4*)at2;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = vu[k];
-                        }
-                        if constexpr (EPI == EPI_FORWARD) {
-                            finish_forward<GATED>(p.e, cols, base, m, z, u, x[part][q]);
-                        } else {
-                            finish_backward<GATED>(p.e, cols, base, m, z, u, x[part][q]);
-                            store_gradient(p.e, m, ncol, 0, z);
-                            if (GATED) store_gradient(p.e, m, ncol, 1, u);
-                            *(f32x4*)at = f32x4{z[0], z[1], z[2], z[3]};
-                            if (GATED) *(f32x4*)at2 = f32x4{u[0], u[1], u[2], u[3]};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) { sz[k] += z[k]; su[k] += u[k]; }
-                        }
-                    }
+                for (int k = 0; k < 8; ++k) {
+                    sz[k] += z[k];
+                    if (GATED) su[k] += u[k];
                 }
             }
-        }
+        };
+        const int64_t u0 = (int64_t)mh * e.N + nw, up = mh * e.ldp + nw;
+        const uint32_t o0 = (uint32_t)(row_in * e.N + oct * 8), op = (uint32_t)(row_in * (int)e.ldp + oct * 8);
+        const uint32_t so = (uint32_t)(RPP * e.N), sp = (uint32_t)(RPP * (int)e.ldp);
+        // Wholly inside: the next pass's residuals or gradients are under way, as they are, before this one's results are stored: a load
+        // that follows stores waits for them too.
+        auto passes = [&](auto act) {
+            u32x4 raw[2][2];
+            auto fetch = [&](int g, u32x4 (&w)[2]) {
+                const At i = {u0, o0 + g * so};
+                if (extra && extra_type == LBA_F32) {
+                    w[0] = *(const u32x4_any*)at((const float*)extra, i);
+                    w[1] = *(const u32x4_any*)(at((const float*)extra, i) + 4);
+                } else if (extra) {
+                    w[0] = *(const u32x4_any*)at((const bf16_t*)extra, i);
+                }
+            };
+            auto work = [&](int g, const u32x4 (&w)[2]) {
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+                if (extra && extra_type == LBA_F32) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(w[k / 4][k % 4]);
+                } else if (extra) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(k % 2 ? w[0][k / 2] & 0xFFFF0000u : w[0][k / 2] << 16);
+                }
+                pass(Known<1>{}, act, g * RPP + row_in, At{u0, o0 + g * so}, At{up, op + g * sp}, x);
+            };
+            fetch(0, raw[0]);
+#pragma unroll 1
+            for (int g = 0; g < PASSES; g += 2) {
+                if (g + 1 < PASSES) fetch(g + 1, raw[1]);
+                work(g, raw[0]);
+                if (g + 1 < PASSES) {
+                    if (g + 2 < PASSES) fetch(g + 2, raw[0]);
+                    work(g + 1, raw[1]);
+                }
+            }
+        };
+        // The last rows and columns: what is beyond them reads as the last one and is not stored.
+        auto edge_passes = [&](auto act) {
+#pragma unroll 1
+            for (int g = 0; g < PASSES; ++g) {
+                const int r = g * RPP + row_in, m = mh + r;
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int64_t i = (int64_t)(m < e.M ? m : e.M - 1) * e.N + (ncol + k < e.N ? ncol + k : e.N - 1);
+                    x[k] = !extra ? 0.0f : extra_type == LBA_F32 ? ((const float*)extra)[i] : (float)((const bf16_t*)extra)[i];
+                }
+                pass(Known<0>{}, act, r, At{u0, o0 + g * so}, At{up, op + g * sp}, x);
+            }
+        };
+        const bool inside = mh + EH * 16 <= e.M && nw + LPR * 8 <= e.N;
+        const bool some = EPI == EPI_BACKWARD ? mh < up_to_8(e.M) && nw < e.wide : mh < e.M && nw < e.N;
+        with_act(e.act, [&](auto act) {
+            if (inside) passes(act);
+            else if (some) edge_passes(act);
+        });
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if constexpr (EPI == EPI_BACKWARD) {
-            if (p.e.PT) {                                // the transposed copy: eight rows of one column a lane
+            if (e.PT && mh < e.ldt && nw < e.N) {        // the transposed copy: eight rows of one column a lane
                 constexpr int LM = EH * 2, NPP = 64 / LM;                            // lanes along m, columns of a pass
                 const int r0 = (lane % LM) * 8, m = mh + r0;
 #pragma unroll 1
                 for (int c0 = 0; c0 < CH * 4; c0 += NPP) {
                     const int c = c0 + lane / LM;
-                    const int n = n0 + wn * (GATED ? FN * 8 : FN * 16) + (GATED ? c / 32 * 16 + c % 16 : c);
+                    const int n = nw + (GATED ? c / 32 * 16 + c % 16 : c);
                     const int half = GATED ? c / 16 % 2 : 0;
-                    typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-                    u16x8 w[3];
+                    float d[8];
+                    if (lane < LM * NPP && c < CH * 4 && n < e.N && m < e.ldt) {     // ldt and m are multiples of 8: zeros beyond M are part of the copy
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int r = r0 + k;
-                        bf16_t b[3];
-                        bf16_pieces(mine[(r * CH + ((c / 4) ^ (r % CH))) * 4 + c % 4], p.e.pieces, b);
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) w[q][k] = __builtin_bit_cast(uint16_t, b[q]);
-                    }
-                    if (n < p.e.N && m < p.e.ldt) {      // ldt and m are multiples of 8: zeros beyond M are part of the copy
-                        bf16_t* at = p.e.PT + ((int64_t)half * p.e.N + n) * p.e.ldt + m;
-#pragma unroll
-                        for (int q = 0; q < 3; ++q)
-                            if (q < p.e.pieces) *(u16x8*)(at + q * p.e.pt_piece) = w[q];
+                        for (int k = 0; k < 8; ++k) d[k] = mine[((r0 + k) * CH + ((c / 4) ^ ((r0 + k) % CH))) * 4 + c % 4];
+                        const At it = {((int64_t)half * e.N + n) * e.ldt + m, 0};
+                        store_eight(e.PT, it, e.pieces, e.pt_piece, d);
                     }
                 }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -440,28 +525,32 @@ __global__ __launch_bounds__(WM * WN * 64) void dense_kernel(GemmParams p) {
         }
     }
     if constexpr (EPI == EPI_BACKWARD) {
-        if (p.e.part) {                                  // column sums of the wave's rows: over the lanes that share a column
+        if (e.part) {                                    // column sums of the wave's rows: over the lanes that share a column
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) {
 #pragma unroll
                 for (int d = LPR; d < 64; d *= 2) {
                     sz[k] += __shfl_xor(sz[k], d);
                     if (GATED) su[k] += __shfl_xor(su[k], d);
                 }
             }
-            if (row_in == 0 && ncol < p.e.N) {
-                float* out = p.e.part + (int64_t)(tm * WM + wm) * (GATED ? 2 * p.e.N : p.e.N);
-                store_some<4>(out + ncol, p.e.N - ncol, sz, p.e.fmt);
-                if (GATED) store_some<4>(out + p.e.N + ncol, p.e.N - ncol, su, p.e.fmt);
+            if (lane < LPR && ncol < e.N) {
+                float* out = e.part + (int64_t)(tm * WM + wm) * (GATED ? 2 * e.N : e.N);
+                store_some<8>(out + ncol, e.N - ncol, sz, e.fmt);
+                if (GATED) store_some<8>(out + e.N + ncol, e.N - ncol, su, e.fmt);
             }
         }
     }
 }
 
-// tiles: rows of outputs, columns of B and waves over m
-enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2 };
+// Tiles: rows of outputs, columns of B, waves over m and buffers.  The deep ones have four buffers, for grids that leave CUs to themselves: with
+// two, a step of a workgroup alone waits for its loads.
+enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5 };
 struct TileShape { int bm, bn, wm; };
-inline TileShape tile_shape(int tile) { return tile == TILE_256 ? TileShape{256, 256, 2} : tile == TILE_128 ? TileShape{128, 128, 2} : TileShape{64, 64, 2}; }
+inline TileShape tile_shape(int tile) {
+    static const TileShape all[] = {{256, 256, 2}, {128, 128, 2}, {64, 64, 2}, {192, 256, 2}, {128, 128, 2}, {64, 64, 2}};
+    return all[tile];
+}
 
 // code -> value at the canonical bias 2^(E-1) - 1, exact (at most 6 significant bits: a bfloat16 number)
 struct CodeBits { int32_t sh; uint32_t exp0, sub; float two; };   // 23 - M, (127 - bias) << 23, 1 << M, 2^(1 - bias)
@@ -487,7 +576,7 @@ __device__ __forceinline__ void code_bf16(uint32_t w, const CodeBits& b, uint32_
 struct ElemFmt { int elem, shift; uint32_t keep; float factor; };
 inline ElemFmt make_elem(const lba_infmt& f, int elem) {
     const int bc = (1 << (f.exp_bits - 1)) - 1;
-    ElemFmt e = {elem, f.man_bits - 2, (0x7Fu << (10 - f.man_bits)) * 0x10001u, 0.0f};
+    ElemFmt e = {elem, f.man_bits - 2, (0x8000u | 0x7Fu << (10 - f.man_bits)) * 0x10001u, 0.0f};
     e.factor = __builtin_ldexpf(1.0f, elem == ELEM_F16 ? 15 - f.bias : bc - f.bias);
     return e;
 }
@@ -509,27 +598,41 @@ struct TokenParams {
 };
 void launch_dense_token(const TokenParams& p, int elem, bool gated, hipStream_t st);
 
-// launches a product whose parameters are complete but for the grid
-void launch_dense_e4m3(GemmParams& p, int tile, bool gated, int epi, hipStream_t st);
-void launch_dense_f16(GemmParams& p, int tile, bool gated, int epi, hipStream_t st);
-void launch_dense_bf16(GemmParams& p, int tile, bool gated, int epi, hipStream_t st);
+// launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape
+void launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+void launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+void launch_dense_bf16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
 
-template <int ELEM> void launch_dense(GemmParams& p, int tile, bool gated, int epi, hipStream_t st) {
-    const TileShape s = tile_shape(tile);
+inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     p.gx = (p.e.M + s.bm - 1) / s.bm;
     p.gy = gated ? (p.half + s.bn / 2 - 1) / (s.bn / 2) : (p.rows_b + s.bn - 1) / s.bn;
-    const dim3 grid((unsigned)(p.gx * p.gy), (unsigned)(p.slices > 1 ? p.slices : 1));
-#define LBA_DENSE(TILE, WM, WN, FM, FN, GATED, EPI) \
+    return p.gx * p.gy * (p.slices > 1 ? p.slices : 1);
+}
+
+template <int ELEM> void launch_dense(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
+    const TileShape s = tile_shape(tile);
+    GemmPair pair;
+    pair.g[0] = a;
+    pair.g[1] = b ? *b : a;
+    pair.blocks = dense_grid(pair.g[0], s, gated);
+    const dim3 grid((unsigned)(pair.blocks + (b ? dense_grid(pair.g[1], s, gated) : 0)));
+#define LBA_DENSE(TILE, WM, WN, FM, FN, NST, GATED, EPI) \
     if (tile == TILE && gated == GATED && epi == EPI) { \
-        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, p); \
+        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \
         return; \
     }
 #define LBA_DENSE_TILES(GATED, EPI) \
-    LBA_DENSE(TILE_256, 2, 4, 8, 4, GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, GATED, EPI)
+    LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, GATED, EPI) \
+    LBA_DENSE(TILE_128_DEEP, 2, 2, 4, 4, 4, GATED, EPI) LBA_DENSE(TILE_64_DEEP, 2, 2, 2, 2, 4, GATED, EPI)
+#define LBA_DENSE_LARGE(GATED) \
+    LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, GATED, EPI_FORWARD)
     LBA_DENSE_TILES(false, EPI_FORWARD)
     LBA_DENSE_TILES(true, EPI_FORWARD)
+    LBA_DENSE_LARGE(false)
+    LBA_DENSE_LARGE(true)
     LBA_DENSE_TILES(false, EPI_BACKWARD)
     LBA_DENSE_TILES(true, EPI_BACKWARD)
+#undef LBA_DENSE_LARGE
 #undef LBA_DENSE_TILES
 #undef LBA_DENSE
 }

@@ -11,61 +11,60 @@ constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // ---- operands laid out for the tile ---------------------------------------------------------
 
-struct RowsParams {
+// One launch lays out up to five operands: workgroups from `first` on belong to a job.
+enum { LAY_CODES = 0, LAY_BF16 = 1, LAY_TRANSPOSED = 2 };
+struct LayJob {
     const uint8_t* src;      // [R, K] codes
-    uint8_t* dst;            // rows of ld bytes, zeros behind K
-    int64_t R, ld;
+    uint8_t* dst;
+    int64_t R;
+    int64_t ld;              // bytes of a row of dst
     int32_t K;
+    int32_t wide;            // LAY_TRANSPOSED: R rounded up to 8: columns of dst, zeros from R on
+    int32_t tiles_k;         // LAY_TRANSPOSED: tiles of 64 along k
+    int32_t kind;
+    uint32_t first;
     CodeBits bits;
 };
+struct LayJobs { LayJob job[5]; int32_t n; };
 
-// 16 bytes of output a lane: codes as they are, or as bfloat16 numbers
-template <bool BF16> __global__ __launch_bounds__(256) void dense_rows_kernel(RowsParams p) {
+// rows of codes or of bfloat16 numbers, zeros behind K: 16 bytes of output a lane
+template <bool BF16> __device__ __forceinline__ void lay_rows(const LayJob& p, int64_t block) {
     constexpr int PER = BF16 ? 8 : 16;
-    const int64_t per_row = p.ld / 16, total = p.R * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per_row;
-        const int k = (int)(i - r * per_row) * PER;
-        const uint8_t* s = p.src + r * p.K + k;
-        uint32_t w[PER / 4];
-        if (k + PER <= p.K) {
-            typedef uint32_t words __attribute__((ext_vector_type(PER / 4), aligned(1)));
-            const words x = *(const words*)s;
+    const int64_t per_row = p.ld / 16, i = block * 256 + threadIdx.x;
+    if (i >= p.R * per_row) return;
+    const int64_t r = i / per_row;
+    const int k = (int)(i - r * per_row) * PER;
+    const uint8_t* s = p.src + r * p.K + k;
+    uint32_t w[PER / 4];
+    if (k + PER <= p.K) {
+        typedef uint32_t words __attribute__((ext_vector_type(PER / 4), aligned(1)));
+        const words x = *(const words*)s;
 #pragma unroll
-            for (int j = 0; j < PER / 4; ++j) w[j] = x[j];
-        } else {
+        for (int j = 0; j < PER / 4; ++j) w[j] = x[j];
+    } else {
 #pragma unroll
-            for (int j = 0; j < PER / 4; ++j) w[j] = 0;
+        for (int j = 0; j < PER / 4; ++j) w[j] = 0;
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
-        }
-        i32x4 o;
-        if (BF16) {
-            uint32_t lo, hi;
-            code_bf16(w[0], p.bits, lo, hi); o[0] = (int32_t)lo; o[1] = (int32_t)hi;
-            code_bf16(w[1], p.bits, lo, hi); o[2] = (int32_t)lo; o[3] = (int32_t)hi;
-        } else {
-            for (int j = 0; j < 4; ++j) o[j] = (int32_t)w[j % (PER / 4)];
-        }
-        *(i32x4*)(p.dst + r * p.ld + (int64_t)(i - r * per_row) * 16) = o;
+        for (int j = 0; j < PER; ++j)
+            if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
     }
+    i32x4 o;
+    if constexpr (BF16) {
+        uint32_t lo, hi;
+        code_bf16(w[0], p.bits, lo, hi); o[0] = (int32_t)lo; o[1] = (int32_t)hi;
+        code_bf16(w[1], p.bits, lo, hi); o[2] = (int32_t)lo; o[3] = (int32_t)hi;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = (int32_t)w[j];
+    }
+    *(i32x4*)(p.dst + r * p.ld + (i - r * per_row) * 16) = o;
 }
 
-struct TransposedParams {
-    const uint8_t* src;      // [R, K] codes
-    bf16_t* dst;             // [K][ld], R columns and zeros up to `wide`, a multiple of 8
-    int64_t R, ld, wide;
-    int32_t K;
-    int32_t tiles_k;
-    CodeBits bits;
-};
-
-// 64 x 64 codes through LDS: read along k, written along the rows as bfloat16
-__global__ __launch_bounds__(256) void dense_transposed_kernel(TransposedParams p) {
+// dst [K][ld] bfloat16: 64 x 64 codes through LDS, read along k, written along the rows
+__device__ __forceinline__ void lay_transposed(const LayJob& p, int64_t block) {
     __shared__ uint8_t t[64][68];
-    const int64_t r0 = (int64_t)(blockIdx.x / p.tiles_k) * 64;
-    const int k0 = (int)(blockIdx.x % p.tiles_k) * 64;
+    const int64_t r0 = block / p.tiles_k * 64;
+    const int k0 = (int)(block % p.tiles_k) * 64;
     for (int i = threadIdx.x; i < 64 * 16; i += 256) {
         const int r = i / 16, k = (i % 16) * 4;
         uint32_t w = 0;
@@ -89,52 +88,77 @@ __global__ __launch_bounds__(256) void dense_transposed_kernel(TransposedParams 
             const uint32_t a = __float_as_uint(code_value(t[r + 2 * j][k], p.bits)), b = __float_as_uint(code_value(t[r + 2 * j + 1][k], p.bits));
             o[j] = (int32_t)__builtin_amdgcn_perm(b, a, 0x07060302u);
         }
-        *(i32x4*)(p.dst + (int64_t)(k0 + k) * p.ld + r0 + r) = o;
+        *(i32x4*)(p.dst + (k0 + k) * p.ld + (r0 + r) * 2) = o;
     }
 }
 
-// adds the slices of a product's sums, in order, and finishes the outputs
-template <bool GATED> __global__ __launch_bounds__(256) void dense_join_kernel(EpiParams e, const float* split, int32_t slices, int32_t cols) {
-    const int64_t quads = (e.N + 3) / 4, total = quads * e.M, plane = (int64_t)e.M * cols;
+__global__ __launch_bounds__(256) void dense_lay_kernel(LayJobs jobs) {
+    int j = 0;
+    while (j + 1 < jobs.n && blockIdx.x >= jobs.job[j + 1].first) ++j;
+    const LayJob& p = jobs.job[j];
+    const int64_t block = blockIdx.x - p.first;
+    if (p.kind == LAY_CODES) lay_rows<false>(p, block);
+    else if (p.kind == LAY_BF16) lay_rows<true>(p, block);
+    else lay_transposed(p, block);
+}
+
+// adds the slices of a product's sums, in order, and finishes the outputs: of one product or of two
+struct JoinPart { EpiParams e; const float* split; int32_t slices, cols; };
+struct JoinPair { JoinPart p[2]; int32_t blocks; };
+template <bool GATED> __global__ __launch_bounds__(256) void dense_join_kernel(JoinPair both) {
+    const bool second = (int)blockIdx.x >= both.blocks;
+    const JoinPart& p = both.p[second];
+    const EpiParams& e = p.e;
+    const int64_t first = second ? (int64_t)blockIdx.x - both.blocks : (int64_t)blockIdx.x, blocks = second ? (int64_t)gridDim.x - both.blocks : (int64_t)both.blocks;
+    const int64_t quads = (e.N + 3) / 4, total = quads * e.M, plane = (int64_t)e.M * p.cols;
     const uint64_t base = e.drop.threshold ? drop_base(e.drop) : 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = first * 256 + threadIdx.x; i < total; i += blocks * 256) {
         const int64_t m = i / quads;
         const int n = (int)(i - m * quads) * 4;
-        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4];
-        const float* s = split + m * cols + n;
-        for (int q = 0; q < slices; ++q) {
+        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f}, r[4], v[4], w[4];
+        const float* s = p.split + m * p.cols + n;
+        load_extra<4>(e, (int)m, n, r);
+#pragma unroll 4
+        for (int q = 0; q < p.slices; ++q) {
             load_some<4>(s + q * plane, e.N - n, v);
+            if (GATED) load_some<4>(s + q * plane + e.N, e.N - n, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[j] += v[j];
-            if (GATED) {
-                load_some<4>(s + q * plane + e.N, e.N - n, v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) u[j] += v[j];
+            for (int j = 0; j < 4; ++j) {
+                z[j] += v[j];
+                if (GATED) u[j] += w[j];
             }
         }
-        float r[4];
-        load_extra(e, e.R, e.r_type, (int)m, n, r);
-        finish_forward<GATED>(e, columns_of<GATED>(e, n), base, (int)m, z, u, r);
+        with_act(e.act, [&](auto act) { finish_forward<GATED, false, decltype(act)::value, 4>(e, columns_of<GATED, 4>(e, n), base, (int)m, At{m * e.N + n, 0}, z, u, r); });
     }
 }
 
 // ---- plan -----------------------------------------------------------------------------------
 
-static unsigned grid_of(int64_t items) {
-    const int64_t blocks = (items + 255) / 256;
-    return (unsigned)(blocks < 1 ? 1 : blocks < 65536 ? blocks : 65536);
+static int32_t join_blocks(const EpiParams& e) {
+    const int64_t blocks = ((int64_t)e.M * ((e.N + 3) / 4) + 255) / 256;
+    return (int32_t)(blocks < 16384 ? blocks : 16384);
 }
 
-// tile and slices of a product of rows x cols outputs over `steps` steps
-struct TilePlan { int tile, slices, per_slice; int64_t split_floats; };
-static TilePlan plan_tile(int64_t rows, int64_t cols, bool gated, int64_t steps, bool may_split) {
-    (void)may_split;
-    TilePlan t = {TILE_64, 1, (int)steps, 0};
-    const int64_t c = gated ? cols / 2 * 2 : cols;
-    auto tiles = [&](int b) { return ((rows + b - 1) / b) * ((c + b - 1) / b); };
-    if (tiles(256) >= 192) t.tile = TILE_256;
-    else if (tiles(128) >= 192) t.tile = TILE_128;
-    return t;
+// A product of rows x cols outputs over `steps` steps, and how it is cut.
+struct Product { int64_t rows, cols, steps; int slices; int64_t per_slice; };
+static int64_t tiles_of(const Product& p, int tile) {
+    const TileShape s = tile_shape(tile);
+    return ((p.rows + s.bm - 1) / s.bm) * ((p.cols + s.bn - 1) / s.bn);
+}
+static void cut(Product& p, int64_t slices) {
+    p.per_slice = (p.steps + slices - 1) / slices;
+    p.slices = p.per_slice > 0 ? (int)((p.steps + p.per_slice - 1) / p.per_slice) : 1;
+    if (p.slices < 1) p.slices = 1;
+}
+static size_t split_bytes(const Product& p) { return p.slices > 1 ? align256((size_t)(p.slices * p.rows * p.cols) * 4) : 0; }
+
+// chooses the tile of a product, or of two that share a launch, and their slices
+static int plan_tile(Product* p, int n, bool may_slice) {
+    (void)may_slice;
+    for (int i = 0; i < n; ++i) cut(p[i], 1);
+    int64_t t256 = 0, t128 = 0;
+    for (int i = 0; i < n; ++i) { t256 += tiles_of(p[i], TILE_256); t128 += tiles_of(p[i], TILE_128); }
+    return t256 >= 192 && may_slice ? TILE_256 : t128 >= 192 ? TILE_128 : TILE_64;
 }
 
 static int check_infmt(const lba_infmt& f) {
@@ -152,7 +176,8 @@ struct DensePlan {
     int64_t cols;            // rows of B
     int64_t ld;              // bytes of a laid-out row
     int64_t steps, chunks;
-    TilePlan fwd;
+    Product fwd;
+    int tile;
     size_t copy_a, copy_b, split, bytes;
 };
 
@@ -170,8 +195,9 @@ static DensePlan plan_forward(int64_t M, int64_t N, int64_t K, const lba_infmt& 
         d.copy_a = at; at += align256((size_t)(M * d.ld));
         d.copy_b = at; at += align256((size_t)(d.cols * d.ld));
     }
-    d.fwd = plan_tile(M, d.cols, gated, d.steps, true);
-    d.split = at; at += align256((size_t)d.fwd.split_floats * 4);
+    d.fwd = {M, d.cols, d.steps, 1, d.steps};
+    d.tile = plan_tile(&d.fwd, 1, true);
+    d.split = at; at += split_bytes(d.fwd);
     d.bytes = d.token ? 0 : at;
     return d;
 }
@@ -181,9 +207,10 @@ struct BwdPlan {
     bool sums;               // whether they are
     int pieces;
     int64_t ldp, ldt;        // elements of a row of the gradient matrix and of its transpose
-    TilePlan da, db;
+    Product out[2];          // dA and dB, in one launch
+    int tile;
     int64_t part_rows;
-    size_t p, pt, at, bt, part, split, bytes;
+    size_t p, pt, at, bt, part, split_a, split_b, bytes;
 };
 
 static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, int act, int g_type, bool aligned) {
@@ -194,7 +221,7 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
     // the sums again, always by the tile: few rows as well
     f.token = false;
     f.in_place = f.elem != ELEM_BF16 && K % 16 == 0 && aligned;
-    f.fwd = plan_tile(M, f.cols, gated, f.steps, false);
+    f.tile = plan_tile(&f.fwd, 1, false);
     size_t at = 0;
     if (b.sums && !f.in_place) {
         f.copy_a = at; at += align256((size_t)(M * f.ld));
@@ -207,49 +234,53 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
     b.pt = at; at += align256((size_t)(b.pieces * f.cols * b.ldt) * 2);
     b.at = at; at += align256((size_t)(K * b.ldt) * 2);
     b.bt = at; at += align256((size_t)(K * b.ldp) * 2);
-    const TileShape s = tile_shape(f.fwd.tile);
+    const TileShape s = tile_shape(f.tile);
     b.part_rows = (M + s.bm - 1) / s.bm * s.wm;
     b.part = at; at += align256((size_t)(b.part_rows * f.cols) * 4);
-    b.da = plan_tile(M, K, false, (b.ldp * 2 + 127) / 128 * b.pieces, true);
-    b.db = plan_tile(f.cols, K, false, (b.ldt * 2 + 127) / 128 * b.pieces, true);
-    const int64_t most = b.da.split_floats > b.db.split_floats ? b.da.split_floats : b.db.split_floats;
-    b.split = at; at += align256((size_t)most * 4);
+    b.out[0] = {M, K, (b.ldp * 2 + 127) / 128 * b.pieces, 1, 0};
+    b.out[1] = {f.cols, K, (b.ldt * 2 + 127) / 128 * b.pieces, 1, 0};
+    b.tile = plan_tile(b.out, 2, true);
+    b.split_a = at; at += split_bytes(b.out[0]);
+    b.split_b = at; at += split_bytes(b.out[1]);
     b.bytes = at;
     return b;
 }
 
-static bool fits_a_launch(int64_t rows, int64_t cols, const TilePlan& t) {
-    const TileShape s = tile_shape(t.tile);
-    const int64_t tiles = ((rows + s.bm - 1) / s.bm) * ((cols + s.bn / 2 - 1) / (s.bn / 2));
-    return tiles < ((int64_t)1 << 22);                   // fewer than 2^32 lanes
+static bool fits_a_launch(const Product* p, int n, int tile) {
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) tiles += tiles_of(p[i], tile) * p[i].slices;
+    return 2 * tiles < ((int64_t)1 << 22);               // fewer than 2^32 lanes; a gated product's half tiles may be one more column
 }
 
-static void lay_rows(const uint8_t* src, uint8_t* dst, int64_t R, int64_t K, int64_t ld, int elem, const lba_infmt& f, hipStream_t st) {
-    if (R == 0 || ld == 0) return;
-    RowsParams p = {src, dst, R, ld, (int32_t)K, make_code_bits(f)};
-    const dim3 grid(grid_of(R * (ld / 16)));
-    if (elem != ELEM_BF16) hipLaunchKernelGGL(dense_rows_kernel<false>, grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL(dense_rows_kernel<true>, grid, dim3(256), 0, st, p);
+static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* dst, int64_t R, int64_t K, int64_t ld, int kind, const lba_infmt& f) {
+    if (R == 0 || K == 0) return;
+    LayJob& j = jobs.job[jobs.n++];
+    j.src = src; j.dst = (uint8_t*)dst; j.R = R; j.ld = ld; j.K = (int32_t)K; j.kind = kind; j.first = blocks; j.bits = make_code_bits(f);
+    j.wide = (int32_t)up_to(R, 8);
+    j.tiles_k = (int32_t)((K + 63) / 64);
+    blocks += (uint32_t)(kind == LAY_TRANSPOSED ? j.tiles_k * ((R + 63) / 64) : (R * (ld / 16) + 255) / 256);
 }
+// a job's workgroups take 2048 codes or more: five jobs stay under 2^32 lanes
+static bool lay_fits(int64_t R, int64_t K) { return (R + 64) * (K + 64) <= ((int64_t)1 << 32); }
 
-static void lay_transposed(const uint8_t* src, bf16_t* dst, int64_t R, int64_t K, int64_t ld, const lba_infmt& f, hipStream_t st) {
-    if (K == 0 || ld == 0) return;
-    TransposedParams p = {src, dst, R, ld, up_to(R, 8), (int32_t)K, (int32_t)((K + 63) / 64), make_code_bits(f)};
-    hipLaunchKernelGGL(dense_transposed_kernel, dim3((unsigned)(p.tiles_k * ((R + 63) / 64))), dim3(256), 0, st, p);
-}
-
-static void run_product(GemmParams& g, const TilePlan& t, int elem, bool gated, int epi, float* split, hipStream_t st) {
-    g.slices = t.slices;
-    g.per_slice = t.per_slice;
-    g.split = t.slices > 1 ? split : nullptr;
-    if (elem == ELEM_E4M3) launch_dense_e4m3(g, t.tile, gated, epi, st);
-    else if (elem == ELEM_F16) launch_dense_f16(g, t.tile, gated, epi, st);
-    else launch_dense_bf16(g, t.tile, gated, epi, st);
-    if (t.slices > 1) {
-        const dim3 grid(grid_of((int64_t)g.e.M * ((g.e.N + 3) / 4)));
-        if (gated) hipLaunchKernelGGL(dense_join_kernel<true>, grid, dim3(256), 0, st, g.e, split, t.slices, g.rows_b);
-        else hipLaunchKernelGGL(dense_join_kernel<false>, grid, dim3(256), 0, st, g.e, split, t.slices, g.rows_b);
+// one product, or two that share a launch
+static void run_products(GemmParams* g, const Product* p, int n, int tile, int elem, bool gated, int epi, hipStream_t st) {
+    JoinPair join = {};
+    int sliced = 0;
+    for (int i = 0; i < n; ++i) {
+        g[i].slices = p[i].slices;
+        g[i].per_slice = (int32_t)p[i].per_slice;
+        if (p[i].slices > 1) join.p[sliced++] = {g[i].e, g[i].split, p[i].slices, g[i].rows_b};
     }
+    const GemmParams* second = n > 1 ? &g[1] : nullptr;
+    if (elem == ELEM_E4M3) launch_dense_e4m3(g[0], second, tile, gated, epi, st);
+    else if (elem == ELEM_F16) launch_dense_f16(g[0], second, tile, gated, epi, st);
+    else launch_dense_bf16(g[0], second, tile, gated, epi, st);
+    if (!sliced) return;
+    join.blocks = join_blocks(join.p[0].e);
+    const dim3 grid((unsigned)(join.blocks + (sliced > 1 ? join_blocks(join.p[1].e) : 0)));
+    if (gated) hipLaunchKernelGGL(dense_join_kernel<true>, grid, dim3(256), 0, st, join);
+    else hipLaunchKernelGGL(dense_join_kernel<false>, grid, dim3(256), 0, st, join);
 }
 
 static int check_workspace(const void* ws, size_t have, size_t need) {
@@ -286,7 +317,7 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
     if (!Y || (K > 0 && (!A || !B))) return LBA_ERR_NULL;
     const bool two = gated != 0;
     const DensePlan d = plan_forward(M, N, K, fmt_a, fmt_b, two, aligned16(A, B));
-    if (!d.token && !fits_a_launch(M, d.cols, d.fwd)) return LBA_ERR_SHAPE;
+    if (!d.token && (!fits_a_launch(&d.fwd, 1, d.tile) || (!d.in_place && (!lay_fits(M, K) || !lay_fits(d.cols, K))))) return LBA_ERR_SHAPE;
     rc = check_workspace(workspace, workspace_bytes, d.bytes);
     if (rc != LBA_OK) return rc;
     const ElemFmt ea = make_elem(fmt_a, d.elem), eb = make_elem(fmt_b, d.elem);
@@ -304,15 +335,20 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
     GemmParams g = {};
     g.A = A; g.B = B; g.lda = g.ldb = d.ld;
     if (!d.in_place) {
-        lay_rows(A, ws + d.copy_a, M, K, d.ld, d.elem, fmt_a, st);
-        lay_rows(B, ws + d.copy_b, d.cols, K, d.ld, d.elem, fmt_b, st);
+        LayJobs jobs = {};
+        uint32_t blocks = 0;
+        const int kind = d.elem == ELEM_BF16 ? LAY_BF16 : LAY_CODES;
+        add_job(jobs, blocks, A, ws + d.copy_a, M, K, d.ld, kind, fmt_a);
+        add_job(jobs, blocks, B, ws + d.copy_b, d.cols, K, d.ld, kind, fmt_b);
+        if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
         g.A = ws + d.copy_a; g.B = ws + d.copy_b;
     }
     g.pieces = 1; g.rows_a = (int32_t)M; g.rows_b = (int32_t)d.cols; g.half = (int32_t)N;
     g.chunks = (int32_t)d.chunks; g.steps = (int32_t)d.steps;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
-    run_product(g, d.fwd, d.elem, two, EPI_FORWARD, (float*)(ws + d.split), st);
+    g.split = (float*)(ws + d.split);
+    run_products(&g, &d.fwd, 1, d.tile, d.elem, two, EPI_FORWARD, st);
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 
@@ -343,7 +379,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     }
     const BwdPlan b = plan_backward(M, N, K, fmt_a, fmt_b, two, act, g_type, aligned16(A, B));
     if (!G || (K > 0 && (((dA || b.sums) && !B) || ((dB || b.sums) && !A)))) return LBA_ERR_NULL;
-    if (!fits_a_launch(M, cols, b.f.fwd) || !fits_a_launch(M, K, b.da) || !fits_a_launch(cols, K, b.db)) return LBA_ERR_SHAPE;
+    if (!fits_a_launch(&b.f.fwd, 1, b.f.tile) || !fits_a_launch(b.out, 2, b.tile) || !lay_fits(M, K) || !lay_fits(cols, K)) return LBA_ERR_SHAPE;
     rc = check_workspace(workspace, workspace_bytes, b.bytes);
     if (rc != LBA_OK) return rc;
     uint8_t* ws = (uint8_t*)workspace;
@@ -360,41 +396,54 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     e.part = dbias ? (float*)(ws + b.part) : nullptr;
     GemmParams g = {};
     g.A = A; g.B = B; g.lda = g.ldb = b.f.ld;
+    const int32_t wide = (int32_t)up_to(N, 8);
+    LayJobs jobs = {};
+    uint32_t blocks = 0;
     if (b.sums && !b.f.in_place) {
-        lay_rows(A, ws + b.f.copy_a, M, K, b.f.ld, b.f.elem, fmt_a, st);
-        lay_rows(B, ws + b.f.copy_b, cols, K, b.f.ld, b.f.elem, fmt_b, st);
+        const int kind = b.f.elem == ELEM_BF16 ? LAY_BF16 : LAY_CODES;
+        add_job(jobs, blocks, A, ws + b.f.copy_a, M, K, b.f.ld, kind, fmt_a);
+        add_job(jobs, blocks, B, ws + b.f.copy_b, cols, K, b.f.ld, kind, fmt_b);
         g.A = ws + b.f.copy_a; g.B = ws + b.f.copy_b;
     }
+    if (dA) {
+        add_job(jobs, blocks, B, ws + b.bt, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
+        if (two) add_job(jobs, blocks, B + N * K, ws + b.bt + wide * 2, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
+    }
+    if (dB) add_job(jobs, blocks, A, ws + b.at, M, K, b.ldt * 2, LAY_TRANSPOSED, fmt_a);
+    if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
     g.pieces = 1; g.rows_a = (int32_t)M; g.rows_b = (int32_t)cols; g.half = (int32_t)N;
     g.chunks = b.sums ? (int32_t)b.f.chunks : 0; g.steps = b.sums ? (int32_t)b.f.steps : 0;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
-    run_product(g, b.f.fwd, b.f.elem, two, EPI_BACKWARD, nullptr, st);
+    run_products(&g, &b.f.fwd, 1, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
     if (dbias) launch_column_sum(e.part, b.part_rows, cols, dbias, nullptr, cols, st);
 
     // the two products of it
-    EpiParams o = {};
-    o.y_type = g_type;
-    GemmParams q = {};
-    q.pieces = b.pieces;
-    q.rows_b = (int32_t)K; q.half = (int32_t)K;
-    if (dA && K > 0) {
-        lay_transposed(B, (bf16_t*)(ws + b.bt), N, K, b.ldp, fmt_b, st);
-        if (two) lay_transposed(B + N * K, (bf16_t*)(ws + b.bt) + e.wide, N, K, b.ldp, fmt_b, st);
-        q.A = (const uint8_t*)P; q.B = ws + b.bt; q.lda = q.ldb = b.ldp * 2; q.a_piece = e.p_piece * 2;
-        q.rows_a = (int32_t)M; q.chunks = (int32_t)(b.ldp / 8); q.steps = (int32_t)((b.ldp * 2 + 127) / 128 * b.pieces);
-        o.scale = make_elem(fmt_b, ELEM_BF16).factor; o.M = (int32_t)M; o.N = (int32_t)K; o.Y = dA;
-        q.e = o;
-        run_product(q, b.da, ELEM_BF16, false, EPI_FORWARD, (float*)(ws + b.split), st);
+    if (K == 0 || (!dA && !dB)) return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+    GemmParams q[2] = {};
+    Product parts[2];
+    int n = 0;
+    if (dA) {
+        GemmParams& a = q[n];
+        a.A = (const uint8_t*)P; a.B = ws + b.bt; a.lda = a.ldb = b.ldp * 2; a.a_piece = e.p_piece * 2;
+        a.rows_a = (int32_t)M; a.chunks = (int32_t)(b.ldp / 8); a.split = (float*)(ws + b.split_a);
+        a.e.scale = make_elem(fmt_b, ELEM_BF16).factor; a.e.M = (int32_t)M; a.e.Y = dA;
+        parts[n++] = b.out[0];
     }
-    if (dB && K > 0) {
-        lay_transposed(A, (bf16_t*)(ws + b.at), M, K, b.ldt, fmt_a, st);
-        q.A = (const uint8_t*)PT; q.B = ws + b.at; q.lda = q.ldb = b.ldt * 2; q.a_piece = e.pt_piece * 2;
-        q.rows_a = (int32_t)cols; q.chunks = (int32_t)(b.ldt / 8); q.steps = (int32_t)((b.ldt * 2 + 127) / 128 * b.pieces);
-        o.scale = make_elem(fmt_a, ELEM_BF16).factor; o.M = (int32_t)cols; o.N = (int32_t)K; o.Y = dB;
-        q.e = o;
-        run_product(q, b.db, ELEM_BF16, false, EPI_FORWARD, (float*)(ws + b.split), st);
+    if (dB) {
+        GemmParams& a = q[n];
+        a.A = (const uint8_t*)PT; a.B = ws + b.at; a.lda = a.ldb = b.ldt * 2; a.a_piece = e.pt_piece * 2;
+        a.rows_a = (int32_t)cols; a.chunks = (int32_t)(b.ldt / 8); a.split = (float*)(ws + b.split_b);
+        a.e.scale = make_elem(fmt_a, ELEM_BF16).factor; a.e.M = (int32_t)cols; a.e.Y = dB;
+        parts[n++] = b.out[1];
     }
+    for (int i = 0; i < n; ++i) {
+        q[i].pieces = b.pieces;
+        q[i].rows_b = q[i].half = (int32_t)K;
+        q[i].steps = (int32_t)parts[i].steps;
+        q[i].e.N = (int32_t)K; q[i].e.y_type = g_type;
+    }
+    run_products(q, parts, n, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 

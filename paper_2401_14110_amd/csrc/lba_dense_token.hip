@@ -95,9 +95,9 @@ __global__ __launch_bounds__(512) void dense_token_kernel(TokenParams p) {
     __syncthreads();
     if (wave >= MF) return;
     const int m = wave * 16 + (lane & 15);
-    const Columns<GATED> cols = columns_of<GATED>(p.e, n0 + (lane / 16) * 4);
+    const Columns<GATED, 4> cols = columns_of<GATED, 4>(p.e, n0 + (lane / 16) * 4);
     float r[4];
-    load_extra(p.e, p.e.R, p.e.r_type, m, cols.n, r);
+    load_extra<4>(p.e, m, cols.n, r);
     f32x4 s[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(512) void dense_token_kernel(TokenParams p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) { z[j] = s[0][j]; u[j] = s[H - 1][j]; }
     const uint64_t base = p.e.drop.threshold ? drop_base(p.e.drop) : 0;
-    finish_forward<GATED>(p.e, cols, base, m, z, u, r);
+    with_act(p.e.act, [&](auto act) { finish_forward<GATED, false, decltype(act)::value, 4>(p.e, cols, base, m, At{(int64_t)m * p.e.N + cols.n, 0}, z, u, r); });
 }
 
 void launch_dense_token(const TokenParams& p, int elem, bool gated, hipStream_t st) {

@@ -21,7 +21,6 @@ struct DropoutParams {
     int64_t M;
     int32_t N;
     int32_t r_type;
-    int32_t act;
     float scale;
     int32_t strips;          // full strips of 64 vectors; workgroups below main_blocks belong to them
     int32_t main_blocks, main_chunks, tail_chunks;
@@ -55,7 +54,7 @@ template <int V> __device__ __forceinline__ void load_typed(const void* at, int 
     else load_some<V>((const bf16_t*)at + i, n, v);
 }
 
-template <typename TX, typename TY>
+template <typename TX, typename TY, int ACT>
 __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
     constexpr int V = 16 / sizeof(TX);
     const LanePlace q = lane_place<V>(p);
@@ -70,10 +69,10 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
         float x[V], f[V], r[V];
         load_some<V>((const TX*)p.X + i, q.cols, x);
         if (p.R) load_typed<V>(p.R, p.r_type, i, q.cols, r);
-        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, f);
+        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, (p.N & 3) == 0, f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            float z = act_value(fmaf(x[j], p.scale, bias[j]), p.act);
+            float z = act_value<ACT>(fmaf(x[j], p.scale, bias[j]));
             if (p.drop.threshold) z = f[j] != 0.0f ? z * f[j] : 0.0f;
             x[j] = p.R ? z + r[j] : z;
         }
@@ -81,7 +80,7 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
     }
 }
 
-template <typename TG, typename TX>
+template <typename TG, typename TX, int ACT>
 __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
     constexpr int V = 16 / sizeof(TX);
     const LanePlace q = lane_place<V>(p);
@@ -89,7 +88,7 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
     float bias[V], sum[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) bias[j] = sum[j] = 0.0f;
-    const bool read_x = p.act != LBA_ACT_NONE;
+    constexpr bool read_x = ACT != LBA_ACT_NONE;
     if (p.bias && read_x) load_some<V>(p.bias + q.col, q.cols, bias);
     if (q.cols > 0)
     for (int64_t row = q.row; row < q.end; row += q.step) {
@@ -97,13 +96,13 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
         float x[V], g[V], f[V];
         load_some<V>((const TG*)p.G + i, q.cols, g);
         if (read_x) load_some<V>((const TX*)p.X + i, q.cols, x);
-        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, f);
+        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, (p.N & 3) == 0, f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             float d = g[j];
             if (read_x) {
                 float value, slope;
-                act_both(fmaf(x[j], p.scale, bias[j]), p.act, value, slope);
+                act_both<ACT>(fmaf(x[j], p.scale, bias[j]), value, slope);
                 d *= slope;
             }
             if (p.drop.threshold) d = f[j] != 0.0f ? d * f[j] : 0.0f;
@@ -184,11 +183,17 @@ int lba_dropout(const void* X, int32_t x_type, float scale, const float* bias, i
     if (rc != LBA_OK) return rc;
     if (M == 0 || N == 0) return LBA_OK;
     if (!X || !Y) return LBA_ERR_NULL;
-    p.X = X; p.R = residual; p.bias = bias; p.Y = Y; p.M = M; p.N = (int32_t)N; p.r_type = r_type; p.act = act; p.scale = scale;
+    p.X = X; p.R = residual; p.bias = bias; p.Y = Y; p.M = M; p.N = (int32_t)N; p.r_type = r_type; p.scale = scale;
     if (y_type == LBA_CODE8) p.fmt = make_code_fmt(y_fmt);
     const dim3 grid(dropout_cut(&p, x_type == LBA_F32 ? 4 : 8, kFwdBlocks));
     const hipStream_t st = (hipStream_t)hip_stream;
-#define LBA_DROPOUT(TX, TY) hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY>), grid, dim3(256), 0, st, p)
+#define LBA_DROPOUT(TX, TY) \
+    do { \
+        if (act == LBA_ACT_NONE) hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY, LBA_ACT_NONE>), grid, dim3(256), 0, st, p); \
+        else if (act == LBA_ACT_RELU) hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY, LBA_ACT_RELU>), grid, dim3(256), 0, st, p); \
+        else if (act == LBA_ACT_GELU) hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY, LBA_ACT_GELU>), grid, dim3(256), 0, st, p); \
+        else hipLaunchKernelGGL((dropout_fwd_kernel<TX, TY, LBA_ACT_SILU>), grid, dim3(256), 0, st, p); \
+    } while (0)
     if (x_type == LBA_F32) {
         if (y_type == LBA_F32) LBA_DROPOUT(float, float);
         else if (y_type == LBA_BF16) LBA_DROPOUT(float, bf16_t);
@@ -239,9 +244,15 @@ int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type
         if (workspace_bytes < lba_dropout_bwd_workspace_bytes(M, N)) return LBA_ERR_SHAPE;
     }
     p.X = X; p.G = G; p.bias = bias; p.Y = dX; p.part = dbias ? (float*)workspace : nullptr;
-    p.M = M; p.N = (int32_t)N; p.act = act; p.scale = scale;
+    p.M = M; p.N = (int32_t)N; p.scale = scale;
     const dim3 grid(dropout_cut(&p, x_type == LBA_F32 ? 4 : 8, kBwdBlocks));
-#define LBA_DROPOUT(TG, TX) hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX>), grid, dim3(256), 0, st, p)
+#define LBA_DROPOUT(TG, TX) \
+    do { \
+        if (act == LBA_ACT_NONE) hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX, LBA_ACT_NONE>), grid, dim3(256), 0, st, p); \
+        else if (act == LBA_ACT_RELU) hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX, LBA_ACT_RELU>), grid, dim3(256), 0, st, p); \
+        else if (act == LBA_ACT_GELU) hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX, LBA_ACT_GELU>), grid, dim3(256), 0, st, p); \
+        else hipLaunchKernelGGL((dropout_bwd_kernel<TG, TX, LBA_ACT_SILU>), grid, dim3(256), 0, st, p); \
+    } while (0)
     if (g_type == LBA_F32) {
         if (x_type == LBA_F32) LBA_DROPOUT(float, float); else LBA_DROPOUT(float, bf16_t);
     } else {

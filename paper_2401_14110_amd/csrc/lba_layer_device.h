@@ -127,29 +127,55 @@ __device__ __forceinline__ float exp_near(float x) {
     return x > 88.72f ? __builtin_inff() : fmaf(e, left * 0.693147181f, e);
 }
 
-__device__ __forceinline__ float act_value(float z, int act) {
-    if (act == LBA_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
-    if (act == LBA_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    if (act == LBA_ACT_SILU) return z / (1.0f + exp_near(-z));
+// The normal distribution function and e^(-z^2/2).  For a = |z|, Phi(-a) = e^(-a^2/2) * h(t) with t = 1 / (1 + 0.28 a); h is smooth and is taken
+// as a polynomial of degree 6 without a constant term, fitted to (1 + a) * Phi in the largest error (1.5e-8).  A negative argument's
+// value is the product itself, so nothing cancels in the tail; the exponential is what the derivative needs as well.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.28f, fabsf(z), 1.0f));
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    float h = fmaf(t, -0.10655423f, 0.39296786f);
+    h = fmaf(t, h, -0.24209468f);
+    h = fmaf(t, h, 0.27308893f);
+    h = fmaf(t, h, 0.065796522f);
+    h = fmaf(t, h, 0.11679558f);
+    const float q = e * (t * h);
+    return z < 0.0f ? q : 1.0f - q;
+}
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_near(-z)); }
+
+template <int ACT> __device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == LBA_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if constexpr (ACT == LBA_ACT_GELU) { float e; return z * normal_cdf(z, e); }
+    if constexpr (ACT == LBA_ACT_SILU) return z * logistic(z);
     return z;
 }
 // act(z) and its derivative
-__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
-    if (act == LBA_ACT_RELU) {
+template <int ACT> __device__ __forceinline__ void act_both(float z, float& value, float& slope) {
+    if constexpr (ACT == LBA_ACT_RELU) {
         value = z > 0.0f ? z : (z != z ? z : 0.0f);
         slope = z > 0.0f ? 1.0f : 0.0f;
-    } else if (act == LBA_ACT_GELU) {
-        const float phi = 0.5f * (1.0f + erff(z * 0.70710678f));
+    } else if constexpr (ACT == LBA_ACT_GELU) {
+        float e;
+        const float phi = normal_cdf(z, e);
         value = z * phi;
-        slope = fmaf(z * 0.39894228f, exp_near(-0.5f * z * z), phi);
-    } else if (act == LBA_ACT_SILU) {
-        const float h = 1.0f / (1.0f + exp_near(-z));
+        slope = fmaf(z * 0.39894228f, e, phi);
+    } else if constexpr (ACT == LBA_ACT_SILU) {
+        const float h = logistic(z);
         value = z * h;
         slope = h * (1.0f + z * (1.0f - h));
     } else {
         value = z;
         slope = 1.0f;
     }
+}
+// a number known when compiling, as an argument
+template <int V> struct Known { static constexpr int value = V; };
+// f(Known<act>): one branch around what is done with the activation, not one an element
+template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
+    if (act == LBA_ACT_NONE) f(Known<LBA_ACT_NONE>{});
+    else if (act == LBA_ACT_RELU) f(Known<LBA_ACT_RELU>{});
+    else if (act == LBA_ACT_GELU) f(Known<LBA_ACT_GELU>{});
+    else f(Known<LBA_ACT_SILU>{});
 }
 
 // ---- dropout --------------------------------------------------------------------------------
@@ -172,28 +198,25 @@ __device__ __forceinline__ uint64_t drop_base(const DropParams& d) {
     const uint64_t s = d.stream + (d.step ? *d.step : 0ull);
     return mix64(mix64(d.seed * 2 + 1) ^ ((s * 2 + 1) * kGolden));
 }
-// factors (0 or keep_scale) of V consecutive elements from index i on
-template <int V> __device__ __forceinline__ void drop_factors(uint64_t i, uint64_t base, uint32_t threshold, float keep_scale, float (&f)[V]) {
-    const uint32_t phase = (uint32_t)i & 3u;
+// Factors (0 or keep_scale) of V consecutive elements from index i on.  `whole`: i is a multiple of 4 (uniform: where rows are multiples of 4);
+// else the elements' bits are cut out of two neighbouring words.
+template <int V> __device__ __forceinline__ void drop_factors(uint64_t i, uint64_t base, uint32_t threshold, float keep_scale, bool whole, float (&f)[V]) {
+    const uint32_t shift = ((uint32_t)i & 3u) * 16;
     uint64_t z = (i >> 2) * kGolden + base;
-    if (phase == 0) {                                    // uniform wherever rows are multiples of 4
-#pragma unroll
-        for (int q = 0; q < (V + 3) / 4; ++q, z += kGolden) {
-            const uint64_t w = mix64(z);
-#pragma unroll
-            for (int j = 0; j < 4 && 4 * q + j < V; ++j) f[4 * q + j] = ((uint32_t)(w >> (16 * j)) & 0xFFFFu) >= threshold ? keep_scale : 0.0f;
-        }
-        return;
-    }
     uint64_t w = mix64(z);
 #pragma unroll
     for (int q = 0; q < (V + 3) / 4; ++q) {
-        z += kGolden;
-        const uint64_t next = mix64(z);
-        const uint64_t u = (w >> (16 * phase)) | (next << (64 - 16 * phase));
+        uint64_t u = w;
+        if (!whole) {
+            z += kGolden;
+            w = mix64(z);
+            u = (u >> shift) | ((w << 1) << (63 - shift));
+        } else if (4 * q + 4 < V) {
+            z += kGolden;
+            w = mix64(z);
+        }
 #pragma unroll
         for (int j = 0; j < 4 && 4 * q + j < V; ++j) f[4 * q + j] = ((uint32_t)(u >> (16 * j)) & 0xFFFFu) >= threshold ? keep_scale : 0.0f;
-        w = next;
     }
 }
 
