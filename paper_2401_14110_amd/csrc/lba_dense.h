@@ -12,6 +12,8 @@
 // A row of 128 bytes is 8 pieces of 16; piece c of row r stands at place c ^ (r / 2 % 8), so that the sixteen rows of a fragment
 // read, 16 bytes each, fall on all 64 banks once.  An operand's pieces beyond the end of its rows are read from a zero page and
 // rows beyond the last one repeat it: their outputs are not stored.
+// Conversions and products do not overlap on a SIMD, whichever waves they belong to: a step takes their sum (256 x 256: 4096 cycles of
+// products and 1800 of conversions take 5900), so the largest wave tile that its registers allow converts least.
 // Fragments: lane l holds row l % 16 and pieces l / 16 and l / 16 + 4 of the step, the same places of k for both operands, so it does
 // not matter in which order the matrix core walks over them.  B is the first factor, so lane l ends up with output row l % 16 and
 // four neighbouring columns 4 * (l / 16) ..: epilogues work on four columns at a time.
@@ -272,25 +274,43 @@ __global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(Ge
         }
         src[LA + i] = p.B + r * p.ldb + piece * 16;
     }
+#pragma unroll
+    for (int i = 0; i < LA + LB; ++i) asm volatile("" : "+v"(src[i]));               // one address a load, not a sum of parts at every step
     // what the loop reads of the parameters, once
-    const int pieces = p.pieces, steps_row = p.steps / pieces, chunks = p.chunks, shift_a = p.shift_a, shift_b = p.shift_b;
+    const int steps_row = p.steps / p.pieces, chunks = p.chunks, shift_a = p.shift_a, shift_b = p.shift_b;
     const uint32_t keep_a = p.keep_a, keep_b = p.keep_b;
-    const int64_t a_piece = p.a_piece;
-    auto stage = [&](int step, int buf) {
-        const int q = pieces > 1 ? step / steps_row : 0, s = step - q * steps_row;
-        const int64_t off = (int64_t)s * 128, off_a = off + q * a_piece;
+    const int64_t a_wrap = p.a_piece - (int64_t)steps_row * 128;                     // from the end of a row to its start in the next piece
+    const int first = slice * p.per_slice;
+    const int last = p.slices > 1 ? (first + p.per_slice < p.steps ? first + p.per_slice : p.steps) : p.steps;
+    // the step that is staged next: its number in its row, its place in A's and B's rows
+    int at_step = first;
+    int64_t at_b = 0, at_a = 0;
+    if (p.pieces > 1 && first > 0) {
+        at_step = first % steps_row;
+        at_a = first / steps_row * p.a_piece;
+    }
+    at_b = (int64_t)at_step * 128;
+    at_a += at_b;
+    auto stage = [&](int buf) {
         auto to_lds = [&](int i, const uint8_t* g) {
             uint8_t* l = &lds[buf][((i < LA ? i : i - LA) * THREADS + wave * 64) * 16 + (i < LA ? 0 : BM * 128)];
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)g,
                                              (__attribute__((address_space(3))) uint32_t*)l, 16, 0, 0);
         };
-        if (s * 8 + 8 <= chunks) {
+        if (at_step * 8 + 8 <= chunks) {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) to_lds(i, src[i] + (i < LA ? off_a : off));
+            for (int i = 0; i < LA + LB; ++i) to_lds(i, src[i] + (i < LA ? at_a : at_b));
         } else {                                         // the rows end inside this step
-            const bool in = s * 8 + piece < chunks;
+            const bool in = at_step * 8 + piece < chunks;
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) to_lds(i, in ? src[i] + (i < LA ? off_a : off) : (const uint8_t*)lba_zero_piece);
+            for (int i = 0; i < LA + LB; ++i) to_lds(i, in ? src[i] + (i < LA ? at_a : at_b) : (const uint8_t*)lba_zero_piece);
+        }
+        at_a += 128;
+        at_b += 128;
+        if (++at_step == steps_row) {                    // the next piece of A against the same B
+            at_step = 0;
+            at_a += a_wrap;
+            at_b = 0;
         }
     };
 
@@ -301,53 +321,63 @@ __global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(Ge
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int place = ((lane / 16) ^ ((lane & 15) >> 1)) * 16 + (lane & 15) * 128;
-    const int first = slice * p.per_slice;
-    const int last = p.slices > 1 ? (first + p.per_slice < p.steps ? first + p.per_slice : p.steps) : p.steps;
+    const int flip = (place & 64) ? -64 : 64;            // the second piece of a row is 64 bytes on, modulo the row
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
-        if (first + i < last) stage(first + i, i);
+        if (first + i < last) stage(i);
+    i32x4 ra[2][FM], rb[2][FN];
+    auto read = [&](int h, int buf) {
+        const uint8_t* la = &lds[buf][wm * FM * 2048 + place];
+        const uint8_t* lb = &lds[buf][BM * 128 + wn * FN * 2048 + place];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) rb[h][j] = *(const i32x4*)(lb + j * 2048 + h * flip);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) ra[h][i] = *(const i32x4*)(la + i * 2048 + h * flip);
+    };
+    auto multiply = [&](int h) {
+        if constexpr (ELEM == ELEM_BF16) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(rb[h][j], ra[h][i], acc[i][j]);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                i32x4 fb[FN];
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = eight_codes<ELEM>((uint32_t)rb[h][j][2 * s], (uint32_t)rb[h][j][2 * s + 1], shift_b, keep_b);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    const i32x4 fa = eight_codes<ELEM>((uint32_t)ra[h][i][2 * s], (uint32_t)ra[h][i][2 * s + 1], shift_a, keep_a);
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(fb[j], fa, acc[i][j]);
+                }
+            }
+        }
+    };
     int buf = 0;
 #pragma unroll 1
     for (int step = first; step < last; ++step) {
         // This step's loads have to be done, those of the NST - 2 steps after it may be under way.  A step is LA + LB loads a wave or more,
-        // and loads end in order.
-        if (NST > 3 && step + 2 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (LA + LB)) : "memory");
-        else if (NST > 2 && step + 1 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LA + LB) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();                    // every wave's loads of this step are done, and the step before is worked off
+        // and loads end in order.  What was read of the step before is in registers: its buffer is staged next.
+        if (NST > 3 && step + 2 < last) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * (LA + LB)) : "memory");
+        else if (NST > 2 && step + 1 < last) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LA + LB) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();                    // every wave's loads of this step are done, and the step before is read
         asm volatile("" ::: "memory");
-        if (step + NST - 1 < last) stage(step + NST - 1, buf == 0 ? NST - 1 : buf - 1);
-        const uint8_t* la = &lds[buf][wm * FM * 2048 + place];
-        const uint8_t* lb = &lds[buf][BM * 128 + wn * FN * 2048 + place];
-        // the second piece of a row is 64 bytes on, modulo the row
-        const int flip = (place & 64) ? -64 : 64;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 rb[FN], ra[FM];
-#pragma unroll
-            for (int j = 0; j < FN; ++j) rb[j] = *(const i32x4*)(lb + j * 2048 + h * flip);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) ra[i] = *(const i32x4*)(la + i * 2048 + h * flip);
-            if constexpr (ELEM == ELEM_BF16) {
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(rb[j], ra[i], acc[i][j]);
-            } else {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    i32x4 fb[FN];
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) fb[j] = eight_codes<ELEM>((uint32_t)rb[j][2 * s], (uint32_t)rb[j][2 * s + 1], shift_b, keep_b);
-#pragma unroll
-                    for (int i = 0; i < FM; ++i) {
-                        const i32x4 fa = eight_codes<ELEM>((uint32_t)ra[i][2 * s], (uint32_t)ra[i][2 * s + 1], shift_a, keep_a);
-#pragma unroll
-                        for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(fb[j], fa, acc[i][j]);
-                    }
-                }
-            }
+        // the first half's fragments are read before the next step's loads are issued, the second half's before the first half's products
+        read(0, buf);
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + NST - 1 < last) stage(buf == 0 ? NST - 1 : buf - 1);
+        if (FM < 6) {                                    // (large tiles have no registers for both halves)
+            read(1, buf);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+        } else {
+            multiply(0);
+            read(1, buf);
         }
+        multiply(1);
         buf = buf == NST - 1 ? 0 : buf + 1;
     }
     __syncthreads();
@@ -543,8 +573,8 @@ __global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(Ge
     }
 }
 
-// Tiles: rows of outputs, columns of B, waves over m and buffers.  The deep ones have four buffers, for grids that leave CUs to themselves: with
-// two, a step of a workgroup alone waits for its loads.
+// Tiles: rows of outputs, columns of B, waves over m.  The deep ones have four buffers instead of two, for bfloat16 rows: their steps are shorter
+// than the time a load takes where a CU has one workgroup (codes' are not: conversions fill them, and four buffers gained nothing).
 enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5 };
 struct TileShape { int bm, bn, wm; };
 inline TileShape tile_shape(int tile) {
@@ -599,9 +629,9 @@ struct TokenParams {
 void launch_dense_token(const TokenParams& p, int elem, bool gated, hipStream_t st);
 
 // launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape
-void launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
-void launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
-void launch_dense_bf16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_bf16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
 
 inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     p.gx = (p.e.M + s.bm - 1) / s.bm;
@@ -609,7 +639,7 @@ inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     return p.gx * p.gy * (p.slices > 1 ? p.slices : 1);
 }
 
-template <int ELEM> void launch_dense(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
+template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
     const TileShape s = tile_shape(tile);
     GemmPair pair;
     pair.g[0] = a;
@@ -619,22 +649,24 @@ template <int ELEM> void launch_dense(const GemmParams& a, const GemmParams* b, 
 #define LBA_DENSE(TILE, WM, WN, FM, FN, NST, GATED, EPI) \
     if (tile == TILE && gated == GATED && epi == EPI) { \
         hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \
-        return; \
+        return LBA_OK; \
     }
-#define LBA_DENSE_TILES(GATED, EPI) \
-    LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, GATED, EPI) \
-    LBA_DENSE(TILE_128_DEEP, 2, 2, 4, 4, 4, GATED, EPI) LBA_DENSE(TILE_64_DEEP, 2, 2, 2, 2, 4, GATED, EPI)
-#define LBA_DENSE_LARGE(GATED) \
-    LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, GATED, EPI_FORWARD)
-    LBA_DENSE_TILES(false, EPI_FORWARD)
-    LBA_DENSE_TILES(true, EPI_FORWARD)
+#define LBA_DENSE_SMALL(GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, GATED, EPI)
+#define LBA_DENSE_LARGE(GATED) LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, GATED, EPI_FORWARD)
+    LBA_DENSE_SMALL(false, EPI_FORWARD)
+    LBA_DENSE_SMALL(true, EPI_FORWARD)
     LBA_DENSE_LARGE(false)
     LBA_DENSE_LARGE(true)
-    LBA_DENSE_TILES(false, EPI_BACKWARD)
-    LBA_DENSE_TILES(true, EPI_BACKWARD)
+    LBA_DENSE_SMALL(false, EPI_BACKWARD)
+    LBA_DENSE_SMALL(true, EPI_BACKWARD)
+    if constexpr (ELEM == ELEM_BF16) {
+        LBA_DENSE(TILE_128_DEEP, 2, 2, 4, 4, 4, false, EPI_FORWARD)
+        LBA_DENSE(TILE_64_DEEP, 2, 2, 2, 2, 4, false, EPI_FORWARD)
+    }
 #undef LBA_DENSE_LARGE
-#undef LBA_DENSE_TILES
+#undef LBA_DENSE_SMALL
 #undef LBA_DENSE
+    return LBA_ERR_UNSUPPORTED;                          // a tile that the plan must not choose here
 }
 
 }  // namespace lba

@@ -152,13 +152,89 @@ static void cut(Product& p, int64_t slices) {
 }
 static size_t split_bytes(const Product& p) { return p.slices > 1 ? align256((size_t)(p.slices * p.rows * p.cols) * 4) : 0; }
 
-// chooses the tile of a product, or of two that share a launch, and their slices
-static int plan_tile(Product* p, int n, bool may_slice) {
-    (void)may_slice;
-    for (int i = 0; i < n; ++i) cut(p[i], 1);
-    int64_t t256 = 0, t128 = 0;
-    for (int i = 0; i < n; ++i) { t256 += tiles_of(p[i], TILE_256); t128 += tiles_of(p[i], TILE_128); }
-    return t256 >= 192 && may_slice ? TILE_256 : t128 >= 192 ? TILE_128 : TILE_64;
+// What a launch takes, in microseconds: a tile's workgroup needs `fixed` and `step` for each step where every CU holds `per_cu` of them, and
+// `fixed1` and `step1` where it has the CU to itself.  Measured on grids of 1 to 8 rounds and 1 to 64 steps (4096 x 4096 and 1024 x 1024 outputs,
+// K = 128 to 4096); a step of codes is 128 long, of bfloat16 rows 64.
+struct TileCost { int tile, per_cu; float fixed, step, fixed1, step1; };
+static const TileCost kCodes[] = {
+    {TILE_256, 1, 9.0f, 2.45f, 9.0f, 2.3f}, {TILE_192, 1, 7.0f, 1.9f, 7.0f, 1.85f}, {TILE_128, 2, 4.0f, 1.45f, 2.7f, 0.95f}, {TILE_64, 4, 2.6f, 0.95f, 0.6f, 0.47f}};
+static const TileCost kRows[] = {
+    {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.5f}, {TILE_128, 2, 4.0f, 1.0f, 2.7f, 0.85f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f},
+    {TILE_64, 4, 2.6f, 0.62f, 0.6f, 0.55f}, {TILE_64_DEEP, 2, 1.4f, 0.5f, 0.6f, 0.42f}};
+constexpr float kLaunch = 4.5f, kJoinRate = 6e6f;         // a launch alone; bytes a microsecond that the join moves
+constexpr int kCus = 256;
+
+// the end of `a` workgroups of duration da and then `b` of db on `slots` places, da >= db
+static double finish_of(int64_t a, double da, int64_t b, double db, int64_t slots) {
+    const int64_t rounds = a / slots, rest = a % slots;
+    const double at = (double)rounds * da;
+    if (b == 0) return at + (rest ? da : 0.0);
+    if (rest == 0) return at + (double)((b + slots - 1) / slots) * db;
+    const int64_t beside = (slots - rest) * (int64_t)(da / db);                      // of the second kind, beside the first's last round
+    if (b <= beside) return at + da;
+    return at + da + (double)((b - beside + slots - 1) / slots) * db;
+}
+
+static double cost_of(const Product* p, const int64_t* tiles, int n, const TileCost& c, float step_scale, float fixed_scale) {
+    int64_t wgs[2] = {0, 0};
+    double t = kLaunch, d[2] = {0.0, 0.0};
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) all += wgs[i] = tiles[i] * p[i].slices;
+    const bool alone = all <= kCus;
+    for (int i = 0; i < n; ++i) {
+        d[i] = (alone ? c.fixed1 : c.fixed) * fixed_scale + (double)p[i].per_slice * (alone ? c.step1 : c.step) * step_scale;
+        if (p[i].slices > 1) t += (p[i].slices + 1.0) * (double)p[i].rows * (double)p[i].cols * 4.0 / kJoinRate;
+    }
+    if (p[0].slices > 1 || (n > 1 && p[1].slices > 1)) t += kLaunch;
+    const int x = n > 1 && d[1] > d[0] ? 1 : 0;
+    const int64_t slots = (int64_t)kCus * c.per_cu;
+    // between one and all places of a CU taken, a round is between the two durations
+    if (!alone && all < slots && c.per_cu > 1) {
+        const double share = (double)(all - kCus) / (double)(slots - kCus);
+        for (int i = 0; i < n; ++i) {
+            const double d1 = c.fixed1 * fixed_scale + (double)p[i].per_slice * c.step1 * step_scale;
+            d[i] = d1 + (d[i] - d1) * share;
+        }
+    }
+    return t + finish_of(wgs[x], d[x], wgs[1 - x], n > 1 ? d[1 - x] : 1.0, slots);
+}
+
+// Chooses the tile of a product, or of two that share a launch, and their slices: the least cost.
+enum { PLAN_FORWARD = 0, PLAN_BACKWARD = 1 };             // with the backward epilogue only small tiles, and no slices
+static int plan_tile(Product* p, int n, int elem, int kind, bool gated) {
+    const TileCost* all = elem == ELEM_BF16 ? kRows : kCodes;
+    const int count = elem == ELEM_BF16 ? (int)(sizeof(kRows) / sizeof(kRows[0])) : (int)(sizeof(kCodes) / sizeof(kCodes[0]));
+    const float step_scale = elem == ELEM_F16 ? 1.25f : 1.0f;                        // its conversions take five instructions for E4M3's two
+    static const int kSlices[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
+    int best = TILE_64;
+    double least = 1e300;
+    Product cut_best[2];
+    for (int t = 0; t < count; ++t) {
+        if (kind == PLAN_BACKWARD && all[t].tile != TILE_128 && all[t].tile != TILE_64) continue;
+        if (gated && (all[t].tile == TILE_128_DEEP || all[t].tile == TILE_64_DEEP)) continue;          // built for plain products
+        const int64_t slots = (int64_t)kCus * all[t].per_cu;
+        int64_t tiles[2] = {tiles_of(p[0], all[t].tile), n > 1 ? tiles_of(p[1], all[t].tile) : 0};
+        // slices as long as they are four steps or more and the chip has room for them
+        auto may = [&](int i, int s) { return s == 1 || (kind == PLAN_FORWARD && p[i].steps >= 4 * s && tiles[i] * s <= 2 * slots); };
+        for (int s0 : kSlices) {
+            if (!may(0, s0)) break;
+            for (int s1 : kSlices) {
+                if (n > 1 ? !may(1, s1) : s1 > 1) break;
+                Product q[2] = {p[0], n > 1 ? p[1] : p[0]};
+                cut(q[0], s0);
+                if (n > 1) cut(q[1], s1);
+                const double c = cost_of(q, tiles, n, all[t], step_scale, kind == PLAN_BACKWARD ? 3.0f : 1.0f);
+                if (c < least) {
+                    least = c;
+                    best = all[t].tile;
+                    cut_best[0] = q[0];
+                    cut_best[1] = q[1];
+                }
+            }
+        }
+    }
+    for (int i = 0; i < n; ++i) p[i] = cut_best[i];
+    return best;
 }
 
 static int check_infmt(const lba_infmt& f) {
@@ -181,24 +257,29 @@ struct DensePlan {
     size_t copy_a, copy_b, split, bytes;
 };
 
-static DensePlan plan_forward(int64_t M, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, bool aligned) {
-    DensePlan d = {};
+static void lay_out(DensePlan& d, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, bool aligned) {
     d.elem = elem_of(fa, fb);
-    d.token = M <= kTokenRows;
     d.cols = gated ? 2 * N : N;
-    d.in_place = d.token || (d.elem != ELEM_BF16 && K % 16 == 0 && aligned);
+    d.in_place = d.elem != ELEM_BF16 && K % 16 == 0 && aligned;
     d.ld = d.elem != ELEM_BF16 ? up_to(K, 16) : 2 * up_to(K, 8);
     d.chunks = d.ld / 16;
     d.steps = (d.ld + 127) / 128;
+}
+
+static DensePlan plan_forward(int64_t M, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, bool aligned) {
+    DensePlan d = {};
+    lay_out(d, N, K, fa, fb, gated, aligned);
+    d.token = M <= kTokenRows;
+    if (d.token) return d;                               // reads its operands where they are
     size_t at = 0;
     if (!d.in_place) {
         d.copy_a = at; at += align256((size_t)(M * d.ld));
         d.copy_b = at; at += align256((size_t)(d.cols * d.ld));
     }
     d.fwd = {M, d.cols, d.steps, 1, d.steps};
-    d.tile = plan_tile(&d.fwd, 1, true);
+    d.tile = plan_tile(&d.fwd, 1, d.elem, PLAN_FORWARD, gated);
     d.split = at; at += split_bytes(d.fwd);
-    d.bytes = d.token ? 0 : at;
+    d.bytes = at;
     return d;
 }
 
@@ -216,12 +297,10 @@ struct BwdPlan {
 static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, int act, int g_type, bool aligned) {
     BwdPlan b = {};
     b.sums = act != LBA_ACT_NONE || gated;
-    b.f = plan_forward(M, N, K, fa, fb, gated, aligned);
     DensePlan& f = b.f;
-    // the sums again, always by the tile: few rows as well
-    f.token = false;
-    f.in_place = f.elem != ELEM_BF16 && K % 16 == 0 && aligned;
-    f.tile = plan_tile(&f.fwd, 1, false);
+    lay_out(f, N, K, fa, fb, gated, aligned);            // the sums again, always by the tile: few rows as well
+    f.fwd = {M, f.cols, b.sums ? f.steps : 0, 1, 0};
+    f.tile = plan_tile(&f.fwd, 1, f.elem, PLAN_BACKWARD, gated);
     size_t at = 0;
     if (b.sums && !f.in_place) {
         f.copy_a = at; at += align256((size_t)(M * f.ld));
@@ -239,7 +318,7 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
     b.part = at; at += align256((size_t)(b.part_rows * f.cols) * 4);
     b.out[0] = {M, K, (b.ldp * 2 + 127) / 128 * b.pieces, 1, 0};
     b.out[1] = {f.cols, K, (b.ldt * 2 + 127) / 128 * b.pieces, 1, 0};
-    b.tile = plan_tile(b.out, 2, true);
+    b.tile = plan_tile(b.out, 2, ELEM_BF16, PLAN_FORWARD, false);
     b.split_a = at; at += split_bytes(b.out[0]);
     b.split_b = at; at += split_bytes(b.out[1]);
     b.bytes = at;
@@ -264,7 +343,7 @@ static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* d
 static bool lay_fits(int64_t R, int64_t K) { return (R + 64) * (K + 64) <= ((int64_t)1 << 32); }
 
 // one product, or two that share a launch
-static void run_products(GemmParams* g, const Product* p, int n, int tile, int elem, bool gated, int epi, hipStream_t st) {
+static int run_products(GemmParams* g, const Product* p, int n, int tile, int elem, bool gated, int epi, hipStream_t st) {
     JoinPair join = {};
     int sliced = 0;
     for (int i = 0; i < n; ++i) {
@@ -272,15 +351,18 @@ static void run_products(GemmParams* g, const Product* p, int n, int tile, int e
         g[i].per_slice = (int32_t)p[i].per_slice;
         if (p[i].slices > 1) join.p[sliced++] = {g[i].e, g[i].split, p[i].slices, g[i].rows_b};
     }
-    const GemmParams* second = n > 1 ? &g[1] : nullptr;
-    if (elem == ELEM_E4M3) launch_dense_e4m3(g[0], second, tile, gated, epi, st);
-    else if (elem == ELEM_F16) launch_dense_f16(g[0], second, tile, gated, epi, st);
-    else launch_dense_bf16(g[0], second, tile, gated, epi, st);
-    if (!sliced) return;
+    const int x = n > 1 && p[1].per_slice > p[0].per_slice ? 1 : 0;                  // the longer workgroups first
+    const GemmParams* second = n > 1 ? &g[1 - x] : nullptr;
+    int rc;
+    if (elem == ELEM_E4M3) rc = launch_dense_e4m3(g[x], second, tile, gated, epi, st);
+    else if (elem == ELEM_F16) rc = launch_dense_f16(g[x], second, tile, gated, epi, st);
+    else rc = launch_dense_bf16(g[x], second, tile, gated, epi, st);
+    if (rc != LBA_OK || !sliced) return rc;
     join.blocks = join_blocks(join.p[0].e);
     const dim3 grid((unsigned)(join.blocks + (sliced > 1 ? join_blocks(join.p[1].e) : 0)));
     if (gated) hipLaunchKernelGGL(dense_join_kernel<true>, grid, dim3(256), 0, st, join);
     else hipLaunchKernelGGL(dense_join_kernel<false>, grid, dim3(256), 0, st, join);
+    return LBA_OK;
 }
 
 static int check_workspace(const void* ws, size_t have, size_t need) {
@@ -348,7 +430,8 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
     g.split = (float*)(ws + d.split);
-    run_products(&g, &d.fwd, 1, d.tile, d.elem, two, EPI_FORWARD, st);
+    rc = run_products(&g, &d.fwd, 1, d.tile, d.elem, two, EPI_FORWARD, st);
+    if (rc != LBA_OK) return rc;
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 
@@ -415,7 +498,8 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     g.chunks = b.sums ? (int32_t)b.f.chunks : 0; g.steps = b.sums ? (int32_t)b.f.steps : 0;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
-    run_products(&g, &b.f.fwd, 1, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
+    rc = run_products(&g, &b.f.fwd, 1, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
+    if (rc != LBA_OK) return rc;
     if (dbias) launch_column_sum(e.part, b.part_rows, cols, dbias, nullptr, cols, st);
 
     // the two products of it
@@ -443,7 +527,8 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
         q[i].steps = (int32_t)parts[i].steps;
         q[i].e.N = (int32_t)K; q[i].e.y_type = g_type;
     }
-    run_products(q, parts, n, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
+    rc = run_products(q, parts, n, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
+    if (rc != LBA_OK) return rc;
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 

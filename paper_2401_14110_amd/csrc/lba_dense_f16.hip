@@ -2,7 +2,7 @@
 #include "lba_dense.h"
 
 namespace lba {
-void launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
-    launch_dense<ELEM_F16>(a, b, tile, gated, epi, st);
+int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
+    return launch_dense<ELEM_F16>(a, b, tile, gated, epi, st);
 }
 }  // namespace lba
