@@ -114,11 +114,11 @@ __device__ __forceinline__ void finish_forward(const EpiParams& e, const Columns
         z[j] = act_value<ACT>(fmaf(z[j], e.scale, c.b[j]));
         if (GATED) z[j] *= fmaf(u[j], e.scale, c.bu[j]);
     }
-    if (e.drop.threshold) {
-        float f[V];
-        drop_factors<V>((uint64_t)i.u + i.o, base, e.drop.threshold, e.drop.keep_scale, (e.N & 3) == 0, f);
+    if (e.drop.on) {
+        bool keep[V];
+        drop_keeps<V>((uint64_t)i.u + i.o, base, e.drop, (e.N & 3) == 0, keep);
 #pragma unroll
-        for (int j = 0; j < V; ++j) z[j] = f[j] != 0.0f ? z[j] * f[j] : 0.0f;
+        for (int j = 0; j < V; ++j) z[j] = keep[j] ? z[j] * e.drop.keep_scale : 0.0f;
     }
     if (e.R) {
 #pragma unroll
@@ -141,17 +141,17 @@ template <int V> __device__ __forceinline__ void load_extra(const EpiParams& e, 
 template <bool GATED, bool INSIDE, int ACT, int V>
 __device__ __forceinline__ void finish_backward(const EpiParams& e, const Columns<GATED, V>& c, uint64_t base, int m, const At& i, float (&z)[V], float (&u)[V],
                                                 const float (&g)[V]) {
-    float f[V];
+    bool keep[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = 1.0f;
-    if (e.drop.threshold) drop_factors<V>((uint64_t)i.u + i.o, base, e.drop.threshold, e.drop.keep_scale, (e.N & 3) == 0, f);
+    for (int j = 0; j < V; ++j) keep[j] = true;
+    if (e.drop.on) drop_keeps<V>((uint64_t)i.u + i.o, base, e.drop, (e.N & 3) == 0, keep);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         if (j == 4) __builtin_amdgcn_sched_barrier(0);
-        const bool on = (INSIDE || (m < e.M && j < c.cnt)) && f[j] != 0.0f;        // a dropped element's sums do not matter
+        const bool on = (INSIDE || (m < e.M && j < c.cnt)) && keep[j];               // a dropped element's sums do not matter
         float value, slope;
         act_both<ACT>(fmaf(z[j], e.scale, c.b[j]), value, slope);
-        const float d = g[j] * f[j];
+        const float d = g[j] * e.drop.keep_scale;                                    // 1 where nothing is dropped
         z[j] = on ? (GATED ? d * fmaf(u[j], e.scale, c.bu[j]) * slope : d * slope) : 0.0f;
         if (GATED) u[j] = on ? d * value : 0.0f;
     }
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(Ge
     static_assert(PASSES >= 1 && FM / EH <= 2 && FM % EH == 0 && sizeof(lds) >= (size_t)WM * WN * EH * 16 * CH * 16, "epilogue");
     float* mine = (float*)&lds[0][0] + wave * (EH * 16 * CH * 4);
     const EpiParams e = p.e;
-    const uint64_t base = e.drop.threshold ? drop_base(e.drop) : 0;
+    const uint64_t base = e.drop.on ? drop_base(e.drop) : 0;
     const int oct = lane % LPR;
     const int cz = GATED ? oct / 2 * 8 + oct % 2 * 2 : oct * 2;                      // the first of its two places in the row of sums
     const int nw = n0 + wn * (GATED ? FN * 8 : FN * 16), ncol = nw + oct * 8;

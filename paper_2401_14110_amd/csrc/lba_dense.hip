@@ -111,7 +111,7 @@ template <bool GATED> __global__ __launch_bounds__(256) void dense_join_kernel(J
     const EpiParams& e = p.e;
     const int64_t first = second ? (int64_t)blockIdx.x - both.blocks : (int64_t)blockIdx.x, blocks = second ? (int64_t)gridDim.x - both.blocks : (int64_t)both.blocks;
     const int64_t quads = (e.N + 3) / 4, total = quads * e.M, plane = (int64_t)e.M * p.cols;
-    const uint64_t base = e.drop.threshold ? drop_base(e.drop) : 0;
+    const uint64_t base = e.drop.on ? drop_base(e.drop) : 0;
     for (int64_t i = first * 256 + threadIdx.x; i < total; i += blocks * 256) {
         const int64_t m = i / quads;
         const int n = (int)(i - m * quads) * 4;

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(512) void dense_token_kernel(TokenParams p) {
     float z[4], u[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) { z[j] = s[0][j]; u[j] = s[H - 1][j]; }
-    const uint64_t base = p.e.drop.threshold ? drop_base(p.e.drop) : 0;
+    const uint64_t base = p.e.drop.on ? drop_base(p.e.drop) : 0;
     with_act(p.e.act, [&](auto act) { finish_forward<GATED, false, decltype(act)::value, 4>(p.e, cols, base, m, At{(int64_t)m * p.e.N + cols.n, 0}, z, u, r); });
 }
 

@@ -49,9 +49,18 @@ template <int V> __device__ __forceinline__ LanePlace lane_place(const DropoutPa
     return q;
 }
 
-template <int V> __device__ __forceinline__ void load_typed(const void* at, int type, int64_t i, int n, float (&v)[V]) {
-    if (type == LBA_F32) load_some<V>((const float*)at + i, n, v);
-    else load_some<V>((const bf16_t*)at + i, n, v);
+// A row's vector of a lane: in a full strip whole, and the wave's lanes, all of which take part, share the words of the generator.
+template <bool FULL, int V, typename T> __device__ __forceinline__ void load_part(const T* at, int n, float (&v)[V]) {
+    if constexpr (FULL) load_vec<V>(at, v);
+    else load_some<V>(at, n, v);
+}
+template <bool FULL, int V> __device__ __forceinline__ void keeps(const DropoutParams& p, const LanePlace& q, int64_t row, int64_t i, uint64_t base, bool (&keep)[V]) {
+    if constexpr (FULL && V == 8) {
+        const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane((int)row) * p.N + __builtin_amdgcn_readfirstlane(q.col);
+        drop_keeps_wave((uint64_t)first, base, p.drop, (p.N & 3) == 0, keep);
+    } else {
+        drop_keeps<V>((uint64_t)i, base, p.drop, (p.N & 3) == 0, keep);
+    }
 }
 
 template <typename TX, typename TY, int ACT>
@@ -64,20 +73,33 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) bias[j] = 0.0f;
     if (p.bias) load_some<V>(p.bias + q.col, q.cols, bias);
-    for (int64_t row = q.row; row < q.end; row += q.step) {
-        const int64_t i = row * p.N + q.col;
-        float x[V], f[V], r[V];
-        load_some<V>((const TX*)p.X + i, q.cols, x);
-        if (p.R) load_typed<V>(p.R, p.r_type, i, q.cols, r);
-        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, (p.N & 3) == 0, f);
+    auto rows = [&](auto full) {
+        constexpr bool FULL = decltype(full)::value != 0;
+#pragma unroll 1
+        for (int64_t row = q.row; row < q.end; row += q.step) {
+            const int64_t i = row * p.N + q.col;
+            float x[V], r[V];
+            bool keep[V];
+            load_part<FULL, V>((const TX*)p.X + i, q.cols, x);
+            if (p.R && p.r_type == LBA_F32) load_part<FULL, V>((const float*)p.R + i, q.cols, r);
+            else if (p.R) load_part<FULL, V>((const bf16_t*)p.R + i, q.cols, r);
+            if (p.drop.on) keeps<FULL, V>(p, q, row, i, base, keep);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float z = act_value<ACT>(fmaf(x[j], p.scale, bias[j]));
-            if (p.drop.threshold) z = f[j] != 0.0f ? z * f[j] : 0.0f;
-            x[j] = p.R ? z + r[j] : z;
+            for (int j = 0; j < V; ++j) x[j] = act_value<ACT>(fmaf(x[j], p.scale, bias[j]));
+            if (p.drop.on) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = keep[j] ? x[j] * p.drop.keep_scale : 0.0f;
+            }
+            if (p.R) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] += r[j];
+            }
+            if constexpr (FULL) store_vec<V>((TY*)p.Y + i, x, p.fmt);
+            else store_some<V>((TY*)p.Y + i, q.cols, x, p.fmt);
         }
-        store_some<V>((TY*)p.Y + i, q.cols, x, p.fmt);
-    }
+    };
+    if ((int)blockIdx.x < p.main_blocks) rows(Known<1>{});
+    else rows(Known<0>{});
 }
 
 template <typename TG, typename TX, int ACT>
@@ -90,40 +112,57 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
     for (int j = 0; j < V; ++j) bias[j] = sum[j] = 0.0f;
     constexpr bool read_x = ACT != LBA_ACT_NONE;
     if (p.bias && read_x) load_some<V>(p.bias + q.col, q.cols, bias);
-    if (q.cols > 0)
-    for (int64_t row = q.row; row < q.end; row += q.step) {
-        const int64_t i = row * p.N + q.col;
-        float x[V], g[V], f[V];
-        load_some<V>((const TG*)p.G + i, q.cols, g);
-        if (read_x) load_some<V>((const TX*)p.X + i, q.cols, x);
-        if (p.drop.threshold) drop_factors<V>((uint64_t)i, base, p.drop.threshold, p.drop.keep_scale, (p.N & 3) == 0, f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float d = g[j];
+    auto rows = [&](auto full) {
+        constexpr bool FULL = decltype(full)::value != 0;
+#pragma unroll 1
+        for (int64_t row = q.row; row < q.end; row += q.step) {
+            const int64_t i = row * p.N + q.col;
+            float x[V], g[V];
+            bool keep[V];
+            load_part<FULL, V>((const TG*)p.G + i, q.cols, g);
+            if (read_x) load_part<FULL, V>((const TX*)p.X + i, q.cols, x);
+            if (p.drop.on) keeps<FULL, V>(p, q, row, i, base, keep);
             if (read_x) {
-                float value, slope;
-                act_both<ACT>(fmaf(x[j], p.scale, bias[j]), value, slope);
-                d *= slope;
-            }
-            if (p.drop.threshold) d = f[j] != 0.0f ? d * f[j] : 0.0f;
-            sum[j] += d;
-            x[j] = d * p.scale;
-        }
-        if (p.Y) store_some<V>((TX*)p.Y + i, q.cols, x, p.fmt);
-    }
-    if (!p.part) return;
-    // the lanes of the workgroup that own the same columns, one after the other
-    __shared__ float lds[256 * V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) lds[j * 256 + threadIdx.x] = sum[j];
-    __syncthreads();
+                for (int j = 0; j < V; ++j) {
+                    float value, slope;
+                    act_both<ACT>(fmaf(x[j], p.scale, bias[j]), value, slope);
+                    g[j] *= slope;
+                }
+            }
+            if (p.drop.on) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) g[j] = keep[j] ? g[j] * p.drop.keep_scale : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                sum[j] += g[j];
+                g[j] *= p.scale;
+            }
+            if (p.Y) {
+                if constexpr (FULL) store_vec<V>((TX*)p.Y + i, g, p.fmt);
+                else store_some<V>((TX*)p.Y + i, q.cols, g, p.fmt);
+            }
+        }
+    };
+    if ((int)blockIdx.x < p.main_blocks) rows(Known<1>{});
+    else if (q.cols > 0) rows(Known<0>{});
+    if (!p.part) return;
+    // the lanes that own the same columns: within the wave, then its four sums
     const int lanes = 1 << q.lanes_log;
+    for (int d = lanes; d < 64; d *= 2) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += __shfl_xor(sum[j], d);
+    }
+    __shared__ float lds[4][64 * V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) lds[threadIdx.x / 64][j * 64 + (threadIdx.x & 63)] = sum[j];
+    __syncthreads();
     if ((int)threadIdx.x >= lanes || q.cols <= 0) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        float s = 0.0f;
-        for (int t = threadIdx.x; t < 256; t += lanes) s += lds[j * 256 + t];
-        sum[j] = s;
+        const int at = j * 64 + threadIdx.x;
+        sum[j] = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
     }
     store_some<V>(p.part + (int64_t)q.chunk * p.N + q.col, q.cols, sum, p.fmt);
 }

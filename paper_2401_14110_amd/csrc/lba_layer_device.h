@@ -183,7 +183,8 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
 struct DropParams {
     uint64_t seed, stream;
     const uint64_t* step;
-    uint32_t threshold;      // an element stays iff its 16 bits are at least this; 0: nothing is dropped
+    uint32_t on;             // 0: nothing is dropped (T = 0)
+    uint32_t above;          // 65536 T - 1: an element stays iff its 16 bits, in the high half of a word, are above it
     float keep_scale;        // 65536 / (65536 - threshold); 0 where everything is dropped
 };
 
@@ -198,26 +199,45 @@ __device__ __forceinline__ uint64_t drop_base(const DropParams& d) {
     const uint64_t s = d.stream + (d.step ? *d.step : 0ull);
     return mix64(mix64(d.seed * 2 + 1) ^ ((s * 2 + 1) * kGolden));
 }
-// Factors (0 or keep_scale) of V consecutive elements from index i on.  `whole`: i is a multiple of 4 (uniform: where rows are multiples of 4);
-// else the elements' bits are cut out of two neighbouring words.
-template <int V> __device__ __forceinline__ void drop_factors(uint64_t i, uint64_t base, uint32_t threshold, float keep_scale, bool whole, float (&f)[V]) {
-    const uint32_t shift = ((uint32_t)i & 3u) * 16;
-    uint64_t z = (i >> 2) * kGolden + base;
-    uint64_t w = mix64(z);
+// the words of V / 4 consecutive groups of four elements -> which of them stay
+template <int V> __device__ __forceinline__ void kept_of(const uint64_t (&u)[(V + 3) / 4], const DropParams& d, bool (&keep)[V]) {
 #pragma unroll
-    for (int q = 0; q < (V + 3) / 4; ++q) {
-        uint64_t u = w;
-        if (!whole) {
-            z += kGolden;
-            w = mix64(z);
-            u = (u >> shift) | ((w << 1) << (63 - shift));
-        } else if (4 * q + 4 < V) {
-            z += kGolden;
-            w = mix64(z);
-        }
-#pragma unroll
-        for (int j = 0; j < 4 && 4 * q + j < V; ++j) f[4 * q + j] = ((uint32_t)(u >> (16 * j)) & 0xFFFFu) >= threshold ? keep_scale : 0.0f;
+    for (int j = 0; j < V; ++j) {
+        const uint32_t half = (uint32_t)(u[j / 4] >> (32 * ((j % 4) / 2)));
+        keep[j] = (j % 2 ? half : half << 16) > d.above;         // what is below the high half decides nothing
     }
+}
+// Which of V consecutive elements from index i on stay.  `whole`: i is a multiple of 4 (uniform: where rows are multiples of 4); else the
+// elements' bits are cut out of two neighbouring words.
+template <int V> __device__ __forceinline__ void drop_keeps(uint64_t i, uint64_t base, const DropParams& d, bool whole, bool (&keep)[V]) {
+    constexpr int Q = (V + 3) / 4;
+    const uint32_t shift = ((uint32_t)i & 3u) * 16;
+    uint64_t z = (i >> 2) * kGolden + base, u[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q, z += kGolden) u[q] = mix64(z);
+    if (!whole) {
+        const uint64_t last = mix64(z);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) u[q] = (u[q] >> shift) | (((q + 1 < Q ? u[q + 1] : last) << 1) << (63 - shift));
+    }
+    kept_of<V>(u, d, keep);
+}
+// The same for a wave whose 64 lanes hold neighbouring groups of 8 elements of one row, the first of index `first` (uniform): the word behind a lane's two
+// is its neighbour's first, and the last lane's is made once for the wave.
+__device__ __forceinline__ void drop_keeps_wave(uint64_t first, uint64_t base, const DropParams& d, bool whole, bool (&keep)[8]) {
+    const uint32_t shift = ((uint32_t)first & 3u) * 16;
+    const uint64_t row = (first >> 2) * kGolden + base;  // uniform
+    const uint64_t z = row + (uint64_t)(2 * (threadIdx.x & 63)) * kGolden;
+    uint64_t u[2] = {mix64(z), mix64(z + kGolden)};
+    if (!whole) {
+        const uint64_t last = mix64(row + 128 * kGolden);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)(uint32_t)last, (int)(uint32_t)u[0], 0x130, 0xF, 0xF, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(last >> 32), (int)(u[0] >> 32), 0x130, 0xF, 0xF, false);
+        const uint64_t next = ((uint64_t)hi << 32) | lo;
+        u[0] = (u[0] >> shift) | ((u[1] << 1) << (63 - shift));
+        u[1] = (u[1] >> shift) | ((next << 1) << (63 - shift));
+    }
+    kept_of<8>(u, d, keep);
 }
 
 // ---- sums over a wave -----------------------------------------------------------------------

@@ -148,11 +148,31 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormParams p) {
     }
 }
 
+// a vector as it comes from memory: converted where it is used, so that nothing waits for a load that is under way
+template <typename T, int V> struct Raw { typename Vec<T, V>::type v; };
+template <int V> __device__ __forceinline__ float raw_at(const Raw<float, V>& r, int j) { return r.v[j]; }
+template <int V> __device__ __forceinline__ float raw_at(const Raw<uint16_t, V>& r, int j) { return __uint_as_float((uint32_t)r.v[j] << 16); }
+template <typename T> struct Bits { typedef uint16_t type; };
+template <> struct Bits<float> { typedef float type; };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p, int n) {
+    Raw<T, V> r;
+    if (n >= V) {
+        r.v = *(const typename Vec<T, V>::type*)p;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = j < n ? p[j] : (T)0;
+    }
+    return r;
+}
+
+// The next row of a lane group is loaded while this one is worked on (two sets of registers, so that none is moved while in flight).
 template <typename TG, typename TX, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
+    typedef typename Bits<TX>::type BX;
+    typedef typename Bits<TG>::type BG;
     __shared__ float lds[4 * (T / 64)];
-    const int t = threadIdx.x % T, sub = threadIdx.x / T;
+    const int t = threadIdx.x % T, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
     float ga[NV][V], dga[NV][V], dbe[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -164,33 +184,37 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams 
             dga[i][j] = dbe[i][j] = 0.0f;
         }
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < p.M; row += (int64_t)gridDim.x * RPB) {
-        const TX* x = (const TX*)p.X + row * p.N;
-        const TG* gr = (const TG*)p.G + row * p.N;
-        float n[NV][V], g[NV][V];
+    struct Row { Raw<BX, V> x[NV]; Raw<BG, V> g[NV]; float mean, rstd; };
+    auto load = [&](int64_t row, Row& r) {
+        const BX* x = (const BX*)p.X + row * p.N;
+        const BG* g = (const BG*)p.G + row * p.N;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * T + t) * V;
-            load_some<V>(x + c, p.N - c, n[i]);
-            load_some<V>(gr + c, p.N - c, g[i]);
+            r.x[i] = load_raw<BX, V>(x + c, p.N - c);
+            r.g[i] = load_raw<BG, V>(g + c, p.N - c);
         }
-        const float mean = p.mean[row], rstd = p.rstd[row];
-        float s[2] = {0.0f, 0.0f};
+        r.mean = p.mean[row];
+        r.rstd = p.rstd[row];
+    };
+    int turn = 0;
+    auto work = [&](int64_t row, const Row& r) {
+        float s[2] = {0.0f, 0.0f}, n[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * T + t) * V;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                n[i][j] = c + j < p.N ? (n[i][j] - mean) * rstd : 0.0f;
-                const float h = g[i][j] * ga[i][j];
-                dga[i][j] = fmaf(g[i][j], n[i][j], dga[i][j]);
-                dbe[i][j] += g[i][j];
+                const float g = raw_at(r.g[i], j);
+                n[i][j] = c + j < p.N ? (raw_at(r.x[i], j) - r.mean) * r.rstd : 0.0f;
+                const float h = g * ga[i][j];
+                dga[i][j] = fmaf(g, n[i][j], dga[i][j]);
+                dbe[i][j] += g;
                 s[0] += h;
                 s[1] = fmaf(h, n[i][j], s[1]);
             }
         }
-        if (!p.Y) continue;
+        if (!p.Y) return;
         row_sums<T, 2>(s, lds, turn++);
         const float mh = s[0] / p.n, mhn = s[1] / p.n;
         TX* dx = (TX*)p.Y + row * p.N;
@@ -199,9 +223,21 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams 
             const int c = (i * T + t) * V;
             if (c >= p.N) break;
 #pragma unroll
-            for (int j = 0; j < V; ++j) n[i][j] = rstd * (g[i][j] * ga[i][j] - fmaf(n[i][j], mhn, mh));
+            for (int j = 0; j < V; ++j) n[i][j] = r.rstd * (raw_at(r.g[i], j) * ga[i][j] - fmaf(n[i][j], mhn, mh));
             store_some<V>(dx + c, p.N - c, n[i], p.fmt);
         }
+    };
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    Row a, b;
+    int64_t row = (int64_t)blockIdx.x * RPB + sub;
+    if (row < p.M) load(row, a);
+    for (; row < p.M; row += 2 * step) {
+        const bool more = row + step < p.M;
+        if (more) load(row + step, b);
+        work(row, a);
+        if (!more) break;
+        if (row + 2 * step < p.M) load(row + 2 * step, a);
+        work(row + step, b);
     }
     if (!p.part) return;
     if (RPB > 1) {                                       // the workgroup's rows first: one after the other into LDS
@@ -212,9 +248,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams 
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        float* a = acc + ((i * V + j) * T + t) * 2;
-                        a[0] = r ? a[0] + dga[i][j] : dga[i][j];
-                        a[1] = r ? a[1] + dbe[i][j] : dbe[i][j];
+                        float* at = acc + (i * V + j) * T + t;
+                        at[0] = r ? at[0] + dga[i][j] : dga[i][j];
+                        at[T * NV * V] = r ? at[T * NV * V] + dbe[i][j] : dbe[i][j];
                     }
             }
             __syncthreads();
@@ -224,8 +260,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams 
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                dga[i][j] = acc[((i * V + j) * T + t) * 2];
-                dbe[i][j] = acc[((i * V + j) * T + t) * 2 + 1];
+                dga[i][j] = acc[(i * V + j) * T + t];
+                dbe[i][j] = acc[(i * V + j) * T + t + T * NV * V];
             }
     }
     float* out = p.part + (int64_t)blockIdx.x * 2 * p.N;
@@ -351,7 +387,7 @@ void launch_zero(void* out, int64_t bytes, hipStream_t st) {
 // lanes that share a row and vectors of 16 bytes a lane holds: the least that hold N elements (0 lanes: none does)
 struct RowShape { int lanes, vecs; };
 static RowShape row_shape(int64_t N, int v) {
-    static const RowShape all[] = {{64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {1024, 2}, {1024, 4}};
+    static const RowShape all[] = {{64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {512, 2}, {512, 4}, {1024, 2}, {1024, 4}};
     for (const RowShape& r : all)
         if (N <= (int64_t)r.lanes * r.vecs * v && r.vecs * v <= 16) return r;
     return {0, 0};
@@ -366,21 +402,23 @@ template <typename TX, typename TY> static void norm_fwd(const NormParams& p, hi
     LBA_NORM_FWD(64, 1, four)
     LBA_NORM_FWD(64, 2, four)
     LBA_NORM_FWD(256, 2, wide)
+    LBA_NORM_FWD(512, 2, wide)
     LBA_NORM_FWD(1024, 2, wide)
     if constexpr (sizeof(TX) == 4) {
         LBA_NORM_FWD(64, 4, four)
         LBA_NORM_FWD(256, 4, wide)
+        LBA_NORM_FWD(512, 4, wide)
         LBA_NORM_FWD(1024, 4, wide)
     }
 #undef LBA_NORM_FWD
     hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), wide, dim3(1024), 0, st, p);
 }
 
-// Workgroups of the backward pass that write partial sums: enough to fill the chip, few enough that their rows of partial sums stay a
+// Workgroups of the backward pass, each of which writes a row of partial sums: enough to fill the chip, few enough that these rows stay a
 // small part of the traffic
 static int64_t norm_bwd_blocks(int64_t M, int64_t N) {
-    const int64_t most = N <= 1024 ? 1024 : 512;
-    const int64_t groups = N <= 1024 ? (M + 3) / 4 : M;
+    const int64_t groups = N <= 1024 ? (M + 3) / 4 : M;                              // rows that workgroups take at a time
+    const int64_t most = groups >= 4096 || N <= 1024 ? 512 : 256;                    // few long rows: half of the partial sums
     return groups < most ? groups : most;
 }
 
@@ -395,10 +433,12 @@ template <typename TG, typename TX> static void norm_bwd(NormParams p, hipStream
     LBA_NORM_BWD(64, 1)
     LBA_NORM_BWD(64, 2)
     LBA_NORM_BWD(256, 2)
+    LBA_NORM_BWD(512, 2)
     LBA_NORM_BWD(1024, 2)
     if constexpr (sizeof(TX) == 4) {
         LBA_NORM_BWD(64, 4)
         LBA_NORM_BWD(256, 4)
+        LBA_NORM_BWD(512, 4)
         LBA_NORM_BWD(1024, 4)
     }
 #undef LBA_NORM_BWD
@@ -417,8 +457,10 @@ int check_out_type(int32_t t, const lba_infmt& f) {
 int check_drop(const lba_drop& d, DropParams* out) {
     if (!(d.p >= 0.0 && d.p <= 1.0)) return LBA_ERR_FORMAT;
     out->seed = d.seed; out->stream = d.stream; out->step = d.step;
-    out->threshold = (uint32_t)(d.p * 65536.0 + 0.5);
-    out->keep_scale = out->threshold >= 65536u ? 0.0f : (float)(65536.0 / (65536.0 - out->threshold));
+    const uint32_t t = (uint32_t)(d.p * 65536.0 + 0.5);
+    out->on = t > 0 ? 1 : 0;
+    out->above = t * 65536u - 1u;                        // all ones for T = 65536: nothing is above
+    out->keep_scale = t >= 65536u ? 0.0f : (float)(65536.0 / (65536.0 - t));
     return LBA_OK;
 }
 int check_rows(int64_t M, int64_t N) {
