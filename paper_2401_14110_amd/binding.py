@@ -4,6 +4,8 @@ Every step of the computation runs in the HIP library; there is no CPU fallback:
 has not been built, loading raises.  torch is used for device memory and for the current stream.
 """
 import ctypes
+import functools
+import math
 import os
 
 import torch
@@ -628,64 +630,103 @@ def conv2d(X, W, qprod, qacc, stride=1, pad=0, order=ORDER_SEQ, planes=False, st
 # Codes in and out are uint8 tensors with a format (exp_bits, man_bits, bias), whose bias carries the tensor's power-of-two scale: the
 # E4M3 codes of x * 2^t are those of (4, 3, 7 + t).  Temporaries belong to the stream that the call runs on.
 
-_E4M3 = lba_infmt(4, 3, 7)
+_E4M3 = (4, 3, 7)
+_NO_FORMAT = lba_infmt(4, 3, 7)
 _NO_DROP = lba_drop(0.0, 0, 0, None)
 _TYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.uint8: CODE8}
 _WORD = (1 << 64) - 1
 
 
-class _On:
-    """The stream of one call: its handle, and the tensors made here kept for it where it is not the current stream."""
+@functools.lru_cache(maxsize=1024)
+def _layer_bytes(name, *shape):
+    """A workspace's size, which the library derives from the shape alone."""
+    return getattr(lib(), name)(*shape)
 
-    __slots__ = ("stream", "handle")
 
-    def __init__(self, stream):
-        self.handle = _stream(stream)
-        if stream is None or hasattr(stream, "cuda_stream"):
-            self.stream = stream
-        else:
-            self.stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+class _Format(lba_infmt):
+    __hash__ = object.__hash__
 
-    def whole(self, t):
-        """t as the library reads it: contiguous (a copy is made on the call's stream)."""
-        if t.is_contiguous():
-            return t
-        if self.stream is None:
-            return t.contiguous()
-        with torch.cuda.stream(self.stream):
-            return t.contiguous()
 
-    def empty(self, shape, dtype, device):
-        t = torch.empty(shape, dtype=dtype, device=device)
-        if self.stream is not None:
-            t.record_stream(self.stream)
+_format = functools.lru_cache(maxsize=256)(_Format)   # one object a format, by its value, handed to nobody who might change it
+
+
+def _infmt(f):
+    if isinstance(f, lba_infmt):
+        return _format(f.exp_bits, f.man_bits, f.bias)
+    e, m, b = f
+    return _format(int(e), int(m), int(b))
+
+
+def _on(stream, device):
+    """(handle, stream) of a call on tensors of the device: stream is None where it is the current one, else the object that
+    tensors made here are recorded on."""
+    if device != torch.cuda.current_device():
+        raise ValueError("the tensors' device is not the current one")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device), None
+    handle = _stream(stream)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    return handle, stream
+
+
+def _whole(t, on):
+    """t as the library reads it: contiguous (a copy is made on the call's stream)."""
+    if t is None or t.is_contiguous():
         return t
+    if on is None:
+        return t.contiguous()
+    with torch.cuda.stream(on):
+        return t.contiguous()
 
 
-def _rows(t, what, dtypes=(torch.float32, torch.bfloat16)):
-    """(M, N) of a device tensor whose rows run along its last axis."""
-    if t.dtype not in dtypes or not t.is_cuda:
+def _empty(shape, dtype, device, on):
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if on is not None:
+        t.record_stream(on)
+    return t
+
+
+def _empty_as(t, dtype, on):
+    """A tensor of the contiguous t's shape (0.5 us less than from the shape)."""
+    t = torch.empty_like(t, dtype=dtype)
+    if on is not None:
+        t.record_stream(on)
+    return t
+
+
+def _workspace(size, device, on):
+    return _empty((size,), torch.uint8, device, on) if size else None
+
+
+_REAL = (torch.float32, torch.bfloat16)
+
+
+def _rows(t, what, dtypes=_REAL):
+    """(M, N, device) of a device tensor whose rows run along its last axis."""
+    device = t.get_device()
+    if t.dtype not in dtypes or device < 0:
         raise TypeError("%s must be a device tensor of %s" % (what, " or ".join(str(d) for d in dtypes)))
-    if t.dim() < 1:
+    shape = t.shape
+    if not shape:
         raise ValueError("%s must have at least one axis" % what)
-    n = t.shape[-1]
-    return (t.numel() // n if n else 0), n
+    return math.prod(shape[:-1]), shape[-1], device
 
 
-def _like(t, shape, what, dtypes=(torch.float32, torch.bfloat16)):
-    if t.dtype not in dtypes or not t.is_cuda:
-        raise TypeError("%s must be a device tensor of %s" % (what, " or ".join(str(d) for d in dtypes)))
+def _like(t, shape, device, what, dtypes=_REAL):
+    if t.dtype not in dtypes or t.get_device() != device:
+        raise TypeError("%s must be a tensor of %s on the call's device" % (what, " or ".join(str(d) for d in dtypes)))
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
     return t
 
 
-def _vector(on, t, n, what):
+def _vector(t, n, device, what, on):
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_cuda or tuple(t.shape) != (n,):
-        raise ValueError("%s must be a float32 device tensor [%d]" % (what, n))
-    return on.whole(t)
+    if t.dtype != torch.float32 or t.get_device() != device or t.shape != (n,):
+        raise ValueError("%s must be a float32 tensor [%d] on the call's device" % (what, n))
+    return _whole(t, on)
 
 
 def _out_type(dtype, fmt):
@@ -695,21 +736,21 @@ def _out_type(dtype, fmt):
     if dtype is torch.uint8:
         if fmt is None:
             raise ValueError("codes need out_fmt = (exp_bits, man_bits, bias)")
-        return CODE8, infmt(fmt)
+        return CODE8, _infmt(fmt)
     if fmt is not None:
         raise ValueError("out_fmt is for torch.uint8 codes")
-    return _TYPE[dtype], _E4M3
+    return _TYPE[dtype], _NO_FORMAT
 
 
-def _output(on, out, shape, dtype, device):
+def _output(out, like, shape, dtype, on):
     if out is None:
-        return on.empty(shape, dtype, device)
-    if out.dtype != dtype or out.shape != shape or not out.is_cuda or not out.is_contiguous():
-        raise ValueError("out must be a contiguous device tensor %s of %s" % (tuple(shape), dtype))
+        return _empty_as(like, dtype, on) if shape == like.shape else _empty(shape, dtype, like.device, on)
+    if out.dtype != dtype or out.shape != shape or out.get_device() != like.get_device() or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor %s of %s on the call's device" % (tuple(shape), dtype))
     return out
 
 
-def _drop(drop):
+def _drop(drop, device):
     """None, (p, seed, stream) or (p, seed, stream, step) with step a one-element int64 device tensor (read when the kernel runs)."""
     if drop is None:
         return _NO_DROP
@@ -717,8 +758,8 @@ def _drop(drop):
         return drop
     p, seed, stream = drop[:3]
     step = drop[3] if len(drop) > 3 else None
-    if step is not None and (step.dtype != torch.int64 or not step.is_cuda or step.numel() != 1):
-        raise ValueError("step must be an int64 device tensor of one element")
+    if step is not None and (step.dtype != torch.int64 or step.get_device() != device or step.numel() != 1):
+        raise ValueError("step must be an int64 tensor of one element on the call's device")
     return lba_drop(float(p), int(seed) & _WORD, int(stream) & _WORD, step.data_ptr() if step is not None else None)
 
 
@@ -729,34 +770,34 @@ def _at(t):
 def layernorm(x, gamma=None, beta=None, eps=1e-5, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None):
     """Layer norm over the last axis of x (float32 or bfloat16): y of out_dtype (x's by default; torch.uint8 codes need out_fmt), and
     with want_stats (y, mean, rstd), float32 tensors of x's leading shape, which layernorm_bwd reads."""
-    M, N = _rows(x, "x")
+    M, N, device = _rows(x, "x")
     dtype = out_dtype or x.dtype
     y_type, fmt = _out_type(dtype, out_fmt)
-    on = _On(stream)
-    x, gamma, beta = on.whole(x), _vector(on, gamma, N, "gamma"), _vector(on, beta, N, "beta")
-    y = _output(on, out, x.shape, dtype, x.device)
-    mean = on.empty(x.shape[:-1], torch.float32, x.device) if want_stats else None
-    rstd = on.empty(x.shape[:-1], torch.float32, x.device) if want_stats else None
-    _check(lib().lba_layernorm(_at(x), _TYPE[x.dtype], _at(gamma), _at(beta), eps, _at(y), y_type, fmt, _at(mean), _at(rstd), M, N,
-                               on.handle))
+    handle, on = _on(stream, device)
+    x, gamma, beta = _whole(x, on), _vector(gamma, N, device, "gamma", on), _vector(beta, N, device, "beta", on)
+    y = _output(out, x, x.shape, dtype, on)
+    mean = _empty(x.shape[:-1], torch.float32, x.device, on) if want_stats else None
+    rstd = _empty(x.shape[:-1], torch.float32, x.device, on) if want_stats else None
+    _check(lib().lba_layernorm(_at(x), _TYPE[x.dtype], _at(gamma), _at(beta), eps, _at(y), y_type, fmt, _at(mean), _at(rstd), M, N, handle))
     return (y, mean, rstd) if want_stats else y
 
 
 def layernorm_bwd(G, x, gamma, mean, rstd, want_dx=True, want_params=True, stream=None):
     """Gradients of layernorm: (dx of x's type or None, dgamma, dbeta: float32 or None)."""
-    M, N = _rows(x, "x")
-    _like(G, x.shape, "G")
-    _like(mean, x.shape[:-1], "mean", (torch.float32,))
-    _like(rstd, x.shape[:-1], "rstd", (torch.float32,))
-    on = _On(stream)
-    G, x, mean, rstd, gamma = on.whole(G), on.whole(x), on.whole(mean), on.whole(rstd), _vector(on, gamma, N, "gamma")
-    dx = on.empty(x.shape, x.dtype, x.device) if want_dx else None
-    params = on.empty((2, N), torch.float32, x.device) if want_params else None
-    size = lib().lba_layernorm_bwd_workspace_bytes(M, N) if want_params else 0
-    ws = on.empty((size,), torch.uint8, x.device) if size else None
-    dgamma, dbeta = params if want_params else (None, None)
+    M, N, device = _rows(x, "x")
+    rows = x.shape[:-1]
+    _like(G, x.shape, device, "G")
+    _like(mean, rows, device, "mean", (torch.float32,))
+    _like(rstd, rows, device, "rstd", (torch.float32,))
+    handle, on = _on(stream, device)
+    G, x, mean, rstd, gamma = _whole(G, on), _whole(x, on), _whole(mean, on), _whole(rstd, on), _vector(gamma, N, device, "gamma", on)
+    dx = _empty_as(x, x.dtype, on) if want_dx else None
+    dgamma = _empty((N,), torch.float32, x.device, on) if want_params else None
+    dbeta = _empty((N,), torch.float32, x.device, on) if want_params else None
+    size = _layer_bytes("lba_layernorm_bwd_workspace_bytes", M, N) if want_params else 0
+    ws = _workspace(size, x.device, on)
     _check(lib().lba_layernorm_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[x.dtype], _at(gamma), _at(mean), _at(rstd), _at(dx),
-                                   _at(dgamma), _at(dbeta), M, N, _at(ws), size, on.handle))
+                                   _at(dgamma), _at(dbeta), M, N, _at(ws), size, handle))
     return dx, dgamma, dbeta
 
 
@@ -764,79 +805,73 @@ def dropout(x, drop, bias=None, act=ACT_NONE, residual=None, scale=1.0, out_dtyp
     """residual + keep * act(scale * x + bias) / (1 - p) with drop = (p, seed, stream[, step]) or None; x and residual are float32
     or bfloat16, bias runs along the last axis, y is of out_dtype (x's by default; torch.uint8 codes need out_fmt).  After a simulated
     product scale = 2^-T undoes its operands' scales."""
-    M, N = _rows(x, "x")
+    M, N, device = _rows(x, "x")
     dtype = out_dtype or x.dtype
     y_type, fmt = _out_type(dtype, out_fmt)
-    d = _drop(drop)
-    on = _On(stream)
-    x, bias = on.whole(x), _vector(on, bias, N, "bias")
+    d = _drop(drop, device)
+    handle, on = _on(stream, device)
+    x, bias = _whole(x, on), _vector(bias, N, device, "bias", on)
     if residual is not None:
-        residual = on.whole(_like(residual, x.shape, "residual"))
-    y = _output(on, out, x.shape, dtype, x.device)
+        residual = _whole(_like(residual, x.shape, device, "residual"), on)
+    y = _output(out, x, x.shape, dtype, on)
     _check(lib().lba_dropout(_at(x), _TYPE[x.dtype], scale, _at(bias), act, d, _at(residual),
-                             _TYPE[residual.dtype] if residual is not None else F32, _at(y), y_type, fmt, M, N, on.handle))
+                             _TYPE[residual.dtype] if residual is not None else F32, _at(y), y_type, fmt, M, N, handle))
     return y
 
 
 def dropout_bwd(G, drop, x=None, bias=None, act=ACT_NONE, scale=1.0, want_dx=True, want_dbias=False, out_dtype=None, stream=None):
     """Gradients of dropout: (dx or None, dbias or None).  x and bias are needed where act is not ACT_NONE; dx is of x's type, of
     out_dtype without x, of G's without both.  The residual's gradient is G."""
-    M, N = _rows(G, "G")
+    M, N, device = _rows(G, "G")
     dtype = x.dtype if x is not None else out_dtype or G.dtype
     if out_dtype is not None and out_dtype != dtype:
         raise ValueError("dx has x's type")
     if x is not None:
-        _like(x, G.shape, "x")
+        _like(x, G.shape, device, "x")
     elif act != ACT_NONE:
         raise ValueError("the gradient of an activation needs x")
-    if dtype not in (torch.float32, torch.bfloat16):
+    if dtype not in _REAL:
         raise TypeError("dx is torch.float32 or torch.bfloat16")
-    d = _drop(drop)
-    on = _On(stream)
-    G, bias = on.whole(G), _vector(on, bias, N, "bias")
-    if x is not None:
-        x = on.whole(x)
-    dx = on.empty(G.shape, dtype, G.device) if want_dx else None
-    dbias = on.empty((N,), torch.float32, G.device) if want_dbias else None
-    size = lib().lba_dropout_bwd_workspace_bytes(M, N) if want_dbias else 0
-    ws = on.empty((size,), torch.uint8, G.device) if size else None
+    d = _drop(drop, device)
+    handle, on = _on(stream, device)
+    G, x, bias = _whole(G, on), _whole(x, on), _vector(bias, N, device, "bias", on)
+    dx = _empty_as(G, dtype, on) if want_dx else None
+    dbias = _empty((N,), torch.float32, G.device, on) if want_dbias else None
+    size = _layer_bytes("lba_dropout_bwd_workspace_bytes", M, N) if want_dbias else 0
+    ws = _workspace(size, G.device, on)
     _check(lib().lba_dropout_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[dtype], scale, _at(bias), act, d, _at(dx), _at(dbias), M, N,
-                                 _at(ws), size, on.handle))
+                                 _at(ws), size, handle))
     return dx, dbias
 
 
 def _codes2(A, B, gated):
-    """(M, N, K) of the operands of a dense product: A [..., K], B [N, K], gated [2 N, K]."""
-    M, K = _rows(A, "A", (torch.uint8,))
-    if B.dtype != torch.uint8 or not B.is_cuda:
-        raise TypeError("B must be a device tensor of torch.uint8 codes")
+    """(M, N, K, device) of the operands of a dense product: A [..., K], B [N, K], gated [2 N, K]."""
+    M, K, device = _rows(A, "A", (torch.uint8,))
+    if B.dtype != torch.uint8 or B.get_device() != device:
+        raise TypeError("B must be a tensor of torch.uint8 codes on A's device")
     if B.dim() != 2 or B.shape[1] != K or (gated and B.shape[0] % 2):
         raise ValueError("B must be [%s, %d]" % ("2 N" if gated else "N", K))
-    if K == 0:
-        M = 1
-        for n in A.shape[:-1]:
-            M *= n
-    return M, B.shape[0] // 2 if gated else B.shape[0], K
+    return M, B.shape[0] // 2 if gated else B.shape[0], K, device
 
 
 def dense(A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, residual=None, drop=None, gated=False, out_dtype=torch.float32,
           out_fmt=None, out=None, stream=None):
     """residual + keep * act(A . B^T + bias) / (1 - p) on codes A [..., K], B [N, K] with float32 accumulation; gated:
     act(A . Bg^T + bg) * (A . Bu^T + bu) with B [2 N, K] and bias [2 N], the gate's rows first.  drop = (p, seed, stream[, step]) or None."""
-    M, N, K = _codes2(A, B, gated)
+    M, N, K, device = _codes2(A, B, gated)
     y_type, y_fmt = _out_type(out_dtype, out_fmt)
-    d = _drop(drop)
-    on = _On(stream)
-    A, B, bias = on.whole(A), on.whole(B), _vector(on, bias, 2 * N if gated else N, "bias")
+    d = _drop(drop, device)
+    handle, on = _on(stream, device)
+    A, B, bias = _whole(A, on), _whole(B, on), _vector(bias, 2 * N if gated else N, device, "bias", on)
     shape = A.shape[:-1] + (N,)
     if residual is not None:
-        residual = on.whole(_like(residual, shape, "residual"))
-    y = _output(on, out, shape, out_dtype, A.device)
-    L, fa, fb, a, b = lib(), infmt(fmt_a), infmt(fmt_b), _at(A), _at(B)
-    size = L.lba_dense_workspace_bytes(M, N, K, fa, fb, gated, ((a or 0) | (b or 0)) % 16 == 0)
-    ws = on.empty((size,), torch.uint8, A.device) if size else None
-    _check(L.lba_dense(a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(residual), _TYPE[residual.dtype] if residual is not None else F32,
-                       _at(y), y_type, y_fmt, _at(ws), size, on.handle))
+        residual = _whole(_like(residual, shape, device, "residual"), on)
+    y = _output(out, A, shape, out_dtype, on)
+    fa, fb, a, b = _infmt(fmt_a), _infmt(fmt_b), _at(A), _at(B)
+    size = _layer_bytes("lba_dense_workspace_bytes", M, N, K, fa, fb, gated, ((a or 0) | (b or 0)) % 16 == 0)
+    ws = _workspace(size, A.device, on)
+    _check(lib().lba_dense(a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(residual),
+                           _TYPE[residual.dtype] if residual is not None else F32, _at(y), y_type, y_fmt, _at(ws), size, handle))
     return y
 
 
@@ -844,17 +879,18 @@ def dense_bwd(G, A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, drop=N
               want_dbias=False, stream=None):
     """Gradients of dense: (dA, dB of G's type, dbias float32; None where not asked for), of the operands' real values.  The sums that an
     activation or a gate needs are computed again from A, B and bias.  The residual's gradient is G."""
-    M, N, K = _codes2(A, B, gated)
-    _like(G, A.shape[:-1] + (N,), "G")
-    d = _drop(drop)
-    on = _On(stream)
+    M, N, K, device = _codes2(A, B, gated)
+    _like(G, A.shape[:-1] + (N,), device, "G")
+    d = _drop(drop, device)
+    handle, on = _on(stream, device)
     cols = 2 * N if gated else N
-    G, A, B, bias = on.whole(G), on.whole(A), on.whole(B), _vector(on, bias, cols, "bias")
-    dA = on.empty(A.shape, G.dtype, A.device) if want_da else None
-    dB = on.empty(B.shape, G.dtype, A.device) if want_db else None
-    dbias = on.empty((cols,), torch.float32, A.device) if want_dbias else None
-    L, fa, fb, a, b, t = lib(), infmt(fmt_a), infmt(fmt_b), _at(A), _at(B), _TYPE[G.dtype]
-    size = L.lba_dense_bwd_workspace_bytes(M, N, K, fa, fb, gated, act, t, ((a or 0) | (b or 0)) % 16 == 0)
-    ws = on.empty((size,), torch.uint8, A.device) if size else None
-    _check(L.lba_dense_bwd(_at(G), t, a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(dA), _at(dB), _at(dbias), _at(ws), size, on.handle))
+    G, A, B, bias = _whole(G, on), _whole(A, on), _whole(B, on), _vector(bias, cols, device, "bias", on)
+    dA = _empty_as(A, G.dtype, on) if want_da else None
+    dB = _empty_as(B, G.dtype, on) if want_db else None
+    dbias = _empty((cols,), torch.float32, A.device, on) if want_dbias else None
+    fa, fb, a, b, t = _infmt(fmt_a), _infmt(fmt_b), _at(A), _at(B), _TYPE[G.dtype]
+    size = _layer_bytes("lba_dense_bwd_workspace_bytes", M, N, K, fa, fb, gated, act, t, ((a or 0) | (b or 0)) % 16 == 0)
+    ws = _workspace(size, A.device, on)
+    _check(lib().lba_dense_bwd(_at(G), t, a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(dA), _at(dB), _at(dbias), _at(ws), size,
+                               handle))
     return dA, dB, dbias
