@@ -190,11 +190,14 @@ __device__ __forceinline__ void store_eight(bf16_t* to, const At& i, int pieces,
     for (int q = 0; q < 3; ++q) *(u16x8*)at(to + q * piece, i) = w[q];
 }
 
-// which tile a workgroup takes: consecutive workgroups go to the eight dies in turn, so that a die gets a contiguous run of tiles, and
-// a run goes down eight tiles of m before it moves on in n: both operands of a run are shared in the die's L2
-__device__ __forceinline__ void tile_of(int gx, int gy, int id, int& tm, int& tn) {
-    const int total = gx * gy, per = total / 8, rem = total % 8, die = id % 8, local = id / 8;
-    const int t = die * per + (die < rem ? die : rem) + local;
+// Which slice and tile a workgroup takes: consecutive workgroups go to the eight dies in turn, so that a die gets a contiguous run, of one
+// slice before the next: the columns of a slice are read by the dies that have it.  A run goes down eight tiles of m before it moves on in n:
+// both operands of a run are shared in the die's L2.
+__device__ __forceinline__ void tile_of(int gx, int gy, int slices, int id, int& slice, int& tm, int& tn) {
+    const int tiles = gx * gy, total = slices > 1 ? tiles * slices : tiles, per = total / 8, rem = total % 8, die = id % 8, local = id / 8;
+    int t = die * per + (die < rem ? die : rem) + local;
+    slice = slices > 1 ? t / tiles : 0;
+    t -= slice * tiles;
     const int wide = 8 * gy, group = t / wide, first = group * 8, in = t % wide;
     const int rows = gx - first < 8 ? gx - first : 8;
     tm = first + in % rows;
@@ -246,10 +249,8 @@ __global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(Ge
     __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(BM + BN) * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wm = wave / WN, wn = wave % WN;
-    int tm, tn;
-    const int id = second ? (int)blockIdx.x - both.blocks : (int)blockIdx.x;
-    const int slice = p.slices > 1 ? id / (p.gx * p.gy) : 0;
-    tile_of(p.gx, p.gy, id - slice * (p.gx * p.gy), tm, tn);
+    int slice, tm, tn;
+    tile_of(p.gx, p.gy, p.slices, second ? (int)blockIdx.x - both.blocks : (int)blockIdx.x, slice, tm, tn);
     const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
 
     // staging: lane's rows and its piece of each

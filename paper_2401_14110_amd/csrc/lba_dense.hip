@@ -159,7 +159,7 @@ struct TileCost { int tile, per_cu; float fixed, step, fixed1, step1; };
 static const TileCost kCodes[] = {
     {TILE_256, 1, 9.0f, 2.45f, 9.0f, 2.3f}, {TILE_192, 1, 7.0f, 1.9f, 7.0f, 1.85f}, {TILE_128, 2, 4.0f, 1.45f, 2.7f, 0.95f}, {TILE_64, 4, 2.6f, 0.95f, 0.6f, 0.47f}};
 static const TileCost kRows[] = {
-    {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.5f}, {TILE_128, 2, 4.0f, 1.0f, 2.7f, 0.85f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f},
+    {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.75f}, {TILE_128, 2, 4.0f, 0.97f, 2.7f, 0.85f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f},
     {TILE_64, 4, 2.6f, 0.62f, 0.6f, 0.55f}, {TILE_64_DEEP, 2, 1.4f, 0.5f, 0.6f, 0.42f}};
 constexpr float kLaunch = 4.5f, kJoinRate = 6e6f;         // a launch alone; bytes a microsecond that the join moves
 constexpr int kCus = 256;
