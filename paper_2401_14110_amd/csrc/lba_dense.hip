@@ -20,7 +20,7 @@ struct LayJob {
     int64_t ld;              // bytes of a row of dst
     int32_t K;
     int32_t wide;            // LAY_TRANSPOSED: R rounded up to 8: columns of dst, zeros from R on
-    int32_t tiles_k;         // LAY_TRANSPOSED: tiles of 64 along k
+    int32_t tiles_k;         // LAY_TRANSPOSED: tiles along k
     int32_t kind;
     uint32_t first;
     CodeBits bits;
@@ -30,11 +30,11 @@ struct LayJobs { LayJob job[5]; int32_t n; };
 // rows of codes or of bfloat16 numbers, zeros behind K: 16 bytes of output a lane
 template <bool BF16> __device__ __forceinline__ void lay_rows(const LayJob& p, int64_t block) {
     constexpr int PER = BF16 ? 8 : 16;
-    const int64_t per_row = p.ld / 16, i = block * 256 + threadIdx.x;
-    if (i >= p.R * per_row) return;
-    const int64_t r = i / per_row;
+    const uint32_t per_row = (uint32_t)(p.ld / 16), i = (uint32_t)block * 256 + threadIdx.x;   // fewer than 2^30 pieces (lay_fits)
+    if (i >= (uint32_t)p.R * per_row) return;
+    const uint32_t r = i / per_row;
     const int k = (int)(i - r * per_row) * PER;
-    const uint8_t* s = p.src + r * p.K + k;
+    const uint8_t* s = p.src + (int64_t)r * p.K + k;
     uint32_t w[PER / 4];
     if (k + PER <= p.K) {
         typedef uint32_t words __attribute__((ext_vector_type(PER / 4), aligned(1)));
@@ -57,38 +57,52 @@ template <bool BF16> __device__ __forceinline__ void lay_rows(const LayJob& p, i
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = (int32_t)w[j];
     }
-    *(i32x4*)(p.dst + r * p.ld + (i - r * per_row) * 16) = o;
+    *(i32x4*)(p.dst + (int64_t)r * p.ld + (i - r * per_row) * 16) = o;
 }
 
-// dst [K][ld] bfloat16: 64 x 64 codes through LDS, read along k, written along the rows
+// dst [K][ld] bfloat16: 64 rows of 128 codes through LDS.  A lane reads four neighbouring codes of eight rows and writes four pieces of 16 bytes,
+// eight lanes side by side; rows of 33 words put the words that a wave reads at a time into 64 different banks.
+constexpr int kLayK = 128;
 __device__ __forceinline__ void lay_transposed(const LayJob& p, int64_t block) {
-    __shared__ uint8_t t[64][68];
+    __shared__ uint32_t t[64][kLayK / 4 + 1];
     const int64_t r0 = block / p.tiles_k * 64;
-    const int k0 = (int)(block % p.tiles_k) * 64;
-    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-        const int r = i / 16, k = (i % 16) * 4;
-        uint32_t w = 0;
-        if (r0 + r < p.R) {
-            const uint8_t* s = p.src + (r0 + r) * p.K + k0 + k;
-            typedef uint32_t word_any __attribute__((aligned(1)));
-            if (k0 + k + 4 <= p.K) w = *(const word_any*)s;
-            else
-                for (int j = 0; j < 4; ++j)
-                    if (k0 + k + j < p.K) w |= (uint32_t)s[j] << (8 * j);
+    const int k0 = (int)(block % p.tiles_k) * kLayK;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = h * 256 + threadIdx.x, r = i / 8, c = i % 8, k = k0 + c * 16;
+        u32x4 w = {0, 0, 0, 0};
+        if (r0 + r < p.R && k < p.K) {
+            const uint8_t* s = p.src + (r0 + r) * p.K + k;
+            if (k + 16 <= p.K) {
+                typedef uint32_t words __attribute__((ext_vector_type(4), aligned(1)));
+                w = *(const words*)s;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
+            }
         }
-        *(uint32_t*)&t[r][k] = w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[r][c * 4 + j] = w[j];
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-        const int k = i / 8, r = (i % 8) * 8;
-        if (k0 + k >= p.K || r0 + r >= p.wide) continue;
+    const int r = threadIdx.x % 8 * 8, kw = threadIdx.x / 8;
+    if (r0 + r >= p.wide) return;
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = t[r + j][kw];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int k = k0 + kw * 4 + q;
+        if (k >= p.K) return;
         i32x4 o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t a = __float_as_uint(code_value(t[r + 2 * j][k], p.bits)), b = __float_as_uint(code_value(t[r + 2 * j + 1][k], p.bits));
+            const uint32_t a = __float_as_uint(code_value((w[2 * j] >> (8 * q)) & 0xFFu, p.bits));
+            const uint32_t b = __float_as_uint(code_value((w[2 * j + 1] >> (8 * q)) & 0xFFu, p.bits));
             o[j] = (int32_t)__builtin_amdgcn_perm(b, a, 0x07060302u);
         }
-        *(i32x4*)(p.dst + (k0 + k) * p.ld + (r0 + r) * 2) = o;
+        *(i32x4*)(p.dst + k * p.ld + (r0 + r) * 2) = o;
     }
 }
 
@@ -336,7 +350,7 @@ static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* d
     LayJob& j = jobs.job[jobs.n++];
     j.src = src; j.dst = (uint8_t*)dst; j.R = R; j.ld = ld; j.K = (int32_t)K; j.kind = kind; j.first = blocks; j.bits = make_code_bits(f);
     j.wide = (int32_t)up_to(R, 8);
-    j.tiles_k = (int32_t)((K + 63) / 64);
+    j.tiles_k = (int32_t)((K + kLayK - 1) / kLayK);
     blocks += (uint32_t)(kind == LAY_TRANSPOSED ? j.tiles_k * ((R + 63) / 64) : (R * (ld / 16) + 255) / 256);
 }
 // a job's workgroups take 2048 codes or more: five jobs stay under 2^32 lanes
