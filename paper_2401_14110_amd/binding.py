@@ -695,7 +695,7 @@ def _empty_as(t, dtype, on):
     return t
 
 
-def _workspace(size, device, on):
+def _scratch(size, device, on):
     return _empty((size,), torch.uint8, device, on) if size else None
 
 
@@ -795,7 +795,7 @@ def layernorm_bwd(G, x, gamma, mean, rstd, want_dx=True, want_params=True, strea
     dgamma = _empty((N,), torch.float32, x.device, on) if want_params else None
     dbeta = _empty((N,), torch.float32, x.device, on) if want_params else None
     size = _layer_bytes("lba_layernorm_bwd_workspace_bytes", M, N) if want_params else 0
-    ws = _workspace(size, x.device, on)
+    ws = _scratch(size, x.device, on)
     _check(lib().lba_layernorm_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[x.dtype], _at(gamma), _at(mean), _at(rstd), _at(dx),
                                    _at(dgamma), _at(dbeta), M, N, _at(ws), size, handle))
     return dx, dgamma, dbeta
@@ -838,7 +838,7 @@ def dropout_bwd(G, drop, x=None, bias=None, act=ACT_NONE, scale=1.0, want_dx=Tru
     dx = _empty_as(G, dtype, on) if want_dx else None
     dbias = _empty((N,), torch.float32, G.device, on) if want_dbias else None
     size = _layer_bytes("lba_dropout_bwd_workspace_bytes", M, N) if want_dbias else 0
-    ws = _workspace(size, G.device, on)
+    ws = _scratch(size, G.device, on)
     _check(lib().lba_dropout_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[dtype], scale, _at(bias), act, d, _at(dx), _at(dbias), M, N,
                                  _at(ws), size, handle))
     return dx, dbias
@@ -869,7 +869,7 @@ def dense(A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, residual=None
     y = _output(out, A, shape, out_dtype, on)
     fa, fb, a, b = _infmt(fmt_a), _infmt(fmt_b), _at(A), _at(B)
     size = _layer_bytes("lba_dense_workspace_bytes", M, N, K, fa, fb, gated, ((a or 0) | (b or 0)) % 16 == 0)
-    ws = _workspace(size, A.device, on)
+    ws = _scratch(size, A.device, on)
     _check(lib().lba_dense(a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(residual),
                            _TYPE[residual.dtype] if residual is not None else F32, _at(y), y_type, y_fmt, _at(ws), size, handle))
     return y
@@ -890,7 +890,7 @@ def dense_bwd(G, A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, drop=N
     dbias = _empty((cols,), torch.float32, A.device, on) if want_dbias else None
     fa, fb, a, b, t = _infmt(fmt_a), _infmt(fmt_b), _at(A), _at(B), _TYPE[G.dtype]
     size = _layer_bytes("lba_dense_bwd_workspace_bytes", M, N, K, fa, fb, gated, act, t, ((a or 0) | (b or 0)) % 16 == 0)
-    ws = _workspace(size, A.device, on)
+    ws = _scratch(size, A.device, on)
     _check(lib().lba_dense_bwd(_at(G), t, a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(dA), _at(dB), _at(dbias), _at(ws), size,
                                handle))
     return dA, dB, dbias
