@@ -240,7 +240,7 @@ template <int ELEM> __device__ __forceinline__ f32x4 product_16x16x32(i32x4 b, i
 
 // WM x WN waves of FM x FN fragments of 16 x 16, NST buffers of a step
 template <int ELEM, int WM, int WN, int FM, int FN, int NST, bool GATED, int EPI>
-__global__ __launch_bounds__(WM * WN * 64, FM == 2 ? 4 : 2) void dense_kernel(GemmPair both) {
+__global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)) void dense_kernel(GemmPair both) {
     const bool second = (int)blockIdx.x >= both.blocks;
     const GemmParams& p = both.g[second];
     constexpr int THREADS = WM * WN * 64, BM = WM * FM * 16, BN = WN * FN * 16;

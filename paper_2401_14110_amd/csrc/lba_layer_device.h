@@ -199,45 +199,57 @@ __device__ __forceinline__ uint64_t drop_base(const DropParams& d) {
     const uint64_t s = d.stream + (d.step ? *d.step : 0ull);
     return mix64(mix64(d.seed * 2 + 1) ^ ((s * 2 + 1) * kGolden));
 }
-// the words of V / 4 consecutive groups of four elements -> which of them stay
-template <int V> __device__ __forceinline__ void kept_of(const uint64_t (&u)[(V + 3) / 4], const DropParams& d, bool (&keep)[V]) {
+// 32-bit halves of the generator's words, two elements each -> which of the elements stay
+template <int V> __device__ __forceinline__ void kept_of(const uint32_t (&h)[V / 2], const DropParams& d, bool (&keep)[V]) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const uint32_t half = (uint32_t)(u[j / 4] >> (32 * ((j % 4) / 2)));
-        keep[j] = (j % 2 ? half : half << 16) > d.above;         // what is below the high half decides nothing
-    }
+    for (int j = 0; j < V; ++j) keep[j] = (j % 2 ? h[j / 2] : h[j / 2] << 16) > d.above;           // what is below the high half decides nothing
+}
+// The halves from element `i % 4` of the first word on: `h` has two more halves than come out.  In 32-bit steps: a 64-bit shift whose amount is
+// a register read its amount wrong on gfx950 where that was the last one of the wave's allocation (8192 x 4107 bfloat16 elements with GELU:
+// thousands of wrong bits, others from run to run), and the compiler does not keep it off that register.
+template <int H> __device__ __forceinline__ void halves_from(uint64_t i, const uint32_t (&h)[H + 2], uint32_t (&out)[H]) {
+    const bool odd_half = (i & 2) != 0;
+    const uint32_t bits = ((uint32_t)i & 1u) * 16;
+    uint32_t s[H + 1];
+#pragma unroll
+    for (int j = 0; j <= H; ++j) s[j] = odd_half ? h[j + 1] : h[j];
+#pragma unroll
+    for (int j = 0; j < H; ++j) out[j] = __builtin_amdgcn_alignbit(s[j + 1], s[j], bits);
 }
 // Which of V consecutive elements from index i on stay.  `whole`: i is a multiple of 4 (uniform: where rows are multiples of 4); else the
-// elements' bits are cut out of two neighbouring words.
+// elements' bits are cut out of one more word.
 template <int V> __device__ __forceinline__ void drop_keeps(uint64_t i, uint64_t base, const DropParams& d, bool whole, bool (&keep)[V]) {
-    constexpr int Q = (V + 3) / 4;
-    const uint32_t shift = ((uint32_t)i & 3u) * 16;
-    uint64_t z = (i >> 2) * kGolden + base, u[Q];
+    static_assert(V % 4 == 0, "whole words");
+    uint64_t z = (i >> 2) * kGolden + base;
+    uint32_t h[V / 2 + 2], out[V / 2];
 #pragma unroll
-    for (int q = 0; q < Q; ++q, z += kGolden) u[q] = mix64(z);
+    for (int q = 0; q < V / 4; ++q, z += kGolden) {
+        const uint64_t u = mix64(z);
+        out[2 * q] = h[2 * q] = (uint32_t)u;
+        out[2 * q + 1] = h[2 * q + 1] = (uint32_t)(u >> 32);
+    }
     if (!whole) {
         const uint64_t last = mix64(z);
-#pragma unroll
-        for (int q = 0; q < Q; ++q) u[q] = (u[q] >> shift) | (((q + 1 < Q ? u[q + 1] : last) << 1) << (63 - shift));
+        h[V / 2] = (uint32_t)last;
+        h[V / 2 + 1] = (uint32_t)(last >> 32);
+        halves_from<V / 2>(i, h, out);
     }
-    kept_of<V>(u, d, keep);
+    kept_of<V>(out, d, keep);
 }
 // The same for a wave whose 64 lanes hold neighbouring groups of 8 elements of one row, the first of index `first` (uniform): the word behind a lane's two
 // is its neighbour's first, and the last lane's is made once for the wave.
 __device__ __forceinline__ void drop_keeps_wave(uint64_t first, uint64_t base, const DropParams& d, bool whole, bool (&keep)[8]) {
-    const uint32_t shift = ((uint32_t)first & 3u) * 16;
     const uint64_t row = (first >> 2) * kGolden + base;  // uniform
-    const uint64_t z = row + (uint64_t)(2 * (threadIdx.x & 63)) * kGolden;
-    uint64_t u[2] = {mix64(z), mix64(z + kGolden)};
+    const uint64_t z = row + (uint64_t)(2 * (threadIdx.x & 63)) * kGolden, u0 = mix64(z), u1 = mix64(z + kGolden);
+    uint32_t out[4] = {(uint32_t)u0, (uint32_t)(u0 >> 32), (uint32_t)u1, (uint32_t)(u1 >> 32)};
     if (!whole) {
         const uint64_t last = mix64(row + 128 * kGolden);
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)(uint32_t)last, (int)(uint32_t)u[0], 0x130, 0xF, 0xF, false);
-        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(last >> 32), (int)(u[0] >> 32), 0x130, 0xF, 0xF, false);
-        const uint64_t next = ((uint64_t)hi << 32) | lo;
-        u[0] = (u[0] >> shift) | ((u[1] << 1) << (63 - shift));
-        u[1] = (u[1] >> shift) | ((next << 1) << (63 - shift));
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)(uint32_t)last, (int)out[0], 0x130, 0xF, 0xF, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(last >> 32), (int)out[1], 0x130, 0xF, 0xF, false);
+        const uint32_t h[6] = {out[0], out[1], out[2], out[3], lo, hi};
+        halves_from<4>(first, h, out);
     }
-    kept_of<8>(u, d, keep);
+    kept_of<8>(out, d, keep);
 }
 
 // ---- sums over a wave -----------------------------------------------------------------------

@@ -58,6 +58,18 @@ def test_mask_is_the_generators_and_the_same_in_both_passes():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", [lb.ACT_NONE, lb.ACT_RELU, lb.ACT_GELU, lb.ACT_SILU])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_masks_of_many_rows_that_end_inside_a_word(act, dtype):
+    """Every bit of the mask, both passes, where the chip is full and the elements' bits are cut out of two words."""
+    M, N = 8192, 4107
+    x = torch.ones(M, N, device=DEV, dtype=torch.float32 if dtype == "f32" else torch.bfloat16)
+    keep = torch.from_numpy(lo.drop_factors(0.5, 7, 3, 0, M * N).reshape(M, N) > 0).to(DEV)
+    assert torch.equal(lb.dropout(x, (0.5, 7, 3), act=act) != 0, keep)
+    assert torch.equal(lb.dropout_bwd(x, (0.5, 7, 3), x=x, act=act)[0] != 0, keep)
+
+
+@pytest.mark.gpu
 def test_rates_at_the_ends_and_values_that_are_dropped():
     x = torch.randn(33, 130, device=DEV)
     r = torch.randn(33, 130, device=DEV)
