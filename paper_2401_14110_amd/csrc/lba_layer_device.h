@@ -208,11 +208,11 @@ template <int V> __device__ __forceinline__ void kept_of(const uint32_t (&h)[V /
 // a register read its amount wrong on gfx950 where that was the last one of the wave's allocation (8192 x 4107 bfloat16 elements with GELU:
 // thousands of wrong bits, others from run to run), and the compiler does not keep it off that register.
 template <int H> __device__ __forceinline__ void halves_from(uint64_t i, const uint32_t (&h)[H + 2], uint32_t (&out)[H]) {
-    const bool odd_half = (i & 2) != 0;
+    const uint32_t later = 0u - (((uint32_t)i >> 1) & 1u);                           // all ones: one half further (by masks: a choice of
     const uint32_t bits = ((uint32_t)i & 1u) * 16;
     uint32_t s[H + 1];
 #pragma unroll
-    for (int j = 0; j <= H; ++j) s[j] = odd_half ? h[j + 1] : h[j];
+    for (int j = 0; j <= H; ++j) s[j] = (h[j + 1] & later) | (h[j] & ~later);        // elements would put them into scratch memory)
 #pragma unroll
     for (int j = 0; j < H; ++j) out[j] = __builtin_amdgcn_alignbit(s[j + 1], s[j], bits);
 }
