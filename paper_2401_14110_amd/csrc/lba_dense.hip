@@ -142,7 +142,8 @@ template <bool GATED> __global__ __launch_bounds__(256) void dense_join_kernel(J
                 if (GATED) u[j] += w[j];
             }
         }
-        with_act(e.act, [&](auto act) { finish_forward<GATED, false, decltype(act)::value, 4>(e, columns_of<GATED, 4>(e, n), base, (int)m, At{m * e.N + n, 0}, z, u, r); });
+        const Columns<GATED, 4> cols = columns_of<GATED, 4>(e, n);
+        with_act(e.act, [&](auto act) { finish_forward<GATED, false, decltype(act)::value, 4>(e, cols, base, (int)m, At{m * e.N + n, 0}, z, u, r); });
     }
 }
 

@@ -165,7 +165,8 @@ template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const
     return r;
 }
 
-// The next row of a lane group is loaded while this one is worked on (two sets of registers, so that none is moved while in flight).
+// The next row of a lane group is loaded while this one is worked on (two sets of registers, so that none is moved while in flight), but for
+// workgroups of 1024 lanes, whose 128 registers do not hold both.
 template <typename TG, typename TX, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
@@ -228,16 +229,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams 
         }
     };
     const int64_t step = (int64_t)gridDim.x * RPB;
-    Row a, b;
     int64_t row = (int64_t)blockIdx.x * RPB + sub;
-    if (row < p.M) load(row, a);
-    for (; row < p.M; row += 2 * step) {
-        const bool more = row + step < p.M;
-        if (more) load(row + step, b);
-        work(row, a);
-        if (!more) break;
-        if (row + 2 * step < p.M) load(row + 2 * step, a);
-        work(row + step, b);
+    Row a;
+    if constexpr (T >= 1024) {
+        for (; row < p.M; row += step) {
+            load(row, a);
+            work(row, a);
+        }
+    } else {
+        Row b;
+        if (row < p.M) load(row, a);
+        for (; row < p.M; row += 2 * step) {
+            const bool more = row + step < p.M;
+            if (more) load(row + step, b);
+            work(row, a);
+            if (!more) break;
+            if (row + 2 * step < p.M) load(row + 2 * step, a);
+            work(row + step, b);
+        }
     }
     if (!p.part) return;
     if (RPB > 1) {                                       // the workgroup's rows first: one after the other into LDS
