@@ -170,12 +170,15 @@ static size_t split_bytes(const Product& p) { return p.slices > 1 ? align256((si
 // What a launch takes, in microseconds: a tile's workgroup needs `fixed` and `step` for each step where every CU holds `per_cu` of them, and
 // `fixed1` and `step1` where it has the CU to itself.  Measured on grids of 1 to 8 rounds and 1 to 64 steps (4096 x 4096 and 1024 x 1024 outputs,
 // K = 128 to 4096); a step of codes is 128 long, of bfloat16 rows 64.
-struct TileCost { int tile, per_cu; float fixed, step, fixed1, step1; };
+// `f16`: what a step of codes that become FP16 numbers takes, whose conversions are five instructions for E4M3's two, and the more of them the
+// smaller a wave's part of the tile is.
+struct TileCost { int tile, per_cu; float fixed, step, fixed1, step1, f16; };
 static const TileCost kCodes[] = {
-    {TILE_256, 1, 9.0f, 2.45f, 9.0f, 2.3f}, {TILE_192, 1, 7.0f, 1.9f, 7.0f, 1.85f}, {TILE_128, 2, 4.0f, 1.45f, 2.7f, 0.95f}, {TILE_64, 4, 2.6f, 0.95f, 0.6f, 0.47f}};
+    {TILE_256, 1, 9.0f, 2.45f, 9.0f, 2.3f, 1.2f}, {TILE_192, 1, 7.0f, 1.9f, 7.0f, 1.85f, 1.25f},
+    {TILE_128, 2, 4.0f, 1.45f, 2.7f, 0.95f, 1.33f}, {TILE_64, 4, 2.6f, 0.95f, 0.6f, 0.47f, 1.5f}};
 static const TileCost kRows[] = {
-    {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.75f}, {TILE_128, 2, 4.0f, 0.97f, 2.7f, 0.85f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f},
-    {TILE_64, 4, 2.6f, 0.62f, 0.6f, 0.55f}, {TILE_64_DEEP, 2, 1.4f, 0.5f, 0.6f, 0.42f}};
+    {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.75f, 1.0f}, {TILE_128, 2, 4.0f, 0.97f, 2.7f, 0.85f, 1.0f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f, 1.0f},
+    {TILE_64, 4, 2.6f, 0.62f, 0.6f, 0.55f, 1.0f}, {TILE_64_DEEP, 2, 1.4f, 0.5f, 0.6f, 0.42f, 1.0f}};
 constexpr float kLaunch = 4.5f, kJoinRate = 6e6f;         // a launch alone; bytes a microsecond that the join moves
 constexpr int kCus = 256;
 
@@ -219,12 +222,12 @@ enum { PLAN_FORWARD = 0, PLAN_BACKWARD = 1 };             // with the backward e
 static int plan_tile(Product* p, int n, int elem, int kind, bool gated) {
     const TileCost* all = elem == ELEM_BF16 ? kRows : kCodes;
     const int count = elem == ELEM_BF16 ? (int)(sizeof(kRows) / sizeof(kRows[0])) : (int)(sizeof(kCodes) / sizeof(kCodes[0]));
-    const float step_scale = elem == ELEM_F16 ? 1.25f : 1.0f;                        // its conversions take five instructions for E4M3's two
     static const int kSlices[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
     int best = TILE_64;
     double least = 1e300;
     Product cut_best[2];
     for (int t = 0; t < count; ++t) {
+        const float step_scale = elem == ELEM_F16 ? all[t].f16 : 1.0f;
         if (kind == PLAN_BACKWARD && all[t].tile != TILE_128 && all[t].tile != TILE_64) continue;
         if (gated && (all[t].tile == TILE_128_DEEP || all[t].tile == TILE_64_DEEP)) continue;          // built for plain products
         const int64_t slots = (int64_t)kCus * all[t].per_cu;

@@ -301,12 +301,7 @@ int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type
     if (dbias) {
         // full strips and the tail are cut into chunks of their own number
         const int64_t full = (int64_t)p.strips * 64 * (x_type == LBA_F32 ? 4 : 8);
-        if (p.main_chunks == p.tail_chunks || full == 0 || full == N)
-            launch_column_sum(p.part, full == 0 ? p.tail_chunks : p.main_chunks, N, dbias, nullptr, N, st);
-        else {
-            launch_column_sum(p.part, p.main_chunks, N, dbias, nullptr, full, st);
-            launch_column_sum(p.part + full, p.tail_chunks, N, dbias + full, nullptr, N - full, st);
-        }
+        launch_column_sum(p.part, p.main_chunks, N, dbias, nullptr, N, st, full, p.tail_chunks);
     }
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }

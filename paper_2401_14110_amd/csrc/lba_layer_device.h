@@ -271,8 +271,9 @@ __device__ __forceinline__ float wave_sum(float v) {
 // ---- column sums ----------------------------------------------------------------------------
 
 // out0[n] = sum over `parts` rows of part[row * ld + n], and with out1 out1[n] that of part[row * ld + N + n] (out0 may be null then),
-// always in the same order
-void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st);
+// always in the same order; columns from `split` on have `parts2` rows
+void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st, int64_t split = INT64_MAX,
+                       int64_t parts2 = 0);
 // zeros (an even number of bytes; a kernel, so that it can be captured)
 void launch_zero(void* out, int64_t bytes, hipStream_t st);
 

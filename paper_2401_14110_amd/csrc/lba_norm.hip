@@ -347,11 +347,13 @@ __global__ __launch_bounds__(256) void norm_bwd_long_params_kernel(NormParams p)
 
 // A workgroup takes 16 columns: thread t adds every 64th row of column t % 16, eight loads in flight, then the 64 sums of a column are added
 // in a fixed order.  (One lane a column and four rows in flight left the loads' latency bare: 1024 rows of 1536 columns took 23 us.)
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N) {
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, int64_t split,
+                                                         int64_t parts2) {
     __shared__ float lds[16][16];
     const int c = threadIdx.x & 15;
     const int64_t n = (int64_t)blockIdx.x * 16 + c;
     const int64_t cols = out1 ? 2 * N : N;
+    if (n >= split) parts = parts2;
     float s = 0.0f;
     if (n < cols) {
         int64_t r = threadIdx.x / 16;
@@ -378,9 +380,9 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int
     else if (out0) out0[n] = total;
 }
 
-void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st) {
+void launch_column_sum(const float* part, int64_t parts, int64_t ld, float* out0, float* out1, int64_t N, hipStream_t st, int64_t split, int64_t parts2) {
     const int64_t cols = out1 ? 2 * N : N;
-    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, part, parts, ld, out0, out1, N);
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, part, parts, ld, out0, out1, N, split, parts2);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* out, int64_t n) {
