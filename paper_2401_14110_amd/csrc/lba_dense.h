@@ -61,12 +61,11 @@ struct GemmParams {
     const uint8_t* A;
     const uint8_t* B;
     int64_t lda, ldb;        // bytes from row to row
-    int64_t a_piece;         // bytes from piece to piece of A (a sum over pieces of A against the same B)
-    int32_t pieces;
+    int64_t a_piece;         // bytes from piece to piece of A where it comes in three
     int32_t rows_a, rows_b;
     int32_t half;            // gated: first row of B's second half
     int32_t chunks;          // 16-byte pieces of a row
-    int32_t steps;           // steps of 128 bytes over all pieces of A
+    int32_t steps;           // steps of a row: of 128 bytes, of 64 where A comes in three pieces
     int32_t gx, gy;          // tiles over m and n
     int32_t slices;          // > 1: the steps are cut into so many slices of `per_slice`, each of which stores its sums in `split`
     int32_t per_slice;
@@ -238,15 +237,18 @@ template <int ELEM> __device__ __forceinline__ f32x4 product_16x16x32(i32x4 b, i
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b), __builtin_bit_cast(bf16x8_t, a), c, 0, 0, 0);
 }
 
-// WM x WN waves of FM x FN fragments of 16 x 16, NST buffers of a step
-template <int ELEM, int WM, int WN, int FM, int FN, int NST, bool GATED, int EPI>
+// WM x WN waves of FM x FN fragments of 16 x 16, NST buffers of a step.  NA == 3: A comes in three pieces, whose products with a step of B are
+// made together: a step is 64 bytes of a row, and B's rows and fragments are read once for the three.
+template <int ELEM, int WM, int WN, int FM, int FN, int NST, int NA, bool GATED, int EPI>
 __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)) void dense_kernel(GemmPair both) {
     const bool second = (int)blockIdx.x >= both.blocks;
     const GemmParams& p = both.g[second];
     constexpr int THREADS = WM * WN * 64, BM = WM * FM * 16, BN = WN * FN * 16;
-    constexpr int LA = BM * 8 / THREADS, LB = BN * 8 / THREADS;          // pieces a lane stages for a step
-    static_assert(BM * 8 % THREADS == 0 && BN * 8 % THREADS == 0 && (!GATED || FN % 2 == 0), "tile");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(BM + BN) * 128];
+    constexpr int CH16 = NA == 3 ? 4 : 8, ROW = CH16 * 16;               // sixteens of bytes of a row in a step, bytes
+    constexpr int LA = NA * BM * CH16 / THREADS, LB = BN * CH16 / THREADS;           // sixteens that a lane stages for a step
+    static_assert(NA * BM * CH16 % THREADS == 0 && BN * CH16 % THREADS == 0 && THREADS / CH16 <= BM && (!GATED || FN % 2 == 0), "tile");
+    static_assert(NA == 1 || (NA == 3 && ELEM == ELEM_BF16 && !GATED && NST == 2), "three pieces");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(NA * BM + BN) * ROW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wm = wave / WN, wn = wave % WN;
     int slice, tm, tn;
@@ -254,17 +256,18 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
 
     // staging: lane's rows and its piece of each
-    const int piece = (tid & 7) ^ ((tid >> 4) & 7);
+    const int piece = (tid & (CH16 - 1)) ^ ((tid / CH16 / 2) & (CH16 - 1));
     const uint8_t* src[LA + LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        int r = m0 + tid / 8 + i * (THREADS / 8);
+        const int t = tid / CH16 + i * (THREADS / CH16);
+        int r = m0 + t % BM;
         r = r < p.rows_a ? r : p.rows_a - 1;
-        src[i] = p.A + r * p.lda + piece * 16;
+        src[i] = p.A + r * p.lda + t / BM * p.a_piece + piece * 16;
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        const int t = tid / 8 + i * (THREADS / 8);
+        const int t = tid / CH16 + i * (THREADS / CH16);
         int r;
         if (GATED) {                                     // fragments alternate between the halves, so that a wave has both of a column
             const int n = n0 + (t / 32) * 16 + t % 16;
@@ -278,41 +281,28 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
 #pragma unroll
     for (int i = 0; i < LA + LB; ++i) asm volatile("" : "+v"(src[i]));               // one address a load, not a sum of parts at every step
     // what the loop reads of the parameters, once
-    const int steps_row = p.steps / p.pieces, chunks = p.chunks, shift_a = p.shift_a, shift_b = p.shift_b;
+    const int chunks = p.chunks, shift_a = p.shift_a, shift_b = p.shift_b;
     const uint32_t keep_a = p.keep_a, keep_b = p.keep_b;
-    const int64_t a_wrap = p.a_piece - (int64_t)steps_row * 128;                     // from the end of a row to its start in the next piece
     const int first = slice * p.per_slice;
     const int last = p.slices > 1 ? (first + p.per_slice < p.steps ? first + p.per_slice : p.steps) : p.steps;
-    // the step that is staged next: its number in its row, its place in A's and B's rows
-    int at_step = first;
-    int64_t at_b = 0, at_a = 0;
-    if (p.pieces > 1 && first > 0) {
-        at_step = first % steps_row;
-        at_a = first / steps_row * p.a_piece;
-    }
-    at_b = (int64_t)at_step * 128;
-    at_a += at_b;
+    int at_step = first;                                 // the step that is staged next, and its place in the rows
+    int64_t at_byte = (int64_t)first * ROW;
     auto stage = [&](int buf) {
         auto to_lds = [&](int i, const uint8_t* g) {
-            uint8_t* l = &lds[buf][((i < LA ? i : i - LA) * THREADS + wave * 64) * 16 + (i < LA ? 0 : BM * 128)];
+            uint8_t* l = &lds[buf][((i < LA ? i : i - LA) * THREADS + wave * 64) * 16 + (i < LA ? 0 : NA * BM * ROW)];
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)g,
                                              (__attribute__((address_space(3))) uint32_t*)l, 16, 0, 0);
         };
-        if (at_step * 8 + 8 <= chunks) {
+        if (at_step * CH16 + CH16 <= chunks) {
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) to_lds(i, src[i] + (i < LA ? at_a : at_b));
+            for (int i = 0; i < LA + LB; ++i) to_lds(i, src[i] + at_byte);
         } else {                                         // the rows end inside this step
-            const bool in = at_step * 8 + piece < chunks;
+            const bool in = at_step * CH16 + piece < chunks;
 #pragma unroll
-            for (int i = 0; i < LA + LB; ++i) to_lds(i, in ? src[i] + (i < LA ? at_a : at_b) : (const uint8_t*)lba_zero_piece);
+            for (int i = 0; i < LA + LB; ++i) to_lds(i, in ? src[i] + at_byte : (const uint8_t*)lba_zero_piece);
         }
-        at_a += 128;
-        at_b += 128;
-        if (++at_step == steps_row) {                    // the next piece of A against the same B
-            at_step = 0;
-            at_a += a_wrap;
-            at_b = 0;
-        }
+        at_byte += ROW;
+        ++at_step;
     };
 
     f32x4 acc[FM][FN];
@@ -321,19 +311,19 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int place = ((lane / 16) ^ ((lane & 15) >> 1)) * 16 + (lane & 15) * 128;
+    const int place = ((lane / 16) ^ (((lane & 15) >> 1) & (CH16 - 1))) * 16 + (lane & 15) * ROW;
     const int flip = (place & 64) ? -64 : 64;            // the second piece of a row is 64 bytes on, modulo the row
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
         if (first + i < last) stage(i);
     i32x4 ra[2][FM], rb[2][FN];
     auto read = [&](int h, int buf) {
-        const uint8_t* la = &lds[buf][wm * FM * 2048 + place];
-        const uint8_t* lb = &lds[buf][BM * 128 + wn * FN * 2048 + place];
+        const uint8_t* la = &lds[buf][wm * FM * 16 * ROW + place];
+        const uint8_t* lb = &lds[buf][NA * BM * ROW + wn * FN * 16 * ROW + place];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) rb[h][j] = *(const i32x4*)(lb + j * 2048 + h * flip);
+        for (int j = 0; j < FN; ++j) rb[h][j] = *(const i32x4*)(lb + j * 16 * ROW + h * flip);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) ra[h][i] = *(const i32x4*)(la + i * 2048 + h * flip);
+        for (int i = 0; i < FM; ++i) ra[h][i] = *(const i32x4*)(la + i * 16 * ROW + h * flip);
     };
     auto multiply = [&](int h) {
         if constexpr (ELEM == ELEM_BF16) {
@@ -366,6 +356,26 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();                    // every wave's loads of this step are done, and the step before is read
         asm volatile("" ::: "memory");
+        if constexpr (NA == 3) {
+            read(0, buf);
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + 1 < last) stage(buf ^ 1);
+            const uint8_t* la = &lds[buf][wm * FM * 16 * ROW + place];
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {                // the next piece's fragments are read before this one's products
+                if (q < 2) {
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) ra[(q + 1) & 1][i] = *(const i32x4*)(la + ((q + 1) * BM + i * 16) * ROW);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[i][j] = product_16x16x32<ELEM>(rb[0][j], ra[q & 1][i], acc[i][j]);
+            }
+            buf ^= 1;
+            continue;
+        }
         // the first half's fragments are read before the next step's loads are issued, the second half's before the first half's products
         read(0, buf);
         __builtin_amdgcn_sched_barrier(0);
@@ -534,7 +544,7 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         if constexpr (EPI == EPI_BACKWARD) {
-            if (e.PT && mh < e.ldt && nw < e.N) {        // the transposed copy: eight rows of one column a lane
+            if (e.PT && mh < up_to_8(e.M) && nw < e.N) {        // the transposed copy: eight rows of one column a lane
                 constexpr int LM = EH * 2, NPP = 64 / LM;                            // lanes along m, columns of a pass
                 const int r0 = (lane % LM) * 8, m = mh + r0;
 #pragma unroll 1
@@ -543,7 +553,7 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
                     const int n = nw + (GATED ? c / 32 * 16 + c % 16 : c);
                     const int half = GATED ? c / 16 % 2 : 0;
                     float d[8];
-                    if (lane < LM * NPP && c < CH * 4 && n < e.N && m < e.ldt) {     // ldt and m are multiples of 8: zeros beyond M are part of the copy
+                    if (lane < LM * NPP && c < CH * 4 && n < e.N && m < up_to_8(e.M)) {          // m is a multiple of 8: zeros beyond M are part of the copy
 #pragma unroll
                         for (int k = 0; k < 8; ++k) d[k] = mine[((r0 + k) * CH + ((c / 4) ^ ((r0 + k) % CH))) * 4 + c % 4];
                         const At it = {((int64_t)half * e.N + n) * e.ldt + m, 0};
@@ -576,10 +586,10 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
 
 // Tiles: rows of outputs, columns of B, waves over m.  The deep ones have four buffers instead of two, for bfloat16 rows: their steps are shorter
 // than the time a load takes where a CU has one workgroup (codes' are not: conversions fill them, and four buffers gained nothing).
-enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5 };
+enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5, TILE_256_THREE = 6, TILE_128_THREE = 7, TILE_64_THREE = 8 };
 struct TileShape { int bm, bn, wm; };
 inline TileShape tile_shape(int tile) {
-    static const TileShape all[] = {{256, 256, 2}, {128, 128, 2}, {64, 64, 2}, {192, 256, 2}, {128, 128, 2}, {64, 64, 2}};
+    static const TileShape all[] = {{256, 256, 2}, {128, 128, 2}, {64, 64, 2}, {192, 256, 2}, {128, 128, 2}, {64, 64, 2}, {256, 256, 2}, {128, 128, 2}, {64, 64, 2}};
     return all[tile];
 }
 
@@ -647,13 +657,13 @@ template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, i
     pair.g[1] = b ? *b : a;
     pair.blocks = dense_grid(pair.g[0], s, gated);
     const dim3 grid((unsigned)(pair.blocks + (b ? dense_grid(pair.g[1], s, gated) : 0)));
-#define LBA_DENSE(TILE, WM, WN, FM, FN, NST, GATED, EPI) \
+#define LBA_DENSE(TILE, WM, WN, FM, FN, NST, NA, GATED, EPI) \
     if (tile == TILE && gated == GATED && epi == EPI) { \
-        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \
+        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, NA, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \
         return LBA_OK; \
     }
-#define LBA_DENSE_SMALL(GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, GATED, EPI)
-#define LBA_DENSE_LARGE(GATED) LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, GATED, EPI_FORWARD)
+#define LBA_DENSE_SMALL(GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, 1, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, 1, GATED, EPI)
+#define LBA_DENSE_LARGE(GATED) LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, 1, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, 1, GATED, EPI_FORWARD)
     LBA_DENSE_SMALL(false, EPI_FORWARD)
     LBA_DENSE_SMALL(true, EPI_FORWARD)
     LBA_DENSE_LARGE(false)
@@ -661,8 +671,11 @@ template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, i
     LBA_DENSE_SMALL(false, EPI_BACKWARD)
     LBA_DENSE_SMALL(true, EPI_BACKWARD)
     if constexpr (ELEM == ELEM_BF16) {
-        LBA_DENSE(TILE_128_DEEP, 2, 2, 4, 4, 4, false, EPI_FORWARD)
-        LBA_DENSE(TILE_64_DEEP, 2, 2, 2, 2, 4, false, EPI_FORWARD)
+        LBA_DENSE(TILE_128_DEEP, 2, 2, 4, 4, 4, 1, false, EPI_FORWARD)
+        LBA_DENSE(TILE_64_DEEP, 2, 2, 2, 2, 4, 1, false, EPI_FORWARD)
+        LBA_DENSE(TILE_256_THREE, 2, 4, 8, 4, 2, 3, false, EPI_FORWARD)
+        LBA_DENSE(TILE_128_THREE, 2, 2, 4, 4, 2, 3, false, EPI_FORWARD)
+        LBA_DENSE(TILE_64_THREE, 2, 2, 2, 2, 2, 3, false, EPI_FORWARD)
     }
 #undef LBA_DENSE_LARGE
 #undef LBA_DENSE_SMALL

@@ -179,7 +179,9 @@ static const TileCost kCodes[] = {
 static const TileCost kRows[] = {
     {TILE_256, 1, 9.0f, 2.0f, 9.0f, 1.75f, 1.0f}, {TILE_128, 2, 4.0f, 0.97f, 2.7f, 0.85f, 1.0f}, {TILE_128_DEEP, 1, 3.0f, 0.75f, 3.0f, 0.6f, 1.0f},
     {TILE_64, 4, 2.6f, 0.62f, 0.6f, 0.55f, 1.0f}, {TILE_64_DEEP, 2, 1.4f, 0.5f, 0.6f, 0.42f, 1.0f}};
-constexpr float kLaunch = 4.5f, kJoinRate = 6e6f;         // a launch alone; bytes a microsecond that the join moves
+static const TileCost kThree[] = {                         // three pieces of A: steps of 64 bytes
+    {TILE_256_THREE, 1, 9.0f, 2.4f, 9.0f, 2.4f, 1.0f}, {TILE_128_THREE, 2, 4.0f, 1.42f, 2.7f, 0.8f, 1.0f}, {TILE_64_THREE, 4, 2.6f, 1.1f, 0.6f, 0.5f, 1.0f}};
+constexpr float kLaunch = 4.5f, kJoinRate = 5e6f;         // a launch alone; bytes a microsecond that the join moves
 constexpr int kCus = 256;
 
 // the end of `a` workgroups of duration da and then `b` of db on `slots` places, da >= db
@@ -219,11 +221,12 @@ static double cost_of(const Product* p, const int64_t* tiles, int n, const TileC
 
 // Chooses the tile of a product, or of two that share a launch, and their slices: the least cost.
 enum { PLAN_FORWARD = 0, PLAN_BACKWARD = 1 };             // with the backward epilogue only small tiles, and no slices
-static int plan_tile(Product* p, int n, int elem, int kind, bool gated) {
-    const TileCost* all = elem == ELEM_BF16 ? kRows : kCodes;
-    const int count = elem == ELEM_BF16 ? (int)(sizeof(kRows) / sizeof(kRows[0])) : (int)(sizeof(kCodes) / sizeof(kCodes[0]));
+static int plan_tile(Product* p, int n, int elem, int kind, bool gated, int pieces = 1) {
+    const TileCost* all = pieces == 3 ? kThree : elem == ELEM_BF16 ? kRows : kCodes;
+    const size_t bytes = pieces == 3 ? sizeof(kThree) : elem == ELEM_BF16 ? sizeof(kRows) : sizeof(kCodes);
+    const int count = (int)(bytes / sizeof(TileCost));
     static const int kSlices[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
-    int best = TILE_64;
+    int best = all[count - 1].tile;
     double least = 1e300;
     Product cut_best[2];
     for (int t = 0; t < count; ++t) {
@@ -275,13 +278,18 @@ struct DensePlan {
     size_t copy_a, copy_b, split, bytes;
 };
 
+// Bytes from row to row of a copy of rows of `bytes`: whole cache lines but for short rows.  (The gradient products of 3985 x 770 x 771, whose steps
+// of 64 or 128 bytes straddled two lines, took 53 us instead of 41.)
+static int64_t pitch(int64_t bytes) { return bytes < 512 ? bytes : up_to(bytes, 128); }
+
 static void lay_out(DensePlan& d, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, bool aligned) {
     d.elem = elem_of(fa, fb);
     d.cols = gated ? 2 * N : N;
     d.in_place = d.elem != ELEM_BF16 && K % 16 == 0 && aligned;
-    d.ld = d.elem != ELEM_BF16 ? up_to(K, 16) : 2 * up_to(K, 8);
-    d.chunks = d.ld / 16;
-    d.steps = (d.ld + 127) / 128;
+    const int64_t bytes = d.elem != ELEM_BF16 ? up_to(K, 16) : 2 * up_to(K, 8);
+    d.ld = d.in_place ? K : pitch(bytes);
+    d.chunks = bytes / 16;
+    d.steps = (bytes + 127) / 128;
 }
 
 static DensePlan plan_forward(int64_t M, int64_t N, int64_t K, const lba_infmt& fa, const lba_infmt& fb, bool gated, bool aligned) {
@@ -305,7 +313,8 @@ struct BwdPlan {
     DensePlan f;             // the sums computed again
     bool sums;               // whether they are
     int pieces;
-    int64_t ldp, ldt;        // elements of a row of the gradient matrix and of its transpose
+    int64_t np, mp;          // columns of the gradient matrix and of its transpose, with the zeros up to multiples of 8
+    int64_t ldp, ldt;        // elements from row to row of them
     Product out[2];          // dA and dB, in one launch
     int tile;
     int64_t part_rows;
@@ -325,8 +334,10 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
         f.copy_b = at; at += align256((size_t)(f.cols * f.ld));
     }
     b.pieces = g_type == LBA_F32 ? 3 : 1;
-    b.ldp = (gated ? 2 : 1) * up_to(N, 8);
-    b.ldt = up_to(M, 8);
+    b.np = (gated ? 2 : 1) * up_to(N, 8);
+    b.mp = up_to(M, 8);
+    b.ldp = pitch(b.np * 2) / 2;
+    b.ldt = pitch(b.mp * 2) / 2;
     b.p = at; at += align256((size_t)(b.pieces * M * b.ldp) * 2);
     b.pt = at; at += align256((size_t)(b.pieces * f.cols * b.ldt) * 2);
     b.at = at; at += align256((size_t)(K * b.ldt) * 2);
@@ -334,9 +345,10 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
     const TileShape s = tile_shape(f.tile);
     b.part_rows = (M + s.bm - 1) / s.bm * s.wm;
     b.part = at; at += align256((size_t)(b.part_rows * f.cols) * 4);
-    b.out[0] = {M, K, (b.ldp * 2 + 127) / 128 * b.pieces, 1, 0};
-    b.out[1] = {f.cols, K, (b.ldt * 2 + 127) / 128 * b.pieces, 1, 0};
-    b.tile = plan_tile(b.out, 2, ELEM_BF16, PLAN_FORWARD, false);
+    const int64_t step = b.pieces == 3 ? 64 : 128;
+    b.out[0] = {M, K, (b.np * 2 + step - 1) / step, 1, 0};
+    b.out[1] = {f.cols, K, (b.mp * 2 + step - 1) / step, 1, 0};
+    b.tile = plan_tile(b.out, 2, ELEM_BF16, PLAN_FORWARD, false, b.pieces);
     b.split_a = at; at += split_bytes(b.out[0]);
     b.split_b = at; at += split_bytes(b.out[1]);
     b.bytes = at;
@@ -443,7 +455,7 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
         if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
         g.A = ws + d.copy_a; g.B = ws + d.copy_b;
     }
-    g.pieces = 1; g.rows_a = (int32_t)M; g.rows_b = (int32_t)d.cols; g.half = (int32_t)N;
+    g.rows_a = (int32_t)M; g.rows_b = (int32_t)d.cols; g.half = (int32_t)N;
     g.chunks = (int32_t)d.chunks; g.steps = (int32_t)d.steps;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
@@ -512,7 +524,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     }
     if (dB) add_job(jobs, blocks, A, ws + b.at, M, K, b.ldt * 2, LAY_TRANSPOSED, fmt_a);
     if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
-    g.pieces = 1; g.rows_a = (int32_t)M; g.rows_b = (int32_t)cols; g.half = (int32_t)N;
+    g.rows_a = (int32_t)M; g.rows_b = (int32_t)cols; g.half = (int32_t)N;
     g.chunks = b.sums ? (int32_t)b.f.chunks : 0; g.steps = b.sums ? (int32_t)b.f.steps : 0;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
@@ -528,19 +540,18 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     if (dA) {
         GemmParams& a = q[n];
         a.A = (const uint8_t*)P; a.B = ws + b.bt; a.lda = a.ldb = b.ldp * 2; a.a_piece = e.p_piece * 2;
-        a.rows_a = (int32_t)M; a.chunks = (int32_t)(b.ldp / 8); a.split = (float*)(ws + b.split_a);
+        a.rows_a = (int32_t)M; a.chunks = (int32_t)(b.np / 8); a.split = (float*)(ws + b.split_a);
         a.e.scale = make_elem(fmt_b, ELEM_BF16).factor; a.e.M = (int32_t)M; a.e.Y = dA;
         parts[n++] = b.out[0];
     }
     if (dB) {
         GemmParams& a = q[n];
         a.A = (const uint8_t*)PT; a.B = ws + b.at; a.lda = a.ldb = b.ldt * 2; a.a_piece = e.pt_piece * 2;
-        a.rows_a = (int32_t)cols; a.chunks = (int32_t)(b.ldt / 8); a.split = (float*)(ws + b.split_b);
+        a.rows_a = (int32_t)cols; a.chunks = (int32_t)(b.mp / 8); a.split = (float*)(ws + b.split_b);
         a.e.scale = make_elem(fmt_a, ELEM_BF16).factor; a.e.M = (int32_t)cols; a.e.Y = dB;
         parts[n++] = b.out[1];
     }
     for (int i = 0; i < n; ++i) {
-        q[i].pieces = b.pieces;
         q[i].rows_b = q[i].half = (int32_t)K;
         q[i].steps = (int32_t)parts[i].steps;
         q[i].e.N = (int32_t)K; q[i].e.y_type = g_type;
