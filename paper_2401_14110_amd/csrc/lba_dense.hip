@@ -1,7 +1,8 @@
 // lba_dense.hip -- the dense product's plan, its operands' copies, the joining of sliced sums, and the entry points.
 //
 // Operands whose rows the tile cannot read where they are (rows off 16 bytes, codes of five exponent bits, sums over rows) are laid out once
-// per call in the workspace: a pass over one byte an element beside a product of K (or N) operations on each.
+// per call in the workspace: a pass over one byte an element beside a product of K (or N) operations on each (12 M codes transposed to
+// bfloat16: 10 us, 3.6 TB/s; 6 M codes to rows of their own: 5 us).
 #include "lba_dense.h"
 #include "lba_internal.h"
 
