@@ -81,8 +81,36 @@ struct GemmParams {
     EpiParams e;
 };
 
-// one launch of one product or two: workgroups below `blocks` belong to the first
-struct GemmPair { GemmParams g[2]; int32_t blocks; };
+// column sums that a launch of the gradient products makes beside them: out[n] = sum over `parts` rows of part[row][n], n < cols
+struct SideSums { const float* part; float* out; int32_t parts, cols; };
+// one launch of one product or two: workgroups below `blocks` belong to the first, from `all` on to the column sums
+struct GemmPair { GemmParams g[2]; int32_t blocks, all; SideSums sums; };
+
+// 16 columns a workgroup, THREADS / 16 lanes a column, which take its rows in turn, then their sums in a fixed order
+template <int THREADS> __device__ __forceinline__ void side_sums(const SideSums& q, int block, float* lds) {
+    constexpr int LANES = THREADS / 16;
+    const int c = threadIdx.x & 15, n = block * 16 + c;
+    float s = 0.0f;
+    if (n < q.cols) {
+        int r = threadIdx.x / 16;
+        for (; r + 3 * LANES < q.parts; r += 4 * LANES) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = q.part[(int64_t)(r + k * LANES) * q.cols + n];
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; r < q.parts; r += LANES) s += q.part[(int64_t)r * q.cols + n];
+    }
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 48) == 0) lds[threadIdx.x / 64 * 16 + c] = s;
+    __syncthreads();
+    if (threadIdx.x >= 16 || n >= q.cols) return;
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) s += lds[w * 16 + c];
+    q.out[n] = s;
+}
 
 __device__ __forceinline__ int up_to_8(int x) { return (x + 7) & ~7; }
 
@@ -255,6 +283,12 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     static_assert(NA * BM * CH16 % THREADS == 0 && BN * CH16 % THREADS == 0 && THREADS / CH16 <= BM && (!GATED || FN % 2 == 0), "tile");
     static_assert(NA == 1 || (NA == 3 && ELEM == ELEM_BF16 && !GATED && NST == 2), "three pieces");
     __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(NA * BM + BN) * ROW];
+    if constexpr (ELEM == ELEM_BF16 && !GATED && EPI == EPI_FORWARD) {
+        if ((int)blockIdx.x >= both.all) {
+            side_sums<THREADS>(both.sums, (int)blockIdx.x - both.all, (float*)&lds[0][0]);
+            return;
+        }
+    }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wm = wave / WN, wn = wave % WN;
     int slice, tm, tn;
@@ -645,10 +679,11 @@ struct TokenParams {
 };
 void launch_dense_token(const TokenParams& p, int elem, bool gated, hipStream_t st);
 
-// launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape
+// launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape, and column sums
+// beside a plain product of bfloat16 rows (sums may be null)
 int launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
 int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
-int launch_dense_bf16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_bf16(const GemmParams& a, const GemmParams* b, const SideSums* sums, int tile, bool gated, int epi, hipStream_t st);
 
 inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     p.gx = (p.e.M + s.bm - 1) / s.bm;
@@ -656,13 +691,15 @@ inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     return p.gx * p.gy * (p.slices > 1 ? p.slices : 1);
 }
 
-template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
+template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, const SideSums* sums, int tile, bool gated, int epi, hipStream_t st) {
     const TileShape s = tile_shape(tile);
     GemmPair pair;
     pair.g[0] = a;
     pair.g[1] = b ? *b : a;
     pair.blocks = dense_grid(pair.g[0], s, gated);
-    const dim3 grid((unsigned)(pair.blocks + (b ? dense_grid(pair.g[1], s, gated) : 0)));
+    pair.all = pair.blocks + (b ? dense_grid(pair.g[1], s, gated) : 0);
+    pair.sums = sums ? *sums : SideSums{};
+    const dim3 grid((unsigned)(pair.all + (pair.sums.cols + 15) / 16));
 #define LBA_DENSE(TILE, WM, WN, FM, FN, NST, NA, GATED, EPI) \
     if (tile == TILE && gated == GATED && epi == EPI) { \
         hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, NA, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \

@@ -374,7 +374,7 @@ static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* d
 static bool lay_fits(int64_t R, int64_t K) { return (R + 64) * (K + 64) <= ((int64_t)1 << 32); }
 
 // one product, or two that share a launch
-static int run_products(GemmParams* g, const Product* p, int n, int tile, int elem, bool gated, int epi, hipStream_t st) {
+static int run_products(GemmParams* g, const Product* p, int n, const SideSums* sums, int tile, int elem, bool gated, int epi, hipStream_t st) {
     JoinPair join = {};
     int sliced = 0;
     for (int i = 0; i < n; ++i) {
@@ -387,7 +387,7 @@ static int run_products(GemmParams* g, const Product* p, int n, int tile, int el
     int rc;
     if (elem == ELEM_E4M3) rc = launch_dense_e4m3(g[x], second, tile, gated, epi, st);
     else if (elem == ELEM_F16) rc = launch_dense_f16(g[x], second, tile, gated, epi, st);
-    else rc = launch_dense_bf16(g[x], second, tile, gated, epi, st);
+    else rc = launch_dense_bf16(g[x], second, sums, tile, gated, epi, st);
     if (rc != LBA_OK || !sliced) return rc;
     join.blocks = join_blocks(join.p[0].e);
     const dim3 grid((unsigned)(join.blocks + (sliced > 1 ? join_blocks(join.p[1].e) : 0)));
@@ -461,7 +461,7 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
     g.split = (float*)(ws + d.split);
-    rc = run_products(&g, &d.fwd, 1, d.tile, d.elem, two, EPI_FORWARD, st);
+    rc = run_products(&g, &d.fwd, 1, nullptr, d.tile, d.elem, two, EPI_FORWARD, st);
     if (rc != LBA_OK) return rc;
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
@@ -529,12 +529,15 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     g.chunks = b.sums ? (int32_t)b.f.chunks : 0; g.steps = b.sums ? (int32_t)b.f.steps : 0;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
-    rc = run_products(&g, &b.f.fwd, 1, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
+    rc = run_products(&g, &b.f.fwd, 1, nullptr, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
     if (rc != LBA_OK) return rc;
-    if (dbias) launch_column_sum(e.part, b.part_rows, cols, dbias, nullptr, cols, st);
 
-    // the two products of it
-    if (K == 0 || (!dA && !dB)) return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+    // the two products of it, and dbias beside them
+    if (K == 0 || (!dA && !dB)) {
+        if (dbias) launch_column_sum(e.part, b.part_rows, cols, dbias, nullptr, cols, st);
+        return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
+    }
+    const SideSums sums = {e.part, dbias, (int32_t)b.part_rows, (int32_t)cols};
     GemmParams q[2] = {};
     Product parts[2];
     int n = 0;
@@ -557,7 +560,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
         q[i].steps = (int32_t)parts[i].steps;
         q[i].e.N = (int32_t)K; q[i].e.y_type = g_type;
     }
-    rc = run_products(q, parts, n, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
+    rc = run_products(q, parts, n, dbias ? &sums : nullptr, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
     if (rc != LBA_OK) return rc;
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }

@@ -3,6 +3,6 @@
 
 namespace lba {
 int launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
-    return launch_dense<ELEM_E4M3>(a, b, tile, gated, epi, st);
+    return launch_dense<ELEM_E4M3>(a, b, nullptr, tile, gated, epi, st);
 }
 }  // namespace lba

@@ -3,6 +3,6 @@
 
 namespace lba {
 int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
-    return launch_dense<ELEM_F16>(a, b, tile, gated, epi, st);
+    return launch_dense<ELEM_F16>(a, b, nullptr, tile, gated, epi, st);
 }
 }  // namespace lba

@@ -144,6 +144,22 @@ def test_exact_sums_and_repeats():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(3985, 771, 770), (8192, 304, 2048), (257, 5000, 1300), (70, 1024, 1024), (9000, 2100, 1030), (2048, 2048, 4096)])
+def test_exact_gradients_in_every_tile(M, N, K):
+    # small integers again, at sizes that take tiles of every shape, whole and in slices
+    rng = np.random.default_rng(M)
+    pick = np.array([0x00, 0x38, 0x40, 0xB8, 0xC0], np.uint8)                         # 0, 1, 2, -1, -2
+    A, B = pick[rng.integers(0, 5, (M, K))], pick[rng.integers(0, 5, (N, K))]
+    a, b = (lo.code_values(4, 3, 7)[v].astype(np.float32) for v in (A, B))           # float32 sums of these are exact in any order
+    G = rng.integers(-8, 9, (M, N)).astype(np.float32)
+    for dtype in ("f32", "bf16"):
+        out = lb.dense_bwd(dev(G, dtype), dev(A), dev(B), want_dbias=True)
+        for got, want in zip(out, (G @ b, G.T @ a, G.sum(0))):
+            want = want if got.dtype == torch.float32 else lo.bf16(want)
+            assert np.array_equal(host(got), want)
+
+
+@pytest.mark.gpu
 def test_parts_of_the_gradients():
     A, B, fa, fb, b, _, G, _, _ = problem(8, 200, 90, 75, E4M3, E4M3, False, True, "f32", False, 0.0)
     args = (dev(G), dev(A), dev(B), fa, fb)
