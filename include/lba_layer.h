@@ -23,7 +23,7 @@ extern "C" {
 /* Element types.  LBA_CODE8: 8-bit codes of an lba_infmt (lba.h), whose bias carries the tensor's power-of-two scale: the codes of
  * {4, 3, 7 + t} are the E4M3 codes of x * 2^t.  Written codes are rounded to nearest, ties to even, and saturate at the largest
  * value of the format (exp_bits 4: +-448 of the canonical bias, the codes 0x7f and 0xff are not written for numbers); a NaN is
- * written as 0x7f. */
+ * written as 0x7f or 0xff. */
 enum { LBA_F32 = 0, LBA_BF16 = 1, LBA_CODE8 = 2 };
 
 /* Activations: none, max(z, 0), z * Phi(z) with the normal distribution function Phi, z / (1 + exp(-z)). */

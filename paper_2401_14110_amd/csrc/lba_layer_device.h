@@ -57,8 +57,8 @@ __device__ __forceinline__ uint32_t code_four(float a, float b, float c, float d
         float s[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float u = v[j] * f.scale;
-            s[j] = u > 448.0f ? 448.0f : (u < -448.0f ? -448.0f : u);      // a NaN stays one: the conversion writes 0x7f for it
+            // these keep a NaN, for which the conversion writes 0x7f or 0xff
+            s[j] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(v[j] * f.scale, -448.0f), 448.0f);
         }
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], 0, false);
         return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], w, true);
@@ -127,25 +127,30 @@ __device__ __forceinline__ float exp_near(float x) {
     return x > 88.72f ? __builtin_inff() : fmaf(e, left * 0.693147181f, e);
 }
 
-// The normal distribution function and e^(-z^2/2).  For a = |z|, Phi(-a) = e^(-a^2/2) * h(t) with t = 1 / (1 + 0.28 a); h is smooth and is taken
-// as a polynomial of degree 6 without a constant term, fitted to (1 + a) * Phi in the largest error (1.5e-8).  A negative argument's
-// value is the product itself, so nothing cancels in the tail; the exponential is what the derivative needs as well.
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.28f, fabsf(z), 1.0f));
+// The normal distribution's tail Phi(-a) for a = |z|, and e^(-z^2/2).  Phi(-a) = e^(-a^2/2) * h(t) with t = 1 / (1 + 0.28 a); h is smooth and is
+// taken as a polynomial of degree 6 without a constant term, fitted to (1 + a) * Phi in the largest error (1.5e-8).  With it z * Phi(z) is
+// max(z, 0) - a * Phi(-a) for either sign: nothing cancels in the tail, and nothing is chosen by a comparison.  `a` is at most 64, where
+// the tail is 0 as a float32 number, so that an infinity does not meet that zero; a NaN comes through the exponential.
+__device__ __forceinline__ float normal_tail(float z, float& a, float& e) {
+    a = fminf(fabsf(z), 64.0f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.28f, a, 1.0f));
     e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
     float h = fmaf(t, -0.10655423f, 0.39296786f);
     h = fmaf(t, h, -0.24209468f);
     h = fmaf(t, h, 0.27308893f);
     h = fmaf(t, h, 0.065796522f);
     h = fmaf(t, h, 0.11679558f);
-    const float q = e * (t * h);
-    return z < 0.0f ? q : 1.0f - q;
+    return e * (t * h);
 }
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_near(-z)); }
 
 template <int ACT> __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == LBA_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
-    if constexpr (ACT == LBA_ACT_GELU) { float e; return z * normal_cdf(z, e); }
+    if constexpr (ACT == LBA_ACT_GELU) {
+        float a, e;
+        const float q = normal_tail(z, a, e);
+        return fmaf(-a, q, fmaxf(z, 0.0f));
+    }
     if constexpr (ACT == LBA_ACT_SILU) return z * logistic(z);
     return z;
 }
@@ -155,10 +160,10 @@ template <int ACT> __device__ __forceinline__ void act_both(float z, float& valu
         value = z > 0.0f ? z : (z != z ? z : 0.0f);
         slope = z > 0.0f ? 1.0f : 0.0f;
     } else if constexpr (ACT == LBA_ACT_GELU) {
-        float e;
-        const float phi = normal_cdf(z, e);
-        value = z * phi;
-        slope = fmaf(z * 0.39894228f, e, phi);
+        float a, e;
+        const float q = normal_tail(z, a, e);
+        value = fmaf(-a, q, fmaxf(z, 0.0f));
+        slope = fmaf(copysignf(a, z) * 0.39894228f, e, z < 0.0f ? q : 1.0f - q);
     } else if constexpr (ACT == LBA_ACT_SILU) {
         const float h = logistic(z);
         value = z * h;

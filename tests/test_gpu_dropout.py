@@ -142,6 +142,17 @@ def test_activations_far_out():
 
 
 @pytest.mark.gpu
+def test_gelu_of_what_is_no_number():
+    z = torch.tensor([float("inf"), float("-inf"), float("nan"), 1.0], device=DEV)
+    y = lb.dropout(z, None, act=lb.ACT_GELU).cpu()
+    assert y[0] == float("inf") and y[1] == 0 and y[2].isnan() and y[3].isfinite()
+    dx = lb.dropout_bwd(torch.ones(4, device=DEV), None, x=z, act=lb.ACT_GELU)[0].cpu()
+    assert dx[0] == 1 and dx[1] == 0 and dx[2].isnan() and dx[3].isfinite()
+    code = lb.dropout(z, None, out_dtype=torch.uint8, out_fmt=(4, 3, 7)).cpu()
+    assert code[:2].tolist() == [0x7E, 0xFE] and int(code[2]) in (0x7F, 0xFF) and code[3] == 0x38
+
+
+@pytest.mark.gpu
 def test_differences():
     rng = np.random.default_rng(12)
     M, N, eps = 16, 48, 2.0 ** -7
