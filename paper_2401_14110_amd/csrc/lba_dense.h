@@ -81,10 +81,142 @@ struct GemmParams {
     EpiParams e;
 };
 
+// code -> value at the canonical bias 2^(E-1) - 1, exact (at most 6 significant bits: a bfloat16 number)
+struct CodeBits { int32_t sh; uint32_t exp0, sub; float two; };   // 23 - M, (127 - bias) << 23, 1 << M, 2^(1 - bias)
+inline CodeBits make_code_bits(const lba_infmt& f) {
+    const int bc = (1 << (f.exp_bits - 1)) - 1;
+    return {23 - f.man_bits, (uint32_t)(127 - bc) << 23, 1u << f.man_bits, __builtin_ldexpf(1.0f, 1 - bc)};
+}
+__device__ __forceinline__ float code_value(uint32_t code, const CodeBits& b) {
+    const uint32_t mag = code & 0x7Fu;
+    float f = __uint_as_float((mag << b.sh) + b.exp0);
+    if (mag < b.sub) f = fmaf(2.0f, f, -b.two);          // subnormal: the leading one does not count
+    return __uint_as_float(__float_as_uint(f) | ((code & 0x80u) << 24));
+}
+// four codes of a word -> four bfloat16 numbers
+__device__ __forceinline__ void code_bf16(uint32_t w, const CodeBits& b, uint32_t& lo, uint32_t& hi) {
+    const uint32_t v0 = __float_as_uint(code_value(w & 0xFFu, b)), v1 = __float_as_uint(code_value((w >> 8) & 0xFFu, b));
+    const uint32_t v2 = __float_as_uint(code_value((w >> 16) & 0xFFu, b)), v3 = __float_as_uint(code_value(w >> 24, b));
+    lo = __builtin_amdgcn_perm(v1, v0, 0x07060302u);
+    hi = __builtin_amdgcn_perm(v3, v2, 0x07060302u);
+}
+
+// ---- operands laid out for the tile ---------------------------------------------------------
+
+// Up to five operands are laid out by 256 lanes a workgroup: those from `first` on belong to a job.
+enum { LAY_CODES = 0, LAY_BF16 = 1, LAY_TRANSPOSED = 2 };
+struct LayJob {
+    const uint8_t* src;      // [R, K] codes
+    uint8_t* dst;
+    int64_t R;
+    int64_t ld;              // bytes of a row of dst
+    int32_t K;
+    int32_t wide;            // LAY_TRANSPOSED: R rounded up to 8: columns of dst, zeros from R on
+    int32_t tiles_k;         // LAY_TRANSPOSED: tiles along k
+    int32_t kind;
+    uint32_t first;
+    CodeBits bits;
+};
+struct LayJobs { LayJob job[5]; int32_t n; };
+
+// rows of codes or of bfloat16 numbers, zeros behind K: 16 bytes of output a lane
+template <bool BF16> __device__ __forceinline__ void lay_rows(const LayJob& p, int64_t block) {
+    constexpr int PER = BF16 ? 8 : 16;
+    const uint32_t per_row = (uint32_t)(p.ld / 16), i = (uint32_t)block * 256 + threadIdx.x;   // fewer than 2^30 pieces (lay_fits)
+    if (i >= (uint32_t)p.R * per_row) return;
+    const uint32_t r = i / per_row;
+    const int k = (int)(i - r * per_row) * PER;
+    const uint8_t* s = p.src + (int64_t)r * p.K + k;
+    uint32_t w[PER / 4];
+    if (k + PER <= p.K) {
+        typedef uint32_t words __attribute__((ext_vector_type(PER / 4), aligned(1)));
+        const words x = *(const words*)s;
+#pragma unroll
+        for (int j = 0; j < PER / 4; ++j) w[j] = x[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER / 4; ++j) w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
+    }
+    i32x4 o;
+    if constexpr (BF16) {
+        uint32_t lo, hi;
+        code_bf16(w[0], p.bits, lo, hi); o[0] = (int32_t)lo; o[1] = (int32_t)hi;
+        code_bf16(w[1], p.bits, lo, hi); o[2] = (int32_t)lo; o[3] = (int32_t)hi;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = (int32_t)w[j];
+    }
+    *(i32x4*)(p.dst + (int64_t)r * p.ld + (i - r * per_row) * 16) = o;
+}
+
+// dst [K][ld] bfloat16: 64 rows of 128 codes through LDS.  A lane reads four neighbouring codes of eight rows and writes four pieces of 16 bytes,
+// eight lanes side by side; rows of 33 words put the words that a wave reads at a time into 64 different banks.
+constexpr int kLayK = 128;
+constexpr int kLayRow = kLayK / 4 + 1, kLayWords = 64 * kLayRow;
+__device__ __forceinline__ void lay_transposed(const LayJob& p, int64_t block, uint32_t* t) {
+    const int64_t r0 = block / p.tiles_k * 64;
+    const int k0 = (int)(block % p.tiles_k) * kLayK;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = h * 256 + threadIdx.x, r = i / 8, c = i % 8, k = k0 + c * 16;
+        u32x4 w = {0, 0, 0, 0};
+        if (r0 + r < p.R && k < p.K) {
+            const uint8_t* s = p.src + (r0 + r) * p.K + k;
+            if (k + 16 <= p.K) {
+                typedef uint32_t words __attribute__((ext_vector_type(4), aligned(1)));
+                w = *(const words*)s;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[r * kLayRow + c * 4 + j] = w[j];
+    }
+    __syncthreads();
+    const int r = threadIdx.x % 8 * 8, kw = threadIdx.x / 8;
+    if (r0 + r >= p.wide) return;
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = t[(r + j) * kLayRow + kw];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int k = k0 + kw * 4 + q;
+        if (k >= p.K) return;
+        i32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a = __float_as_uint(code_value((w[2 * j] >> (8 * q)) & 0xFFu, p.bits));
+            const uint32_t b = __float_as_uint(code_value((w[2 * j + 1] >> (8 * q)) & 0xFFu, p.bits));
+            o[j] = (int32_t)__builtin_amdgcn_perm(b, a, 0x07060302u);
+        }
+        *(i32x4*)(p.dst + k * p.ld + (r0 + r) * 2) = o;
+    }
+}
+
+// what workgroup `at` of the jobs does; `t`: kLayWords words of LDS
+__device__ __forceinline__ void lay_block(const LayJobs& jobs, uint32_t at, uint32_t* t) {
+    int j = 0;
+    while (j + 1 < jobs.n && at >= jobs.job[j + 1].first) ++j;
+    const LayJob& p = jobs.job[j];
+    const int64_t block = at - p.first;
+    if (p.kind == LAY_CODES) lay_rows<false>(p, block);
+    else if (p.kind == LAY_BF16) lay_rows<true>(p, block);
+    else lay_transposed(p, block, t);
+}
+
 // column sums that a launch of the gradient products makes beside them: out[n] = sum over `parts` rows of part[row][n], n < cols
 struct SideSums { const float* part; float* out; int32_t parts, cols; };
-// one launch of one product or two: workgroups below `blocks` belong to the first, from `all` on to the column sums
-struct GemmPair { GemmParams g[2]; int32_t blocks, all; SideSums sums; };
+
+enum { EPI_FORWARD = 0, EPI_BACKWARD = 1 };
+// One launch of one product or two: workgroups below `blocks` belong to the first, from `all` on to the column sums; of the gradient of the
+// sums: from `all` on to the operands that the gradient products read.
+template <int EPI> struct DenseArgs { GemmParams g[2]; int32_t blocks, all; SideSums side; };
+template <> struct DenseArgs<EPI_BACKWARD> { GemmParams g[1]; int32_t all; LayJobs side; };
 
 // 16 columns a workgroup, THREADS / 16 lanes a column, which take its rows in turn, then their sums in a fixed order
 template <int THREADS> __device__ __forceinline__ void side_sums(const SideSums& q, int block, float* lds) {
@@ -239,8 +371,6 @@ __device__ __forceinline__ void tile_of(int gx, int gy, int slices, int id, int&
 
 __device__ const uint32_t lba_zero_piece[4] = {0, 0, 0, 0};
 
-enum { EPI_FORWARD = 0, EPI_BACKWARD = 1 };
-
 // what the rows hold: E4M3 codes, codes of at most 4 exponent bits that become FP16 numbers, or bfloat16 numbers
 enum { ELEM_E4M3 = 0, ELEM_F16 = 1, ELEM_BF16 = 2 };
 
@@ -274,8 +404,13 @@ template <int ELEM> __device__ __forceinline__ f32x4 product_16x16x32(i32x4 b, i
 // WM x WN waves of FM x FN fragments of 16 x 16, NST buffers of a step.  NA == 3: A comes in three pieces, whose products with a step of B are
 // made together: a step is 64 bytes of a row, and B's rows and fragments are read once for the three.
 template <int ELEM, int WM, int WN, int FM, int FN, int NST, int NA, bool GATED, int EPI>
-__global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)) void dense_kernel(GemmPair both) {
-    const bool second = (int)blockIdx.x >= both.blocks;
+__global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)) void dense_kernel(DenseArgs<EPI> both) {
+    bool second = false;
+    int id = (int)blockIdx.x;
+    if constexpr (EPI == EPI_FORWARD) {
+        second = id >= both.blocks;
+        if (second) id -= both.blocks;
+    }
     const GemmParams& p = both.g[second];
     constexpr int THREADS = WM * WN * 64, BM = WM * FM * 16, BN = WN * FN * 16;
     constexpr int CH16 = NA == 3 ? 4 : 8, ROW = CH16 * 16;               // sixteens of bytes of a row in a step, bytes
@@ -283,16 +418,22 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     static_assert(NA * BM * CH16 % THREADS == 0 && BN * CH16 % THREADS == 0 && THREADS / CH16 <= BM && (!GATED || FN % 2 == 0), "tile");
     static_assert(NA == 1 || (NA == 3 && ELEM == ELEM_BF16 && !GATED && NST == 2), "three pieces");
     __shared__ __attribute__((aligned(16))) uint8_t lds[NST][(NA * BM + BN) * ROW];
-    if constexpr (ELEM == ELEM_BF16 && !GATED && EPI == EPI_FORWARD) {
+    if constexpr (EPI == EPI_BACKWARD) {
+        static_assert(THREADS == 256 && sizeof(lds) >= kLayWords * 4, "jobs beside the tile");
         if ((int)blockIdx.x >= both.all) {
-            side_sums<THREADS>(both.sums, (int)blockIdx.x - both.all, (float*)&lds[0][0]);
+            lay_block(both.side, blockIdx.x - both.all, (uint32_t*)&lds[0][0]);
+            return;
+        }
+    } else if constexpr (ELEM == ELEM_BF16 && !GATED) {
+        if ((int)blockIdx.x >= both.all) {
+            side_sums<THREADS>(both.side, (int)blockIdx.x - both.all, (float*)&lds[0][0]);
             return;
         }
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wm = wave / WN, wn = wave % WN;
     int slice, tm, tn;
-    tile_of(p.gx, p.gy, p.slices, second ? (int)blockIdx.x - both.blocks : (int)blockIdx.x, slice, tm, tn);
+    tile_of(p.gx, p.gy, p.slices, id, slice, tm, tn);
     const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
 
     // staging: lane's rows and its piece of each
@@ -633,26 +774,6 @@ inline TileShape tile_shape(int tile) {
     return all[tile];
 }
 
-// code -> value at the canonical bias 2^(E-1) - 1, exact (at most 6 significant bits: a bfloat16 number)
-struct CodeBits { int32_t sh; uint32_t exp0, sub; float two; };   // 23 - M, (127 - bias) << 23, 1 << M, 2^(1 - bias)
-inline CodeBits make_code_bits(const lba_infmt& f) {
-    const int bc = (1 << (f.exp_bits - 1)) - 1;
-    return {23 - f.man_bits, (uint32_t)(127 - bc) << 23, 1u << f.man_bits, __builtin_ldexpf(1.0f, 1 - bc)};
-}
-__device__ __forceinline__ float code_value(uint32_t code, const CodeBits& b) {
-    const uint32_t mag = code & 0x7Fu;
-    float f = __uint_as_float((mag << b.sh) + b.exp0);
-    if (mag < b.sub) f = fmaf(2.0f, f, -b.two);          // subnormal: the leading one does not count
-    return __uint_as_float(__float_as_uint(f) | ((code & 0x80u) << 24));
-}
-// four codes of a word -> four bfloat16 numbers
-__device__ __forceinline__ void code_bf16(uint32_t w, const CodeBits& b, uint32_t& lo, uint32_t& hi) {
-    const uint32_t v0 = __float_as_uint(code_value(w & 0xFFu, b)), v1 = __float_as_uint(code_value((w >> 8) & 0xFFu, b));
-    const uint32_t v2 = __float_as_uint(code_value((w >> 16) & 0xFFu, b)), v3 = __float_as_uint(code_value(w >> 24, b));
-    lo = __builtin_amdgcn_perm(v1, v0, 0x07060302u);
-    hi = __builtin_amdgcn_perm(v3, v2, 0x07060302u);
-}
-
 // A format as the kernels read it: how its codes become 16-bit operands, and the factor that is left (value = operand * factor).
 struct ElemFmt { int elem, shift; uint32_t keep; float factor; };
 inline ElemFmt make_elem(const lba_infmt& f, int elem) {
@@ -679,11 +800,13 @@ struct TokenParams {
 };
 void launch_dense_token(const TokenParams& p, int elem, bool gated, hipStream_t st);
 
-// launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape, and column sums
-// beside a plain product of bfloat16 rows (sums may be null)
-int launch_dense_e4m3(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
-int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st);
-int launch_dense_bf16(const GemmParams& a, const GemmParams* b, const SideSums* sums, int tile, bool gated, int epi, hipStream_t st);
+// what runs beside: column sums (of a plain product of bfloat16 rows), or workgroups of jobs (of the gradient of the sums)
+struct Beside { SideSums sums; LayJobs jobs; uint32_t job_blocks; };
+
+// launches one or two products (b may be null) whose parameters are complete but for the grid, all in tiles of one shape; `side` may be null
+int launch_dense_e4m3(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_f16(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st);
+int launch_dense_bf16(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st);
 
 inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     p.gx = (p.e.M + s.bm - 1) / s.bm;
@@ -691,18 +814,31 @@ inline int dense_grid(GemmParams& p, const TileShape& s, bool gated) {
     return p.gx * p.gy * (p.slices > 1 ? p.slices : 1);
 }
 
-template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, const SideSums* sums, int tile, bool gated, int epi, hipStream_t st) {
+template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st) {
     const TileShape s = tile_shape(tile);
-    GemmPair pair;
-    pair.g[0] = a;
-    pair.g[1] = b ? *b : a;
-    pair.blocks = dense_grid(pair.g[0], s, gated);
-    pair.all = pair.blocks + (b ? dense_grid(pair.g[1], s, gated) : 0);
-    pair.sums = sums ? *sums : SideSums{};
-    const dim3 grid((unsigned)(pair.all + (pair.sums.cols + 15) / 16));
+    DenseArgs<EPI_FORWARD> fwd;
+    DenseArgs<EPI_BACKWARD> bwd;
+    dim3 grid;
+    if (epi == EPI_FORWARD) {
+        fwd.g[0] = a;
+        fwd.g[1] = b ? *b : a;
+        fwd.blocks = dense_grid(fwd.g[0], s, gated);
+        fwd.all = fwd.blocks + (b ? dense_grid(fwd.g[1], s, gated) : 0);
+        fwd.side = side ? side->sums : SideSums{};
+        grid = dim3((unsigned)(fwd.all + (fwd.side.cols + 15) / 16));
+    } else {
+        bwd.g[0] = a;
+        bwd.all = dense_grid(bwd.g[0], s, gated);
+        bwd.side = side ? side->jobs : LayJobs{};
+        grid = dim3((unsigned)bwd.all + (side ? side->job_blocks : 0u));
+    }
+    auto args = [&](auto e) -> auto& {
+        if constexpr (decltype(e)::value == EPI_FORWARD) return fwd;
+        else return bwd;
+    };
 #define LBA_DENSE(TILE, WM, WN, FM, FN, NST, NA, GATED, EPI) \
     if (tile == TILE && gated == GATED && epi == EPI) { \
-        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, NA, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, pair); \
+        hipLaunchKernelGGL((dense_kernel<ELEM, WM, WN, FM, FN, NST, NA, GATED, EPI>), grid, dim3(WM * WN * 64), 0, st, args(Known<EPI>{})); \
         return LBA_OK; \
     }
 #define LBA_DENSE_SMALL(GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, 1, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, 1, GATED, EPI)

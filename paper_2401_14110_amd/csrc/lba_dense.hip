@@ -1,8 +1,9 @@
 // lba_dense.hip -- the dense product's plan, its operands' copies, the joining of sliced sums, and the entry points.
 //
 // Operands whose rows the tile cannot read where they are (rows off 16 bytes, codes of five exponent bits, sums over rows) are laid out once
-// per call in the workspace: a pass over one byte an element beside a product of K (or N) operations on each (12 M codes transposed to
-// bfloat16: 10 us, 3.6 TB/s; 6 M codes to rows of their own: 5 us).
+// per call in the workspace: a pass over one byte an element beside a product of K (or N) operations on each.  What the gradient products read is
+// laid out by workgroups beside those of the gradient of the sums (12 M codes: 10 us in a launch of their own, none beside 105 us of sums);
+// what the sums themselves read takes a launch before them (6 M codes: 5 us).
 #include "lba_dense.h"
 #include "lba_internal.h"
 
@@ -10,111 +11,9 @@ namespace lba {
 
 constexpr int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// ---- operands laid out for the tile ---------------------------------------------------------
-
-// One launch lays out up to five operands: workgroups from `first` on belong to a job.
-enum { LAY_CODES = 0, LAY_BF16 = 1, LAY_TRANSPOSED = 2 };
-struct LayJob {
-    const uint8_t* src;      // [R, K] codes
-    uint8_t* dst;
-    int64_t R;
-    int64_t ld;              // bytes of a row of dst
-    int32_t K;
-    int32_t wide;            // LAY_TRANSPOSED: R rounded up to 8: columns of dst, zeros from R on
-    int32_t tiles_k;         // LAY_TRANSPOSED: tiles along k
-    int32_t kind;
-    uint32_t first;
-    CodeBits bits;
-};
-struct LayJobs { LayJob job[5]; int32_t n; };
-
-// rows of codes or of bfloat16 numbers, zeros behind K: 16 bytes of output a lane
-template <bool BF16> __device__ __forceinline__ void lay_rows(const LayJob& p, int64_t block) {
-    constexpr int PER = BF16 ? 8 : 16;
-    const uint32_t per_row = (uint32_t)(p.ld / 16), i = (uint32_t)block * 256 + threadIdx.x;   // fewer than 2^30 pieces (lay_fits)
-    if (i >= (uint32_t)p.R * per_row) return;
-    const uint32_t r = i / per_row;
-    const int k = (int)(i - r * per_row) * PER;
-    const uint8_t* s = p.src + (int64_t)r * p.K + k;
-    uint32_t w[PER / 4];
-    if (k + PER <= p.K) {
-        typedef uint32_t words __attribute__((ext_vector_type(PER / 4), aligned(1)));
-        const words x = *(const words*)s;
-#pragma unroll
-        for (int j = 0; j < PER / 4; ++j) w[j] = x[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < PER / 4; ++j) w[j] = 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
-    }
-    i32x4 o;
-    if constexpr (BF16) {
-        uint32_t lo, hi;
-        code_bf16(w[0], p.bits, lo, hi); o[0] = (int32_t)lo; o[1] = (int32_t)hi;
-        code_bf16(w[1], p.bits, lo, hi); o[2] = (int32_t)lo; o[3] = (int32_t)hi;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = (int32_t)w[j];
-    }
-    *(i32x4*)(p.dst + (int64_t)r * p.ld + (i - r * per_row) * 16) = o;
-}
-
-// dst [K][ld] bfloat16: 64 rows of 128 codes through LDS.  A lane reads four neighbouring codes of eight rows and writes four pieces of 16 bytes,
-// eight lanes side by side; rows of 33 words put the words that a wave reads at a time into 64 different banks.
-constexpr int kLayK = 128;
-__device__ __forceinline__ void lay_transposed(const LayJob& p, int64_t block) {
-    __shared__ uint32_t t[64][kLayK / 4 + 1];
-    const int64_t r0 = block / p.tiles_k * 64;
-    const int k0 = (int)(block % p.tiles_k) * kLayK;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = h * 256 + threadIdx.x, r = i / 8, c = i % 8, k = k0 + c * 16;
-        u32x4 w = {0, 0, 0, 0};
-        if (r0 + r < p.R && k < p.K) {
-            const uint8_t* s = p.src + (r0 + r) * p.K + k;
-            if (k + 16 <= p.K) {
-                typedef uint32_t words __attribute__((ext_vector_type(4), aligned(1)));
-                w = *(const words*)s;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (k + j < p.K) w[j / 4] |= (uint32_t)s[j] << (8 * (j % 4));
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) t[r][c * 4 + j] = w[j];
-    }
-    __syncthreads();
-    const int r = threadIdx.x % 8 * 8, kw = threadIdx.x / 8;
-    if (r0 + r >= p.wide) return;
-    uint32_t w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = t[r + j][kw];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int k = k0 + kw * 4 + q;
-        if (k >= p.K) return;
-        i32x4 o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t a = __float_as_uint(code_value((w[2 * j] >> (8 * q)) & 0xFFu, p.bits));
-            const uint32_t b = __float_as_uint(code_value((w[2 * j + 1] >> (8 * q)) & 0xFFu, p.bits));
-            o[j] = (int32_t)__builtin_amdgcn_perm(b, a, 0x07060302u);
-        }
-        *(i32x4*)(p.dst + k * p.ld + (r0 + r) * 2) = o;
-    }
-}
-
 __global__ __launch_bounds__(256) void dense_lay_kernel(LayJobs jobs) {
-    int j = 0;
-    while (j + 1 < jobs.n && blockIdx.x >= jobs.job[j + 1].first) ++j;
-    const LayJob& p = jobs.job[j];
-    const int64_t block = blockIdx.x - p.first;
-    if (p.kind == LAY_CODES) lay_rows<false>(p, block);
-    else if (p.kind == LAY_BF16) lay_rows<true>(p, block);
-    else lay_transposed(p, block);
+    __shared__ uint32_t t[kLayWords];
+    lay_block(jobs, blockIdx.x, t);
 }
 
 // adds the slices of a product's sums, in order, and finishes the outputs: of one product or of two
@@ -374,7 +273,7 @@ static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* d
 static bool lay_fits(int64_t R, int64_t K) { return (R + 64) * (K + 64) <= ((int64_t)1 << 32); }
 
 // one product, or two that share a launch
-static int run_products(GemmParams* g, const Product* p, int n, const SideSums* sums, int tile, int elem, bool gated, int epi, hipStream_t st) {
+static int run_products(GemmParams* g, const Product* p, int n, const Beside* side, int tile, int elem, bool gated, int epi, hipStream_t st) {
     JoinPair join = {};
     int sliced = 0;
     for (int i = 0; i < n; ++i) {
@@ -385,9 +284,9 @@ static int run_products(GemmParams* g, const Product* p, int n, const SideSums* 
     const int x = n > 1 && p[1].per_slice > p[0].per_slice ? 1 : 0;                  // the longer workgroups first
     const GemmParams* second = n > 1 ? &g[1 - x] : nullptr;
     int rc;
-    if (elem == ELEM_E4M3) rc = launch_dense_e4m3(g[x], second, tile, gated, epi, st);
-    else if (elem == ELEM_F16) rc = launch_dense_f16(g[x], second, tile, gated, epi, st);
-    else rc = launch_dense_bf16(g[x], second, sums, tile, gated, epi, st);
+    if (elem == ELEM_E4M3) rc = launch_dense_e4m3(g[x], second, side, tile, gated, epi, st);
+    else if (elem == ELEM_F16) rc = launch_dense_f16(g[x], second, side, tile, gated, epi, st);
+    else rc = launch_dense_bf16(g[x], second, side, tile, gated, epi, st);
     if (rc != LBA_OK || !sliced) return rc;
     join.blocks = join_blocks(join.p[0].e);
     const dim3 grid((unsigned)(join.blocks + (sliced > 1 ? join_blocks(join.p[1].e) : 0)));
@@ -511,25 +410,26 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     GemmParams g = {};
     g.A = A; g.B = B; g.lda = g.ldb = b.f.ld;
     const int32_t wide = (int32_t)up_to(N, 8);
-    LayJobs jobs = {};
-    uint32_t blocks = 0;
-    if (b.sums && !b.f.in_place) {
+    Beside side = {};
+    if (b.sums && !b.f.in_place) {                       // what the sums read, before them
+        LayJobs jobs = {};
+        uint32_t blocks = 0;
         const int kind = b.f.elem == ELEM_BF16 ? LAY_BF16 : LAY_CODES;
         add_job(jobs, blocks, A, ws + b.f.copy_a, M, K, b.f.ld, kind, fmt_a);
         add_job(jobs, blocks, B, ws + b.f.copy_b, cols, K, b.f.ld, kind, fmt_b);
+        if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
         g.A = ws + b.f.copy_a; g.B = ws + b.f.copy_b;
     }
-    if (dA) {
-        add_job(jobs, blocks, B, ws + b.bt, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
-        if (two) add_job(jobs, blocks, B + N * K, ws + b.bt + wide * 2, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
+    if (dA) {                                            // what the gradient products read, beside them
+        add_job(side.jobs, side.job_blocks, B, ws + b.bt, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
+        if (two) add_job(side.jobs, side.job_blocks, B + N * K, ws + b.bt + wide * 2, N, K, b.ldp * 2, LAY_TRANSPOSED, fmt_b);
     }
-    if (dB) add_job(jobs, blocks, A, ws + b.at, M, K, b.ldt * 2, LAY_TRANSPOSED, fmt_a);
-    if (jobs.n) hipLaunchKernelGGL(dense_lay_kernel, dim3(blocks), dim3(256), 0, st, jobs);
+    if (dB) add_job(side.jobs, side.job_blocks, A, ws + b.at, M, K, b.ldt * 2, LAY_TRANSPOSED, fmt_a);
     g.rows_a = (int32_t)M; g.rows_b = (int32_t)cols; g.half = (int32_t)N;
     g.chunks = b.sums ? (int32_t)b.f.chunks : 0; g.steps = b.sums ? (int32_t)b.f.steps : 0;
     g.shift_a = ea.shift; g.shift_b = eb.shift; g.keep_a = ea.keep; g.keep_b = eb.keep;
     g.e = e;
-    rc = run_products(&g, &b.f.fwd, 1, nullptr, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
+    rc = run_products(&g, &b.f.fwd, 1, &side, b.f.tile, b.f.elem, two, EPI_BACKWARD, st);
     if (rc != LBA_OK) return rc;
 
     // the two products of it, and dbias beside them
@@ -537,7 +437,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
         if (dbias) launch_column_sum(e.part, b.part_rows, cols, dbias, nullptr, cols, st);
         return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
     }
-    const SideSums sums = {e.part, dbias, (int32_t)b.part_rows, (int32_t)cols};
+    if (dbias) side.sums = {e.part, dbias, (int32_t)b.part_rows, (int32_t)cols};
     GemmParams q[2] = {};
     Product parts[2];
     int n = 0;
@@ -560,7 +460,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
         q[i].steps = (int32_t)parts[i].steps;
         q[i].e.N = (int32_t)K; q[i].e.y_type = g_type;
     }
-    rc = run_products(q, parts, n, dbias ? &sums : nullptr, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
+    rc = run_products(q, parts, n, &side, b.tile, ELEM_BF16, false, EPI_FORWARD, st);
     if (rc != LBA_OK) return rc;
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }

@@ -3,7 +3,7 @@
 #include "lba_dense.h"
 
 namespace lba {
-int launch_dense_bf16(const GemmParams& a, const GemmParams* b, const SideSums* sums, int tile, bool gated, int epi, hipStream_t st) {
-    return launch_dense<ELEM_BF16>(a, b, sums, tile, gated, epi, st);
+int launch_dense_bf16(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st) {
+    return launch_dense<ELEM_BF16>(a, b, side, tile, gated, epi, st);
 }
 }  // namespace lba

@@ -2,7 +2,7 @@
 #include "lba_dense.h"
 
 namespace lba {
-int launch_dense_f16(const GemmParams& a, const GemmParams* b, int tile, bool gated, int epi, hipStream_t st) {
-    return launch_dense<ELEM_F16>(a, b, nullptr, tile, gated, epi, st);
+int launch_dense_f16(const GemmParams& a, const GemmParams* b, const Beside* side, int tile, bool gated, int epi, hipStream_t st) {
+    return launch_dense<ELEM_F16>(a, b, side, tile, gated, epi, st);
 }
 }  // namespace lba
