@@ -660,7 +660,7 @@ def _infmt(f):
 def _on(stream, device):
     """(handle, stream) of a call on tensors of the device: stream is None where it is the current one, else the object that
     tensors made here are recorded on."""
-    if device != torch.cuda.current_device():
+    if device != torch._C._cuda_getDevice():
         raise ValueError("the tensors' device is not the current one")
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(device), None
@@ -707,10 +707,10 @@ def _rows(t, what, dtypes=_REAL):
     device = t.get_device()
     if t.dtype not in dtypes or device < 0:
         raise TypeError("%s must be a device tensor of %s" % (what, " or ".join(str(d) for d in dtypes)))
-    shape = t.shape
-    if not shape:
+    if t.dim() < 1:
         raise ValueError("%s must have at least one axis" % what)
-    return math.prod(shape[:-1]), shape[-1], device
+    n = t.size(-1)
+    return t.numel() // n if n else math.prod(t.shape[:-1]), n, device
 
 
 def _like(t, shape, device, what, dtypes=_REAL):
@@ -724,7 +724,7 @@ def _like(t, shape, device, what, dtypes=_REAL):
 def _vector(t, n, device, what, on):
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.get_device() != device or t.shape != (n,):
+    if t.dtype != torch.float32 or t.get_device() != device or t.dim() != 1 or t.numel() != n:
         raise ValueError("%s must be a float32 tensor [%d] on the call's device" % (what, n))
     return _whole(t, on)
 
@@ -777,7 +777,7 @@ def layernorm(x, gamma=None, beta=None, eps=1e-5, out_dtype=None, out_fmt=None, 
     x, gamma, beta = _whole(x, on), _vector(gamma, N, device, "gamma", on), _vector(beta, N, device, "beta", on)
     y = _output(out, x, x.shape, dtype, on)
     mean = _empty(x.shape[:-1], torch.float32, x.device, on) if want_stats else None
-    rstd = _empty(x.shape[:-1], torch.float32, x.device, on) if want_stats else None
+    rstd = _empty_as(mean, torch.float32, on) if want_stats else None
     _check(lib().lba_layernorm(_at(x), _TYPE[x.dtype], _at(gamma), _at(beta), eps, _at(y), y_type, fmt, _at(mean), _at(rstd), M, N, handle))
     return (y, mean, rstd) if want_stats else y
 
@@ -793,7 +793,7 @@ def layernorm_bwd(G, x, gamma, mean, rstd, want_dx=True, want_params=True, strea
     G, x, mean, rstd, gamma = _whole(G, on), _whole(x, on), _whole(mean, on), _whole(rstd, on), _vector(gamma, N, device, "gamma", on)
     dx = _empty_as(x, x.dtype, on) if want_dx else None
     dgamma = _empty((N,), torch.float32, x.device, on) if want_params else None
-    dbeta = _empty((N,), torch.float32, x.device, on) if want_params else None
+    dbeta = _empty_as(dgamma, torch.float32, on) if want_params else None
     size = _layer_bytes("lba_layernorm_bwd_workspace_bytes", M, N) if want_params else 0
     ws = _scratch(size, x.device, on)
     _check(lib().lba_layernorm_bwd(_at(G), _TYPE[G.dtype], _at(x), _TYPE[x.dtype], _at(gamma), _at(mean), _at(rstd), _at(dx),
