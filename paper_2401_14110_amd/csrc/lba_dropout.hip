@@ -7,7 +7,7 @@
 // backward pass, dbias, stay in registers; a workgroup writes one row of partial sums, and a second launch adds them in a fixed order.
 // Columns beyond the last full strip of 64 vectors have lanes of their own: as many rows side by side in a wave as they fit.
 // Measured, memory the bound: 4096 x 768 float32 with bias and residual 8.0 us, 4.7 TB/s; 16411 x 4099 bfloat16 with GELU forward 61 us,
-// 4.4 TB/s, backward with the column sums 96 + 5 us, 4.0 TB/s (there the words of the mask and GELU's slope are most of the time that is left:
+// 4.4 TB/s, backward with the column sums 96 + 5 us, 4.0 TB/s (a tenth fewer instructions changed nothing;
 // at a width of 4096 it is 92).
 #include "lba_layer_device.h"
 #include "lba_internal.h"
@@ -114,6 +114,7 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) bias[j] = sum[j] = 0.0f;
     constexpr bool read_x = ACT != LBA_ACT_NONE;
+    const float keep_scale = p.drop.on ? p.drop.keep_scale : 1.0f, dx_scale = p.scale * keep_scale;
     if (p.bias && read_x) load_some<V>(p.bias + q.col, q.cols, bias);
     auto rows = [&](auto full) {
         constexpr bool FULL = decltype(full)::value != 0;
@@ -135,12 +136,12 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
             }
             if (p.drop.on) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) g[j] = keep[j] ? g[j] * p.drop.keep_scale : 0.0f;
+                for (int j = 0; j < V; ++j) g[j] = keep[j] ? g[j] : 0.0f;
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                sum[j] += g[j];
-                g[j] *= p.scale;
+                sum[j] += g[j];                          // what is kept is scaled once, at the end
+                g[j] *= dx_scale;
             }
             if (p.Y) {
                 if constexpr (FULL) store_vec<V>((TX*)p.Y + i, g, p.fmt);
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int at = j * 64 + threadIdx.x;
-        sum[j] = (lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at]);
+        sum[j] = ((lds[0][at] + lds[1][at]) + (lds[2][at] + lds[3][at])) * keep_scale;
     }
     store_some<V>(p.part + (int64_t)q.chunk * p.N + q.col, q.cols, sum, p.fmt);
 }

@@ -127,28 +127,28 @@ __device__ __forceinline__ float exp_near(float x) {
     return x > 88.72f ? __builtin_inff() : fmaf(e, left * 0.693147181f, e);
 }
 
-// The normal distribution's tail Phi(-a) for a = |z|, and e^(-z^2/2).  Phi(-a) = e^(-a^2/2) * h(t) with t = 1 / (1 + 0.28 a); h is smooth and is
+// The normal distribution's tail Phi(-a) for a = |z|, and its density phi.  Phi(-a) = phi(a) * h(t) with t = 1 / (1 + 0.28 a); h is smooth and is
 // taken as a polynomial of degree 6 without a constant term, fitted to (1 + a) * Phi in the largest error (1.5e-8).  With it z * Phi(z) is
 // max(z, 0) - a * Phi(-a) for either sign: nothing cancels in the tail, and nothing is chosen by a comparison.  `a` is at most 64, where
 // the tail is 0 as a float32 number, so that an infinity does not meet that zero; a NaN comes through the exponential.
-__device__ __forceinline__ float normal_tail(float z, float& a, float& e) {
+__device__ __forceinline__ float normal_tail(float z, float& a, float& phi) {
     a = fminf(fabsf(z), 64.0f);
     const float t = __builtin_amdgcn_rcpf(fmaf(0.28f, a, 1.0f));
-    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-    float h = fmaf(t, -0.10655423f, 0.39296786f);
-    h = fmaf(t, h, -0.24209468f);
-    h = fmaf(t, h, 0.27308893f);
-    h = fmaf(t, h, 0.065796522f);
-    h = fmaf(t, h, 0.11679558f);
-    return e * (t * h);
+    phi = __builtin_amdgcn_exp2f(fmaf(z * z, -0.72134752f, -1.32574809f));
+    float h = fmaf(t, -0.267091841f, 0.985024333f);
+    h = fmaf(t, h, -0.606841385f);
+    h = fmaf(t, h, 0.684532404f);
+    h = fmaf(t, h, 0.164927423f);
+    h = fmaf(t, h, 0.292763114f);
+    return phi * (t * h);
 }
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_near(-z)); }
 
 template <int ACT> __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == LBA_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
     if constexpr (ACT == LBA_ACT_GELU) {
-        float a, e;
-        const float q = normal_tail(z, a, e);
+        float a, phi;
+        const float q = normal_tail(z, a, phi);
         return fmaf(-a, q, fmaxf(z, 0.0f));
     }
     if constexpr (ACT == LBA_ACT_SILU) return z * logistic(z);
@@ -160,10 +160,10 @@ template <int ACT> __device__ __forceinline__ void act_both(float z, float& valu
         value = z > 0.0f ? z : (z != z ? z : 0.0f);
         slope = z > 0.0f ? 1.0f : 0.0f;
     } else if constexpr (ACT == LBA_ACT_GELU) {
-        float a, e;
-        const float q = normal_tail(z, a, e);
+        float a, phi;
+        const float q = normal_tail(z, a, phi);
         value = fmaf(-a, q, fmaxf(z, 0.0f));
-        slope = fmaf(copysignf(a, z) * 0.39894228f, e, z < 0.0f ? q : 1.0f - q);
+        slope = fmaf(copysignf(a, z), phi, z < 0.0f ? q : 1.0f - q);
     } else if constexpr (ACT == LBA_ACT_SILU) {
         const float h = logistic(z);
         value = z * h;
