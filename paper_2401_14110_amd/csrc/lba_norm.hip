@@ -7,7 +7,7 @@
 // a second launch adds them in a fixed order.
 // Both are bound by memory: every element is moved once.  A row belongs to a wave where four vectors of 16 bytes a lane hold it (two of
 // bfloat16), else to a workgroup of 256, 512 or 1024 lanes; rows beyond 16384 elements are read again from cache for each pass.
-// Measured (bytes that have to move over the kernel's time; a copy of 1 GiB reaches 5.2 TB/s): 16384 x 4096 bfloat16 forward 67 us, 4.0 TB/s,
+// Measured (bytes that have to move over the kernel's time; a copy of 1 GiB reaches 5.2 TB/s): 16384 x 4096 bfloat16 forward 53 us, 5.1 TB/s,
 // backward 78 + 7 us for the column sums, 4.8 TB/s; 4096 x 768 float32 to codes 6.3 us, backward 9.8 + 3.7; 1024 x 16384 float32 backward
 // 38 + 11; one row of 768: 3 us, a launch.
 #include "lba_layer_device.h"
@@ -51,59 +51,97 @@ struct NormParams {
     CodeFmt fmt;
 };
 
+// a vector as it comes from memory: converted where it is used, so that nothing waits for a load that is under way
+template <typename T, int V> struct Raw { typename Vec<T, V>::type v; };
+template <int V> __device__ __forceinline__ float raw_at(const Raw<float, V>& r, int j) { return r.v[j]; }
+template <int V> __device__ __forceinline__ float raw_at(const Raw<uint16_t, V>& r, int j) { return __uint_as_float((uint32_t)r.v[j] << 16); }
+template <typename T> struct Bits { typedef uint16_t type; };
+template <> struct Bits<float> { typedef float type; };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p, int n) {
+    Raw<T, V> r;
+    if (n >= V) {
+        r.v = *(const typename Vec<T, V>::type*)p;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = j < n ? p[j] : (T)0;
+    }
+    return r;
+}
+
+// A lane group walks over rows: gamma and beta stay in registers and the next row is loaded while this one is worked on (two sets of registers,
+// so that none is moved while in flight).
 template <typename TX, typename TY, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_fwd_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
+    typedef typename Bits<TX>::type BX;
     __shared__ float lds[2 * (T / 64)];
-    const int t = threadIdx.x % T;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T; row < p.M; row += (int64_t)gridDim.x * RPB) {
-    const TX* x = (const TX*)p.X + row * p.N;
-    float v[NV][V];
-    float s[1] = {0.0f};
+    const int t = threadIdx.x % T, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
+    struct Row { Raw<BX, V> x[NV]; };
+    auto load = [&](int64_t row, Row& r) {
+        const BX* x = (const BX*)p.X + row * p.N;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * T + t) * V;
-        load_some<V>(x + c, p.N - c, v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[0] += v[i][j];
-    row_sums<T, 1>(s, lds, 0);
-    const float mean = s[0] / p.n;
-    s[0] = 0.0f;
+        for (int i = 0; i < NV; ++i) r.x[i] = load_raw<BX, V>(x + (i * T + t) * V, p.N - (i * T + t) * V);
+    };
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + sub;
+    Row a, b;
+    if (row < p.M) load(row, a);
+    float ga[NV][V], be[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * T + t) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            v[i][j] -= mean;
-            if (c + j < p.N) s[0] = fmaf(v[i][j], v[i][j], s[0]);
+            ga[i][j] = 1.0f;
+            be[i][j] = 0.0f;
         }
+        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, ga[i]);
+        if (p.beta) load_some<V>(p.beta + c, p.N - c, be[i]);
     }
-    row_sums<T, 1>(s, lds, 1);
-    const float rstd = 1.0f / sqrtf(s[0] / p.n + p.eps);
-    if (t == 0) {
-        if (p.mean) p.mean[row] = mean;
-        if (p.rstd) p.rstd[row] = rstd;
-    }
-    TY* y = (TY*)p.Y + row * p.N;
+    auto work = [&](int64_t at, const Row& r) {
+        float v[NV][V], s[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * T + t) * V;
-        if (c >= p.N) break;
-        float ga[V], be[V];
-        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, ga);
-        if (p.beta) load_some<V>(p.beta + c, p.N - c, be);
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float o = v[i][j] * rstd;
-            if (p.gamma) o *= ga[j];
-            if (p.beta) o += be[j];
-            v[i][j] = o;
+            for (int j = 0; j < V; ++j) {
+                v[i][j] = raw_at(r.x[i], j);             // 0 beyond the row
+                s[0] += v[i][j];
+            }
+        row_sums<T, 1>(s, lds, 0);
+        const float mean = s[0] / p.n;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * T + t) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[i][j] -= mean;
+                if (c + j < p.N) s[0] = fmaf(v[i][j], v[i][j], s[0]);
+            }
         }
-        store_some<V>(y + c, p.N - c, v[i], p.fmt);
-    }
+        row_sums<T, 1>(s, lds, 1);
+        const float rstd = 1.0f / sqrtf(s[0] / p.n + p.eps);
+        if (t == 0) {
+            if (p.mean) p.mean[at] = mean;
+            if (p.rstd) p.rstd[at] = rstd;
+        }
+        TY* y = (TY*)p.Y + at * p.N;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * T + t) * V;
+            if (c >= p.N) break;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[i][j] = fmaf(v[i][j] * rstd, ga[i][j], be[i][j]);
+            store_some<V>(y + c, p.N - c, v[i], p.fmt);
+        }
+    };
+    for (; row < p.M; row += 2 * step) {
+        const bool more = row + step < p.M;
+        if (more) load(row + step, b);
+        work(row, a);
+        if (!more) break;
+        if (row + 2 * step < p.M) load(row + 2 * step, a);
+        work(row + step, b);
     }
 }
 
@@ -151,24 +189,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormParams p) {
     }
 }
 
-// a vector as it comes from memory: converted where it is used, so that nothing waits for a load that is under way
-template <typename T, int V> struct Raw { typename Vec<T, V>::type v; };
-template <int V> __device__ __forceinline__ float raw_at(const Raw<float, V>& r, int j) { return r.v[j]; }
-template <int V> __device__ __forceinline__ float raw_at(const Raw<uint16_t, V>& r, int j) { return __uint_as_float((uint32_t)r.v[j] << 16); }
-template <typename T> struct Bits { typedef uint16_t type; };
-template <> struct Bits<float> { typedef float type; };
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p, int n) {
-    Raw<T, V> r;
-    if (n >= V) {
-        r.v = *(const typename Vec<T, V>::type*)p;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = j < n ? p[j] : (T)0;
-    }
-    return r;
-}
-
-// The next row of a lane group is loaded while this one is worked on (two sets of registers, so that none is moved while in flight), but for
+// The next row of a lane group is loaded while this one is worked on, but for
 // workgroups of 1024 lanes, whose 128 registers do not hold both.
 template <typename TG, typename TX, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_bwd_kernel(NormParams p) {
@@ -407,25 +428,30 @@ static RowShape row_shape(int64_t N, int v) {
     return {0, 0};
 }
 
+// lanes of a forward launch: as many as the chip holds at a time, each of which walks over rows
+constexpr int64_t kNormLanes = 256 * 2048;
+
 template <typename TX, typename TY> static void norm_fwd(const NormParams& p, hipStream_t st) {
     const RowShape r = row_shape(p.N, 16 / (int)sizeof(TX));
-    const int64_t most = 1 << 20;                        // a launch holds fewer than 2^32 lanes: the kernels walk over the rows beyond
-    const dim3 wide((unsigned)(p.M < most ? p.M : most)), four((unsigned)((p.M + 3) / 4 < most ? (p.M + 3) / 4 : most));
-#define LBA_NORM_FWD(T, NV, GRID) \
-    if (r.lanes == T && r.vecs == NV) { hipLaunchKernelGGL((norm_fwd_kernel<TX, TY, T, NV>), GRID, dim3(T < 256 ? 256 : T), 0, st, p); return; }
-    LBA_NORM_FWD(64, 1, four)
-    LBA_NORM_FWD(64, 2, four)
-    LBA_NORM_FWD(256, 2, wide)
-    LBA_NORM_FWD(512, 2, wide)
-    LBA_NORM_FWD(1024, 2, wide)
+    const int lanes = r.lanes < 256 ? 256 : r.lanes;
+    const int64_t groups = r.lanes == 64 ? (p.M + 3) / 4 : p.M, most = kNormLanes / lanes;
+    const dim3 grid((unsigned)(groups < most ? groups : most));
+#define LBA_NORM_FWD(T, NV) \
+    if (r.lanes == T && r.vecs == NV) { hipLaunchKernelGGL((norm_fwd_kernel<TX, TY, T, NV>), grid, dim3(T < 256 ? 256 : T), 0, st, p); return; }
+    LBA_NORM_FWD(64, 1)
+    LBA_NORM_FWD(64, 2)
+    LBA_NORM_FWD(256, 2)
+    LBA_NORM_FWD(512, 2)
+    LBA_NORM_FWD(1024, 2)
     if constexpr (sizeof(TX) == 4) {
-        LBA_NORM_FWD(64, 4, four)
-        LBA_NORM_FWD(256, 4, wide)
-        LBA_NORM_FWD(512, 4, wide)
-        LBA_NORM_FWD(1024, 4, wide)
+        LBA_NORM_FWD(64, 4)
+        LBA_NORM_FWD(256, 4)
+        LBA_NORM_FWD(512, 4)
+        LBA_NORM_FWD(1024, 4)
     }
 #undef LBA_NORM_FWD
-    hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), wide, dim3(1024), 0, st, p);
+    const int64_t rows = 1 << 20;                        // a launch holds fewer than 2^32 lanes: the kernel walks over the rows beyond
+    hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), dim3((unsigned)(p.M < rows ? p.M : rows)), dim3(1024), 0, st, p);
 }
 
 // Workgroups of the backward pass, each of which writes a row of partial sums: enough to fill the chip, few enough that these rows stay a
