@@ -7,8 +7,8 @@
 // backward pass, dbias, stay in registers; a workgroup writes one row of partial sums, and a second launch adds them in a fixed order.
 // Columns beyond the last full strip of 64 vectors have lanes of their own: as many rows side by side in a wave as they fit.
 // Measured, memory the bound: 4096 x 768 float32 with bias and residual 8.0 us, 4.7 TB/s; 16411 x 4099 bfloat16 with GELU forward 61 us,
-// 4.4 TB/s, backward with the column sums 96 + 5 us, 4.0 TB/s (a tenth fewer instructions changed nothing;
-// at a width of 4096 it is 92).
+// 4.4 TB/s, backward with the column sums 88 + 5 us, 4.4 TB/s (95 + 5 without the next row under way; a tenth fewer instructions changed
+// nothing).
 #include "lba_layer_device.h"
 #include "lba_internal.h"
 
@@ -53,9 +53,23 @@ template <int V> __device__ __forceinline__ LanePlace lane_place(const DropoutPa
 }
 
 // A row's vector of a lane: in a full strip whole, and the wave's lanes, all of which take part, share the words of the generator.
-template <bool FULL, int V, typename T> __device__ __forceinline__ void load_part(const T* at, int n, float (&v)[V]) {
-    if constexpr (FULL) load_vec<V>(at, v);
-    else load_some<V>(at, n, v);
+template <bool FULL, typename T, int V> __device__ __forceinline__ Raw<T, V> load_part(const T* at, int n) {
+    return load_raw<T, V>(at, FULL ? V : n);
+}
+// a lane's rows, the next one under way while one is worked on (two sets of registers, so that none is moved while in flight)
+template <typename Row, typename Load, typename Work> __device__ __forceinline__ void walk(const LanePlace& q, const Load& load, const Work& work) {
+    Row a, b;
+    int64_t row = q.row;
+    if (row < q.end) load(row, a);
+#pragma unroll 1
+    for (; row < q.end; row += 2 * q.step) {
+        const bool more = row + q.step < q.end;
+        if (more) load(row + q.step, b);
+        work(row, a);
+        if (!more) break;
+        if (row + 2 * q.step < q.end) load(row + 2 * q.step, a);
+        work(row + q.step, b);
+    }
 }
 template <bool FULL, int V> __device__ __forceinline__ void keeps(const DropoutParams& p, const LanePlace& q, int64_t row, int64_t i, uint64_t base, bool (&keep)[V]) {
     if constexpr (FULL && V == 8) {
@@ -69,6 +83,7 @@ template <bool FULL, int V> __device__ __forceinline__ void keeps(const DropoutP
 template <typename TX, typename TY, int ACT>
 __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
     constexpr int V = 16 / sizeof(TX);
+    typedef typename Bits<TX>::type BX;
     const LanePlace q = lane_place<V>(p);
     if (q.cols <= 0) return;
     const uint64_t base = drop_base(p.drop);
@@ -76,29 +91,44 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) bias[j] = 0.0f;
     if (p.bias) load_some<V>(p.bias + q.col, q.cols, bias);
+    // the residual's vectors of either type are loaded as what they are
+    const int r_kind = !p.R ? 0 : p.r_type == LBA_F32 ? 1 : 2;
     auto rows = [&](auto full) {
         constexpr bool FULL = decltype(full)::value != 0;
-#pragma unroll 1
-        for (int64_t row = q.row; row < q.end; row += q.step) {
+        struct Row { Raw<BX, V> x; Raw<float, V> rf; Raw<uint16_t, V> rh; };
+        auto load = [&](int64_t row, Row& w) {
             const int64_t i = row * p.N + q.col;
-            float x[V], r[V];
+            w.x = load_part<FULL, BX, V>((const BX*)p.X + i, q.cols);
+            if (r_kind == 1) w.rf = load_part<FULL, float, V>((const float*)p.R + i, q.cols);
+            else if (r_kind == 2) w.rh = load_part<FULL, uint16_t, V>((const uint16_t*)p.R + i, q.cols);
+        };
+        auto work = [&](int64_t row, const Row& w) {
+            const int64_t i = row * p.N + q.col;
+            float x[V];
             bool keep[V];
-            load_part<FULL, V>((const TX*)p.X + i, q.cols, x);
-            if (p.R && p.r_type == LBA_F32) load_part<FULL, V>((const float*)p.R + i, q.cols, r);
-            else if (p.R) load_part<FULL, V>((const bf16_t*)p.R + i, q.cols, r);
             if (p.drop.on) keeps<FULL, V>(p, q, row, i, base, keep);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = act_value<ACT>(fmaf(x[j], p.scale, bias[j]));
+            for (int j = 0; j < V; ++j) x[j] = act_value<ACT>(fmaf(raw_at(w.x, j), p.scale, bias[j]));
             if (p.drop.on) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[j] = keep[j] ? x[j] * p.drop.keep_scale : 0.0f;
             }
-            if (p.R) {
+            if (r_kind == 1) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) x[j] += r[j];
+                for (int j = 0; j < V; ++j) x[j] += raw_at(w.rf, j);
+            } else if (r_kind == 2) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] += raw_at(w.rh, j);
             }
             if constexpr (FULL) store_vec<V>((TY*)p.Y + i, x, p.fmt);
             else store_some<V>((TY*)p.Y + i, q.cols, x, p.fmt);
+        };
+        // (the next row under way did not pay here, with four times the workgroups of the backward pass: 61 us became 70)
+#pragma unroll 1
+        for (int64_t row = q.row; row < q.end; row += q.step) {
+            Row w;
+            load(row, w);
+            work(row, w);
         }
     };
     if ((int)blockIdx.x < p.main_blocks) rows(Known<1>{});
@@ -108,6 +138,8 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
 template <typename TG, typename TX, int ACT>
 __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
     constexpr int V = 16 / sizeof(TX);
+    typedef typename Bits<TX>::type BX;
+    typedef typename Bits<TG>::type BG;
     const LanePlace q = lane_place<V>(p);
     const uint64_t base = drop_base(p.drop);
     float bias[V], sum[V];
@@ -118,19 +150,23 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
     if (p.bias && read_x) load_some<V>(p.bias + q.col, q.cols, bias);
     auto rows = [&](auto full) {
         constexpr bool FULL = decltype(full)::value != 0;
-#pragma unroll 1
-        for (int64_t row = q.row; row < q.end; row += q.step) {
+        struct Row { Raw<BG, V> g; Raw<BX, V> x; };
+        auto load = [&](int64_t row, Row& w) {
             const int64_t i = row * p.N + q.col;
-            float x[V], g[V];
+            w.g = load_part<FULL, BG, V>((const BG*)p.G + i, q.cols);
+            if (read_x) w.x = load_part<FULL, BX, V>((const BX*)p.X + i, q.cols);
+        };
+        auto work = [&](int64_t row, const Row& w) {
+            const int64_t i = row * p.N + q.col;
+            float g[V];
             bool keep[V];
-            load_part<FULL, V>((const TG*)p.G + i, q.cols, g);
-            if (read_x) load_part<FULL, V>((const TX*)p.X + i, q.cols, x);
             if (p.drop.on) keeps<FULL, V>(p, q, row, i, base, keep);
-            if (read_x) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
+            for (int j = 0; j < V; ++j) {
+                g[j] = raw_at(w.g, j);
+                if (read_x) {
                     float value, slope;
-                    act_both<ACT>(fmaf(x[j], p.scale, bias[j]), value, slope);
+                    act_both<ACT>(fmaf(raw_at(w.x, j), p.scale, bias[j]), value, slope);
                     g[j] *= slope;
                 }
             }
@@ -147,7 +183,8 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
                 if constexpr (FULL) store_vec<V>((TX*)p.Y + i, g, p.fmt);
                 else store_some<V>((TX*)p.Y + i, q.cols, g, p.fmt);
             }
-        }
+        };
+        walk<Row>(q, load, work);
     };
     if ((int)blockIdx.x < p.main_blocks) rows(Known<1>{});
     else if (q.cols > 0) rows(Known<0>{});

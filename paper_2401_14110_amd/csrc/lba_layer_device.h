@@ -115,6 +115,23 @@ template <int V, typename T> __device__ __forceinline__ void store_some(T* p, in
         if (j < n) store_one(p + j, v[j], f);
 }
 
+// a vector as it comes from memory: converted where it is used, so that nothing waits for a load that is under way
+template <typename T, int V> struct Raw { typename Vec<T, V>::type v; };
+template <int V> __device__ __forceinline__ float raw_at(const Raw<float, V>& r, int j) { return r.v[j]; }
+template <int V> __device__ __forceinline__ float raw_at(const Raw<uint16_t, V>& r, int j) { return __uint_as_float((uint32_t)r.v[j] << 16); }
+template <typename T> struct Bits { typedef uint16_t type; };
+template <> struct Bits<float> { typedef float type; };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p, int n) {
+    Raw<T, V> r;
+    if (n >= V) {
+        r.v = *(const typename Vec<T, V>::type*)p;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = j < n ? p[j] : (T)0;
+    }
+    return r;
+}
+
 // ---- activations ----------------------------------------------------------------------------
 
 // e^x to 1.5 ulp: 2^t of the rounded product t = x log2 e, corrected by what the rounding left off.  Beyond float32's range the

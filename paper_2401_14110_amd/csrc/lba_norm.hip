@@ -51,23 +51,6 @@ struct NormParams {
     CodeFmt fmt;
 };
 
-// a vector as it comes from memory: converted where it is used, so that nothing waits for a load that is under way
-template <typename T, int V> struct Raw { typename Vec<T, V>::type v; };
-template <int V> __device__ __forceinline__ float raw_at(const Raw<float, V>& r, int j) { return r.v[j]; }
-template <int V> __device__ __forceinline__ float raw_at(const Raw<uint16_t, V>& r, int j) { return __uint_as_float((uint32_t)r.v[j] << 16); }
-template <typename T> struct Bits { typedef uint16_t type; };
-template <> struct Bits<float> { typedef float type; };
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_raw(const T* p, int n) {
-    Raw<T, V> r;
-    if (n >= V) {
-        r.v = *(const typename Vec<T, V>::type*)p;
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = j < n ? p[j] : (T)0;
-    }
-    return r;
-}
-
 // A lane group walks over rows: gamma and beta stay in registers and the next row is loaded while this one is worked on (two sets of registers,
 // so that none is moved while in flight).
 template <typename TX, typename TY, int T, int NV>
