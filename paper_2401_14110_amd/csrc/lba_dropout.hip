@@ -53,7 +53,11 @@ template <int V> __device__ __forceinline__ LanePlace lane_place(const DropoutPa
 }
 
 // A row's vector of a lane: in a full strip whole, and the wave's lanes, all of which take part, share the words of the generator.
-template <bool FULL, typename T, int V> __device__ __forceinline__ Raw<T, V> load_part(const T* at, int n) {
+template <bool FULL, int V, typename T> __device__ __forceinline__ void load_part(const T* at, int n, float (&v)[V]) {
+    if constexpr (FULL) load_vec<V>(at, v);
+    else load_some<V>(at, n, v);
+}
+template <bool FULL, typename T, int V> __device__ __forceinline__ Raw<T, V> raw_part(const T* at, int n) {
     return load_raw<T, V>(at, FULL ? V : n);
 }
 // a lane's rows, the next one under way while one is worked on (two sets of registers, so that none is moved while in flight)
@@ -83,7 +87,6 @@ template <bool FULL, int V> __device__ __forceinline__ void keeps(const DropoutP
 template <typename TX, typename TY, int ACT>
 __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
     constexpr int V = 16 / sizeof(TX);
-    typedef typename Bits<TX>::type BX;
     const LanePlace q = lane_place<V>(p);
     if (q.cols <= 0) return;
     const uint64_t base = drop_base(p.drop);
@@ -91,44 +94,30 @@ __global__ __launch_bounds__(256) void dropout_fwd_kernel(DropoutParams p) {
 #pragma unroll
     for (int j = 0; j < V; ++j) bias[j] = 0.0f;
     if (p.bias) load_some<V>(p.bias + q.col, q.cols, bias);
-    // the residual's vectors of either type are loaded as what they are
-    const int r_kind = !p.R ? 0 : p.r_type == LBA_F32 ? 1 : 2;
     auto rows = [&](auto full) {
         constexpr bool FULL = decltype(full)::value != 0;
-        struct Row { Raw<BX, V> x; Raw<float, V> rf; Raw<uint16_t, V> rh; };
-        auto load = [&](int64_t row, Row& w) {
+        // (The next row under way, as in the backward pass, did not pay here, with four times its workgroups: 61 us became 70.)
+#pragma unroll 1
+        for (int64_t row = q.row; row < q.end; row += q.step) {
             const int64_t i = row * p.N + q.col;
-            w.x = load_part<FULL, BX, V>((const BX*)p.X + i, q.cols);
-            if (r_kind == 1) w.rf = load_part<FULL, float, V>((const float*)p.R + i, q.cols);
-            else if (r_kind == 2) w.rh = load_part<FULL, uint16_t, V>((const uint16_t*)p.R + i, q.cols);
-        };
-        auto work = [&](int64_t row, const Row& w) {
-            const int64_t i = row * p.N + q.col;
-            float x[V];
+            float x[V], r[V];
             bool keep[V];
+            load_part<FULL, V>((const TX*)p.X + i, q.cols, x);
+            if (p.R && p.r_type == LBA_F32) load_part<FULL, V>((const float*)p.R + i, q.cols, r);
+            else if (p.R) load_part<FULL, V>((const bf16_t*)p.R + i, q.cols, r);
             if (p.drop.on) keeps<FULL, V>(p, q, row, i, base, keep);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = act_value<ACT>(fmaf(raw_at(w.x, j), p.scale, bias[j]));
+            for (int j = 0; j < V; ++j) x[j] = act_value<ACT>(fmaf(x[j], p.scale, bias[j]));
             if (p.drop.on) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) x[j] = keep[j] ? x[j] * p.drop.keep_scale : 0.0f;
             }
-            if (r_kind == 1) {
+            if (p.R) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) x[j] += raw_at(w.rf, j);
-            } else if (r_kind == 2) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[j] += raw_at(w.rh, j);
+                for (int j = 0; j < V; ++j) x[j] += r[j];
             }
             if constexpr (FULL) store_vec<V>((TY*)p.Y + i, x, p.fmt);
             else store_some<V>((TY*)p.Y + i, q.cols, x, p.fmt);
-        };
-        // (the next row under way did not pay here, with four times the workgroups of the backward pass: 61 us became 70)
-#pragma unroll 1
-        for (int64_t row = q.row; row < q.end; row += q.step) {
-            Row w;
-            load(row, w);
-            work(row, w);
         }
     };
     if ((int)blockIdx.x < p.main_blocks) rows(Known<1>{});
@@ -153,8 +142,8 @@ __global__ __launch_bounds__(256) void dropout_bwd_kernel(DropoutParams p) {
         struct Row { Raw<BG, V> g; Raw<BX, V> x; };
         auto load = [&](int64_t row, Row& w) {
             const int64_t i = row * p.N + q.col;
-            w.g = load_part<FULL, BG, V>((const BG*)p.G + i, q.cols);
-            if (read_x) w.x = load_part<FULL, BX, V>((const BX*)p.X + i, q.cols);
+            w.g = raw_part<FULL, BG, V>((const BG*)p.G + i, q.cols);
+            if (read_x) w.x = raw_part<FULL, BX, V>((const BX*)p.X + i, q.cols);
         };
         auto work = [&](int64_t row, const Row& w) {
             const int64_t i = row * p.N + q.col;
