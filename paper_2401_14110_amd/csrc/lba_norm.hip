@@ -1,14 +1,14 @@
 // lba_norm.hip -- layer norm over rows and its gradients (include/lba_layer.h).
 //
-// Forward: a row is read once into registers; mean = sum / N, then the sum of squared differences from that mean, both in
-// float32 over the same registers, so nothing cancels.  Backward: with n = (x - mean) * rstd and h = g * gamma the row sums of h and
-// h * n come from registers too, and the column sums of g * n and g, which dgamma and dbeta are, stay in the registers of the lanes
+// Forward: a row is read once into registers; mean = sum / N, then the sum of squared differences from that mean, both in float32 (in 64 bits
+// where codes come out) over the same registers, so nothing cancels.  Backward: with n = (x - mean) * rstd and h = g * gamma the row sums of
+// h and h * n come from registers too, and the column sums of g * n and g, which dgamma and dbeta are, stay in the registers of the lanes
 // that own the columns while a workgroup walks over its rows; one row of partial sums per workgroup goes to the workspace, and
 // a second launch adds them in a fixed order.
 // Both are bound by memory: every element is moved once.  A row belongs to a wave where four vectors of 16 bytes a lane hold it (two of
 // bfloat16), else to a workgroup of 256, 512 or 1024 lanes; rows beyond 16384 elements are read again from cache for each pass.
 // Measured (bytes that have to move over the time; a copy of 1 GiB reaches 5.2 TB/s): 16384 x 4096 bfloat16, forward, backward and column sums
-// together 137 us, 4.9 TB/s; 4096 x 768 float32 to codes 6.3 us, backward 9.8 + 3.7; 1024 x 16384 float32 forward 27, backward 38 + 11; one row
+// together 137 us, 4.9 TB/s; 4096 x 768 float32 to codes 9.2 us, backward 9.8 + 3.7; 1024 x 16384 float32 forward 27, backward 38 + 11; one row
 // of 768: 3 us, a launch.
 #include "lba_layer_device.h"
 #include "lba_internal.h"
@@ -16,25 +16,40 @@
 namespace lba {
 
 // sums of K values over the T lanes that share a row (T = 64: a wave; else the whole workgroup)
-template <int T, int K> __device__ __forceinline__ void row_sums(float (&v)[K], float* lds, int turn) {
+template <int T, int K, typename W> __device__ __forceinline__ void row_sums(W (&v)[K], W* lds, int turn) {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
     if (T == 64) return;
-    constexpr int W = T / 64;
-    float* at = lds + (turn & 1) * (K * W);              // two sets: a wave that is ahead writes the other one
+    constexpr int WAVES = T / 64;
+    W* at = lds + (turn & 1) * (K * WAVES);              // two sets: a wave that is ahead writes the other one
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) at[k * W + threadIdx.x / 64] = v[k];
+        for (int k = 0; k < K; ++k) at[k * WAVES + threadIdx.x / 64] = v[k];
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        float s = 0.0f;
+        W s = 0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) s += at[k * W + w];
+        for (int w = 0; w < WAVES; ++w) s += at[k * WAVES + w];
         v[k] = s;
     }
 }
+
+// What a row is worked on in.  Codes have four significant bits: a float32 result next to the middle of two codes falls on the wrong side once in
+// a million (3 of 3.1 M codes), so codes are made in 64 bits and none does.  It takes 9.2 us instead of 6.3 on 4096 x 768 float32, 68 us on 16384 x
+// 4096 bfloat16 where bfloat16 numbers take 44, and nothing on a single row; keeping the elements in 64 bits gained nothing.
+template <typename TY> struct Work { typedef float type; };
+template <> struct Work<uint8_t> { typedef double type; };
+// 64 bits -> 32, cut off, and the last bit set where something was: rounding that again to fewer bits is rounding once
+__device__ __forceinline__ float to_odd(double d) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, d);
+    const uint32_t lo = (uint32_t)b, rest = lo & 0x1FFFFFFFu;                        // float32 has 29 bits less
+    const float f = (float)__builtin_bit_cast(double, (b >> 32 << 32) | (lo & 0xE0000000u));
+    return __uint_as_float(__float_as_uint(f) | (rest < 1u ? rest : 1u));
+}
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(double v) { return to_odd(v); }
 
 struct NormParams {
     const void* X;
@@ -57,7 +72,8 @@ template <typename TX, typename TY, int T, int NV>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_fwd_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(TX), RPB = T < 256 ? 256 / T : 1;
     typedef typename Bits<TX>::type BX;
-    __shared__ float lds[2 * (T / 64)];
+    typedef typename Work<TY>::type W;
+    __shared__ W lds[2 * (T / 64)];
     const int t = threadIdx.x % T, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / T);
     struct Row { Raw<BX, V> x[NV]; };
     auto load = [&](int64_t row, Row& r) {
@@ -67,64 +83,77 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_fwd_kernel(NormParams 
     };
     const int64_t step = (int64_t)gridDim.x * RPB;
     int64_t row = (int64_t)blockIdx.x * RPB + sub;
-    Row a, b;
+    Row a;
     if (row < p.M) load(row, a);
-    float ga[NV][V], be[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    constexpr bool KEEP = T < 1024 || sizeof(W) == 4;    // else 128 registers hold neither gamma and beta nor a second row
+    float ga[KEEP ? NV : 1][V], be[KEEP ? NV : 1][V];
+    auto columns = [&](int i, float (&g)[V], float (&b)[V]) {
         const int c = (i * T + t) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            ga[i][j] = 1.0f;
-            be[i][j] = 0.0f;
+            g[j] = 1.0f;
+            b[j] = 0.0f;
         }
-        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, ga[i]);
-        if (p.beta) load_some<V>(p.beta + c, p.N - c, be[i]);
+        if (p.gamma) load_some<V>(p.gamma + c, p.N - c, g);
+        if (p.beta) load_some<V>(p.beta + c, p.N - c, b);
+    };
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) columns(i, ga[i], be[i]);
     }
     auto work = [&](int64_t at, const Row& r) {
-        float v[NV][V], s[1] = {0.0f};
+        W s[1] = {0};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[i][j] = raw_at(r.x[i], j);             // 0 beyond the row
-                s[0] += v[i][j];
-            }
+            for (int j = 0; j < V; ++j) s[0] += (W)raw_at(r.x[i], j);                // 0 beyond the row
         row_sums<T, 1>(s, lds, 0);
-        const float mean = s[0] / p.n;
-        s[0] = 0.0f;
+        const W mean = s[0] / (W)p.n;
+        s[0] = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * T + t) * V;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[i][j] -= mean;
-                if (c + j < p.N) s[0] = fmaf(v[i][j], v[i][j], s[0]);
+                const W d = (W)raw_at(r.x[i], j) - mean;
+                if (c + j < p.N) s[0] = fma(d, d, s[0]);
             }
         }
         row_sums<T, 1>(s, lds, 1);
-        const float rstd = 1.0f / sqrtf(s[0] / p.n + p.eps);
+        const W rstd = 1 / sqrt(s[0] / (W)p.n + (W)p.eps);
         if (t == 0) {
-            if (p.mean) p.mean[at] = mean;
-            if (p.rstd) p.rstd[at] = rstd;
+            if (p.mean) p.mean[at] = (float)mean;
+            if (p.rstd) p.rstd[at] = (float)rstd;
         }
         TY* y = (TY*)p.Y + at * p.N;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * T + t) * V;
             if (c >= p.N) break;
+            float v[V];
+            if (!KEEP) columns(i, ga[0], be[0]);
+            constexpr int EVERY = KEEP ? 1 : 0;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = fmaf(v[i][j] * rstd, ga[i][j], be[i][j]);
-            store_some<V>(y + c, p.N - c, v[i], p.fmt);
+            for (int j = 0; j < V; ++j) v[j] = to_float(fma(((W)raw_at(r.x[i], j) - mean) * rstd, (W)ga[i * EVERY][j], (W)be[i * EVERY][j]));
+            store_some<V>(y + c, p.N - c, v, p.fmt);
         }
     };
-    for (; row < p.M; row += 2 * step) {
-        const bool more = row + step < p.M;
-        if (more) load(row + step, b);
-        work(row, a);
-        if (!more) break;
-        if (row + 2 * step < p.M) load(row + 2 * step, a);
-        work(row + step, b);
+    if constexpr (!KEEP) {
+        while (row < p.M) {
+            work(row, a);
+            row += step;
+            if (row < p.M) load(row, a);
+        }
+    } else {
+        Row b;
+        for (; row < p.M; row += 2 * step) {
+            const bool more = row + step < p.M;
+            if (more) load(row + step, b);
+            work(row, a);
+            if (!more) break;
+            if (row + 2 * step < p.M) load(row + 2 * step, a);
+            work(row + step, b);
+        }
     }
 }
 

@@ -71,6 +71,20 @@ def test_codes_out(N, fmt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N", [(4096, 768), (700, 4100), (300, 16384)])
+@pytest.mark.parametrize("fmt", [(4, 3, 12), (3, 4, 6)])
+def test_codes_are_the_nearest(M, N, fmt):
+    """Rows that stay in registers: the code of every element is that of the exact value, also next to the middle of two codes."""
+    rng = np.random.default_rng(M)
+    x, g, b = values(rng, (M, N), "f32", 2.0, 0.5), values(rng, N, "f32", 0.3, 1.0), values(rng, N, "f32", 0.2)
+    y64, _, _, _ = lo.norm(x.astype(np.float64), g.astype(np.float64), b.astype(np.float64), 1e-5)
+    codes = lb.layernorm(dev(x), dev(g), dev(b), 1e-5, out_dtype=torch.uint8, out_fmt=fmt).cpu().numpy()
+    near64 = lo.nearest_code_value(y64, *fmt)
+    off = lo.code_values(*fmt)[codes] != near64
+    assert off.sum() == 0, (int(off.sum()), y64[off][:4], near64[off][:4])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [16385, 70001])
 def test_rows_beyond_the_registers(N, dtype):
