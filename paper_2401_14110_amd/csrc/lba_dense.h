@@ -17,7 +17,7 @@
 // Fragments: lane l holds row l % 16 and pieces l / 16 and l / 16 + 4 of the step, the same places of k for both operands, so it does
 // not matter in which order the matrix core walks over them.  B is the first factor, so lane l ends up with output row l % 16 and
 // four neighbouring columns 4 * (l / 16) ..; the epilogue takes the sums through LDS, eight columns a lane.
-// Measured: 8192 x 8192 x 4096 E4M3 with GELU to codes 400 us, 1.37 PFLOP/s (360 us, 1.53, without the activation; a library product of
+// Measured: 8192 x 8192 x 4096 E4M3 with GELU to codes 400 to 411 us, 1.35 PFLOP/s (360 us, 1.53, without the activation; a library product of
 // bfloat16 numbers reaches 1.34 to 1.37 at 8192^3); 4096 x 2304 x 768 to bfloat16 22 us, 0.65 (198 tiles on 256 CUs, six steps); 3136 x 512 x 4608 on
 // M4E3 34 us, 0.43; 4096 x (2 x 4096) x 1024 gated 71 us, 0.97.  The gradients' products of bfloat16 rows are bound by LDS as much as by the
 // matrix cores: 4096 x 8192 x 1024, both, 119 us and 11 to join the slices, 1.15; with float32 gradients, three pieces, 8192 x 2048 x 2048, both,
