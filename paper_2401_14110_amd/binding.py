@@ -628,7 +628,7 @@ def conv2d(X, W, qprod, qacc, stride=1, pad=0, order=ORDER_SEQ, planes=False, st
 # ---- the operators of include/lba_layer.h -----------------------------------------------------
 #
 # Codes in and out are uint8 tensors with a format (exp_bits, man_bits, bias), whose bias carries the tensor's power-of-two scale: the
-# E4M3 codes of x * 2^t are those of (4, 3, 7 + t).  Temporaries belong to the stream that the call runs on.
+# E4M3 codes of x * 2^t are those of (4, 3, 7 + t).  Outputs and temporaries come from the pool of the stream that the call runs on.
 
 _E4M3 = (4, 3, 7)
 _NO_FORMAT = lba_infmt(4, 3, 7)
@@ -658,8 +658,8 @@ def _infmt(f):
 
 
 def _on(stream, device):
-    """(handle, stream) of a call on tensors of the device: stream is None where it is the current one, else the object that
-    tensors made here are recorded on."""
+    """(handle, stream) of a call on tensors of the device: stream is None where it is the current one, else the object whose pool
+    tensors made here come from."""
     if device != torch._C._cuda_getDevice():
         raise ValueError("the tensors' device is not the current one")
     if stream is None:
@@ -680,23 +680,32 @@ def _whole(t, on):
         return t.contiguous()
 
 
+# Memory for a call on another stream than the current one comes from that stream's pool: a block of the current stream's pool may have been
+# freed a moment ago with kernels at work on it, for which the call's stream does not wait.
+def _of_pool(make, on):
+    with torch.cuda.stream(on):
+        return make()
+
+
 def _empty(shape, dtype, device, on):
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if on is not None:
-        t.record_stream(on)
+    """An output.  It is recorded on the current stream, where the caller uses it and may free it."""
+    if on is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    t = _of_pool(lambda: torch.empty(shape, dtype=dtype, device=device), on)
+    t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
 def _empty_as(t, dtype, on):
     """A tensor of the contiguous t's shape (0.5 us less than from the shape)."""
-    t = torch.empty_like(t, dtype=dtype)
-    if on is not None:
-        t.record_stream(on)
-    return t
+    return torch.empty_like(t, dtype=dtype) if on is None else _empty(t.shape, dtype, t.device, on)
 
 
 def _scratch(size, device, on):
-    return _empty((size,), torch.uint8, device, on) if size else None
+    if not size:
+        return None
+    make = lambda: torch.empty((size,), dtype=torch.uint8, device=device)  # noqa: E731
+    return make() if on is None else _of_pool(make, on)
 
 
 _REAL = (torch.float32, torch.bfloat16)
