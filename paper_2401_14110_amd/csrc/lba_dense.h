@@ -27,6 +27,7 @@
 #define LBA_DENSE_H_
 
 #include "lba_layer_device.h"
+#include "lba_dense_index.h"
 
 namespace lba {
 
@@ -245,12 +246,6 @@ template <int THREADS> __device__ __forceinline__ void side_sums(const SideSums&
 }
 
 __device__ __forceinline__ int up_to_8(int x) { return (x + 7) & ~7; }
-
-// An element's index in two parts: `u` is the same for a wave in the tile (a scalar register), `o` a lane's 32-bit offset from it.
-struct At { int64_t u; uint32_t o; };
-template <typename T> __device__ __forceinline__ T* at(const T* p, const At& i) {
-    return (T*)((char*)p + i.u * (int64_t)sizeof(T) + (uint32_t)(i.o * (uint32_t)sizeof(T)));
-}
 
 // a lane's V columns: how many of them there are and their bias
 template <bool GATED, int V> struct Columns { int n, cnt; float b[V], bu[V]; };
@@ -594,8 +589,9 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     // The sums go through LDS, at most 64 rows of a wave at a time, so that a lane has eight neighbouring columns and neighbouring lanes the next
     // ones: a wave works on its own part, without barriers.  Place of the four columns c of row r: (c / 4) ^ (r % CH), which spreads a
     // column over the banks.
-    constexpr int EH = FM == 8 ? 4 : FM == 6 ? 3 : FM, CH = FN * 4, LPR = GATED ? CH / 4 : CH / 2;   // rows of fragments, fours of a row, lanes of a row
-    constexpr int RPP = 64 / LPR, PASSES = EH * 16 / RPP;      // rows of a pass, passes
+    typedef PartShape<FN, GATED> Part;
+    constexpr int EH = FM == 8 ? 4 : FM == 6 ? 3 : FM, CH = Part::CH, LPR = Part::LPR;               // rows of fragments, fours of a row, lanes of a row
+    constexpr int RPP = Part::RPP, PASSES = EH * 16 / RPP;     // rows of a pass, passes
     static_assert(PASSES >= 1 && FM / EH <= 2 && FM % EH == 0 && sizeof(lds) >= (size_t)WM * WN * EH * 16 * CH * 16, "epilogue");
     float* mine = (float*)&lds[0][0] + wave * (EH * 16 * CH * 4);
     const EpiParams e = p.e;
@@ -663,14 +659,15 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
             }
         };
         const int64_t u0 = (int64_t)mh * e.N + nw, up = mh * e.ldp + nw;
-        const uint32_t o0 = (uint32_t)(row_in * e.N + oct * 8), op = (uint32_t)(row_in * (int)e.ldp + oct * 8);
-        const uint32_t so = (uint32_t)(RPP * e.N), sp = (uint32_t)(RPP * (int)e.ldp);
+        constexpr bool LONG = ELEM == ELEM_BF16 && !GATED && EPI == EPI_FORWARD;     // the gradients of the operands
+        auto out_at = [&](int g) { return lane_at<FN, GATED, LONG>(u0, e.N, l, g); };
+        auto grad_at = [&](int g) { return lane_at<FN, GATED, false>(up, e.ldp, l, g); };
         // Wholly inside: the next pass's residuals or gradients are under way, as they are, before this one's results are stored: a load
         // that follows stores waits for them too.
         auto passes = [&](auto act) {
             u32x4 raw[2][2];
             auto fetch = [&](int g, u32x4 (&w)[2]) {
-                const At i = {u0, o0 + g * so};
+                const At i = out_at(g);
                 if (extra && extra_type == LBA_F32) {
                     w[0] = *(const u32x4_any*)at((const float*)extra, i);
                     w[1] = *(const u32x4_any*)(at((const float*)extra, i) + 4);
@@ -689,7 +686,7 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(k % 2 ? w[0][k / 2] & 0xFFFF0000u : w[0][k / 2] << 16);
                 }
-                pass(Known<1>{}, act, g * RPP + row_in, At{u0, o0 + g * so}, At{up, op + g * sp}, x);
+                pass(Known<1>{}, act, g * RPP + row_in, out_at(g), grad_at(g), x);
             };
             fetch(0, raw[0]);
 #pragma unroll 1
@@ -713,7 +710,7 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
                     const int64_t i = (int64_t)(m < e.M ? m : e.M - 1) * e.N + (ncol + k < e.N ? ncol + k : e.N - 1);
                     x[k] = !extra ? 0.0f : extra_type == LBA_F32 ? ((const float*)extra)[i] : (float)((const bf16_t*)extra)[i];
                 }
-                pass(Known<0>{}, act, r, At{u0, o0 + g * so}, At{up, op + g * sp}, x);
+                pass(Known<0>{}, act, r, out_at(g), grad_at(g), x);
             }
         };
         const bool inside = mh + EH * 16 <= e.M && nw + LPR * 8 <= e.N;

@@ -272,6 +272,24 @@ def test_offsets_beyond_32_bits():
     assert abs(host(db)[-1] - g.sum()) <= (M + 64) * lo.U * np.abs(g).sum()
 
 
+@pytest.mark.gpu
+def test_gradients_of_long_rows():
+    # rows of which 64 take more than 2^32 bytes; small integers: every sum is exact
+    M, N, K = 64, 8, 17_100_003
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    pick = torch.tensor([0x00, 0x38, 0x40, 0xB8, 0xC0], dtype=torch.uint8, device=DEV)       # 0, 1, 2, -1, -2
+    value = torch.tensor([0.0, 1.0, 2.0, -1.0, -2.0], device=DEV)
+    a, b = (torch.randint(0, 5, (r, K), generator=gen, device=DEV, dtype=torch.uint8) for r in (M, N))
+    take = lambda table, i: torch.index_select(table, 0, i.reshape(-1).int()).view(i.shape)  # noqa: E731
+    A, B = take(pick, a), take(pick, b)
+    G = torch.randint(-8, 9, (M, N), generator=gen, device=DEV).float()
+    dA, dB, db = lb.dense_bwd(G, A, B, want_dbias=True)
+    for k in range(0, K, 1 << 21):
+        s = slice(k, min(k + (1 << 21), K))
+        assert torch.equal(dA[:, s], G @ take(value, b[:, s])) and torch.equal(dB[:, s], G.t().contiguous() @ take(value, a[:, s])), k
+    assert torch.equal(db, G.sum(0))
+
+
 def test_refusals():
     P, W, f, d = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x2000), (4, 3, 7), lb.lba_drop(0.0, 0, 0, None)
     base = dict(A=P, B=P, M=100, N=8, K=32, fa=f, fb=f, gated=0, bias=None, act=0, drop=d, R=None, rt=0, Y=P, yt=0, yf=f, ws=None, n=0)
