@@ -324,6 +324,7 @@ template <typename TG, typename TX>
 __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormParams p) {
     constexpr int V = 16 / sizeof(TX), T = 1024;
     __shared__ float lds[4 * (T / 64)];
+    int turn = 0;                                        // a row has one barrier: a wave that is ahead must not write the set that others read
     for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
     const TX* x = (const TX*)p.X + row * p.N;
     const TG* gr = (const TG*)p.G + row * p.N;
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormParams p) {
             if (c + j < p.N) s[1] = fmaf(h, (n[j] - mean) * rstd, s[1]);
         }
     }
-    row_sums<T, 2>(s, lds, 0);
+    row_sums<T, 2>(s, lds, turn++);
     const float mh = s[0] / p.n, mhn = s[1] / p.n;
     TX* dx = (TX*)p.Y + row * p.N;
     for (int c = threadIdx.x * V; c < p.N; c += T * V) {
@@ -442,6 +443,9 @@ static RowShape row_shape(int64_t N, int v) {
 
 // lanes of a forward launch: as many as the chip holds at a time, each of which walks over rows
 constexpr int64_t kNormLanes = 256 * 2048;
+// Workgroups for rows beyond the registers, which walk over the rows beyond: a launch holds fewer than 2^32 lanes.  (4096 of them, four rows each,
+// took 16384 rows of 20000 bfloat16 elements 1290 us forward instead of 1262.)
+static unsigned long_blocks(int64_t M) { return (unsigned)(M < 65536 ? M : 65536); }
 
 template <typename TX, typename TY> static void norm_fwd(const NormParams& p, hipStream_t st) {
     const RowShape r = row_shape(p.N, 16 / (int)sizeof(TX));
@@ -462,8 +466,7 @@ template <typename TX, typename TY> static void norm_fwd(const NormParams& p, hi
         LBA_NORM_FWD(1024, 4)
     }
 #undef LBA_NORM_FWD
-    const int64_t rows = 1 << 20;                        // a launch holds fewer than 2^32 lanes: the kernel walks over the rows beyond
-    hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), dim3((unsigned)(p.M < rows ? p.M : rows)), dim3(1024), 0, st, p);
+    hipLaunchKernelGGL((norm_fwd_long_kernel<TX, TY>), dim3(long_blocks(p.M)), dim3(1024), 0, st, p);
 }
 
 // Workgroups of the backward pass, each of which writes a row of partial sums: enough to fill the chip, few enough that these rows stay a
@@ -497,7 +500,7 @@ template <typename TG, typename TX> static void norm_bwd(NormParams p, hipStream
     constexpr int V = 16 / sizeof(TX);
     if (p.part)
         hipLaunchKernelGGL((norm_bwd_long_params_kernel<TG, TX>), dim3(blocks, (unsigned)((p.N + 256 * V - 1) / (256 * V))), dim3(256), 0, st, p);
-    if (p.Y) hipLaunchKernelGGL((norm_bwd_long_kernel<TG, TX>), dim3((unsigned)(p.M < (1 << 20) ? p.M : 1 << 20)), dim3(1024), 0, st, p);
+    if (p.Y) hipLaunchKernelGGL((norm_bwd_long_kernel<TG, TX>), dim3(long_blocks(p.M)), dim3(1024), 0, st, p);
 }
 
 int check_out_type(int32_t t, const lba_infmt& f) {

@@ -101,6 +101,24 @@ def test_rows_beyond_the_registers(N, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows_beyond_the_registers(dtype):
+    """More rows than the launch has workgroups: a row's result does not depend on the rows that its workgroup has before and after it."""
+    M, N, part = 150001, 16400, 60000                            # a call of `part` rows gives each of them a workgroup
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, G = (torch.randn(M, N, generator=gen, device=DEV).to(DT[dtype]) for _ in range(2))
+    x *= 1 + torch.arange(M, device=DEV).view(-1, 1) % 7         # another row's sums would show
+    gamma = torch.randn(N, generator=gen, device=DEV)
+    y, m, r = lb.layernorm(x, gamma, want_stats=True)
+    dx, _, _ = lb.layernorm_bwd(G, x, gamma, m, r, want_params=False)
+    for k in range(0, M, part):
+        s = slice(k, k + part)
+        one = lb.layernorm(x[s], gamma, want_stats=True)
+        assert torch.equal(one[0], y[s]) and torch.equal(one[1], m[s]) and torch.equal(one[2], r[s]), k
+        assert torch.equal(lb.layernorm_bwd(G[s], x[s], gamma, m[s], r[s], want_params=False)[0], dx[s]), k
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M", [1023, 4097, 20011])
 def test_many_rows(M):
     # more rows than workgroups write partial sums for
