@@ -83,7 +83,8 @@ size_t lba_dropout_bwd_workspace_bytes(int64_t M, int64_t N);
  * A [M, K] codes of fmt_a, B codes of fmt_b (the biases of the formats are the operands' scales: S is in real units), bias float32 or NULL,
  * residual [M, N] of r_type or NULL, Y [M, N] of y_type.  Products are exact and sums are float32.  The NaN codes of E4M3 are outside the
  * contract, as in lba.h: the outputs they reach are unspecified.  K == 0: S = 0.
- * Limits (else LBA_ERR_SHAPE): M <= 2^30, N <= 2^20, K <= 2^30; (else LBA_ERR_FORMAT): the formats' limits of lba.h.
+ * Limits (else LBA_ERR_SHAPE): M <= 2^30, N <= 2^20, K <= 2^30, and with more than 64 rows fewer than 2^23 tiles of 256 x 256:
+ * ceil(M / 256) * ceil(rows of B / 256) < 2^23; (else LBA_ERR_FORMAT): the formats' limits of lba.h.
  * workspace: lba_dense_workspace_bytes(...) bytes, NULL where that is 0; `aligned`: A and B are 16-byte aligned.  Operands of at most 4
  * exponent bits whose rows are multiples of 16 bytes are used where they are, and those of at most 64 rows of A in any case; others are copied
  * there, and codes of 5 exponent bits as bfloat16, which holds them: then (M + 64) (K + 64) and (rows of B + 64) (K + 64) must not exceed
@@ -99,7 +100,8 @@ size_t lba_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, lba_infmt fmt_
  * dA and dB are of g_type and gradients of the operands' real values; any of the three may be NULL but not all.  Float32: D is split
  * exactly into three bfloat16 pieces and the products are exact, sums float32 (a value of D under 2^-100 may lose pieces to the flush of
  * subnormal numbers, an infinite one gives NaN).  Bfloat16: D is rounded to bfloat16 before the two products, as dA and dB are after
- * them; dbias sums D before that.  Limits as in lba_dense, and (M + 64) (K + 64), (rows of B + 64) (K + 64) <= 2^32 for any operands.
+ * them; dbias sums D before that.  Limits: M, N, K and formats as in lba_dense, (M + 64) (K + 64), (rows of B + 64) (K + 64) <= 2^32 for
+ * any operands, and ceil(M / 128) * ceil(rows of B / 128) < 3 * 2^22.
  * workspace: lba_dense_bwd_workspace_bytes(...) bytes. */
 int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t K,
                   lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated, const float* bias, int32_t act, lba_drop drop,

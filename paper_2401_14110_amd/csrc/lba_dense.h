@@ -762,12 +762,13 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     }
 }
 
-// Tiles: rows of outputs, columns of B, waves over m.  The deep ones have four buffers instead of two, for bfloat16 rows: their steps are shorter
+// Tiles: rows of outputs, columns of B, waves over m, lanes of a workgroup.  The deep ones have four buffers instead of two, for bfloat16 rows: their steps are shorter
 // than the time a load takes where a CU has one workgroup (codes' are not: conversions fill them, and four buffers gained nothing).
 enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5, TILE_256_THREE = 6, TILE_128_THREE = 7, TILE_64_THREE = 8 };
-struct TileShape { int bm, bn, wm; };
+struct TileShape { int bm, bn, wm, threads; };
 inline TileShape tile_shape(int tile) {
-    static const TileShape all[] = {{256, 256, 2}, {128, 128, 2}, {64, 64, 2}, {192, 256, 2}, {128, 128, 2}, {64, 64, 2}, {256, 256, 2}, {128, 128, 2}, {64, 64, 2}};
+    static const TileShape all[] = {{256, 256, 2, 512}, {128, 128, 2, 256}, {64, 64, 2, 256}, {192, 256, 2, 512}, {128, 128, 2, 256}, {64, 64, 2, 256},
+                                    {256, 256, 2, 512}, {128, 128, 2, 256}, {64, 64, 2, 256}};
     return all[tile];
 }
 

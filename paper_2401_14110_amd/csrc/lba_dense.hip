@@ -65,6 +65,15 @@ static void cut(Product& p, int64_t slices) {
     p.slices = p.per_slice > 0 ? (int)((p.steps + p.per_slice - 1) / p.per_slice) : 1;
     if (p.slices < 1) p.slices = 1;
 }
+// A launch holds fewer than 2^32 lanes.  Beside backward sums and gradient products run workgroups of their own: of at most three transposed
+// copies, (R + 64) (K + 128) / 8192 <= 2^20 each, or 2^17 of column sums.
+enum { PLAN_FORWARD = 0, PLAN_BACKWARD = 1 };             // with the backward epilogue only small tiles, and no slices
+constexpr int64_t kBeside = (int64_t)1 << 22;
+static bool fits_a_launch(const Product* p, int n, int tile, int kind) {
+    int64_t tiles = n > 1 || kind == PLAN_BACKWARD ? kBeside : 0;
+    for (int i = 0; i < n; ++i) tiles += tiles_of(p[i], tile) * p[i].slices;
+    return tiles * tile_shape(tile).threads < (int64_t)1 << 32;
+}
 static size_t split_bytes(const Product& p) { return p.slices > 1 ? align256((size_t)(p.slices * p.rows * p.cols) * 4) : 0; }
 
 // What a launch takes, in microseconds: a tile's workgroup needs `fixed` and `step` for each step where every CU holds `per_cu` of them, and
@@ -119,8 +128,7 @@ static double cost_of(const Product* p, const int64_t* tiles, int n, const TileC
     return t + finish_of(wgs[x], d[x], wgs[1 - x], n > 1 ? d[1 - x] : 1.0, slots);
 }
 
-// Chooses the tile of a product, or of two that share a launch, and their slices: the least cost.
-enum { PLAN_FORWARD = 0, PLAN_BACKWARD = 1 };             // with the backward epilogue only small tiles, and no slices
+// Chooses the tile of a product, or of two that share a launch, and their slices: the least cost of those whose workgroups fit a launch.
 static int plan_tile(Product* p, int n, int elem, int kind, bool gated, int pieces = 1) {
     const TileCost* all = pieces == 3 ? kThree : elem == ELEM_BF16 ? kRows : kCodes;
     const size_t bytes = pieces == 3 ? sizeof(kThree) : elem == ELEM_BF16 ? sizeof(kRows) : sizeof(kCodes);
@@ -128,11 +136,13 @@ static int plan_tile(Product* p, int n, int elem, int kind, bool gated, int piec
     static const int kSlices[] = {1, 2, 3, 4, 5, 6, 8, 12, 16};
     int best = all[count - 1].tile;
     double least = 1e300;
-    Product cut_best[2];
+    Product cut_best[2] = {p[0], n > 1 ? p[1] : p[0]};   // (where no tile fits a launch, which the entry points refuse)
+    for (Product& q : cut_best) cut(q, 1);
     for (int t = 0; t < count; ++t) {
         const float step_scale = elem == ELEM_F16 ? all[t].f16 : 1.0f;
         if (kind == PLAN_BACKWARD && all[t].tile != TILE_128 && all[t].tile != TILE_64) continue;
         if (gated && (all[t].tile == TILE_128_DEEP || all[t].tile == TILE_64_DEEP)) continue;          // built for plain products
+        if (!fits_a_launch(p, n, all[t].tile, kind)) continue;
         const int64_t slots = (int64_t)kCus * all[t].per_cu;
         int64_t tiles[2] = {tiles_of(p[0], all[t].tile), n > 1 ? tiles_of(p[1], all[t].tile) : 0};
         // slices as long as they are four steps or more and the chip has room for them
@@ -255,12 +265,6 @@ static BwdPlan plan_backward(int64_t M, int64_t N, int64_t K, const lba_infmt& f
     return b;
 }
 
-static bool fits_a_launch(const Product* p, int n, int tile) {
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += tiles_of(p[i], tile) * p[i].slices;
-    return 2 * tiles < ((int64_t)1 << 22);               // fewer than 2^32 lanes; a gated product's half tiles may be one more column
-}
-
 static void add_job(LayJobs& jobs, uint32_t& blocks, const uint8_t* src, void* dst, int64_t R, int64_t K, int64_t ld, int kind, const lba_infmt& f) {
     if (R == 0 || K == 0) return;
     LayJob& j = jobs.job[jobs.n++];
@@ -329,7 +333,7 @@ int lba_dense(const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t 
     if (!Y || (K > 0 && (!A || !B))) return LBA_ERR_NULL;
     const bool two = gated != 0;
     const DensePlan d = plan_forward(M, N, K, fmt_a, fmt_b, two, aligned16(A, B));
-    if (!d.token && (!fits_a_launch(&d.fwd, 1, d.tile) || (!d.in_place && (!lay_fits(M, K) || !lay_fits(d.cols, K))))) return LBA_ERR_SHAPE;
+    if (!d.token && (!fits_a_launch(&d.fwd, 1, d.tile, PLAN_FORWARD) || (!d.in_place && (!lay_fits(M, K) || !lay_fits(d.cols, K))))) return LBA_ERR_SHAPE;
     rc = check_workspace(workspace, workspace_bytes, d.bytes);
     if (rc != LBA_OK) return rc;
     const ElemFmt ea = make_elem(fmt_a, d.elem), eb = make_elem(fmt_b, d.elem);
@@ -392,7 +396,7 @@ int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t
     }
     const BwdPlan b = plan_backward(M, N, K, fmt_a, fmt_b, two, act, g_type, aligned16(A, B));
     if (!G || (K > 0 && (((dA || b.sums) && !B) || ((dB || b.sums) && !A)))) return LBA_ERR_NULL;
-    if (!fits_a_launch(&b.f.fwd, 1, b.f.tile) || !fits_a_launch(b.out, 2, b.tile) || !lay_fits(M, K) || !lay_fits(cols, K)) return LBA_ERR_SHAPE;
+    if (!fits_a_launch(&b.f.fwd, 1, b.f.tile, PLAN_BACKWARD) || !fits_a_launch(b.out, 2, b.tile, PLAN_FORWARD) || !lay_fits(M, K) || !lay_fits(cols, K)) return LBA_ERR_SHAPE;
     rc = check_workspace(workspace, workspace_bytes, b.bytes);
     if (rc != LBA_OK) return rc;
     uint8_t* ws = (uint8_t*)workspace;

@@ -273,6 +273,26 @@ def test_offsets_beyond_32_bits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N", [(1 << 27, 32), (1 << 13, 1 << 20)])
+def test_many_tiles(M, N):
+    # millions of tiles of 64 x 64; small integers
+    K = 32
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    pick = torch.tensor([0x00, 0x38, 0x40, 0xB8, 0xC0], dtype=torch.uint8, device=DEV)       # 0, 1, 2, -1, -2
+    value = torch.tensor([0.0, 1.0, 2.0, -1.0, -2.0], device=DEV)
+    a, b = (torch.randint(0, 5, (r, K), generator=gen, device=DEV, dtype=torch.uint8) for r in (M, N))
+    take = lambda table, i: torch.index_select(table, 0, i.reshape(-1).int()).view(i.shape)  # noqa: E731
+    A, B = torch.empty_like(a), take(pick, b)
+    step = M // 16
+    for m in range(0, M, step):
+        A[m:m + step] = take(pick, a[m:m + step])
+    y = lb.dense(A, B, out_dtype=torch.bfloat16)
+    for m in range(0, M, step):
+        w = take(value, a[m:m + step]) @ take(value, b).t().contiguous()
+        assert torch.equal(y[m:m + step], w.bfloat16()), m
+
+
+@pytest.mark.gpu
 def test_gradients_of_long_rows():
     # rows of which 64 take more than 2^32 bytes; small integers: every sum is exact
     M, N, K = 64, 8, 17_100_003
