@@ -54,7 +54,8 @@ int lba_layernorm(const void* X, int32_t x_type, const float* gamma, const float
 /* Its gradients.  With n = (x - mean) * rstd, h = G * gamma, and means over a row,
  *   dX = rstd * (h - mean(h) - n * mean(h * n)),   dgamma = sum over rows of G * n,   dbeta = sum over rows of G.
  * G [M, N] of g_type, X as in the forward call, mean and rstd as it stored them; dX [M, N] of x_type, dgamma and dbeta [N] float32;
- * any of the three may be NULL but not all.  dX may be G or X where the types are equal.  M == 0 stores zeros to dgamma and dbeta.
+ * any of the three may be NULL but not all (unless M or N is 0).  dX may be G or X where the types are equal.  M == 0 stores zeros to
+ * dgamma and dbeta.
  * workspace: lba_layernorm_bwd_workspace_bytes(M, N) bytes (needed for dgamma or dbeta only). */
 int lba_layernorm_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type, const float* gamma,
                       const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,
@@ -69,8 +70,8 @@ int lba_dropout(const void* X, int32_t x_type, float scale, const float* bias, i
                 int64_t M, int64_t N, void* hip_stream);
 
 /* Its gradients:  dZ = G * keep / (1 - p) * act'(scale * X + bias),  dX = scale * dZ,  dbias = sum over rows of dZ (either may be
- * NULL but not both; the residual's gradient is G itself).  act' of LBA_ACT_RELU is 0 at 0.  X and bias are read only where act is
- * not LBA_ACT_NONE.  dX is of x_type and may be G or X where the types are equal.
+ * NULL but not both, unless M or N is 0; the residual's gradient is G itself).  M == 0 stores zeros to dbias.  act' of LBA_ACT_RELU is
+ * 0 at 0.  X and bias are read only where act is not LBA_ACT_NONE.  dX is of x_type and may be G or X where the types are equal.
  * workspace: lba_dropout_bwd_workspace_bytes(M, N) bytes (needed for dbias only). */
 int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type, float scale, const float* bias,
                     int32_t act, lba_drop drop, void* dX, float* dbias, int64_t M, int64_t N,
@@ -97,11 +98,12 @@ size_t lba_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, lba_infmt fmt_
 /* Its gradients.  Nothing of the forward call is kept: where act or gated needs S, it is computed again.  With G = dL/dY [M, N] of
  * g_type and D the gradient of the sums ([M, N], gated [M, 2 N]: the gate's columns first),
  *   dA = D . value(B) [M, K],   dB = D^T . value(A) [N or 2 N, K],   dbias = sum over rows of D (float32); the residual's gradient is G.
- * dA and dB are of g_type and gradients of the operands' real values; any of the three may be NULL but not all.  Float32: D is split
- * exactly into three bfloat16 pieces and the products are exact, sums float32 (a value of D under 2^-100 may lose pieces to the flush of
- * subnormal numbers, an infinite one gives NaN).  Bfloat16: D is rounded to bfloat16 before the two products, as dA and dB are after
- * them; dbias sums D before that.  Limits: M, N, K and formats as in lba_dense, (M + 64) (K + 64), (rows of B + 64) (K + 64) <= 2^32 for
- * any operands, and ceil(M / 128) * ceil(rows of B / 128) < 3 * 2^22.
+ * dA and dB are of g_type and gradients of the operands' real values; any of the three may be NULL but not all (unless M, N or K is 0).
+ * Sums over nothing store zeros.  Float32: D is split exactly into three bfloat16 pieces and the products are exact, sums float32 (a
+ * value of D under 2^-100 may lose pieces to the flush of subnormal numbers, an infinite one gives NaN).  Bfloat16: D is rounded to
+ * bfloat16 before the two products, as dA and dB are after them; dbias sums D before that.
+ * Limits: M, N, K and formats as in lba_dense, (M + 64) (K + 64), (rows of B + 64) (K + 64) <= 2^32 for any operands, and
+ * ceil(M / 128) * ceil(rows of B / 128) < 3 * 2^22.
  * workspace: lba_dense_bwd_workspace_bytes(...) bytes. */
 int lba_dense_bwd(const void* G, int32_t g_type, const uint8_t* A, const uint8_t* B, int64_t M, int64_t N, int64_t K,
                   lba_infmt fmt_a, lba_infmt fmt_b, int32_t gated, const float* bias, int32_t act, lba_drop drop,

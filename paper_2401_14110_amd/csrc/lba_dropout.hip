@@ -300,12 +300,13 @@ int lba_dropout_bwd(const void* G, int32_t g_type, const void* X, int32_t x_type
     if (rc == LBA_OK) rc = check_drop(drop, &p.drop);
     if (rc != LBA_OK) return rc;
     if (N == 0) return LBA_OK;
-    if (!dX && !dbias) return LBA_ERR_NULL;
     const hipStream_t st = (hipStream_t)hip_stream;
-    if (M == 0) {
-        if (dbias) launch_zero(dbias, N * 4, st);
+    if (M == 0) {                                        // dX holds nothing: its address may be null
+        if (!dbias) return LBA_OK;
+        launch_zero(dbias, N * 4, st);
         return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
     }
+    if (!dX && !dbias) return LBA_ERR_NULL;
     if (!G || (act != LBA_ACT_NONE && !X)) return LBA_ERR_NULL;
     if (dbias) {
         if (!workspace) return LBA_ERR_NULL;

@@ -568,13 +568,14 @@ int lba_layernorm_bwd(const void* G, int32_t g_type, const void* X, int32_t x_ty
     if (rc == LBA_OK) rc = check_float_type(x_type);
     if (rc != LBA_OK) return rc;
     if (N == 0) return LBA_OK;
-    if (!dX && !dgamma && !dbeta) return LBA_ERR_NULL;
     const hipStream_t st = (hipStream_t)hip_stream;
-    if (M == 0) {
+    if (M == 0) {                                        // dX holds nothing: its address may be null
+        if (!dgamma && !dbeta) return LBA_OK;
         if (dgamma) launch_zero(dgamma, N * 4, st);
         if (dbeta) launch_zero(dbeta, N * 4, st);
         return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
     }
+    if (!dX && !dgamma && !dbeta) return LBA_ERR_NULL;
     if (!G || !X || !mean || !rstd) return LBA_ERR_NULL;
     const bool params = dgamma || dbeta;
     if (params) {
