@@ -46,7 +46,7 @@ typedef struct {
  * (x - mean)^2, all in float32; with codes for Y and N <= 16384 in 64 bits, so that the codes are the nearest to the exact result.
  * X [M, N] of x_type (LBA_F32 or LBA_BF16), gamma and beta [N] float32 (NULL: ones, zeros), Y [M, N] of y_type (y_fmt is read for
  * LBA_CODE8 only), mean and rstd [M] float32 (either may be NULL: not stored).  Y may be X where the types are equal.
- * M <= 2^31 - 1, N <= 2^21 (else LBA_ERR_SHAPE). */
+ * M <= 2^31 - 1, N <= 2^21 (else LBA_ERR_SHAPE).  N == 0: mean and rstd are NaN. */
 int lba_layernorm(const void* X, int32_t x_type, const float* gamma, const float* beta, float eps,
                   void* Y, int32_t y_type, lba_infmt y_fmt, float* mean, float* rstd,
                   int64_t M, int64_t N, void* hip_stream);

@@ -536,8 +536,8 @@ int lba_layernorm(const void* X, int32_t x_type, const float* gamma, const float
     if (rc == LBA_OK) rc = check_float_type(x_type);
     if (rc == LBA_OK) rc = check_out_type(y_type, y_fmt);
     if (rc != LBA_OK) return rc;
-    if (M == 0 || N == 0) return LBA_OK;
-    if (!X || !Y) return LBA_ERR_NULL;
+    if (M == 0 || (N == 0 && !mean && !rstd)) return LBA_OK;
+    if (N > 0 && (!X || !Y)) return LBA_ERR_NULL;        // rows of no elements: the kernel reads none, and their mean is 0 / 0
     NormParams p = {};
     p.X = X; p.gamma = gamma; p.beta = beta; p.Y = Y; p.mean = mean; p.rstd = rstd;
     p.M = M; p.N = (int32_t)N; p.eps = eps; p.n = (float)N;

@@ -57,3 +57,18 @@ def test_calls_on_empty_batches():
     # no columns of outputs
     dA, dB, _ = lb.dense_bwd(torch.empty(70, 0, device="cuda"), torch.zeros(70, 100, dtype=torch.uint8, device="cuda"), B[:0])
     assert dA.shape == (70, 100) and not dA.any() and dB.shape == (0, 100)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_statistics_of_rows_of_nothing(dtype):
+    x, v = torch.empty(300, 0, device="cuda", dtype=dtype), torch.empty(0, device="cuda")
+    junk = [torch.zeros(300, device="cuda") for _ in range(4)]       # memory that the statistics are likely to be given
+    del junk
+    for kw in (dict(), dict(gamma=v, beta=v), dict(out_dtype=torch.uint8, out_fmt=F)):
+        y, mean, rstd = lb.layernorm(x, want_stats=True, **kw)
+        assert y.shape == (300, 0) and mean.shape == rstd.shape == (300,)
+        assert mean.isnan().all() and rstd.isnan().all()             # 0 / 0
+    assert lb.layernorm(x).shape == (300, 0)
+    dx, dg, db = lb.layernorm_bwd(x, x, None, mean, rstd)
+    assert dx.shape == (300, 0) and dg.shape == db.shape == (0,)
