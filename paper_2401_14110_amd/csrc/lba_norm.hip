@@ -41,12 +41,13 @@ template <int T, int K, typename W> __device__ __forceinline__ void row_sums(W (
 // 4096 bfloat16 where bfloat16 numbers take 44, and nothing on a single row; keeping the elements in 64 bits gained nothing.
 template <typename TY> struct Work { typedef float type; };
 template <> struct Work<uint8_t> { typedef double type; };
-// 64 bits -> 32, cut off, and the last bit set where something was: rounding that again to fewer bits is rounding once
+// 64 bits -> 32, cut off, and the last bit set where something was: rounding that again to fewer bits is rounding once.  The bit is set before
+// the conversion, which then is exact or, beyond float32, an infinity.
 __device__ __forceinline__ float to_odd(double d) {
     const uint64_t b = __builtin_bit_cast(uint64_t, d);
     const uint32_t lo = (uint32_t)b, rest = lo & 0x1FFFFFFFu;                        // float32 has 29 bits less
-    const float f = (float)__builtin_bit_cast(double, (b >> 32 << 32) | (lo & 0xE0000000u));
-    return __uint_as_float(__float_as_uint(f) | (rest < 1u ? rest : 1u));
+    const uint32_t kept = (lo | (rest < 1u ? rest : 1u) << 29) & 0xE0000000u;
+    return (float)__builtin_bit_cast(double, (b >> 32 << 32) | kept);
 }
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(double v) { return to_odd(v); }

@@ -85,6 +85,23 @@ def test_codes_are_the_nearest(M, N, fmt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N", [64, 770, 16384, 20000])
+def test_results_beyond_float32_saturate(N):
+    rng = np.random.default_rng(N)
+    x, g = values(rng, (40, N), "f32"), np.where(np.arange(N) % 2, 3e38, -1e38).astype(np.float32)
+    y64, _, _, _ = lo.norm(x.astype(np.float64), g.astype(np.float64), None, 1e-5)
+    assert (np.abs(y64) > 3.5e38).any() and (np.abs(y64) > 1e30).all()
+    for fmt in ((4, 3, 7), (3, 4, 3), (5, 2, 15)):
+        codes = lb.layernorm(dev(x), dev(g), out_dtype=torch.uint8, out_fmt=fmt).cpu().numpy()
+        assert np.array_equal(codes, np.where(y64 < 0, 0x80, 0) + (0x7E if fmt[0] == 4 else 0x7F))
+    # infinities of the parameters saturate, and NaN stays NaN
+    beta = np.zeros(N, np.float32)
+    beta[1], beta[2], beta[3] = np.inf, -np.inf, np.nan
+    codes = lb.layernorm(dev(x), None, dev(beta), out_dtype=torch.uint8, out_fmt=(4, 3, 7)).cpu().numpy()
+    assert (codes[:, 1] == 0x7E).all() and (codes[:, 2] == 0xFE).all() and (codes[:, 3] & 0x7F == 0x7F).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [16385, 70001])
 def test_rows_beyond_the_registers(N, dtype):
