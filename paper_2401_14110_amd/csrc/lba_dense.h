@@ -32,11 +32,9 @@
 namespace lba {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
@@ -840,11 +838,10 @@ template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, c
         return LBA_OK; \
     }
 #define LBA_DENSE_SMALL(GATED, EPI) LBA_DENSE(TILE_128, 2, 2, 4, 4, 2, 1, GATED, EPI) LBA_DENSE(TILE_64, 2, 2, 2, 2, 2, 1, GATED, EPI)
-#define LBA_DENSE_LARGE(GATED) LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, 1, GATED, EPI_FORWARD) LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, 1, GATED, EPI_FORWARD)
     LBA_DENSE_SMALL(false, EPI_FORWARD)
     LBA_DENSE_SMALL(true, EPI_FORWARD)
-    LBA_DENSE_LARGE(false)
-    LBA_DENSE_LARGE(true)
+    LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, 1, false, EPI_FORWARD)
+    LBA_DENSE(TILE_256, 2, 4, 8, 4, 2, 1, true, EPI_FORWARD)
     LBA_DENSE_SMALL(false, EPI_BACKWARD)
     LBA_DENSE_SMALL(true, EPI_BACKWARD)
     if constexpr (ELEM == ELEM_BF16) {
@@ -853,8 +850,10 @@ template <int ELEM> int launch_dense(const GemmParams& a, const GemmParams* b, c
         LBA_DENSE(TILE_256_THREE, 2, 4, 8, 4, 2, 3, false, EPI_FORWARD)
         LBA_DENSE(TILE_128_THREE, 2, 2, 4, 4, 2, 3, false, EPI_FORWARD)
         LBA_DENSE(TILE_64_THREE, 2, 2, 2, 2, 2, 3, false, EPI_FORWARD)
+    } else {                                             // of codes: bfloat16 rows have no costs for it
+        LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, 1, false, EPI_FORWARD)
+        LBA_DENSE(TILE_192, 2, 4, 6, 4, 2, 1, true, EPI_FORWARD)
     }
-#undef LBA_DENSE_LARGE
 #undef LBA_DENSE_SMALL
 #undef LBA_DENSE
     return LBA_ERR_UNSUPPORTED;                          // a tile that the plan must not choose here
