@@ -17,7 +17,7 @@
 // Fragments: lane l holds row l % 16 and pieces l / 16 and l / 16 + 4 of the step, the same places of k for both operands, so it does
 // not matter in which order the matrix core walks over them.  B is the first factor, so lane l ends up with output row l % 16 and
 // four neighbouring columns 4 * (l / 16) ..; the epilogue takes the sums through LDS, eight columns a lane.
-// Measured: 8192 x 8192 x 4096 E4M3 with GELU to codes 400 to 411 us, 1.35 PFLOP/s (360 us, 1.53, without the activation; a library product of
+// Measured: 8192 x 8192 x 4096 E4M3 with GELU to codes 397 to 417 us, 1.35 PFLOP/s (360 to 367 us, 1.5, without the activation; a library product of
 // bfloat16 numbers reaches 1.34 to 1.37 at 8192^3); 4096 x 2304 x 768 to bfloat16 22 us, 0.65 (198 tiles on 256 CUs, six steps); 3136 x 512 x 4608 on
 // M4E3 34 us, 0.43; 4096 x (2 x 4096) x 1024 gated 71 us, 0.97.  The gradients' products of bfloat16 rows are bound by LDS as much as by the
 // matrix cores: 4096 x 8192 x 1024, both, 119 us and 11 to join the slices, 1.15; with float32 gradients, three pieces, 8192 x 2048 x 2048, both,
@@ -336,7 +336,10 @@ __device__ __forceinline__ void eight_pieces(const float (&d)[8], u16x8 (&w)[3])
         w[2][j] = (uint16_t)(__float_as_uint(r2) >> 16);
     }
 }
-// stores eight neighbouring values of the gradient matrix (16-byte aligned), or of its transpose
+// Stores eight neighbouring values of the gradient matrix (16-byte aligned), or of its transpose.  Where the caller's gradients are bfloat16 the
+// matrix is rounded to bfloat16 as well, each element for itself, so that its products are one pass of the matrix cores each: dA and dB of
+// 4096 x (2 x 4096) x 1024 gated come out 2.35e-3 of their norm off, and 1.66e-3 is what their own rounding to bfloat16 leaves.  A second piece
+// would take that away and twice the time of the two products, 117 us of that pass's 233.  Float32 gradients lose nothing.
 __device__ __forceinline__ void store_eight(bf16_t* to, const At& i, int pieces, int64_t piece, const float (&d)[8]) {
     if (pieces == 1) {
         *(u16x8*)at(to, i) = eight_rounded(d);
@@ -760,8 +763,8 @@ __global__ __launch_bounds__(WM * WN * 64, (FM == 2 ? 4 : 2) / (NST > 2 ? 2 : 1)
     }
 }
 
-// Tiles: rows of outputs, columns of B, waves over m, lanes of a workgroup.  The deep ones have four buffers instead of two, for bfloat16 rows: their steps are shorter
-// than the time a load takes where a CU has one workgroup (codes' are not: conversions fill them, and four buffers gained nothing).
+// Tiles: rows of outputs, columns of B, waves over m, lanes of a workgroup.  The deep ones have four buffers instead of two, for bfloat16 rows:
+// their steps are shorter than the time a load takes where a CU has one workgroup (codes' are not: conversions fill them, and four buffers gained nothing).
 enum { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_192 = 3, TILE_128_DEEP = 4, TILE_64_DEEP = 5, TILE_256_THREE = 6, TILE_128_THREE = 7, TILE_64_THREE = 8 };
 struct TileShape { int bm, bn, wm, threads; };
 inline TileShape tile_shape(int tile) {
@@ -784,7 +787,17 @@ inline int elem_of(const lba_infmt& a, const lba_infmt& b) {
     return a.exp_bits <= 4 && b.exp_bits <= 4 ? ELEM_F16 : ELEM_BF16;
 }
 
-// few rows (at most kTokenRows): a pass over B (lba_dense_token.hip)
+// Few rows (at most kTokenRows): a pass over B (lba_dense_token.hip).  It and the tile, in us, operands in the last-level cache:
+//                                   1 row          32             48             64
+//   2304 x 768   E4M3               3.0 /  6.1     3.7 /  6.0     4.1 /  6.2     4.5 /  6.1
+//   4096 x 4096  E4M3               5.2 / 10.1     8.3 / 11.8    10.3 / 11.3    12.2 / 12.0
+//   4096 x 4096  M4E3               5.7 / 11.3     8.4 / 12.9    10.5 / 14.2    12.4 / 16.0
+//   4096 x 4096  E5M2              12.3 / 27.6    17.7 / 25.7    22.2 / 26.1    27.2 / 26.6
+//   2 x 4096 x 2048 E4M3, gated     4.9 / 10.8     6.5 / 10.4     7.6 / 10.5     8.8 / 10.4
+//   8192 x 4096  E4M3               7.5 / 12.7    13.8 / 13.6    17.4 / 14.4    21.9 / 15.1
+//   512 x 4608   E4M3               4.8 /  8.9     8.4 /  9.6    10.4 /  9.7    12.4 /  9.8
+//   771 x 770    E4M3 (copied)      4.9 /  9.6     8.0 / 10.1     9.9 / 10.1    10.9 / 10.2
+// 64 is where the two meet on most of them; from 32 rows on the tile is ahead on long rows of few or of very many columns.
 constexpr int kTokenRows = 64;
 struct TokenParams {
     const uint8_t* A;

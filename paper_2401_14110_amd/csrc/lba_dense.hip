@@ -78,7 +78,10 @@ static size_t split_bytes(const Product& p) { return p.slices > 1 ? align256((si
 
 // What a launch takes, in microseconds: a tile's workgroup needs `fixed` and `step` for each step where every CU holds `per_cu` of them, and
 // `fixed1` and `step1` where it has the CU to itself.  Measured on grids of 1 to 8 rounds and 1 to 64 steps (4096 x 4096 and 1024 x 1024 outputs,
-// K = 128 to 4096); a step of codes is 128 long, of bfloat16 rows 64.
+// K = 128 to 4096); a step of codes is 128 long, of bfloat16 rows 64.  The sums were stored as they are: what an epilogue adds is not in it, 4 us
+// (tiles of 64) to 14 (256) for GELU, dropout and a float32 residual on 3985 x 770 x 768, whose sums take 13.2 us (11.5 here).  It did not change
+// which tile is the fastest: 64 there, 128 on 8192 x 1024 x 1024 (22.5 and 29.4 us; 64: 25.9, 31.0), 256 on 4096 x 4096 x 1024 (38.4 and 47.9;
+// 128: 40.2, 53.9), and backward 64, 128 and 128, as the costs have it.
 // `f16`: what a step of codes that become FP16 numbers takes, whose conversions are five instructions for E4M3's two, and the more of them the
 // smaller a wave's part of the tile is.
 struct TileCost { int tile, per_cu; float fixed, step, fixed1, step1, f16; };

@@ -6,7 +6,8 @@
 // that own the columns while a workgroup walks over its rows; one row of partial sums per workgroup goes to the workspace, and
 // a second launch adds them in a fixed order.
 // Both are bound by memory: every element is moved once.  A row belongs to a wave where four vectors of 16 bytes a lane hold it (two of
-// bfloat16), else to a workgroup of 256, 512 or 1024 lanes; rows beyond 16384 elements are read again from cache for each pass.
+// bfloat16), else to a workgroup of 256, 512 or 1024 lanes; rows beyond 16384 elements are read again from cache for each pass, which is a plain
+// loop: 1024 x 65536 bfloat16 take 269 us forward and 271 + 131 backward, where their bytes would take 52 and 77.
 // Measured (bytes that have to move over the time; a copy of 1 GiB reaches 5.2 TB/s): 16384 x 4096 bfloat16, forward, backward and column sums
 // together 137 us, 4.9 TB/s; 4096 x 768 float32 to codes 9.2 us, backward 9.8 + 3.7; 1024 x 16384 float32 forward 27, backward 38 + 11; one row
 // of 768: 3 us, a launch.
