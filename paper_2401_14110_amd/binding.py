@@ -7,6 +7,7 @@ import ctypes
 import functools
 import math
 import os
+import typing
 
 import torch
 
@@ -36,6 +37,21 @@ def infmt(f):
 
 class lba_drop(ctypes.Structure):
     _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("stream", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class lba_strides(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class lba_attn(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("T", "Tk", "count")] + [(n, ctypes.c_void_p) for n in ("starts", "starts_k")]
+                + [(n, ctypes.c_int32) for n in ("H", "KV", "D", "type", "causal", "clear")] + [("scale", ctypes.c_float)]
+                + [(n, lba_strides) for n in ("q", "k", "v")])
+
+
+class lba_cache4(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "k_scale", "v", "v_scale")] + [(n, ctypes.c_int64) for n in ("pages", "table_row", "count")]
+                + [(n, ctypes.c_void_p) for n in ("table", "lens")] + [(n, ctypes.c_int32) for n in ("page", "KV", "D")])
 
 
 class lba_conv2d_desc(ctypes.Structure):
@@ -147,6 +163,25 @@ def lib(path=None):
         L.lba_dense_bwd.argtypes = [vp, i32, vp, vp, i64, i64, i64, lba_infmt, lba_infmt, i32, vp, i32, lba_drop, vp, vp, vp, vp, size, vp]
         L.lba_dense_bwd_workspace_bytes.restype = size
         L.lba_dense_bwd_workspace_bytes.argtypes = [i64, i64, i64, lba_infmt, lba_infmt, i32, i32, i32, i32]
+        st = lba_strides
+        for name in ("lba_rope", "lba_rope_bwd"):
+            f = getattr(L, name)
+            f.restype = ctypes.c_int
+            f.argtypes = [vp, st, i32, vp, i32, vp, i64, i32, f32, vp, st, i64, i64, i64, vp]
+        L.lba_attention.restype = ctypes.c_int
+        L.lba_attention.argtypes = [lba_attn, vp, vp, vp, vp, i32, lba_infmt, vp, vp]
+        L.lba_attention_bwd.restype = ctypes.c_int
+        L.lba_attention_bwd.argtypes = [lba_attn, vp, vp, vp, vp, vp, vp, vp, st, vp, st, vp, st, vp, size, vp]
+        L.lba_attention_bwd_workspace_bytes.restype = size
+        L.lba_attention_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.lba_cache_write.restype = ctypes.c_int
+        L.lba_cache_write.argtypes = [lba_cache4, vp, i64, vp, st, vp, st, i32, vp]
+        L.lba_cache_read.restype = ctypes.c_int
+        L.lba_cache_read.argtypes = [lba_cache4, vp, i64, vp, st, vp, st, i32, i32, vp]
+        L.lba_cache_attention.restype = ctypes.c_int
+        L.lba_cache_attention.argtypes = [lba_cache4, vp, st, i32, i64, i64, f32, vp, i32, lba_infmt, vp, size, vp]
+        L.lba_cache_attention_workspace_bytes.restype = size
+        L.lba_cache_attention_workspace_bytes.argtypes = [i64, i64, i32, i64, i64, i32, i32]
         _lib = L
     return _lib
 
@@ -370,6 +405,42 @@ def lba_dense_bwd(G, g_type, A, B, M, N, K, fmt_a, fmt_b, gated, bias, act, drop
 
 def lba_dense_bwd_workspace_bytes(M, N, K, fmt_a, fmt_b, gated, act, g_type, aligned=1):
     return int(lib().lba_dense_bwd_workspace_bytes(M, N, K, infmt(fmt_a), infmt(fmt_b), gated, act, g_type, aligned))
+
+
+def lba_rope(X, x_at, type, positions, pos_bits, freq, pairs, interleaved, gain, Y, y_at, T, H, D, hip_stream=None):
+    return lib().lba_rope(X, x_at, type, positions, pos_bits, freq, pairs, interleaved, gain, Y, y_at, T, H, D, hip_stream)
+
+
+def lba_rope_bwd(G, g_at, type, positions, pos_bits, freq, pairs, interleaved, gain, dX, dx_at, T, H, D, hip_stream=None):
+    return lib().lba_rope_bwd(G, g_at, type, positions, pos_bits, freq, pairs, interleaved, gain, dX, dx_at, T, H, D, hip_stream)
+
+
+def lba_attention(a, Q, K, V, O, o_type, o_fmt, lse, hip_stream=None):
+    return lib().lba_attention(a, Q, K, V, O, o_type, infmt(o_fmt), lse, hip_stream)
+
+
+def lba_attention_bwd(a, G, Q, K, V, O, lse, dQ, dq_at, dK, dk_at, dV, dv_at, workspace, workspace_bytes, hip_stream=None):
+    return lib().lba_attention_bwd(a, G, Q, K, V, O, lse, dQ, dq_at, dK, dk_at, dV, dv_at, workspace, workspace_bytes, hip_stream)
+
+
+def lba_attention_bwd_workspace_bytes(T, H):
+    return int(lib().lba_attention_bwd_workspace_bytes(T, H))
+
+
+def lba_cache_write(c, starts, T, K, k_at, V, v_at, type, hip_stream=None):
+    return lib().lba_cache_write(c, starts, T, K, k_at, V, v_at, type, hip_stream)
+
+
+def lba_cache_read(c, starts, T, K, k_at, V, v_at, type, clear, hip_stream=None):
+    return lib().lba_cache_read(c, starts, T, K, k_at, V, v_at, type, clear, hip_stream)
+
+
+def lba_cache_attention(c, Q, q_at, type, fresh, H, scale, O, o_type, o_fmt, workspace, workspace_bytes, hip_stream=None):
+    return lib().lba_cache_attention(c, Q, q_at, type, fresh, H, scale, O, o_type, infmt(o_fmt), workspace, workspace_bytes, hip_stream)
+
+
+def lba_cache_attention_workspace_bytes(count, table_row, page, fresh, H, KV, D):
+    return int(lib().lba_cache_attention_workspace_bytes(count, table_row, page, fresh, H, KV, D))
 
 
 # ---- tensor conveniences --------------------------------------------------------------------
@@ -903,3 +974,272 @@ def dense_bwd(G, A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, drop=N
     _check(lib().lba_dense_bwd(_at(G), t, a, b, M, N, K, fa, fb, gated, _at(bias), act, d, _at(dA), _at(dB), _at(dbias), _at(ws), size,
                                handle))
     return dA, dB, dbias
+
+
+# ---- the operators of include/lba_attention.h -------------------------------------------------
+#
+# Tensors of heads are [rows, heads, D], or [batch, length, heads, D], float32 or bfloat16, and may be views whose rows and heads are any distance
+# apart (the queries inside the output of one product): what is read or written is where it is, and copied only where D is not the last
+# axis in memory.  `starts`: an int32 device tensor [sequences + 1] of packed sequences' first rows and the end of the last, read when the
+# kernels run; without it [rows, heads, D] is one sequence and [batch, length, heads, D] are `batch` of them.
+
+def _heads(t, what, on, device=None, dtype=None):
+    """(t as [rows, heads, D] with D along memory, its strides) of an input."""
+    if t.dtype not in _REAL or t.get_device() < 0 or (dtype is not None and (t.dtype != dtype or t.get_device() != device)):
+        raise TypeError("%s must be a tensor of %s on %s device" % (what, dtype or "torch.float32 or torch.bfloat16", "a" if dtype is None else "the call's"))
+    if t.dim() < 3:
+        raise ValueError("%s must be [rows, heads, D] or have more leading axes" % what)
+    if t.dim() > 3 or (t.stride(-1) != 1 and t.size(-1) != 1):
+        shape = (math.prod(t.shape[:-2]),) + tuple(t.shape[-2:])
+        try:
+            v = t.view(shape)
+        except RuntimeError:
+            v = None
+        if v is None or (v.stride(2) != 1 and shape[2] != 1):
+            v = _whole(t, on).view(shape) if not t.is_contiguous() else t.view(shape)
+        t = v
+    return t, lba_strides(t.stride(0), t.stride(1))
+
+
+def _heads_out(t, like, what):
+    """The same of an output given by the caller: a view that can be written where it is, no element of which shares another's place."""
+    if t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape != like.shape:
+        raise ValueError("%s must be a tensor %s of %s on the call's device" % (what, tuple(like.shape), like.dtype))
+    try:
+        v = t.view((math.prod(t.shape[:-2]),) + tuple(t.shape[-2:]))
+    except RuntimeError:
+        raise ValueError("%s must be a view whose leading axes are one in memory" % what) from None
+    (T, H, D), (r, h, d) = v.shape, v.stride()
+    inner, outer = ((H, h), (T, r)) if h <= r or T <= 1 else ((T, r), (H, h))
+    end = D
+    for n, step in (inner, outer):
+        if n > 1:
+            if step < end:
+                raise ValueError("%s has elements that share a place" % what)
+            end = (n - 1) * step + end
+    if d != 1 and D > 1:
+        raise ValueError("%s must have its last axis along memory" % what)
+    return v, lba_strides(r, h)
+
+
+def _starts(t, device, what, on):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.get_device() != device or t.dim() != 1 or t.numel() < 1:
+        raise ValueError("%s must be an int32 tensor [sequences + 1] on the call's device" % what)
+    return _whole(t, on)
+
+
+def _rope(fn, x, positions, freq, interleaved, gain, out, stream):
+    device = x.get_device()
+    if device < 0:
+        raise TypeError("x must be a device tensor")
+    handle, on = _on(stream, device)
+    v, at = _heads(x, "x", on)
+    T, H, D = v.shape
+    if positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != device or positions.shape != x.shape[:-2]:
+        raise ValueError("positions must be an int32 or int64 tensor %s on the call's device" % (tuple(x.shape[:-2]),))
+    if freq.dtype != torch.float64 or freq.get_device() != device or freq.dim() != 1 or 2 * freq.numel() > D:
+        raise ValueError("freq must be a float64 tensor of at most %d elements on the call's device" % (D // 2))
+    positions, freq = _whole(positions, on), _whole(freq, on)
+    y = _empty(x.shape, x.dtype, x.device, on) if out is None else out
+    w, y_at = _heads_out(y, x, "out")
+    _check(fn(_at(v), at, _TYPE[x.dtype], _at(positions), 8 * positions.element_size(), _at(freq), freq.numel(), interleaved, gain, _at(w), y_at, T, H, D,
+              handle))
+    return y
+
+
+def rope(x, positions, freq, interleaved=False, gain=1.0, out=None, stream=None):
+    """Rotary positions on x [..., heads, D]: the pairs (i, i + R / 2), interleaved (2 i, 2 i + 1), of the first R = 2 * len(freq) elements of a head
+    are turned by positions * freq and scaled by gain; the rest is copied.  positions: int32 or int64 of x's leading shape; freq: float64,
+    radians a position.  out may be x."""
+    return _rope(lib().lba_rope, x, positions, freq, interleaved, gain, out, stream)
+
+
+def rope_bwd(G, positions, freq, interleaved=False, gain=1.0, out=None, stream=None):
+    """The gradient of rope: G turned back.  out may be G."""
+    return _rope(lib().lba_rope_bwd, G, positions, freq, interleaved, gain, out, stream)
+
+
+def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
+    """(lba_attn, what it points to) of a call."""
+    if q.dim() not in (3, 4) or k.dim() != q.dim() or k.shape != v.shape or k.shape[-1] != q.shape[-1]:
+        raise ValueError("q must be [rows, heads, D] or [batch, length, heads, D], k and v alike")
+    H, KV, D = q.shape[-2], k.shape[-2], q.shape[-1]
+    if H and (not KV or H % KV):
+        raise ValueError("%d query heads do not share %d heads of keys" % (H, KV))
+    if not 1 <= D <= 128:
+        raise ValueError("heads have 1 to 128 elements")
+    if starts is None:
+        if starts_k is not None:
+            raise ValueError("starts_k needs starts")
+        count = q.shape[0] if q.dim() == 4 else 1
+        if q.dim() == 4 and k.shape[0] != count:
+            raise ValueError("q and k have different batches")
+    else:
+        if q.dim() != 3:
+            raise ValueError("packed sequences are [rows, heads, D]")
+        starts, starts_k = _starts(starts, device, "starts", on), _starts(starts_k, device, "starts_k", on)
+        count = starts.numel() - 1
+        if starts_k is None and k.shape[0] != q.shape[0]:
+            raise ValueError("q and k have different rows: starts_k is needed")
+        if starts_k is not None and starts_k.numel() != count + 1:
+            raise ValueError("starts and starts_k are of different sequences")
+    (q, q_at), (k, k_at), (v, v_at) = _heads(q, "q", on), _heads(k, "k", on, device, q.dtype), _heads(v, "v", on, device, q.dtype)
+    a = lba_attn(q.shape[0], k.shape[0], count, _at(starts), _at(starts_k), H, KV, D, _TYPE[q.dtype], causal, clear,
+                 D ** -0.5 if scale is None else scale, q_at, k_at, v_at)
+    return a, (q, k, v, starts, starts_k)
+
+
+def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None):
+    """softmax(scale * q . k^T) . v of packed sequences: query head h reads head h * KV // H of k and v, and, causal, query i of n sees key j of m
+    iff j <= i + m - n.  starts_k: the keys' sequences where they are not the queries'.  scale: D^-1/2 by default.  Returns o of q's
+    shape and out_dtype (q's by default; torch.uint8 codes need out_fmt), and with want_stats (o, lse), float32 of q.shape[:-1], which
+    attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were."""
+    device = q.get_device()
+    dtype = out_dtype or q.dtype
+    o_type, fmt = _out_type(dtype, out_fmt)
+    if device < 0:
+        raise TypeError("q must be a device tensor")
+    handle, on = _on(stream, device)
+    a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    o = _empty(q.shape, dtype, q.device, on) if out is None else _output(out, q, q.shape, dtype, on)
+    lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
+    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), handle))
+    return (o, lse) if want_stats else o
+
+
+def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, scale=None, out=None, stream=None):
+    """Gradients of attention: (dq, dk, dv) of the inputs' shapes and type, from G = dL/do and o and lse as the forward call gave them (o of
+    q's type).  out: three tensors, or views of one, to write them to; rows of no sequence are left as they were there, and zeros elsewhere."""
+    device = q.get_device()
+    if device < 0:
+        raise TypeError("q must be a device tensor")
+    _like(G, q.shape, device, "G", (q.dtype,))
+    _like(o, q.shape, device, "o", (q.dtype,))
+    _like(lse, q.shape[:-1], device, "lse", (torch.float32,))
+    handle, on = _on(stream, device)
+    a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    G, o, lse = _whole(G, on), _whole(o, on), _whole(lse, on)
+    got = tuple(_empty(t.shape, t.dtype, t.device, on) for t in (q, k, v)) if out is None else tuple(out)
+    (dq, dq_at), (dk, dk_at), (dv, dv_at) = (_heads_out(t, w, n) for t, w, n in zip(got, (q, k, v), ("dq", "dk", "dv")))
+    size = _layer_bytes("lba_attention_bwd_workspace_bytes", a.T, a.H)
+    ws = _scratch(size, q.device, on)
+    _check(lib().lba_attention_bwd(a, _at(G), _at(q3), _at(k3), _at(v3), _at(o), _at(lse), _at(dq), dq_at, _at(dk), dk_at, _at(dv), dv_at, _at(ws), size,
+                                   handle))
+    return got
+
+
+class KVCache(typing.NamedTuple):
+    """Keys and values in 4 bits: codes uint8 [pages, KV, page, D / 2] and powers of two uint8 [pages, KV, page, D / 32] (include/lba_attention.h)."""
+    k: torch.Tensor
+    k_scale: torch.Tensor
+    v: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def kv_cache(pages, page, heads, D, device="cuda"):
+    """An empty KVCache of `pages` pages of `page` tokens each."""
+    if D % 32 or not 32 <= D <= 128:
+        raise ValueError("heads of a cache have 32, 64, 96 or 128 elements")
+    make = lambda n: torch.zeros((pages, heads, page, n), dtype=torch.uint8, device=device)  # noqa: E731
+    return KVCache(make(D // 2), make(D // 32), make(D // 2), make(D // 32))
+
+
+def _cache4(cache, table, lens, device, on):
+    """(lba_cache4, what it points to)."""
+    shape = cache.k.shape
+    if len(shape) != 4 or shape[3] % 16 or not 16 <= shape[3] <= 64:
+        raise ValueError("a cache's codes are [pages, heads, page, D / 2] with D 32, 64, 96 or 128")
+    for t, n in zip(cache, (shape[3], shape[3] // 16) * 2):
+        if t.dtype != torch.uint8 or t.get_device() != device or t.shape != shape[:3] + (n,) or not t.is_contiguous():
+            raise ValueError("a cache's tensors are contiguous torch.uint8 on the call's device, codes [..., D / 2] and powers [..., D / 32]")
+    if table.dtype != torch.int32 or table.get_device() != device or table.dim() != 2:
+        raise ValueError("table must be an int32 tensor [sequences, pages of each] on the call's device")
+    if lens.dtype != torch.int32 or lens.get_device() != device or lens.shape != table.shape[:1]:
+        raise ValueError("lens must be an int32 tensor [sequences] on the call's device")
+    table, lens = _whole(table, on), _whole(lens, on)
+    c = lba_cache4(*[_at(t) for t in cache], shape[0], table.shape[1], table.shape[0], _at(table), _at(lens), shape[2], shape[1], 2 * shape[3])
+    return c, (table, lens)
+
+
+def _cache_starts(starts, count, shape, device, on):
+    if starts is not None:
+        starts = _starts(starts, device, "starts", on)
+        if starts.numel() != count + 1:
+            raise ValueError("starts and table are of different sequences")
+        if len(shape) != 3:
+            raise ValueError("packed sequences are [rows, heads, D]")
+    elif (len(shape) == 4 and shape[0] != count) or (len(shape) == 3 and count != 1 and shape[0] != count):
+        raise ValueError("without starts rows are [sequences, length, heads, D], or [sequences, heads, D] for one token each")
+    return starts
+
+
+def cache_write(k, v, cache, table, starts, lens, stream=None):
+    """Writes the newest tokens' keys and values to their pages: rows starts[b] .. of k and v [rows, KV, D] are the last ones of sequence b, which has
+    lens[b] tokens with them; position p of it is in page table[b, p // page].  starts None: [sequences, length, KV, D], or
+    [sequences, KV, D] for a token each."""
+    device = k.get_device()
+    if device < 0 or k.shape != v.shape:
+        raise TypeError("k and v must be device tensors of one shape")
+    handle, on = _on(stream, device)
+    c, held = _cache4(cache, table, lens, device, on)
+    starts = _cache_starts(starts, c.count, k.shape, device, on)
+    if tuple(k.shape[-2:]) != (c.KV, c.D):
+        raise ValueError("k and v must be [rows, %d, %d]" % (c.KV, c.D))
+    (k3, k_at), (v3, v_at) = _heads(k, "k", on), _heads(v, "v", on, device, k.dtype)
+    _check(lib().lba_cache_write(c, _at(starts), k3.shape[0], _at(k3), k_at, _at(v3), v_at, _TYPE[k.dtype], handle))
+
+
+def cache_read(cache, table, starts, lens, rows, out_dtype=torch.bfloat16, out=None, stream=None):
+    """The newest tokens' keys and values [rows, KV, D] back from their pages, in the arrangement of cache_write, of out_dtype: exact in float32 and
+    bfloat16.  starts None: rows / sequences tokens each.  out: two tensors to write them to; rows of no sequence are left as they were there,
+    and zeros elsewhere."""
+    device = cache.k.get_device()
+    if device < 0:
+        raise TypeError("a cache is on a device")
+    if out_dtype not in _REAL:
+        raise TypeError("keys and values are torch.float32 or torch.bfloat16")
+    handle, on = _on(stream, device)
+    c, held = _cache4(cache, table, lens, device, on)
+    if starts is None:
+        if rows % max(c.count, 1) or (rows and not c.count):
+            raise ValueError("%d rows of %d sequences need starts" % (rows, c.count))
+    else:
+        starts = _cache_starts(starts, c.count, (rows, c.KV, c.D), device, on)
+    shape = (rows, c.KV, c.D)
+    got = tuple(_empty(shape, out_dtype, cache.k.device, on) for _ in range(2)) if out is None else tuple(out)
+    for t in got:
+        if tuple(t.shape) != shape or t.dtype != out_dtype:
+            raise ValueError("out must be two tensors %s of %s" % (shape, out_dtype))
+    (k3, k_at), (v3, v_at) = (_heads_out(t, got[0], "out") for t in got)
+    if k3.get_device() != device:
+        raise ValueError("out must be on the call's device")
+    _check(lib().lba_cache_read(c, _at(starts), rows, _at(k3), k_at, _at(v3), v_at, _TYPE[out_dtype], out is None, handle))
+    return got
+
+
+def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=None, out=None, stream=None):
+    """Attention of new tokens over a cache: q [sequences, heads, D] for one token each, or [sequences, tokens, heads, D], which have been written
+    (lens counts them): each sees the positions up to its own.  Returns o of q's shape and out_dtype (q's by default; torch.uint8 codes need
+    out_fmt); a query that sees nothing has zeros."""
+    device = q.get_device()
+    dtype = out_dtype or q.dtype
+    o_type, fmt = _out_type(dtype, out_fmt)
+    if device < 0:
+        raise TypeError("q must be a device tensor")
+    handle, on = _on(stream, device)
+    c, held = _cache4(cache, table, lens, device, on)
+    if q.dim() not in (3, 4) or q.shape[0] != c.count or q.shape[-1] != c.D:
+        raise ValueError("q must be [%d, heads, %d] or [%d, tokens, heads, %d]" % (c.count, c.D, c.count, c.D))
+    H = q.shape[-2]
+    if H and (not c.KV or H % c.KV):
+        raise ValueError("%d query heads do not share %d heads of keys" % (H, c.KV))
+    fresh = q.shape[1] if q.dim() == 4 else 1
+    q3, q_at = _heads(q, "q", on)
+    o = _empty(q.shape, dtype, q.device, on) if out is None else _output(out, q, q.shape, dtype, on)
+    size = _layer_bytes("lba_cache_attention_workspace_bytes", c.count, c.table_row, c.page, fresh, H, c.KV, c.D)
+    ws = _scratch(size, q.device, on)
+    _check(lib().lba_cache_attention(c, _at(q3), q_at, _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o), o_type, fmt, _at(ws), size,
+                                     handle))
+    return o

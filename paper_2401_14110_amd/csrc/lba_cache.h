@@ -1,0 +1,39 @@
+// lba_cache.h -- the cache of 4 bits an element on the device: where a position is, what a code stands for.
+#ifndef LBA_CACHE_H_
+#define LBA_CACHE_H_
+
+#include "lba_attn_device.h"
+
+namespace lba {
+
+struct CacheParams {
+    uint8_t *k, *k_scale, *v, *v_scale;
+    const int32_t *table, *lens;
+    int64_t pages, table_row;
+    int32_t count, page, KV, D;
+};
+
+int cache_params(const lba_cache4& c, CacheParams* p);
+
+// The line of a head's pages that sequence b's position `at` has, counted over the whole cache, -1: none.
+__device__ __forceinline__ int64_t line_of(const CacheParams& p, int b, int64_t at, int head) {
+    if (at < 0) return -1;
+    const int64_t column = at / p.page;
+    if (column >= p.table_row) return -1;
+    const int64_t page = p.table[(int64_t)b * p.table_row + column];
+    if (page < 0 || page >= p.pages) return -1;
+    return (page * p.KV + head) * p.page + at % p.page;
+}
+
+// 2^(e - 127) of a scale byte; 0 reads as zero, 255 as NaN
+__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7FC00000u : e << 23); }
+
+// the code in the low 4 bits of c as a number
+__device__ __forceinline__ float four_value(uint32_t c) {
+    const uint32_t m = c & 7;
+    const float a = m < 2 ? 0.5f * (float)m : __uint_as_float((m << 22) + (126u << 23));
+    return __uint_as_float(__float_as_uint(a) | ((c & 8) << 28));
+}
+
+}  // namespace lba
+#endif
