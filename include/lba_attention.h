@@ -47,7 +47,8 @@ int lba_rope_bwd(const void* G, lba_strides g_at, int32_t type, const void* posi
  * causal == 0 or j <= i + m - n: the last query sees all.  What is hidden does not matter, infinities and NaN included.
  * Rows of no sequence are left as they were, or, clear != 0, stored as zeros (-infinity in lse).
  * Q, K and V of `type` (LBA_F32 or LBA_BF16).
- * Limits (else LBA_ERR_SHAPE): T, Tk <= 2^31 - 1, count <= 2^20, H <= 65535, 1 <= D <= 128. */
+ * Limits (else LBA_ERR_SHAPE): T, Tk <= 2^31 - 1, count <= 2^20, H <= 65535, 1 <= D <= 128, and (rows / 128 + count) * heads <= 2^23 for the query
+ * rows with H and for the key rows with KV. */
 typedef struct {
     int64_t T, Tk, count;
     const int32_t *starts, *starts_k;

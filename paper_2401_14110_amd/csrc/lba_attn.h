@@ -18,11 +18,21 @@ struct AttnParams {
     const int32_t *starts, *starts_k;
     lba_strides q, k, v, dq, dk, dv;
     int32_t T, Tk, count, H, KV, group, D;
-    int32_t causal, clear;
+    int32_t causal, clear, o_type;
+    int32_t tiles, units;    // tiles of queries that there may be, and those of all heads
     float scale;
 };
 
 int attn_params(const lba_attn& a, AttnParams* p);       // checks and copies the description
+
+constexpr int64_t kMostUnits = 1 << 23;                  // workgroups of a launch: fewer than 2^32 lanes
+
+// Whether rows can go to LDS in pieces of 16 aligned bytes: one more head or row keeps the place in a piece.
+inline bool whole_pieces(const void* x, const lba_strides& at, int64_t D, int64_t size) {
+    return ((uintptr_t)x | (uintptr_t)(at.row * size) | (uintptr_t)(at.head * size) | (uintptr_t)(D * size)) % 16 == 0;
+}
+
+template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st);
 
 }  // namespace lba
 #endif

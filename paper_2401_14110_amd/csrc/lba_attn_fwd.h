@@ -1,0 +1,195 @@
+// lba_attn_fwd.h -- attention over packed sequences, forward.
+//
+// A workgroup has 128 queries of a head, a wave 32 of them, one a lane pair; it walks over the keys in tiles of KT, which go to LDS in two buffers. S^T = K . Q^T
+// puts a query's scores into its own two lanes, so that the running maximum and sum are a lane's own numbers but for one exchange a tile, and
+// P^T goes on to O^T = V^T . P^T without leaving its registers.  The maximum is moved (and the sums multiplied) only where a score is more than 8
+// above it in units of log 2: weights are then at most 256 times the final ones, which changes no rounding.
+#ifndef LBA_ATTN_FWD_H_
+#define LBA_ATTN_FWD_H_
+
+#include "lba_attn_tile.h"
+
+namespace lba {
+
+constexpr int kQueries = 128;                            // of a workgroup
+constexpr int kClearBlocks = 16;
+
+// the rows of no sequence, by the last blocks of the grid
+template <typename T> __device__ __forceinline__ void clear_rows(const int32_t* starts, int T_rows, int count, int block, int blocks, T* out, int64_t row_stride,
+                                                                 int64_t head_stride, int H, int D, float* lse, const CodeFmt& fmt) {
+    const int first = count > 0 ? min(max(starts[0], 0), T_rows) : T_rows, last = count > 0 ? min(max(starts[count], first), T_rows) : T_rows;
+    const int64_t rows = (int64_t)first + (T_rows - last);
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < rows * H * D; i += (int64_t)blocks * 256) {
+        const int d = (int)(i % D), h = (int)(i / D % H);
+        const int64_t r = i / D / H, t = r < first ? r : last + (r - first);
+        store_one(out + t * row_stride + h * head_stride + d, 0.0f, fmt);
+        if (lse && d == 0) lse[t * H + h] = -__builtin_inff();
+    }
+}
+
+template <typename T, int DP, bool DIRECT>
+__global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnParams p) {
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
+    constexpr int TILE = KT * DP * (int)sizeof(T);
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
+    if ((int)blockIdx.x >= p.units) {
+        const int block = blockIdx.x - p.units;
+        if (p.o_type == LBA_F32) clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (float*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
+        else if (p.o_type == LBA_BF16) clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (bf16_t*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
+        else clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (uint8_t*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
+        return;
+    }
+    const int unit = unit_of(blockIdx.x, p.units), per = p.tiles * p.group;
+    const int kv = unit / per, h = kv * p.group + unit % per % p.group;
+    const TileOf at = find_tile(p.starts, p.T, p.count, kQueries, p.tiles - 1 - unit % per / p.group);               // later tiles of a sequence, which see more, first
+    if (at.b < 0) return;
+    const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
+    const int ahead = rk.n - rq.n;
+    auto limit = [&](int i) { return p.causal ? max(0, min(rk.n, i + ahead + 1)) : rk.n; };                          // keys that query i sees
+    const int i0 = at.t * kQueries + wave * 32, i = i0 + (lane & 31);
+    const int lim = limit(i), least = limit(i0), most = i0 < rq.n ? limit(min(i0 + 31, rq.n - 1)) : 0;
+    const int tiles = (limit(min(at.t * kQueries + kQueries, rq.n) - 1) + KT - 1) / KT, least_all = limit(at.t * kQueries);
+
+    Loader<T, DP, KT, DIRECT> lk, lv;
+    lk.start((const T*)p.K + (int64_t)rk.first * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
+    lv.start((const T*)p.V + (int64_t)rk.first * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
+    if (tiles > 0) {
+        lk.load(lds[0][0], rk.n);
+        lv.load(lds[0][1], rk.n);
+    }
+    Frag<T> q[KC];
+    load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, i < rq.n, p.D, half, q);
+    float c = p.scale * 1.44269504f;                     // weights are 2^(c s); c > 0 after this
+    if (!(c > 0.0f)) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            if constexpr (sizeof(T) == 2) {
+                q[k].w = c == 0.0f ? i32x4_t{0, 0, 0, 0} : q[k].w ^ (int32_t)0x80008000;
+            } else {
+                q[k].a = c == 0.0f ? f32x4_t{0, 0, 0, 0} : -q[k].a;
+                q[k].b = c == 0.0f ? f32x4_t{0, 0, 0, 0} : -q[k].b;
+            }
+        }
+        c = c == 0.0f ? 1.0f : -c;
+    }
+
+    f32x16 acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
+    float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
+    for (int kt = 0; kt < tiles; ++kt) {
+        const int k0 = kt * KT;
+        uint8_t* const tk = lds[kt & 1][0];
+        uint8_t* const tv = lds[kt & 1][1];
+        lk.put(tk);
+        lv.put(tv);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();                    // this tile is there, and the one before it has been read
+        asm volatile("" ::: "memory");
+        if (kt + 1 < tiles) {
+            lk.load(lds[(kt + 1) & 1][0], rk.n - k0 - KT);
+            lv.load(lds[(kt + 1) & 1][1], rk.n - k0 - KT);
+        }
+        const bool broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv);
+        if (k0 >= most) continue;                        // (the barriers above are everybody's)
+        f32x16 s[KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            s[b] = f32x16{};
+#pragma unroll
+            for (int k = 0; k < KC; ++k) s[b] = product(row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half), q[k], s[b]);
+        }
+        if (k0 + KT > least) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (k0 + 32 * b + row_of(r) + 4 * half >= lim) s[b][r] = -__builtin_inff();
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+        mx = fmaxf(mx, other_half(mx)) * c;
+        if (__any(mx > top + 8.0f)) {
+            const float now = fmaxf(mx, top);
+            const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] *= f;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : -top;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
+                sum += s[b][r];
+            }
+        if (!broken) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const Frag<T> w = as_frag<T>(s[b], k);
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
+                }
+        } else {                                         // a zero weight must not meet an infinity: key by key, where it is seen
+            for (int j = 0; j < KT && k0 + j < rk.n; ++j) {
+                float w = 0.0f;
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * b + row_of(r) == (j & ~4)) w = s[b][r];
+                w = __shfl(w, (lane & 31) + 8 * (j & 4));
+                if (k0 + j < lim) {
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(w, tile_at<T, DP>(tv, j, 32 * t + row_of(r) + 4 * half), acc[t][r]);
+                }
+            }
+        }
+    }
+    sum += other_half(sum);
+    if (i >= rq.n) return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t row = (int64_t)(rq.first + i) * p.H + h;
+    if (p.lse && half == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
+    auto store = [&](auto* o) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int d = 32 * t + 8 * g + 4 * half;
+                const float v[4] = {acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv, acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv};
+                if (d < p.D) store_some<4>(o + row * p.D + d, p.D - d, v, p.fmt);
+            }
+    };
+    if (p.o_type == LBA_F32) store((float*)p.O);
+    else if (p.o_type == LBA_BF16) store((bf16_t*)p.O);
+    else store((uint8_t*)p.O);
+}
+
+template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st) {
+    const dim3 grid((unsigned)(p.units + (p.clear && p.starts ? kClearBlocks : 0)));
+#define LBA_ATTN(DP) \
+    if (p.D <= DP) { \
+        if (direct) hipLaunchKernelGGL((attn_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
+        else hipLaunchKernelGGL((attn_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
+        return; \
+    }
+    LBA_ATTN(32)
+    LBA_ATTN(64)
+    LBA_ATTN(96)
+    LBA_ATTN(128)
+#undef LBA_ATTN
+}
+
+}  // namespace lba
+#endif

@@ -1,0 +1,245 @@
+// lba_attn_tile.h -- the tiles of the attention kernels: rows of heads in LDS, fragments of the matrix cores, which tile a workgroup has.
+//
+// A wave owns 32 columns of a product, one a lane pair (l, l + 32): the queries of S^T = K . Q^T and O^T = V^T . P^T, the keys of the backward
+// pass's S = Q . K^T, dV^T = G^T . P and dK^T = Q^T . S.  The 32 x 32 result of a product has in lane l column l % 32 and in register r row
+//   (r % 4) + 8 (r / 4) + 4 (l / 32),
+// and the 16 x 32 factor of the next product needs of its 16 rows eight in each half of the wave: any eight, if the other factor is read in
+// the same order.  So a result's registers 8 k .. 8 k + 7 are, rounded, the next factor's fragment as they are, what is per column (a query's
+// maximum and sum) is per lane, and the other factor is read with rows (j % 4) + 8 (j / 4) + 4 (l / 32) of each 16: transposed reads of 4 x 16
+// elements from LDS.
+#ifndef LBA_ATTN_TILE_H_
+#define LBA_ATTN_TILE_H_
+
+#include "lba_attn.h"
+
+namespace lba {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int16_t i16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_v __attribute__((ext_vector_type(2)));
+
+__device__ __attribute__((aligned(16))) const uint32_t attn_zeros[4] = {0, 0, 0, 0};
+
+// eight elements of a factor's row
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> { i32x4_t w; };
+template <> struct Frag<float> { f32x4_t a, b; };
+
+// c + a . b of 32 x 16 and 16 x 32.  Float32: eight products of depth 2, the two halves of the wave one row each
+__device__ __forceinline__ f32x16 product(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_v, a.w), __builtin_bit_cast(bf16x8_v, b.w), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 product(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.a[j], b.a[j], c, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.b[j], b.b[j], c, 0, 0, 0);
+    return c;
+}
+
+// registers 8 k .. 8 k + 7 of a result as a fragment
+template <typename T> __device__ __forceinline__ Frag<T> as_frag(const f32x16& s, int k) {
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bf16x2_v two = {(bf16_t)s[8 * k + 2 * j], (bf16_t)s[8 * k + 2 * j + 1]};
+            f.w[j] = __builtin_bit_cast(int32_t, two);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { f.a[j] = s[8 * k + j]; f.b[j] = s[8 * k + 4 + j]; }
+    }
+    return f;
+}
+
+// row of the result's register r in this lane's half
+__device__ __forceinline__ constexpr int row_of(int r) { return (r % 4) + 8 * (r / 4); }
+
+// ---- tiles in LDS ---------------------------------------------------------------------------
+//
+// A row of DP elements (D rounded up to 32, zeros behind D) is C = DP * sizeof(T) / 16 pieces of 16 bytes; piece c of row r stands at place
+// c ^ turn(r) of its row.  Then the 16 lanes of a row read (one piece of 16 rows) and those of a transposed read (four pieces of four rows)
+// meet 64 different banks.
+template <int C> __device__ __forceinline__ int turn(int r) {
+    if constexpr (C % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else if constexpr (C % 8 == 0) return ((r & 2) << 1) | ((r >> 2) & 3);
+    else return (r >> 2) & 3;
+}
+
+// the fragment of row `row` (this lane's) with elements 16 k + 8 (l / 32) ..
+template <typename T, int DP> __device__ __forceinline__ Frag<T> row_frag(const uint8_t* tile, int row, int k, int half) {
+    constexpr int C = DP * sizeof(T) / 16;
+    const uint8_t* at = tile + row * (C * 16);
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        f.w = *(const i32x4_t*)(at + ((2 * k + half) ^ turn<C>(row)) * 16);
+    } else {
+        f.a = *(const f32x4_t*)(at + ((4 * k + 2 * half) ^ turn<C>(row)) * 16);
+        f.b = *(const f32x4_t*)(at + ((4 * k + 2 * half + 1) ^ turn<C>(row)) * 16);
+    }
+    return f;
+}
+// The fragment of column 32 t + l % 32 with rows row0 + (j % 4) + 8 (j / 4) + 4 (l / 32), row0 a multiple of 16.  A transposed read gives each of 16 lanes
+// column i of a 4 x 16 block whose rows four lanes each address.
+template <typename T, int DP> __device__ __forceinline__ Frag<T> column_frag(const uint8_t* tile, int row0, int t, int lane) {
+    constexpr int C = DP * sizeof(T) / 16;
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        const int r = row0 + 4 * (lane / 32) + (lane & 15) / 4, c = 4 * t + 2 * ((lane / 16) & 1) + (lane & 3) / 2;
+        typedef __attribute__((address_space(3))) i16x4_t* lds_ptr;
+        union { i16x4_t s[2]; i32x4_t w; } u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (r + 8 * i) * (C * 16) + (c ^ turn<C>(r + 8 * i)) * 16 + (lane & 1) * 8));
+        f.w = u.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = row0 + row_of(j) + 4 * (lane / 32);
+            const float x = *(const float*)(tile + r * (C * 16) + ((8 * t + (lane & 31) / 4) ^ turn<C>(r)) * 16 + (lane & 3) * 4);
+            if (j < 4) f.a[j] = x; else f.b[j - 4] = x;
+        }
+    }
+    return f;
+}
+// element (row, d) of a tile
+template <typename T, int DP> __device__ __forceinline__ float tile_at(const uint8_t* tile, int row, int d) {
+    constexpr int C = DP * sizeof(T) / 16, V = 16 / sizeof(T);
+    return load_one((const T*)(tile + row * (C * 16) + ((d / V) ^ turn<C>(row)) * 16) + d % V);
+}
+
+// Rows of a head on their way to a tile of ROWS rows.  DIRECT: rows are whole pieces of 16 aligned bytes and go from memory to LDS without
+// registers in between; else a lane holds them until they are put down.  What is behind `rows` rows or D elements is zeros.
+template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
+    static constexpr int C = DP * sizeof(T) / 16, V = 16 / sizeof(T), N = ROWS * C / 256;
+    static_assert(ROWS * C % 256 == 0, "whole pieces a lane");
+    // 256 pieces are whole groups of 16 rows, after which turn() is the same: a lane's pieces are the same ones of rows 256 / C apart
+    static constexpr bool EVEN = 4096 % (C * 256) == 0 && C <= 16;
+    static constexpr int P = EVEN ? 1 : N;
+    typedef typename Bits<T>::type B;
+    const B* at[P];          // this lane's pieces in the first tile
+    int64_t stride;
+    int left[P];             // how many elements of the row are from there on
+    Raw<B, V> held[DIRECT ? 1 : N];
+
+    __device__ __forceinline__ void start(const void* base, int64_t row_stride, int D) {
+        stride = row_stride;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int p = threadIdx.x + 256 * i, r = p / C, c = (p % C) ^ turn<C>(r);
+            left[i] = D - c * V;
+            at[i] = (const B*)base + (int64_t)r * row_stride + c * V;
+        }
+    }
+    // the next tile, of which `rows` rows are there
+    __device__ __forceinline__ void load(uint8_t* tile, int rows) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const B* src = EVEN ? at[0] + i * (256 / C) * stride : at[i];
+            const int more = left[EVEN ? 0 : i];
+            const bool in = ((int)threadIdx.x + 256 * i) / C < rows && more > 0;
+            if constexpr (DIRECT) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(in ? (const void*)src : (const void*)attn_zeros),
+                                                 (__attribute__((address_space(3))) uint32_t*)(tile + (256 * i + (threadIdx.x & 192)) * 16), 16, 0, 0);
+            } else {
+                held[i] = load_raw<B, V>(src, in ? more : 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) at[i] += stride * ROWS;
+    }
+    __device__ __forceinline__ void put(uint8_t* tile) const {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) *(i32x4_t*)(tile + (threadIdx.x + 256 * i) * 16) = __builtin_bit_cast(i32x4_t, held[i].v);
+        }
+    }
+};
+
+// Whether the tile holds an infinity or a NaN, looked for by the whole workgroup (a barrier: all of it calls).
+template <typename T, int DP, int ROWS> __device__ __forceinline__ bool tile_is_broken(const uint8_t* tile) {
+    constexpr int N = ROWS * DP * (int)sizeof(T) / 16 / 256;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const i32x4_t w = *(const i32x4_t*)(tile + (threadIdx.x + 256 * i) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = (uint32_t)w[j];
+            if constexpr (sizeof(T) == 2) bad |= (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
+            else bad |= (x & 0x7F800000u) == 0x7F800000u;
+        }
+    }
+    return __syncthreads_or(bad) != 0;
+}
+
+// a lane's row of a head as fragments: `D` elements from `at`, zeros behind; row < 0: zeros.  FLIP: with the other sign.
+template <typename T, int DP> __device__ __forceinline__ void load_frags(const void* at, bool there, int D, int half, Frag<T> (&f)[DP / 16]) {
+    typedef typename Bits<T>::type B;
+    const B* p = (const B*)at;
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const int d = 16 * k + 8 * half;
+        if constexpr (sizeof(T) == 2) {
+            const Raw<B, 8> r = load_raw<B, 8>(p + d, there ? D - d : 0);
+            f[k].w = __builtin_bit_cast(i32x4_t, r.v);
+        } else {
+            f[k].a = __builtin_bit_cast(f32x4_t, load_raw<B, 4>(p + d, there ? D - d : 0).v);
+            f[k].b = __builtin_bit_cast(f32x4_t, load_raw<B, 4>(p + d + 4, there ? D - d - 4 : 0).v);
+        }
+    }
+}
+
+// the larger of a value's copies in lanes l and l ^ 32, and their sum
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ---- which tile -----------------------------------------------------------------------------
+
+struct TileOf {
+    int b, t;                // sequence (-1: none) and its tile
+};
+
+// Tile `index` of the tiles of `size` rows that the sequences have one after another; the whole wave calls.
+__device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, int count, int size, int index) {
+    if (!starts) {
+        const int per = (T / count + size - 1) / size;
+        if (per == 0 || index / per >= count) return {-1, 0};
+        return {index / per, index % per};
+    }
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < count; b0 += 64) {
+        const int n = b0 + lane < count ? (rows_of(starts, T, count, b0 + lane).n + size - 1) / size : 0;
+        int upto = n;
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            const int v = __shfl_up(upto, x);
+            if (lane >= x) upto += v;
+        }
+        const uint64_t behind = __ballot(upto > index);
+        if (behind) {
+            const int f = __builtin_ctzll(behind);
+            return {b0 + f, index - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(n, f))};
+        }
+        index -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {-1, 0};
+}
+// how many tiles there may be
+inline int64_t most_tiles(const int32_t* starts, int64_t T, int64_t count, int size) {
+    if (count < 1 || T < 1) return 0;
+    if (!starts) return count * ((T / count + size - 1) / size);
+    return T / size + (count < T ? count : T);
+}
+
+// Workgroups go to the eight dies in turn; each die takes a run of neighbouring units, which share a head's keys in its cache.
+__device__ __forceinline__ int unit_of(int block, int units) {
+    const int per = units / 8, more = units % 8, die = block % 8;
+    return die * per + min(die, more) + block / 8;
+}
+
+}  // namespace lba
+#endif

@@ -281,9 +281,9 @@ def test_many_sequences():
     rng = np.random.default_rng(9)
     lens = [int(n) for n in rng.integers(0, 6, 700)]
     check(lens, lens, 2, 1, 16, True, "bf16")
-    count = 5000                                         # one token each: the value itself
+    count = 5000                                         # one token each: the value itself, but for w v and 1 / w, whose weight w is near 1: 8 roundings
     v = torch.randn(count, 2, 8, device=DEV)
-    assert torch.equal(lb.attention(v, v, v, starts=torch.arange(count + 1, dtype=torch.int32, device=DEV)), v)
+    near(lb.attention(v, v, v, starts=torch.arange(count + 1, dtype=torch.int32, device=DEV)), host(v), 8 * lo.U * np.abs(host(v)), "f32")
 
 
 @pytest.mark.gpu
