@@ -25,6 +25,8 @@ struct AttnParams {
 
 int attn_params(const lba_attn& a, AttnParams* p);       // checks and copies the description
 
+constexpr int kTileRows = 128;                           // queries (keys, where keys have the sums) of a workgroup
+constexpr int kClearBlocks = 16;                         // workgroups behind the others, for rows of no sequence
 constexpr int64_t kMostUnits = 1 << 23;                  // workgroups of a launch: fewer than 2^32 lanes
 
 // Whether rows can go to LDS in pieces of 16 aligned bytes: one more head or row keeps the place in a piece.
@@ -32,6 +34,8 @@ inline bool whole_pieces(const void* x, const lba_strides& at, int64_t D, int64_
     return ((uintptr_t)x | (uintptr_t)(at.row * size) | (uintptr_t)(at.head * size) | (uintptr_t)(D * size)) % 16 == 0;
 }
 
+template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipStream_t st);
+template <typename T> void launch_attn_dkv(const AttnParams& p, bool direct, hipStream_t st);
 template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st);
 
 }  // namespace lba

@@ -40,7 +40,7 @@ extern "C" int lba_attention(lba_attn a, const void* Q, const void* K, const voi
     p.Q = Q; p.K = K; p.V = V; p.O = O; p.lse = lse;
     if (o_type == LBA_CODE8) p.fmt = make_code_fmt(o_fmt);
     p.o_type = o_type;
-    const int64_t tiles = most_tiles(p.starts, p.T, p.count, 128);
+    const int64_t tiles = most_tiles(p.starts, p.T, p.count, kTileRows);
     if (tiles * p.H > kMostUnits) return LBA_ERR_SHAPE;
     p.tiles = (int32_t)tiles;
     p.units = (int32_t)(tiles * p.H);

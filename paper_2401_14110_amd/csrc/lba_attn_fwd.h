@@ -11,22 +11,6 @@
 
 namespace lba {
 
-constexpr int kQueries = 128;                            // of a workgroup
-constexpr int kClearBlocks = 16;
-
-// the rows of no sequence, by the last blocks of the grid
-template <typename T> __device__ __forceinline__ void clear_rows(const int32_t* starts, int T_rows, int count, int block, int blocks, T* out, int64_t row_stride,
-                                                                 int64_t head_stride, int H, int D, float* lse, const CodeFmt& fmt) {
-    const int first = count > 0 ? min(max(starts[0], 0), T_rows) : T_rows, last = count > 0 ? min(max(starts[count], first), T_rows) : T_rows;
-    const int64_t rows = (int64_t)first + (T_rows - last);
-    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < rows * H * D; i += (int64_t)blocks * 256) {
-        const int d = (int)(i % D), h = (int)(i / D % H);
-        const int64_t r = i / D / H, t = r < first ? r : last + (r - first);
-        store_one(out + t * row_stride + h * head_stride + d, 0.0f, fmt);
-        if (lse && d == 0) lse[t * H + h] = -__builtin_inff();
-    }
-}
-
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnParams p) {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
@@ -41,15 +25,15 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     }
     const int unit = unit_of(blockIdx.x, p.units), per = p.tiles * p.group;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
-    const TileOf at = find_tile(p.starts, p.T, p.count, kQueries, p.tiles - 1 - unit % per / p.group);               // later tiles of a sequence, which see more, first
+    const TileOf at = find_tile(p.starts, p.T, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);               // later tiles of a sequence, which see more, first
     if (at.b < 0) return;
     const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
     const int ahead = rk.n - rq.n;
     auto limit = [&](int i) { return p.causal ? max(0, min(rk.n, i + ahead + 1)) : rk.n; };                          // keys that query i sees
-    const int i0 = at.t * kQueries + wave * 32, i = i0 + (lane & 31);
+    const int i0 = at.t * kTileRows + wave * 32, i = i0 + (lane & 31);
     const int lim = limit(i), least = limit(i0), most = i0 < rq.n ? limit(min(i0 + 31, rq.n - 1)) : 0;
-    const int tiles = (limit(min(at.t * kQueries + kQueries, rq.n) - 1) + KT - 1) / KT, least_all = limit(at.t * kQueries);
+    const int tiles = (limit(min(at.t * kTileRows + kTileRows, rq.n) - 1) + KT - 1) / KT, least_all = limit(at.t * kTileRows);
 
     Loader<T, DP, KT, DIRECT> lk, lv;
     lk.start((const T*)p.K + (int64_t)rk.first * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);

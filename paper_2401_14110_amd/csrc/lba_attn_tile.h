@@ -40,6 +40,24 @@ __device__ __forceinline__ f32x16 product(const Frag<float>& a, const Frag<float
     return c;
 }
 
+// the sum of the fragments' eight products
+__device__ __forceinline__ float dot(const Frag<bf16_t>& a, const Frag<bf16_t>& b) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = (uint32_t)a.w[j], y = (uint32_t)b.w[j];
+        s = fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), s);
+        s = fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), s);
+    }
+    return s;
+}
+__device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = fmaf(a.b[j], b.b[j], fmaf(a.a[j], b.a[j], s));
+    return s;
+}
+
 // registers 8 k .. 8 k + 7 of a result as a fragment
 template <typename T> __device__ __forceinline__ Frag<T> as_frag(const f32x16& s, int k) {
     Frag<T> f;
@@ -196,6 +214,22 @@ template <typename T, int DP> __device__ __forceinline__ void load_frags(const v
 
 // the larger of a value's copies in lanes l and l ^ 32, and their sum
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ---- rows of no sequence ----------------------------------------------------------------------
+
+
+// the rows of no sequence, by the last blocks of the grid
+template <typename T> __device__ __forceinline__ void clear_rows(const int32_t* starts, int T_rows, int count, int block, int blocks, T* out, int64_t row_stride,
+                                                                 int64_t head_stride, int H, int D, float* lse, const CodeFmt& fmt) {
+    const int first = count > 0 ? min(max(starts[0], 0), T_rows) : T_rows, last = count > 0 ? min(max(starts[count], first), T_rows) : T_rows;
+    const int64_t rows = (int64_t)first + (T_rows - last);
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < rows * H * D; i += (int64_t)blocks * 256) {
+        const int d = (int)(i % D), h = (int)(i / D % H);
+        const int64_t r = i / D / H, t = r < first ? r : last + (r - first);
+        store_one(out + t * row_stride + h * head_stride + d, 0.0f, fmt);
+        if (lse && d == 0) lse[t * H + h] = -__builtin_inff();
+    }
+}
 
 // ---- which tile -----------------------------------------------------------------------------
 
