@@ -11,6 +11,13 @@ struct CacheParams {
     const int32_t *table, *lens;
     int64_t pages, table_row;
     int32_t count, page, KV, D;
+    uint32_t page_mul, page_shift;                       // position / page without a division, for positions below 2^31
+
+    __device__ __forceinline__ int64_t page_div(int64_t at) const {
+        const uint32_t x = (uint32_t)at, t = __umulhi(page_mul, x);
+        return page_shift == 0 ? x : (t + ((x - t) >> 1)) >> (page_shift - 1);
+    }
+    __device__ __forceinline__ int32_t page_mod(int64_t at) const { return (int32_t)(at - page_div(at) * page); }
 };
 
 int cache_params(const lba_cache4& c, CacheParams* p);
@@ -18,11 +25,11 @@ int cache_params(const lba_cache4& c, CacheParams* p);
 // The line of a head's pages that sequence b's position `at` has, counted over the whole cache, -1: none.
 __device__ __forceinline__ int64_t line_of(const CacheParams& p, int b, int64_t at, int head) {
     if (at < 0) return -1;
-    const int64_t column = at / p.page;
+    const int64_t column = p.page_div(at);
     if (column >= p.table_row) return -1;
     const int64_t page = p.table[(int64_t)b * p.table_row + column];
     if (page < 0 || page >= p.pages) return -1;
-    return (page * p.KV + head) * p.page + at % p.page;
+    return (page * p.KV + head) * p.page + p.page_mod(at);
 }
 
 // 2^(e - 127) of a scale byte; 0 reads as zero, 255 as NaN

@@ -20,6 +20,12 @@ int cache_params(const lba_cache4& c, CacheParams* p) {
     if (c.page < 1 || c.page > 65536 || c.KV < 0 || c.KV > 65535 || c.D < 32 || c.D > 128 || c.D % 32 != 0) return LBA_ERR_SHAPE;
     p->k = c.k; p->k_scale = c.k_scale; p->v = c.v; p->v_scale = c.v_scale; p->table = c.table; p->lens = c.lens;
     p->pages = c.pages; p->table_row = c.table_row; p->count = (int32_t)c.count; p->page = c.page; p->KV = c.KV; p->D = c.D;
+    // floor(x / d) for x < 2^32: with 2^s the first power at or above d and m = floor(2^32 (2^s - d) / d) + 1,
+    // (t + (x - t) / 2) / 2^(s - 1) where t is the high word of m x
+    uint32_t s = 0;
+    while ((1 << s) < c.page) ++s;
+    p->page_shift = s;
+    p->page_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - (uint64_t)c.page)) / (uint64_t)c.page + 1);
     return LBA_OK;
 }
 

@@ -1,0 +1,370 @@
+// lba_cache_attn.h -- attention of new tokens over a cache of 4 bits an element.
+//
+// A token reads its whole cache, so this is a pass over codes.  A workgroup takes one head of keys of one sequence, up to 16 R rows (the new tokens'
+// query heads that share it) and a chunk of positions; its four waves take steps of 32 positions in turn, each with a softmax of its own,
+// and meet in LDS at the end.  Chunks leave their sums, maximum and rows in the workspace, where a second launch joins them, always in the
+// same order.
+// In a step lane l has position l % 16 (and that + 16), elements D / 4 * (l / 16) ..: codes come as they are packed, 512 bytes a load, and become bfloat16
+// in registers, which holds a code times a power of two exactly.  S^T = K . Q^T on 16 x 16 x 32 leaves a row's scores in four lanes; their
+// weights are the other factor of O^T = V^T . P^T without moving, and V, whose rows have to become columns, goes through 32 rows of LDS that
+// are the wave's own: no barriers.  Float32: queries and weights are split into three bfloat16 pieces each, so that products are exact.
+#ifndef LBA_CACHE_ATTN_H_
+#define LBA_CACHE_ATTN_H_
+
+#include "lba_cache.h"
+
+namespace lba {
+
+typedef float f32x4_c __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4_c __attribute__((ext_vector_type(4)));
+typedef int16_t i16x4_c __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_c __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_c __attribute__((ext_vector_type(2)));
+
+struct CacheAttnParams {
+    CacheParams c;
+    const void* Q;
+    void* O;
+    float* part;             // [rows][chunks][D]: sums; then [rows][chunks][2]: maximum, sum of weights; null: one chunk
+    CodeFmt fmt;
+    lba_strides q;
+    int32_t room;            // positions of a sequence's table
+    int32_t fresh, H, group, o_type;
+    int32_t chunk, chunks, row_tiles;
+    float scale;
+};
+
+// how many positions a row sees; of a tile its last row sees most
+__device__ __forceinline__ int row_seen(const CacheAttnParams& p, int b, int row) {
+    return (int)max((int64_t)0, min((int64_t)p.c.lens[b] - p.fresh + row / p.group + 1, (int64_t)p.room));
+}
+
+__device__ __forceinline__ float max_of_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_of_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// a number in N bfloat16 pieces
+template <int N> __device__ __forceinline__ void split(float x, bf16_t (&piece)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        piece[i] = (bf16_t)x;
+        x -= (float)piece[i];
+    }
+}
+
+__device__ __forceinline__ f32x4_c product16(const i32x4_c& a, const i32x4_c& b, f32x4_c c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_c, a), __builtin_bit_cast(bf16x8_c, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ i32x4_c eight_fours(uint32_t w, float scale) {
+    return i32x4_c{__builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)), __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                   __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)), __builtin_bit_cast(int32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+
+// A lane's part of a position: D / 4 codes, and the powers of the blocks they are in
+template <int D> struct Part {
+    static constexpr int KC = D / 32, NS = D == 96 ? 3 : 1;                          // words of codes; blocks that differ between them
+    uint32_t w[KC];
+    uint8_t e[NS];
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t line, int quarter) {
+        if (line < 0) {
+#pragma unroll
+            for (int i = 0; i < KC; ++i) w[i] = 0;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) e[i] = 127;
+            return;
+        }
+        typedef typename Vec<uint32_t, KC>::type V;
+        typedef V AnyV __attribute__((aligned(1)));
+        const V x = *(const AnyV*)(codes + line * (D / 2) + quarter * (D / 8));
+        if constexpr (KC == 1) {
+            w[0] = x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < KC; ++i) w[i] = x[i];
+        }
+#pragma unroll
+        for (int i = 0; i < NS; ++i) e[i] = scales[line * (D / 32) + (quarter * (D / 4) + 8 * i) / 32];
+    }
+    // word i as bfloat16 numbers
+    __device__ __forceinline__ i32x4_c values(int i) const {
+        const uint32_t s = e[NS == 1 ? 0 : i];
+        return eight_fours(s == 0 ? 0u : w[i], __uint_as_float(s << 23));            // the conversion reads an exponent of all ones as NaN
+    }
+    __device__ __forceinline__ bool broken() const {     // NaN, or codes that may be beyond the numbers
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) bad |= e[i] >= 253;
+        return bad;
+    }
+};
+
+// Rows of values in LDS: piece c of 16 bytes stands at c ^ this, so that 16 rows of one piece, and eight rows of two, meet different banks.
+template <int D> __device__ __forceinline__ int value_turn(int r) {
+    if constexpr (D == 128) return 2 * (r & 7) + ((r >> 3) & 1);
+    else if constexpr (D == 64) return 2 * ((r >> 1) & 3) + ((r >> 3) & 1);
+    else return 2 * ((r >> 2) & 1) + ((r >> 3) & 1);
+}
+
+template <typename T, int D, int R>
+__global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 2) void cache_attn_kernel(CacheAttnParams p) {
+    constexpr int KC = D / 32, DT = D / 16, NP = sizeof(T) == 2 ? 1 : 3;
+    constexpr int ROWB = D * 2, WAVE = (32 * ROWB > 16 * R * D * 4 ? 32 * ROWB : 16 * R * D * 4);    // values of a step; at the end a wave's sums
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4][WAVE];
+    __shared__ float ends[4][2][16 * R];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = lane & 15, quarter = lane / 16;
+    const int b = blockIdx.z, kv = blockIdx.y / p.row_tiles, row0 = blockIdx.y % p.row_tiles * (16 * R), rows = p.fresh * p.group;
+    const int seen = row_seen(p, b, min(row0 + 16 * R, rows) - 1), c0 = blockIdx.x * p.chunk;
+    if (c0 >= seen && blockIdx.x > 0) return;
+    const int c1 = min(c0 + p.chunk, seen);
+    const bool alone = seen <= p.chunk;                  // the only chunk that there is
+
+    // this lane's rows, and how far they see (rows that are not there: as far as any)
+    int lim[R];
+    i32x4_c q[R][NP][KC];
+    float c = p.scale * 1.44269504f;
+    const float flip = c < 0.0f ? -1.0f : c == 0.0f ? 0.0f : 1.0f;
+    c = c < 0.0f ? -c : c == 0.0f ? 1.0f : c;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        const int r = row0 + 16 * t + col, i = r / p.group, h = kv * p.group + r % p.group;
+        const int64_t token = (int64_t)b * p.fresh + i;
+        lim[t] = r < rows ? row_seen(p, b, r) : seen;
+        const T* x = (const T*)p.Q + token * p.q.row + (int64_t)h * p.q.head + quarter * (D / 4);
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            if (r < rows) load_vec<8>(x + 8 * k, v);
+            bf16_t piece[8][NP];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) split<NP>(flip == 0.0f ? 0.0f : v[j] * flip, piece[j]);
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) q[t][n][k][j] = __builtin_bit_cast(int32_t, bf16x2_c{piece[2 * j][n], piece[2 * j + 1][n]});
+        }
+    }
+
+    auto page_of = [&](int pos) -> int32_t { return pos < c1 ? p.c.table[(int64_t)b * p.c.table_row + p.c.page_div(pos)] : -1; };
+    auto line_at = [&](int pos, int32_t page) -> int64_t {
+        return pos < c1 && page >= 0 && page < p.c.pages ? ((int64_t)page * p.c.KV + kv) * p.c.page + p.c.page_mod(pos) : -1;
+    };
+    f32x4_c acc[R][DT];
+    float top[R], sum[R];
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        top[t] = -__builtin_inff();
+        sum[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[t][d] = f32x4_c{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    int k0 = c0 + wave * 32;
+    Part<D> nk[2], nv[2];
+    int64_t line[2];
+    int32_t page[2];
+    auto fetch = [&](int at0) {                      // codes of the step at at0, whose pages are known; then the next step's pages
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            line[u] = line_at(at0 + 16 * u + col, page[u]);
+            nk[u].load(p.c.k, p.c.k_scale, line[u], quarter);
+            nv[u].load(p.c.v, p.c.v_scale, line[u], quarter);
+            page[u] = page_of(at0 + 128 + 16 * u + col);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < 2; ++u) page[u] = page_of(k0 + 16 * u + col);
+    if (k0 < c1) fetch(k0);
+    uint8_t* const mine = lds[wave];
+    for (; k0 < c1; k0 += 128) {
+        Part<D> kp[2] = {nk[0], nk[1]}, vp[2] = {nv[0], nv[1]};
+        const bool there[2] = {line[0] >= 0, line[1] >= 0};
+        fetch(k0 + 128);
+        f32x4_c s[R][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) s[t][u] = f32x4_c{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const i32x4_c a = kp[u].values(k);
+#pragma unroll
+                for (int t = 0; t < R; ++t)
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) s[t][u] = product16(a, q[t][n][k], s[t][u]);
+            }
+        }
+        // values to this wave's rows, after the reads of the step before
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int r = 16 * u + col;
+                *(i32x4_c*)(mine + r * ROWB + ((quarter * KC + k) ^ value_turn<D>(r)) * 16) = vp[u].values(k);
+            }
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t held = (uint32_t)(__ballot(there[0]) & 0xFFFF) | (uint32_t)((__ballot(there[1]) & 0xFFFF) << 16);       // positions that hold something
+        bool partly = held != 0xFFFFFFFFu;
+        bool hidden = false;                             // a position that one row sees and another does not
+#pragma unroll
+        for (int t = 0; t < R; ++t) hidden |= lim[t] < min(k0 + 32, c1);
+        hidden = __any(hidden);
+        partly |= hidden;
+        if (partly) {
+#pragma unroll
+            for (int t = 0; t < R; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int j = 16 * u + 4 * quarter + r;
+                        if (k0 + j >= lim[t] || !((held >> j) & 1)) s[t][u][r] = -__builtin_inff();
+                    }
+        }
+        bool move = false;
+        float now[R];
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            float m = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+            m = max_of_quarters(m) * c;
+            now[t] = fmaxf(m, top[t]);
+            move |= m > top[t] + 8.0f;
+        }
+        if (__any(move)) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                const float f = now[t] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top[t] - now[t]);
+                top[t] = now[t];
+                sum[t] *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[t][d] *= f;
+            }
+        }
+        i32x4_c w[R][NP];
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+            const float base = top[t] == -__builtin_inff() ? 0.0f : -top[t];
+            bf16_t piece[8][NP];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[t][u][r] = __builtin_amdgcn_exp2f(fmaf(s[t][u][r], c, base));
+                    sum[t] += s[t][u][r];
+                    split<NP>(s[t][u][r], piece[4 * u + r]);
+                }
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[t][n][j] = __builtin_bit_cast(int32_t, bf16x2_c{piece[2 * j][n], piece[2 * j + 1][n]});
+        }
+        if (!(hidden && __any(vp[0].broken() || vp[1].broken()))) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                typedef __attribute__((address_space(3))) i16x4_c* lds_ptr;
+                union { i16x4_c h[2]; i32x4_c v; } x;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int r = 16 * u + 4 * quarter + col / 4;
+                    x.h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(mine + r * ROWB + ((2 * d + (col & 3) / 2) ^ value_turn<D>(r)) * 16 + (col & 1) * 8));
+                }
+#pragma unroll
+                for (int t = 0; t < R; ++t)
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
+            }
+        } else {                                         // a zero weight must not meet an infinity: position by position, where it is seen
+            for (int j = 0; j < 32; ++j) {
+                if (!((held >> j) & 1)) continue;
+#pragma unroll
+                for (int t = 0; t < R; ++t) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (16 * u + r == (j & ~12)) x = s[t][u][r];
+                    x = __shfl(x, col + 4 * (j & 12));
+                    if (k0 + j < lim[t]) {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int e = 16 * d + 4 * quarter + r;
+                                acc[t][d][r] = fmaf(x, load_one((const bf16_t*)(mine + j * ROWB + ((e / 8) ^ value_turn<D>(j)) * 16) + e % 8), acc[t][d][r]);
+                            }
+                    }
+                }
+            }
+        }
+    }
+
+    // the four waves' maxima, then their sums in one scale
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        sum[t] = sum_of_quarters(sum[t]);
+        if (quarter == 0) { ends[wave][0][16 * t + col] = top[t]; ends[wave][1][16 * t + col] = sum[t]; }
+    }
+    __syncthreads();
+    float* const sums = (float*)mine;
+#pragma unroll
+    for (int t = 0; t < R; ++t) {
+        float m = ends[0][0][16 * t + col];
+#pragma unroll
+        for (int x = 1; x < 4; ++x) m = fmaxf(m, ends[x][0][16 * t + col]);
+        const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[t] - m);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4_c*)&sums[(16 * t + col) * D + ((4 * d + quarter) ^ (col & 7)) * 4] = acc[t][d] * f;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * R * (D / 4); i += 256) {
+        const int r = i / (D / 4), piece = i % (D / 4), row = row0 + r;
+        if (row >= rows) continue;
+        float m = ends[0][0][r];
+#pragma unroll
+        for (int x = 1; x < 4; ++x) m = fmaxf(m, ends[x][0][r]);
+        f32x4_c v = {0.0f, 0.0f, 0.0f, 0.0f};
+        float l = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            v += *(const f32x4_c*)&((const float*)lds[x])[r * D + (piece ^ (r & 7)) * 4];
+            if (m != -__builtin_inff()) l = fmaf(ends[x][1][r], __builtin_amdgcn_exp2f(ends[x][0][r] - m), l);
+        }
+        const int64_t out = ((int64_t)b * p.fresh + row / p.group) * p.H + kv * p.group + row % p.group;
+        if (alone) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const float o[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+            if (p.o_type == LBA_F32) store_vec<4>((float*)p.O + out * D + piece * 4, o, p.fmt);
+            else if (p.o_type == LBA_BF16) store_vec<4>((bf16_t*)p.O + out * D + piece * 4, o, p.fmt);
+            else store_vec<4>((uint8_t*)p.O + out * D + piece * 4, o, p.fmt);
+        } else {
+            const int64_t to = out * p.chunks + blockIdx.x;
+            *(f32x4_c*)&p.part[to * D + piece * 4] = v;
+            if (piece == 0) {
+                float* e = p.part + (int64_t)p.c.count * p.fresh * p.H * p.chunks * D + to * 2;
+                e[0] = m;
+                e[1] = l;
+            }
+        }
+    }
+}
+
+template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st) {
+    const dim3 grid((unsigned)p.chunks, (unsigned)(p.c.KV * p.row_tiles), (unsigned)p.c.count);
+#define LBA_CACHE_ATTN(D_, R_) \
+    if (p.c.D == D_ && r == R_) { hipLaunchKernelGGL((cache_attn_kernel<T, D_, R_>), grid, dim3(256), 0, st, p); return; }
+    LBA_CACHE_ATTN(32, 1) LBA_CACHE_ATTN(64, 1) LBA_CACHE_ATTN(96, 1) LBA_CACHE_ATTN(128, 1)
+    LBA_CACHE_ATTN(32, 2) LBA_CACHE_ATTN(64, 2) LBA_CACHE_ATTN(96, 2) LBA_CACHE_ATTN(128, 2)
+#undef LBA_CACHE_ATTN
+}
+
+}  // namespace lba
+#endif

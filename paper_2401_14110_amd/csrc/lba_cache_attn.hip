@@ -1,68 +1,76 @@
-// lba_cache_attn.hip -- attention of new tokens over a cache of 4 bits an element: one wave to a token's query head.
-#include "lba_cache.h"
+// lba_cache_attn.hip -- attention over the cache: how it is cut, the join of the chunks, entry points.
+#include "lba_cache_attn.h"
 
 namespace lba {
 
-struct CacheAttnParams {
-    CacheParams c;
-    const void* Q;
-    void* O;
-    CodeFmt fmt;
-    lba_strides q;
-    int32_t fresh, H, group;
-    float scale;
-};
+template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st);
 
-__device__ __forceinline__ float cache_value(const CacheParams& c, const uint8_t* codes, const uint8_t* scales, int64_t line, int d) {
-    return four_value(codes[line * (c.D / 2) + d / 2] >> (d % 2 * 4)) * power_of(scales[line * (c.D / 32) + d / 32]);
+// Row `out` of O from its chunks: a workgroup a row, a group of lanes for every piece of four elements, chunks in turn over the groups.
+template <typename TO> __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int rows_of_tile) {
+    __shared__ float weight[256];
+    __shared__ f32x4_c sums[256];
+    __shared__ float parts[4];
+    const int64_t out = blockIdx.x;
+    const int D = p.c.D, h = (int)(out % p.H);
+    const int64_t token = out / p.H;
+    const int b = (int)(token / p.fresh), r = (int)(token % p.fresh) * p.group + h % p.group, rows = p.fresh * p.group;
+    const int seen = row_seen(p, b, min(r / rows_of_tile * rows_of_tile + rows_of_tile, rows) - 1);
+    const int n = (seen + p.chunk - 1) / p.chunk;
+    if (n <= 1) return;                                  // stored by its only workgroup
+    const float* part = p.part + out * p.chunks * D;
+    const float* end = p.part + (int64_t)p.c.count * p.fresh * p.H * p.chunks * D + out * p.chunks * 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    float m = -__builtin_inff();
+    for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, end[2 * i]);
+#pragma unroll
+    for (int x = 32; x; x /= 2) m = fmaxf(m, __shfl_xor(m, x));
+    if (lane == 0) parts[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3]));
+    const int pieces = D / 4, groups = 256 / pieces, g = (int)threadIdx.x / pieces, piece = (int)threadIdx.x % pieces;
+    f32x4_c v = {0.0f, 0.0f, 0.0f, 0.0f};
+    float l = 0.0f;
+    for (int i0 = 0; i0 < n; i0 += 256) {
+        __syncthreads();
+        const int i = i0 + (int)threadIdx.x;
+        const float w = i < n && m != -__builtin_inff() ? __builtin_amdgcn_exp2f(end[2 * i] - m) : 0.0f;
+        weight[threadIdx.x] = w;
+        if (i < n) l = fmaf(w, end[2 * i + 1], l);
+        __syncthreads();
+        if (g < groups)
+            for (int k = g; k < 256 && i0 + k < n; k += groups) v += weight[k] * *(const f32x4_c*)&part[(int64_t)(i0 + k) * D + piece * 4];
+    }
+    l = wave_sum(l);
+    __syncthreads();
+    if (lane == 0) parts[wave] = l;
+    sums[threadIdx.x] = v;
+    __syncthreads();
+    if (g != 0) return;
+    l = (parts[0] + parts[1]) + (parts[2] + parts[3]);
+    for (int x = 1; x < groups; ++x) v += sums[x * pieces + piece];
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float o[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+    store_vec<4>((TO*)p.O + out * D + piece * 4, o, p.fmt);
 }
 
-template <typename T, typename TO>
-__global__ __launch_bounds__(64) void cache_attn_plain_kernel(CacheAttnParams p) {
-    __shared__ float q[128], w[64];
-    const int lane = threadIdx.x, D = p.c.D;
-    const int64_t total = (int64_t)p.c.count * p.fresh * p.H;
-    for (int64_t i = blockIdx.x; i < total; i += gridDim.x) {
-        const int h = (int)(i % p.H), kv = h / p.group;
-        const int64_t t = i / p.H;
-        const int b = (int)(t / p.fresh);
-        const int64_t seen = min((int64_t)p.c.lens[b] - p.fresh + t % p.fresh + 1, p.c.table_row * p.c.page);
-        TO* o = (TO*)p.O + i * D;
-        __syncthreads();
-        for (int d = lane; d < D; d += 64) q[d] = load_one((const T*)p.Q + t * p.q.row + (int64_t)h * p.q.head + d);
-        float m = -__builtin_inff(), l = 0.0f, acc0 = 0.0f, acc1 = 0.0f;
-        for (int64_t j0 = 0; j0 < seen; j0 += 64) {
-            __syncthreads();
-            float s = -__builtin_inff();
-            const int64_t mine = j0 + lane < seen ? line_of(p.c, b, j0 + lane, kv) : -1;
-            if (mine >= 0) {
-                s = 0.0f;
-                for (int d = 0; d < D; ++d) s = fmaf(q[d], cache_value(p.c, p.c.k, p.c.k_scale, mine, d), s);
-                s *= p.scale;
-            }
-            float top = s;
-            for (int x = 32; x; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
-            top = fmaxf(top, m);
-            const float base = top == -__builtin_inff() ? 0.0f : top;
-            const float e = mine >= 0 ? exp_near(s - base) : 0.0f, f = exp_near(m - base);
-            m = top;
-            l = l * f + wave_sum(e);
-            w[lane] = e;
-            __syncthreads();
-            acc0 *= f; acc1 *= f;
-            const int n = (int)min((int64_t)64, seen - j0);
-            for (int j = 0; j < n; ++j) {
-                const int64_t line = line_of(p.c, b, j0 + j, kv);
-                if (line < 0) continue;
-                if (lane < D) acc0 = fmaf(w[j], cache_value(p.c, p.c.v, p.c.v_scale, line, lane), acc0);
-                if (lane + 64 < D) acc1 = fmaf(w[j], cache_value(p.c, p.c.v, p.c.v_scale, line, lane + 64), acc1);
-            }
-        }
-        const bool some = l > 0.0f || l != l;
-        const float inv = some ? 1.0f / l : 0.0f;
-        if (lane < D) store_one(o + lane, some ? acc0 * inv : 0.0f, p.fmt);
-        if (lane + 64 < D) store_one(o + lane + 64, some ? acc1 * inv : 0.0f, p.fmt);
-    }
+// How the rows and positions are cut: rows of a tile, and a chunk's positions, so many that there are about 2048 workgroups where every
+// sequence fills its table (four on every CU twice), and 256 at least (two steps of each wave).
+struct CachePlan {
+    int32_t r, row_tiles;
+    int64_t chunk, chunks, rows;
+};
+static int cache_plan(int64_t count, int64_t table_row, int64_t page, int64_t fresh, int64_t H, int64_t KV, CachePlan* c) {
+    const int64_t room = table_row * page, rows = fresh * (H / KV);
+    c->r = rows > 16 ? 2 : 1;
+    const int64_t row_tiles = (rows + 16 * c->r - 1) / (16 * c->r), units = count * KV * row_tiles;
+    if (room > (1 << 30) || KV * row_tiles > 65535 || count > 65535) return LBA_ERR_SHAPE;
+    c->row_tiles = (int32_t)row_tiles;
+    c->chunk = (room * units + 2047) / 2048;
+    c->chunk = (c->chunk + 127) / 128 * 128;
+    if (c->chunk < 256) c->chunk = 256;
+    c->chunks = room > c->chunk ? (room + c->chunk - 1) / c->chunk : 1;
+    c->rows = count * fresh * H;
+    return c->chunks * units < (1 << 24) && c->rows < (1 << 24) ? LBA_OK : LBA_ERR_SHAPE;
 }
 
 }  // namespace lba
@@ -72,8 +80,11 @@ using namespace lba;
 extern "C" {
 
 size_t lba_cache_attention_workspace_bytes(int64_t count, int64_t table_row, int32_t page, int64_t fresh, int64_t H, int32_t KV, int32_t D) {
-    (void)count; (void)table_row; (void)page; (void)fresh; (void)H; (void)KV; (void)D;
-    return 0;
+    CachePlan c;
+    if (count < 1 || table_row < 0 || page < 1 || fresh < 1 || H < 1 || KV < 1 || H % KV != 0 || count > (1 << 20) || table_row > 2147483647LL || page > 65536 ||
+        fresh > 2147483647LL / (count * H) || cache_plan(count, table_row, page, fresh, H, KV, &c) != LBA_OK || c.chunks == 1)
+        return 0;
+    return align256((size_t)c.rows * (size_t)c.chunks * (size_t)(D + 2) * sizeof(float));
 }
 
 int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t type, int64_t fresh, int64_t H, float scale, void* O, int32_t o_type,
@@ -89,6 +100,8 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     if (c.count == 0 || fresh == 0 || H == 0) return LBA_OK;
     const bool lines = c.table_row > 0 && c.pages > 0;
     if (!Q || !O || !c.lens || (c.table_row > 0 && !c.table) || (lines && (!c.k || !c.k_scale || !c.v || !c.v_scale))) return LBA_ERR_NULL;
+    CachePlan plan;
+    if (cache_plan(c.count, c.table_row, c.page, fresh, H, c.KV, &plan) != LBA_OK) return LBA_ERR_SHAPE;
     const size_t need = lba_cache_attention_workspace_bytes(c.count, c.table_row, c.page, fresh, H, c.KV, c.D);
     if (need > 0) {
         if (!workspace) return LBA_ERR_NULL;
@@ -97,17 +110,17 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     }
     p.Q = Q; p.O = O; p.q = q_at; p.fresh = (int32_t)fresh; p.H = (int32_t)H; p.group = (int32_t)(H / c.KV); p.scale = scale;
     if (o_type == LBA_CODE8) p.fmt = make_code_fmt(o_fmt);
-    const int64_t rows = c.count * fresh * H;
-    const dim3 grid((unsigned)(rows < (1 << 20) ? rows : (1 << 20)));
+    p.o_type = o_type; p.part = (float*)workspace; p.room = (int32_t)(c.table_row * c.page);
+    if (!lines) p.room = 0;                              // nothing is held anywhere
+    p.chunk = (int32_t)plan.chunk; p.chunks = (int32_t)plan.chunks; p.row_tiles = plan.row_tiles;
     const hipStream_t st = (hipStream_t)hip_stream;
-#define LBA_CACHE_ATTN(T) \
-    do { \
-        if (o_type == LBA_F32) hipLaunchKernelGGL((cache_attn_plain_kernel<T, float>), grid, dim3(64), 0, st, p); \
-        else if (o_type == LBA_BF16) hipLaunchKernelGGL((cache_attn_plain_kernel<T, bf16_t>), grid, dim3(64), 0, st, p); \
-        else hipLaunchKernelGGL((cache_attn_plain_kernel<T, uint8_t>), grid, dim3(64), 0, st, p); \
-    } while (0)
-    if (type == LBA_F32) LBA_CACHE_ATTN(float); else LBA_CACHE_ATTN(bf16_t);
-#undef LBA_CACHE_ATTN
+    if (type == LBA_F32) launch_cache_attn<float>(p, plan.r, st); else launch_cache_attn<bf16_t>(p, plan.r, st);
+    if (plan.chunks > 1) {
+        const dim3 grid((unsigned)plan.rows);
+        if (o_type == LBA_F32) hipLaunchKernelGGL((cache_join_kernel<float>), grid, dim3(256), 0, st, p, 16 * plan.r);
+        else if (o_type == LBA_BF16) hipLaunchKernelGGL((cache_join_kernel<bf16_t>), grid, dim3(256), 0, st, p, 16 * plan.r);
+        else hipLaunchKernelGGL((cache_join_kernel<uint8_t>), grid, dim3(256), 0, st, p, 16 * plan.r);
+    }
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 

@@ -1,0 +1,6 @@
+// lba_cache_attn_f32.hip -- attention over the cache with float32 queries
+#include "lba_cache_attn.h"
+
+namespace lba {
+template void launch_cache_attn<float>(const CacheAttnParams& p, int r, hipStream_t st);
+}
