@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     load_frags<T, DP>((const T*)p.O + row * p.D, there, p.D, half, q);
 #pragma unroll
     for (int k = 0; k < KC; ++k) delta += dot(g[k], q[k]);
-    delta += other_half(delta);
+    delta = sum_of_halves(delta);
     if (there && half == 0) p.delta[row] = delta;
     const float base = there ? -p.lse[row] * kLog2e : 0.0f;
     load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, there, p.D, half, q);

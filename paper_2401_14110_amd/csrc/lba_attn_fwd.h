@@ -62,7 +62,9 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
     float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
-    for (int kt = 0; kt < tiles; ++kt) {
+    // One tile.  EDGE: some query may not see all of it; the tiles before are seen whole by every query of the workgroup.
+    auto step = [&](int kt, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value != 0;
         const int k0 = kt * KT;
         uint8_t* const tk = lds[kt & 1][0];
         uint8_t* const tv = lds[kt & 1][1];
@@ -75,16 +77,19 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
             lk.load(lds[(kt + 1) & 1][0], rk.n - k0 - KT);
             lv.load(lds[(kt + 1) & 1][1], rk.n - k0 - KT);
         }
-        const bool broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv);
-        if (k0 >= most) continue;                        // (the barriers above are everybody's)
+        bool broken = false;
+        if constexpr (EDGE) {
+            broken = p.causal && tile_is_broken<T, DP, KT>(tv);
+            if (k0 >= most) return;                      // (the barriers above are everybody's)
+        }
         f32x16 s[KB];
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            s[b] = f32x16{};
+        for (int b = 0; b < KB; ++b) s[b] = f32x16{};
 #pragma unroll
-            for (int k = 0; k < KC; ++k) s[b] = product(row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half), q[k], s[b]);
-        }
-        if (k0 + KT > least) {
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) s[b] = product(row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half), q[k], s[b]);
+        if (EDGE && k0 + KT > least) {
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -96,7 +101,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-        mx = fmaxf(mx, other_half(mx)) * c;
+        mx = max_of_halves(mx) * c;
         if (__any(mx > top + 8.0f)) {
             const float now = fmaxf(mx, top);
             const float f = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - now);
@@ -113,16 +118,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
                 s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
                 sum += s[b][r];
             }
-        if (!broken) {
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const Frag<T> w = as_frag<T>(s[b], k);
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
-                }
-        } else {                                         // a zero weight must not meet an infinity: key by key, where it is seen
+        if (EDGE && broken) {                            // a zero weight must not meet an infinity: key by key, where it is seen
             for (int j = 0; j < KT && k0 + j < rk.n; ++j) {
                 float w = 0.0f;
 #pragma unroll
@@ -138,9 +134,21 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
                         for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(w, tile_at<T, DP>(tv, j, 32 * t + row_of(r) + 4 * half), acc[t][r]);
                 }
             }
+            return;
         }
-    }
-    sum += other_half(sum);
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Frag<T> w = as_frag<T>(s[b], k);
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
+            }
+    };
+    const int whole = min(tiles, least_all / KT);
+    for (int kt = 0; kt < whole; ++kt) step(kt, Known<0>{});
+    for (int kt = whole; kt < tiles; ++kt) step(kt, Known<1>{});
+    sum = sum_of_halves(sum);
     if (i >= rq.n) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;

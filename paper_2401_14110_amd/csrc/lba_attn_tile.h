@@ -212,8 +212,16 @@ template <typename T, int DP> __device__ __forceinline__ void load_frags(const v
     }
 }
 
-// the larger of a value's copies in lanes l and l ^ 32, and their sum
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// the larger of a value's copies in lanes l and l ^ 32, and their sum: of the exchange's two results one is the wave's lower half twice, the other its
+// upper half
+__device__ __forceinline__ float max_of_halves(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
 
 // ---- rows of no sequence ----------------------------------------------------------------------
 
