@@ -29,9 +29,9 @@ constexpr int kTileRows = 128;                           // queries (keys, where
 constexpr int kClearBlocks = 16;                         // workgroups behind the others, for rows of no sequence
 constexpr int64_t kMostUnits = 1 << 23;                  // workgroups of a launch: fewer than 2^32 lanes
 
-// Whether rows can go to LDS in pieces of 16 aligned bytes: one more head or row keeps the place in a piece.
+// Whether rows can go to LDS in pieces of 16 aligned bytes (one more head or row keeps the place in a piece), 64 rows within 2^31 bytes.
 inline bool whole_pieces(const void* x, const lba_strides& at, int64_t D, int64_t size) {
-    return ((uintptr_t)x | (uintptr_t)(at.row * size) | (uintptr_t)(at.head * size) | (uintptr_t)(D * size)) % 16 == 0;
+    return ((uintptr_t)x | (uintptr_t)(at.row * size) | (uintptr_t)(at.head * size) | (uintptr_t)(D * size)) % 16 == 0 && at.row < (1 << 22);
 }
 
 template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipStream_t st);

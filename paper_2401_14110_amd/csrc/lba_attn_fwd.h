@@ -63,32 +63,44 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
     float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
     // One tile.  EDGE: some query may not see all of it; the tiles before are seen whole by every query of the workgroup.
-    auto step = [&](int kt, auto edge) {
+    auto step = [&](int kt, auto edge, auto buffer) {
         constexpr bool EDGE = decltype(edge)::value != 0;
+        constexpr int BUF = decltype(buffer)::value;
         const int k0 = kt * KT;
-        uint8_t* const tk = lds[kt & 1][0];
-        uint8_t* const tv = lds[kt & 1][1];
+        uint8_t* const tk = lds[BUF][0];
+        uint8_t* const tv = lds[BUF][1];
         lk.put(tk);
         lv.put(tv);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();                    // this tile is there, and the one before it has been read
         asm volatile("" ::: "memory");
         if (kt + 1 < tiles) {
-            lk.load(lds[(kt + 1) & 1][0], rk.n - k0 - KT);
-            lv.load(lds[(kt + 1) & 1][1], rk.n - k0 - KT);
+            lk.load(lds[BUF ^ 1][0], rk.n - k0 - KT);
+            lv.load(lds[BUF ^ 1][1], rk.n - k0 - KT);
         }
         bool broken = false;
         if constexpr (EDGE) {
-            broken = p.causal && tile_is_broken<T, DP, KT>(tv);
+            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv);
             if (k0 >= most) return;                      // (the barriers above are everybody's)
         }
         f32x16 s[KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) s[b] = f32x16{};
+        Frag<T> f[3][KB];                                // two steps' rows are on their way while the third's are multiplied
+        auto fetch = [&](int k) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
+            for (int b = 0; b < KB; ++b) f[k % 3][b] = row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half);
+        };
+        fetch(0);
+        if (KC > 1) fetch(1);
 #pragma unroll
-            for (int b = 0; b < KB; ++b) s[b] = product(row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half), q[k], s[b]);
+        for (int k = 0; k < KC; ++k) {
+            if (k + 2 < KC) fetch(k + 2);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < KB; ++b) s[b] = product(f[k % 3][b], q[k], s[b]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if (EDGE && k0 + KT > least) {
 #pragma unroll
             for (int b = 0; b < KB; ++b)
@@ -146,8 +158,15 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
             }
     };
     const int whole = min(tiles, least_all / KT);
-    for (int kt = 0; kt < whole; ++kt) step(kt, Known<0>{});
-    for (int kt = whole; kt < tiles; ++kt) step(kt, Known<1>{});
+    int kt = 0;
+    for (; kt + 1 < whole; kt += 2) {
+        step(kt, Known<0>{}, Known<0>{});
+        step(kt + 1, Known<0>{}, Known<1>{});
+    }
+    for (; kt < tiles; kt += 2) {
+        step(kt, Known<1>{}, Known<0>{});
+        if (kt + 1 < tiles) step(kt + 1, Known<1>{}, Known<1>{});
+    }
     sum = sum_of_halves(sum);
     if (i >= rq.n) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;

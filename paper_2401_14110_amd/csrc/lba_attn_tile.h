@@ -10,6 +10,8 @@
 #ifndef LBA_ATTN_TILE_H_
 #define LBA_ATTN_TILE_H_
 
+#include <type_traits>
+
 #include "lba_attn.h"
 
 namespace lba {
@@ -130,8 +132,9 @@ template <typename T, int DP> __device__ __forceinline__ float tile_at(const uin
     return load_one((const T*)(tile + row * (C * 16) + ((d / V) ^ turn<C>(row)) * 16) + d % V);
 }
 
-// Rows of a head on their way to a tile of ROWS rows.  DIRECT: rows are whole pieces of 16 aligned bytes and go from memory to LDS without
-// registers in between; else a lane holds them until they are put down.  What is behind `rows` rows or D elements is zeros.
+// Rows of a head on their way to a tile of ROWS rows.  DIRECT: rows are whole pieces of 16 aligned bytes, a tile's rows within 2^31 bytes, and go
+// from memory to LDS without registers in between; else a lane holds them until they are put down.  What is behind `rows` rows or D elements
+// is zeros.
 template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
     static constexpr int C = DP * sizeof(T) / 16, V = 16 / sizeof(T), N = ROWS * C / 256;
     static_assert(ROWS * C % 256 == 0, "whole pieces a lane");
@@ -139,36 +142,51 @@ template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
     static constexpr bool EVEN = 4096 % (C * 256) == 0 && C <= 16;
     static constexpr int P = EVEN ? 1 : N;
     typedef typename Bits<T>::type B;
-    const B* at[P];          // this lane's pieces in the first tile
+    const B* base;           // the next tile
     int64_t stride;
+    typename std::conditional<DIRECT, uint32_t, int64_t>::type at[P];                // this lane's pieces in a tile: bytes, or elements, from its start
     int left[P];             // how many elements of the row are from there on
+    bool full;               // rows have no pieces of zeros
     Raw<B, V> held[DIRECT ? 1 : N];
 
-    __device__ __forceinline__ void start(const void* base, int64_t row_stride, int D) {
+    __device__ __forceinline__ void start(const void* rows, int64_t row_stride, int D) {
+        base = (const B*)rows;
         stride = row_stride;
+        full = D == DP;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int p = threadIdx.x + 256 * i, r = p / C, c = (p % C) ^ turn<C>(r);
             left[i] = D - c * V;
-            at[i] = (const B*)base + (int64_t)r * row_stride + c * V;
+            at[i] = (r * row_stride + c * V) * (DIRECT ? (int)sizeof(T) : 1);
         }
     }
     // the next tile, of which `rows` rows are there
     __device__ __forceinline__ void load(uint8_t* tile, int rows) {
+        if constexpr (DIRECT) {
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+            auto to_lds = [&](int i, const void* src) {
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
+                                                 (__attribute__((address_space(3))) uint32_t*)(tile + (256 * i + 64 * wave) * 16), 16, 0, 0);
+            };
+            if (full && rows >= ROWS) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const B* src = EVEN ? at[0] + i * (256 / C) * stride : at[i];
-            const int more = left[EVEN ? 0 : i];
-            const bool in = ((int)threadIdx.x + 256 * i) / C < rows && more > 0;
-            if constexpr (DIRECT) {
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(in ? (const void*)src : (const void*)attn_zeros),
-                                                 (__attribute__((address_space(3))) uint32_t*)(tile + (256 * i + (threadIdx.x & 192)) * 16), 16, 0, 0);
+                for (int i = 0; i < N; ++i) to_lds(i, (const char*)(EVEN ? base + i * (256 / C) * stride : base) + at[EVEN ? 0 : i]);
             } else {
-                held[i] = load_raw<B, V>(src, in ? more : 0);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const bool in = ((int)threadIdx.x + 256 * i) / C < rows && left[EVEN ? 0 : i] > 0;
+                    const char* src = (const char*)(EVEN ? base + i * (256 / C) * stride : base) + at[EVEN ? 0 : i];
+                    to_lds(i, in ? (const void*)src : (const void*)attn_zeros);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool in = ((int)threadIdx.x + 256 * i) / C < rows;
+                held[i] = load_raw<B, V>((EVEN ? base + i * (256 / C) * stride : base) + at[EVEN ? 0 : i], in ? left[EVEN ? 0 : i] : 0);
             }
         }
-#pragma unroll
-        for (int i = 0; i < P; ++i) at[i] += stride * ROWS;
+        base += stride * ROWS;
     }
     __device__ __forceinline__ void put(uint8_t* tile) const {
         if constexpr (!DIRECT) {
