@@ -27,20 +27,18 @@ template <typename T, int DT> __device__ __forceinline__ void store_columns(T* r
         }
 }
 
-// acc += w * (row j of the tile), the columns of this lane's registers: for tiles that hold infinities
-template <typename T, int DP, int DT> __device__ __forceinline__ void add_row(f32x16 (&acc)[DT], float w, const uint8_t* tile, int j, int half) {
+// The order of what has been written since the last barrier of the scheduler: after each of N products some of what does not belong to the
+// matrix cores, VALU instructions and reads from LDS.
+template <typename T, int N, int VALU, int READS> __device__ __forceinline__ void interleave(bool valu) {
+    if constexpr (sizeof(T) == 2) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(w, tile_at<T, DP>(tile, j, 32 * t + row_of(r) + 4 * half), acc[t][r]);
-}
-// the value that row j of a block of 32 has in this lane's column
-__device__ __forceinline__ float value_of_row(const f32x16& s, int j, int lane) {
-    float w = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-        if (row_of(r) == (j & ~4)) w = s[r];
-    return __shfl(w, (lane & 31) + 8 * (j & 4));
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            if (valu) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        }
+    }
 }
 
 template <typename T, int DP, bool DIRECT>
@@ -89,53 +87,120 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     f32x16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
-    for (int kt = 0; kt < tiles; ++kt) {
+    auto step = [&](int kt, auto edge, auto buffer) {
+        constexpr bool EDGE = decltype(edge)::value != 0;
+        constexpr int BUF = decltype(buffer)::value;
         const int k0 = kt * KT;
-        uint8_t* const tk = lds[kt & 1][0];
-        uint8_t* const tv = lds[kt & 1][1];
+        uint8_t* const tk = lds[BUF][0];
+        uint8_t* const tv = lds[BUF][1];
         lk.put(tk);
         lv.put(tv);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (kt + 1 < tiles) {
-            lk.load(lds[(kt + 1) & 1][0], rk.n - k0 - KT);
-            lv.load(lds[(kt + 1) & 1][1], rk.n - k0 - KT);
+            lk.load(lds[BUF ^ 1][0], rk.n - k0 - KT);
+            lv.load(lds[BUF ^ 1][1], rk.n - k0 - KT);
         }
-        const bool broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tk);
-        if (k0 >= most) continue;
-        const bool masked = k0 + KT > least;
+        bool broken = false;
+        if constexpr (EDGE) {
+            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tk);
+            if (k0 >= most) return;
+        }
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             f32x16 s = {}, u = {};
+            Frag<T> ring[2][2];
+            auto fetch = [&](int x) {
+                ring[x % 2][0] = row_frag<T, DP>(tk, 32 * b + (lane & 31), x, half);
+                ring[x % 2][1] = row_frag<T, DP>(tv, 32 * b + (lane & 31), x, half);
+            };
+            fetch(0);
 #pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                s = product(row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half), q[k], s);
-                u = product(row_frag<T, DP>(tv, 32 * b + (lane & 31), k, half), g[k], u);
+            for (int x = 0; x < KC; ++x) {
+                if (x + 1 < KC) fetch(x + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                s = product(ring[x % 2][0], q[x], s);
+                u = product(ring[x % 2][1], g[x], u);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, base)) * (u[r] - delta);
-            if (masked) {
+            if (EDGE && k0 + KT > least) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (k0 + 32 * b + row_of(r) + 4 * half >= lim) s[r] = 0.0f;
             }
-            if (!broken) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const Frag<T> w = as_frag<T>(s, k);
+            for (int x = 0; x < 2; ++x) {
+                const Frag<T> w = as_frag<T>(s, x);
+                // a hidden key's infinity must not meet a zero; one that is seen has made the weight itself NaN
 #pragma unroll
-                    for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tk, 32 * b + 16 * k, t, lane), w, acc[t]);
-                }
-            } else {                                     // a hidden key's infinity must not meet a zero: key by key, where it is seen
-                for (int j = 0; j < 32 && k0 + 32 * b + j < rk.n; ++j) {
-                    const float w = value_of_row(s, j, lane);
-                    if (k0 + 32 * b + j < lim) add_row<T, DP>(acc, w, tk, 32 * b + j, half);
+                for (int t = 0; t < DT; ++t) {
+                    const Frag<T> a = column_frag<T, DP>(tk, 32 * b + 16 * x, t, lane);
+                    acc[t] = product(EDGE && broken ? without_broken(a) : a, w, acc[t]);
                 }
             }
         }
+    };
+    const int whole = min(tiles, least_all / KT);
+    int kt = 0;
+    for (; kt + 1 < whole; kt += 2) {
+        step(kt, Known<0>{}, Known<0>{});
+        step(kt + 1, Known<0>{}, Known<1>{});
+    }
+    for (; kt < tiles; kt += 2) {
+        step(kt, Known<1>{}, Known<0>{});
+        if (kt + 1 < tiles) step(kt + 1, Known<1>{}, Known<1>{});
     }
     if (there) store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, p.scale, p.D, half);
+}
+
+// One key by one wave, over the queries of its sequence from `first` on: a lane a query, then a lane two columns.  words: 384 of LDS.
+template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& p, float* words, int kv, int t, Rows rq, int first) {
+    const int lane = threadIdx.x & 63;
+    const CodeFmt none = {};
+    float *const v = words + 128, *const wp = words + 256, *const ws = words + 320;
+    wave_words_done();
+    for (int d = lane; d < 128; d += 64) {
+        words[d] = d < p.D ? load_one((const T*)p.K + (int64_t)t * p.k.row + (int64_t)kv * p.k.head + d) : 0.0f;
+        v[d] = d < p.D ? load_one((const T*)p.V + (int64_t)t * p.v.row + (int64_t)kv * p.v.head + d) : 0.0f;
+    }
+    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
+    for (int h = kv * p.group; h < (kv + 1) * p.group; ++h)
+        for (int i0 = first; i0 < rq.n; i0 += 64) {
+            wave_words_done();
+            float e = 0.0f, f = 0.0f;
+            if (i0 + lane < rq.n) {
+                const int64_t at = rq.first + i0 + lane, row = at * p.H + h;
+                const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
+                const T* g = (const T*)p.G + row * p.D;
+                float s = 0.0f, u = 0.0f;
+                for (int d = 0; d < p.D; ++d) { s = fmaf(words[d], load_one(q + d), s); u = fmaf(v[d], load_one(g + d), u); }
+                e = exp_near(s * p.scale - p.lse[row]);
+                f = e * (u - p.delta[row]);
+            }
+            wp[lane] = e;
+            ws[lane] = f;
+            wave_words_done();
+            for (int j = 0; j < 64 && i0 + j < rq.n; ++j) {
+                const int64_t at = rq.first + i0 + j;
+                const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
+                const T* g = (const T*)p.G + (at * p.H + h) * p.D;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (lane + 64 * x < p.D) {
+                        dk[x] = fmaf(ws[j], load_one(q + lane + 64 * x), dk[x]);
+                        dv[x] = fmaf(wp[j], load_one(g + lane + 64 * x), dv[x]);
+                    }
+            }
+        }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 64 * x < p.D) {
+            store_one((T*)p.dK + (int64_t)t * p.dk.row + (int64_t)kv * p.dk.head + lane + 64 * x, dk[x] * p.scale, none);
+            store_one((T*)p.dV + (int64_t)t * p.dv.row + (int64_t)kv * p.dv.head + lane + 64 * x, dv[x], none);
+        }
 }
 
 template <typename T, int DP, bool DIRECT>
@@ -161,7 +226,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     const bool there = j < rk.n;
     const int lo = first_of(j), lo_wave = first_of(j0), lo_last = first_of(j0 + 31), lo_all = first_of(at.t * kTileRows);
     const int t0 = lo_all / QT, steps_head = rq.n > lo_all ? (rq.n + QT - 1) / QT - t0 : 0, steps = steps_head * p.group;
-    const int masked_all = p.causal ? first_of(at.t * kTileRows + kTileRows - 1) : 0;            // from this query on, all of the workgroup's keys are seen
+    const int masked_all = first_of(at.t * kTileRows + kTileRows - 1);                           // from this query on, all of the workgroup's keys are seen
 
     Loader<T, DP, QT, DIRECT> lq, lg;
     float side_next = 0.0f;                              // lane t of the first two waves: query t % QT of the step's lse or sum
@@ -191,69 +256,100 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) { dk[t] = f32x16{}; dv[t] = f32x16{}; }
+    auto steps_whole = [&](int n) { return (t0 + n % steps_head) * QT >= masked_all; };              // all the workgroup's keys are seen by the step's queries
     int tile = 0;
-    for (int step = 0; step < steps; ++step) {
+    bool broken = false;                                 // a tile that some key sees in part holds infinities or NaN
+    // One tile of queries.  EDGE: some key may not be seen by all of them.  The products of one block of 32 queries run while the weights of the
+    // other are worked out: a wave is alone on its SIMD, and its own instructions are all there is to fill it.
+    auto step = [&](int n, auto edge, auto buffer) {
+        constexpr bool EDGE = decltype(edge)::value != 0;
+        constexpr int BUF = decltype(buffer)::value;
         const int q0 = (t0 + tile) * QT;
         if (++tile == steps_head) tile = 0;
-        uint8_t* const tq = lds[step & 1][0];
-        uint8_t* const tg = lds[step & 1][1];
+        uint8_t* const tq = lds[BUF][0];
+        uint8_t* const tg = lds[BUF][1];
         lq.put(tq);
         lg.put(tg);
-        if (threadIdx.x < 2 * QT) side[step & 1][threadIdx.x / QT][threadIdx.x % QT] = side_next;
+        if (threadIdx.x < 2 * QT) side[BUF][threadIdx.x / QT][threadIdx.x % QT] = side_next;
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (step + 1 < steps) load((step + 1) & 1);
-        bool broken = p.causal && q0 < masked_all;
-        if (broken) {
-            const bool a = tile_is_broken<T, DP, QT>(tq);
-            broken = tile_is_broken<T, DP, QT>(tg) || a;
-        }
-        if (q0 + QT <= lo_wave) continue;
-        const bool masked = q0 < lo_last;
-#pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            f32x16 s = {}, u = {};
-#pragma unroll
-            for (int x = 0; x < KC; ++x) {
-                s = product(row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half), k[x], s);
-                u = product(row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half), v[x], u);
+        if (n + 1 < steps) load(BUF ^ 1);
+        if constexpr (EDGE) {
+            if (p.causal && q0 < masked_all) {
+                const bool a = tile_is_broken<T, DP, QT>(tq);
+                if (tile_is_broken<T, DP, QT>(tg) || a) { broken = true; return; }
             }
+            if (q0 + QT <= lo_wave) return;
+        }
+        f32x16 s[QB], u[QB];
+        Frag<T> w[QB][2], f[QB][2];
+        Frag<T> ring[3][2];
+        auto fetch = [&](int b, int x) {
+            ring[x % 3][0] = row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half);
+            ring[x % 3][1] = row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half);
+        };
+        auto weights = [&](int b) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const f32x4_t base = *(const f32x4_t*)&side[step & 1][0][32 * b + 8 * x + 4 * half];
-                const f32x4_t delta = *(const f32x4_t*)&side[step & 1][1][32 * b + 8 * x + 4 * half];
+                const f32x4_t base = *(const f32x4_t*)&side[BUF][0][32 * b + 8 * x + 4 * half];
+                const f32x4_t delta = *(const f32x4_t*)&side[BUF][1][32 * b + 8 * x + 4 * half];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    s[4 * x + y] = __builtin_amdgcn_exp2f(fmaf(s[4 * x + y], c, base[y]));
-                    u[4 * x + y] = s[4 * x + y] * (u[4 * x + y] - delta[y]);
+                    s[b][4 * x + y] = __builtin_amdgcn_exp2f(fmaf(s[b][4 * x + y], c, base[y]));
+                    u[b][4 * x + y] = s[b][4 * x + y] * (u[b][4 * x + y] - delta[y]);
                 }
             }
-            if (masked) {
+            if (EDGE && q0 < lo_last) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (q0 + 32 * b + row_of(r) + 4 * half < lo) s[r] = u[r] = 0.0f;
+                    if (q0 + 32 * b + row_of(r) + 4 * half < lo) s[b][r] = u[b][r] = 0.0f;
             }
-            if (!broken) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const Frag<T> w = as_frag<T>(s, x), f = as_frag<T>(u, x);
+            for (int x = 0; x < 2; ++x) { w[b][x] = as_frag<T>(s[b], x); f[b][x] = as_frag<T>(u[b], x); }
+        };
 #pragma unroll
-                    for (int t = 0; t < DT; ++t) {
-                        dv[t] = product(column_frag<T, DP>(tg, 32 * b + 16 * x, t, lane), w, dv[t]);
-                        dk[t] = product(column_frag<T, DP>(tq, 32 * b + 16 * x, t, lane), f, dk[t]);
-                    }
-                }
-            } else {
-                for (int i = 0; i < 32 && q0 + 32 * b + i < rq.n; ++i) {
-                    const float w = value_of_row(s, i, lane), f = value_of_row(u, i, lane);
-                    if (q0 + 32 * b + i >= lo) {
-                        add_row<T, DP>(dv, w, tg, 32 * b + i, half);
-                        add_row<T, DP>(dk, f, tq, 32 * b + i, half);
-                    }
-                }
+        for (int b = 0; b < QB; ++b) {
+            s[b] = u[b] = f32x16{};
+            fetch(b, 0);
+            if (KC > 1) fetch(b, 1);
+            if (b > 0) weights(b - 1);
+#pragma unroll
+            for (int x = 0; x < KC; ++x) {
+                if (x + 2 < KC) fetch(b, x + 2);
+                s[b] = product(ring[x % 3][0], k[x], s[b]);
+                u[b] = product(ring[x % 3][1], v[x], u[b]);
             }
+            interleave<T, 2 * KC, 6, 2>(b > 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (QB == 1) weights(0);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            if (QB > 1 && b == 0) weights(QB - 1);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    dv[t] = product(column_frag<T, DP>(tg, 32 * b + 16 * x, t, lane), w[b][x], dv[t]);
+                    dk[t] = product(column_frag<T, DP>(tq, 32 * b + 16 * x, t, lane), f[b][x], dk[t]);
+                }
+            interleave<T, 4 * DT, 6, 2>(b == 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // steps of whole tiles come after those at the edge, for every head
+    for (int n = 0; n < steps && !broken; n += 2) {
+        if (steps_whole(n)) step(n, Known<0>{}, Known<0>{}); else step(n, Known<1>{}, Known<0>{});
+        if (n + 1 < steps && !broken) {
+            if (steps_whole(n + 1)) step(n + 1, Known<0>{}, Known<1>{}); else step(n + 1, Known<1>{}, Known<1>{});
+        }
+    }
+    if (broken) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+        for (int x = 0; x < 32 && j0 + x < rk.n; ++x) dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x));
+        return;
     }
     if (!there) return;
     store_columns((T*)p.dK + (int64_t)(rk.first + j) * p.dk.row + (int64_t)kv * p.dk.head, dk, p.scale, p.D, half);

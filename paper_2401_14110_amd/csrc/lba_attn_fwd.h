@@ -11,16 +11,61 @@
 
 namespace lba {
 
+// store(pointer to O's type): O as what it is
+template <typename F> __device__ __forceinline__ void with_output(const AttnParams& p, F store) {
+    if (p.o_type == LBA_F32) store((float*)p.O);
+    else if (p.o_type == LBA_BF16) store((bf16_t*)p.O);
+    else store((uint8_t*)p.O);
+}
+
+// One query by one wave, over the `seen` keys from row k0 on and nothing else: a lane a key, then a lane two columns.  words: 192 of LDS.
+template <typename T> __device__ __forceinline__ void attn_row(const AttnParams& p, float* words, int h, int kv, int t, int k0, int seen) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)t * p.H + h;
+    float* const w = words + 128;
+    wave_words_done();
+    for (int d = lane; d < 128; d += 64) words[d] = d < p.D ? load_one((const T*)p.Q + (int64_t)t * p.q.row + (int64_t)h * p.q.head + d) : 0.0f;
+    float top = -__builtin_inff(), sum = 0.0f, acc[2] = {0.0f, 0.0f};
+    for (int j0 = 0; j0 < seen; j0 += 64) {
+        wave_words_done();
+        float s = -__builtin_inff();
+        if (j0 + lane < seen) {
+            const T* k = (const T*)p.K + (int64_t)(k0 + j0 + lane) * p.k.row + (int64_t)kv * p.k.head;
+            s = 0.0f;
+            for (int d = 0; d < p.D; ++d) s = fmaf(words[d], load_one(k + d), s);
+            s *= p.scale;
+        }
+        const float now = fmaxf(wave_max(s), top), base = now == -__builtin_inff() ? 0.0f : now;
+        const float e = j0 + lane < seen ? exp_near(s - base) : 0.0f, f = exp_near(top - base);
+        top = now;
+        sum = sum * f + wave_sum(e);
+        w[lane] = e;
+        wave_words_done();
+        acc[0] *= f;
+        acc[1] *= f;
+        for (int j = 0; j < 64 && j0 + j < seen; ++j) {
+            const T* v = (const T*)p.V + (int64_t)(k0 + j0 + j) * p.v.row + (int64_t)kv * p.v.head;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (lane + 64 * x < p.D) acc[x] = fmaf(w[j], load_one(v + lane + 64 * x), acc[x]);
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    with_output(p, [&](auto* o) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (lane + 64 * x < p.D) store_one(o + row * p.D + lane + 64 * x, acc[x] * inv, p.fmt);
+    });
+    if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(sum) * 0.693147181f;
+}
+
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnParams p) {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
     constexpr int TILE = KT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
     if ((int)blockIdx.x >= p.units) {
-        const int block = blockIdx.x - p.units;
-        if (p.o_type == LBA_F32) clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (float*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
-        else if (p.o_type == LBA_BF16) clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (bf16_t*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
-        else clear_rows(p.starts, p.T, p.count, block, kClearBlocks, (uint8_t*)p.O, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt);
+        with_output(p, [&](auto* o) { clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units, kClearBlocks, o, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt); });
         return;
     }
     const int unit = unit_of(blockIdx.x, p.units), per = p.tiles * p.group;
@@ -62,6 +107,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
     float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
+    bool broken = false;                                 // a tile that some query sees in part holds infinities or NaN
     // One tile.  EDGE: some query may not see all of it; the tiles before are seen whole by every query of the workgroup.
     auto step = [&](int kt, auto edge, auto buffer) {
         constexpr bool EDGE = decltype(edge)::value != 0;
@@ -78,9 +124,8 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
             lk.load(lds[BUF ^ 1][0], rk.n - k0 - KT);
             lv.load(lds[BUF ^ 1][1], rk.n - k0 - KT);
         }
-        bool broken = false;
         if constexpr (EDGE) {
-            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv);
+            if (p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv)) { broken = true; return; }
             if (k0 >= most) return;                      // (the barriers above are everybody's)
         }
         f32x16 s[KB];
@@ -130,24 +175,6 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
                 s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, base));
                 sum += s[b][r];
             }
-        if (EDGE && broken) {                            // a zero weight must not meet an infinity: key by key, where it is seen
-            for (int j = 0; j < KT && k0 + j < rk.n; ++j) {
-                float w = 0.0f;
-#pragma unroll
-                for (int b = 0; b < KB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (32 * b + row_of(r) == (j & ~4)) w = s[b][r];
-                w = __shfl(w, (lane & 31) + 8 * (j & 4));
-                if (k0 + j < lim) {
-#pragma unroll
-                    for (int t = 0; t < DT; ++t)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(w, tile_at<T, DP>(tv, j, 32 * t + row_of(r) + 4 * half), acc[t][r]);
-                }
-            }
-            return;
-        }
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -163,16 +190,22 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
         step(kt, Known<0>{}, Known<0>{});
         step(kt + 1, Known<0>{}, Known<1>{});
     }
-    for (; kt < tiles; kt += 2) {
+    for (; kt < tiles && !broken; kt += 2) {
         step(kt, Known<1>{}, Known<0>{});
-        if (kt + 1 < tiles) step(kt + 1, Known<1>{}, Known<1>{});
+        if (kt + 1 < tiles && !broken) step(kt + 1, Known<1>{}, Known<1>{});
+    }
+    if (broken) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+        for (int j = 0; j < 32 && i0 + j < rq.n; ++j) attn_row<T>(p, (float*)&lds[0][0][0] + wave * 192, h, kv, rq.first + i0 + j, rk.first, limit(i0 + j));
+        return;
     }
     sum = sum_of_halves(sum);
     if (i >= rq.n) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;
     if (p.lse && half == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
-    auto store = [&](auto* o) {
+    with_output(p, [&](auto* o) {
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -181,10 +214,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
                 const float v[4] = {acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv, acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv};
                 if (d < p.D) store_some<4>(o + row * p.D + d, p.D - d, v, p.fmt);
             }
-    };
-    if (p.o_type == LBA_F32) store((float*)p.O);
-    else if (p.o_type == LBA_BF16) store((bf16_t*)p.O);
-    else store((uint8_t*)p.O);
+    });
 }
 
 template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st) {

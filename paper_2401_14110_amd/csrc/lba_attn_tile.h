@@ -126,12 +126,6 @@ template <typename T, int DP> __device__ __forceinline__ Frag<T> column_frag(con
     }
     return f;
 }
-// element (row, d) of a tile
-template <typename T, int DP> __device__ __forceinline__ float tile_at(const uint8_t* tile, int row, int d) {
-    constexpr int C = DP * sizeof(T) / 16, V = 16 / sizeof(T);
-    return load_one((const T*)(tile + row * (C * 16) + ((d / V) ^ turn<C>(row)) * 16) + d % V);
-}
-
 // Rows of a head on their way to a tile of ROWS rows.  DIRECT: rows are whole pieces of 16 aligned bytes, a tile's rows within 2^31 bytes, and go
 // from memory to LDS without registers in between; else a lane holds them until they are put down.  What is behind `rows` rows or D elements
 // is zeros.
@@ -211,6 +205,39 @@ template <typename T, int DP, int ROWS> __device__ __forceinline__ bool tile_is_
         }
     }
     return __syncthreads_or(bad) != 0;
+}
+
+// ---- tiles that hold infinities or NaN -----------------------------------------------------
+//
+// A product over rows some of which a column does not see must not multiply their infinities with its zeros.  Where a tile that is seen in part
+// holds any, the weights' own NaN is enough for what is seen (dQ), or the workgroup's rows are done again, one by one over what each sees.
+
+// the fragment with zeros for infinities and NaN
+__device__ __forceinline__ Frag<bf16_t> without_broken(Frag<bf16_t> f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = (uint32_t)f.w[j];
+        f.w[j] &= (int32_t)~(((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u));
+    }
+    return f;
+}
+__device__ __forceinline__ Frag<float> without_broken(Frag<float> f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f.a[j] = (__float_as_uint(f.a[j]) & 0x7F800000u) == 0x7F800000u ? 0.0f : f.a[j];
+        f.b[j] = (__float_as_uint(f.b[j]) & 0x7F800000u) == 0x7F800000u ? 0.0f : f.b[j];
+    }
+    return f;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int x = 32; x; x /= 2) v = fmaxf(v, __shfl_xor(v, x));
+    return v;
+}
+// before a wave's own words of LDS are used for something else
+__device__ __forceinline__ void wave_words_done() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // a lane's row of a head as fragments: `D` elements from `at`, zeros behind; row < 0: zeros.  FLIP: with the other sign.
