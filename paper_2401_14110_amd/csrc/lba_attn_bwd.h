@@ -27,20 +27,6 @@ template <typename T, int DT> __device__ __forceinline__ void store_columns(T* r
         }
 }
 
-// The order of what has been written since the last barrier of the scheduler: after each of N products some of what does not belong to the
-// matrix cores, VALU instructions and reads from LDS.
-template <typename T, int N, int VALU, int READS> __device__ __forceinline__ void interleave(bool valu) {
-    if constexpr (sizeof(T) == 2) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            if (valu) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-        }
-    }
-}
-
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
@@ -206,6 +192,7 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams p) {
     constexpr int QT = sizeof(T) == 2 ? 64 : 32, QB = QT / 32, KC = DP / 16, DT = DP / 32;
+    constexpr bool PIPE = !(DIRECT && sizeof(T) == 2 && DP <= 64);
     constexpr int TILE = QT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of queries and their outputs' gradients
     __shared__ __attribute__((aligned(16))) float side[2][2][QT];                    // -lse in units of log 2, rowsum(G * O)
@@ -230,6 +217,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
 
     Loader<T, DP, QT, DIRECT> lq, lg;
     float side_next = 0.0f;                              // lane t of the first two waves: query t % QT of the step's lse or sum
+    bool side_there = false;
     int next_tile = 0, next_head = 0;
     auto load = [&](int buf) {                           // the step after those that have been loaded
         const int h = kv * p.group + next_head, q0 = (t0 + next_tile) * QT;
@@ -242,8 +230,9 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         if (threadIdx.x < 2 * QT) {
             const int i = q0 + (int)threadIdx.x % QT;
             const int64_t row = (int64_t)(rq.first + i) * p.H + h;
-            if ((int)threadIdx.x < QT) side_next = i < rq.n ? -p.lse[row] * kLog2e : -__builtin_inff();              // rows that are not there have no weight
-            else side_next = i < rq.n ? p.delta[row] : 0.0f;
+            const float* from = (int)threadIdx.x < QT ? p.lse : p.delta;
+            side_next = from[i < rq.n ? row : (int64_t)rq.first * p.H];              // (used only where it is put down: nothing waits for it here)
+            side_there = i < rq.n;
         }
         if (++next_tile == steps_head) { next_tile = 0; ++next_head; }
     };
@@ -256,25 +245,25 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) { dk[t] = f32x16{}; dv[t] = f32x16{}; }
-    auto steps_whole = [&](int n) { return (t0 + n % steps_head) * QT >= masked_all; };              // all the workgroup's keys are seen by the step's queries
-    int tile = 0;
+    int n = 0;                                           // steps that are done
     bool broken = false;                                 // a tile that some key sees in part holds infinities or NaN
-    // One tile of queries.  EDGE: some key may not be seen by all of them.  The products of one block of 32 queries run while the weights of the
-    // other are worked out: a wave is alone on its SIMD, and its own instructions are all there is to fill it.
-    auto step = [&](int n, auto edge, auto buffer) {
+    // One tile of queries.  EDGE: some key may not be seen by all of them.  PIPE: the products of one block of 32 queries run while the weights of the
+    // other are worked out, since a wave that is alone on its SIMD has only its own instructions to fill it; else two waves share it.
+    auto step = [&](int tile, auto edge) {
         constexpr bool EDGE = decltype(edge)::value != 0;
-        constexpr int BUF = decltype(buffer)::value;
-        const int q0 = (t0 + tile) * QT;
-        if (++tile == steps_head) tile = 0;
-        uint8_t* const tq = lds[BUF][0];
-        uint8_t* const tg = lds[BUF][1];
+        const int q0 = (t0 + tile) * QT, buf = n & 1;
+        uint8_t* const tq = lds[buf][0];
+        uint8_t* const tg = lds[buf][1];
         lq.put(tq);
         lg.put(tg);
-        if (threadIdx.x < 2 * QT) side[BUF][threadIdx.x / QT][threadIdx.x % QT] = side_next;
+        if (threadIdx.x < 2 * QT) {                      // rows that are not there have no weight
+            const bool sum = threadIdx.x >= QT;
+            side[buf][sum][threadIdx.x % QT] = sum ? (side_there ? side_next : 0.0f) : side_there ? -side_next * kLog2e : -__builtin_inff();
+        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (n + 1 < steps) load(BUF ^ 1);
+        if (++n < steps) load(buf ^ 1);
         if constexpr (EDGE) {
             if (p.causal && q0 < masked_all) {
                 const bool a = tile_is_broken<T, DP, QT>(tq);
@@ -282,68 +271,96 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
             }
             if (q0 + QT <= lo_wave) return;
         }
-        f32x16 s[QB], u[QB];
-        Frag<T> w[QB][2], f[QB][2];
-        Frag<T> ring[3][2];
-        auto fetch = [&](int b, int x) {
-            ring[x % 3][0] = row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half);
-            ring[x % 3][1] = row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half);
-        };
-        auto weights = [&](int b) {
+        f32x16 s[PIPE ? QB : 1], u[PIPE ? QB : 1];
+        Frag<T> w[PIPE ? QB : 1][2], f[PIPE ? QB : 1][2];
+        f32x4_t base[4], delta[4];
+        auto at = [](int b) { return PIPE ? b : 0; };
+        auto sides = [&](int b) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const f32x4_t base = *(const f32x4_t*)&side[BUF][0][32 * b + 8 * x + 4 * half];
-                const f32x4_t delta = *(const f32x4_t*)&side[BUF][1][32 * b + 8 * x + 4 * half];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    s[b][4 * x + y] = __builtin_amdgcn_exp2f(fmaf(s[b][4 * x + y], c, base[y]));
-                    u[b][4 * x + y] = s[b][4 * x + y] * (u[b][4 * x + y] - delta[y]);
-                }
+                base[x] = *(const f32x4_t*)&side[buf][0][32 * b + 8 * x + 4 * half];
+                delta[x] = *(const f32x4_t*)&side[buf][1][32 * b + 8 * x + 4 * half];
             }
-            if (EDGE && q0 < lo_last) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (q0 + 32 * b + row_of(r) + 4 * half < lo) s[b][r] = u[b][r] = 0.0f;
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) { w[b][x] = as_frag<T>(s[b], x); f[b][x] = as_frag<T>(u[b], x); }
         };
+        auto weights = [&](int b, int first, int last) { // registers first .. last - 1 of block b
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            s[b] = u[b] = f32x16{};
-            fetch(b, 0);
-            if (KC > 1) fetch(b, 1);
-            if (b > 0) weights(b - 1);
+            for (int r = first; r < last; ++r) {
+                float& x = ((float*)&s[at(b)])[r];
+                float& y = ((float*)&u[at(b)])[r];
+                x = __builtin_amdgcn_exp2f(fmaf(x, c, base[r / 4][r % 4]));
+                y = x * (y - delta[r / 4][r % 4]);
+                if (EDGE && q0 + 32 * b + row_of(r) + 4 * half < lo) x = y = 0.0f;
+            }
+        };
+        auto pack = [&](int b) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) { w[at(b)][x] = as_frag<T>(s[at(b)], x); f[at(b)][x] = as_frag<T>(u[at(b)], x); }
+        };
+        auto scores = [&](int b) {                       // and PIPE the weights of the block before
+            Frag<T> ring[3][2];
+            auto fetch = [&](int x) {
+                ring[x % 3][0] = row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half);
+                ring[x % 3][1] = row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half);
+            };
+            s[at(b)] = u[at(b)] = f32x16{};
+            fetch(0);
+            fetch(1);
+            if (!PIPE) sides(b);
+            else if (b > 0) sides(b - 1);
 #pragma unroll
             for (int x = 0; x < KC; ++x) {
-                if (x + 2 < KC) fetch(b, x + 2);
-                s[b] = product(ring[x % 3][0], k[x], s[b]);
-                u[b] = product(ring[x % 3][1], v[x], u[b]);
+                if (x + 2 < KC) fetch(x + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                s[at(b)] = product(ring[x % 3][0], k[x], s[at(b)]);
+                u[at(b)] = product(ring[x % 3][1], v[x], u[at(b)]);
+                if (PIPE && b > 0) weights(b - 1, 16 * x / KC, 16 * (x + 1) / KC);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            interleave<T, 2 * KC, 6, 2>(b > 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (QB == 1) weights(0);
+            if (PIPE && b > 0) pack(b - 1);
+        };
+        auto sums = [&](int b) {                         // and PIPE, with the first block, the weights of the last
+            constexpr int N = 2 * DT;                    // column tiles of both halves of the block
+            const bool last = PIPE && QB > 1 && b == 0;
+            Frag<T> ring[3][2];
+            auto fetch = [&](int i) {
+                ring[i % 3][0] = column_frag<T, DP>(tg, 32 * b + 16 * (i / DT), i % DT, lane);
+                ring[i % 3][1] = column_frag<T, DP>(tq, 32 * b + 16 * (i / DT), i % DT, lane);
+            };
+            fetch(0);
+            fetch(1);
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            if (QB > 1 && b == 0) weights(QB - 1);
+            for (int i = 0; i < N; ++i) {
+                if (i + 2 < N) fetch(i + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                dv[i % DT] = product(ring[i % 3][0], w[at(b)][i / DT], dv[i % DT]);
+                dk[i % DT] = product(ring[i % 3][1], f[at(b)][i / DT], dk[i % DT]);
+                if (last) weights(QB - 1, 16 * i / N, 16 * (i + 1) / N);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (last) pack(QB - 1);
+        };
+        if constexpr (PIPE && QB > 1) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int b = 0; b < QB; ++b) scores(b);
+            sides(QB - 1);
 #pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    dv[t] = product(column_frag<T, DP>(tg, 32 * b + 16 * x, t, lane), w[b][x], dv[t]);
-                    dk[t] = product(column_frag<T, DP>(tq, 32 * b + 16 * x, t, lane), f[b][x], dk[t]);
-                }
-            interleave<T, 4 * DT, 6, 2>(b == 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int b = 0; b < QB; ++b) sums(b);
+        } else {
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                scores(b);
+                if (PIPE) sides(b);
+                weights(b, 0, 16);
+                pack(b);
+                sums(b);
+            }
         }
     };
-    // steps of whole tiles come after those at the edge, for every head
-    for (int n = 0; n < steps && !broken; n += 2) {
-        if (steps_whole(n)) step(n, Known<0>{}, Known<0>{}); else step(n, Known<1>{}, Known<0>{});
-        if (n + 1 < steps && !broken) {
-            if (steps_whole(n + 1)) step(n + 1, Known<0>{}, Known<1>{}); else step(n + 1, Known<1>{}, Known<1>{});
-        }
+    // of every head the steps at the edge, then those that all the workgroup's keys are seen by
+    const int edge = max(0, min(steps_head, (masked_all + QT - 1) / QT - t0));
+    for (int h = 0; h < p.group && steps_head > 0 && !broken; ++h) {
+        for (int tile = 0; tile < edge && !broken; ++tile) step(tile, Known<1>{});
+        for (int tile = edge; tile < steps_head && !broken; ++tile) step(tile, Known<0>{});
     }
     if (broken) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
