@@ -107,9 +107,8 @@ int lba_cache_read(lba_cache4 c, const int32_t* starts, int64_t T, void* K, lba_
  * sees positions 0 .. lens[b] - fresh + i, as far as they hold something.  O [count, fresh, H, D] contiguous of o_type; a query that sees nothing has zeros.
  * Scores, maxima and sums are float32; with LBA_BF16 the weights are rounded to bfloat16 for the product with the values, with LBA_F32 they
  * and the queries are split into three bfloat16 pieces, which hold them.
- * Limits (else LBA_ERR_SHAPE): H a multiple of KV, H <= 65535, count <= 65535, count * fresh * H < 2^24, table_row * page <= 2^30; with 16 rows (fresh
- * queries of the H / KV heads that share one) a tile, 32 where there are more, and C chunks of positions, tiles * KV <= 65535 and C * tiles * KV *
- * count < 2^24, where C is at most 2049 / (tiles * KV * count) + 1.
+ * Limits (else LBA_ERR_SHAPE): H a multiple of KV, H <= 65535, count * fresh * H < 2^24, table_row * page <= 2^30, and with tiles of 16 rows (the fresh
+ * queries of the H / KV heads that share one; 32 where there are more) tiles * KV * count < 2^23.
  * workspace: lba_cache_attention_workspace_bytes(...) bytes, for the longest sequence that the table has room for. */
 int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t type, int64_t fresh, int64_t H, float scale, void* O, int32_t o_type,
                         lba_infmt o_fmt, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -114,16 +114,77 @@ template <int D> __device__ __forceinline__ int value_turn(int r) {
     else return 2 * ((r >> 2) & 1) + ((r >> 3) & 1);
 }
 
+__device__ __forceinline__ void lds_words_done() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+// One row by one wave, over the positions c0 .. c1 - 1 that it sees and nothing else: a lane a position, then a lane two columns.  words: 192 of LDS;
+// its sums, maximum (times c, as in the kernel) and sum of weights go to `sums` and ends[0][.][r].
+template <typename T, int D>
+__device__ __forceinline__ void chunk_row(const CacheAttnParams& p, int b, int kv, int row, int rows, int c0, int c1, float* words, float* sums, int r, float* ends,
+                                          int stride) {
+    const int lane = threadIdx.x & 63;
+    float top = -__builtin_inff(), sum = 0.0f, acc[2] = {0.0f, 0.0f};
+    if (row < rows) {
+        const int lim = min(c1, row_seen(p, b, row));
+        const T* x = (const T*)p.Q + ((int64_t)b * p.fresh + row / p.group) * p.q.row + (int64_t)(kv * p.group + row % p.group) * p.q.head;
+        lds_words_done();
+        for (int d = lane; d < D; d += 64) words[d] = load_one(x + d);
+        auto value = [&](const uint8_t* codes, const uint8_t* scales, int64_t line, int d) {
+            return four_value(codes[line * (D / 2) + d / 2] >> (d % 2 * 4)) * power_of(scales[line * (D / 32) + d / 32]);
+        };
+        for (int k0 = c0; k0 < lim; k0 += 64) {
+            lds_words_done();
+            const int64_t line = k0 + lane < lim ? line_of(p.c, b, k0 + lane, kv) : -1;
+            float s = -__builtin_inff();
+            if (line >= 0) {
+                s = 0.0f;
+                for (int d = 0; d < D; ++d) s = fmaf(words[d], value(p.c.k, p.c.k_scale, line, d), s);
+                s *= p.scale * 1.44269504f;
+            }
+            float now = s;
+#pragma unroll
+            for (int y = 32; y; y /= 2) now = fmaxf(now, __shfl_xor(now, y));
+            now = fmaxf(now, top);
+            const float base = now == -__builtin_inff() ? 0.0f : now;
+            const float e = line >= 0 ? __builtin_amdgcn_exp2f(s - base) : 0.0f, f = __builtin_amdgcn_exp2f(top - base);
+            top = now;
+            sum = sum * f + wave_sum(e);
+            words[128 + lane] = e;
+            lds_words_done();
+            acc[0] *= f;
+            acc[1] *= f;
+            for (int j = 0; j < 64 && k0 + j < lim; ++j) {
+                const int64_t at = line_of(p.c, b, k0 + j, kv);
+                if (at < 0) continue;
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    if (lane + 64 * y < D) acc[y] = fmaf(words[128 + j], value(p.c.v, p.c.v_scale, at, lane + 64 * y), acc[y]);
+            }
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        const int d = lane + 64 * y;
+        if (d < D) sums[((d / 4) ^ (r & 7)) * 4 + d % 4] = acc[y];
+    }
+    if (lane == 0) { ends[r] = top; ends[stride + r] = sum; }
+}
+
 template <typename T, int D, int R>
-__global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 2) void cache_attn_kernel(CacheAttnParams p) {
+__global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2) void cache_attn_kernel(CacheAttnParams p) {
     constexpr int KC = D / 32, DT = D / 16, NP = sizeof(T) == 2 ? 1 : 3;
     constexpr int ROWB = D * 2, WAVE = (32 * ROWB > 16 * R * D * 4 ? 32 * ROWB : 16 * R * D * 4);    // values of a step; at the end a wave's sums
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][WAVE];
     __shared__ float ends[4][2][16 * R];
+    __shared__ float words[4][192];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = lane & 15, quarter = lane / 16;
-    const int b = blockIdx.z, kv = blockIdx.y / p.row_tiles, row0 = blockIdx.y % p.row_tiles * (16 * R), rows = p.fresh * p.group;
-    const int seen = row_seen(p, b, min(row0 + 16 * R, rows) - 1), c0 = blockIdx.x * p.chunk;
-    if (c0 >= seen && blockIdx.x > 0) return;
+    // Workgroups go to the eight dies in turn, so that neighbours are different heads and sequences, and all have as many: with a sequence's
+    // chunks as neighbours the dies of the last ones idle where most sequences are short.
+    const int units = p.c.count * p.c.KV * p.row_tiles, unit = blockIdx.x % units, chunk = blockIdx.x / units;
+    const int b = unit / (p.c.KV * p.row_tiles), kv = unit / p.row_tiles % p.c.KV, row0 = unit % p.row_tiles * (16 * R), rows = p.fresh * p.group;
+    const int seen = row_seen(p, b, min(row0 + 16 * R, rows) - 1), c0 = chunk * p.chunk;
+    if (c0 >= seen && chunk > 0) return;
     const int c1 = min(c0 + p.chunk, seen);
     const bool alone = seen <= p.chunk;                  // the only chunk that there is
 
@@ -167,26 +228,41 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
         for (int d = 0; d < DT; ++d) acc[t][d] = f32x4_c{0.0f, 0.0f, 0.0f, 0.0f};
     }
     int k0 = c0 + wave * 32;
+    // Codes are loaded as soon as those of the step before are in use, the pages they are in a step ahead of that.  (Codes two steps ahead, with
+    // two waves a SIMD fewer: no faster.)
     Part<D> nk[2], nv[2];
-    int64_t line[2];
+    bool there[2];
     int32_t page[2];
-    auto fetch = [&](int at0) {                      // codes of the step at at0, whose pages are known; then the next step's pages
+    auto fetch = [&](int at0) {                          // codes of the step at at0, whose pages are known; then the next step's pages
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            line[u] = line_at(at0 + 16 * u + col, page[u]);
-            nk[u].load(p.c.k, p.c.k_scale, line[u], quarter);
-            nv[u].load(p.c.v, p.c.v_scale, line[u], quarter);
+            const int64_t line = line_at(at0 + 16 * u + col, page[u]);
+            nk[u].load(p.c.k, p.c.k_scale, line, quarter);
+            nv[u].load(p.c.v, p.c.v_scale, line, quarter);
+            there[u] = line >= 0;
             page[u] = page_of(at0 + 128 + 16 * u + col);
         }
     };
 #pragma unroll
     for (int u = 0; u < 2; ++u) page[u] = page_of(k0 + 16 * u + col);
-    if (k0 < c1) fetch(k0);
+    fetch(k0);
     uint8_t* const mine = lds[wave];
+    bool again = false;
     for (; k0 < c1; k0 += 128) {
-        Part<D> kp[2] = {nk[0], nk[1]}, vp[2] = {nv[0], nv[1]};
-        const bool there[2] = {line[0] >= 0, line[1] >= 0};
-        fetch(k0 + 128);
+        const uint32_t held = (uint32_t)(__ballot(there[0]) & 0xFFFF) | (uint32_t)((__ballot(there[1]) & 0xFFFF) << 16);       // positions that hold something
+        const bool broken = p.fresh > 1 && __any(nv[0].broken() || nv[1].broken());
+        // values to this wave's rows, after the reads of the step before
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                const int r = 16 * u + col;
+                *(i32x4_c*)(mine + r * ROWB + ((quarter * KC + k) ^ value_turn<D>(r)) * 16) = nv[u].values(k);
+            }
+            __builtin_amdgcn_sched_barrier(0);           // (here and below: all of a step's conversions at once would cost a third of the waves)
+        }
+        __builtin_amdgcn_wave_barrier();
         f32x4_c s[R][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -194,24 +270,16 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
             for (int t = 0; t < R; ++t) s[t][u] = f32x4_c{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < KC; ++k) {
-                const i32x4_c a = kp[u].values(k);
+                const i32x4_c a = nk[u].values(k);
 #pragma unroll
                 for (int t = 0; t < R; ++t)
 #pragma unroll
                     for (int n = 0; n < NP; ++n) s[t][u] = product16(a, q[t][n][k], s[t][u]);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // values to this wave's rows, after the reads of the step before
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                const int r = 16 * u + col;
-                *(i32x4_c*)(mine + r * ROWB + ((quarter * KC + k) ^ value_turn<D>(r)) * 16) = vp[u].values(k);
-            }
-        __builtin_amdgcn_wave_barrier();
-        const uint32_t held = (uint32_t)(__ballot(there[0]) & 0xFFFF) | (uint32_t)((__ballot(there[1]) & 0xFFFF) << 16);       // positions that hold something
+        fetch(k0 + 128);
+        __builtin_amdgcn_sched_barrier(0);
         bool partly = held != 0xFFFFFFFFu;
         bool hidden = false;                             // a position that one row sees and another does not
 #pragma unroll
@@ -266,47 +334,33 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[t][n][j] = __builtin_bit_cast(int32_t, bf16x2_c{piece[2 * j][n], piece[2 * j + 1][n]});
         }
-        if (!(hidden && __any(vp[0].broken() || vp[1].broken()))) {
+        again |= hidden && broken;                       // a zero weight has met an infinity, or may have
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                typedef __attribute__((address_space(3))) i16x4_c* lds_ptr;
-                union { i16x4_c h[2]; i32x4_c v; } x;
+        for (int d = 0; d < DT; ++d) {
+            typedef __attribute__((address_space(3))) i16x4_c* lds_ptr;
+            union { i16x4_c h[2]; i32x4_c v; } x;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int r = 16 * u + 4 * quarter + col / 4;
-                    x.h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(mine + r * ROWB + ((2 * d + (col & 3) / 2) ^ value_turn<D>(r)) * 16 + (col & 1) * 8));
-                }
-#pragma unroll
-                for (int t = 0; t < R; ++t)
-#pragma unroll
-                    for (int n = 0; n < NP; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
+            for (int u = 0; u < 2; ++u) {
+                const int r = 16 * u + 4 * quarter + col / 4;
+                x.h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(mine + r * ROWB + ((2 * d + (col & 3) / 2) ^ value_turn<D>(r)) * 16 + (col & 1) * 8));
             }
-        } else {                                         // a zero weight must not meet an infinity: position by position, where it is seen
-            for (int j = 0; j < 32; ++j) {
-                if (!((held >> j) & 1)) continue;
 #pragma unroll
-                for (int t = 0; t < R; ++t) {
-                    float x = 0.0f;
+            for (int t = 0; t < R; ++t)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (16 * u + r == (j & ~12)) x = s[t][u][r];
-                    x = __shfl(x, col + 4 * (j & 12));
-                    if (k0 + j < lim[t]) {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const int e = 16 * d + 4 * quarter + r;
-                                acc[t][d][r] = fmaf(x, load_one((const bf16_t*)(mine + j * ROWB + ((e / 8) ^ value_turn<D>(j)) * 16) + e % 8), acc[t][d][r]);
-                            }
-                    }
-                }
-            }
+                for (int n = 0; n < NP; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
         }
     }
 
+    if (p.fresh > 1 && __syncthreads_or(again)) {        // the chunk's rows once more, one by one over what each sees
+        for (int r = wave; r < 16 * R; r += 4) chunk_row<T, D>(p, b, kv, row0 + r, rows, c0, c1, &words[wave][0], (float*)lds[0] + r * D, r, &ends[0][0][0], 16 * R);
+        for (int i = threadIdx.x; i < 3 * 16 * R; i += 256) {
+            ends[1 + i / (16 * R)][0][i % (16 * R)] = -__builtin_inff();
+            ends[1 + i / (16 * R)][1][i % (16 * R)] = 0.0f;
+        }
+        for (int x = 1; x < 4; ++x)
+            for (int i = threadIdx.x; i < 16 * R * D; i += 256) ((float*)lds[x])[i] = 0.0f;
+        __syncthreads();
+    } else {
     // the four waves' maxima, then their sums in one scale
 #pragma unroll
     for (int t = 0; t < R; ++t) {
@@ -325,6 +379,7 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
         for (int d = 0; d < DT; ++d) *(f32x4_c*)&sums[(16 * t + col) * D + ((4 * d + quarter) ^ (col & 7)) * 4] = acc[t][d] * f;
     }
     __syncthreads();
+    }
     for (int i = threadIdx.x; i < 16 * R * (D / 4); i += 256) {
         const int r = i / (D / 4), piece = i % (D / 4), row = row0 + r;
         if (row >= rows) continue;
@@ -346,7 +401,7 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
             else if (p.o_type == LBA_BF16) store_vec<4>((bf16_t*)p.O + out * D + piece * 4, o, p.fmt);
             else store_vec<4>((uint8_t*)p.O + out * D + piece * 4, o, p.fmt);
         } else {
-            const int64_t to = out * p.chunks + blockIdx.x;
+            const int64_t to = out * p.chunks + chunk;
             *(f32x4_c*)&p.part[to * D + piece * 4] = v;
             if (piece == 0) {
                 float* e = p.part + (int64_t)p.c.count * p.fresh * p.H * p.chunks * D + to * 2;
@@ -358,7 +413,7 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D > 64 ? 3 : 4) : 
 }
 
 template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st) {
-    const dim3 grid((unsigned)p.chunks, (unsigned)(p.c.KV * p.row_tiles), (unsigned)p.c.count);
+    const dim3 grid((unsigned)p.chunks * (unsigned)(p.c.count * p.c.KV * p.row_tiles));
 #define LBA_CACHE_ATTN(D_, R_) \
     if (p.c.D == D_ && r == R_) { hipLaunchKernelGGL((cache_attn_kernel<T, D_, R_>), grid, dim3(256), 0, st, p); return; }
     LBA_CACHE_ATTN(32, 1) LBA_CACHE_ATTN(64, 1) LBA_CACHE_ATTN(96, 1) LBA_CACHE_ATTN(128, 1)

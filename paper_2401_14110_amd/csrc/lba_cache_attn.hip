@@ -5,21 +5,57 @@ namespace lba {
 
 template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st);
 
-// Row `out` of O from its chunks: a workgroup a row, a group of lanes for every piece of four elements, chunks in turn over the groups.
-template <typename TO> __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int rows_of_tile) {
+// where row `out` of O has its chunks, and how many there are
+__device__ __forceinline__ int chunks_of_row(const CacheAttnParams& p, int64_t out, int rows_of_tile) {
+    const int64_t token = out / p.H;
+    const int b = (int)(token / p.fresh), r = (int)(token % p.fresh) * p.group + (int)(out % p.H) % p.group, rows = p.fresh * p.group;
+    return (row_seen(p, b, min(r / rows_of_tile * rows_of_tile + rows_of_tile, rows) - 1) + p.chunk - 1) / p.chunk;
+}
+__device__ __forceinline__ const float* ends_of_row(const CacheAttnParams& p, int64_t out) {
+    return p.part + (int64_t)p.c.count * p.fresh * p.H * p.chunks * p.c.D + out * p.chunks * 2;
+}
+__device__ __forceinline__ void store_joined(const CacheAttnParams& p, int64_t at, f32x4_c v, float l) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float o[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+    if (p.o_type == LBA_F32) store_vec<4>((float*)p.O + at, o, p.fmt);
+    else if (p.o_type == LBA_BF16) store_vec<4>((bf16_t*)p.O + at, o, p.fmt);
+    else store_vec<4>((uint8_t*)p.O + at, o, p.fmt);
+}
+
+// Few chunks a row: D / 4 lanes take a row, each its four elements of every chunk.
+__global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnParams p, int rows_of_tile, int64_t rows) {
+    const int pieces = p.c.D / 4, per = 256 / pieces, piece = (int)threadIdx.x % pieces;
+    const int64_t out = (int64_t)blockIdx.x * per + (int)threadIdx.x / pieces;
+    if ((int)threadIdx.x / pieces >= per || out >= rows) return;
+    const int n = chunks_of_row(p, out, rows_of_tile);
+    if (n <= 1) return;                                  // stored by its only workgroup
+    const float* end = ends_of_row(p, out);
+    const float* part = p.part + out * p.chunks * p.c.D + piece * 4;
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, end[2 * i]);
+    f32x4_c v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (m != -__builtin_inff()) {
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const float w = __builtin_amdgcn_exp2f(end[2 * i] - m);
+            l = fmaf(w, end[2 * i + 1], l);
+            v += w * *(const f32x4_c*)&part[(int64_t)i * p.c.D];
+        }
+    }
+    store_joined(p, out * p.c.D + piece * 4, v, l);
+}
+
+// Many: row blockIdx.x, elements 32 blockIdx.y ..: eight lanes for the 32 elements, the chunks in turn over the 32 groups of lanes.
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int rows_of_tile) {
     __shared__ float weight[256];
-    __shared__ f32x4_c sums[256];
+    __shared__ f32x4_c sums[4][8];
     __shared__ float parts[4];
     const int64_t out = blockIdx.x;
-    const int D = p.c.D, h = (int)(out % p.H);
-    const int64_t token = out / p.H;
-    const int b = (int)(token / p.fresh), r = (int)(token % p.fresh) * p.group + h % p.group, rows = p.fresh * p.group;
-    const int seen = row_seen(p, b, min(r / rows_of_tile * rows_of_tile + rows_of_tile, rows) - 1);
-    const int n = (seen + p.chunk - 1) / p.chunk;
-    if (n <= 1) return;                                  // stored by its only workgroup
-    const float* part = p.part + out * p.chunks * D;
-    const float* end = p.part + (int64_t)p.c.count * p.fresh * p.H * p.chunks * D + out * p.chunks * 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const int n = chunks_of_row(p, out, rows_of_tile);
+    if (n <= 1) return;
+    const int D = p.c.D, lane = threadIdx.x & 63, wave = threadIdx.x / 64, g = (int)threadIdx.x / 8, piece = (int)threadIdx.x % 8;
+    const float* part = p.part + out * p.chunks * D + blockIdx.y * 32 + piece * 4;
+    const float* end = ends_of_row(p, out);
     float m = -__builtin_inff();
     for (int i = threadIdx.x; i < n; i += 256) m = fmaxf(m, end[2 * i]);
 #pragma unroll
@@ -27,7 +63,6 @@ template <typename TO> __global__ __launch_bounds__(256) void cache_join_kernel(
     if (lane == 0) parts[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3]));
-    const int pieces = D / 4, groups = 256 / pieces, g = (int)threadIdx.x / pieces, piece = (int)threadIdx.x % pieces;
     f32x4_c v = {0.0f, 0.0f, 0.0f, 0.0f};
     float l = 0.0f;
     for (int i0 = 0; i0 < n; i0 += 256) {
@@ -37,24 +72,30 @@ template <typename TO> __global__ __launch_bounds__(256) void cache_join_kernel(
         weight[threadIdx.x] = w;
         if (i < n) l = fmaf(w, end[2 * i + 1], l);
         __syncthreads();
-        if (g < groups)
-            for (int k = g; k < 256 && i0 + k < n; k += groups) v += weight[k] * *(const f32x4_c*)&part[(int64_t)(i0 + k) * D + piece * 4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                    // chunks that are not there: the first one's, with no weight
+            const int at = g + 32 * k;
+            const f32x4_c x = *(const f32x4_c*)&part[(int64_t)(i0 + at < n ? i0 + at : 0) * D];
+            if (i0 + at < n) v += weight[at] * x;
+        }
     }
     l = wave_sum(l);
+#pragma unroll
+    for (int x = 8; x < 64; x *= 2)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], x);
     __syncthreads();
     if (lane == 0) parts[wave] = l;
-    sums[threadIdx.x] = v;
+    if (lane < 8) sums[wave][lane] = v;
     __syncthreads();
-    if (g != 0) return;
-    l = (parts[0] + parts[1]) + (parts[2] + parts[3]);
-    for (int x = 1; x < groups; ++x) v += sums[x * pieces + piece];
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const float o[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-    store_vec<4>((TO*)p.O + out * D + piece * 4, o, p.fmt);
+    if (threadIdx.x >= 8) return;
+    store_joined(p, out * D + blockIdx.y * 32 + piece * 4, (sums[0][piece] + sums[1][piece]) + (sums[2][piece] + sums[3][piece]),
+                 (parts[0] + parts[1]) + (parts[2] + parts[3]));
 }
 
-// How the rows and positions are cut: rows of a tile, and a chunk's positions, so many that there are about 2048 workgroups where every
-// sequence fills its table (four on every CU twice), and 256 at least (two steps of each wave).
+// How the rows and positions are cut: rows of a tile, and a chunk's positions, so many that there are about 1024 workgroups (three on a CU at a time)
+// where every sequence fills its table, and 256 at least (two steps of each wave).  With 1024, 2048, 4096 and 8192: 64 sequences of 1000 to
+// 8000 tokens 70, 72, 72 and 80 us, one of 131071 43, 45, 58 and 58.
 struct CachePlan {
     int32_t r, row_tiles;
     int64_t chunk, chunks, rows;
@@ -63,9 +104,9 @@ static int cache_plan(int64_t count, int64_t table_row, int64_t page, int64_t fr
     const int64_t room = table_row * page, rows = fresh * (H / KV);
     c->r = rows > 16 ? 2 : 1;
     const int64_t row_tiles = (rows + 16 * c->r - 1) / (16 * c->r), units = count * KV * row_tiles;
-    if (room > (1 << 30) || KV * row_tiles > 65535 || count > 65535) return LBA_ERR_SHAPE;
+    if (room > (1 << 30) || units >= (1 << 23)) return LBA_ERR_SHAPE;
     c->row_tiles = (int32_t)row_tiles;
-    c->chunk = (room * units + 2047) / 2048;
+    c->chunk = (room * units + 1023) / 1024;
     c->chunk = (c->chunk + 127) / 128 * 128;
     if (c->chunk < 256) c->chunk = 256;
     c->chunks = room > c->chunk ? (room + c->chunk - 1) / c->chunk : 1;
@@ -116,10 +157,10 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     const hipStream_t st = (hipStream_t)hip_stream;
     if (type == LBA_F32) launch_cache_attn<float>(p, plan.r, st); else launch_cache_attn<bf16_t>(p, plan.r, st);
     if (plan.chunks > 1) {
-        const dim3 grid((unsigned)plan.rows);
-        if (o_type == LBA_F32) hipLaunchKernelGGL((cache_join_kernel<float>), grid, dim3(256), 0, st, p, 16 * plan.r);
-        else if (o_type == LBA_BF16) hipLaunchKernelGGL((cache_join_kernel<bf16_t>), grid, dim3(256), 0, st, p, 16 * plan.r);
-        else hipLaunchKernelGGL((cache_join_kernel<uint8_t>), grid, dim3(256), 0, st, p, 16 * plan.r);
+        // a row's chunks one after another by one group of lanes, or side by side (64 sequences of up to 4 chunks, 2048 rows: 16 us side by side)
+        const int per = 256 / (c.D / 4);
+        if (plan.chunks <= 16) hipLaunchKernelGGL(cache_join_few_kernel, dim3((unsigned)((plan.rows + per - 1) / per)), dim3(256), 0, st, p, 16 * plan.r, plan.rows);
+        else hipLaunchKernelGGL(cache_join_kernel, dim3((unsigned)plan.rows, (unsigned)c.D / 32), dim3(256), 0, st, p, 16 * plan.r);
     }
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
