@@ -60,19 +60,21 @@ typedef struct {
 /* O = softmax over the seen keys of (scale * q . k) times V; a query that sees nothing has zeros.  Scores, the softmax's maximum and sum and O's
  * sums are float32; with LBA_BF16 the weights are rounded to bfloat16 for the product with V.
  * O [T, H, D] contiguous of o_type (o_fmt is read for LBA_CODE8 only); lse [T, H] float32 (NULL: not stored): ln of the sum over the seen
- * keys of exp(scale * q . k), -infinity where there are none. */
-int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void* O, int32_t o_type, lba_infmt o_fmt, float* lse,
-                  void* hip_stream);
+ * keys of exp(scale * q . k), -infinity where there are none.
+ * workspace: lba_attention_workspace_bytes(a) bytes, which reads no pointer of `a` but whether it is NULL; 0 where there are many rows. */
+int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void* O, int32_t o_type, lba_infmt o_fmt, float* lse, void* workspace,
+                  size_t workspace_bytes, void* hip_stream);
+size_t lba_attention_workspace_bytes(lba_attn a);
 
 /* Its gradients.  With P the weights, made again from lse, and G = dL/dO,
  *   dV = P^T . G,   S = P * (G . V^T - rowsum(G * O)),   dQ = scale * S . K,   dK = scale * S^T . Q,
  * summed over the query heads of a key head.  G and O [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D],
  * dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the products; sums are float32.
- * workspace: lba_attention_bwd_workspace_bytes(T, H) bytes. */
+ * workspace: lba_attention_bwd_workspace_bytes(a) bytes. */
 int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, const void* V, const void* O, const float* lse, void* dQ,
                       lba_strides dq_at, void* dK, lba_strides dk_at, void* dV, lba_strides dv_at, void* workspace, size_t workspace_bytes,
                       void* hip_stream);
-size_t lba_attention_bwd_workspace_bytes(int64_t T, int64_t H);
+size_t lba_attention_bwd_workspace_bytes(lba_attn a);
 
 /* A cache of keys and values in 4 bits.  Each 32 consecutive elements of a head are held as a power of two, one byte e for 2^(e - 127) (0: for zero), and
  * 4-bit codes, two a byte, the first in the low half: sign, two exponent bits, one mantissa bit, the numbers 0, 0.5, 1, 1.5, 2, 3, 4, 6 and

@@ -169,11 +169,13 @@ def lib(path=None):
             f.restype = ctypes.c_int
             f.argtypes = [vp, st, i32, vp, i32, vp, i64, i32, f32, vp, st, i64, i64, i64, vp]
         L.lba_attention.restype = ctypes.c_int
-        L.lba_attention.argtypes = [lba_attn, vp, vp, vp, vp, i32, lba_infmt, vp, vp]
+        L.lba_attention.argtypes = [lba_attn, vp, vp, vp, vp, i32, lba_infmt, vp, vp, size, vp]
+        L.lba_attention_workspace_bytes.restype = size
+        L.lba_attention_workspace_bytes.argtypes = [lba_attn]
         L.lba_attention_bwd.restype = ctypes.c_int
         L.lba_attention_bwd.argtypes = [lba_attn, vp, vp, vp, vp, vp, vp, vp, st, vp, st, vp, st, vp, size, vp]
         L.lba_attention_bwd_workspace_bytes.restype = size
-        L.lba_attention_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.lba_attention_bwd_workspace_bytes.argtypes = [lba_attn]
         L.lba_cache_write.restype = ctypes.c_int
         L.lba_cache_write.argtypes = [lba_cache4, vp, i64, vp, st, vp, st, i32, vp]
         L.lba_cache_read.restype = ctypes.c_int
@@ -415,16 +417,20 @@ def lba_rope_bwd(G, g_at, type, positions, pos_bits, freq, pairs, interleaved, g
     return lib().lba_rope_bwd(G, g_at, type, positions, pos_bits, freq, pairs, interleaved, gain, dX, dx_at, T, H, D, hip_stream)
 
 
-def lba_attention(a, Q, K, V, O, o_type, o_fmt, lse, hip_stream=None):
-    return lib().lba_attention(a, Q, K, V, O, o_type, infmt(o_fmt), lse, hip_stream)
+def lba_attention(a, Q, K, V, O, o_type, o_fmt, lse, workspace, workspace_bytes, hip_stream=None):
+    return lib().lba_attention(a, Q, K, V, O, o_type, infmt(o_fmt), lse, workspace, workspace_bytes, hip_stream)
+
+
+def lba_attention_workspace_bytes(a):
+    return int(lib().lba_attention_workspace_bytes(a))
 
 
 def lba_attention_bwd(a, G, Q, K, V, O, lse, dQ, dq_at, dK, dk_at, dV, dv_at, workspace, workspace_bytes, hip_stream=None):
     return lib().lba_attention_bwd(a, G, Q, K, V, O, lse, dQ, dq_at, dK, dk_at, dV, dv_at, workspace, workspace_bytes, hip_stream)
 
 
-def lba_attention_bwd_workspace_bytes(T, H):
-    return int(lib().lba_attention_bwd_workspace_bytes(T, H))
+def lba_attention_bwd_workspace_bytes(a):
+    return int(lib().lba_attention_bwd_workspace_bytes(a))
 
 
 def lba_cache_write(c, starts, T, K, k_at, V, v_at, type, hip_stream=None):
@@ -1091,6 +1097,17 @@ def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
     return a, (q, k, v, starts, starts_k)
 
 
+@functools.lru_cache(maxsize=1024)
+def _attn_bytes_of(name, T, Tk, count, starts, starts_k, H, KV, D, type):
+    a = lba_attn(T, Tk, count, 256 if starts else None, 256 if starts_k else None, H, KV, D, type)
+    return getattr(lib(), name)(a)
+
+
+def _attn_bytes(name, a):
+    """A workspace's size, which the library derives from the shape, and from which lists there are."""
+    return _attn_bytes_of(name, a.T, a.Tk, a.count, bool(a.starts), bool(a.starts_k), a.H, a.KV, a.D, a.type)
+
+
 def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None):
     """softmax(scale * q . k^T) . v of packed sequences: query head h reads head h * KV // H of k and v, and, causal, query i of n sees key j of m
     iff j <= i + m - n.  starts_k: the keys' sequences where they are not the queries'.  scale: D^-1/2 by default.  Returns o of q's
@@ -1105,7 +1122,9 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
     o = _empty(q.shape, dtype, q.device, on) if out is None else _output(out, q, q.shape, dtype, on)
     lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
-    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), handle))
+    size = _attn_bytes("lba_attention_workspace_bytes", a)
+    ws = _scratch(size, q.device, on)
+    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), _at(ws), size, handle))
     return (o, lse) if want_stats else o
 
 
@@ -1123,7 +1142,7 @@ def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, s
     G, o, lse = _whole(G, on), _whole(o, on), _whole(lse, on)
     got = tuple(_empty(t.shape, t.dtype, t.device, on) for t in (q, k, v)) if out is None else tuple(out)
     (dq, dq_at), (dk, dk_at), (dv, dv_at) = (_heads_out(t, w, n) for t, w, n in zip(got, (q, k, v), ("dq", "dk", "dv")))
-    size = _layer_bytes("lba_attention_bwd_workspace_bytes", a.T, a.H)
+    size = _attn_bytes("lba_attention_bwd_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
     _check(lib().lba_attention_bwd(a, _at(G), _at(q3), _at(k3), _at(v3), _at(o), _at(lse), _at(dq), dq_at, _at(dk), dk_at, _at(dv), dv_at, _at(ws), size,
                                    handle))

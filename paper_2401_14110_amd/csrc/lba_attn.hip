@@ -25,12 +25,42 @@ int attn_params(const lba_attn& a, AttnParams* p) {
     return LBA_OK;
 }
 
+// With few workgroups the steps of each are cut into parts, whose sums are joined by a launch of their own: so many that the card is full, but parts
+// of `least` steps at least of an average sequence.
+static int slices_for(int64_t units, int64_t steps, int64_t slots, int64_t least) {
+    if (units < 1) return 1;
+    int64_t n = slots / units;
+    if (n > steps / least) n = steps / least;
+    return (int)(n < 1 ? 1 : n > kMostSlices ? kMostSlices : n);
+}
+
+int attn_plan(const lba_attn& a, AttnPlan* plan) {
+    plan->tiles_q = most_tiles(a.starts, a.T, a.count, kTileRows);
+    plan->tiles_k = most_tiles(a.starts_k ? a.starts_k : a.starts, a.Tk, a.count, kTileRows);
+    if (plan->tiles_q * a.H > kMostUnits || plan->tiles_k * a.KV > kMostUnits) return LBA_ERR_SHAPE;
+    const int64_t step = a.type == LBA_F32 ? 32 : 64, count = a.count > 0 ? a.count : 1;
+    const int64_t keys = a.Tk / count / step, queries = a.T / count / step * (a.KV > 0 ? a.H / a.KV : 1);
+    const bool f32 = a.type == LBA_F32;                  // its steps take four times as long: shorter parts are worth a join
+    plan->slices = plan->slices_dq = slices_for(plan->tiles_q * a.H, keys, 512, f32 ? 2 : 4);
+    plan->slices_dkv = slices_for(plan->tiles_k * a.KV, queries, f32 || a.D <= 64 ? 512 : 256, f32 ? 2 : 4);
+    return LBA_OK;
+}
+
 }  // namespace lba
 
 using namespace lba;
 
-extern "C" int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void* O, int32_t o_type, lba_infmt o_fmt, float* lse,
-                             void* hip_stream) {
+extern "C" {
+
+size_t lba_attention_workspace_bytes(lba_attn a) {
+    AttnParams p = {};
+    AttnPlan plan;
+    if (attn_params(a, &p) != LBA_OK || attn_plan(a, &plan) != LBA_OK || plan.slices == 1) return 0;
+    return align256((size_t)plan.slices * (size_t)p.T * (size_t)p.H * (size_t)(p.D + 2) * sizeof(float));
+}
+
+int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void* O, int32_t o_type, lba_infmt o_fmt, float* lse, void* workspace,
+                  size_t workspace_bytes, void* hip_stream) {
     AttnParams p = {};
     int rc = attn_params(a, &p);
     if (rc == LBA_OK) rc = check_out_type(o_type, o_fmt);
@@ -40,14 +70,24 @@ extern "C" int lba_attention(lba_attn a, const void* Q, const void* K, const voi
     p.Q = Q; p.K = K; p.V = V; p.O = O; p.lse = lse;
     if (o_type == LBA_CODE8) p.fmt = make_code_fmt(o_fmt);
     p.o_type = o_type;
-    const int64_t tiles = most_tiles(p.starts, p.T, p.count, kTileRows);
-    if (tiles * p.H > kMostUnits) return LBA_ERR_SHAPE;
-    p.tiles = (int32_t)tiles;
-    p.units = (int32_t)(tiles * p.H);
+    AttnPlan plan;
+    rc = attn_plan(a, &plan);
+    if (rc != LBA_OK) return rc;
+    p.tiles = (int32_t)plan.tiles_q;
+    p.units = (int32_t)(plan.tiles_q * p.H);
+    p.slices = plan.slices;
     if (p.units == 0 && !p.clear) return LBA_OK;
+    if (p.slices > 1) {
+        if (!workspace) return LBA_ERR_NULL;
+        if ((uintptr_t)workspace % 256 != 0) return LBA_ERR_ALIGN;
+        if (workspace_bytes < lba_attention_workspace_bytes(a)) return LBA_ERR_SHAPE;
+        p.part = (float*)workspace;
+    }
     const int64_t size = a.type == LBA_F32 ? 4 : 2;
     const bool direct = whole_pieces(K, a.k, a.D, size) && whole_pieces(V, a.v, a.D, size);
     const hipStream_t st = (hipStream_t)hip_stream;
     if (a.type == LBA_F32) launch_attn<float>(p, direct, st); else launch_attn<bf16_t>(p, direct, st);
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
+
+}  // extern "C"

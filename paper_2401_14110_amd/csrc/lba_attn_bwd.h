@@ -14,48 +14,36 @@ namespace lba {
 
 constexpr float kLog2e = 1.44269504f;
 
-// registers 4 g .. 4 g + 3 of column tiles, times f, to a row
-template <typename T, int DT> __device__ __forceinline__ void store_columns(T* row, const f32x16 (&acc)[DT], float f, int D, int half) {
-    const CodeFmt none = {};
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int d = 32 * t + 8 * g + 4 * half;
-            const float v[4] = {acc[t][4 * g] * f, acc[t][4 * g + 1] * f, acc[t][4 * g + 2] * f, acc[t][4 * g + 3] * f};
-            if (d < D) store_some<4>(row + d, D - d, v, none);
-        }
-}
-
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
+    constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
     constexpr int TILE = KT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
-    if ((int)blockIdx.x >= p.units) {
+    if ((int)blockIdx.x >= p.units * p.slices) {
         const CodeFmt none = {};
-        clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units, kClearBlocks, (T*)p.dQ, p.dq.row, p.dq.head, p.H, p.D, (float*)nullptr, none);
+        clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, (T*)p.dQ, p.dq.row, p.dq.head, p.H, p.D, (float*)nullptr, none);
         return;
     }
-    const int unit = unit_of(blockIdx.x, p.units), per = p.tiles * p.group;
+    const int unit = unit_of(blockIdx.x % p.units, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
     const TileOf at = find_tile(p.starts, p.T, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);
     if (at.b < 0) return;
     const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
-    const int ahead = rk.n - rq.n;
-    auto limit = [&](int i) { return p.causal ? max(0, min(rk.n, i + ahead + 1)) : rk.n; };
+    auto limit = [&](int i) { return keys_seen(p, rq, rk, i); };
     const int i0 = at.t * kTileRows + wave * 32, i = i0 + (lane & 31);
     const int lim = limit(i), least = limit(i0), most = i0 < rq.n ? limit(min(i0 + 31, rq.n - 1)) : 0;
-    const int tiles = (limit(min(at.t * kTileRows + kTileRows, rq.n) - 1) + KT - 1) / KT, least_all = limit(at.t * kTileRows);
+    const Slice part = slice_of(steps_of_queries(p, rq, rk, at.t, KT), p.slices, slice);
+    const int first = part.first, tiles = part.last, least_all = limit(at.t * kTileRows);
+    if (first >= tiles && slice > 0) return;
     const bool there = i < rq.n;
 
     Loader<T, DP, KT, DIRECT> lk, lv;
-    lk.start((const T*)p.K + (int64_t)rk.first * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
-    lv.start((const T*)p.V + (int64_t)rk.first * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
-    if (tiles > 0) {
-        lk.load(lds[0][0], rk.n);
-        lv.load(lds[0][1], rk.n);
+    lk.start((const T*)p.K + (int64_t)(rk.first + first * KT) * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
+    lv.start((const T*)p.V + (int64_t)(rk.first + first * KT) * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
+    if (tiles > first) {
+        lk.load(lds[0][0], rk.n - first * KT);
+        lv.load(lds[0][1], rk.n - first * KT);
     }
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;
     Frag<T> q[KC], g[KC];
@@ -65,7 +53,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
 #pragma unroll
     for (int k = 0; k < KC; ++k) delta += dot(g[k], q[k]);
     delta = sum_of_halves(delta);
-    if (there && half == 0) p.delta[row] = delta;
+    if (there && half == 0 && slice == 0) p.delta[row] = delta;
     const float base = there ? -p.lse[row] * kLog2e : 0.0f;
     load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, there, p.D, half, q);
     const float c = p.scale * kLog2e;
@@ -130,7 +118,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
         }
     };
     const int whole = min(tiles, least_all / KT);
-    int kt = 0;
+    int kt = first;
     for (; kt + 1 < whole; kt += 2) {
         step(kt, Known<0>{}, Known<0>{});
         step(kt + 1, Known<0>{}, Known<1>{});
@@ -139,11 +127,15 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
         step(kt, Known<1>{}, Known<0>{});
         if (kt + 1 < tiles) step(kt + 1, Known<1>{}, Known<1>{});
     }
-    if (there) store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, p.scale, p.D, half);
+    if (!there) return;
+    if (!part.alone) store_columns(p.part + ((int64_t)slice * p.T * p.H + row) * p.D, acc, p.scale, p.D, half);
+    else store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, p.scale, p.D, half);
 }
 
-// One key by one wave, over the queries of its sequence from `first` on: a lane a query, then a lane two columns.  words: 384 of LDS.
-template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& p, float* words, int kv, int t, Rows rq, int first) {
+// One key by one wave, over the queries of its sequence from `lo` on that steps first .. last - 1 have (steps_head a head, `size` queries each from q0 on): a lane a
+// query, then a lane two columns.  words: 384 of LDS.  slice: -1 where these are all.
+template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& p, float* words, int kv, int t, Rows rq, int lo, int first, int last, int steps_head, int q0,
+                                                              int size, int slice) {
     const int lane = threadIdx.x & 63;
     const CodeFmt none = {};
     float *const v = words + 128, *const wp = words + 256, *const ws = words + 320;
@@ -153,23 +145,23 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
         v[d] = d < p.D ? load_one((const T*)p.V + (int64_t)t * p.v.row + (int64_t)kv * p.v.head + d) : 0.0f;
     }
     float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    for (int h = kv * p.group; h < (kv + 1) * p.group; ++h)
-        for (int i0 = first; i0 < rq.n; i0 += 64) {
+    for (int n = first; n < last; ++n) {
+            const int h = kv * p.group + n / steps_head, i0 = max(lo, q0 + n % steps_head * size), end = min(rq.n, q0 + n % steps_head * size + size);
             wave_words_done();
             float e = 0.0f, f = 0.0f;
-            if (i0 + lane < rq.n) {
+            if (i0 + lane < end) {
                 const int64_t at = rq.first + i0 + lane, row = at * p.H + h;
                 const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
                 const T* g = (const T*)p.G + row * p.D;
                 float s = 0.0f, u = 0.0f;
                 for (int d = 0; d < p.D; ++d) { s = fmaf(words[d], load_one(q + d), s); u = fmaf(v[d], load_one(g + d), u); }
-                e = exp_near(s * p.scale - p.lse[row]);
+                e = __builtin_amdgcn_exp2f((s * p.scale - p.lse[row]) * kLog2e);
                 f = e * (u - p.delta[row]);
             }
             wp[lane] = e;
             ws[lane] = f;
             wave_words_done();
-            for (int j = 0; j < 64 && i0 + j < rq.n; ++j) {
+            for (int j = 0; j < 64 && i0 + j < end; ++j) {
                 const int64_t at = rq.first + i0 + j;
                 const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
                 const T* g = (const T*)p.G + (at * p.H + h) * p.D;
@@ -181,6 +173,16 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
                     }
             }
         }
+    if (slice >= 0) {
+        const int64_t rows = (int64_t)p.Tk * p.KV, to = slice * rows + (int64_t)t * p.KV + kv;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (lane + 64 * x < p.D) {
+                p.part[to * p.D + lane + 64 * x] = dk[x] * p.scale;
+                p.part[(p.slices * rows + to) * p.D + lane + 64 * x] = dv[x];
+            }
+        return;
+    }
 #pragma unroll
     for (int x = 0; x < 2; ++x)
         if (lane + 64 * x < p.D) {
@@ -191,37 +193,40 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams p) {
-    constexpr int QT = sizeof(T) == 2 ? 64 : 32, QB = QT / 32, KC = DP / 16, DT = DP / 32;
+    constexpr int QT = kStep<T>, QB = QT / 32, KC = DP / 16, DT = DP / 32;
     constexpr bool PIPE = !(DIRECT && sizeof(T) == 2 && DP <= 64);
     constexpr int TILE = QT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of queries and their outputs' gradients
     __shared__ __attribute__((aligned(16))) float side[2][2][QT];                    // -lse in units of log 2, rowsum(G * O)
-    if ((int)blockIdx.x >= p.units) {
+    if ((int)blockIdx.x >= p.units * p.slices) {
         const CodeFmt none = {};
-        clear_rows(p.starts_k, p.Tk, p.count, blockIdx.x - p.units, kClearBlocks, (T*)p.dK, p.dk.row, p.dk.head, p.KV, p.D, (float*)nullptr, none);
-        clear_rows(p.starts_k, p.Tk, p.count, blockIdx.x - p.units, kClearBlocks, (T*)p.dV, p.dv.row, p.dv.head, p.KV, p.D, (float*)nullptr, none);
+        clear_rows(p.starts_k, p.Tk, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, (T*)p.dK, p.dk.row, p.dk.head, p.KV, p.D, (float*)nullptr, none);
+        clear_rows(p.starts_k, p.Tk, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, (T*)p.dV, p.dv.row, p.dv.head, p.KV, p.D, (float*)nullptr, none);
         return;
     }
-    const int unit = unit_of(blockIdx.x, p.units), kv = unit / p.tiles;
+    const int unit = unit_of(blockIdx.x % p.units, p.units), kv = unit / p.tiles, slice = blockIdx.x / p.units;
     const TileOf at = find_tile(p.starts_k, p.Tk, p.count, kTileRows, unit % p.tiles);           // earlier tiles, which more queries see, first
     if (at.b < 0) return;
     const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
-    const int ahead = rk.n - rq.n;
-    auto first_of = [&](int j) { return p.causal ? max(0, j - ahead) : 0; };                     // the first query that sees key j
+    auto first_of = [&](int j) { return first_query(p, rq, rk, j); };
     const int j0 = at.t * kTileRows + wave * 32, j = j0 + (lane & 31);
     const bool there = j < rk.n;
     const int lo = first_of(j), lo_wave = first_of(j0), lo_last = first_of(j0 + 31), lo_all = first_of(at.t * kTileRows);
-    const int t0 = lo_all / QT, steps_head = rq.n > lo_all ? (rq.n + QT - 1) / QT - t0 : 0, steps = steps_head * p.group;
+    const int t0 = lo_all / QT, steps_head = steps_of_keys(p, rq, rk, at.t, QT);                // tiles of queries of a head; a step is one of a head of the group
+    const Slice part = slice_of(steps_head * p.group, p.slices, slice);
+    const int steps = part.last;
+    if (part.first >= steps && slice > 0) return;
     const int masked_all = first_of(at.t * kTileRows + kTileRows - 1);                           // from this query on, all of the workgroup's keys are seen
 
     Loader<T, DP, QT, DIRECT> lq, lg;
     float side_next = 0.0f;                              // lane t of the first two waves: query t % QT of the step's lse or sum
     bool side_there = false;
-    int next_tile = 0, next_head = 0;
+    int next_tile = part.first % max(1, steps_head), next_head = part.first / max(1, steps_head);
+    bool fresh_head = true;
     auto load = [&](int buf) {                           // the step after those that have been loaded
         const int h = kv * p.group + next_head, q0 = (t0 + next_tile) * QT;
-        if (next_tile == 0) {
+        if (fresh_head) {
             lq.start((const T*)p.Q + (int64_t)(rq.first + q0) * p.q.row + (int64_t)h * p.q.head, p.q.row, p.D);
             lg.start((const T*)p.G + ((int64_t)(rq.first + q0) * p.H + h) * p.D, (int64_t)p.H * p.D, p.D);
         }
@@ -234,9 +239,10 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
             side_next = from[i < rq.n ? row : (int64_t)rq.first * p.H];              // (used only where it is put down: nothing waits for it here)
             side_there = i < rq.n;
         }
-        if (++next_tile == steps_head) { next_tile = 0; ++next_head; }
+        fresh_head = ++next_tile == steps_head;
+        if (fresh_head) { next_tile = 0; ++next_head; }
     };
-    if (steps > 0) load(0);
+    if (steps > part.first) load(0);
     Frag<T> k[KC], v[KC];
     load_frags<T, DP>((const T*)p.K + (int64_t)(rk.first + j) * p.k.row + (int64_t)kv * p.k.head, there, p.D, half, k);
     load_frags<T, DP>((const T*)p.V + (int64_t)(rk.first + j) * p.v.row + (int64_t)kv * p.v.head, there, p.D, half, v);
@@ -245,13 +251,13 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     f32x16 dk[DT], dv[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) { dk[t] = f32x16{}; dv[t] = f32x16{}; }
-    int n = 0;                                           // steps that are done
+    int n = part.first;                                  // steps that are done
     bool broken = false;                                 // a tile that some key sees in part holds infinities or NaN
     // One tile of queries.  EDGE: some key may not be seen by all of them.  PIPE: the products of one block of 32 queries run while the weights of the
     // other are worked out, since a wave that is alone on its SIMD has only its own instructions to fill it; else two waves share it.
     auto step = [&](int tile, auto edge) {
         constexpr bool EDGE = decltype(edge)::value != 0;
-        const int q0 = (t0 + tile) * QT, buf = n & 1;
+        const int q0 = (t0 + tile) * QT, buf = (n - part.first) & 1;
         uint8_t* const tq = lds[buf][0];
         uint8_t* const tg = lds[buf][1];
         lq.put(tq);
@@ -358,27 +364,63 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     };
     // of every head the steps at the edge, then those that all the workgroup's keys are seen by
     const int edge = max(0, min(steps_head, (masked_all + QT - 1) / QT - t0));
-    for (int h = 0; h < p.group && steps_head > 0 && !broken; ++h) {
-        for (int tile = 0; tile < edge && !broken; ++tile) step(tile, Known<1>{});
-        for (int tile = edge; tile < steps_head && !broken; ++tile) step(tile, Known<0>{});
+    while (n < steps && !broken) {
+        const int tile = n % steps_head, head = n - tile;
+        for (int last = min(steps, head + edge); n < last && !broken;) step(n - head, Known<1>{});
+        for (int last = min(steps, head + steps_head); n < last && !broken;) step(n - head, Known<0>{});
     }
     if (broken) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
-        for (int x = 0; x < 32 && j0 + x < rk.n; ++x) dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x));
+        for (int x = 0; x < 32 && j0 + x < rk.n; ++x) 
+            dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x), part.first, steps, steps_head, t0 * QT, QT, part.alone ? -1 : slice);
         return;
     }
     if (!there) return;
+    if (!part.alone) {
+        const int64_t rows = (int64_t)p.Tk * p.KV, to = slice * rows + (int64_t)(rk.first + j) * p.KV + kv;
+        store_columns(p.part + to * p.D, dk, p.scale, p.D, half);
+        store_columns(p.part + (p.slices * rows + to) * p.D, dv, 1.0f, p.D, half);
+        return;
+    }
     store_columns((T*)p.dK + (int64_t)(rk.first + j) * p.dk.row + (int64_t)kv * p.dk.head, dk, p.scale, p.D, half);
     store_columns((T*)p.dV + (int64_t)(rk.first + j) * p.dv.row + (int64_t)kv * p.dv.head, dv, 1.0f, p.D, half);
 }
 
+// Gradients from the parts: a workgroup a row, a lane an element of its heads.  KEYS: dK, and blockIdx.y == 1: dV; else dQ.
+template <typename T, bool KEYS> __global__ __launch_bounds__(256) void attn_join_grad_kernel(AttnParams p) {
+    const int heads = KEYS ? p.KV : p.H, total = KEYS ? p.Tk : p.T;
+    const int64_t all = (int64_t)total * heads * p.D;
+    const float* part = p.part + blockIdx.y * p.slices * all;
+    T* out = (T*)(!KEYS ? p.dQ : blockIdx.y ? p.dV : p.dK);
+    const lba_strides at = !KEYS ? p.dq : blockIdx.y ? p.dv : p.dk;
+    const CodeFmt none = {};
+    for (int t = blockIdx.x; t < total; t += gridDim.x) {
+        const int b = KEYS ? sequence_of(p.starts_k, p.Tk, p.count, t) : sequence_of(p.starts, p.T, p.count, t);
+        if (b < 0) continue;
+        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const int steps = KEYS ? steps_of_keys(p, rq, rk, (t - rk.first) / kTileRows, kStep<T>) * p.group : steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>);
+        const int n = slices_used(steps, p.slices);
+        if (n <= 1) continue;                            // stored by its only workgroup
+        for (int i = threadIdx.x; i < heads * p.D; i += 256) {
+            float v = 0.0f;
+            for (int x = 0; x < n; ++x) v += part[x * all + (int64_t)t * heads * p.D + i];
+            store_one(out + (int64_t)t * at.row + (int64_t)(i / p.D) * at.head + i % p.D, v, none);
+        }
+    }
+}
+template <typename T, bool KEYS> void launch_join_grad(const AttnParams& p, hipStream_t st) {
+    const int rows = KEYS ? p.Tk : p.T;
+    hipLaunchKernelGGL((attn_join_grad_kernel<T, KEYS>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20)), KEYS ? 2 : 1), dim3(256), 0, st, p);
+}
+
 template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipStream_t st) {
-    const dim3 grid((unsigned)(p.units + (p.clear && p.starts ? kClearBlocks : 0)));
+    const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
+        if (p.slices > 1) launch_join_grad<T, false>(p, st); \
         return; \
     }
     LBA_ATTN(32)
@@ -388,11 +430,12 @@ template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipS
 #undef LBA_ATTN
 }
 template <typename T> void launch_attn_dkv(const AttnParams& p, bool direct, hipStream_t st) {
-    const dim3 grid((unsigned)(p.units + (p.clear && p.starts_k ? kClearBlocks : 0)));
+    const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts_k ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_dkv_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dkv_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
+        if (p.slices > 1) launch_join_grad<T, true>(p, st); \
         return; \
     }
     LBA_ATTN(32)

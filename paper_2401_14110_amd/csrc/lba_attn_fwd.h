@@ -18,8 +18,16 @@ template <typename F> __device__ __forceinline__ void with_output(const AttnPara
     else store((uint8_t*)p.O);
 }
 
-// One query by one wave, over the `seen` keys from row k0 on and nothing else: a lane a key, then a lane two columns.  words: 192 of LDS.
-template <typename T> __device__ __forceinline__ void attn_row(const AttnParams& p, float* words, int h, int kv, int t, int k0, int seen) {
+// a part's maximum, in units of log 2, and sum of weights
+__device__ __forceinline__ void store_end(const AttnParams& p, int64_t to, float top, float sum) {
+    float* end = p.part + (int64_t)p.slices * p.T * p.H * p.D + to * 2;
+    end[0] = top;
+    end[1] = sum;
+}
+
+// One query by one wave, over the `seen` keys from row k0 on and nothing else: a lane a key, then a lane two columns.  words: 192 of LDS.  slice: -1
+// where these are all its keys.
+template <typename T> __device__ __forceinline__ void attn_row(const AttnParams& p, float* words, int h, int kv, int t, int k0, int seen, int slice) {
     const int lane = threadIdx.x & 63;
     const int64_t row = (int64_t)t * p.H + h;
     float* const w = words + 128;
@@ -33,10 +41,10 @@ template <typename T> __device__ __forceinline__ void attn_row(const AttnParams&
             const T* k = (const T*)p.K + (int64_t)(k0 + j0 + lane) * p.k.row + (int64_t)kv * p.k.head;
             s = 0.0f;
             for (int d = 0; d < p.D; ++d) s = fmaf(words[d], load_one(k + d), s);
-            s *= p.scale;
+            s *= p.scale * 1.44269504f;
         }
         const float now = fmaxf(wave_max(s), top), base = now == -__builtin_inff() ? 0.0f : now;
-        const float e = j0 + lane < seen ? exp_near(s - base) : 0.0f, f = exp_near(top - base);
+        const float e = j0 + lane < seen ? __builtin_amdgcn_exp2f(s - base) : 0.0f, f = __builtin_amdgcn_exp2f(top - base);
         top = now;
         sum = sum * f + wave_sum(e);
         w[lane] = e;
@@ -50,42 +58,51 @@ template <typename T> __device__ __forceinline__ void attn_row(const AttnParams&
                 if (lane + 64 * x < p.D) acc[x] = fmaf(w[j], load_one(v + lane + 64 * x), acc[x]);
         }
     }
+    if (slice >= 0) {
+        const int64_t to = (int64_t)slice * p.T * p.H + row;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (lane + 64 * x < p.D) p.part[to * p.D + lane + 64 * x] = acc[x];
+        if (lane == 0) store_end(p, to, top, sum);
+        return;
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     with_output(p, [&](auto* o) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
             if (lane + 64 * x < p.D) store_one(o + row * p.D + lane + 64 * x, acc[x] * inv, p.fmt);
     });
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(sum) * 0.693147181f;
+    if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
 }
 
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnParams p) {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, KB = KT / 32, KC = DP / 16, DT = DP / 32;
+    constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
     constexpr int TILE = KT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
-    if ((int)blockIdx.x >= p.units) {
-        with_output(p, [&](auto* o) { clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units, kClearBlocks, o, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt); });
+    if ((int)blockIdx.x >= p.units * p.slices) {
+        with_output(p, [&](auto* o) { clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, o, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt); });
         return;
     }
-    const int unit = unit_of(blockIdx.x, p.units), per = p.tiles * p.group;
+    const int unit = unit_of(blockIdx.x % p.units, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
     const TileOf at = find_tile(p.starts, p.T, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);               // later tiles of a sequence, which see more, first
     if (at.b < 0) return;
     const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
-    const int ahead = rk.n - rq.n;
-    auto limit = [&](int i) { return p.causal ? max(0, min(rk.n, i + ahead + 1)) : rk.n; };                          // keys that query i sees
+    auto limit = [&](int i) { return keys_seen(p, rq, rk, i); };
     const int i0 = at.t * kTileRows + wave * 32, i = i0 + (lane & 31);
     const int lim = limit(i), least = limit(i0), most = i0 < rq.n ? limit(min(i0 + 31, rq.n - 1)) : 0;
-    const int tiles = (limit(min(at.t * kTileRows + kTileRows, rq.n) - 1) + KT - 1) / KT, least_all = limit(at.t * kTileRows);
+    const Slice part = slice_of(steps_of_queries(p, rq, rk, at.t, KT), p.slices, slice);
+    const int first = part.first, tiles = part.last, least_all = limit(at.t * kTileRows);
+    if (first >= tiles && slice > 0) return;
 
     Loader<T, DP, KT, DIRECT> lk, lv;
-    lk.start((const T*)p.K + (int64_t)rk.first * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
-    lv.start((const T*)p.V + (int64_t)rk.first * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
-    if (tiles > 0) {
-        lk.load(lds[0][0], rk.n);
-        lv.load(lds[0][1], rk.n);
+    lk.start((const T*)p.K + (int64_t)(rk.first + first * KT) * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
+    lv.start((const T*)p.V + (int64_t)(rk.first + first * KT) * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
+    if (tiles > first) {
+        lk.load(lds[0][0], rk.n - first * KT);
+        lv.load(lds[0][1], rk.n - first * KT);
     }
     Frag<T> q[KC];
     load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, i < rq.n, p.D, half, q);
@@ -185,7 +202,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
             }
     };
     const int whole = min(tiles, least_all / KT);
-    int kt = 0;
+    int kt = first;
     for (; kt + 1 < whole; kt += 2) {
         step(kt, Known<0>{}, Known<0>{});
         step(kt + 1, Known<0>{}, Known<1>{});
@@ -197,13 +214,22 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     if (broken) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
-        for (int j = 0; j < 32 && i0 + j < rq.n; ++j) attn_row<T>(p, (float*)&lds[0][0][0] + wave * 192, h, kv, rq.first + i0 + j, rk.first, limit(i0 + j));
+        for (int j = 0; j < 32 && i0 + j < rq.n; ++j) {
+            const int seen = min(limit(i0 + j), tiles * KT) - first * KT;
+            attn_row<T>(p, (float*)&lds[0][0][0] + wave * 192, h, kv, rq.first + i0 + j, rk.first + first * KT, seen, part.alone ? -1 : slice);
+        }
         return;
     }
     sum = sum_of_halves(sum);
     if (i >= rq.n) return;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;
+    if (!part.alone) {
+        const int64_t rows = (int64_t)p.T * p.H, to = slice * rows + row;
+        store_columns(p.part + to * p.D, acc, 1.0f, p.D, half);
+        if (half == 0) store_end(p, to, top, sum);
+        return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     if (p.lse && half == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
     with_output(p, [&](auto* o) {
 #pragma unroll
@@ -217,12 +243,39 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     });
 }
 
+// O and lse from the parts: a workgroup a row, a lane an element of its heads.
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+    const int64_t rows = (int64_t)p.T * p.H;
+    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
+        const int b = sequence_of(p.starts, p.T, p.count, t);
+        if (b < 0) continue;
+        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const int n = slices_used(steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>), p.slices);
+        if (n <= 1) continue;                            // stored by its only workgroup
+        for (int i = threadIdx.x; i < p.H * p.D; i += 256) {
+            const int64_t row = (int64_t)t * p.H + i / p.D;
+            const float* end = p.part + p.slices * rows * p.D + row * 2;
+            float top = -__builtin_inff(), sum = 0.0f, v = 0.0f;
+            for (int x = 0; x < n; ++x) top = fmaxf(top, end[x * rows * 2]);
+            const float base = top == -__builtin_inff() ? 0.0f : top;
+            for (int x = 0; x < n; ++x) {
+                const float f = __builtin_amdgcn_exp2f(end[x * rows * 2] - base);
+                sum = fmaf(f, end[x * rows * 2 + 1], sum);
+                v = fmaf(f, p.part[x * rows * p.D + row * p.D + i % p.D], v);
+            }
+            with_output(p, [&](auto* o) { store_one(o + (int64_t)t * p.H * p.D + i, sum == 0.0f ? 0.0f : v / sum, p.fmt); });
+            if (p.lse && i % p.D == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
+        }
+    }
+}
+
 template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st) {
-    const dim3 grid((unsigned)(p.units + (p.clear && p.starts ? kClearBlocks : 0)));
+    const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
+        if (p.slices > 1) hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(p.T < (1 << 20) ? p.T : (1 << 20))), dim3(256), 0, st, p); \
         return; \
     }
     LBA_ATTN(32)

@@ -257,6 +257,19 @@ template <typename T, int DP> __device__ __forceinline__ void load_frags(const v
     }
 }
 
+// registers 4 g .. 4 g + 3 of column tiles, times f, to a row
+template <typename T, int DT> __device__ __forceinline__ void store_columns(T* row, const f32x16 (&acc)[DT], float f, int D, int half) {
+    const CodeFmt none = {};
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * t + 8 * g + 4 * half;
+            const float v[4] = {acc[t][4 * g] * f, acc[t][4 * g + 1] * f, acc[t][4 * g + 2] * f, acc[t][4 * g + 3] * f};
+            if (d < D) store_some<4>(row + d, D - d, v, none);
+        }
+}
+
 // the larger of a value's copies in lanes l and l ^ 32, and their sum: of the exchange's two results one is the wave's lower half twice, the other its
 // upper half
 __device__ __forceinline__ float max_of_halves(float v) {
@@ -315,6 +328,32 @@ __device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, int co
     }
     return {-1, 0};
 }
+// Part `slice` of what a workgroup does in n steps, cut into at most `slices` parts of two steps or more: steps first .. last - 1 (none in some of
+// the later ones), `alone` where one part has them all.
+struct Slice {
+    int first, last;
+    bool alone;
+};
+__device__ __forceinline__ int slice_steps(int n, int slices) { return max(2, (n + slices - 1) / slices); }
+__device__ __forceinline__ Slice slice_of(int n, int slices, int slice) {
+    const int per = slice_steps(n, slices);
+    return {min(n, slice * per), min(n, slice * per + per), n <= per};
+}
+__device__ __forceinline__ int slices_used(int n, int slices) { return (n + slice_steps(n, slices) - 1) / slice_steps(n, slices); }
+
+// how many keys query i of a sequence sees, and the first query that sees key j
+__device__ __forceinline__ int keys_seen(const AttnParams& p, const Rows& rq, const Rows& rk, int i) { return p.causal ? max(0, min(rk.n, i + rk.n - rq.n + 1)) : rk.n; }
+__device__ __forceinline__ int first_query(const AttnParams& p, const Rows& rq, const Rows& rk, int j) { return p.causal ? max(0, j - (rk.n - rq.n)) : 0; }
+// steps of a tile of queries over tiles of `size` keys, and of a tile of keys over tiles of `size` queries of one head
+__device__ __forceinline__ int steps_of_queries(const AttnParams& p, const Rows& rq, const Rows& rk, int t, int size) {
+    return (keys_seen(p, rq, rk, min(t * kTileRows + kTileRows, rq.n) - 1) + size - 1) / size;
+}
+__device__ __forceinline__ int steps_of_keys(const AttnParams& p, const Rows& rq, const Rows& rk, int t, int size) {
+    const int lo = first_query(p, rq, rk, t * kTileRows);
+    return rq.n > lo ? (rq.n + size - 1) / size - lo / size : 0;
+}
+template <typename T> constexpr int kStep = sizeof(T) == 2 ? 64 : 32;                // keys or queries of a step
+
 // how many tiles there may be
 inline int64_t most_tiles(const int32_t* starts, int64_t T, int64_t count, int size) {
     if (count < 1 || T < 1) return 0;

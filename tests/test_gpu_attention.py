@@ -331,8 +331,8 @@ def desc(**k):
 
 def test_refusals():
     P, W, f, s = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x2000), (4, 3, 7), lb.lba_strides(64, 16)
-    call = lambda a=None, **k: lb.lba_attention(*{**dict(a=a or desc(), Q=P, K=P, V=P, O=P, t=0, f=f, lse=None), **k}.values())  # noqa: E731
-    need = lb.lba_attention_bwd_workspace_bytes(8, 4)
+    call = lambda a=None, **k: lb.lba_attention(*{**dict(a=a or desc(), Q=P, K=P, V=P, O=P, t=0, f=f, lse=None, ws=None, n=0), **k}.values())  # noqa: E731
+    need = lb.lba_attention_bwd_workspace_bytes(desc())
     assert need >= 8 * 4 * 4
     back = lambda a=None, **k: lb.lba_attention_bwd(*{**dict(a=a or desc(), G=P, Q=P, K=P, V=P, O=P, lse=P, dQ=P, qa=s, dK=P, ka=s, dV=P, va=s, ws=W, n=need), **k}.values())  # noqa: E731
     for fn in (call, back):
