@@ -991,20 +991,30 @@ def dense_bwd(G, A, B, fmt_a=_E4M3, fmt_b=_E4M3, bias=None, act=ACT_NONE, drop=N
 
 def _heads(t, what, on, device=None, dtype=None):
     """(t as [rows, heads, D] with D along memory, its strides) of an input."""
-    if t.dtype not in _REAL or t.get_device() < 0 or (dtype is not None and (t.dtype != dtype or t.get_device() != device)):
+    if (t.dtype is not dtype or t.get_device() != device) if dtype is not None else (t.dtype not in _REAL or t.get_device() < 0):
         raise TypeError("%s must be a tensor of %s on %s device" % (what, dtype or "torch.float32 or torch.bfloat16", "a" if dtype is None else "the call's"))
+    if t.dim() == 3:
+        row, head, step = t.stride()
+        if step == 1 or t.size(2) == 1:
+            return t, (row, head)
+        t = _whole(t, on)
+        return t, t.stride()[:2]
     if t.dim() < 3:
         raise ValueError("%s must be [rows, heads, D] or have more leading axes" % what)
-    if t.dim() > 3 or (t.stride(-1) != 1 and t.size(-1) != 1):
-        shape = (math.prod(t.shape[:-2]),) + tuple(t.shape[-2:])
-        try:
-            v = t.view(shape)
-        except RuntimeError:
-            v = None
-        if v is None or (v.stride(2) != 1 and shape[2] != 1):
-            v = _whole(t, on).view(shape) if not t.is_contiguous() else t.view(shape)
-        t = v
-    return t, lba_strides(t.stride(0), t.stride(1))
+    shape = (math.prod(t.shape[:-2]),) + tuple(t.shape[-2:])
+    try:
+        v = t.view(shape)
+    except RuntimeError:
+        v = None
+    if v is None or (v.stride(2) != 1 and shape[2] != 1):
+        v = _whole(t, on).view(shape)
+    return v, v.stride()[:2]
+
+
+def _heads_made(t):
+    """The same of a contiguous output that the call has made."""
+    n = t.dim()
+    return t, (t.stride(n - 3), t.stride(n - 2))
 
 
 def _heads_out(t, like, what):
@@ -1012,10 +1022,12 @@ def _heads_out(t, like, what):
     if t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape != like.shape:
         raise ValueError("%s must be a tensor %s of %s on the call's device" % (what, tuple(like.shape), like.dtype))
     try:
-        v = t.view((math.prod(t.shape[:-2]),) + tuple(t.shape[-2:]))
+        v = t.view((math.prod(t.shape[:-2]),) + tuple(t.shape[-2:])) if t.dim() != 3 else t
     except RuntimeError:
         raise ValueError("%s must be a view whose leading axes are one in memory" % what) from None
     (T, H, D), (r, h, d) = v.shape, v.stride()
+    if d != 1 and D > 1:
+        raise ValueError("%s must have its last axis along memory" % what)
     inner, outer = ((H, h), (T, r)) if h <= r or T <= 1 else ((T, r), (H, h))
     end = D
     for n, step in (inner, outer):
@@ -1023,9 +1035,12 @@ def _heads_out(t, like, what):
             if step < end:
                 raise ValueError("%s has elements that share a place" % what)
             end = (n - 1) * step + end
-    if d != 1 and D > 1:
-        raise ValueError("%s must have its last axis along memory" % what)
-    return v, lba_strides(r, h)
+    return v, (r, h)
+
+
+def _made(t, dtype, on):
+    """A contiguous tensor of t's shape."""
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format) if on is None else _empty(t.shape, dtype, t.device, on)
 
 
 def _starts(t, device, what, on):
@@ -1043,15 +1058,16 @@ def _rope(fn, x, positions, freq, interleaved, gain, out, stream):
     handle, on = _on(stream, device)
     v, at = _heads(x, "x", on)
     T, H, D = v.shape
+    at = lba_strides(*at)
     if positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != device or positions.shape != x.shape[:-2]:
         raise ValueError("positions must be an int32 or int64 tensor %s on the call's device" % (tuple(x.shape[:-2]),))
     if freq.dtype != torch.float64 or freq.get_device() != device or freq.dim() != 1 or 2 * freq.numel() > D:
         raise ValueError("freq must be a float64 tensor of at most %d elements on the call's device" % (D // 2))
     positions, freq = _whole(positions, on), _whole(freq, on)
-    y = _empty(x.shape, x.dtype, x.device, on) if out is None else out
-    w, y_at = _heads_out(y, x, "out")
-    _check(fn(_at(v), at, _TYPE[x.dtype], _at(positions), 8 * positions.element_size(), _at(freq), freq.numel(), interleaved, gain, _at(w), y_at, T, H, D,
-              handle))
+    y = _made(x, x.dtype, on) if out is None else out
+    w, y_at = _heads_made(y) if out is None else _heads_out(y, x, "out")
+    _check(fn(_at(v), at, _TYPE[x.dtype], _at(positions), 64 if positions.dtype is torch.int64 else 32, _at(freq), freq.numel(), interleaved, gain, _at(w),
+              lba_strides(*y_at), T, H, D, handle))
     return y
 
 
@@ -1069,9 +1085,10 @@ def rope_bwd(G, positions, freq, interleaved=False, gain=1.0, out=None, stream=N
 
 def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
     """(lba_attn, what it points to) of a call."""
-    if q.dim() not in (3, 4) or k.dim() != q.dim() or k.shape != v.shape or k.shape[-1] != q.shape[-1]:
+    n, qs, ks = q.dim(), q.shape, k.shape
+    if n not in (3, 4) or len(ks) != n or ks != v.shape or ks[-1] != qs[-1]:
         raise ValueError("q must be [rows, heads, D] or [batch, length, heads, D], k and v alike")
-    H, KV, D = q.shape[-2], k.shape[-2], q.shape[-1]
+    H, KV, D = qs[-2], ks[-2], qs[-1]
     if H and (not KV or H % KV):
         raise ValueError("%d query heads do not share %d heads of keys" % (H, KV))
     if not 1 <= D <= 128:
@@ -1079,21 +1096,25 @@ def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
     if starts is None:
         if starts_k is not None:
             raise ValueError("starts_k needs starts")
-        count = q.shape[0] if q.dim() == 4 else 1
-        if q.dim() == 4 and k.shape[0] != count:
+        count = qs[0] if n == 4 else 1
+        if n == 4 and ks[0] != count:
             raise ValueError("q and k have different batches")
     else:
-        if q.dim() != 3:
+        if n != 3:
             raise ValueError("packed sequences are [rows, heads, D]")
-        starts, starts_k = _starts(starts, device, "starts", on), _starts(starts_k, device, "starts_k", on)
+        starts = _starts(starts, device, "starts", on)
         count = starts.numel() - 1
-        if starts_k is None and k.shape[0] != q.shape[0]:
-            raise ValueError("q and k have different rows: starts_k is needed")
-        if starts_k is not None and starts_k.numel() != count + 1:
-            raise ValueError("starts and starts_k are of different sequences")
-    (q, q_at), (k, k_at), (v, v_at) = _heads(q, "q", on), _heads(k, "k", on, device, q.dtype), _heads(v, "v", on, device, q.dtype)
-    a = lba_attn(q.shape[0], k.shape[0], count, _at(starts), _at(starts_k), H, KV, D, _TYPE[q.dtype], causal, clear,
-                 D ** -0.5 if scale is None else scale, q_at, k_at, v_at)
+        if starts_k is None:
+            if ks[0] != qs[0]:
+                raise ValueError("q and k have different rows: starts_k is needed")
+        else:
+            starts_k = _starts(starts_k, device, "starts_k", on)
+            if starts_k.numel() != count + 1:
+                raise ValueError("starts and starts_k are of different sequences")
+    dtype = q.dtype
+    (q, q_at), (k, k_at), (v, v_at) = _heads(q, "q", on), _heads(k, "k", on, device, dtype), _heads(v, "v", on, device, dtype)
+    a = lba_attn(q.size(0), k.size(0), count, _at(starts), _at(starts_k), H, KV, D, _TYPE[dtype], causal, clear, D ** -0.5 if scale is None else scale,
+                 q_at, k_at, v_at)
     return a, (q, k, v, starts, starts_k)
 
 
@@ -1120,7 +1141,7 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
         raise TypeError("q must be a device tensor")
     handle, on = _on(stream, device)
     a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
-    o = _empty(q.shape, dtype, q.device, on) if out is None else _output(out, q, q.shape, dtype, on)
+    o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
     size = _attn_bytes("lba_attention_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
@@ -1140,12 +1161,16 @@ def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, s
     handle, on = _on(stream, device)
     a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
     G, o, lse = _whole(G, on), _whole(o, on), _whole(lse, on)
-    got = tuple(_empty(t.shape, t.dtype, t.device, on) for t in (q, k, v)) if out is None else tuple(out)
-    (dq, dq_at), (dk, dk_at), (dv, dv_at) = (_heads_out(t, w, n) for t, w, n in zip(got, (q, k, v), ("dq", "dk", "dv")))
+    if out is None:
+        got = (_made(q, q.dtype, on), _made(k, k.dtype, on), _made(v, v.dtype, on))
+        (dq, dq_at), (dk, dk_at), (dv, dv_at) = (_heads_made(t) for t in got)
+    else:
+        got = tuple(out)
+        (dq, dq_at), (dk, dk_at), (dv, dv_at) = (_heads_out(t, w, n) for t, w, n in zip(got, (q, k, v), ("dq", "dk", "dv")))
     size = _attn_bytes("lba_attention_bwd_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_attention_bwd(a, _at(G), _at(q3), _at(k3), _at(v3), _at(o), _at(lse), _at(dq), dq_at, _at(dk), dk_at, _at(dv), dv_at, _at(ws), size,
-                                   handle))
+    _check(lib().lba_attention_bwd(a, _at(G), _at(q3), _at(k3), _at(v3), _at(o), _at(lse), _at(dq), lba_strides(*dq_at), _at(dk),
+                                   lba_strides(*dk_at), _at(dv), lba_strides(*dv_at), _at(ws), size, handle))
     return got
 
 
@@ -1167,18 +1192,22 @@ def kv_cache(pages, page, heads, D, device="cuda"):
 
 def _cache4(cache, table, lens, device, on):
     """(lba_cache4, what it points to)."""
-    shape = cache.k.shape
-    if len(shape) != 4 or shape[3] % 16 or not 16 <= shape[3] <= 64:
-        raise ValueError("a cache's codes are [pages, heads, page, D / 2] with D 32, 64, 96 or 128")
-    for t, n in zip(cache, (shape[3], shape[3] // 16) * 2):
-        if t.dtype != torch.uint8 or t.get_device() != device or t.shape != shape[:3] + (n,) or not t.is_contiguous():
-            raise ValueError("a cache's tensors are contiguous torch.uint8 on the call's device, codes [..., D / 2] and powers [..., D / 32]")
-    if table.dtype != torch.int32 or table.get_device() != device or table.dim() != 2:
+    k, k_scale, v, v_scale = cache
+    shape, powers = k.shape, k_scale.shape
+    if len(shape) != 4 or shape[3] % 16 or not 16 <= shape[3] <= 64 or powers != shape[:3] + (shape[3] // 16,):
+        raise ValueError("a cache's codes are [pages, heads, page, D / 2] with D 32, 64, 96 or 128, its powers [pages, heads, page, D / 32]")
+    if v.shape != shape or v_scale.shape != powers:
+        raise ValueError("a cache's keys and values are of one shape")
+    for t in cache:
+        if t.dtype is not torch.uint8 or t.get_device() != device or not t.is_contiguous():
+            raise ValueError("a cache's tensors are contiguous torch.uint8 on the call's device")
+    if table.dtype is not torch.int32 or table.get_device() != device or table.dim() != 2:
         raise ValueError("table must be an int32 tensor [sequences, pages of each] on the call's device")
-    if lens.dtype != torch.int32 or lens.get_device() != device or lens.shape != table.shape[:1]:
+    count, row = table.shape
+    if lens.dtype is not torch.int32 or lens.get_device() != device or lens.dim() != 1 or lens.size(0) != count:
         raise ValueError("lens must be an int32 tensor [sequences] on the call's device")
     table, lens = _whole(table, on), _whole(lens, on)
-    c = lba_cache4(*[_at(t) for t in cache], shape[0], table.shape[1], table.shape[0], _at(table), _at(lens), shape[2], shape[1], 2 * shape[3])
+    c = lba_cache4(_at(k), _at(k_scale), _at(v), _at(v_scale), shape[0], row, count, _at(table), _at(lens), shape[2], shape[1], 2 * shape[3])
     return c, (table, lens)
 
 
@@ -1207,7 +1236,7 @@ def cache_write(k, v, cache, table, starts, lens, stream=None):
     if tuple(k.shape[-2:]) != (c.KV, c.D):
         raise ValueError("k and v must be [rows, %d, %d]" % (c.KV, c.D))
     (k3, k_at), (v3, v_at) = _heads(k, "k", on), _heads(v, "v", on, device, k.dtype)
-    _check(lib().lba_cache_write(c, _at(starts), k3.shape[0], _at(k3), k_at, _at(v3), v_at, _TYPE[k.dtype], handle))
+    _check(lib().lba_cache_write(c, _at(starts), k3.size(0), _at(k3), lba_strides(*k_at), _at(v3), lba_strides(*v_at), _TYPE[k.dtype], handle))
 
 
 def cache_read(cache, table, starts, lens, rows, out_dtype=torch.bfloat16, out=None, stream=None):
@@ -1227,14 +1256,16 @@ def cache_read(cache, table, starts, lens, rows, out_dtype=torch.bfloat16, out=N
     else:
         starts = _cache_starts(starts, c.count, (rows, c.KV, c.D), device, on)
     shape = (rows, c.KV, c.D)
-    got = tuple(_empty(shape, out_dtype, cache.k.device, on) for _ in range(2)) if out is None else tuple(out)
-    for t in got:
-        if tuple(t.shape) != shape or t.dtype != out_dtype:
-            raise ValueError("out must be two tensors %s of %s" % (shape, out_dtype))
-    (k3, k_at), (v3, v_at) = (_heads_out(t, got[0], "out") for t in got)
-    if k3.get_device() != device:
-        raise ValueError("out must be on the call's device")
-    _check(lib().lba_cache_read(c, _at(starts), rows, _at(k3), k_at, _at(v3), v_at, _TYPE[out_dtype], out is None, handle))
+    if out is None:
+        got = (_empty(shape, out_dtype, cache.k.device, on), _empty(shape, out_dtype, cache.k.device, on))
+        (k3, k_at), (v3, v_at) = (_heads_made(t) for t in got)
+    else:
+        got = tuple(out)
+        for t in got:
+            if tuple(t.shape) != shape or t.dtype != out_dtype or t.get_device() != device:
+                raise ValueError("out must be two tensors %s of %s on the call's device" % (shape, out_dtype))
+        (k3, k_at), (v3, v_at) = (_heads_out(t, got[0], "out") for t in got)
+    _check(lib().lba_cache_read(c, _at(starts), rows, _at(k3), lba_strides(*k_at), _at(v3), lba_strides(*v_at), _TYPE[out_dtype], out is None, handle))
     return got
 
 
@@ -1256,9 +1287,9 @@ def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=N
         raise ValueError("%d query heads do not share %d heads of keys" % (H, c.KV))
     fresh = q.shape[1] if q.dim() == 4 else 1
     q3, q_at = _heads(q, "q", on)
-    o = _empty(q.shape, dtype, q.device, on) if out is None else _output(out, q, q.shape, dtype, on)
+    o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     size = _layer_bytes("lba_cache_attention_workspace_bytes", c.count, c.table_row, c.page, fresh, H, c.KV, c.D)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_cache_attention(c, _at(q3), q_at, _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o), o_type, fmt, _at(ws), size,
+    _check(lib().lba_cache_attention(c, _at(q3), lba_strides(*q_at), _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o), o_type, fmt, _at(ws), size,
                                      handle))
     return o
