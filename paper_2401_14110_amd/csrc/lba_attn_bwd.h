@@ -26,9 +26,9 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     }
     const int unit = unit_of(blockIdx.x % p.units, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
-    const TileOf at = find_tile(p.starts, p.T, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);
+    const TileOf at = find_tile(p.starts, p.T, p.starts_k, p.Tk, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);
     if (at.b < 0) return;
-    const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
+    const Rows rq = at.mine, rk = at.other;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
     auto limit = [&](int i) { return keys_seen(p, rq, rk, i); };
     const int i0 = at.t * kTileRows + wave * 32, i = i0 + (lane & 31);
@@ -205,9 +205,9 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         return;
     }
     const int unit = unit_of(blockIdx.x % p.units, p.units), kv = unit / p.tiles, slice = blockIdx.x / p.units;
-    const TileOf at = find_tile(p.starts_k, p.Tk, p.count, kTileRows, unit % p.tiles);           // earlier tiles, which more queries see, first
+    const TileOf at = find_tile(p.starts_k, p.Tk, p.starts, p.T, p.count, kTileRows, unit % p.tiles);           // earlier tiles, which more queries see, first
     if (at.b < 0) return;
-    const Rows rq = rows_of(p.starts, p.T, p.count, at.b), rk = rows_of(p.starts_k, p.Tk, p.count, at.b);
+    const Rows rq = at.other, rk = at.mine;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, half = lane / 32;
     auto first_of = [&](int j) { return first_query(p, rq, rk, j); };
     const int j0 = at.t * kTileRows + wave * 32, j = j0 + (lane & 31);

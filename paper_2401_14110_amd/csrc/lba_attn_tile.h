@@ -301,18 +301,23 @@ template <typename T> __device__ __forceinline__ void clear_rows(const int32_t* 
 
 struct TileOf {
     int b, t;                // sequence (-1: none) and its tile
+    Rows mine, other;        // the sequence's rows in the list that has the tiles, and in the other one
 };
 
-// Tile `index` of the tiles of `size` rows that the sequences have one after another; the whole wave calls.
-__device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, int count, int size, int index) {
+// Tile `index` of the tiles of `size` rows that the sequences have one after another in `starts` (T rows); the whole wave calls.  Both lists are read
+// at once, 64 sequences at a time: a workgroup waits for memory once before it knows its rows.
+__device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, const int32_t* others, int T_other, int count, int size, int index) {
     if (!starts) {
-        const int per = (T / count + size - 1) / size;
-        if (per == 0 || index / per >= count) return {-1, 0};
-        return {index / per, index % per};
+        const int n = T / count, m = T_other / count, per = (n + size - 1) / size;
+        if (per == 0 || index / per >= count) return {-1, 0, {0, 0}, {0, 0}};
+        const int b = index / per;
+        return {b, index % per, {b * n, n}, {b * m, m}};
     }
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < count; b0 += 64) {
-        const int n = b0 + lane < count ? (rows_of(starts, T, count, b0 + lane).n + size - 1) / size : 0;
+        const int b = min(b0 + lane, count - 1);
+        const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
+        const int n = b0 + lane < count ? (mine.n + size - 1) / size : 0;
         int upto = n;
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) {
@@ -322,12 +327,14 @@ __device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, int co
         const uint64_t behind = __ballot(upto > index);
         if (behind) {
             const int f = __builtin_ctzll(behind);
-            return {b0 + f, index - (__builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(n, f))};
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+            return {b0 + f, index - (of(upto) - of(n)), {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
         }
         index -= __builtin_amdgcn_readlane(upto, 63);
     }
-    return {-1, 0};
+    return {-1, 0, {0, 0}, {0, 0}};
 }
+
 // Part `slice` of what a workgroup does in n steps, cut into at most `slices` parts of two steps or more: steps first .. last - 1 (none in some of
 // the later ones), `alone` where one part has them all.
 struct Slice {
