@@ -1,0 +1,170 @@
+"""An attention block of a transformer layer on 8-bit codes, from the operators of include/lba_attention.h and include/lba_layer.h.
+
+    y = x + dropout(u Wo^T + bo),   u = attention(rope(q), rope(k), v),   (q, k, v) = n W^T + b,   n = layernorm(x)
+
+n, u and the weights are codes, as in the feed-forward block.  Rows are those of packed sequences, or of one.  The same calls train on
+them, take the prompts of a server into a cache of 4 bits, and then a token of each sequence at a time.  What rounding to codes does is
+passed straight through in the backward pass.
+
+    python -m paper_2401_14110_amd.attention [--steps 20] [--rows 256] [--width 256] [--heads 4] [--kv-heads 2]
+"""
+import argparse
+import math
+
+import torch
+
+from . import binding as lba
+from .feed_forward import codes_of, scale_of, scaled_format
+
+
+def frequencies(dim, base=10000.0, factor=1.0, kind="linear", original=4096, device="cuda"):
+    """(freq, gain) for lba.rope on `dim` elements of a head: base^(-2 i / dim), for contexts of `factor` times the `original` length
+    "linear": all divided by factor (position interpolation);
+    "base":   of the base times factor^(dim / (dim - 2)), so that the slowest is divided by factor and the fastest is not (NTK-aware);
+    "ramp":   divided by factor where the original length is less than one turn, not at all where it is more than 32, in between in
+              proportion, and cosine and sine times 0.1 ln(factor) + 1 (YaRN)."""
+    i = torch.arange(0, dim, 2, dtype=torch.float64)
+    if kind == "base":
+        base = base * factor ** (dim / (dim - 2))
+    f = base ** (-i / dim)
+    gain = 1.0
+    if kind == "linear":
+        f = f / factor
+    elif kind == "ramp":
+        keep = ((original * f / (2 * math.pi) - 1) / 31).clamp(0.0, 1.0)
+        f = f * (keep + (1 - keep) / factor)
+        gain = 0.1 * math.log(factor) + 1 if factor > 1 else 1.0
+    elif kind != "base":
+        raise ValueError("kind is linear, base or ramp")
+    return f.to(device), gain
+
+
+class SelfAttention:
+    """Parameters are float32 tensors (`params`), `refresh` makes the weights' codes from them.  `inner`: the type of queries, keys and values."""
+
+    def __init__(self, width, heads, kv_heads=None, dim=None, causal=True, p=0.1, eps=1e-5, freq=None, gain=1.0, inner=torch.bfloat16, seed=0, device="cuda"):
+        g = torch.Generator().manual_seed(seed)
+        kv_heads = heads if kv_heads is None else kv_heads
+        dim = width // heads if dim is None else dim
+        self.heads, self.kv_heads, self.dim, self.causal, self.p, self.eps, self.inner = heads, kv_heads, dim, causal, p, eps, inner
+        self.freq, self.gain = (frequencies(dim // 2 * 2, device=device)[0] if freq is None else freq), gain
+        rows = (heads + 2 * kv_heads) * dim
+        p = {"gamma": torch.ones(width), "beta": torch.zeros(width),
+             "w": torch.randn((rows, width), generator=g) / math.sqrt(width), "b": torch.zeros(rows),
+             "wo": torch.randn((width, heads * dim), generator=g) / math.sqrt(heads * dim), "bo": torch.zeros(width)}
+        self.params = {k: v.to(device) for k, v in p.items()}
+        self.t_n, self.t_u = 5, 6                        # normalised rows, and averages of values: up to 14 and 7 in size
+        self.t_w, self.t_o = scale_of(p["w"]) - 1, scale_of(p["wo"]) - 1             # room for the weights to double
+        self.refresh()
+
+    def refresh(self):
+        self.w, self.wo = codes_of(self.params["w"], self.t_w), codes_of(self.params["wo"], self.t_o)
+
+    def split(self, qkv):
+        return qkv.split((self.heads, self.kv_heads, self.kv_heads), -2)
+
+    def project(self, x, positions, want_stats=False):
+        """(n, its statistics, rotated queries, keys and values [..., heads + 2 kv_heads, dim]) of x [..., width]."""
+        q = self.params
+        n = lba.layernorm(x, q["gamma"], q["beta"], self.eps, out_dtype=torch.uint8, out_fmt=scaled_format(self.t_n), want_stats=want_stats)
+        n, mean, rstd = n if want_stats else (n, None, None)
+        qkv = lba.dense(n, self.w, scaled_format(self.t_n), scaled_format(self.t_w), bias=q["b"], out_dtype=self.inner)
+        qkv = qkv.unflatten(-1, (-1, self.dim))
+        turned = qkv[..., :self.heads + self.kv_heads, :]
+        lba.rope(turned, positions, self.freq, gain=self.gain, out=turned)
+        return n, mean, rstd, qkv
+
+    def finish(self, u, x, drop=None):
+        return lba.dense(u, self.wo, scaled_format(self.t_u), scaled_format(self.t_o), bias=self.params["bo"], drop=drop, residual=x, out_dtype=x.dtype)
+
+    def forward(self, x, positions, starts=None, seed=0, train=False, cache=None):
+        """y of x [rows, width], and with train what `backward` reads.  positions [rows]; starts: as lba.attention takes it.  cache: (KVCache, table,
+        lens), which get the rows' keys and values."""
+        fmt = scaled_format(self.t_u)
+        n, mean, rstd, qkv = self.project(x, positions, train)
+        q, k, v = self.split(qkv)
+        if cache is not None:
+            lba.cache_write(k, v, cache[0], cache[1], torch.tensor([0, len(x)], dtype=torch.int32, device=x.device) if starts is None else starts, cache[2])
+        if not train:
+            u = lba.attention(q, k, v, starts=starts, causal=self.causal, out_dtype=torch.uint8, out_fmt=fmt)
+            return self.finish(u.flatten(-2), x)
+        o, lse = lba.attention(q, k, v, starts=starts, causal=self.causal, want_stats=True)
+        u = lba.dropout(o.flatten(-2), None, out_dtype=torch.uint8, out_fmt=fmt)
+        drop = (self.p, seed, 0) if self.p > 0 else None
+        return self.finish(u, x, drop), (x, positions, starts, n, mean, rstd, qkv, o, lse, u, drop)
+
+    def backward(self, G, kept):
+        """(dx, the gradients of `params`) for dL/dy = G and what `forward` kept."""
+        p, (x, positions, starts, n, mean, rstd, qkv, o, lse, u, drop) = self.params, kept
+        d = {}
+        du, d["wo"], d["bo"] = lba.dense_bwd(G, u, self.wo, scaled_format(self.t_u), scaled_format(self.t_o), drop=drop, want_dbias=True)
+        if du.dtype != self.inner:
+            du = lba.dropout(du, None, out_dtype=self.inner)
+        dqkv = torch.empty_like(qkv) if starts is None else torch.zeros_like(qkv)    # (rows of no sequence)
+        lba.attention_bwd(du.view(o.shape), *self.split(qkv), o, lse, starts=starts, causal=self.causal, out=self.split(dqkv))
+        turned = dqkv[:, :self.heads + self.kv_heads]
+        lba.rope_bwd(turned, positions, self.freq, gain=self.gain, out=turned)
+        dqkv = dqkv.flatten(-2)
+        if dqkv.dtype != torch.float32:
+            dqkv = lba.dropout(dqkv, None, out_dtype=torch.float32)                  # the products with the weights and n keep float32 sums
+        dn, d["w"], d["b"] = lba.dense_bwd(dqkv, n, self.w, scaled_format(self.t_n), scaled_format(self.t_w), want_dbias=True)
+        dx, d["gamma"], d["beta"] = lba.layernorm_bwd(dn, x, p["gamma"], mean, rstd)
+        return dx.add_(G), d
+
+    def attend(self, x, cache):
+        """Codes of the attention of new tokens x [sequences, width] or [sequences, tokens, width] over the cache, which they are written to first
+        (lens counts them)."""
+        held, table, lens = cache
+        at = lens if x.dim() == 2 else lens[:, None] - x.shape[1] + 1 + torch.arange(x.shape[1], dtype=torch.int32, device=x.device)
+        _, _, _, qkv = self.project(x, at - 1)
+        q, k, v = self.split(qkv)
+        lba.cache_write(k, v, held, table, None, lens)
+        return lba.cache_attention(q, held, table, lens, out_dtype=torch.uint8, out_fmt=scaled_format(self.t_u)).flatten(-2)
+
+    def tokens(self, x, cache):
+        """y of new tokens, causal."""
+        return self.finish(self.attend(x, cache), x)
+
+    def step(self, grads, rate):
+        for k, w in self.params.items():
+            w.add_(grads[k], alpha=-rate)
+        self.refresh()
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description="trains an attention block on a fixed map of packed sequences, then serves one through the cache")
+    ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--rows", type=int, default=256)
+    ap.add_argument("--width", type=int, default=256)
+    ap.add_argument("--heads", type=int, default=4)
+    ap.add_argument("--kv-heads", type=int, default=2)
+    ap.add_argument("--rate", type=float, default=None, help="learning rate (1 / width)")
+    a = ap.parse_args(argv)
+    block = SelfAttention(a.width, a.heads, a.kv_heads, p=0.05)
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn((a.rows, a.width), generator=g).cuda()
+    target = (x.cpu() @ (torch.randn((a.width, a.width), generator=g) / math.sqrt(a.width))).cuda()
+    cut = a.rows // 3
+    starts = torch.tensor([0, cut, a.rows], dtype=torch.int32, device="cuda")
+    positions = torch.cat([torch.arange(cut), torch.arange(a.rows - cut)]).cuda()
+    losses = []
+    for i in range(a.steps):
+        y, kept = block.forward(x, positions, starts, seed=i, train=True)
+        err = y - target
+        losses.append((err * err).mean())
+        _, grads = block.backward(err * (2.0 / a.rows), kept)
+        block.step(grads, a.rate or 1.0 / a.width)
+    losses = [float(v) for v in losses]
+    # the first sequence: a prompt, then its last token by itself over the cache
+    page = 16
+    held = lba.kv_cache(cut // page + 1, page, a.kv_heads, a.width // a.heads)
+    table, lens = torch.arange(cut // page + 1, dtype=torch.int32, device="cuda")[None], torch.tensor([cut - 1], dtype=torch.int32, device="cuda")
+    whole = block.forward(x[:cut], positions[:cut])
+    block.forward(x[:cut - 1], positions[:cut - 1], cache=(held, table, lens))
+    token = block.tokens(x[cut - 1:cut], (held, table, lens + 1))
+    print("loss %.4f -> %.4f; a token over the cache: %.4f from the prompt's" % (losses[0], losses[-1], float((token - whole[-1:]).abs().max())))
+    return losses
+
+
+if __name__ == "__main__":
+    main()

@@ -62,18 +62,19 @@ def attend(q, k, v, see, scale, dtype, pieces=1):
     return {"q": q, "k": k, "v": v, "see": see, "s": s, "es": es, "p": p, "o": o, "to": 1.1 * to, "lse": lse, "tl": tl, "scale": scale, "dtype": dtype, "some": some}
 
 
-def attend_bwd(f, g):
-    """(dq, dk, dv) and their bounds before the results are rounded, of one query head."""
+def attend_bwd(f, g, tg=None):
+    """(dq, dk, dv) and their bounds before the results are rounded, of one query head; tg: how far g may be off itself."""
     g = g.astype(np.float64)
+    tg = np.zeros(g.shape) if tg is None else tg
     q, k, v, p, D = f["q"], f["k"], f["v"], f["p"], f["q"].shape[1]
     n, m = p.shape
     bf = 2.0 ** -8 if f["dtype"] == "bf16" else 0.0
     lse = np.where(f["some"], f["lse"], 0.0)
     dp = np.where(f["see"], f["es"] + 6 * U * (np.abs(f["s"]) + np.abs(lse)[:, None] + 1) + f["tl"][:, None], 0.0)
     u = g @ v.T
-    eu = (D + 4) * U * (np.abs(g) @ np.abs(v).T)
+    eu = (D + 4) * U * (np.abs(g) @ np.abs(v).T) + tg @ np.abs(v).T
     delta = (g * f["o"]).sum(1)
-    ed = (np.abs(g) * (f["to"] + (bf + U) * np.abs(f["o"]) * 1.01)).sum(1) + (D + 4) * U * (np.abs(g) * np.abs(f["o"])).sum(1)
+    ed = (np.abs(g) * (f["to"] + (bf + U) * np.abs(f["o"]) * 1.01)).sum(1) + (D + 4) * U * (np.abs(g) * np.abs(f["o"])).sum(1) + (tg * np.abs(f["o"])).sum(1)
     w = u - delta[:, None]
     ds = p * w
     es = p * (dp * 1.1 * np.abs(w) + eu + ed[:, None] + 2 * U * np.abs(w)) + (bf + 2 * U) * np.abs(ds) * 1.01 + 4 * TINY * (1 + np.abs(w))
@@ -81,11 +82,11 @@ def attend_bwd(f, g):
     dq, dk, dv = f["scale"] * (ds @ k), f["scale"] * (ds.T @ q), p.T @ g
     tq = sc * (es @ np.abs(k) + (m + 8) * U * (np.abs(ds) @ np.abs(k))) + 4 * TINY
     tk = sc * (es.T @ np.abs(q) + (n + 8) * U * (np.abs(ds).T @ np.abs(q))) + 4 * TINY
-    tv = (p * (dp * 1.1 + bf + (n + 8) * U)).T @ np.abs(g) + 4 * TINY * (1 + np.abs(g).sum(0))
+    tv = (p * (dp * 1.1 + bf + (n + 8) * U)).T @ np.abs(g) + 1.1 * p.T @ tg + 4 * TINY * (1 + np.abs(g).sum(0))
     return (dq, dk, dv), (1.1 * tq, 1.1 * tk, 1.1 * tv)
 
 
-def packed(q, k, v, lens, lens_k, causal, scale, dtype, G=None, first=0, first_k=0):
+def packed(q, k, v, lens, lens_k, causal, scale, dtype, G=None, first=0, first_k=0, tG=None):
     """Everything of packed sequences: dict of (value, bound) for o, lse and, with G, dq, dk, dv.  Rows before `first` and behind the last
     sequence are zeros (-infinity in lse), with bound 0."""
     H, KV = q.shape[1], k.shape[1]
@@ -101,7 +102,7 @@ def packed(q, k, v, lens, lens_k, causal, scale, dtype, G=None, first=0, first_k
             f = attend(q[i, h], k[j, kv], v[j, kv], seen(n, m, causal), scale, dtype)
             o[i, h], to[i, h], lse[i, h], tl[i, h] = f["o"], f["to"], f["lse"], f["tl"]
             if G is not None:
-                for (w, r, hh), x, t in zip((("dq", i, h), ("dk", j, kv), ("dv", j, kv)), *attend_bwd(f, G[i, h])):
+                for (w, r, hh), x, t in zip((("dq", i, h), ("dk", j, kv), ("dv", j, kv)), *attend_bwd(f, G[i, h], None if tG is None else tG[i, h])):
                     grads[w][0][r, hh] += x
                     grads[w][1][r, hh] += t + 2 * U * np.abs(x)                      # the sum over a group's heads
     got = {"o": (o, to), "lse": (lse, tl)}

@@ -1,0 +1,178 @@
+"""The attention block on codes: its outputs and gradients against the formulas in 64 bits at the codes that it used, every bound from the number of
+float32 sums and roundings that an output goes through; prompts and tokens through the cache."""
+import numpy as np
+import pytest
+import torch
+
+import attention_oracle as ao
+import layer_oracle as lo
+from paper_2401_14110_amd import attention as at
+from paper_2401_14110_amd import binding as lb
+from paper_2401_14110_amd.feed_forward import scaled_format
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def near(got, want, tol, what):
+    err = np.abs(host(got) - want)
+    assert (err <= tol).all(), (what, float((err / np.maximum(tol, 1e-300)).max()))
+
+
+def rounded(v, tol, dtype):
+    """The bound of v, off by tol, after it is rounded to the type."""
+    return tol + ao.rounding(dtype) * (np.abs(v) + tol) + ao.TINY
+
+
+def projected(block, n, positions, dtype):
+    """(value, bound) of the rotated queries, keys and values from n's codes."""
+    q = {k: host(v) for k, v in block.params.items()}
+    z, tz, parts = lo.dense(n, block.w.cpu().numpy(), scaled_format(block.t_n), scaled_format(block.t_w), q["b"], 0, False, None, None)
+    tz = rounded(z, tz, dtype)
+    shape = z.shape[:-1] + (-1, block.dim)
+    z, tz = z.reshape(shape), tz.reshape(shape)
+    turned = block.heads + block.kv_heads
+    freq, R = block.freq.cpu().numpy(), 2 * len(block.freq)
+    y, ty = ao.rope(z[:, :turned], positions, freq, False, block.gain)
+    e = tz[:, :turned].copy()
+    e[..., :R // 2] = e[..., R // 2:R] = abs(block.gain) * (tz[:, :turned, :R // 2] + tz[:, :turned, R // 2:R])
+    return np.concatenate([y, z[:, turned:]], 1), np.concatenate([rounded(y, ty + e, dtype), tz[:, turned:]], 1), parts
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,width,heads,kv_heads,dim,causal,p", [([33], 40, 2, 1, 24, True, 0.1), ([70, 0, 45], 96, 4, 2, 32, True, 0.0), ([20, 90], 72, 3, 3, 50, False, 0.25)])
+def test_training_step(lens, width, heads, kv_heads, dim, causal, p, dtype):
+    rows = sum(lens)
+    rng = np.random.default_rng(rows)
+    freq, gain = at.frequencies(dim // 4 * 2, factor=2.0, kind="ramp", original=64)
+    block = at.SelfAttention(width, heads, kv_heads, dim, causal=causal, p=p, freq=freq, gain=gain, inner=DT[dtype], seed=rows)
+    x = torch.from_numpy(rng.standard_normal((rows, width)).astype(np.float32)).cuda()
+    G = rng.standard_normal((rows, width)).astype(np.float32)
+    positions = np.concatenate([np.arange(n) + 7 for n in lens])
+    s = torch.tensor(np.cumsum([0] + lens), dtype=torch.int32).cuda()
+    y, kept = block.forward(x, torch.from_numpy(positions).cuda(), s, seed=5, train=True)
+    _, _, _, n, mean, rstd, qkv, o, lse, u, _ = kept
+    q = {k: host(v) for k, v in block.params.items()}
+    want, _, _, tol = lo.norm(host(x), q["gamma"], q["beta"], block.eps)
+    lo.check_codes(n.cpu().numpy(), want, tol, scaled_format(block.t_n))
+    want, tol, first = projected(block, n.cpu().numpy(), positions, dtype)
+    near(qkv, want, tol, "qkv")
+    cut = lambda t: np.split(host(t), [heads, heads + kv_heads], 1)  # noqa: E731
+    scale = float(np.float32(dim ** -0.5))
+    f = ao.packed(*cut(qkv), lens, lens, causal, scale, dtype)
+    near(o, f["o"][0], rounded(*f["o"], dtype), "o")
+    lo.check_codes(u.cpu().numpy(), host(o).reshape(rows, -1), 2 * lo.U * np.abs(host(o)).reshape(rows, -1), scaled_format(block.t_u))
+    drop = lo.drop_factors(p, 5, 0, 0, rows * width).reshape(rows, width) if p else None
+    want, tol, second = lo.dense(u.cpu().numpy(), block.wo.cpu().numpy(), scaled_format(block.t_u), scaled_format(block.t_o), q["bo"], 0, False, drop, host(x))
+    near(y, want, tol, "y")
+    # backwards: each operator's gradient from the one before it, whose bound goes through
+    dx, grads = block.backward(torch.from_numpy(G).cuda(), kept)
+    (du, dwo, dbo), (tu, tw, tb) = lo.dense_bwd(G.astype(np.float64), second, False)
+    near(grads["wo"], dwo, tw, "wo")
+    near(grads["bo"], dbo, tb, "bo")
+    if dtype == "bf16":
+        tu = rounded(du, tu, dtype)
+    b = ao.packed(*cut(qkv), lens, lens, causal, scale, dtype, du.reshape(o.shape), tG=tu.reshape(o.shape))
+    d = np.concatenate([b[w][0] for w in ("dq", "dk", "dv")], 1)
+    e = np.concatenate([rounded(*b[w], dtype) for w in ("dq", "dk", "dv")], 1)
+    turned, R = heads + kv_heads, 2 * len(freq)
+    back, tback = ao.rope(d[:, :turned], positions, freq.cpu().numpy(), False, gain, -1.0)
+    e[:, :turned, :R // 2] = e[:, :turned, R // 2:R] = gain * (e[:, :turned, :R // 2] + e[:, :turned, R // 2:R])
+    d[:, :turned], e[:, :turned] = back, rounded(back, e[:, :turned] + tback, dtype)
+    d, e = d.reshape(rows, -1), e.reshape(rows, -1)
+    (dn, dw, db), (tn, tw, tb) = lo.dense_bwd(d, first, False)
+    near(grads["w"], dw, tw + e.T @ np.abs(first["a"]), "w")
+    near(grads["b"], db, tb + e.sum(0), "b")
+    tn = tn + e @ np.abs(first["b"])
+    mean, rstd = host(mean), host(rstd)
+    (dxn, dg, dbeta), (tx, tg, tbeta) = lo.norm_bwd(dn, host(x), q["gamma"], mean, rstd)
+    c = (host(x) - mean[:, None]) * rstd[:, None]
+    h = tn * np.abs(q["gamma"])
+    tx = tx + rstd[:, None] * (h + h.mean(1, keepdims=True) + np.abs(c) * (h * np.abs(c)).mean(1, keepdims=True)) + 2 * lo.U * np.abs(dxn + G)
+    near(dx, dxn + G, tx, "dx")
+    near(grads["gamma"], dg, tg + (tn * np.abs(c)).sum(0), "gamma")
+    near(grads["beta"], dbeta, tbeta + tn.sum(0), "beta")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fresh", [1, 3])
+def test_prompts_then_tokens(fresh, dtype):
+    """Two prompts into the cache, then new tokens: their codes are those of attention over what the cache holds."""
+    rng = np.random.default_rng(4)
+    width, heads, kv_heads, dim, page, lens = 64, 4, 2, 32, 8, [21, 5]
+    block = at.SelfAttention(width, heads, kv_heads, dim, inner=DT[dtype], seed=2)
+    x = torch.from_numpy(rng.standard_normal((sum(lens), width)).astype(np.float32)).cuda()
+    s = torch.tensor(np.cumsum([0] + lens), dtype=torch.int32).cuda()
+    positions = torch.cat([torch.arange(n) for n in lens]).cuda()
+    held = lb.kv_cache(9, page, kv_heads, dim)
+    table = torch.tensor([[8, 1, 6, 3], [0, 7, 2, 5]], dtype=torch.int32).cuda()
+    ln = torch.tensor(lens, dtype=torch.int32).cuda()
+    y = block.forward(x, positions, s, cache=(held, table, ln))
+    assert torch.equal(y, block.forward(x, positions, s))
+    ln += fresh
+    new = torch.from_numpy(rng.standard_normal((2, fresh, width)).astype(np.float32)).cuda()
+    if fresh == 1:
+        new = new[:, 0]
+    u = block.attend(new, (held, table, ln)).reshape(2, fresh, heads, dim).cpu().numpy()
+    # the tokens' queries, and what the cache holds now
+    n, _, _, qkv = block.project(new, (ln[:, None] - fresh + torch.arange(fresh, device="cuda")).reshape(new.shape[:-1]))
+    q = host(qkv).reshape(2, fresh, -1, dim)[:, :, :heads]
+    k, v = lb.cache_read(held, table, torch.cat([ln.new_zeros(1), ln.cumsum(0, dtype=torch.int32)]), ln, int(ln.sum()), out_dtype=torch.float32)
+    at_ = 0
+    for b in range(2):
+        m = int(ln[b])
+        for h in range(heads):
+            kv = h // 2
+            f = ao.attend(q[b, :, h], host(k[at_:at_ + m, kv]), host(v[at_:at_ + m, kv]), ao.seen(fresh, m, True), float(np.float32(dim ** -0.5)), dtype, 1 if dtype == "bf16" else 3)
+            lo.check_codes(u[b, :, h], f["o"], f["to"] + 2 * lo.U * np.abs(f["o"]), scaled_format(block.t_u))
+        at_ += m
+    want, tol, _ = lo.dense(u.reshape(2 * fresh, -1), block.wo.cpu().numpy(), scaled_format(block.t_u), scaled_format(block.t_o), host(block.params["bo"]), 0, False, None,
+                            host(new).reshape(2 * fresh, -1))
+    near(block.tokens(new, (held, table, ln)).reshape(2 * fresh, -1), want, tol, "tokens")
+
+
+@pytest.mark.gpu
+def test_a_step_of_a_server_in_a_graph():
+    """One token of each sequence, captured once and replayed as the sequences grow."""
+    block = at.SelfAttention(64, 4, 2, 32, seed=3)
+    held, eager = lb.kv_cache(8, 4, 2, 32), lb.kv_cache(8, 4, 2, 32)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 4)
+    lens = torch.tensor([1, 4], dtype=torch.int32, device="cuda")
+    x = torch.randn(2, 64, device="cuda")
+    block.tokens(x, (eager, table, lens))                # (what a first call sets up is not captured)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = block.tokens(x, (held, table, lens))
+    for a, b in zip(held, eager):
+        a.copy_(b)
+    for _ in range(10):
+        x.copy_(torch.randn_like(x))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, block.tokens(x, (eager, table, lens))) and all(torch.equal(a, b) for a, b in zip(held, eager))
+        lens.add_(1)
+
+
+def test_frequencies():
+    plain, one = at.frequencies(64, device="cpu")
+    assert one == 1.0 and plain[0] == 1.0 and torch.allclose(plain, 10000.0 ** (-torch.arange(32, dtype=torch.float64) / 32), rtol=1e-14)
+    assert torch.equal(at.frequencies(64, factor=4.0, device="cpu")[0], plain / 4)
+    spread, _ = at.frequencies(64, factor=4.0, kind="base", device="cpu")
+    assert spread[0] == 1.0 and abs(spread[-1] / plain[-1] - 0.25) < 1e-12 and (spread <= plain).all()
+    ramp, gain = at.frequencies(64, factor=4.0, kind="ramp", original=4096, device="cpu")
+    turns = 4096 * plain / (2 * np.pi)
+    assert torch.equal(ramp[turns > 32], plain[turns > 32]) and torch.allclose(ramp[turns < 1], plain[turns < 1] / 4, rtol=1e-14)
+    assert ((ramp <= plain) & (ramp >= plain / 4 * (1 - 1e-14))).all() and abs(gain - (0.1 * np.log(4) + 1)) < 1e-15
+    with pytest.raises(ValueError):
+        at.frequencies(64, kind="other", device="cpu")
+
+
+@pytest.mark.gpu
+def test_the_command_runs():
+    losses = at.main(["--steps", "3", "--rows", "100", "--width", "64", "--heads", "2", "--kv-heads", "1"])
+    assert len(losses) == 3 and np.isfinite(losses).all()
