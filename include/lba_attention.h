@@ -57,8 +57,8 @@ typedef struct {
     lba_strides q, k, v;
 } lba_attn;
 
-/* O = softmax over the seen keys of (scale * q . k) times V; a query that sees nothing has zeros.  Scores, the softmax's maximum and sum and O's
- * sums are float32; with LBA_BF16 the weights are rounded to bfloat16 for the product with V.
+/* O = softmax over the seen keys of (scale * q . k) times V; a query that sees nothing, or whose scores are all -infinity, has
+ * zeros.  Scores, the softmax's maximum and sum and O's sums are float32; with LBA_BF16 the weights are rounded to bfloat16 for the product with V.
  * O [T, H, D] contiguous of o_type (o_fmt is read for LBA_CODE8 only); lse [T, H] float32 (NULL: not stored): ln of the sum over the seen
  * keys of exp(scale * q . k), -infinity where there are none.
  * workspace: lba_attention_workspace_bytes(a) bytes, which reads no pointer of `a` but whether it is NULL; 0 where there are many rows. */
@@ -68,8 +68,8 @@ size_t lba_attention_workspace_bytes(lba_attn a);
 
 /* Its gradients.  With P the weights, made again from lse, and G = dL/dO,
  *   dV = P^T . G,   S = P * (G . V^T - rowsum(G * O)),   dQ = scale * S . K,   dK = scale * S^T . Q,
- * summed over the query heads of a key head.  G and O [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D],
- * dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the products; sums are float32.
+ * summed over the query heads of a key head.  Gradients that a seen infinity or NaN reaches are unspecified.  G and O
+ * [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D], dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the products; sums are float32.
  * workspace: lba_attention_bwd_workspace_bytes(a) bytes. */
 int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, const void* V, const void* O, const float* lse, void* dQ,
                       lba_strides dq_at, void* dK, lba_strides dk_at, void* dV, lba_strides dv_at, void* workspace, size_t workspace_bytes,
@@ -96,12 +96,12 @@ typedef struct {
 
 /* Writes the newest tokens: rows starts[b] .. starts[b + 1] - 1 of K and V ([T, KV, D] of `type`) go to positions
  * lens[b] - (starts[b + 1] - starts[b]) .. lens[b] - 1 of sequence b (lens counts them); those below 0 are dropped.  starts NULL: T / count rows
- * each.  Two rows that go to one place leave one of the two there, in whole blocks. */
+ * each.  Two rows that go to one place leave a mix of the two there. */
 int lba_cache_write(lba_cache4 c, const int32_t* starts, int64_t T, const void* K, lba_strides k_at, const void* V, lba_strides v_at, int32_t type,
                     void* hip_stream);
 
-/* Reads the newest tokens back, in the same arrangement, exactly: K and V [T, KV, D] of `type`.  Positions below 0 read as zeros.  Rows of no
- * sequence are left as they were, or, clear != 0, stored as zeros. */
+/* Reads the newest tokens back, in the same arrangement, exactly (numbers under 2^-126 in size as zero): K and V [T, KV, D] of `type`.
+ * Positions below 0 read as zeros.  Rows of no sequence are left as they were, or, clear != 0, stored as zeros. */
 int lba_cache_read(lba_cache4 c, const int32_t* starts, int64_t T, void* K, lba_strides k_at, void* V, lba_strides v_at, int32_t type, int32_t clear,
                    void* hip_stream);
 

@@ -24,6 +24,7 @@ __device__ __forceinline__ Rows rows_of(const int32_t* starts, int T, int count,
 
 // The sequence that row `t` belongs to, -1: none.  The last one whose start is not behind t (empty ones share their start with the next).
 __device__ __forceinline__ int sequence_of(const int32_t* starts, int T, int count, int t) {
+    if (count < 1) return -1;
     if (!starts) return t / (T / count);
     int lo = 0, hi = count;                              // starts[lo] <= t < starts[hi], were the list extended so
     while (hi - lo > 1) {

@@ -107,6 +107,7 @@ static int cache_plan(int64_t count, int64_t table_row, int64_t page, int64_t fr
     if (room > (1 << 30) || units >= (1 << 23)) return LBA_ERR_SHAPE;
     c->row_tiles = (int32_t)row_tiles;
     c->chunk = (room * units + 1023) / 1024;
+    if (c->chunk > room) c->chunk = room;                // (and within 32 bits)
     c->chunk = (c->chunk + 127) / 128 * 128;
     if (c->chunk < 256) c->chunk = 256;
     c->chunks = room > c->chunk ? (room + c->chunk - 1) / c->chunk : 1;

@@ -324,6 +324,33 @@ def desc(**k):
     return lb.lba_cache4(*{**d, **k}.values())
 
 
+@pytest.mark.gpu
+def test_tables_with_room_for_more_than_a_launch_has_workgroups():
+    """2048 sequences that may have 2^30 positions each: a chunk is then a whole sequence, not 2^31 positions."""
+    count, row, page = 2048, 16384, 65536
+    cache = lb.kv_cache(1, page, 1, 32)
+    table = torch.full((count, row), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    k, v, q = (torch.randn(1, 5, h, 32, device="cuda") for h in (1, 1, 2))
+    lens = torch.full((count,), 5, dtype=torch.int32, device="cuda")
+    lb.cache_write(k, v, cache, table[:1], None, lens[:1])
+    got = lb.cache_attention(q[:, 4].expand(count, 2, 32), cache, table, lens)
+    want = lb.cache_attention(q[:, 4], cache, table[:1, :1], lens[:1])
+    assert bool(want.any()) and torch.equal(got, want.expand(count, 2, 32))
+
+
+@pytest.mark.gpu
+def test_rows_of_no_sequences_at_all():
+    cache = lb.kv_cache(2, 4, 1, 32)
+    none, starts = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    k, v = lb.cache_read(cache, none.view(0, 3), starts, none, 4)
+    assert k.shape == (4, 1, 32) and not k.any() and not v.any()
+    q = torch.randn(4, 2, 32, device="cuda")
+    o, lse = lb.attention(q, q, q, starts=starts, want_stats=True)
+    assert not o.any() and bool((lse == -np.inf).all())
+    assert not any(d.any() for d in lb.attention_bwd(q, q, q, q, o, lse, starts=starts))
+
+
 def test_refusals():
     P, W, f, s = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x2000), (4, 3, 7), lb.lba_strides(128, 64)
     write = lambda c=None, **k: lb.lba_cache_write(*{**dict(c=c or desc(), st=None, T=4, K=P, ka=s, V=P, va=s, t=0), **k}.values())  # noqa: E731
