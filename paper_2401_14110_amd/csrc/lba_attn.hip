@@ -1,4 +1,5 @@
-// lba_attn.hip -- attention over packed sequences: the description's checks and the forward entry point.
+// lba_attn.hip -- attention over packed sequences: the description's checks, how passes are cut into parts and the join of the forward pass's, its
+// entry point.
 #include "lba_attn_tile.h"
 
 namespace lba {
@@ -46,6 +47,36 @@ int attn_plan(const lba_attn& a, AttnPlan* plan) {
     return LBA_OK;
 }
 
+// O and lse from the parts: a workgroup a row, a lane an element of its heads.
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+    const int64_t rows = (int64_t)p.T * p.H;
+    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
+        const int b = sequence_of(p.starts, p.T, p.count, t);
+        if (b < 0) continue;
+        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const int n = slices_used(steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>), p.slices);
+        if (n <= 1) continue;                            // stored by its only workgroup
+        for (int i = threadIdx.x; i < p.H * p.D; i += 256) {
+            const int64_t row = (int64_t)t * p.H + i / p.D;
+            const float* end = p.part + p.slices * rows * p.D + row * 2;
+            float top = -__builtin_inff(), sum = 0.0f, v = 0.0f;
+            for (int x = 0; x < n; ++x) top = fmaxf(top, end[x * rows * 2]);
+            const float base = top == -__builtin_inff() ? 0.0f : top;
+            for (int x = 0; x < n; ++x) {
+                const float f = __builtin_amdgcn_exp2f(end[x * rows * 2] - base);
+                sum = fmaf(f, end[x * rows * 2 + 1], sum);
+                v = fmaf(f, p.part[x * rows * p.D + row * p.D + i % p.D], v);
+            }
+            with_output(p, [&](auto* o) { store_one(o + (int64_t)t * p.H * p.D + i, sum == 0.0f ? 0.0f : v / sum, p.fmt); });
+            if (p.lse && i % p.D == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
+        }
+    }
+}
+
+template <typename T> static void launch_join(const AttnParams& p, hipStream_t st) {
+    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(p.T < (1 << 20) ? p.T : (1 << 20))), dim3(256), 0, st, p);
+}
+
 }  // namespace lba
 
 using namespace lba;
@@ -87,6 +118,7 @@ int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void*
     const bool direct = whole_pieces(K, a.k, a.D, size) && whole_pieces(V, a.v, a.D, size);
     const hipStream_t st = (hipStream_t)hip_stream;
     if (a.type == LBA_F32) launch_attn<float>(p, direct, st); else launch_attn<bf16_t>(p, direct, st);
+    if (p.slices > 1) { if (a.type == LBA_F32) launch_join<float>(p, st); else launch_join<bf16_t>(p, st); }
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }
 

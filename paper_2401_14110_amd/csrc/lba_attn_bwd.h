@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     auto first_of = [&](int j) { return first_query(p, rq, rk, j); };
     const int j0 = at.t * kTileRows + wave * 32, j = j0 + (lane & 31);
     const bool there = j < rk.n;
-    const int lo = first_of(j), lo_wave = first_of(j0), lo_last = first_of(j0 + 31), lo_all = first_of(at.t * kTileRows);
+    const int lo = first_of(j), lo_wave = first_of(j0), lo_all = first_of(at.t * kTileRows);
     const int t0 = lo_all / QT, steps_head = steps_of_keys(p, rq, rk, at.t, QT);                // tiles of queries of a head; a step is one of a head of the group
     const Slice part = slice_of(steps_head * p.group, p.slices, slice);
     const int steps = part.last;
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     if (broken) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
-        for (int x = 0; x < 32 && j0 + x < rk.n; ++x) 
+        for (int x = 0; x < 32 && j0 + x < rk.n; ++x)
             dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x), part.first, steps, steps_head, t0 * QT, QT, part.alone ? -1 : slice);
         return;
     }
@@ -387,40 +387,12 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     store_columns((T*)p.dV + (int64_t)(rk.first + j) * p.dv.row + (int64_t)kv * p.dv.head, dv, 1.0f, p.D, half);
 }
 
-// Gradients from the parts: a workgroup a row, a lane an element of its heads.  KEYS: dK, and blockIdx.y == 1: dV; else dQ.
-template <typename T, bool KEYS> __global__ __launch_bounds__(256) void attn_join_grad_kernel(AttnParams p) {
-    const int heads = KEYS ? p.KV : p.H, total = KEYS ? p.Tk : p.T;
-    const int64_t all = (int64_t)total * heads * p.D;
-    const float* part = p.part + blockIdx.y * p.slices * all;
-    T* out = (T*)(!KEYS ? p.dQ : blockIdx.y ? p.dV : p.dK);
-    const lba_strides at = !KEYS ? p.dq : blockIdx.y ? p.dv : p.dk;
-    const CodeFmt none = {};
-    for (int t = blockIdx.x; t < total; t += gridDim.x) {
-        const int b = KEYS ? sequence_of(p.starts_k, p.Tk, p.count, t) : sequence_of(p.starts, p.T, p.count, t);
-        if (b < 0) continue;
-        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
-        const int steps = KEYS ? steps_of_keys(p, rq, rk, (t - rk.first) / kTileRows, kStep<T>) * p.group : steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>);
-        const int n = slices_used(steps, p.slices);
-        if (n <= 1) continue;                            // stored by its only workgroup
-        for (int i = threadIdx.x; i < heads * p.D; i += 256) {
-            float v = 0.0f;
-            for (int x = 0; x < n; ++x) v += part[x * all + (int64_t)t * heads * p.D + i];
-            store_one(out + (int64_t)t * at.row + (int64_t)(i / p.D) * at.head + i % p.D, v, none);
-        }
-    }
-}
-template <typename T, bool KEYS> void launch_join_grad(const AttnParams& p, hipStream_t st) {
-    const int rows = KEYS ? p.Tk : p.T;
-    hipLaunchKernelGGL((attn_join_grad_kernel<T, KEYS>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20)), KEYS ? 2 : 1), dim3(256), 0, st, p);
-}
-
 template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipStream_t st) {
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
-        if (p.slices > 1) launch_join_grad<T, false>(p, st); \
         return; \
     }
     LBA_ATTN(32)
@@ -435,7 +407,6 @@ template <typename T> void launch_attn_dkv(const AttnParams& p, bool direct, hip
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_dkv_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dkv_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
-        if (p.slices > 1) launch_join_grad<T, true>(p, st); \
         return; \
     }
     LBA_ATTN(32)

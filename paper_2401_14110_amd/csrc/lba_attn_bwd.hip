@@ -1,5 +1,36 @@
-// lba_attn_bwd.hip -- the gradients of attention over packed sequences: entry points.
+// lba_attn_bwd.hip -- the gradients of attention over packed sequences: the join of parts, entry points.
 #include "lba_attn_tile.h"
+
+namespace lba {
+
+// Gradients from the parts: a workgroup a row, a lane an element of its heads.  KEYS: dK, and blockIdx.y == 1: dV; else dQ.
+template <typename T, bool KEYS> __global__ __launch_bounds__(256) void attn_join_grad_kernel(AttnParams p) {
+    const int heads = KEYS ? p.KV : p.H, total = KEYS ? p.Tk : p.T;
+    const int64_t all = (int64_t)total * heads * p.D;
+    const float* part = p.part + blockIdx.y * p.slices * all;
+    T* out = (T*)(!KEYS ? p.dQ : blockIdx.y ? p.dV : p.dK);
+    const lba_strides at = !KEYS ? p.dq : blockIdx.y ? p.dv : p.dk;
+    const CodeFmt none = {};
+    for (int t = blockIdx.x; t < total; t += gridDim.x) {
+        const int b = KEYS ? sequence_of(p.starts_k, p.Tk, p.count, t) : sequence_of(p.starts, p.T, p.count, t);
+        if (b < 0) continue;
+        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const int steps = KEYS ? steps_of_keys(p, rq, rk, (t - rk.first) / kTileRows, kStep<T>) * p.group : steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>);
+        const int n = slices_used(steps, p.slices);
+        if (n <= 1) continue;                            // stored by its only workgroup
+        for (int i = threadIdx.x; i < heads * p.D; i += 256) {
+            float v = 0.0f;
+            for (int x = 0; x < n; ++x) v += part[x * all + (int64_t)t * heads * p.D + i];
+            store_one(out + (int64_t)t * at.row + (int64_t)(i / p.D) * at.head + i % p.D, v, none);
+        }
+    }
+}
+template <typename T, bool KEYS> static void launch_join_grad(const AttnParams& p, hipStream_t st) {
+    const int rows = KEYS ? p.Tk : p.T;
+    hipLaunchKernelGGL((attn_join_grad_kernel<T, KEYS>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20)), KEYS ? 2 : 1), dim3(256), 0, st, p);
+}
+
+}  // namespace lba
 
 using namespace lba;
 
@@ -43,6 +74,7 @@ int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, c
         p.units = (int32_t)(plan.tiles_q * p.H);
         p.slices = plan.slices_dq;
         if (a.type == LBA_F32) launch_attn_dq<float>(p, direct, st); else launch_attn_dq<bf16_t>(p, direct, st);
+        if (p.slices > 1) { if (a.type == LBA_F32) launch_join_grad<float, false>(p, st); else launch_join_grad<bf16_t, false>(p, st); }
     }
     if (keys && (plan.tiles_k > 0 || p.clear)) {
         const lba_strides g = {(int64_t)a.H * a.D, a.D};
@@ -51,6 +83,7 @@ int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, c
         p.units = (int32_t)(plan.tiles_k * p.KV);
         p.slices = plan.slices_dkv;
         if (a.type == LBA_F32) launch_attn_dkv<float>(p, direct, st); else launch_attn_dkv<bf16_t>(p, direct, st);
+        if (p.slices > 1) { if (a.type == LBA_F32) launch_join_grad<float, true>(p, st); else launch_join_grad<bf16_t, true>(p, st); }
     }
     return hipGetLastError() == hipSuccess ? LBA_OK : LBA_ERR_LAUNCH;
 }

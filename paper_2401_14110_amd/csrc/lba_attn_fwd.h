@@ -11,13 +11,6 @@
 
 namespace lba {
 
-// store(pointer to O's type): O as what it is
-template <typename F> __device__ __forceinline__ void with_output(const AttnParams& p, F store) {
-    if (p.o_type == LBA_F32) store((float*)p.O);
-    else if (p.o_type == LBA_BF16) store((bf16_t*)p.O);
-    else store((uint8_t*)p.O);
-}
-
 // a part's maximum, in units of log 2, and sum of weights
 __device__ __forceinline__ void store_end(const AttnParams& p, int64_t to, float top, float sum) {
     float* end = p.part + (int64_t)p.slices * p.T * p.H * p.D + to * 2;
@@ -243,39 +236,12 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     });
 }
 
-// O and lse from the parts: a workgroup a row, a lane an element of its heads.
-template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
-    const int64_t rows = (int64_t)p.T * p.H;
-    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-        const int b = sequence_of(p.starts, p.T, p.count, t);
-        if (b < 0) continue;
-        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
-        const int n = slices_used(steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>), p.slices);
-        if (n <= 1) continue;                            // stored by its only workgroup
-        for (int i = threadIdx.x; i < p.H * p.D; i += 256) {
-            const int64_t row = (int64_t)t * p.H + i / p.D;
-            const float* end = p.part + p.slices * rows * p.D + row * 2;
-            float top = -__builtin_inff(), sum = 0.0f, v = 0.0f;
-            for (int x = 0; x < n; ++x) top = fmaxf(top, end[x * rows * 2]);
-            const float base = top == -__builtin_inff() ? 0.0f : top;
-            for (int x = 0; x < n; ++x) {
-                const float f = __builtin_amdgcn_exp2f(end[x * rows * 2] - base);
-                sum = fmaf(f, end[x * rows * 2 + 1], sum);
-                v = fmaf(f, p.part[x * rows * p.D + row * p.D + i % p.D], v);
-            }
-            with_output(p, [&](auto* o) { store_one(o + (int64_t)t * p.H * p.D + i, sum == 0.0f ? 0.0f : v / sum, p.fmt); });
-            if (p.lse && i % p.D == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
-        }
-    }
-}
-
 template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st) {
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
         if (direct) hipLaunchKernelGGL((attn_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
-        if (p.slices > 1) hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(p.T < (1 << 20) ? p.T : (1 << 20))), dim3(256), 0, st, p); \
         return; \
     }
     LBA_ATTN(32)

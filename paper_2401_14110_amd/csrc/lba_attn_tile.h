@@ -246,7 +246,7 @@ __device__ __forceinline__ void wave_words_done() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// a lane's row of a head as fragments: `D` elements from `at`, zeros behind; row < 0: zeros.  FLIP: with the other sign.
+// a lane's row of a head as fragments: `D` elements from `at`, zeros behind; zeros where it is not there
 template <typename T, int DP> __device__ __forceinline__ void load_frags(const void* at, bool there, int D, int half, Frag<T> (&f)[DP / 16]) {
     typedef typename Bits<T>::type B;
     const B* p = (const B*)at;
@@ -287,8 +287,14 @@ __device__ __forceinline__ float sum_of_halves(float v) {
     return __uint_as_float(x[0]) + __uint_as_float(x[1]);
 }
 
-// ---- rows of no sequence ----------------------------------------------------------------------
+// store(pointer to O's type): O as what it is
+template <typename F> __device__ __forceinline__ void with_output(const AttnParams& p, F store) {
+    if (p.o_type == LBA_F32) store((float*)p.O);
+    else if (p.o_type == LBA_BF16) store((bf16_t*)p.O);
+    else store((uint8_t*)p.O);
+}
 
+// ---- rows of no sequence ----------------------------------------------------------------------
 
 // the rows of no sequence, by the last blocks of the grid
 template <typename T> __device__ __forceinline__ void clear_rows(const int32_t* starts, int T_rows, int count, int block, int blocks, T* out, int64_t row_stride,

@@ -19,7 +19,6 @@ struct RopeParams {
     int32_t T, H, D, pairs;
     int32_t wide;            // positions of 64 bits
     int32_t rows;            // rows of a workgroup at a time
-    int32_t heads;           // heads of a workgroup
     float gain, sign;
 };
 
@@ -65,7 +64,6 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
     T* Y = (T*)p.Y;
     const CodeFmt none = {};
     const int turned = (p.pairs + PV - 1) / PV, copied = (p.D - 2 * p.pairs + V - 1) / V, items = turned + copied;
-    const int h0 = blockIdx.y * p.heads, heads = min(p.heads, p.H - h0);
     for (int64_t t0 = (int64_t)blockIdx.x * p.rows; t0 < p.T; t0 += (int64_t)gridDim.x * p.rows) {
         const int rows = (int)min((int64_t)p.rows, p.T - t0);
         __syncthreads();
@@ -75,10 +73,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
             angle[i] = turn_of(m, p.freq[i % p.pairs], p.gain, p.sign);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < rows * heads * items; i += 256) {
-            const int c = i % items, rh = i / items, h = rh % heads, r = rh / heads;
-            const T* x = X + (t0 + r) * p.x.row + (int64_t)(h0 + h) * p.x.head;
-            T* y = Y + (t0 + r) * p.y.row + (int64_t)(h0 + h) * p.y.head;
+        for (int i = threadIdx.x; i < rows * p.H * items; i += 256) {
+            const int c = i % items, rh = i / items, h = rh % p.H, r = rh / p.H;
+            const T* x = X + (t0 + r) * p.x.row + (int64_t)h * p.x.head;
+            T* y = Y + (t0 + r) * p.y.row + (int64_t)h * p.y.head;
             if (c >= turned) {
                 const int d = 2 * p.pairs + (c - turned) * V;
                 copy_some<V>((const typename Bits<T>::type*)x + d, (typename Bits<T>::type*)y + d, p.D - d);
@@ -129,9 +127,8 @@ static int rope(const void* X, lba_strides x_at, int32_t type, const void* posit
     p.T = (int32_t)T; p.H = (int32_t)H; p.D = (int32_t)D; p.pairs = (int32_t)pairs; p.wide = pos_bits == 64;
     p.gain = gain; p.sign = sign;
     p.rows = pairs > 256 ? 1 : pairs > 64 ? 2 : 4;
-    p.heads = p.H;
     const int64_t blocks = (T + p.rows - 1) / p.rows;
-    const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), (unsigned)((p.H + p.heads - 1) / p.heads));
+    const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
     if (type == LBA_F32) {
         if (interleaved) hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(256), 0, st, p);
         else hipLaunchKernelGGL((rope_kernel<float, false>), grid, dim3(256), 0, st, p);
