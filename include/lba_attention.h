@@ -46,7 +46,8 @@ int lba_rope_bwd(const void* G, lba_strides g_at, int32_t type, const void* posi
  * Query head h reads head h / (H / KV) of the keys and values (H a multiple of KV, else LBA_ERR_SHAPE).  Query i of n sees key j of m iff
  * causal == 0 or j <= i + m - n: the last query sees all.  What is hidden does not matter, infinities and NaN included.
  * Rows of no sequence are left as they were, or, clear != 0, stored as zeros (-infinity in lse).
- * Q, K and V of `type` (LBA_F32 or LBA_BF16).
+ * Q, K and V of `type` (LBA_F32 or LBA_BF16).  Float32 factors of products are three bfloat16 pieces, which hold them (numbers of 2^-100 or more
+ * in size); of the nine products of pieces the six largest are summed, the others are under 2^-24 of the whole.
  * Limits (else LBA_ERR_SHAPE): T, Tk <= 2^31 - 1, count <= 2^20, H <= 65535, 1 <= D <= 128, and (rows / 128 + count) * heads <= 2^23 for the query
  * rows with H and for the key rows with KV. */
 typedef struct {

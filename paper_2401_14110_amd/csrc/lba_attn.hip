@@ -41,40 +41,61 @@ int attn_plan(const lba_attn& a, AttnPlan* plan) {
     if (plan->tiles_q * a.H > kMostUnits || plan->tiles_k * a.KV > kMostUnits) return LBA_ERR_SHAPE;
     const int64_t step = a.type == LBA_F32 ? 32 : 64, count = a.count > 0 ? a.count : 1;
     const int64_t keys = a.Tk / count / step, queries = a.T / count / step * (a.KV > 0 ? a.H / a.KV : 1);
-    const bool f32 = a.type == LBA_F32;                  // its steps take four times as long: shorter parts are worth a join
-    plan->slices = plan->slices_dq = slices_for(plan->tiles_q * a.H, keys, 512, f32 ? 2 : 4);
-    plan->slices_dkv = slices_for(plan->tiles_k * a.KV, queries, f32 || a.D <= 64 ? 512 : 256, f32 ? 2 : 4);
+    // Float32's steps of half as many rows take three times as long, so shorter parts are worth a join, and a pass whose workgroups have a CU each is cut
+    // for one round of them.  7 sequences of 33 to 517, 6 heads of 83, with 384, 512 and 1024 workgroups: forward 35, 31 and 30 us (two on a CU), dQ 51,
+    // 61 and 72, dK and dV 64, 60 and 59, their join 11, 12 and 13.
+    const bool f32 = a.type == LBA_F32;
+    const int64_t least = f32 ? 2 : 4;
+    plan->slices = slices_for(plan->tiles_q * a.H, keys, f32 ? 1024 : 512, least);
+    plan->slices_dq = slices_for(plan->tiles_q * a.H, keys, f32 ? 384 : 512, least);
+    plan->slices_dkv = slices_for(plan->tiles_k * a.KV, queries, f32 || a.D <= 64 ? 512 : 256, least);
     return LBA_OK;
 }
 
-// O and lse from the parts: a workgroup a row, a lane an element of its heads.
+// O and lse from the parts: a workgroup eight heads of a row, a wave two, a lane a part's weight and then two elements.
 template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
     const int64_t rows = (int64_t)p.T * p.H;
+    const int lane = threadIdx.x & 63;
     for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-        const int b = sequence_of(p.starts, p.T, p.count, t);
-        if (b < 0) continue;
-        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const TileOf at = find_row(p.starts, p.T, p.starts_k, p.Tk, p.count, t);
+        if (at.b < 0) continue;
+        const Rows rq = at.mine, rk = at.other;
         const int n = slices_used(steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>), p.slices);
         if (n <= 1) continue;                            // stored by its only workgroup
-        for (int i = threadIdx.x; i < p.H * p.D; i += 256) {
-            const int64_t row = (int64_t)t * p.H + i / p.D;
-            const float* end = p.part + p.slices * rows * p.D + row * 2;
-            float top = -__builtin_inff(), sum = 0.0f, v = 0.0f;
-            for (int x = 0; x < n; ++x) top = fmaxf(top, end[x * rows * 2]);
-            const float base = top == -__builtin_inff() ? 0.0f : top;
-            for (int x = 0; x < n; ++x) {
-                const float f = __builtin_amdgcn_exp2f(end[x * rows * 2] - base);
-                sum = fmaf(f, end[x * rows * 2 + 1], sum);
-                v = fmaf(f, p.part[x * rows * p.D + row * p.D + i % p.D], v);
-            }
-            with_output(p, [&](auto* o) { store_one(o + (int64_t)t * p.H * p.D + i, sum == 0.0f ? 0.0f : v / sum, p.fmt); });
-            if (p.lse && i % p.D == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
+        const int h0 = blockIdx.y * 8 + threadIdx.x / 64 * 2, heads = min(2, p.H - h0);
+        if (heads < 1) return;
+        const int64_t row = (int64_t)t * p.H + h0;
+        float most[2], weight[2], sum[2], v[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float* end = p.part + p.slices * rows * p.D + (min(lane, n - 1) * rows + row + (h < heads ? h : 0)) * 2;
+            most[h] = end[0];
+            sum[h] = end[1];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float top = wave_max(most[h]), base = top == -__builtin_inff() ? 0.0f : top;
+            weight[h] = __builtin_amdgcn_exp2f(most[h] - base);
+            sum[h] = wave_sum(lane < n ? weight[h] * sum[h] : 0.0f);
+            most[h] = top;
+        }
+        sum_parts(p.part + row * p.D, rows * p.D, n, heads, p.D, [&](int h, int x) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight[h]), x)); }, v);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (h >= heads) break;
+            const float inv = sum[h] == 0.0f ? 0.0f : 1.0f / sum[h];
+            with_output(p, [&](auto* o) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (lane + 64 * i < p.D) store_one(o + (row + h) * p.D + lane + 64 * i, v[h][i] * inv, p.fmt);
+            });
+            if (p.lse && lane == 0) p.lse[row + h] = sum[h] == 0.0f ? -__builtin_inff() : (most[h] + __builtin_amdgcn_logf(sum[h])) * 0.693147181f;
         }
     }
 }
 
 template <typename T> static void launch_join(const AttnParams& p, hipStream_t st) {
-    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(p.T < (1 << 20) ? p.T : (1 << 20))), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)(p.T < (1 << 20) ? p.T : (1 << 20)), (unsigned)(p.H + 7) / 8), dim3(256), 0, st, p);
 }
 
 }  // namespace lba

@@ -15,16 +15,15 @@ namespace lba {
 constexpr float kLog2e = 1.44269504f;
 
 template <typename T, int DP, bool DIRECT>
-__global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq_kernel(AttnParams p) {
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 32) ? 2 : 1) void attn_dq_kernel(AttnParams p) {
     constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
-    constexpr int TILE = KT * DP * (int)sizeof(T);
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of keys and values
     if ((int)blockIdx.x >= p.units * p.slices) {
         const CodeFmt none = {};
         clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, (T*)p.dQ, p.dq.row, p.dq.head, p.H, p.D, (float*)nullptr, none);
         return;
     }
-    const int unit = unit_of(blockIdx.x % p.units, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
+    const int unit = p.slices > 1 ? blockIdx.x % p.units : unit_of(blockIdx.x, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
     const TileOf at = find_tile(p.starts, p.T, p.starts_k, p.Tk, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);
     if (at.b < 0) return;
@@ -38,7 +37,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     if (first >= tiles && slice > 0) return;
     const bool there = i < rq.n;
 
-    Loader<T, DP, KT, DIRECT> lk, lv;
+    Loader<T, DP, DIRECT> lk, lv;
     lk.start((const T*)p.K + (int64_t)(rk.first + first * KT) * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
     lv.start((const T*)p.V + (int64_t)(rk.first + first * KT) * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
     if (tiles > first) {
@@ -61,24 +60,23 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     f32x16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
-    auto step = [&](int kt, auto edge, auto buffer) {
+    auto step = [&](int kt, auto edge, int buf) {
         constexpr bool EDGE = decltype(edge)::value != 0;
-        constexpr int BUF = decltype(buffer)::value;
         const int k0 = kt * KT;
-        uint8_t* const tk = lds[BUF][0];
-        uint8_t* const tv = lds[BUF][1];
+        uint8_t* const tk = lds[buf][0];
+        uint8_t* const tv = lds[buf][1];
         lk.put(tk);
         lv.put(tv);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (kt + 1 < tiles) {
-            lk.load(lds[BUF ^ 1][0], rk.n - k0 - KT);
-            lv.load(lds[BUF ^ 1][1], rk.n - k0 - KT);
+            lk.load(lds[buf ^ 1][0], rk.n - k0 - KT);
+            lv.load(lds[buf ^ 1][1], rk.n - k0 - KT);
         }
         bool broken = false;
         if constexpr (EDGE) {
-            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tk);
+            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP>(tk);
             if (k0 >= most) return;
         }
 #pragma unroll
@@ -119,14 +117,13 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_dq
     };
     const int whole = min(tiles, least_all / KT);
     int kt = first;
-    for (; kt + 1 < whole; kt += 2) {
-        step(kt, Known<0>{}, Known<0>{});
-        step(kt + 1, Known<0>{}, Known<1>{});
+    if constexpr (DIRECT) {
+        for (; kt + 1 < whole; kt += 2) {
+            step(kt, Known<0>{}, 0);
+            step(kt + 1, Known<0>{}, 1);
+        }
     }
-    for (; kt < tiles; kt += 2) {
-        step(kt, Known<1>{}, Known<0>{});
-        if (kt + 1 < tiles) step(kt + 1, Known<1>{}, Known<1>{});
-    }
+    for (; kt < tiles; ++kt) step(kt, Known<1>{}, (kt - first) & 1);
     if (!there) return;
     if (!part.alone) store_columns(p.part + ((int64_t)slice * p.T * p.H + row) * p.D, acc, p.scale, p.D, half);
     else store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, p.scale, p.D, half);
@@ -195,8 +192,7 @@ template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams p) {
     constexpr int QT = kStep<T>, QB = QT / 32, KC = DP / 16, DT = DP / 32;
     constexpr bool PIPE = !(DIRECT && sizeof(T) == 2 && DP <= 64);
-    constexpr int TILE = QT * DP * (int)sizeof(T);
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of queries and their outputs' gradients
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of queries and their outputs' gradients
     __shared__ __attribute__((aligned(16))) float side[2][2][QT];                    // -lse in units of log 2, rowsum(G * O)
     if ((int)blockIdx.x >= p.units * p.slices) {
         const CodeFmt none = {};
@@ -204,7 +200,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         clear_rows(p.starts_k, p.Tk, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, (T*)p.dV, p.dv.row, p.dv.head, p.KV, p.D, (float*)nullptr, none);
         return;
     }
-    const int unit = unit_of(blockIdx.x % p.units, p.units), kv = unit / p.tiles, slice = blockIdx.x / p.units;
+    const int unit = p.slices > 1 ? blockIdx.x % p.units : unit_of(blockIdx.x, p.units), kv = unit / p.tiles, slice = blockIdx.x / p.units;
     const TileOf at = find_tile(p.starts_k, p.Tk, p.starts, p.T, p.count, kTileRows, unit % p.tiles);           // earlier tiles, which more queries see, first
     if (at.b < 0) return;
     const Rows rq = at.other, rk = at.mine;
@@ -219,7 +215,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     if (part.first >= steps && slice > 0) return;
     const int masked_all = first_of(at.t * kTileRows + kTileRows - 1);                           // from this query on, all of the workgroup's keys are seen
 
-    Loader<T, DP, QT, DIRECT> lq, lg;
+    Loader<T, DP, DIRECT> lq, lg;
     float side_next = 0.0f;                              // lane t of the first two waves: query t % QT of the step's lse or sum
     bool side_there = false;
     int next_tile = part.first % max(1, steps_head), next_head = part.first / max(1, steps_head);
@@ -272,11 +268,12 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         if (++n < steps) load(buf ^ 1);
         if constexpr (EDGE) {
             if (p.causal && q0 < masked_all) {
-                const bool a = tile_is_broken<T, DP, QT>(tq);
-                if (tile_is_broken<T, DP, QT>(tg) || a) { broken = true; return; }
+                const bool a = tile_is_broken<T, DP>(tq);
+                if (tile_is_broken<T, DP>(tg) || a) { broken = true; return; }
             }
             if (q0 + QT <= lo_wave) return;
         }
+        constexpr int RING = sizeof(T) == 2 ? 3 : 2;     // fragments that are under way or in use
         f32x16 s[PIPE ? QB : 1], u[PIPE ? QB : 1];
         Frag<T> w[PIPE ? QB : 1][2], f[PIPE ? QB : 1][2];
         f32x4_t base[4], delta[4];
@@ -303,22 +300,22 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
             for (int x = 0; x < 2; ++x) { w[at(b)][x] = as_frag<T>(s[at(b)], x); f[at(b)][x] = as_frag<T>(u[at(b)], x); }
         };
         auto scores = [&](int b) {                       // and PIPE the weights of the block before
-            Frag<T> ring[3][2];
+            Frag<T> ring[RING][2];
             auto fetch = [&](int x) {
-                ring[x % 3][0] = row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half);
-                ring[x % 3][1] = row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half);
+                ring[x % RING][0] = row_frag<T, DP>(tq, 32 * b + (lane & 31), x, half);
+                ring[x % RING][1] = row_frag<T, DP>(tg, 32 * b + (lane & 31), x, half);
             };
             s[at(b)] = u[at(b)] = f32x16{};
             fetch(0);
-            fetch(1);
+            if (RING > 2) fetch(1);
             if (!PIPE) sides(b);
             else if (b > 0) sides(b - 1);
 #pragma unroll
             for (int x = 0; x < KC; ++x) {
-                if (x + 2 < KC) fetch(x + 2);
+                if (x + RING - 1 < KC) fetch(x + RING - 1);
                 __builtin_amdgcn_sched_barrier(0);
-                s[at(b)] = product(ring[x % 3][0], k[x], s[at(b)]);
-                u[at(b)] = product(ring[x % 3][1], v[x], u[at(b)]);
+                s[at(b)] = product(ring[x % RING][0], k[x], s[at(b)]);
+                u[at(b)] = product(ring[x % RING][1], v[x], u[at(b)]);
                 if (PIPE && b > 0) weights(b - 1, 16 * x / KC, 16 * (x + 1) / KC);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -327,19 +324,19 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         auto sums = [&](int b) {                         // and PIPE, with the first block, the weights of the last
             constexpr int N = 2 * DT;                    // column tiles of both halves of the block
             const bool last = PIPE && QB > 1 && b == 0;
-            Frag<T> ring[3][2];
+            Frag<T> ring[RING][2];
             auto fetch = [&](int i) {
-                ring[i % 3][0] = column_frag<T, DP>(tg, 32 * b + 16 * (i / DT), i % DT, lane);
-                ring[i % 3][1] = column_frag<T, DP>(tq, 32 * b + 16 * (i / DT), i % DT, lane);
+                ring[i % RING][0] = column_frag<T, DP>(tg, 32 * b + 16 * (i / DT), i % DT, lane);
+                ring[i % RING][1] = column_frag<T, DP>(tq, 32 * b + 16 * (i / DT), i % DT, lane);
             };
             fetch(0);
-            fetch(1);
+            if (RING > 2) fetch(1);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (i + 2 < N) fetch(i + 2);
+                if (i + RING - 1 < N) fetch(i + RING - 1);
                 __builtin_amdgcn_sched_barrier(0);
-                dv[i % DT] = product(ring[i % 3][0], w[at(b)][i / DT], dv[i % DT]);
-                dk[i % DT] = product(ring[i % 3][1], f[at(b)][i / DT], dk[i % DT]);
+                dv[i % DT] = product(ring[i % RING][0], w[at(b)][i / DT], dv[i % DT]);
+                dk[i % DT] = product(ring[i % RING][1], f[at(b)][i / DT], dk[i % DT]);
                 if (last) weights(QB - 1, 16 * i / N, 16 * (i + 1) / N);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -391,7 +388,7 @@ template <typename T> void launch_attn_dq(const AttnParams& p, bool direct, hipS
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
-        if (direct) hipLaunchKernelGGL((attn_dq_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
+        if (sizeof(T) == 2 && direct) hipLaunchKernelGGL((attn_dq_kernel<T, DP, sizeof(T) == 2>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dq_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
         return; \
     }
@@ -405,7 +402,7 @@ template <typename T> void launch_attn_dkv(const AttnParams& p, bool direct, hip
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts_k ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
-        if (direct) hipLaunchKernelGGL((attn_dkv_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
+        if (sizeof(T) == 2 && direct) hipLaunchKernelGGL((attn_dkv_kernel<T, DP, sizeof(T) == 2>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_dkv_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
         return; \
     }

@@ -3,31 +3,35 @@
 
 namespace lba {
 
-// Gradients from the parts: a workgroup a row, a lane an element of its heads.  KEYS: dK, and blockIdx.y == 1: dV; else dQ.
+// Gradients from the parts: a workgroup eight heads of a row, a wave two, a lane two elements.  KEYS: dK, and blockIdx.z == 1: dV; else dQ.
 template <typename T, bool KEYS> __global__ __launch_bounds__(256) void attn_join_grad_kernel(AttnParams p) {
     const int heads = KEYS ? p.KV : p.H, total = KEYS ? p.Tk : p.T;
     const int64_t all = (int64_t)total * heads * p.D;
-    const float* part = p.part + blockIdx.y * p.slices * all;
-    T* out = (T*)(!KEYS ? p.dQ : blockIdx.y ? p.dV : p.dK);
-    const lba_strides at = !KEYS ? p.dq : blockIdx.y ? p.dv : p.dk;
+    const float* part = p.part + blockIdx.z * p.slices * all;
+    T* out = (T*)(!KEYS ? p.dQ : blockIdx.z ? p.dV : p.dK);
+    const lba_strides at = !KEYS ? p.dq : blockIdx.z ? p.dv : p.dk;
     const CodeFmt none = {};
     for (int t = blockIdx.x; t < total; t += gridDim.x) {
-        const int b = KEYS ? sequence_of(p.starts_k, p.Tk, p.count, t) : sequence_of(p.starts, p.T, p.count, t);
-        if (b < 0) continue;
-        const Rows rq = rows_of(p.starts, p.T, p.count, b), rk = rows_of(p.starts_k, p.Tk, p.count, b);
+        const TileOf own = KEYS ? find_row(p.starts_k, p.Tk, p.starts, p.T, p.count, t) : find_row(p.starts, p.T, p.starts_k, p.Tk, p.count, t);
+        if (own.b < 0) continue;
+        const Rows rq = KEYS ? own.other : own.mine, rk = KEYS ? own.mine : own.other;
         const int steps = KEYS ? steps_of_keys(p, rq, rk, (t - rk.first) / kTileRows, kStep<T>) * p.group : steps_of_queries(p, rq, rk, (t - rq.first) / kTileRows, kStep<T>);
         const int n = slices_used(steps, p.slices);
         if (n <= 1) continue;                            // stored by its only workgroup
-        for (int i = threadIdx.x; i < heads * p.D; i += 256) {
-            float v = 0.0f;
-            for (int x = 0; x < n; ++x) v += part[x * all + (int64_t)t * heads * p.D + i];
-            store_one(out + (int64_t)t * at.row + (int64_t)(i / p.D) * at.head + i % p.D, v, none);
-        }
+        const int h0 = blockIdx.y * 8 + threadIdx.x / 64 * 2, lane = threadIdx.x & 63, some = min(2, heads - h0);
+        if (some < 1) return;
+        float v[2][2];
+        sum_parts(part + ((int64_t)t * heads + h0) * p.D, all, n, some, p.D, [](int, int) { return 1.0f; }, v);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (h < some && lane + 64 * i < p.D) store_one(out + (int64_t)t * at.row + (int64_t)(h0 + h) * at.head + lane + 64 * i, v[h][i], none);
     }
 }
 template <typename T, bool KEYS> static void launch_join_grad(const AttnParams& p, hipStream_t st) {
-    const int rows = KEYS ? p.Tk : p.T;
-    hipLaunchKernelGGL((attn_join_grad_kernel<T, KEYS>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20)), KEYS ? 2 : 1), dim3(256), 0, st, p);
+    const int rows = KEYS ? p.Tk : p.T, heads = KEYS ? p.KV : p.H;
+    hipLaunchKernelGGL((attn_join_grad_kernel<T, KEYS>), dim3((unsigned)(rows < (1 << 20) ? rows : (1 << 20)), (unsigned)(heads + 7) / 8, KEYS ? 2 : 1), dim3(256), 0, st, p);
 }
 
 }  // namespace lba

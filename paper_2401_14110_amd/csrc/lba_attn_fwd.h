@@ -68,16 +68,16 @@ template <typename T> __device__ __forceinline__ void attn_row(const AttnParams&
     if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
 }
 
+// Where rows do not go straight to LDS one loop has all tiles: the code of two, read once each by short sequences, costs more than its edge's tests.
 template <typename T, int DP, bool DIRECT>
-__global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(AttnParams p) {
     constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
-    constexpr int TILE = KT * DP * (int)sizeof(T);
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILE];                 // buffers of keys and values
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of keys and values
     if ((int)blockIdx.x >= p.units * p.slices) {
         with_output(p, [&](auto* o) { clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, o, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt); });
         return;
     }
-    const int unit = unit_of(blockIdx.x % p.units, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
+    const int unit = p.slices > 1 ? blockIdx.x % p.units : unit_of(blockIdx.x, p.units), per = p.tiles * p.group, slice = blockIdx.x / p.units;
     const int kv = unit / per, h = kv * p.group + unit % per % p.group;
     const TileOf at = find_tile(p.starts, p.T, p.starts_k, p.Tk, p.count, kTileRows, p.tiles - 1 - unit % per / p.group);               // later tiles of a sequence, which see more, first
     if (at.b < 0) return;
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     const int first = part.first, tiles = part.last, least_all = limit(at.t * kTileRows);
     if (first >= tiles && slice > 0) return;
 
-    Loader<T, DP, KT, DIRECT> lk, lv;
+    Loader<T, DP, DIRECT> lk, lv;
     lk.start((const T*)p.K + (int64_t)(rk.first + first * KT) * p.k.row + (int64_t)kv * p.k.head, p.k.row, p.D);
     lv.start((const T*)p.V + (int64_t)(rk.first + first * KT) * p.v.row + (int64_t)kv * p.v.head, p.v.row, p.D);
     if (tiles > first) {
@@ -106,8 +106,8 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
             if constexpr (sizeof(T) == 2) {
                 q[k].w = c == 0.0f ? i32x4_t{0, 0, 0, 0} : q[k].w ^ (int32_t)0x80008000;
             } else {
-                q[k].a = c == 0.0f ? f32x4_t{0, 0, 0, 0} : -q[k].a;
-                q[k].b = c == 0.0f ? f32x4_t{0, 0, 0, 0} : -q[k].b;
+#pragma unroll
+                for (int n = 0; n < 3; ++n) q[k].w[n] = c == 0.0f ? i32x4_t{0, 0, 0, 0} : q[k].w[n] ^ (int32_t)0x80008000;
             }
         }
         c = c == 0.0f ? 1.0f : -c;
@@ -119,41 +119,41 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
     bool broken = false;                                 // a tile that some query sees in part holds infinities or NaN
     // One tile.  EDGE: some query may not see all of it; the tiles before are seen whole by every query of the workgroup.
-    auto step = [&](int kt, auto edge, auto buffer) {
+    auto step = [&](int kt, auto edge, int buf) {
         constexpr bool EDGE = decltype(edge)::value != 0;
-        constexpr int BUF = decltype(buffer)::value;
         const int k0 = kt * KT;
-        uint8_t* const tk = lds[BUF][0];
-        uint8_t* const tv = lds[BUF][1];
+        uint8_t* const tk = lds[buf][0];
+        uint8_t* const tv = lds[buf][1];
         lk.put(tk);
         lv.put(tv);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();                    // this tile is there, and the one before it has been read
         asm volatile("" ::: "memory");
         if (kt + 1 < tiles) {
-            lk.load(lds[BUF ^ 1][0], rk.n - k0 - KT);
-            lv.load(lds[BUF ^ 1][1], rk.n - k0 - KT);
+            lk.load(lds[buf ^ 1][0], rk.n - k0 - KT);
+            lv.load(lds[buf ^ 1][1], rk.n - k0 - KT);
         }
         if constexpr (EDGE) {
-            if (p.causal && k0 + KT > least_all && tile_is_broken<T, DP, KT>(tv)) { broken = true; return; }
+            if (p.causal && k0 + KT > least_all && tile_is_broken<T, DP>(tv)) { broken = true; return; }
             if (k0 >= most) return;                      // (the barriers above are everybody's)
         }
         f32x16 s[KB];
 #pragma unroll
         for (int b = 0; b < KB; ++b) s[b] = f32x16{};
-        Frag<T> f[3][KB];                                // two steps' rows are on their way while the third's are multiplied
+        constexpr int RING = sizeof(T) == 2 ? 3 : 2;     // two steps' rows (float32, of three pieces: one's) are on their way while those before are multiplied
+        Frag<T> f[RING][KB];
         auto fetch = [&](int k) {
 #pragma unroll
-            for (int b = 0; b < KB; ++b) f[k % 3][b] = row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half);
+            for (int b = 0; b < KB; ++b) f[k % RING][b] = row_frag<T, DP>(tk, 32 * b + (lane & 31), k, half);
         };
         fetch(0);
-        if (KC > 1) fetch(1);
+        if (RING > 2) fetch(1);
 #pragma unroll
         for (int k = 0; k < KC; ++k) {
-            if (k + 2 < KC) fetch(k + 2);
+            if (k + RING - 1 < KC) fetch(k + RING - 1);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int b = 0; b < KB; ++b) s[b] = product(f[k % 3][b], q[k], s[b]);
+            for (int b = 0; b < KB; ++b) s[b] = product(f[k % RING][b], q[k], s[b]);
             __builtin_amdgcn_sched_barrier(0);
         }
         if (EDGE && k0 + KT > least) {
@@ -196,14 +196,13 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 ? 2 : 1) void attn_ke
     };
     const int whole = min(tiles, least_all / KT);
     int kt = first;
-    for (; kt + 1 < whole; kt += 2) {
-        step(kt, Known<0>{}, Known<0>{});
-        step(kt + 1, Known<0>{}, Known<1>{});
+    if constexpr (DIRECT) {
+        for (; kt + 1 < whole; kt += 2) {
+            step(kt, Known<0>{}, 0);
+            step(kt + 1, Known<0>{}, 1);
+        }
     }
-    for (; kt < tiles && !broken; kt += 2) {
-        step(kt, Known<1>{}, Known<0>{});
-        if (kt + 1 < tiles && !broken) step(kt + 1, Known<1>{}, Known<1>{});
-    }
+    for (; kt < tiles && !broken; ++kt) step(kt, Known<1>{}, (kt - first) & 1);
     if (broken) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
@@ -240,7 +239,7 @@ template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStre
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
-        if (direct) hipLaunchKernelGGL((attn_kernel<T, DP, true>), grid, dim3(256), 0, st, p); \
+        if (sizeof(T) == 2 && direct) hipLaunchKernelGGL((attn_kernel<T, DP, sizeof(T) == 2>), grid, dim3(256), 0, st, p); \
         else hipLaunchKernelGGL((attn_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
         return; \
     }

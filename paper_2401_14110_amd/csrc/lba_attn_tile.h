@@ -19,26 +19,54 @@ namespace lba {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x2_t __attribute__((ext_vector_type(2)));
 typedef int16_t i16x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_v __attribute__((ext_vector_type(2)));
 
 __device__ __attribute__((aligned(16))) const uint32_t attn_zeros[4] = {0, 0, 0, 0};
 
-// eight elements of a factor's row
+// Eight elements of a factor's row.  Float32: in three bfloat16 pieces, which hold all 24 bits (of numbers of 2^-100 or more)
 template <typename T> struct Frag;
 template <> struct Frag<bf16_t> { i32x4_t w; };
-template <> struct Frag<float> { f32x4_t a, b; };
+template <> struct Frag<float> { i32x4_t w[3]; };
 
-// c + a . b of 32 x 16 and 16 x 32.  Float32: eight products of depth 2, the two halves of the wave one row each
+// Two numbers' pieces: the nearest bfloat16 number, that of what is left, and the rest.  Not FINITE: first pieces stay within bfloat16, so that an
+// infinity or a NaN is in the last, and numbers that would round up to infinity do not get one.
+template <bool FINITE> __device__ __forceinline__ void split_two(float x, float y, int32_t (&w)[3]) {
+    constexpr float TOP = 3.38953139e38f;                // bfloat16's largest number
+    auto near = [](float v) { return FINITE ? v : __builtin_amdgcn_fmed3f(v, -TOP, TOP); };
+    const bf16x2_v a = {(bf16_t)near(x), (bf16_t)near(y)};
+    x -= (float)a[0];
+    y -= (float)a[1];
+    const bf16x2_v b = {(bf16_t)near(x), (bf16_t)near(y)};
+    const bf16x2_v c = {(bf16_t)(x - (float)b[0]), (bf16_t)(y - (float)b[1])};
+    w[0] = __builtin_bit_cast(int32_t, a);
+    w[1] = __builtin_bit_cast(int32_t, b);
+    w[2] = __builtin_bit_cast(int32_t, c);
+}
+template <bool FINITE> __device__ __forceinline__ Frag<float> split_eight(const float (&x)[8]) {
+    Frag<float> f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        int32_t w[3];
+        split_two<FINITE>(x[2 * j], x[2 * j + 1], w);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) f.w[n][j] = w[n];
+    }
+    return f;
+}
+
+// c + a . b of 32 x 16 and 16 x 32.  Float32: the six products of pieces that are 2^-16 or more of the whole; the three others are under 2^-24 of it
+// together.  (They take 192 cycles, float32's own instructions 512.)
 __device__ __forceinline__ f32x16 product(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_v, a.w), __builtin_bit_cast(bf16x8_v, b.w), c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x16 product(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.a[j], b.a[j], c, 0, 0, 0);
+    for (int n = 2; n >= 0; --n)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.b[j], b.b[j], c, 0, 0, 0);
+        for (int j = 0; j <= n; ++j) c = product(Frag<bf16_t>{a.w[j]}, Frag<bf16_t>{b.w[n - j]}, c);
     return c;
 }
 
@@ -54,26 +82,32 @@ __device__ __forceinline__ float dot(const Frag<bf16_t>& a, const Frag<bf16_t>& 
     return s;
 }
 __device__ __forceinline__ float dot(const Frag<float>& a, const Frag<float>& b) {
+    auto low = [](const Frag<float>& f, int j) { return (__uint_as_float((uint32_t)f.w[2][j] << 16) + __uint_as_float((uint32_t)f.w[1][j] << 16)) + __uint_as_float((uint32_t)f.w[0][j] << 16); };
+    auto high = [](const Frag<float>& f, int j) {
+        return (__uint_as_float((uint32_t)f.w[2][j] & 0xFFFF0000u) + __uint_as_float((uint32_t)f.w[1][j] & 0xFFFF0000u)) + __uint_as_float((uint32_t)f.w[0][j] & 0xFFFF0000u);
+    };
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s = fmaf(a.b[j], b.b[j], fmaf(a.a[j], b.a[j], s));
+    for (int j = 0; j < 4; ++j) s = fmaf(high(a, j), high(b, j), fmaf(low(a, j), low(b, j), s));
     return s;
 }
 
 // registers 8 k .. 8 k + 7 of a result as a fragment
 template <typename T> __device__ __forceinline__ Frag<T> as_frag(const f32x16& s, int k) {
-    Frag<T> f;
     if constexpr (sizeof(T) == 2) {
+        Frag<T> f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const bf16x2_v two = {(bf16_t)s[8 * k + 2 * j], (bf16_t)s[8 * k + 2 * j + 1]};
             f.w[j] = __builtin_bit_cast(int32_t, two);
         }
+        return f;
     } else {
+        float x[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { f.a[j] = s[8 * k + j]; f.b[j] = s[8 * k + 4 + j]; }
+        for (int j = 0; j < 8; ++j) x[j] = s[8 * k + j];
+        return split_eight<true>(x);
     }
-    return f;
 }
 
 // row of the result's register r in this lane's half
@@ -81,48 +115,50 @@ __device__ __forceinline__ constexpr int row_of(int r) { return (r % 4) + 8 * (r
 
 // ---- tiles in LDS ---------------------------------------------------------------------------
 //
-// A row of DP elements (D rounded up to 32, zeros behind D) is C = DP * sizeof(T) / 16 pieces of 16 bytes; piece c of row r stands at place
-// c ^ turn(r) of its row.  Then the 16 lanes of a row read (one piece of 16 rows) and those of a transposed read (four pieces of four rows)
-// meet 64 different banks.
+// A row of DP elements (D rounded up to 32, zeros behind D) is C = DP / 8 pieces of 16 bytes; piece c of row r stands at place c ^ turn(r) of its row.
+// Then the 16 lanes of a row read (one piece of 16 rows) and those of a transposed read (four pieces of four rows) meet 64 different banks.
+// Float32: three such tiles one behind another, of the numbers' first, second and third pieces.
 template <int C> __device__ __forceinline__ int turn(int r) {
     if constexpr (C % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
     else if constexpr (C % 8 == 0) return ((r & 2) << 1) | ((r >> 2) & 3);
     else return (r >> 2) & 3;
 }
+template <typename T> constexpr int kStep = sizeof(T) == 2 ? 64 : 32;                // rows of a tile: keys or queries of a step
+template <typename T> constexpr int kPieces = sizeof(T) == 2 ? 1 : 3;
+template <typename T, int DP> constexpr int kTileBytes = kStep<T> * DP * 2 * kPieces<T>;
 
 // the fragment of row `row` (this lane's) with elements 16 k + 8 (l / 32) ..
 template <typename T, int DP> __device__ __forceinline__ Frag<T> row_frag(const uint8_t* tile, int row, int k, int half) {
-    constexpr int C = DP * sizeof(T) / 16;
-    const uint8_t* at = tile + row * (C * 16);
+    constexpr int C = DP / 8;
+    const uint8_t* at = tile + row * (C * 16) + ((2 * k + half) ^ turn<C>(row)) * 16;
     Frag<T> f;
     if constexpr (sizeof(T) == 2) {
-        f.w = *(const i32x4_t*)(at + ((2 * k + half) ^ turn<C>(row)) * 16);
+        f.w = *(const i32x4_t*)at;
     } else {
-        f.a = *(const f32x4_t*)(at + ((4 * k + 2 * half) ^ turn<C>(row)) * 16);
-        f.b = *(const f32x4_t*)(at + ((4 * k + 2 * half + 1) ^ turn<C>(row)) * 16);
+#pragma unroll
+        for (int n = 0; n < 3; ++n) f.w[n] = *(const i32x4_t*)(at + n * (kTileBytes<T, DP> / 3));
     }
     return f;
 }
 // The fragment of column 32 t + l % 32 with rows row0 + (j % 4) + 8 (j / 4) + 4 (l / 32), row0 a multiple of 16.  A transposed read gives each of 16 lanes
 // column i of a 4 x 16 block whose rows four lanes each address.
 template <typename T, int DP> __device__ __forceinline__ Frag<T> column_frag(const uint8_t* tile, int row0, int t, int lane) {
-    constexpr int C = DP * sizeof(T) / 16;
-    Frag<T> f;
-    if constexpr (sizeof(T) == 2) {
-        const int r = row0 + 4 * (lane / 32) + (lane & 15) / 4, c = 4 * t + 2 * ((lane / 16) & 1) + (lane & 3) / 2;
+    constexpr int C = DP / 8;
+    const int r = row0 + 4 * (lane / 32) + (lane & 15) / 4, c = 4 * t + 2 * ((lane / 16) & 1) + (lane & 3) / 2;
+    auto columns = [&](const uint8_t* at) {
         typedef __attribute__((address_space(3))) i16x4_t* lds_ptr;
         union { i16x4_t s[2]; i32x4_t w; } u;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (r + 8 * i) * (C * 16) + (c ^ turn<C>(r + 8 * i)) * 16 + (lane & 1) * 8));
-        f.w = u.w;
+            u.s[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + (r + 8 * i) * (C * 16) + (c ^ turn<C>(r + 8 * i)) * 16 + (lane & 1) * 8));
+        return u.w;
+    };
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        f.w = columns(tile);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = row0 + row_of(j) + 4 * (lane / 32);
-            const float x = *(const float*)(tile + r * (C * 16) + ((8 * t + (lane & 31) / 4) ^ turn<C>(r)) * 16 + (lane & 3) * 4);
-            if (j < 4) f.a[j] = x; else f.b[j - 4] = x;
-        }
+        for (int n = 0; n < 3; ++n) f.w[n] = columns(tile + n * (kTileBytes<T, DP> / 3));
     }
     return f;
 }
@@ -136,12 +172,51 @@ __device__ __forceinline__ void piece_to_lds(uint32_t to, const void* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 
-// Rows of a head on their way to a tile of ROWS rows.  DIRECT: rows are whole pieces of 16 aligned bytes, a tile's rows within 2^31 bytes, and go
-// from memory to LDS without registers in between; else a lane holds them until they are put down.  What is behind `rows` rows or D elements
-// is zeros.
-template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
-    static constexpr int C = DP * sizeof(T) / 16, V = 16 / sizeof(T), N = ROWS * C / 256;
-    static_assert(ROWS * C % 256 == 0, "whole pieces a lane");
+// The end of a row that is no whole vector: the row's last V elements are loaded, and moved down by those that belong to the vector before, once
+// they are there.  (One by one they would be waited for where they are loaded, and with them all that is under way.)
+template <typename B, int V> __device__ __forceinline__ Raw<B, V> load_all(const B* p, bool there) {
+    Raw<B, V> r = {};
+    if (there) r.v = *(const typename Vec<B, V>::type*)p;
+    return r;
+}
+// the first `n` of fewer than V elements (a loop: such heads are rare, and this stands wherever a tile is loaded)
+template <typename B, int V> __device__ __forceinline__ Raw<B, V> load_few(const B* p, int n) {
+    i32x4_t w = {0, 0, 0, 0};
+#pragma clang loop unroll(disable)
+    for (int j = n - 1; j >= 0; --j) {
+        if constexpr (sizeof(B) == 2) {
+            w = i32x4_t{w[0] << 16, (int32_t)__builtin_amdgcn_alignbit(w[1], w[0], 16), (int32_t)__builtin_amdgcn_alignbit(w[2], w[1], 16),
+                        (int32_t)__builtin_amdgcn_alignbit(w[3], w[2], 16)};
+            w[0] |= p[j];
+        } else {
+            w = i32x4_t{(int32_t)__float_as_uint(p[j]), w[0], w[1], w[2]};
+        }
+    }
+    Raw<B, V> r;
+    r.v = __builtin_bit_cast(decltype(r.v), w);
+    return r;
+}
+template <typename B, int V> __device__ __forceinline__ int before_end(int left) { return left > 0 && left < V ? V - left : 0; }
+template <typename B, int V> __device__ __forceinline__ void move_down(Raw<B, V>& r, int by) {
+    i32x4_t w = __builtin_bit_cast(i32x4_t, r.v);
+    int step = by;
+    if constexpr (sizeof(B) == 2) {
+        const i32x4_t m = {(int32_t)__builtin_amdgcn_alignbit(w[1], w[0], 16), (int32_t)__builtin_amdgcn_alignbit(w[2], w[1], 16),
+                           (int32_t)__builtin_amdgcn_alignbit(w[3], w[2], 16), (int32_t)((uint32_t)w[3] >> 16)};
+        w = step & 1 ? m : w;
+        step >>= 1;
+    }
+    w = step & 1 ? i32x4_t{w[1], w[2], w[3], 0} : w;
+    w = step & 2 ? i32x4_t{w[2], w[3], 0, 0} : w;
+    r.v = __builtin_bit_cast(decltype(r.v), w);
+}
+
+// Rows of a head on their way to a tile.  DIRECT: rows are whole pieces of 16 aligned bytes of bfloat16, a tile's rows within 2^31 bytes, and go from
+// memory to LDS without registers in between; else a lane holds 16 bytes each until they are put down.  What is behind `rows` rows or D
+// elements is zeros.
+template <typename T, int DP, bool DIRECT> struct Loader {
+    static constexpr int ROWS = kStep<T>, C = DP * sizeof(T) / 16, V = 16 / sizeof(T), N = ROWS * C / 256;
+    static_assert(ROWS * C % 256 == 0 && !(DIRECT && sizeof(T) != 2), "whole pieces a lane");
     // 256 pieces are whole groups of 16 rows, after which turn() is the same: a lane's pieces are the same ones of rows 256 / C apart
     static constexpr bool EVEN = 4096 % (C * 256) == 0 && C <= 16;
     static constexpr int P = EVEN ? 1 : N;
@@ -150,7 +225,9 @@ template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
     int64_t stride;
     typename std::conditional<DIRECT, uint32_t, int64_t>::type at[P];                // this lane's pieces in a tile: bytes, or elements, from its start
     int left[P];             // how many elements of the row are from there on
+    int down[P];             // not DIRECT: by how many elements a piece is moved down
     bool full;               // rows have no pieces of zeros
+    bool ragged, tiny;       // not DIRECT: rows end inside a piece, the first one
     Raw<B, V> held[DIRECT ? 1 : N];
 
     __device__ __forceinline__ void start(const void* rows, int64_t row_stride, int D) {
@@ -159,10 +236,13 @@ template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
         full = D == DP;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int p = threadIdx.x + 256 * i, r = p / C, c = (p % C) ^ turn<C>(r);
+            const int p = threadIdx.x + 256 * i, r = p / C, c = sizeof(T) == 2 ? (p % C) ^ turn<C>(r) : p % C;
             left[i] = D - c * V;
-            at[i] = (r * row_stride + c * V) * (DIRECT ? (int)sizeof(T) : 1);
+            down[i] = DIRECT || D < V ? 0 : before_end<B, V>(left[i]);
+            at[i] = (r * row_stride + c * V - down[i]) * (DIRECT ? (int)sizeof(T) : 1);
         }
+        ragged = D % V != 0 && D >= V;
+        tiny = D < V;
     }
     // the next tile, of which `rows` rows are there
     __device__ __forceinline__ void load(uint8_t* tile, int rows) {
@@ -183,32 +263,47 @@ template <typename T, int DP, int ROWS, bool DIRECT> struct Loader {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const bool in = ((int)threadIdx.x + 256 * i) / C < rows;
-                held[i] = load_raw<B, V>((EVEN ? base + i * (256 / C) * stride : base) + at[EVEN ? 0 : i], in ? left[EVEN ? 0 : i] : 0);
+                const B* src = (EVEN ? base + i * (256 / C) * stride : base) + at[EVEN ? 0 : i];
+                if (tiny) held[i] = load_few<B, V>(src, in ? left[EVEN ? 0 : i] : 0);
+                else held[i] = load_all<B, V>(src, in && left[EVEN ? 0 : i] > 0);
             }
         }
         base += stride * ROWS;
     }
-    __device__ __forceinline__ void put(uint8_t* tile) const {
+    __device__ __forceinline__ void put(uint8_t* tile) {
         if constexpr (!DIRECT) {
+            if (ragged) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) *(i32x4_t*)(tile + (threadIdx.x + 256 * i) * 16) = __builtin_bit_cast(i32x4_t, held[i].v);
+                for (int i = 0; i < N; ++i) move_down<B, V>(held[i], down[EVEN ? 0 : i]);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int p = threadIdx.x + 256 * i;
+                if constexpr (sizeof(T) == 2) {
+                    *(i32x4_t*)(tile + p * 16) = __builtin_bit_cast(i32x4_t, held[i].v);
+                } else {                                 // four numbers: half a piece of each tile
+                    const f32x4_t x = __builtin_bit_cast(f32x4_t, held[i].v);
+                    const int r = p / C, c = p % C;
+                    uint8_t* const at = tile + r * (DP * 2) + ((c / 2) ^ turn<DP / 8>(r)) * 16 + (c & 1) * 8;
+                    int32_t a[3], b[3];
+                    split_two<false>(x[0], x[1], a);
+                    split_two<false>(x[2], x[3], b);
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) *(i32x2_t*)(at + n * (kTileBytes<T, DP> / 3)) = i32x2_t{a[n], b[n]};
+                }
+            }
         }
     }
 };
 
-// Whether the tile holds an infinity or a NaN, looked for by the whole workgroup (a barrier: all of it calls).
-template <typename T, int DP, int ROWS> __device__ __forceinline__ bool tile_is_broken(const uint8_t* tile) {
-    constexpr int N = ROWS * DP * (int)sizeof(T) / 16 / 256;
+// Whether the tile holds an infinity or a NaN (float32: its last pieces do), looked for by the whole workgroup (a barrier: all of it calls).
+template <typename T, int DP> __device__ __forceinline__ bool tile_is_broken(const uint8_t* tile) {
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const i32x4_t w = *(const i32x4_t*)(tile + (threadIdx.x + 256 * i) * 16);
+    for (int i = threadIdx.x; i < kStep<T> * DP / 8; i += 256) {
+        const i32x4_t w = *(const i32x4_t*)(tile + (kPieces<T> - 1) * (kTileBytes<T, DP> / kPieces<T>) + i * 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x = (uint32_t)w[j];
-            if constexpr (sizeof(T) == 2) bad |= (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
-            else bad |= (x & 0x7F800000u) == 0x7F800000u;
-        }
+        for (int j = 0; j < 4; ++j) bad |= ((uint32_t)w[j] & 0x7F80u) == 0x7F80u || ((uint32_t)w[j] & 0x7F800000u) == 0x7F800000u;
     }
     return __syncthreads_or(bad) != 0;
 }
@@ -227,12 +322,8 @@ __device__ __forceinline__ Frag<bf16_t> without_broken(Frag<bf16_t> f) {
     }
     return f;
 }
-__device__ __forceinline__ Frag<float> without_broken(Frag<float> f) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        f.a[j] = (__float_as_uint(f.a[j]) & 0x7F800000u) == 0x7F800000u ? 0.0f : f.a[j];
-        f.b[j] = (__float_as_uint(f.b[j]) & 0x7F800000u) == 0x7F800000u ? 0.0f : f.b[j];
-    }
+__device__ __forceinline__ Frag<float> without_broken(Frag<float> f) {                // (the other pieces of such are numbers)
+    f.w[2] = without_broken(Frag<bf16_t>{f.w[2]}).w;
     return f;
 }
 __device__ __forceinline__ float wave_max(float v) {
@@ -249,16 +340,31 @@ __device__ __forceinline__ void wave_words_done() {
 // a lane's row of a head as fragments: `D` elements from `at`, zeros behind; zeros where it is not there
 template <typename T, int DP> __device__ __forceinline__ void load_frags(const void* at, bool there, int D, int half, Frag<T> (&f)[DP / 16]) {
     typedef typename Bits<T>::type B;
+    constexpr int V = 16 / sizeof(T), N = 8 / V;         // N vectors a fragment
     const B* p = (const B*)at;
+    Raw<B, V> r[DP / 16][N];
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int d = 16 * k + 8 * half + V * i, left = there ? D - d : 0;
+            if (D < V) r[k][i] = load_few<B, V>(p + d, left);
+            else r[k][i] = load_all<B, V>(p + d - before_end<B, V>(left), left > 0);
+        }
+    if (D % V != 0 && D >= V) {
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) move_down<B, V>(r[k][i], before_end<B, V>(D - 16 * k - 8 * half - V * i));
+    }
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
-        const int d = 16 * k + 8 * half;
         if constexpr (sizeof(T) == 2) {
-            const Raw<B, 8> r = load_raw<B, 8>(p + d, there ? D - d : 0);
-            f[k].w = __builtin_bit_cast(i32x4_t, r.v);
+            f[k].w = __builtin_bit_cast(i32x4_t, r[k][0].v);
         } else {
-            f[k].a = __builtin_bit_cast(f32x4_t, load_raw<B, 4>(p + d, there ? D - d : 0).v);
-            f[k].b = __builtin_bit_cast(f32x4_t, load_raw<B, 4>(p + d + 4, there ? D - d - 4 : 0).v);
+            const f32x4_t a = __builtin_bit_cast(f32x4_t, r[k][0].v), b = __builtin_bit_cast(f32x4_t, r[k][1].v);
+            const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            f[k] = split_eight<false>(x);
         }
     }
 }
@@ -347,6 +453,55 @@ __device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, const 
     return {-1, 0, {0, 0}, {0, 0}};
 }
 
+// The sequence that row `t` of T belongs to in `starts`, with t as the tile; the whole wave calls.  64 starts at a time, then both lists at once.
+__device__ __forceinline__ TileOf find_row(const int32_t* starts, int T, const int32_t* others, int T_other, int count, int t) {
+    if (count < 1) return {-1, 0, {0, 0}, {0, 0}};
+    if (!starts) {
+        const int n = T / count, m = T_other / count, b = t / n;
+        return {b, t, {b * n, n}, {b * m, m}};
+    }
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = count;                              // it is one of lo .. hi - 1, if any
+    while (hi - lo > 64) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint64_t before = __ballot(at < hi && starts[min(at, hi - 1)] <= t);
+        if (before) lo += (63 - __builtin_clzll(before)) * step;
+        hi = min(hi, lo + step);
+    }
+    const int b = min(lo + lane, hi - 1);
+    const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
+    const uint64_t has = __ballot(t >= mine.first && t < mine.first + mine.n);
+    if (!has) return {-1, 0, {0, 0}, {0, 0}};
+    const int f = __builtin_ctzll(has);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+    return {of(b), t, {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
+}
+
+// Elements `lane` and lane + 64 of `heads` (1 or 2) neighbouring heads of a row, of n parts `stride` apart times their weights: v = the sums.  All loads of
+// four parts are on their way at once: what another workgroup has just stored is a microsecond away.
+template <typename F> __device__ __forceinline__ void sum_parts(const float* part, int64_t stride, int n, int heads, int D, F weight, float (&v)[2][2]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h][0] = v[h][1] = 0.0f;
+    for (int x0 = 0; x0 < n; x0 += 4) {
+        float y[4][2][2];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) y[x][h][i] = part[min(x0 + x, n - 1) * stride + (h < heads ? h : 0) * D + min(lane + 64 * i, D - 1)];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            if (x0 + x >= n) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) v[h][i] = fmaf(weight(h, x0 + x), y[x][h][i], v[h][i]);
+        }
+    }
+}
+
 // Part `slice` of what a workgroup does in n steps, cut into at most `slices` parts of two steps or more: steps first .. last - 1 (none in some of
 // the later ones), `alone` where one part has them all.
 struct Slice {
@@ -371,7 +526,6 @@ __device__ __forceinline__ int steps_of_keys(const AttnParams& p, const Rows& rq
     const int lo = first_query(p, rq, rk, t * kTileRows);
     return rq.n > lo ? (rq.n + size - 1) / size - lo / size : 0;
 }
-template <typename T> constexpr int kStep = sizeof(T) == 2 ? 64 : 32;                // keys or queries of a step
 
 // how many tiles there may be
 inline int64_t most_tiles(const int32_t* starts, int64_t T, int64_t count, int size) {
