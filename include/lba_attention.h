@@ -101,7 +101,7 @@ typedef struct {
 int lba_cache_write(lba_cache4 c, const int32_t* starts, int64_t T, const void* K, lba_strides k_at, const void* V, lba_strides v_at, int32_t type,
                     void* hip_stream);
 
-/* Reads the newest tokens back, in the same arrangement, exactly (numbers under 2^-126 in size as zero): K and V [T, KV, D] of `type`.
+/* Reads the newest tokens back, in the same arrangement, exactly (numbers under 2^-126 in size as they are or as zero): K and V [T, KV, D] of `type`.
  * Positions below 0 read as zeros.  Rows of no sequence are left as they were, or, clear != 0, stored as zeros. */
 int lba_cache_read(lba_cache4 c, const int32_t* starts, int64_t T, void* K, lba_strides k_at, void* V, lba_strides v_at, int32_t type, int32_t clear,
                    void* hip_stream);
