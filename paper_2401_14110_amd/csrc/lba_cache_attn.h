@@ -74,8 +74,8 @@ template <int D> struct Part {
     static constexpr int KC = D / 32, NS = D == 96 ? 3 : 1;                          // words of codes; blocks that differ between them
     uint32_t w[KC];
     uint8_t e[NS];
-    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int64_t line, int quarter) {
-        if (line < 0) {
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, bool there, uint64_t at, int quarter) {         // at: of the position, in codes
+        if (!there) {
 #pragma unroll
             for (int i = 0; i < KC; ++i) w[i] = 0;
 #pragma unroll
@@ -84,7 +84,7 @@ template <int D> struct Part {
         }
         typedef typename Vec<uint32_t, KC>::type V;
         typedef V AnyV __attribute__((aligned(1)));
-        const V x = *(const AnyV*)(codes + line * (D / 2) + quarter * (D / 8));
+        const V x = *(const AnyV*)(codes + at + quarter * (D / 8));
         if constexpr (KC == 1) {
             w[0] = x;
         } else {
@@ -92,7 +92,7 @@ template <int D> struct Part {
             for (int i = 0; i < KC; ++i) w[i] = x[i];
         }
 #pragma unroll
-        for (int i = 0; i < NS; ++i) e[i] = scales[line * (D / 32) + (quarter * (D / 4) + 8 * i) / 32];
+        for (int i = 0; i < NS; ++i) e[i] = scales[(at >> 4) + (quarter * (D / 4) + 8 * i) / 32];
     }
     // word i as bfloat16 numbers
     __device__ __forceinline__ i32x4_c values(int i) const {
@@ -214,10 +214,6 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) :
         }
     }
 
-    auto page_of = [&](int pos) -> int32_t { return pos < c1 ? p.c.table[(int64_t)b * p.c.table_row + p.c.page_div(pos)] : -1; };
-    auto line_at = [&](int pos, int32_t page) -> int64_t {
-        return pos < c1 && page >= 0 && page < p.c.pages ? ((int64_t)page * p.c.KV + kv) * p.c.page + p.c.page_mod(pos) : -1;
-    };
     f32x4_c acc[R][DT];
     float top[R], sum[R];
 #pragma unroll
@@ -232,19 +228,31 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) :
     // two waves a SIMD fewer: no faster.)
     Part<D> nk[2], nv[2];
     bool there[2];
-    int32_t page[2];
+    int32_t page[2], column[2], line[2];                 // of the next step's positions: their page, its place in the table, their line in it
+    const int columns = p.c.by_page.of(128), lines = 128 - columns * p.c.page;       // from one step to the next
+    const uint64_t page_bytes = (uint64_t)p.c.KV * p.c.page * (D / 2), head_bytes = (uint64_t)kv * p.c.page * (D / 2);
+    const int32_t* const pages = p.c.table + (int64_t)b * p.c.table_row;
     auto fetch = [&](int at0) {                          // codes of the step at at0, whose pages are known; then the next step's pages
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t line = line_at(at0 + 16 * u + col, page[u]);
-            nk[u].load(p.c.k, p.c.k_scale, line, quarter);
-            nv[u].load(p.c.v, p.c.v_scale, line, quarter);
-            there[u] = line >= 0;
-            page[u] = page_of(at0 + 128 + 16 * u + col);
+            const int pos = at0 + 16 * u + col;
+            there[u] = pos < c1 && (uint32_t)page[u] < (uint32_t)p.c.pages;
+            const uint64_t at = page[u] * page_bytes + (head_bytes + __umul24(line[u], D / 2));
+            nk[u].load(p.c.k, p.c.k_scale, there[u], at, quarter);
+            nv[u].load(p.c.v, p.c.v_scale, there[u], at, quarter);
+            column[u] += columns;
+            line[u] += lines;
+            if (line[u] >= p.c.page) { line[u] -= p.c.page; ++column[u]; }
+            if (pos + 128 < c1) page[u] = pages[column[u]];
         }
     };
 #pragma unroll
-    for (int u = 0; u < 2; ++u) page[u] = page_of(k0 + 16 * u + col);
+    for (int u = 0; u < 2; ++u) {
+        const int pos = k0 + 16 * u + col;
+        column[u] = p.c.by_page.of(pos);
+        line[u] = pos - column[u] * p.c.page;
+        page[u] = pos < c1 ? pages[column[u]] : -1;
+    }
     fetch(k0);
     uint8_t* const mine = lds[wave];
     bool again = false;
