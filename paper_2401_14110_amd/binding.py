@@ -1,4 +1,4 @@
-"""Thin ctypes binding over the C ABI in include/lba.h (argument marshalling only).
+"""Thin ctypes binding over the C ABI in include/lba.h, lba_layer.h and lba_attention.h (argument marshalling only).
 
 Every step of the computation runs in the HIP library; there is no CPU fallback: if the library
 has not been built, loading raises.  torch is used for device memory and for the current stream.

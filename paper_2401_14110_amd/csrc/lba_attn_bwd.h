@@ -5,6 +5,11 @@
 // one pass with sums in memory needs five).  In the first a lane pair owns a query, as in the forward pass: dQ^T = K^T . S^T.  In the second
 // it owns a key: S = Q . K^T, dV^T = G^T . P, dK^T = Q^T . S; what belongs to a query, lse and rowsum(G * O), which the first pass leaves in
 // the workspace, is then per register, and read from LDS.
+//
+// P and S are rounded to bfloat16 (float32: split into pieces) as factors of the sums' products; scores, weights and S themselves are float32.
+// Bound by the matrix cores and the weights beside them.  2 sequences of 4096 causal, 32 heads of 128 on 8: dQ, two waves a SIMD, 382 us (1080 TFLOP/s
+// of three products), dK and dV 713 (770 of four): its sums, factors and fragments are 448 registers, so that a wave is alone on its SIMD
+// and one block's products have to fill what the other's weights leave.  Two waves with half the keys each would read twice the queries.
 #ifndef LBA_ATTN_BWD_H_
 #define LBA_ATTN_BWD_H_
 

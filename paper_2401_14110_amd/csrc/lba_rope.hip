@@ -5,7 +5,7 @@
 // bytes of pairs) at a time.  The angle is a float64 product in turns, m * (f / 2 pi), from which whole quarter turns are taken before anything
 // is rounded to float32: positions of 10^6 are off by 2^-33 of a turn.  What is left is at most an eighth of a turn, where the series of cosine and sine
 // are taken to the terms of x^10 and x^9, under 2^-28 off.
-// Bound by memory: one read and one write of the tensor.
+// Bound by memory: one read and one write of the tensor (16384 rows of 40 heads of 128 in bfloat16, 336 MB: 68 us, 4.9 TB/s; a copy's 5.2).
 #include "lba_attn_device.h"
 
 namespace lba {
@@ -126,7 +126,9 @@ static int rope(const void* X, lba_strides x_at, int32_t type, const void* posit
     p.X = X; p.Y = Y; p.positions = positions; p.freq = freq; p.x = x_at; p.y = y_at;
     p.T = (int32_t)T; p.H = (int32_t)H; p.D = (int32_t)D; p.pairs = (int32_t)pairs; p.wide = pos_bits == 64;
     p.gain = gain; p.sign = sign;
+    // (the angles of four rows at once, but where there are few rows one a workgroup: 9 rows of 40 heads 6.8 us by fours)
     p.rows = pairs > 256 ? 1 : pairs > 64 ? 2 : 4;
+    if (T < 256 * p.rows) p.rows = 1;
     const int64_t blocks = (T + p.rows - 1) / p.rows;
     const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
     if (type == LBA_F32) {
