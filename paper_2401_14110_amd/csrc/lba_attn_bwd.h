@@ -52,14 +52,18 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 3
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;
     Frag<T> q[KC], g[KC];
     float delta = 0.0f;
+    const float lse = p.lse[there ? row : (int64_t)rq.first * p.H];
     load_frags<T, DP>((const T*)p.G + row * p.D, there, p.D, half, g);
-    load_frags<T, DP>((const T*)p.O + row * p.D, there, p.D, half, q);
+    {
+        Frag<T> o[KC];
+        load_frags<T, DP>((const T*)p.O + row * p.D, there, p.D, half, o);
+        load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, there, p.D, half, q);
 #pragma unroll
-    for (int k = 0; k < KC; ++k) delta += dot(g[k], q[k]);
+        for (int k = 0; k < KC; ++k) delta += dot(g[k], o[k]);
+    }
     delta = sum_of_halves(delta);
     if (there && half == 0 && slice == 0) p.delta[row] = delta;
-    const float base = there ? -p.lse[row] * kLog2e : 0.0f;
-    load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, there, p.D, half, q);
+    const float base = there ? -lse * kLog2e : 0.0f;
     const float c = p.scale * kLog2e;
 
     f32x16 acc[DT];
