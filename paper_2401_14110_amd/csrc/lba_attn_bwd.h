@@ -61,6 +61,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 3
 #pragma unroll
         for (int k = 0; k < KC; ++k) delta += dot(g[k], o[k]);
     }
+    arrived(q);
     delta = sum_of_halves(delta);
     if (there && half == 0 && slice == 0) p.delta[row] = delta;
     const float base = there ? -lse * kLog2e : 0.0f;
@@ -251,6 +252,8 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     Frag<T> k[KC], v[KC];
     load_frags<T, DP>((const T*)p.K + (int64_t)(rk.first + j) * p.k.row + (int64_t)kv * p.k.head, there, p.D, half, k);
     load_frags<T, DP>((const T*)p.V + (int64_t)(rk.first + j) * p.v.row + (int64_t)kv * p.v.head, there, p.D, half, v);
+    arrived(k);
+    arrived(v);
     const float c = p.scale * kLog2e;
 
     f32x16 dk[DT], dv[DT];

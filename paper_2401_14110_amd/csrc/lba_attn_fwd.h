@@ -104,6 +104,7 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
     }
     Frag<T> q[KC];
     load_frags<T, DP>((const T*)p.Q + (int64_t)(rq.first + i) * p.q.row + (int64_t)h * p.q.head, i < rq.n, p.D, half, q);
+    arrived(q);
     float c = p.scale * 1.44269504f;                     // weights are 2^(c s); c > 0 after this
     if (!(c > 0.0f)) {
 #pragma unroll
