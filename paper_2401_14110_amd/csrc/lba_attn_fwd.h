@@ -5,7 +5,8 @@
 // P^T goes on to O^T = V^T . P^T without leaving its registers.  The maximum is moved (and the sums multiplied) only where a score is more than 8
 // above it in units of log 2: weights are then at most 256 times the final ones, which changes no rounding.
 //
-// Weights are rounded to bfloat16 for the second product (float32: split into pieces), which is what the matrix cores take; their sum is not.
+// Weights are rounded to bfloat16 for the second product, which is what the matrix cores take; their sum is not.  Float32, and outputs of float32: split
+// into pieces.
 // Bound by the matrix cores and what stands beside their 32 products of a wave's step (64 keys, heads of 128): a maximum, a multiply-add, an exponential,
 // an addition and half a conversion for each of a lane's 32 scores.  Two waves a SIMD take turns: 2 sequences of 4096 causal, 32 heads of 128, 285 us (960
 // TFLOP/s), where 8192^3 of a library product reach 1340.  Short sequences are bound by a workgroup's chain of reads: starts, first tiles, stores.
@@ -73,9 +74,11 @@ template <typename T> __device__ __forceinline__ void attn_row(const AttnParams&
     if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
 }
 
+// FINE: bfloat16 whose weights are three pieces too, for an output of float32.
 // Where rows do not go straight to LDS one loop has all tiles: the code of two, read once each by short sequences, costs more than its edge's tests.
-template <typename T, int DP, bool DIRECT>
+template <typename T, int DP, bool DIRECT, bool FINE>
 __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(AttnParams p) {
+    static_assert(!FINE || sizeof(T) == 2, "float32 has three pieces in any case");
     constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of keys and values
     if ((int)blockIdx.x >= p.units * p.slices) {
@@ -195,9 +198,20 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const Frag<T> w = as_frag<T>(s[b], k);
+                if constexpr (sizeof(T) == 2) {
+                    Frag<bf16_t> w[FINE ? 3 : 1];
+                    as_factors(s[b], k, w);
 #pragma unroll
-                for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
+                    for (int t = 0; t < DT; ++t) {
+                        const Frag<bf16_t> x = column_frag<bf16_t, DP>(tv, 32 * b + 16 * k, t, lane);
+#pragma unroll
+                        for (int n = FINE ? 2 : 0; n >= 0; --n) acc[t] = product(x, w[n], acc[t]);
+                    }
+                } else {
+                    const Frag<T> w = as_frag<T>(s[b], k);
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
+                }
             }
     };
     const int whole = min(tiles, least_all / KT);
@@ -242,11 +256,15 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
 }
 
 template <typename T> void launch_attn(const AttnParams& p, bool direct, hipStream_t st) {
+    constexpr bool BF = sizeof(T) == 2;
+    const bool fine = BF && p.o_type == LBA_F32;
     const dim3 grid((unsigned)(p.units * p.slices + (p.clear && p.starts ? kClearBlocks : 0)));
 #define LBA_ATTN(DP) \
     if (p.D <= DP) { \
-        if (sizeof(T) == 2 && direct) hipLaunchKernelGGL((attn_kernel<T, DP, sizeof(T) == 2>), grid, dim3(256), 0, st, p); \
-        else hipLaunchKernelGGL((attn_kernel<T, DP, false>), grid, dim3(256), 0, st, p); \
+        if (fine && direct) hipLaunchKernelGGL((attn_kernel<T, DP, BF, BF>), grid, dim3(256), 0, st, p); \
+        else if (fine) hipLaunchKernelGGL((attn_kernel<T, DP, false, BF>), grid, dim3(256), 0, st, p); \
+        else if (BF && direct) hipLaunchKernelGGL((attn_kernel<T, DP, BF, false>), grid, dim3(256), 0, st, p); \
+        else hipLaunchKernelGGL((attn_kernel<T, DP, false, false>), grid, dim3(256), 0, st, p); \
         return; \
     }
     LBA_ATTN(32)

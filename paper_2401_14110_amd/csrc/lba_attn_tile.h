@@ -110,6 +110,17 @@ template <typename T> __device__ __forceinline__ Frag<T> as_frag(const f32x16& s
     }
 }
 
+// The same as `N` bfloat16 factors: the numbers rounded, or (3) pieces that hold them.
+template <int N> __device__ __forceinline__ void as_factors(const f32x16& s, int k, Frag<bf16_t> (&f)[N]) {
+    if constexpr (N == 1) {
+        f[0] = as_frag<bf16_t>(s, k);
+    } else {
+        const Frag<float> x = as_frag<float>(s, k);
+#pragma unroll
+        for (int n = 0; n < N; ++n) f[n].w = x.w[n];
+    }
+}
+
 // row of the result's register r in this lane's half
 __device__ __forceinline__ constexpr int row_of(int r) { return (r % 4) + 8 * (r / 4); }
 

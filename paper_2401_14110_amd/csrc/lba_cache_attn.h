@@ -8,7 +8,7 @@
 // in registers, which holds a code times a power of two exactly.  S^T = K . Q^T on 16 x 16 x 32 leaves a row's scores in four lanes; their
 // weights are the other factor of O^T = V^T . P^T without moving, and V, whose rows have to become columns, goes through 32 rows of LDS that
 // are the wave's own: no barriers.  Bound by reading the codes: one sequence of 131071, 8 heads of 128 (143 MB), 31 us, 4.5 TB/s; 64 of 1000 to 8000 (233
-// MB) 58 us, 4.0 TB/s, where a library's sum over 1 GiB reads 3.9.  Weights are rounded to bfloat16 for the product with the values.  Float32: queries and weights are split into three bfloat16 pieces each, so that products are exact.
+// MB) 58 us, 4.0 TB/s, where a library's sum over 1 GiB reads 3.9.  Weights are rounded to bfloat16 for the product with the values.  Float32 (outputs: weights): queries and weights are split into three bfloat16 pieces each, so that products are exact.
 #ifndef LBA_CACHE_ATTN_H_
 #define LBA_CACHE_ATTN_H_
 
@@ -172,8 +172,9 @@ __device__ __forceinline__ void chunk_row(const CacheAttnParams& p, int b, int k
     if (lane == 0) { ends[r] = top; ends[stride + r] = sum; }
 }
 
-template <typename T, int D, int R>
-__global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2) void cache_attn_kernel(CacheAttnParams p) {
+// NW: pieces of the weights (float32 outputs: three).
+template <typename T, int D, int R, int NW>
+__global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) void cache_attn_kernel(CacheAttnParams p) {
     constexpr int KC = D / 32, DT = D / 16, NP = sizeof(T) == 2 ? 1 : 3;
     constexpr int ROWB = D * 2, WAVE = (32 * ROWB > 16 * R * D * 4 ? 32 * ROWB : 16 * R * D * 4);    // values of a step; at the end a wave's sums
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][WAVE];
@@ -325,21 +326,21 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) :
                 for (int d = 0; d < DT; ++d) acc[t][d] *= f;
             }
         }
-        i32x4_c w[R][NP];
+        i32x4_c w[R][NW];
 #pragma unroll
         for (int t = 0; t < R; ++t) {
             const float base = top[t] == -__builtin_inff() ? 0.0f : -top[t];
-            bf16_t piece[8][NP];
+            bf16_t piece[8][NW];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[t][u][r] = __builtin_amdgcn_exp2f(fmaf(s[t][u][r], c, base));
                     sum[t] += s[t][u][r];
-                    split<NP>(s[t][u][r], piece[4 * u + r]);
+                    split<NW>(s[t][u][r], piece[4 * u + r]);
                 }
 #pragma unroll
-            for (int n = 0; n < NP; ++n)
+            for (int n = 0; n < NW; ++n)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[t][n][j] = __builtin_bit_cast(int32_t, bf16x2_c{piece[2 * j][n], piece[2 * j + 1][n]});
         }
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) :
 #pragma unroll
             for (int t = 0; t < R; ++t)
 #pragma unroll
-                for (int n = 0; n < NP; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
+                for (int n = 0; n < NW; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
         }
     }
 
@@ -422,9 +423,14 @@ __global__ __launch_bounds__(256, R == 1 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) :
 }
 
 template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st) {
+    const bool fine = sizeof(T) == 4 || p.o_type == LBA_F32;
     const dim3 grid((unsigned)p.chunks * (unsigned)(p.c.count * p.c.KV * p.row_tiles));
 #define LBA_CACHE_ATTN(D_, R_) \
-    if (p.c.D == D_ && r == R_) { hipLaunchKernelGGL((cache_attn_kernel<T, D_, R_>), grid, dim3(256), 0, st, p); return; }
+    if (p.c.D == D_ && r == R_) { \
+        if (fine) hipLaunchKernelGGL((cache_attn_kernel<T, D_, R_, 3>), grid, dim3(256), 0, st, p); \
+        else hipLaunchKernelGGL((cache_attn_kernel<T, D_, R_, sizeof(T) == 2 ? 1 : 3>), grid, dim3(256), 0, st, p); \
+        return; \
+    }
     LBA_CACHE_ATTN(32, 1) LBA_CACHE_ATTN(64, 1) LBA_CACHE_ATTN(96, 1) LBA_CACHE_ATTN(128, 1)
     LBA_CACHE_ATTN(32, 2) LBA_CACHE_ATTN(64, 2) LBA_CACHE_ATTN(96, 2) LBA_CACHE_ATTN(128, 2)
 #undef LBA_CACHE_ATTN

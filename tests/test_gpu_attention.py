@@ -99,6 +99,19 @@ def test_output_types(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens,H,KV,D,causal", [([1], 1, 1, 1, True), ([33, 0, 130], 4, 2, 64, True), ([200, 65], 6, 2, 83, False), ([300], 2, 1, 128, True), ([2, 129], 3, 3, 96, True),
+                                               ([70], 2, 2, 116, True)])
+def test_float32_outputs_of_bfloat16_inputs(lens, H, KV, D, causal):
+    """Weights are not rounded then: the bounds are those of float32."""
+    g = torch.Generator(device="cuda").manual_seed(sum(lens))
+    q, k, v = (torch.randn(sum(lens), h, D, device="cuda", generator=g).bfloat16() for h in (H, KV, KV))
+    s = torch.tensor(np.cumsum([0] + lens), dtype=torch.int32).cuda()
+    want = ao.packed(*(t.double().cpu().numpy() for t in (q, k, v)), lens, lens, causal, float(np.float32(D ** -0.5)), "f32")
+    got = lb.attention(q, k, v, starts=s, causal=causal, out_dtype=torch.float32)
+    near(got, *want["o"], "o")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_views_batches_and_given_outputs(dtype):
     rng = np.random.default_rng(3)

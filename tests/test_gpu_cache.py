@@ -232,6 +232,23 @@ def test_attention_output_types(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("length,fresh,H,KV,D", [(70, 1, 4, 2, 64), (700, 2, 2, 1, 128), (9, 3, 20, 1, 32), (33, 1, 3, 3, 96), (2100, 1, 2, 2, 128)])
+def test_float32_outputs_of_bfloat16_queries(length, fresh, H, KV, D):
+    """Weights are not rounded then: the bounds are those of three pieces."""
+    g = torch.Generator(device="cuda").manual_seed(length)
+    cache, table, lens = lb.kv_cache(length // 16 + 1, 16, KV, D), torch.arange(length // 16 + 1, dtype=torch.int32, device="cuda")[None], torch.tensor([length], dtype=torch.int32).cuda()
+    x = torch.randn(2, 1, length, KV, D, device="cuda", generator=g)
+    lb.cache_write(x[0], x[1], cache, table, None, lens)
+    k, v = lb.cache_read(cache, table, None, lens, length, out_dtype=torch.float32)
+    q = torch.randn(1, fresh, H, D, device="cuda", generator=g).bfloat16()
+    got = lb.cache_attention(q, cache, table, lens, out_dtype=torch.float32)
+    for h in range(H):
+        kv = h // (H // KV)
+        f = ao.attend(*(t.double().cpu().numpy() for t in (q[0, :, h], k[:, kv], v[:, kv])), ao.seen(fresh, length, True), float(np.float32(D ** -0.5)), "f32", 3)
+        near(got[0, :, h], f["o"], f["to"] + 2 * lo.U * np.abs(f["o"]), h)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_what_is_not_seen_does_not_matter(dtype):
     """NaN in the lines behind a sequence's last token, in other pages, and in tokens that a query does not see yet."""
