@@ -7,9 +7,9 @@
 // the workspace, is then per register, and read from LDS.
 //
 // P and S are rounded to bfloat16 (float32: split into pieces) as factors of the sums' products; scores, weights and S themselves are float32.
-// Bound by the matrix cores and the weights beside them.  2 sequences of 4096 causal, 32 heads of 128 on 8: dQ, two waves a SIMD, 382 us (1080 TFLOP/s
-// of three products), dK and dV 713 (770 of four): its sums, factors and fragments are 448 registers, so that a wave is alone on its SIMD
-// and one block's products have to fill what the other's weights leave.  Two waves with half the keys each would read twice the queries.
+// Bound by the matrix cores and the weights beside them.  2 sequences of 4096 causal, 32 heads of 128 on 8: dQ, two waves a SIMD, 385 us (1070 TFLOP/s
+// of three products), dK and dV 670 (820 of four): its sums, factors and fragments are 448 registers, so that a wave is alone on its SIMD
+// and one block's products have to fill what the other's weights leave.
 #ifndef LBA_ATTN_BWD_H_
 #define LBA_ATTN_BWD_H_
 
@@ -135,14 +135,15 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 3
     }
     for (; kt < tiles; ++kt) step(kt, Known<1>{}, (kt - first) & 1);
     if (!there) return;
-    if (!part.alone) store_columns(p.part + ((int64_t)slice * p.T * p.H + row) * p.D, acc, p.scale, p.D, half);
-    else store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, p.scale, p.D, half);
+    const float scale = lim == 1 ? 0.0f : p.scale;       // the weight of an only key is 1 whatever its score is: no residue of G . V^T - rowsum(G * O)
+    if (!part.alone) store_columns(p.part + ((int64_t)slice * p.T * p.H + row) * p.D, acc, scale, p.D, half);
+    else store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, scale, p.D, half);
 }
 
 // One key by one wave, over the queries of its sequence from `lo` on that steps first .. last - 1 have (steps_head a head, `size` queries each from q0 on): a lane a
 // query, then a lane two columns.  words: 384 of LDS.  slice: -1 where these are all.
 template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& p, float* words, int kv, int t, Rows rq, int lo, int first, int last, int steps_head, int q0,
-                                                              int size, int slice) {
+                                                              int size, int slice, int lone, float scale) {
     const int lane = threadIdx.x & 63;
     const CodeFmt none = {};
     float *const v = words + 128, *const wp = words + 256, *const ws = words + 320;
@@ -163,7 +164,7 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
                 float s = 0.0f, u = 0.0f;
                 for (int d = 0; d < p.D; ++d) { s = fmaf(words[d], load_one(q + d), s); u = fmaf(v[d], load_one(g + d), u); }
                 e = __builtin_amdgcn_exp2f((s * p.scale - p.lse[row]) * kLog2e);
-                f = e * (u - p.delta[row]);
+                f = i0 + lane == lone ? 0.0f : e * (u - p.delta[row]);
             }
             wp[lane] = e;
             ws[lane] = f;
@@ -185,7 +186,7 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
 #pragma unroll
         for (int x = 0; x < 2; ++x)
             if (lane + 64 * x < p.D) {
-                p.part[to * p.D + lane + 64 * x] = dk[x] * p.scale;
+                p.part[to * p.D + lane + 64 * x] = dk[x] * scale;
                 p.part[(p.slices * rows + to) * p.D + lane + 64 * x] = dv[x];
             }
         return;
@@ -193,7 +194,7 @@ template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& 
 #pragma unroll
     for (int x = 0; x < 2; ++x)
         if (lane + 64 * x < p.D) {
-            store_one((T*)p.dK + (int64_t)t * p.dk.row + (int64_t)kv * p.dk.head + lane + 64 * x, dk[x] * p.scale, none);
+            store_one((T*)p.dK + (int64_t)t * p.dk.row + (int64_t)kv * p.dk.head + lane + 64 * x, dk[x] * scale, none);
             store_one((T*)p.dV + (int64_t)t * p.dv.row + (int64_t)kv * p.dv.head + lane + 64 * x, dv[x], none);
         }
 }
@@ -223,6 +224,9 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     const Slice part = slice_of(steps_head * p.group, p.slices, slice);
     const int steps = part.last;
     if (part.first >= steps && slice > 0) return;
+    // a query that sees one key alone has no gradient of its score: where there is one key, all have; else, causal, this one
+    const int lone = p.causal ? rq.n - rk.n : -1;
+    const float scale = rk.n == 1 ? 0.0f : p.scale;
     const int masked_all = first_of(at.t * kTileRows + kTileRows - 1);                           // from this query on, all of the workgroup's keys are seen
 
     Loader<T, DP, DIRECT> lq, lg;
@@ -305,6 +309,7 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
                 x = __builtin_amdgcn_exp2f(fmaf(x, c, base[r / 4][r % 4]));
                 y = x * (y - delta[r / 4][r % 4]);
                 if (EDGE && q0 + 32 * b + row_of(r) + 4 * half < lo) x = y = 0.0f;
+                if (EDGE && q0 + 32 * b + row_of(r) + 4 * half == lone) y = 0.0f;
             }
         };
         auto pack = [&](int b) {
@@ -382,17 +387,17 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
         for (int x = 0; x < 32 && j0 + x < rk.n; ++x)
-            dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x), part.first, steps, steps_head, t0 * QT, QT, part.alone ? -1 : slice);
+            dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x), part.first, steps, steps_head, t0 * QT, QT, part.alone ? -1 : slice, lone, scale);
         return;
     }
     if (!there) return;
     if (!part.alone) {
         const int64_t rows = (int64_t)p.Tk * p.KV, to = slice * rows + (int64_t)(rk.first + j) * p.KV + kv;
-        store_columns(p.part + to * p.D, dk, p.scale, p.D, half);
+        store_columns(p.part + to * p.D, dk, scale, p.D, half);
         store_columns(p.part + (p.slices * rows + to) * p.D, dv, 1.0f, p.D, half);
         return;
     }
-    store_columns((T*)p.dK + (int64_t)(rk.first + j) * p.dk.row + (int64_t)kv * p.dk.head, dk, p.scale, p.D, half);
+    store_columns((T*)p.dK + (int64_t)(rk.first + j) * p.dk.row + (int64_t)kv * p.dk.head, dk, scale, p.D, half);
     store_columns((T*)p.dV + (int64_t)(rk.first + j) * p.dv.row + (int64_t)kv * p.dv.head, dv, 1.0f, p.D, half);
 }
 

@@ -556,7 +556,9 @@ inline int64_t most_tiles(const int32_t* starts, int64_t T, int64_t count, int s
     return T / size + (count < T ? count : T);
 }
 
-// Workgroups go to the eight dies in turn; each die takes a run of neighbouring units, which share a head's keys in its cache.
+// Workgroups go to the eight dies in turn; each die takes a run of neighbouring units, which share a head's keys (or queries) in its cache: 2 sequences of
+// 4096, 32 heads of 128 on 8, forward 285 us, dQ 382, dK and dV 713, with units in turn 338, 457 and 1159.  (Cut into parts there are few workgroups,
+// which then are in turn, so that all dies have as many.)
 __device__ __forceinline__ int unit_of(int block, int units) {
     const int per = units / 8, more = units % 8, die = block % 8;
     return die * per + min(die, more) + block / 8;

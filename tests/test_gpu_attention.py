@@ -113,6 +113,31 @@ def test_float32_outputs_of_bfloat16_inputs(lens, H, KV, D, causal):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,lens_k,causal", [([1, 5, 1, 200], [1, 5, 1, 200], True), ([3, 140], [1, 1], False), ([4, 70], [1, 1], True), ([9, 130], [4, 129], True)])
+def test_a_query_that_sees_one_key_has_no_gradient_of_its_score(lens, lens_k, causal, dtype):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(sum(lens), 4, 64, device="cuda", generator=g).to(DT[dtype])
+    k, v = (torch.randn(sum(lens_k), 2, 64, device="cuda", generator=g).to(DT[dtype]) for _ in range(2))
+    s, sk = (torch.tensor(np.cumsum([0] + n), dtype=torch.int32).cuda() for n in (lens, lens_k))
+    o, lse = lb.attention(q, k, v, starts=s, starts_k=sk, causal=causal, want_stats=True)
+    G = torch.randn(q.shape, device="cuda", generator=g).to(DT[dtype])
+    dq, dk, dv = lb.attention_bwd(G, q, k, v, o, lse, starts=s, starts_k=sk, causal=causal)
+    a = b = 0
+    for n, m in zip(lens, lens_k):
+        seen = [min(m, max(0, i + m - n + 1)) if causal else m for i in range(n)]
+        rows = torch.tensor([a + i for i in range(n) if seen[i] == 1], dtype=torch.long, device="cuda")
+        assert len(rows) and not dq[rows].any()
+        assert m > 1 or (not dk[b:b + 1].any() and bool(dv[b:b + 1].any()))
+        a, b = a + n, b + m
+    # what the lone query leaves to its key's gradient: nothing, of whatever size its own gradient is
+    lone = torch.tensor(np.cumsum([0] + lens[:-1]) + np.maximum(0, np.array(lens) - np.array(lens_k)), device="cuda")
+    if causal:
+        G[lone] *= 1024.0
+        assert torch.equal(lb.attention_bwd(G, q, k, v, o, lse, starts=s, starts_k=sk)[1], dk)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_views_batches_and_given_outputs(dtype):
     rng = np.random.default_rng(3)
     B, L, H, KV, D = 3, 70, 4, 2, 48
