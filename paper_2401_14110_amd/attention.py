@@ -24,7 +24,7 @@ def frequencies(dim, base=10000.0, factor=1.0, kind="linear", original=4096, dev
     "ramp":   divided by factor where the original length is less than one turn, not at all where it is more than 32, in between in
               proportion, and cosine and sine times 0.1 ln(factor) + 1 (YaRN)."""
     i = torch.arange(0, dim, 2, dtype=torch.float64)
-    if kind == "base":
+    if kind == "base" and dim > 2:                       # (one frequency is the fastest)
         base = base * factor ** (dim / (dim - 2))
     f = base ** (-i / dim)
     gain = 1.0

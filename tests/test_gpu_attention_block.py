@@ -168,6 +168,7 @@ def test_frequencies():
     turns = 4096 * plain / (2 * np.pi)
     assert torch.equal(ramp[turns > 32], plain[turns > 32]) and torch.allclose(ramp[turns < 1], plain[turns < 1] / 4, rtol=1e-14)
     assert ((ramp <= plain) & (ramp >= plain / 4 * (1 - 1e-14))).all() and abs(gain - (0.1 * np.log(4) + 1)) < 1e-15
+    assert at.frequencies(2, factor=4.0, kind="base", device="cpu")[0].tolist() == [1.0] and len(at.frequencies(0, device="cpu")[0]) == 0
     with pytest.raises(ValueError):
         at.frequencies(64, kind="other", device="cpu")
 
