@@ -1084,7 +1084,8 @@ def rope_bwd(G, positions, freq, interleaved=False, gain=1.0, out=None, stream=N
 
 
 def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
-    """(lba_attn, what it points to) of a call."""
+    """(lba_attn, (q, k, v, starts, starts_k) as they are read) of a call, which keeps them all until the kernels are launched: copies among them are
+    nobody else's."""
     n, qs, ks = q.dim(), q.shape, k.shape
     if n not in (3, 4) or len(ks) != n or ks != v.shape or ks[-1] != qs[-1]:
         raise ValueError("q must be [rows, heads, D] or [batch, length, heads, D], k and v alike")
@@ -1140,7 +1141,8 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     if device < 0:
         raise TypeError("q must be a device tensor")
     handle, on = _on(stream, device)
-    a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    q3, k3, v3 = held[:3]
     o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
     size = _attn_bytes("lba_attention_workspace_bytes", a)
@@ -1159,7 +1161,8 @@ def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, s
     _like(o, q.shape, device, "o", (q.dtype,))
     _like(lse, q.shape[:-1], device, "lse", (torch.float32,))
     handle, on = _on(stream, device)
-    a, (q3, k3, v3, _, _) = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    q3, k3, v3 = held[:3]
     G, o, lse = _whole(G, on), _whole(o, on), _whole(lse, on)
     if out is None:
         got = (_made(q, q.dtype, on), _made(k, k.dtype, on), _made(v, v.dtype, on))
@@ -1191,7 +1194,7 @@ def kv_cache(pages, page, heads, D, device="cuda"):
 
 
 def _cache4(cache, table, lens, device, on):
-    """(lba_cache4, what it points to)."""
+    """(lba_cache4, what it points to, to be kept as with _attn)."""
     k, k_scale, v, v_scale = cache
     shape, powers = k.shape, k_scale.shape
     if len(shape) != 4 or shape[3] % 16 or not 16 <= shape[3] <= 64 or powers != shape[:3] + (shape[3] // 16,):
