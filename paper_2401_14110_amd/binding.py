@@ -1134,7 +1134,7 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     """softmax(scale * q . k^T) . v of packed sequences: query head h reads head h * KV // H of k and v, and, causal, query i of n sees key j of m
     iff j <= i + m - n.  starts_k: the keys' sequences where they are not the queries'.  scale: D^-1/2 by default.  Returns o of q's
     shape and out_dtype (q's by default; torch.uint8 codes need out_fmt), and with want_stats (o, lse), float32 of q.shape[:-1], which
-    attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were."""
+    attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were, and in lse -infinity."""
     device = q.get_device()
     dtype = out_dtype or q.dtype
     o_type, fmt = _out_type(dtype, out_fmt)
@@ -1145,6 +1145,8 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     q3, k3, v3 = held[:3]
     o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
+    if want_stats and out is not None and starts is not None:        # the library leaves rows of no sequence as they are in both or in neither
+        lse.fill_(-math.inf) if on is None else _of_pool(lambda: lse.fill_(-math.inf), on)
     size = _attn_bytes("lba_attention_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
     _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), _at(ws), size, handle))
