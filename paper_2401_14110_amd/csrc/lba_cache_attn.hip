@@ -33,14 +33,13 @@ __global__ __launch_bounds__(256) void cache_join_few_kernel(CacheAttnParams p, 
     const float* part = p.part + out * p.chunks * p.c.D + piece * 4;
     float m = -__builtin_inff(), l = 0.0f;
     for (int i = 0; i < n; ++i) m = fmaxf(m, end[2 * i]);
+    const float base = m == -__builtin_inff() ? 0.0f : m;            // (all scores -infinity: weights of 0; all NaN, which no maximum is: sums of NaN)
     f32x4_c v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (m != -__builtin_inff()) {
 #pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const float w = __builtin_amdgcn_exp2f(end[2 * i] - m);
-            l = fmaf(w, end[2 * i + 1], l);
-            v += w * *(const f32x4_c*)&part[(int64_t)i * p.c.D];
-        }
+    for (int i = 0; i < n; ++i) {
+        const float w = __builtin_amdgcn_exp2f(end[2 * i] - base);
+        l = fmaf(w, end[2 * i + 1], l);
+        v += w * *(const f32x4_c*)&part[(int64_t)i * p.c.D];
     }
     store_joined(p, out * p.c.D + piece * 4, v, l);
 }
