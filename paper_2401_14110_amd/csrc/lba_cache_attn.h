@@ -53,11 +53,13 @@ __device__ __forceinline__ float sum_of_quarters(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// a number in N bfloat16 pieces
-template <int N> __device__ __forceinline__ void split(float x, bf16_t (&piece)[N]) {
+// A number in N bfloat16 pieces.  Not FINITE: pieces before the last stay within bfloat16, so that an infinity or a NaN is in the last, and numbers that
+// would round up to infinity do not get one.
+template <bool FINITE, int N> __device__ __forceinline__ void split(float x, bf16_t (&piece)[N]) {
+    constexpr float TOP = 3.38953139e38f;                // bfloat16's largest number
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        piece[i] = (bf16_t)x;
+        piece[i] = (bf16_t)(FINITE || i == N - 1 ? x : __builtin_amdgcn_fmed3f(x, -TOP, TOP));
         x -= (float)piece[i];
     }
 }
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
             if (r < rows) load_vec<8>(x + 8 * k, v);
             bf16_t piece[8][NP];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) split<NP>(flip == 0.0f ? 0.0f : v[j] * flip, piece[j]);
+            for (int j = 0; j < 8; ++j) split<false>(flip == 0.0f ? 0.0f : v[j] * flip, piece[j]);
 #pragma unroll
             for (int n = 0; n < NP; ++n)
 #pragma unroll
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
                 for (int r = 0; r < 4; ++r) {
                     s[t][u][r] = __builtin_amdgcn_exp2f(fmaf(s[t][u][r], c, base));
                     sum[t] += s[t][u][r];
-                    split<NW>(s[t][u][r], piece[4 * u + r]);
+                    split<true>(s[t][u][r], piece[4 * u + r]);
                 }
 #pragma unroll
             for (int n = 0; n < NW; ++n)
