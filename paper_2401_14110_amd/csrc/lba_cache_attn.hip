@@ -3,8 +3,6 @@
 
 namespace lba {
 
-template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st);
-
 // where row `out` of O has its chunks, and how many there are
 __device__ __forceinline__ int chunks_of_row(const CacheAttnParams& p, int64_t out, int rows_of_tile) {
     const int64_t token = out / p.H;
