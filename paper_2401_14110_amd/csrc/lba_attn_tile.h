@@ -175,7 +175,8 @@ template <typename T, int DP> __device__ __forceinline__ Frag<T> column_frag(con
 }
 // 16 bytes a lane from memory to LDS, the wave's 64 pieces from the place `to` on.  Not the builtin: behind it the compiler waits for all that is under
 // way before it reads LDS through a pointer that it cannot tell from the one written, the other buffer too (13 prompts forward 133 us with it,
-// 128 so).  No register is written, nothing else here uses m0, and who reads the tile waits for vmcnt(0) and a barrier.
+// 128 so).  No register is written but m0, which the compiler reserves (it takes no mention of it among what is changed): it sets m0 right before an
+// instruction of its own that reads it, and these kernels have none.  Who reads the tile waits for vmcnt(0) and a barrier.
 __device__ __forceinline__ void piece_to_lds(uint32_t to, const void* base, uint32_t offset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
