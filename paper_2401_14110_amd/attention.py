@@ -84,14 +84,16 @@ class SelfAttention:
         n, mean, rstd, qkv = self.project(x, positions, train)
         q, k, v = self.split(qkv)
         if cache is not None:
-            lba.cache_write(k, v, cache[0], cache[1], torch.tensor([0, len(x)], dtype=torch.int32, device=x.device) if starts is None else starts, cache[2])
-        if not train:
-            u = lba.attention(q, k, v, starts=starts, causal=self.causal, out_dtype=torch.uint8, out_fmt=fmt)
-            return self.finish(u.flatten(-2), x)
-        o, lse = lba.attention(q, k, v, starts=starts, causal=self.causal, want_stats=True)
-        u = lba.dropout(o.flatten(-2), None, out_dtype=torch.uint8, out_fmt=fmt)
-        drop = (self.p, seed, 0) if self.p > 0 else None
-        return self.finish(u, x, drop), (x, positions, starts, n, mean, rstd, qkv, o, lse, u, drop)
+            one = starts is None                         # a batch of one, which is not a row of each sequence
+            lba.cache_write(k[None] if one else k, v[None] if one else v, *cache[:2], starts, cache[2])
+        if train:
+            o, lse = lba.attention(q, k, v, starts=starts, causal=self.causal, want_stats=True)
+            u = lba.dropout(o.flatten(-2), None, out_dtype=torch.uint8, out_fmt=fmt)
+        else:
+            u = lba.attention(q, k, v, starts=starts, causal=self.causal, out_dtype=torch.uint8, out_fmt=fmt).flatten(-2)
+        drop = (self.p, seed, 0) if train and self.p > 0 else None
+        y = self.finish(u, x, drop)
+        return (y, (x, positions, starts, n, mean, rstd, qkv, o, lse, u, drop)) if train else y
 
     def backward(self, G, kept):
         """(dx, the gradients of `params`) for dL/dy = G and what `forward` kept."""

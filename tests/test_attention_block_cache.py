@@ -1,0 +1,64 @@
+"""Prompts of the attention block into a cache: nothing waits for the host, and a step can be captured."""
+import pytest
+import torch
+
+from paper_2401_14110_amd import attention as at
+from paper_2401_14110_amd import binding as lb
+
+
+def ints(*v, device="cuda"):
+    return torch.tensor(v, dtype=torch.int32, device=device)
+
+
+def test_one_sequence_takes_no_list_from_the_host(monkeypatch):
+    written = []
+    block = object.__new__(at.SelfAttention)
+    block.heads, block.kv_heads, block.dim, block.causal, block.t_u = 2, 1, 32, True, 6
+    block.project = lambda x, positions, train: (None, None, None, torch.zeros(len(x), 4, 32))
+    block.finish = lambda u, x, drop=None: x.clone()
+    monkeypatch.setattr(lb, "cache_write", lambda *a: written.append(a))
+    monkeypatch.setattr(lb, "attention", lambda q, k, v, **kw: q)
+    x, lens = torch.zeros(5, 8), ints(5, device="cpu")
+
+    def no_list(*a, **k):
+        raise AssertionError("a tensor from host data")
+
+    with monkeypatch.context() as m:
+        for name in ("tensor", "as_tensor", "from_numpy"):
+            m.setattr(torch, name, no_list)
+        y = block.forward(x, torch.arange(5), cache=("held", "table", lens))
+    (k, v, held, table, starts, got), = written
+    # (as a batch of one: [rows, heads, D] could be a row of each sequence)
+    assert k.shape == v.shape == (1, 5, 1, 32) and (held, table, starts, got) == ("held", "table", None, lens)
+    assert torch.equal(y, x)
+
+
+@pytest.fixture
+def server():
+    torch.manual_seed(3)
+    block = at.SelfAttention(64, 4, 2, 32, seed=2)
+    table = ints(8, 1, 6, 3, 0, 7, 2, 5).view(2, 4)
+    return block, lambda: lb.kv_cache(9, 8, 2, 32), table
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("packed", [False, True])
+def test_prompts_in_a_graph(server, packed):
+    block, cache, table = server
+    x, positions = torch.randn(20, 64, device="cuda"), torch.arange(20, device="cuda")
+    s, table, lens = (ints(0, 9, 20), table, ints(9, 11)) if packed else (None, table[:1], ints(20))
+    held, eager = cache(), cache()
+    block.forward(x, positions, s, cache=(eager, table, lens))   # (what a first call sets up is not captured)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = block.forward(x, positions, s, cache=(held, table, lens))
+    for a, b in zip(held, eager):
+        a.copy_(b)
+    for _ in range(4):
+        x.copy_(torch.randn_like(x))
+        g.replay()
+        torch.cuda.synchronize()
+        want = block.forward(x, positions, s, cache=(eager, table, lens))
+        assert torch.equal(y, want) and torch.equal(y, block.forward(x, positions, s)) and all(torch.equal(a, b) for a, b in zip(held, eager))
+    with pytest.raises(ValueError):                      # a row of each of two sequences is not one sequence of two rows
+        block.forward(x[:2], positions[:2], cache=(held, ints(0, 1).view(2, 1), ints(1, 1)))
