@@ -39,6 +39,17 @@ def frequencies(dim, base=10000.0, factor=1.0, kind="linear", original=4096, dev
     return f.to(device), gain
 
 
+def _unless_older(y, starts, lens):
+    """y, in place, with NaN in the rows of sequences that have more tokens than rows here (no host waits for lens, and a captured call looks at each replay)."""
+    if starts is None:
+        older = lens > len(y)
+    else:
+        starts = starts.contiguous()
+        row = torch.arange(len(y), dtype=starts.dtype, device=y.device)
+        older = torch.nn.functional.pad(lens > starts.diff(), (1, 1))[torch.searchsorted(starts, row, right=True)]      # (no sequence: not so)
+    y.masked_fill_(older[:, None], math.nan)
+
+
 class SelfAttention:
     """Parameters are float32 tensors (`params`), `refresh` makes the weights' codes from them.  `inner`: the type of queries, keys and values."""
 
@@ -79,7 +90,8 @@ class SelfAttention:
 
     def forward(self, x, positions, starts=None, seed=0, train=False, cache=None):
         """y of x [rows, width], and with train what `backward` reads.  positions [rows]; starts: as lba.attention takes it.  cache: (KVCache, table,
-        lens), which get the rows' keys and values."""
+        lens), which get the rows' keys and values.  Queries see the call's rows alone, so rows must be the whole of their sequence: where lens counts older
+        tokens besides, which only `tokens` looks at, y is NaN."""
         fmt = scaled_format(self.t_u)
         n, mean, rstd, qkv = self.project(x, positions, train)
         q, k, v = self.split(qkv)
@@ -93,6 +105,8 @@ class SelfAttention:
             u = lba.attention(q, k, v, starts=starts, causal=self.causal, out_dtype=torch.uint8, out_fmt=fmt).flatten(-2)
         drop = (self.p, seed, 0) if train and self.p > 0 else None
         y = self.finish(u, x, drop)
+        if cache is not None:
+            _unless_older(y, starts, cache[2])
         return (y, (x, positions, starts, n, mean, rstd, qkv, o, lse, u, drop)) if train else y
 
     def backward(self, G, kept):
