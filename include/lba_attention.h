@@ -71,7 +71,9 @@ size_t lba_attention_workspace_bytes(lba_attn a);
 /* Its gradients.  With P the weights, made again from lse, and G = dL/dO,
  *   dV = P^T . G,   S = P * (G . V^T - rowsum(G * O)),   dQ = scale * S . K,   dK = scale * S^T . Q,
  * summed over the query heads of a key head.  Gradients that a seen infinity or NaN reaches are unspecified.  G and O
- * [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D], dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the products; sums are float32.
+ * [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D], dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the
+ * products; sums are float32.  rowsum(G * O) is the sum of P * (G . V^T) where a query's tile of 128 sees up to 512 keys; behind that, and with LBA_F32, it
+ * is taken from O as it is stored.
  * workspace: lba_attention_bwd_workspace_bytes(a) bytes. */
 int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, const void* V, const void* O, const float* lse, void* dQ,
                       lba_strides dq_at, void* dK, lba_strides dk_at, void* dV, lba_strides dv_at, void* workspace, size_t workspace_bytes,
