@@ -19,6 +19,7 @@ STE_IDENTITY, STE_IMMEDIATE_OF, STE_RECURSIVE_OF, STE_COEF_PLANE = 0, 1, 2, 3
 ORDER_SEQ, ORDER_CHUNK16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 F32, BF16, CODE8 = 0, 1, 2
+FINE = 0x100                                             # added to an output's type by the attention calls
 OK, ERR_NULL, ERR_SHAPE, ERR_FORMAT, ERR_UNSUPPORTED, ERR_ALIGN, ERR_LAUNCH = range(7)
 
 
@@ -1130,11 +1131,12 @@ def _attn_bytes(name, a):
     return _attn_bytes_of(name, a.T, a.Tk, a.count, bool(a.starts), bool(a.starts_k), a.H, a.KV, a.D, a.type)
 
 
-def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None):
+def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_dtype=None, out_fmt=None, want_stats=False, out=None, stream=None, fine=False):
     """softmax(scale * q . k^T) . v of packed sequences: query head h reads head h * KV // H of k and v, and, causal, query i of n sees key j of m
     iff j <= i + m - n.  starts_k: the keys' sequences where they are not the queries'.  scale: D^-1/2 by default.  Returns o of q's
     shape and out_dtype (q's by default; torch.uint8 codes need out_fmt), and with want_stats (o, lse), float32 of q.shape[:-1], which
-    attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were, and in lse -infinity."""
+    attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were, and in lse -infinity.  Weights of bfloat16 inputs are rounded to bfloat16 for
+    the product with v, but for outputs of float32, and with `fine` not for any: it takes up to 1.7 times as long."""
     device = q.get_device()
     dtype = out_dtype or q.dtype
     o_type, fmt = _out_type(dtype, out_fmt)
@@ -1149,7 +1151,7 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
         lse.fill_(-math.inf) if on is None else _of_pool(lambda: lse.fill_(-math.inf), on)
     size = _attn_bytes("lba_attention_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), _at(ws), size, handle))
+    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type | FINE if fine else o_type, fmt, _at(lse), _at(ws), size, handle))
     return (o, lse) if want_stats else o
 
 
@@ -1274,10 +1276,10 @@ def cache_read(cache, table, starts, lens, rows, out_dtype=torch.bfloat16, out=N
     return got
 
 
-def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=None, out=None, stream=None):
+def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=None, out=None, stream=None, fine=False):
     """Attention of new tokens over a cache: q [sequences, heads, D] for one token each, or [sequences, tokens, heads, D], which have been written
     (lens counts them): each sees the positions up to its own.  Returns o of q's shape and out_dtype (q's by default; torch.uint8 codes need
-    out_fmt); a query that sees nothing has zeros."""
+    out_fmt); a query that sees nothing has zeros.  fine: as in attention."""
     device = q.get_device()
     dtype = out_dtype or q.dtype
     o_type, fmt = _out_type(dtype, out_fmt)
@@ -1295,6 +1297,6 @@ def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=N
     o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     size = _layer_bytes("lba_cache_attention_workspace_bytes", c.count, c.table_row, c.page, fresh, H, c.KV, c.D)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_cache_attention(c, _at(q3), lba_strides(*q_at), _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o), o_type, fmt, _at(ws), size,
-                                     handle))
+    _check(lib().lba_cache_attention(c, _at(q3), lba_strides(*q_at), _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o),
+                                     o_type | FINE if fine else o_type, fmt, _at(ws), size, handle))
     return o

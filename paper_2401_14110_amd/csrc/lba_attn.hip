@@ -115,13 +115,15 @@ int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void*
                   size_t workspace_bytes, void* hip_stream) {
     AttnParams p = {};
     int rc = attn_params(a, &p);
+    const bool fine = (o_type & LBA_FINE) != 0;
+    o_type &= ~LBA_FINE;
     if (rc == LBA_OK) rc = check_out_type(o_type, o_fmt);
     if (rc != LBA_OK) return rc;
     if (p.T == 0 || p.H == 0) return LBA_OK;
     if (!Q || !O || (p.Tk > 0 && (!K || !V))) return LBA_ERR_NULL;
     p.Q = Q; p.K = K; p.V = V; p.O = O; p.lse = lse;
     if (o_type == LBA_CODE8) p.fmt = make_code_fmt(o_fmt);
-    p.o_type = o_type;
+    p.o_type = o_type; p.fine = fine || o_type == LBA_F32;
     AttnPlan plan;
     rc = attn_plan(a, &plan);
     if (rc != LBA_OK) return rc;

@@ -17,6 +17,7 @@ struct CacheAttnParams {
     lba_strides q;
     int32_t room;            // positions of a sequence's table
     int32_t fresh, H, group, o_type;
+    int32_t fine;            // weights of bfloat16 queries are three pieces
     int32_t chunk, chunks, row_tiles;
     float scale;
 };

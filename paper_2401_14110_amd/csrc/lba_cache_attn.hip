@@ -134,6 +134,8 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     if (rc == LBA_OK && (fresh < 0 || fresh > 2147483647LL || H < 0 || H > 65535 || (H > 0 && (c.KV < 1 || H % c.KV != 0)))) rc = LBA_ERR_SHAPE;
     if (rc == LBA_OK && (c.count * H > 0 && fresh > 2147483647LL / (c.count * H))) rc = LBA_ERR_SHAPE;
     if (rc == LBA_OK) rc = check_float_type(type);
+    const bool fine = (o_type & LBA_FINE) != 0;
+    o_type &= ~LBA_FINE;
     if (rc == LBA_OK) rc = check_out_type(o_type, o_fmt);
     if (rc != LBA_OK) return rc;
     if (c.count == 0 || fresh == 0 || H == 0) return LBA_OK;
@@ -149,7 +151,7 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     }
     p.Q = Q; p.O = O; p.q = q_at; p.fresh = (int32_t)fresh; p.H = (int32_t)H; p.group = (int32_t)(H / c.KV); p.scale = scale;
     if (o_type == LBA_CODE8) p.fmt = make_code_fmt(o_fmt);
-    p.o_type = o_type; p.part = (float*)workspace; p.room = (int32_t)(c.table_row * c.page);
+    p.o_type = o_type; p.fine = fine || o_type == LBA_F32; p.part = (float*)workspace; p.room = (int32_t)(c.table_row * c.page);
     if (!lines) p.room = 0;                              // nothing is held anywhere
     p.chunk = (int32_t)plan.chunk; p.chunks = (int32_t)plan.chunks; p.row_tiles = plan.row_tiles;
     const hipStream_t st = (hipStream_t)hip_stream;

@@ -155,7 +155,7 @@ __device__ __forceinline__ void chunk_row(const CacheAttnParams& p, int b, int k
     if (lane == 0) { ends[r] = top; ends[stride + r] = sum; }
 }
 
-// NW: pieces of the weights (float32 outputs: three).
+// NW: pieces of the weights.
 template <typename T, int D, int R, int NW>
 __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) void cache_attn_kernel(CacheAttnParams p) {
     constexpr int KC = D / 32, DT = D / 16, NP = sizeof(T) == 2 ? 1 : 3;
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
 }
 
 template <typename T> void launch_cache_attn(const CacheAttnParams& p, int r, hipStream_t st) {
-    const bool fine = sizeof(T) == 4 || p.o_type == LBA_F32;
+    const bool fine = sizeof(T) == 4 || p.fine;
     const dim3 grid((unsigned)p.chunks * (unsigned)(p.c.count * p.c.KV * p.row_tiles));
 #define LBA_CACHE_ATTN(D_, R_) \
     if (p.c.D == D_ && r == R_) { \
