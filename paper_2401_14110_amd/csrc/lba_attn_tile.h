@@ -445,8 +445,32 @@ struct TileOf {
     Rows mine, other;        // the sequence's rows in the list that has the tiles, and in the other one
 };
 
-// Tile `index` of the tiles of `size` rows that the sequences have one after another in `starts` (T rows); the whole wave calls.  Both lists are read
-// at once, 64 sequences at a time: a workgroup waits for memory once before it knows its rows.
+// The last sequence of 0 .. count - 1 whose `key`, which never falls from one to the next, is not behind `at`, with its rows in both lists (b = -1: there is none);
+// the whole wave calls.  64 keys at a time, then 64 sequences' rows at once: three reads one after another for 2^18 sequences.
+template <typename K> __device__ __forceinline__ TileOf find_last(const int32_t* starts, int T, const int32_t* others, int T_other, int count, int at, K key) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = count;                              // it is one of lo .. hi - 1, if any
+    while (hi - lo > 64) {
+        const int step = (hi - lo + 63) / 64, b = lo + lane * step;
+        const uint64_t before = __ballot(b < hi && key(min(b, hi - 1)) <= at);
+        if (before) lo += (63 - __builtin_clzll(before)) * step;
+        hi = min(hi, lo + step);
+    }
+    const int b = min(lo + lane, hi - 1);
+    const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
+    const uint64_t before = __ballot(lo + lane < hi && key(b) <= at);
+    if (!before) return {-1, 0, {0, 0}, {0, 0}};
+    const int f = 63 - __builtin_clzll(before);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+    return {of(b), 0, {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
+}
+
+constexpr int kPacked = 64;                              // sequences of a list up to which tiles have no gaps
+
+// Tile `index` of the tiles of `size` rows that the sequences have in `starts` (T rows); the whole wave calls.  Up to kPacked sequences have theirs one
+// after another, found by one look at both lists, a sequence a lane: a workgroup waits for memory once before it knows its rows.  Of more, sequence b has its from
+// starts[b] / size + b on, where they fit whatever the others are, so that they can be searched for; the places between are nobody's.  (One after another, every
+// workgroup walked over the list: 5000 sequences of one token, 4 heads, forward 780 us, 2^17 with one head 145 ms; so 141 us and 0.9 ms.)
 __device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, const int32_t* others, int T_other, int count, int size, int index) {
     if (!starts) {
         const int n = T / count, m = T_other / count, per = (n + size - 1) / size;
@@ -454,50 +478,41 @@ __device__ __forceinline__ TileOf find_tile(const int32_t* starts, int T, const 
         const int b = index / per;
         return {b, index % per, {b * n, n}, {b * m, m}};
     }
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < count; b0 += 64) {
-        const int b = min(b0 + lane, count - 1);
-        const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
-        const int n = b0 + lane < count ? (mine.n + size - 1) / size : 0;
-        int upto = n;
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) {
-            const int v = __shfl_up(upto, x);
-            if (lane >= x) upto += v;
-        }
-        const uint64_t behind = __ballot(upto > index);
-        if (behind) {
-            const int f = __builtin_ctzll(behind);
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-            return {b0 + f, index - (of(upto) - of(n)), {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
-        }
-        index -= __builtin_amdgcn_readlane(upto, 63);
+    if (count > kPacked) {
+        auto place = [&](int b) { return min(max(starts[b], 0), T) / size + b; };
+        TileOf at = find_last(starts, T, others, T_other, count, index, place);
+        if (at.b < 0) return at;
+        at.t = index - (at.mine.first / size + at.b);
+        if (at.t >= (at.mine.n + size - 1) / size) at.b = -1;
+        return at;
     }
-    return {-1, 0, {0, 0}, {0, 0}};
+    const int lane = threadIdx.x & 63, b = min(lane, count - 1);
+    const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
+    const int n = lane < count ? (mine.n + size - 1) / size : 0;
+    int upto = n;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+        const int v = __shfl_up(upto, x);
+        if (lane >= x) upto += v;
+    }
+    const uint64_t behind = __ballot(upto > index);
+    if (!behind) return {-1, 0, {0, 0}, {0, 0}};
+    const int f = __builtin_ctzll(behind);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
+    return {f, index - (of(upto) - of(n)), {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
 }
 
-// The sequence that row `t` of T belongs to in `starts`, with t as the tile; the whole wave calls.  64 starts at a time, then both lists at once.
+// The sequence that row `t` of T belongs to in `starts`, with t as the tile; the whole wave calls.
 __device__ __forceinline__ TileOf find_row(const int32_t* starts, int T, const int32_t* others, int T_other, int count, int t) {
     if (count < 1) return {-1, 0, {0, 0}, {0, 0}};
     if (!starts) {
         const int n = T / count, m = T_other / count, b = t / n;
         return {b, t, {b * n, n}, {b * m, m}};
     }
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = count;                              // it is one of lo .. hi - 1, if any
-    while (hi - lo > 64) {
-        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const uint64_t before = __ballot(at < hi && starts[min(at, hi - 1)] <= t);
-        if (before) lo += (63 - __builtin_clzll(before)) * step;
-        hi = min(hi, lo + step);
-    }
-    const int b = min(lo + lane, hi - 1);
-    const Rows mine = rows_of(starts, T, count, b), other = rows_of(others, T_other, count, b);
-    const uint64_t has = __ballot(t >= mine.first && t < mine.first + mine.n);
-    if (!has) return {-1, 0, {0, 0}, {0, 0}};
-    const int f = __builtin_ctzll(has);
-    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, f); };
-    return {of(b), t, {of(mine.first), of(mine.n)}, {of(other.first), of(other.n)}};
+    TileOf at = find_last(starts, T, others, T_other, count, t, [&](int b) { return starts[b]; });
+    if (at.b >= 0 && (t < at.mine.first || t >= at.mine.first + at.mine.n)) at.b = -1;
+    at.t = t;
+    return at;
 }
 
 // Elements `lane` and lane + 64 of `heads` (1 or 2) neighbouring heads of a row, of n parts `stride` apart times their weights: v = the sums.  All loads of
@@ -554,7 +569,7 @@ __device__ __forceinline__ int steps_of_keys(const AttnParams& p, const Rows& rq
 inline int64_t most_tiles(const int32_t* starts, int64_t T, int64_t count, int size) {
     if (count < 1 || T < 1) return 0;
     if (!starts) return count * ((T / count + size - 1) / size);
-    return T / size + (count < T ? count : T);
+    return T / size + (count < T || count > kPacked ? count : T);
 }
 
 // Workgroups go to the eight dies in turn; each die takes a run of neighbouring units, which share a head's keys (or queries) in its cache: 2 sequences of
