@@ -21,7 +21,7 @@
 extern "C" {
 #endif
 
-/* May be added to an o_type of lba_attention and lba_cache_attention: see there. */
+/* May be added to the type of the inputs of lba_attention, lba_attention_bwd and lba_cache_attention, where it is said what it asks for. */
 #define LBA_FINE 0x100
 
 typedef struct {
@@ -63,8 +63,8 @@ typedef struct {
 
 /* O = softmax over the seen keys of (scale * q . k) times V; a query that sees nothing, or whose scores are all -infinity, has
  * zeros.  Scores, the softmax's maximum and sum and O's sums are float32; with LBA_BF16 and an output of
- * another type than LBA_F32 the weights are rounded to bfloat16 for the product with V, unless LBA_FINE is added to o_type: they are three bfloat16
- * pieces then, which hold them, as with LBA_F32.
+ * another type than LBA_F32 the weights are rounded to bfloat16 for the product with V, unless LBA_FINE is added to a.type: they are three
+ * bfloat16 pieces then, which hold them, as with LBA_F32.
  * O [T, H, D] contiguous of o_type (o_fmt is read for LBA_CODE8 only); lse [T, H] float32 (NULL: not stored): ln of the sum over the seen
  * keys of exp(scale * q . k), -infinity where there are none.
  * workspace: lba_attention_workspace_bytes(a) bytes, which reads no pointer of `a` but whether it is NULL; 0 where there are many rows. */
@@ -76,8 +76,8 @@ size_t lba_attention_workspace_bytes(lba_attn a);
  *   dV = P^T . G,   S = P * (G . V^T - rowsum(G * O)),   dQ = scale * S . K,   dK = scale * S^T . Q,
  * summed over the query heads of a key head.  Gradients that a seen infinity or NaN reaches are unspecified.  G and O
  * [T, H, D] contiguous, all of a.type, O and lse as the forward call stored them; dQ [T, H, D], dK and dV [Tk, KV, D] of a.type.  With LBA_BF16 P and S are rounded to bfloat16 for the
- * products; sums are float32.  rowsum(G * O) is the sum of P * (G . V^T) where a query's tile of 128 sees up to 512 keys; behind that, and with LBA_F32, it
- * is taken from O as it is stored.
+ * products; sums are float32.  rowsum(G * O) is the sum of P * (G . V^T) where a query's tile of 128 sees up to 512 keys, and, with LBA_FINE added
+ * to a.type, of all queries; else it is taken from O as it is stored, whose rounding tells where values have a mean.
  * workspace: lba_attention_bwd_workspace_bytes(a) bytes. */
 int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, const void* V, const void* O, const float* lse, void* dQ,
                       lba_strides dq_at, void* dK, lba_strides dk_at, void* dV, lba_strides dv_at, void* workspace, size_t workspace_bytes,
@@ -116,7 +116,7 @@ int lba_cache_read(lba_cache4 c, const int32_t* starts, int64_t T, void* K, lba_
 /* Attention of each sequence's `fresh` newest tokens over its cache: query i of a sequence (Q [count, fresh, H, D], a token's strides q_at, of `type`)
  * sees positions 0 .. lens[b] - fresh + i, as far as they hold something.  O [count, fresh, H, D] contiguous of o_type; a query that sees nothing has zeros.
  * Scores, maxima and sums are float32; with LBA_BF16 and an output of another type than LBA_F32 the weights are rounded to bfloat16 for the
- * product with the values, else, and with LBA_FINE added to o_type, they are split into three bfloat16 pieces, which hold them, as queries of LBA_F32 are.
+ * product with the values, else, and with LBA_FINE added to type, they are split into three bfloat16 pieces, which hold them, as queries of LBA_F32 are.
  * Limits (else LBA_ERR_SHAPE): H a multiple of KV, H <= 65535, count * fresh * H < 2^24, table_row * page <= 2^30, and with tiles of 16 rows (the fresh
  * queries of the H / KV heads that share one; 32 where there are more) tiles * KV * count < 2^23.
  * workspace: lba_cache_attention_workspace_bytes(...) bytes, for the longest sequence that the table has room for. */

@@ -19,7 +19,7 @@ STE_IDENTITY, STE_IMMEDIATE_OF, STE_RECURSIVE_OF, STE_COEF_PLANE = 0, 1, 2, 3
 ORDER_SEQ, ORDER_CHUNK16 = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 F32, BF16, CODE8 = 0, 1, 2
-FINE = 0x100                                             # added to an output's type by the attention calls
+FINE = 0x100                                             # may be added to the type of attention's inputs
 OK, ERR_NULL, ERR_SHAPE, ERR_FORMAT, ERR_UNSUPPORTED, ERR_ALIGN, ERR_LAUNCH = range(7)
 
 
@@ -1084,7 +1084,7 @@ def rope_bwd(G, positions, freq, interleaved=False, gain=1.0, out=None, stream=N
     return _rope(lib().lba_rope_bwd, G, positions, freq, interleaved, gain, out, stream)
 
 
-def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
+def _attn(q, k, v, starts, starts_k, causal, scale, clear, fine, on, device):
     """(lba_attn, (q, k, v, starts, starts_k) as they are read) of a call, which keeps them all until the kernels are launched: copies among them are
     nobody else's."""
     n, qs, ks = q.dim(), q.shape, k.shape
@@ -1115,7 +1115,7 @@ def _attn(q, k, v, starts, starts_k, causal, scale, clear, on, device):
                 raise ValueError("starts and starts_k are of different sequences")
     dtype = q.dtype
     (q, q_at), (k, k_at), (v, v_at) = _heads(q, "q", on), _heads(k, "k", on, device, dtype), _heads(v, "v", on, device, dtype)
-    a = lba_attn(q.size(0), k.size(0), count, _at(starts), _at(starts_k), H, KV, D, _TYPE[dtype], causal, clear, D ** -0.5 if scale is None else scale,
+    a = lba_attn(q.size(0), k.size(0), count, _at(starts), _at(starts_k), H, KV, D, _TYPE[dtype] | (FINE if fine else 0), causal, clear, D ** -0.5 if scale is None else scale,
                  q_at, k_at, v_at)
     return a, (q, k, v, starts, starts_k)
 
@@ -1143,7 +1143,7 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     if device < 0:
         raise TypeError("q must be a device tensor")
     handle, on = _on(stream, device)
-    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, fine, on, device)
     q3, k3, v3 = held[:3]
     o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     lse = _empty(q.shape[:-1], torch.float32, q.device, on) if want_stats else None
@@ -1151,13 +1151,15 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
         lse.fill_(-math.inf) if on is None else _of_pool(lambda: lse.fill_(-math.inf), on)
     size = _attn_bytes("lba_attention_workspace_bytes", a)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type | FINE if fine else o_type, fmt, _at(lse), _at(ws), size, handle))
+    _check(lib().lba_attention(a, _at(q3), _at(k3), _at(v3), _at(o), o_type, fmt, _at(lse), _at(ws), size, handle))
     return (o, lse) if want_stats else o
 
 
-def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, scale=None, out=None, stream=None):
+def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, scale=None, out=None, stream=None, fine=False):
     """Gradients of attention: (dq, dk, dv) of the inputs' shapes and type, from G = dL/do and o and lse as the forward call gave them (o of
-    q's type).  out: three tensors, or views of one, to write them to; rows of no sequence are left as they were there, and zeros elsewhere."""
+    q's type).  out: three tensors, or views of one, to write them to; rows of no sequence are left as they were there, and zeros elsewhere.
+    fine, for bfloat16: rowsum(G * o) has no rounding of o for any query, not only for those that see up to 512 keys;
+    the call takes up to 1.3 times as long.  It tells where values have a mean."""
     device = q.get_device()
     if device < 0:
         raise TypeError("q must be a device tensor")
@@ -1165,7 +1167,7 @@ def attention_bwd(G, q, k, v, o, lse, starts=None, starts_k=None, causal=True, s
     _like(o, q.shape, device, "o", (q.dtype,))
     _like(lse, q.shape[:-1], device, "lse", (torch.float32,))
     handle, on = _on(stream, device)
-    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, on, device)
+    a, held = _attn(q, k, v, starts, starts_k, causal, scale, out is None, fine, on, device)
     q3, k3, v3 = held[:3]
     G, o, lse = _whole(G, on), _whole(o, on), _whole(lse, on)
     if out is None:
@@ -1297,6 +1299,6 @@ def cache_attention(q, cache, table, lens, scale=None, out_dtype=None, out_fmt=N
     o = _made(q, dtype, on) if out is None else _output(out, q, q.shape, dtype, on)
     size = _layer_bytes("lba_cache_attention_workspace_bytes", c.count, c.table_row, c.page, fresh, H, c.KV, c.D)
     ws = _scratch(size, q.device, on)
-    _check(lib().lba_cache_attention(c, _at(q3), lba_strides(*q_at), _TYPE[q.dtype], fresh, H, c.D ** -0.5 if scale is None else scale, _at(o),
-                                     o_type | FINE if fine else o_type, fmt, _at(ws), size, handle))
+    _check(lib().lba_cache_attention(c, _at(q3), lba_strides(*q_at), _TYPE[q.dtype] | (FINE if fine else 0), fresh, H, c.D ** -0.5 if scale is None else scale, _at(o), o_type,
+                                     fmt, _at(ws), size, handle))
     return o

@@ -19,7 +19,7 @@ struct AttnParams {
     lba_strides q, k, v, dq, dk, dv;
     int32_t T, Tk, count, H, KV, group, D;
     int32_t causal, clear, o_type;
-    int32_t fine;            // weights of bfloat16 inputs are three pieces
+    int32_t fine;            // bfloat16 inputs: forward, weights are three pieces; backward, all tiles make rowsum(G * O) from the weights
     int32_t tiles, units;    // tiles of queries (keys) that there may be, and those of all heads
     int32_t slices;          // parts that a workgroup's steps are cut into, where there are few workgroups
     float* part;             // their sums: [slices][rows][D], behind them what else a row has

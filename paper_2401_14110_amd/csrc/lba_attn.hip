@@ -41,9 +41,10 @@ int attn_plan(const lba_attn& a, AttnPlan* plan) {
     if (plan->tiles_q * a.H > kMostUnits || plan->tiles_k * a.KV > kMostUnits) return LBA_ERR_SHAPE;
     const int64_t step = a.type == LBA_F32 ? 32 : 64, count = a.count > 0 ? a.count : 1;
     const int64_t keys = a.Tk / count / step, queries = a.T / count / step * (a.KV > 0 ? a.H / a.KV : 1);
-    // Float32's steps of half as many rows take three times as long, so shorter parts are worth a join, and a pass whose workgroups have a CU each is cut
-    // for one round of them.  7 sequences of 33 to 517, 6 heads of 83, with 384, 512 and 1024 workgroups: forward 35, 31 and 30 us (two on a CU), dQ 51,
-    // 61 and 72, dK and dV 64, 60 and 59, their join 11, 12 and 13.
+    // Bfloat16: two workgroups a CU, which is what the 256 have room for, of dK and dV with heads above 64 one; the tiles counted are those that there may be.
+    // Float32's steps of half as many rows take three times as long, so shorter parts are worth a join.  Its numbers of workgroups are those that took least
+    // for 7 sequences of 33 to 517, 6 heads of 83, where a seventh of the tiles are empty; with 384, 512 and 1024: forward (two on a CU) 35, 31 and 30 us, dQ
+    // (one) 51, 61 and 72, dK and dV (one) 64, 60 and 59, their join 11, 12 and 13.
     const bool f32 = a.type == LBA_F32;
     const int64_t least = f32 ? 2 : 4;
     plan->slices = slices_for(plan->tiles_q * a.H, keys, f32 ? 1024 : 512, least);
@@ -106,6 +107,7 @@ extern "C" {
 
 size_t lba_attention_workspace_bytes(lba_attn a) {
     AttnParams p = {};
+    take_fine(&a.type);
     AttnPlan plan;
     if (attn_params(a, &p) != LBA_OK || attn_plan(a, &plan) != LBA_OK || plan.slices == 1) return 0;
     return align256((size_t)plan.slices * (size_t)p.T * (size_t)p.H * (size_t)(p.D + 2) * sizeof(float));
@@ -114,9 +116,8 @@ size_t lba_attention_workspace_bytes(lba_attn a) {
 int lba_attention(lba_attn a, const void* Q, const void* K, const void* V, void* O, int32_t o_type, lba_infmt o_fmt, float* lse, void* workspace,
                   size_t workspace_bytes, void* hip_stream) {
     AttnParams p = {};
+    const bool fine = take_fine(&a.type);
     int rc = attn_params(a, &p);
-    const bool fine = (o_type & LBA_FINE) != 0;
-    o_type &= ~LBA_FINE;
     if (rc == LBA_OK) rc = check_out_type(o_type, o_fmt);
     if (rc != LBA_OK) return rc;
     if (p.T == 0 || p.H == 0) return LBA_OK;

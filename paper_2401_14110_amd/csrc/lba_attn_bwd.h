@@ -21,10 +21,10 @@ constexpr float kLog2e = 1.44269504f;
 
 // rowsum(G * O), which S takes off G . V^T, is the sum of P * (G . V^T) over a query's keys.  Taken from a bfloat16 O it has that rounding, 2^-9 of
 // |G . O|, which stays where the difference cancels: few keys, or values with a mean.  So tiles of queries of up to this many steps go over their
-// keys before, for the sum itself; the others, whose difference cancels less, take O's.  Off, relative to the gradients' norm, with O's and so: two keys 3.8e-3
+// keys before, for the sum itself; the others take O's, if the caller does not ask for the same.  Off, relative to the gradients' norm, with O's and so: two keys 3.8e-3
 // and 2.4e-3, 100 keys whose values' mean is their spread 3.5e-3 and 2.3e-3, eight times it 2.1e-2 and 2.4e-3.  Backward passes: 32 sequences of
 // 128, 12 heads of 64, 27.7 and 29.7 us, 8 of 512, 16 heads of 64, not causal, 50 and 60, 2 of 4096 causal, 32 heads of 128 on 8, 969 and 973; there
-// with all tiles so 1219, for 2.48e-3 and 2.36e-3 (1500 keys of values around zero).
+// with all tiles so 1219, for 2.48e-3 and 2.36e-3 (1500 keys of values around zero; 4.1e-3 and 2.4e-3 where their mean is their spread).
 constexpr int kFewSteps = 8;
 
 template <typename T, int DP, bool DIRECT>
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 3
     if (first >= tiles && slice > 0) return;
     const bool there = i < rq.n;
     const int all = steps_of_queries(p, rq, rk, at.t, KT);
-    const bool twice = sizeof(T) == 2 && all <= kFewSteps;                           // (also a part of the steps goes over all)
+    const bool twice = sizeof(T) == 2 && (all <= kFewSteps || p.fine);                           // (also a part of the steps goes over all)
 
     Loader<T, DP, DIRECT> lk, lv;
     auto start = [&](int kt, int buf) {                  // tile kt is the next

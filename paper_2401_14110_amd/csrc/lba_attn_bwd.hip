@@ -42,6 +42,7 @@ extern "C" {
 
 size_t lba_attention_bwd_workspace_bytes(lba_attn a) {
     AttnParams p = {};
+    take_fine(&a.type);
     AttnPlan plan;
     if (attn_params(a, &p) != LBA_OK || attn_plan(a, &plan) != LBA_OK) return 0;
     const size_t delta = align256((size_t)p.T * (size_t)p.H * sizeof(float));
@@ -54,6 +55,7 @@ int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, c
                       lba_strides dq_at, void* dK, lba_strides dk_at, void* dV, lba_strides dv_at, void* workspace, size_t workspace_bytes,
                       void* hip_stream) {
     AttnParams p = {};
+    const bool fine = take_fine(&a.type);
     int rc = attn_params(a, &p);
     if (rc == LBA_OK) rc = check_strides(dq_at);
     if (rc == LBA_OK) rc = check_strides(dk_at);
@@ -65,6 +67,7 @@ int lba_attention_bwd(lba_attn a, const void* G, const void* Q, const void* K, c
     if (queries && (uintptr_t)workspace % 256 != 0) return LBA_ERR_ALIGN;
     if (workspace_bytes < lba_attention_bwd_workspace_bytes(a)) return LBA_ERR_SHAPE;
     p.Q = Q; p.K = K; p.V = V; p.O = (void*)O; p.G = G; p.lse = (float*)lse; p.delta = (float*)workspace;
+    p.fine = fine;
     p.dQ = dQ; p.dK = dK; p.dV = dV; p.dq = dq_at; p.dk = dk_at; p.dv = dv_at;
     const hipStream_t st = (hipStream_t)hip_stream;
     AttnPlan plan;

@@ -37,6 +37,12 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int T, int cou
 
 // ---- host checks ----------------------------------------------------------------------------
 
+// whether LBA_FINE was in a type, which is without it then
+inline bool take_fine(int32_t* type) {
+    const bool fine = (*type & LBA_FINE) != 0;
+    *type &= ~LBA_FINE;
+    return fine;
+}
 inline int check_strides(const lba_strides& s) { return s.row < 0 || s.head < 0 ? LBA_ERR_SHAPE : LBA_OK; }
 inline int check_heads(int64_t T, int64_t H, int64_t D) {
     return T < 0 || T > 2147483647LL || H < 0 || H > 65535 || D < 0 || D > 1024 ? LBA_ERR_SHAPE : LBA_OK;

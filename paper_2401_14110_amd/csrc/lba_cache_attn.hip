@@ -90,9 +90,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int 
                  (parts[0] + parts[1]) + (parts[2] + parts[3]));
 }
 
-// How the rows and positions are cut: rows of a tile, and a chunk's positions, so many that there are about 1024 workgroups (three on a CU at a time)
-// where every sequence fills its table, and 256 at least (two steps of each wave).  With 1024, 2048, 4096 and 8192: 64 sequences of 1000 to
-// 8000 tokens 70, 72, 72 and 80 us, one of 131071 43, 45, 58 and 58.
+// How the rows and positions are cut: rows of a tile, and a chunk's positions, so many that there are about 1024 workgroups where every sequence fills its
+// table, and 256 at least (two steps of each wave).  With 1024, 2048, 4096 and 8192: 64 sequences of 1000 to 8000 tokens 70, 72, 72 and 80 us, one of
+// 131071 43, 45, 58 and 58; fewer were not tried (a CU has three at a time, with heads of 64 four).  A table has room for more than a sequence holds, and only the
+// part that is held has work: 16 sequences of 8000, 32 heads of 128 on 8, take 33 us in a table for 8000 and 72 in one for 131072.
 struct CachePlan {
     int32_t r, row_tiles;
     int64_t chunk, chunks, rows;
@@ -133,9 +134,8 @@ int lba_cache_attention(lba_cache4 c, const void* Q, lba_strides q_at, int32_t t
     if (rc == LBA_OK) rc = check_strides(q_at);
     if (rc == LBA_OK && (fresh < 0 || fresh > 2147483647LL || H < 0 || H > 65535 || (H > 0 && (c.KV < 1 || H % c.KV != 0)))) rc = LBA_ERR_SHAPE;
     if (rc == LBA_OK && (c.count * H > 0 && fresh > 2147483647LL / (c.count * H))) rc = LBA_ERR_SHAPE;
+    const bool fine = take_fine(&type);
     if (rc == LBA_OK) rc = check_float_type(type);
-    const bool fine = (o_type & LBA_FINE) != 0;
-    o_type &= ~LBA_FINE;
     if (rc == LBA_OK) rc = check_out_type(o_type, o_fmt);
     if (rc != LBA_OK) return rc;
     if (c.count == 0 || fresh == 0 || H == 0) return LBA_OK;

@@ -4,11 +4,13 @@
 // query heads that share it) and a chunk of positions; its four waves take steps of 32 positions in turn, each with a softmax of its own,
 // and meet in LDS at the end.  Chunks leave their sums, maximum and rows in the workspace, where a second launch joins them, always in the
 // same order.
-// In a step lane l has position l % 16 (and that + 16), elements D / 4 * (l / 16) ..: codes come as they are packed, 512 bytes a load, and become bfloat16
-// in registers, which holds a code times a power of two exactly.  S^T = K . Q^T on 16 x 16 x 32 leaves a row's scores in four lanes; their
-// weights are the other factor of O^T = V^T . P^T without moving, and V, whose rows have to become columns, goes through 32 rows of LDS that
-// are the wave's own: no barriers.  Bound by reading the codes: one sequence of 131071, 8 heads of 128 (143 MB), 31 us, 4.5 TB/s; 64 of 1000 to 8000 (233
-// MB) 58 us, 4.0 TB/s, where a library's sum over 1 GiB reads 3.9.  Weights are rounded to bfloat16 for the product with the values.  Float32 (outputs: weights): queries and weights are split into three bfloat16 pieces each, so that products are exact.
+// In a step lane l has position l % 16 (and that + 16), elements D / 4 * (l / 16) ..: codes come as they are packed, 8 D bytes a load of the wave (1024
+// with heads of 128), and become bfloat16 in registers, which holds a code times a power of two exactly.  S^T = K . Q^T on 16 x 16 x 32 leaves a row's
+// scores in four lanes; their weights are the other factor of O^T = V^T . P^T without moving, and V, whose rows have to become columns, goes through
+// 32 rows of LDS that are the wave's own: no barriers.  Bound by reading the codes: one sequence of 131071, 8 heads of 128 (143 MB), 31 us, 4.5 TB/s; 64
+// of 1000 to 8000 (233 MB) 58 us, 4.0 TB/s, of which the longest chunk, where others have ended, is a part.  Weights are rounded to bfloat16 for
+// the product with the values; queries of float32, and weights of them, of outputs of float32, or where the caller asks, are split into three
+// bfloat16 pieces, so that products are exact (the 64 sequences 73 us for 60 with an output of float32, 89 in float32).
 #ifndef LBA_CACHE_ATTN_FWD_H_
 #define LBA_CACHE_ATTN_FWD_H_
 

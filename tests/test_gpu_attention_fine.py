@@ -1,4 +1,5 @@
-"""Weights that are not rounded to bfloat16, on request, for every output type of both attentions: the bounds are those of float32."""
+"""What bfloat16 inputs may ask for: weights that are not rounded to bfloat16 for any output type of both attentions, whose bounds are those of float32, and
+gradients without the rounding of O for any query."""
 import ctypes
 
 import numpy as np
@@ -9,6 +10,7 @@ import attention_oracle as ao
 import layer_oracle as lo
 from paper_2401_14110_amd import binding as lb
 from test_gpu_attention import desc, starts
+from test_gpu_attention_offset import against_the_formulas
 from test_gpu_cache import a_table, expected, filled, ints, on_device
 from test_gpu_layernorm import DEV, dev, near, values
 
@@ -58,10 +60,33 @@ def test_over_the_cache(lens, fresh, H, KV, D, page):
         lo.check_codes(codes.cpu().numpy(), want, tol + 2 * lo.U * np.abs(want), fmt)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("mean", [0.0, 1.0, 64.0])
+@pytest.mark.parametrize("lens,lens_k,H,KV,D,causal", [([700, 3, 0, 513], [700, 3, 0, 513], 2, 1, 64, True), ([40, 600], [1100, 577], 1, 1, 83, False), ([1500], [1500], 1, 1, 128, True),
+                                                       ([1500], [1500], 1, 1, 128, False), ([2, 200], [2, 200], 2, 2, 32, True)])
+def test_gradients_of_all_queries(lens, lens_k, H, KV, D, causal, mean):
+    against_the_formulas(lens, lens_k, H, KV, D, causal, mean, True)
+
+
+@pytest.mark.gpu
+def test_gradients_in_float32_and_workspaces():
+    q = torch.randn(300, 2, 40, device="cuda")
+    o, lse = lb.attention(q, q, q, want_stats=True)
+    for a, b in zip(lb.attention_bwd(q, q, q, q, o, lse), lb.attention_bwd(q, q, q, q, o, lse, fine=True)):
+        assert torch.equal(a, b)
+
+
 def test_refusals():
     P, f = ctypes.c_void_p(0x1000), (4, 3, 7)
-    call = lambda t, **k: lb.lba_attention(desc(**k), P, P, P, P, t, f, None, None, 0)  # noqa: E731
-    assert call(lb.FINE | 3) == lb.ERR_UNSUPPORTED and call(2 * lb.FINE) == lb.ERR_UNSUPPORTED and call(lb.FINE | lb.CODE8, T=0, Tk=0) == lb.OK
-    cache = lb.lba_cache4(P, P, P, P, 4, 2, 2, P, P, 16, 2, 64)
-    over = lambda t, fresh=1: lb.lba_cache_attention(cache, P, lb.lba_strides(128, 64), 0, fresh, 4, 0.1, P, t, f, P, 1 << 20)  # noqa: E731
-    assert over(lb.FINE | 3) == lb.ERR_UNSUPPORTED and over(2 * lb.FINE) == lb.ERR_UNSUPPORTED and over(lb.FINE | lb.BF16, 0) == lb.OK
+    for t in (lb.F32, lb.BF16):                          # the same workspaces
+        for name in (lb.lba_attention_workspace_bytes, lb.lba_attention_bwd_workspace_bytes):
+            for k in (dict(T=8, Tk=8), dict(T=128, Tk=4096)):
+                assert name(desc(type=t, **k)) == name(desc(type=t | lb.FINE, **k))
+    s = lb.lba_strides(64, 16)
+    back = lambda t: lb.lba_attention_bwd(desc(type=t, T=0, Tk=0), P, P, P, P, P, P, P, s, P, s, P, s, P, 1 << 20)  # noqa: E731
+    call = lambda t, o=0, **k: lb.lba_attention(desc(type=t, **k), P, P, P, P, o, f, None, None, 0)  # noqa: E731
+    over = lambda t, fresh=1: lb.lba_cache_attention(lb.lba_cache4(P, P, P, P, 4, 2, 2, P, P, 16, 2, 64), P, lb.lba_strides(128, 64), t, fresh, 4, 0.1, P, 0, f, P, 1 << 20)  # noqa: E731
+    for fn in (call, back, over):
+        assert fn(lb.FINE | 2) == lb.ERR_UNSUPPORTED and fn(2 * lb.FINE) == lb.ERR_UNSUPPORTED
+    assert call(lb.FINE | lb.BF16, T=0, Tk=0) == lb.OK and back(lb.FINE | lb.BF16) == lb.OK and over(lb.FINE | lb.BF16, 0) == lb.OK
+    assert call(lb.BF16, lb.FINE, T=0, Tk=0) == lb.ERR_UNSUPPORTED                   # (of the inputs' type)

@@ -45,6 +45,10 @@ def gradients(f, g, few):
     # cut into parts, with short sequences and early tiles among them
     ([1500, 100], [1500, 100], 2, 1, 64), ([40, 700, 1], [300, 900, 3000], 1, 1, 128)])
 def test_gradients_of_values_with_a_mean(lens, lens_k, H, KV, D, causal, mean):
+    against_the_formulas(lens, lens_k, H, KV, D, causal, mean, False)
+
+
+def against_the_formulas(lens, lens_k, H, KV, D, causal, mean, fine):
     rng = np.random.default_rng(sum(lens) + D)
     T, Tk = sum(lens), sum(lens_k)
     q, k, G = (values(rng, (t, h, D), "bf16") for t, h in ((T, H), (Tk, KV), (T, H)))
@@ -52,7 +56,7 @@ def test_gradients_of_values_with_a_mean(lens, lens_k, H, KV, D, causal, mean):
     kw = dict(starts=starts(lens), starts_k=starts(lens_k), causal=causal)
     tensors = [dev(x, "bf16") for x in (q, k, v)]
     o, lse = lb.attention(*tensors, want_stats=True, **kw)
-    got = [host(t) for t in lb.attention_bwd(dev(G, "bf16"), *tensors, o, lse, **kw)]
+    got = [host(t) for t in lb.attention_bwd(dev(G, "bf16"), *tensors, o, lse, fine=fine, **kw)]
     want, tol = ([np.zeros(t.shape) for t in (q, k, v)] for _ in range(2))
     a = c = 0
     for n, m in zip(lens, lens_k):
@@ -60,7 +64,7 @@ def test_gradients_of_values_with_a_mean(lens, lens_k, H, KV, D, causal, mean):
         a, c = a + n, c + m
         see = ao.seen(n, m, causal)
         last = np.minimum(np.arange(n) // TILE * TILE + TILE, n) - 1                 # of a query's tile: it sees most
-        few = see.sum(1)[last] <= FEW if n else np.zeros(0, bool)
+        few = (see.sum(1)[last] <= FEW) | fine if n else np.zeros(0, bool)
         for h in range(H):
             kv = h // (H // KV)
             f = ao.attend(q[i, h], k[j, kv], v[j, kv], see, float(np.float32(D ** -0.5)), "bf16")
