@@ -156,6 +156,10 @@ def main(argv=None):
     ap.add_argument("--kv-heads", type=int, default=2)
     ap.add_argument("--rate", type=float, default=None, help="learning rate (1 / width)")
     a = ap.parse_args(argv)
+    if a.rows < 3:
+        ap.error("--rows must be 3 or more: the first third is served too")
+    if a.width // a.heads not in (32, 64, 96, 128):
+        ap.error("--width / --heads must be 32, 64, 96 or 128, which a cache holds")
     block = SelfAttention(a.width, a.heads, a.kv_heads, p=0.05)
     g = torch.Generator().manual_seed(1)
     x = torch.randn((a.rows, a.width), generator=g).cuda()

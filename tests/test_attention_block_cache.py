@@ -34,6 +34,13 @@ def test_one_sequence_takes_no_list_from_the_host(monkeypatch):
     assert block.forward(x, torch.arange(5), cache=("held", "table", ints(6, device="cpu"))).isnan().all()
 
 
+@pytest.mark.parametrize("args", [["--rows", "2"], ["--width", "96", "--heads", "4"], ["--width", "512", "--heads", "2"]])
+def test_the_command_refuses_what_it_cannot_serve(args, capsys):
+    with pytest.raises(SystemExit):
+        at.main(["--steps", "1"] + args)
+    assert "must be" in capsys.readouterr().err
+
+
 @pytest.fixture
 def server():
     torch.manual_seed(3)
@@ -70,6 +77,11 @@ def test_rows_behind_older_tokens(server):
     with pytest.raises(ValueError):                      # a row of each of two sequences is not one sequence of two rows
         block.forward(x[:2], positions[:2], cache=(held, table, ints(1, 1)))
     assert block.forward(x[:0], positions[:0], ints(0), cache=(held, table[:0], table[:0, 0])).shape == (0, 64)
+
+
+@pytest.mark.gpu
+def test_the_shortest_run_of_the_command():
+    assert len(at.main(["--steps", "1", "--rows", "3", "--width", "64", "--heads", "2", "--kv-heads", "1"])) == 1
 
 
 @pytest.mark.gpu
