@@ -187,65 +187,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? DIRECT || DP <= 96 : DP <= 3
     else store_columns((T*)p.dQ + (int64_t)(rq.first + i) * p.dq.row + (int64_t)h * p.dq.head, acc, scale, p.D, half);
 }
 
-// One key by one wave, over the queries of its sequence from `lo` on that steps first .. last - 1 have (steps_head a head, `size` queries each from q0 on): a lane a
-// query, then a lane two columns.  words: 384 of LDS.  slice: -1 where these are all.
-template <typename T> __device__ __forceinline__ void dkv_row(const AttnParams& p, float* words, int kv, int t, Rows rq, int lo, int first, int last, int steps_head, int q0,
-                                                              int size, int slice, int lone, float scale) {
-    const int lane = threadIdx.x & 63;
-    const CodeFmt none = {};
-    float *const v = words + 128, *const wp = words + 256, *const ws = words + 320;
-    wave_words_done();
-    for (int d = lane; d < 128; d += 64) {
-        words[d] = d < p.D ? load_one((const T*)p.K + (int64_t)t * p.k.row + (int64_t)kv * p.k.head + d) : 0.0f;
-        v[d] = d < p.D ? load_one((const T*)p.V + (int64_t)t * p.v.row + (int64_t)kv * p.v.head + d) : 0.0f;
-    }
-    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    for (int n = first; n < last; ++n) {
-            const int h = kv * p.group + n / steps_head, i0 = max(lo, q0 + n % steps_head * size), end = min(rq.n, q0 + n % steps_head * size + size);
-            wave_words_done();
-            float e = 0.0f, f = 0.0f;
-            if (i0 + lane < end) {
-                const int64_t at = rq.first + i0 + lane, row = at * p.H + h;
-                const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
-                const T* g = (const T*)p.G + row * p.D;
-                float s = 0.0f, u = 0.0f;
-                for (int d = 0; d < p.D; ++d) { s = fmaf(words[d], load_one(q + d), s); u = fmaf(v[d], load_one(g + d), u); }
-                e = __builtin_amdgcn_exp2f((s * p.scale - p.lse[row]) * kLog2e);
-                f = i0 + lane == lone ? 0.0f : e * (u - p.delta[row]);
-            }
-            wp[lane] = e;
-            ws[lane] = f;
-            wave_words_done();
-            for (int j = 0; j < 64 && i0 + j < end; ++j) {
-                const int64_t at = rq.first + i0 + j;
-                const T* q = (const T*)p.Q + at * p.q.row + (int64_t)h * p.q.head;
-                const T* g = (const T*)p.G + (at * p.H + h) * p.D;
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (lane + 64 * x < p.D) {
-                        dk[x] = fmaf(ws[j], load_one(q + lane + 64 * x), dk[x]);
-                        dv[x] = fmaf(wp[j], load_one(g + lane + 64 * x), dv[x]);
-                    }
-            }
-        }
-    if (slice >= 0) {
-        const int64_t rows = (int64_t)p.Tk * p.KV, to = slice * rows + (int64_t)t * p.KV + kv;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (lane + 64 * x < p.D) {
-                p.part[to * p.D + lane + 64 * x] = dk[x] * scale;
-                p.part[(p.slices * rows + to) * p.D + lane + 64 * x] = dv[x];
-            }
-        return;
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-        if (lane + 64 * x < p.D) {
-            store_one((T*)p.dK + (int64_t)t * p.dk.row + (int64_t)kv * p.dk.head + lane + 64 * x, dk[x] * scale, none);
-            store_one((T*)p.dV + (int64_t)t * p.dv.row + (int64_t)kv * p.dv.head + lane + 64 * x, dv[x], none);
-        }
-}
-
 template <typename T, int DP, bool DIRECT>
 __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams p) {
     constexpr int QT = kStep<T>, QB = QT / 32, KC = DP / 16, DT = DP / 32;
@@ -311,7 +252,6 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
 #pragma unroll
     for (int t = 0; t < DT; ++t) { dk[t] = f32x16{}; dv[t] = f32x16{}; }
     int n = part.first;                                  // steps that are done
-    bool broken = false;                                 // a tile that some key sees in part holds infinities or NaN
     // One tile of queries.  EDGE: some key may not be seen by all of them.  PIPE: the products of one block of 32 queries run while the weights of the
     // other are worked out, since a wave that is alone on its SIMD has only its own instructions to fill it; else two waves share it.
     auto step = [&](int tile, auto edge) {
@@ -330,9 +270,13 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
         asm volatile("" ::: "memory");
         if (++n < steps) load(buf ^ 1);
         if constexpr (EDGE) {
+            // Some key is not seen by all: zeros for infinities and NaN.  A query that has any has them in lse or rowsum(G * O) too, and so as a weight.
             if (p.causal && q0 < masked_all) {
-                const bool a = tile_is_broken<T, DP>(tq);
-                if (tile_is_broken<T, DP>(tg) || a) { broken = true; return; }
+                const bool a = tile_is_broken<T, DP>(tq), b = tile_is_broken<T, DP>(tg);
+                if (a) clean_tile<T, DP>(tq);
+                if (b) clean_tile<T, DP>(tg);
+                if ((a || b) && threadIdx.x < QT && !(fabsf(side[buf][1][threadIdx.x]) < __builtin_inff())) side[buf][0][threadIdx.x] = __builtin_nanf("");
+                if (a || b) __syncthreads();
             }
             if (q0 + QT <= lo_wave) return;
         }
@@ -425,17 +369,10 @@ __global__ __launch_bounds__(256, DIRECT && sizeof(T) == 2 && DP <= 64 ? 2 : 1) 
     };
     // of every head the steps at the edge, then those that all the workgroup's keys are seen by
     const int edge = max(0, min(steps_head, (masked_all + QT - 1) / QT - t0));
-    while (n < steps && !broken) {
+    while (n < steps) {
         const int tile = n % steps_head, head = n - tile;
-        for (int last = min(steps, head + edge); n < last && !broken;) step(n - head, Known<1>{});
-        for (int last = min(steps, head + steps_head); n < last && !broken;) step(n - head, Known<0>{});
-    }
-    if (broken) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __syncthreads();
-        for (int x = 0; x < 32 && j0 + x < rk.n; ++x)
-            dkv_row<T>(p, (float*)&lds[0][0][0] + wave * 384, kv, rk.first + j0 + x, rq, first_of(j0 + x), part.first, steps, steps_head, t0 * QT, QT, part.alone ? -1 : slice, lone, scale);
-        return;
+        for (int last = min(steps, head + edge); n < last;) step(n - head, Known<1>{});
+        for (int last = min(steps, head + steps_head); n < last;) step(n - head, Known<0>{});
     }
     if (!there) return;
     if (!part.alone) {

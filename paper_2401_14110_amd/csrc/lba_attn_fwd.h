@@ -25,56 +25,6 @@ __device__ __forceinline__ void store_end(const AttnParams& p, int64_t to, float
     end[1] = sum;
 }
 
-// One query by one wave, over the `seen` keys from row k0 on and nothing else: a lane a key, then a lane two columns.  words: 192 of LDS.  slice: -1
-// where these are all its keys.
-template <typename T> __device__ __forceinline__ void attn_row(const AttnParams& p, float* words, int h, int kv, int t, int k0, int seen, int slice) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)t * p.H + h;
-    float* const w = words + 128;
-    wave_words_done();
-    for (int d = lane; d < 128; d += 64) words[d] = d < p.D ? load_one((const T*)p.Q + (int64_t)t * p.q.row + (int64_t)h * p.q.head + d) : 0.0f;
-    float top = -__builtin_inff(), sum = 0.0f, acc[2] = {0.0f, 0.0f};
-    for (int j0 = 0; j0 < seen; j0 += 64) {
-        wave_words_done();
-        float s = -__builtin_inff();
-        if (j0 + lane < seen) {
-            const T* k = (const T*)p.K + (int64_t)(k0 + j0 + lane) * p.k.row + (int64_t)kv * p.k.head;
-            s = 0.0f;
-            for (int d = 0; d < p.D; ++d) s = fmaf(words[d], load_one(k + d), s);
-            s *= p.scale * 1.44269504f;
-        }
-        const float now = fmaxf(wave_max(s), top), base = now == -__builtin_inff() ? 0.0f : now;
-        const float e = j0 + lane < seen ? __builtin_amdgcn_exp2f(s - base) : 0.0f, f = __builtin_amdgcn_exp2f(top - base);
-        top = now;
-        sum = sum * f + wave_sum(e);
-        w[lane] = e;
-        wave_words_done();
-        acc[0] *= f;
-        acc[1] *= f;
-        for (int j = 0; j < 64 && j0 + j < seen; ++j) {
-            const T* v = (const T*)p.V + (int64_t)(k0 + j0 + j) * p.v.row + (int64_t)kv * p.v.head;
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (lane + 64 * x < p.D) acc[x] = fmaf(w[j], load_one(v + lane + 64 * x), acc[x]);
-        }
-    }
-    if (slice >= 0) {
-        const int64_t to = (int64_t)slice * p.T * p.H + row;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (lane + 64 * x < p.D) p.part[to * p.D + lane + 64 * x] = acc[x];
-        if (lane == 0) store_end(p, to, top, sum);
-        return;
-    }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    with_output(p, [&](auto* o) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-            if (lane + 64 * x < p.D) store_one(o + row * p.D + lane + 64 * x, acc[x] * inv, p.fmt);
-    });
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * 0.693147181f;
-}
-
 // FINE: bfloat16 whose weights are three pieces too.
 // Where rows do not go straight to LDS one loop has all tiles: the code of two, read once each by short sequences, costs more than its edge's tests.
 template <typename T, int DP, bool DIRECT, bool FINE>
@@ -82,6 +32,7 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
     static_assert(!FINE || sizeof(T) == 2, "float32 has three pieces in any case");
     constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of keys and values
+    __shared__ uint32_t firsts[DP];                      // of a tile whose values hold infinities or NaN: where
     if ((int)blockIdx.x >= p.units * p.slices) {
         with_output(p, [&](auto* o) { clear_rows(p.starts, p.T, p.count, blockIdx.x - p.units * p.slices, kClearBlocks, o, (int64_t)p.H * p.D, p.D, p.H, p.D, p.lse, p.fmt); });
         return;
@@ -127,7 +78,6 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x16{};
     float top = -__builtin_inff(), sum = 0.0f;           // of this lane's query: the maximum in use, times c, and this half's sum
-    bool broken = false;                                 // a tile that some query sees in part holds infinities or NaN
     // One tile.  EDGE: some query may not see all of it; the tiles before are seen whole by every query of the workgroup.
     auto step = [&](int kt, auto edge, int buf) {
         constexpr bool EDGE = decltype(edge)::value != 0;
@@ -143,8 +93,13 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
             lk.load(lds[buf ^ 1][0], rk.n - k0 - KT);
             lv.load(lds[buf ^ 1][1], rk.n - k0 - KT);
         }
+        bool broken = false;                             // some query sees this tile in part, and its values hold infinities or NaN
         if constexpr (EDGE) {
-            if (p.causal && k0 + KT > least_all && tile_is_broken<T, DP>(tv)) { broken = true; return; }
+            broken = p.causal && k0 + KT > least_all && tile_is_broken<T, DP>(tv);
+            if (broken) {
+                find_broken<T, DP>(tv, firsts);
+                clean_tile<T, DP>(tv);
+            }
             if (k0 >= most) return;                      // (the barriers above are everybody's)
         }
         f32x16 s[KB];
@@ -214,6 +169,15 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
                     for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
                 }
             }
+        if constexpr (EDGE) {
+            if (broken) {
+                const uint32_t rows = min(max(lim - k0, 0), KT);
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[t][r] += broken_sum(firsts[32 * t + row_of(r) + 4 * half], rows);
+            }
+        }
     };
     const int whole = min(tiles, least_all / KT);
     int kt = first;
@@ -223,16 +187,7 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
             step(kt + 1, Known<0>{}, 1);
         }
     }
-    for (; kt < tiles && !broken; ++kt) step(kt, Known<1>{}, (kt - first) & 1);
-    if (broken) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __syncthreads();
-        for (int j = 0; j < 32 && i0 + j < rq.n; ++j) {
-            const int seen = min(limit(i0 + j), tiles * KT) - first * KT;
-            attn_row<T>(p, (float*)&lds[0][0][0] + wave * 192, h, kv, rq.first + i0 + j, rk.first + first * KT, seen, part.alone ? -1 : slice);
-        }
-        return;
-    }
+    for (; kt < tiles; ++kt) step(kt, Known<1>{}, (kt - first) & 1);
     sum = sum_of_halves(sum);
     if (i >= rq.n) return;
     const int64_t row = (int64_t)(rq.first + i) * p.H + h;

@@ -323,7 +323,7 @@ template <typename T, int DP> __device__ __forceinline__ bool tile_is_broken(con
 // ---- tiles that hold infinities or NaN -----------------------------------------------------
 //
 // A product over rows some of which a column does not see must not multiply their infinities with its zeros.  Where a tile that is seen in part
-// holds any, the weights' own NaN is enough for what is seen (dQ), or the workgroup's rows are done again, one by one over what each sees.
+// holds any, zeros stand for them; what they do to columns that see them comes from elsewhere: the weights' own NaN (gradients), or where they are.
 
 // the fragment with zeros for infinities and NaN
 __device__ __forceinline__ Frag<bf16_t> without_broken(Frag<bf16_t> f) {
@@ -343,10 +343,36 @@ __device__ __forceinline__ float wave_max(float v) {
     for (int x = 32; x; x /= 2) v = fmaxf(v, __shfl_xor(v, x));
     return v;
 }
-// before a wave's own words of LDS are used for something else
-__device__ __forceinline__ void wave_words_done() {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
+// The same of a tile in LDS (float32: of its last pieces), by the whole workgroup: a barrier before, when all have read it, and after.
+template <typename T, int DP> __device__ __forceinline__ void clean_tile(uint8_t* tile) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kStep<T> * DP / 8; i += 256) {
+        i32x4_t* const at = (i32x4_t*)(tile + (kPieces<T> - 1) * (kTileBytes<T, DP> / kPieces<T>) + i * 16);
+        *at = without_broken(Frag<bf16_t>{*at}).w;
+    }
+    __syncthreads();
+}
+
+// What infinities and NaN in a tile do to sums over its rows is known by a column's first row with each of them, since a query sees the first rows of a
+// tile: firsts[d] has that of infinity, of its negative and of NaN in a byte each (64: there is none).  The whole workgroup calls, clean_tile comes next.
+template <typename T, int DP> __device__ __forceinline__ void find_broken(const uint8_t* tile, uint32_t* firsts) {
+    const uint8_t* const last = tile + (kPieces<T> - 1) * (kTileBytes<T, DP> / kPieces<T>);
+    const int d = threadIdx.x;
+    if (d >= DP) return;
+    uint32_t plus = 64, minus = 64, none = 64;
+#pragma clang loop unroll(disable)
+    for (int row = kStep<T> - 1; row >= 0; --row) {
+        const uint32_t e = *(const uint16_t*)(last + row * (DP * 2) + ((d / 8) ^ turn<DP / 8>(row)) * 16 + d % 8 * 2);
+        if (e == 0x7F80u) plus = row;
+        if (e == 0xFF80u) minus = row;
+        if ((e & 0x7FFFu) > 0x7F80u) none = row;
+    }
+    firsts[d] = plus | minus << 8 | none << 16;
+}
+// what is added to a column of which `seen` rows are seen
+__device__ __forceinline__ float broken_sum(uint32_t firsts, uint32_t seen) {
+    const bool plus = (firsts & 255) < seen, minus = ((firsts >> 8) & 255) < seen, none = firsts >> 16 < seen;
+    return none || (plus && minus) ? __builtin_nanf("") : plus ? __builtin_inff() : minus ? -__builtin_inff() : 0.0f;
 }
 
 // a lane's row of a head as fragments: `D` elements from `at`, zeros behind; zeros where it is not there
