@@ -1136,7 +1136,7 @@ def attention(q, k, v, starts=None, starts_k=None, causal=True, scale=None, out_
     iff j <= i + m - n.  starts_k: the keys' sequences where they are not the queries'.  scale: D^-1/2 by default.  Returns o of q's
     shape and out_dtype (q's by default; torch.uint8 codes need out_fmt), and with want_stats (o, lse), float32 of q.shape[:-1], which
     attention_bwd reads.  Rows of no sequence are zeros, in `out` left as they were, and in lse -infinity.  Weights of bfloat16 inputs are rounded to bfloat16 for
-    the product with v, but for outputs of float32, and with `fine` not for any: it takes up to 1.7 times as long."""
+    the product with v, but for outputs of float32, and with `fine` not for any: it takes up to twice as long."""
     device = q.get_device()
     dtype = out_dtype or q.dtype
     o_type, fmt = _out_type(dtype, out_fmt)

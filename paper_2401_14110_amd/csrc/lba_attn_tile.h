@@ -343,12 +343,20 @@ __device__ __forceinline__ float wave_max(float v) {
     for (int x = 32; x; x /= 2) v = fmaxf(v, __shfl_xor(v, x));
     return v;
 }
-// The same of a tile in LDS (float32: of its last pieces), by the whole workgroup: a barrier before, when all have read it, and after.
+// The same of a tile in LDS (float32: of all pieces), by the whole workgroup: a barrier before, when all have read it, and after.
 template <typename T, int DP> __device__ __forceinline__ void clean_tile(uint8_t* tile) {
+    constexpr int PIECE = kTileBytes<T, DP> / kPieces<T>;
     __syncthreads();
     for (int i = threadIdx.x; i < kStep<T> * DP / 8; i += 256) {
-        i32x4_t* const at = (i32x4_t*)(tile + (kPieces<T> - 1) * (kTileBytes<T, DP> / kPieces<T>) + i * 16);
-        *at = without_broken(Frag<bf16_t>{*at}).w;
+        const i32x4_t all = *(const i32x4_t*)(tile + (kPieces<T> - 1) * PIECE + i * 16);
+        i32x4_t keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = (uint32_t)all[j];
+            keep[j] = (int32_t)~(((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u));
+        }
+#pragma unroll
+        for (int n = 0; n < kPieces<T>; ++n) *(i32x4_t*)(tile + n * PIECE + i * 16) &= keep;
     }
     __syncthreads();
 }

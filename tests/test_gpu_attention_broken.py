@@ -49,7 +49,8 @@ def test_values(lens, D, dtype):
     for n in lens:
         seen[at:at + n] = torch.cumsum(torch.where(bad[at:at + n].isfinite(), 0.0, bad[at:at + n].float()), 0)
         at += n
-    assert torch.equal(got.isnan(), seen.isnan()) and torch.equal(got == INF, seen == INF) and torch.equal(got == -INF, seen == -INF)
+    for out in (got, lb.attention(q, k, bad, starts=s, out_dtype=torch.float32), lb.attention(q, k, bad, starts=s, fine=True)):
+        assert torch.equal(out.isnan(), seen.isnan()) and torch.equal(out == INF, seen == INF) and torch.equal(out == -INF, seen == -INF)
     fine = seen == 0
     assert bool(fine.any()) and torch.equal(got[fine], want[fine])
 
@@ -95,6 +96,23 @@ def test_keys_queries_and_gradients(lens, x, dtype):
             if n > 1 and where:                          # (a query that sees one key leaves nothing to dK)
                 assert not dk[first:t + 1, 0].isfinite().all(-1).any()
         first += n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("fine", [False, True])
+def test_columns_of_infinities(fine, dtype, causal):
+    """Whole columns, under weights of up to 2^8: none of their pieces makes a NaN of them."""
+    n, D = 300, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.rand(n, 1, D, device="cuda", generator=g).add_(0.5).to(dtype)
+    k = (torch.rand(n, 1, D, device="cuda", generator=g) + torch.linspace(0, 3, n, device="cuda")[:, None, None]).to(dtype)          # the maximum rises with the keys
+    v = torch.randn(n, 1, D, device="cuda", generator=g).to(dtype)
+    v[:, 0, 3], v[:, 0, 4], v[::7, 0, 5] = INF, -INF, -INF
+    for out in (dtype, torch.float32):
+        o = lb.attention(q, k, v, causal=causal, fine=fine, out_dtype=out)
+        assert (o[..., 3] == INF).all() and (o[..., 4] == -INF).all() and (o[..., 5] == -INF).all() and o[..., :3].isfinite().all() and o[..., 6:].isfinite().all()
 
 
 @pytest.mark.gpu
