@@ -6,7 +6,7 @@
 // above it in units of log 2: weights are then at most 256 times the final ones, which changes no rounding.
 //
 // Weights are rounded to bfloat16 for the second product, which is what the matrix cores take; their sum is not.  Float32, outputs of float32, and who
-// asks for it: split into pieces.  (13 prompts of 40 to 2048, 32 heads of 128 on 8, to codes of 4 bits of significand: 116 us so and 200 in pieces.  8.2e-3 of
+// asks for it: split into pieces.  (13 prompts of 40 to 2048, 32 heads of 128 on 8, to codes of 4 bits of significand: 116 us so and 207 in pieces.  8.2e-3 of
 // the codes' norm are neighbours of the nearest code then, but the output is rounded to within 2.66e-2 of its norm either way.)
 // Bound by the matrix cores and what stands beside their 32 products of a wave's step (64 keys, heads of 128): a maximum, a multiply-add, an exponential,
 // an addition and half a conversion for each of a lane's 32 scores.  Two waves a SIMD take turns: 2 sequences of 4096 causal, 32 heads of 128, 285 us (960
@@ -31,7 +31,6 @@ template <typename T, int DP, bool DIRECT, bool FINE>
 __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(AttnParams p) {
     static_assert(!FINE || sizeof(T) == 2, "float32 has three pieces in any case");
     constexpr int KT = kStep<T>, KB = KT / 32, KC = DP / 16, DT = DP / 32;
-    constexpr bool PIECES = FINE || sizeof(T) == 4;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes<T, DP>];                 // buffers of keys and values
     __shared__ uint32_t firsts[DP];                      // of a tile whose values hold infinities or NaN: where
     if ((int)blockIdx.x >= p.units * p.slices) {
@@ -94,10 +93,11 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
             lk.load(lds[buf ^ 1][0], rk.n - k0 - KT);
             lv.load(lds[buf ^ 1][1], rk.n - k0 - KT);
         }
-        // Values that hold infinities or NaN, where some query sees this tile in part, or weights are pieces: the smaller ones may be zero or negative.
+        // Values that hold infinities or NaN, where some query sees this tile in part, or the weights' smaller pieces, zero or negative, would meet them
+        // (float32's values are pieces themselves, of which an infinity is the last, that meets the weight's first alone).
         bool broken = false;
-        if constexpr (EDGE || PIECES) {
-            broken = (PIECES || (p.causal && k0 + KT > least_all)) && tile_is_broken<T, DP>(tv);
+        if constexpr (EDGE || FINE) {
+            broken = (FINE || (p.causal && k0 + KT > least_all)) && tile_is_broken<T, DP>(tv);
             if (broken) {
                 find_broken<T, DP>(tv, firsts);
                 clean_tile<T, DP>(tv);
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256, DIRECT || DP <= 96 ? 2 : 1) void attn_kernel(A
                     for (int t = 0; t < DT; ++t) acc[t] = product(column_frag<T, DP>(tv, 32 * b + 16 * k, t, lane), w, acc[t]);
                 }
             }
-        if constexpr (EDGE || PIECES) {
+        if constexpr (EDGE || FINE) {
             if (broken) {
                 const uint32_t rows = min(max(lim - k0, 0), KT);
 #pragma unroll

@@ -31,15 +31,16 @@ template <typename T> struct Frag;
 template <> struct Frag<bf16_t> { i32x4_t w; };
 template <> struct Frag<float> { i32x4_t w[3]; };
 
-// Two numbers' pieces: the nearest bfloat16 number, that of what is left, and the rest.  Not FINITE: first pieces stay within bfloat16, so that an
-// infinity or a NaN is in the last, and numbers that would round up to infinity do not get one.
+// Two numbers' pieces: the nearest bfloat16 number, that of what is left, and the rest.  Not FINITE: an infinity or a NaN is the last piece, with zeros before
+// it, and first pieces stay within bfloat16, so that numbers that would round up to infinity do not get one.
 template <bool FINITE> __device__ __forceinline__ void split_two(float x, float y, int32_t (&w)[3]) {
     constexpr float TOP = 3.38953139e38f;                // bfloat16's largest number
-    auto near = [](float v) { return FINITE ? v : __builtin_amdgcn_fmed3f(v, -TOP, TOP); };
-    const bf16x2_v a = {(bf16_t)near(x), (bf16_t)near(y)};
+    const bool is[2] = {FINITE || fabsf(x) < __builtin_inff(), FINITE || fabsf(y) < __builtin_inff()};
+    auto near = [&](float v, int i) { return FINITE ? v : is[i] ? __builtin_amdgcn_fmed3f(v, -TOP, TOP) : 0.0f; };
+    const bf16x2_v a = {(bf16_t)near(x, 0), (bf16_t)near(y, 1)};
     x -= (float)a[0];
     y -= (float)a[1];
-    const bf16x2_v b = {(bf16_t)near(x), (bf16_t)near(y)};
+    const bf16x2_v b = {(bf16_t)near(x, 0), (bf16_t)near(y, 1)};
     const bf16x2_v c = {(bf16_t)(x - (float)b[0]), (bf16_t)(y - (float)b[1])};
     w[0] = __builtin_bit_cast(int32_t, a);
     w[1] = __builtin_bit_cast(int32_t, b);
@@ -334,7 +335,7 @@ __device__ __forceinline__ Frag<bf16_t> without_broken(Frag<bf16_t> f) {
     }
     return f;
 }
-__device__ __forceinline__ Frag<float> without_broken(Frag<float> f) {                // (the other pieces of such are numbers)
+__device__ __forceinline__ Frag<float> without_broken(Frag<float> f) {                // (the other pieces of such are zeros)
     f.w[2] = without_broken(Frag<bf16_t>{f.w[2]}).w;
     return f;
 }
@@ -343,20 +344,12 @@ __device__ __forceinline__ float wave_max(float v) {
     for (int x = 32; x; x /= 2) v = fmaxf(v, __shfl_xor(v, x));
     return v;
 }
-// The same of a tile in LDS (float32: of all pieces), by the whole workgroup: a barrier before, when all have read it, and after.
+// The same of a tile in LDS, by the whole workgroup: a barrier before, when all have read it, and after.
 template <typename T, int DP> __device__ __forceinline__ void clean_tile(uint8_t* tile) {
-    constexpr int PIECE = kTileBytes<T, DP> / kPieces<T>;
     __syncthreads();
     for (int i = threadIdx.x; i < kStep<T> * DP / 8; i += 256) {
-        const i32x4_t all = *(const i32x4_t*)(tile + (kPieces<T> - 1) * PIECE + i * 16);
-        i32x4_t keep;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x = (uint32_t)all[j];
-            keep[j] = (int32_t)~(((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u));
-        }
-#pragma unroll
-        for (int n = 0; n < kPieces<T>; ++n) *(i32x4_t*)(tile + n * PIECE + i * 16) &= keep;
+        i32x4_t* const at = (i32x4_t*)(tile + (kPieces<T> - 1) * (kTileBytes<T, DP> / kPieces<T>) + i * 16);
+        *at = without_broken(Frag<bf16_t>{*at}).w;
     }
     __syncthreads();
 }
