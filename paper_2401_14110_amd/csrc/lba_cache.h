@@ -45,15 +45,5 @@ __device__ __forceinline__ int64_t line_of(const CacheParams& p, int b, int64_t 
     return (page * p.KV + head) * p.page + p.page_mod(at);
 }
 
-// 2^(e - 127) of a scale byte; 0 reads as zero, 255 as NaN
-__device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7FC00000u : e << 23); }
-
-// the code in the low 4 bits of c as a number
-__device__ __forceinline__ float four_value(uint32_t c) {
-    const uint32_t m = c & 7;
-    const float a = m < 2 ? 0.5f * (float)m : __uint_as_float((m << 22) + (126u << 23));
-    return __uint_as_float(__float_as_uint(a) | ((c & 8) << 28));
-}
-
 }  // namespace lba
 #endif

@@ -36,13 +36,14 @@ __device__ __forceinline__ float sum_of_quarters(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A number in N bfloat16 pieces.  Not FINITE: pieces before the last stay within bfloat16, so that an infinity or a NaN is in the last, and numbers that
-// would round up to infinity do not get one.
+// A number in N bfloat16 pieces.  Not FINITE: an infinity or a NaN is the last, with zeros before it, and pieces before the last stay within bfloat16, so that
+// numbers that would round up to infinity do not get one.
 template <bool FINITE, int N> __device__ __forceinline__ void split(float x, bf16_t (&piece)[N]) {
     constexpr float TOP = 3.38953139e38f;                // bfloat16's largest number
+    const bool is = FINITE || fabsf(x) < __builtin_inff();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        piece[i] = (bf16_t)(FINITE || i == N - 1 ? x : __builtin_amdgcn_fmed3f(x, -TOP, TOP));
+        piece[i] = (bf16_t)(FINITE || i == N - 1 ? x : is ? __builtin_amdgcn_fmed3f(x, -TOP, TOP) : 0.0f);
         x -= (float)piece[i];
     }
 }
@@ -104,57 +105,40 @@ __device__ __forceinline__ void lds_words_done() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 }
-// One row by one wave, over the positions c0 .. c1 - 1 that it sees and nothing else: a lane a position, then a lane two columns.  words: 192 of LDS;
-// its sums, maximum (times c, as in the kernel) and sum of weights go to `sums` and ends[0][.][r].
-template <typename T, int D>
-__device__ __forceinline__ void chunk_row(const CacheAttnParams& p, int b, int kv, int row, int rows, int c0, int c1, float* words, float* sums, int r, float* ends,
-                                          int stride) {
+// A step's 32 rows of values in the wave's LDS, which hold infinities or NaN: of each column the first row with infinity, with its negative and with NaN, a
+// byte each (64: there is none), goes to firsts, since a query sees the first rows; then zeros stand for them.
+template <int D> __device__ __forceinline__ void clean_values(uint8_t* values, uint32_t* firsts) {
     const int lane = threadIdx.x & 63;
-    float top = -__builtin_inff(), sum = 0.0f, acc[2] = {0.0f, 0.0f};
-    if (row < rows) {
-        const int lim = min(c1, row_seen(p, b, row));
-        const T* x = (const T*)p.Q + ((int64_t)b * p.fresh + row / p.group) * p.q.row + (int64_t)(kv * p.group + row % p.group) * p.q.head;
-        lds_words_done();
-        for (int d = lane; d < D; d += 64) words[d] = load_one(x + d);
-        auto value = [&](const uint8_t* codes, const uint8_t* scales, int64_t line, int d) {
-            return four_value(codes[line * (D / 2) + d / 2] >> (d % 2 * 4)) * power_of(scales[line * (D / 32) + d / 32]);
-        };
-        for (int k0 = c0; k0 < lim; k0 += 64) {
-            lds_words_done();
-            const int64_t line = k0 + lane < lim ? line_of(p.c, b, k0 + lane, kv) : -1;
-            float s = -__builtin_inff();
-            if (line >= 0) {
-                s = 0.0f;
-                for (int d = 0; d < D; ++d) s = fmaf(words[d], value(p.c.k, p.c.k_scale, line, d), s);
-                s *= p.scale * 1.44269504f;
-            }
-            float now = s;
-#pragma unroll
-            for (int y = 32; y; y /= 2) now = fmaxf(now, __shfl_xor(now, y));
-            now = fmaxf(now, top);
-            const float base = now == -__builtin_inff() ? 0.0f : now;
-            const float e = line >= 0 ? __builtin_amdgcn_exp2f(s - base) : 0.0f, f = __builtin_amdgcn_exp2f(top - base);
-            top = now;
-            sum = sum * f + wave_sum(e);
-            words[128 + lane] = e;
-            lds_words_done();
-            acc[0] *= f;
-            acc[1] *= f;
-            for (int j = 0; j < 64 && k0 + j < lim; ++j) {
-                const int64_t at = line_of(p.c, b, k0 + j, kv);
-                if (at < 0) continue;
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    if (lane + 64 * y < D) acc[y] = fmaf(words[128 + j], value(p.c.v, p.c.v_scale, at, lane + 64 * y), acc[y]);
-            }
+    lds_words_done();
+#pragma clang loop unroll(disable)
+    for (int d = lane; d < D; d += 64) {
+        uint32_t plus = 64, minus = 64, none = 64;
+#pragma clang loop unroll(disable)
+        for (int r = 31; r >= 0; --r) {
+            const uint32_t e = *(const uint16_t*)(values + r * (D * 2) + ((d / 8) ^ value_turn<D>(r)) * 16 + d % 8 * 2);
+            if (e == 0x7F80u) plus = r;
+            if (e == 0xFF80u) minus = r;
+            if ((e & 0x7FFFu) > 0x7F80u) none = r;
         }
+        firsts[d] = plus | minus << 8 | none << 16;
     }
+    lds_words_done();
+#pragma clang loop unroll(disable)
+    for (int i = lane; i < 4 * D; i += 64) {
+        i32x4_c x = *(const i32x4_c*)(values + i * 16);
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        const int d = lane + 64 * y;
-        if (d < D) sums[((d / 4) ^ (r & 7)) * 4 + d % 4] = acc[y];
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t e = (uint32_t)x[j];
+            x[j] &= (int32_t)~(((e & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((e & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u));
+        }
+        *(i32x4_c*)(values + i * 16) = x;
     }
-    if (lane == 0) { ends[r] = top; ends[stride + r] = sum; }
+    lds_words_done();
+}
+// what a column gets from its infinities and NaN in the `seen` rows that are seen
+__device__ __forceinline__ float broken_sum(uint32_t firsts, uint32_t seen) {
+    const bool plus = (firsts & 255) < seen, minus = ((firsts >> 8) & 255) < seen, none = firsts >> 16 < seen;
+    return none || (plus && minus) ? __builtin_nanf("") : plus ? __builtin_inff() : minus ? -__builtin_inff() : 0.0f;
 }
 
 // NW: pieces of the weights.
@@ -164,7 +148,7 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
     constexpr int ROWB = D * 2, WAVE = (32 * ROWB > 16 * R * D * 4 ? 32 * ROWB : 16 * R * D * 4);    // values of a step; at the end a wave's sums
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][WAVE];
     __shared__ float ends[4][2][16 * R];
-    __shared__ float words[4][192];
+    __shared__ uint32_t firsts[4][D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = lane & 15, quarter = lane / 16;
     // Workgroups go to the eight dies in turn, so that neighbours are different heads and sequences, and all have as many: with a sequence's
     // chunks as neighbours the dies of the last ones idle where most sequences are short.
@@ -242,10 +226,9 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
     }
     fetch(k0);
     uint8_t* const mine = lds[wave];
-    bool again = false;
     for (; k0 < c1; k0 += 128) {
         const uint32_t held = (uint32_t)(__ballot(there[0]) & 0xFFFF) | (uint32_t)((__ballot(there[1]) & 0xFFFF) << 16);       // positions that hold something
-        const bool broken = p.fresh > 1 && __any(nv[0].broken() || nv[1].broken());
+        const bool broken = (p.fresh > 1 || NW > 1) && __any(nv[0].broken() || nv[1].broken());
         // values to this wave's rows, after the reads of the step before
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -329,7 +312,10 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[t][n][j] = __builtin_bit_cast(int32_t, bf16x2_c{piece[2 * j][n], piece[2 * j + 1][n]});
         }
-        again |= hidden && broken;                       // a zero weight has met an infinity, or may have
+        // infinities and NaN that some row does not see, or weights in pieces, the smaller of which are zero or negative
+        const bool clean = broken && (hidden || NW > 1);
+        if (clean) clean_values<D>(mine, firsts[wave]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             typedef __attribute__((address_space(3))) i16x4_c* lds_ptr;
@@ -344,18 +330,20 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
 #pragma unroll
                 for (int n = 0; n < NW; ++n) acc[t][d] = product16(x.v, w[t][n], acc[t][d]);
         }
+        if (clean) {
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                const uint32_t rows = min(max(lim[t] - k0, 0), 32);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[t][d][r] += broken_sum(firsts[wave][16 * d + 4 * quarter + r], rows);
+                    __builtin_amdgcn_sched_barrier(0);   // (one after another: this is rare, and its registers would be everybody's)
+                }
+            }
+        }
     }
 
-    if (p.fresh > 1 && __syncthreads_or(again)) {        // the chunk's rows once more, one by one over what each sees
-        for (int r = wave; r < 16 * R; r += 4) chunk_row<T, D>(p, b, kv, row0 + r, rows, c0, c1, &words[wave][0], (float*)lds[0] + r * D, r, &ends[0][0][0], 16 * R);
-        for (int i = threadIdx.x; i < 3 * 16 * R; i += 256) {
-            ends[1 + i / (16 * R)][0][i % (16 * R)] = -__builtin_inff();
-            ends[1 + i / (16 * R)][1][i % (16 * R)] = 0.0f;
-        }
-        for (int x = 1; x < 4; ++x)
-            for (int i = threadIdx.x; i < 16 * R * D; i += 256) ((float*)lds[x])[i] = 0.0f;
-        __syncthreads();
-    } else {
     // the four waves' maxima, then their sums in one scale
 #pragma unroll
     for (int t = 0; t < R; ++t) {
@@ -374,7 +362,6 @@ __global__ __launch_bounds__(256, R == 1 && NW == 1 ? (D == 64 ? 4 : 3) : 2) voi
         for (int d = 0; d < DT; ++d) *(f32x4_c*)&sums[(16 * t + col) * D + ((4 * d + quarter) ^ (col & 7)) * 4] = acc[t][d] * f;
     }
     __syncthreads();
-    }
     for (int i = threadIdx.x; i < 16 * R * (D / 4); i += 256) {
         const int r = i / (D / 4), piece = i % (D / 4), row = row0 + r;
         if (row >= rows) continue;
